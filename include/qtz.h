@@ -56,6 +56,7 @@ typedef int32_t qtz_status;
 
 typedef struct qtz_ctx* qtz_handle;     /* library-owned, opaque */
 typedef struct qtz_plan* qtz_conv_plan; /* library-owned: prepacked weights and tables */
+typedef struct qtz_linear* qtz_linear_plan; /* library-owned: prepacked 4-bit weights   */
 
 /* Scale, zero point and the nudged real range of one quantizer (Section 2.1). */
 typedef struct {
@@ -69,6 +70,9 @@ typedef enum {
     QTZ_U8 = 0, QTZ_S8 = 1, QTZ_S4_PACKED = 2, QTZ_S32 = 3, QTZ_U4_PACKED = 4,
     QTZ_U16 = 5, QTZ_S16 = 6   /* 16-bit codes (Section 7: 4, 8 and 16 bits), stored as uint16_t / int16_t */
 } qtz_dtype;
+
+/* Storage of real values in the serving calls (4-bit linear layers, 8-bit key/value cache). */
+typedef enum { QTZ_F32 = 16, QTZ_F16 = 17, QTZ_BF16 = 18 } qtz_ftype;
 
 typedef enum {
     QTZ_W_S8_PER_CHANNEL_SYM = 0,       /* int8 codes, one scale per output channel, z_w = 0 */
@@ -102,8 +106,9 @@ QTZ_API qtz_status qtz_destroy(qtz_handle h);
 QTZ_API const char* qtz_status_string(qtz_status s);
 /* Text of the last CUDA error seen through this handle ("" if none).  Host only.          */
 QTZ_API const char* qtz_last_error(qtz_handle h);
-/* Status word written by device code whose bounded waits gave up: 0, or
- * QTZ_ERR_DEVICE_TIMEOUT with *site_id telling which wait.  Synchronises `stream`.        */
+/* Status word written by device code: 0; QTZ_ERR_DEVICE_TIMEOUT from a bounded wait that gave up; or
+ * QTZ_ERR_INVALID_ARG from a serving call that met a slot or block id outside its cache (and skipped
+ * it: site id 10 append, 11 read, 12 attention).  *site_id tells which place.  Synchronises `stream`. */
 QTZ_API qtz_status qtz_last_device_status(qtz_handle h, int32_t* site_id, void* stream);
 
 /* Cycle budget of every bounded device-side wait of later launches through this handle (default
@@ -459,6 +464,101 @@ QTZ_API qtz_status qtz_maxpool_u8(qtz_handle h, const uint8_t* x_dev, uint8_t* y
 QTZ_API qtz_status qtz_global_avgpool_u8(qtz_handle h, const uint8_t* x_dev, int32_t x_zp, uint8_t* y_dev,
                                  int32_t y_zp, int32_t mult, int32_t rshift, int32_t batch,
                                  int32_t hw, int32_t c, int32_t c_pitch, void* stream);
+
+/* ---- serving: linear layers with 4-bit weights --------------------------------------------- */
+
+/* y[r][o] = sum_k x[r][k] W[o][k] + bias[o],   W[o][k] = (q[o][k] - z[o][k / group]) * scale[o][k / group]
+ * The affine quantizer of Section 2.1 (U4 codes with zero points) or the symmetric one of Section 2.2 (S4
+ * codes, z = 0) at a finer granularity than Section 2.6's channels: `group` neighbouring columns of a row share
+ * one scale.  Activations stay real.  Products are exact, sums are held in fp32, y is rounded once.
+ *   codes   [n][(k + 1) / 2] two 4-bit codes per byte, element 2i of a row in the low nibble (what
+ *           qtz_quantize_tensor writes for QTZ_S4_PACKED / QTZ_U4_PACKED when `inner` is a row or, with k a
+ *           multiple of `group`, a group)
+ *   scales  [n][ceil(k / group)] in the layer's type;  zeros: the same shape, one byte each, 0..15 (larger ones
+ *           count as 15); NULL with QTZ_S4_PACKED, NULL means 0 with QTZ_U4_PACKED;  bias: n values or NULL
+ *   group   32 or a multiple of 64; the last group of a row may be short                                     */
+typedef struct {
+    int32_t n, k, group;
+    int32_t wdtype; /* QTZ_S4_PACKED or QTZ_U4_PACKED                         */
+    int32_t ftype;  /* QTZ_F16 or QTZ_BF16: type of x, y, scales and bias     */
+} qtz_linear_desc;
+/* One-time preparation: copies codes, scales, zero points and bias into the order the kernel reads.  The caller
+ * may free or overwrite all inputs once `stream` has passed this call.                                          */
+QTZ_API qtz_status qtz_linear_create(qtz_handle h, const qtz_linear_desc* desc, const void* codes_dev, const void* scales_dev,
+                                     const uint8_t* zeros_dev, const void* bias_dev, qtz_linear_plan* out, void* stream);
+QTZ_API qtz_status qtz_linear_destroy(qtz_linear_plan p);
+/* x: `rows` rows of k values, x_stride elements apart; base and x_stride * 2 bytes multiples of 16, x_stride >= k.
+ * Values past k in a row are never used.  y: rows of n values, y_stride >= n elements apart, no alignment rule.
+ * rows == 0 does nothing.  Asynchronous on `stream`.                                                            */
+QTZ_API qtz_status qtz_linear_w4(qtz_linear_plan p, const void* x_dev, int64_t x_stride, int64_t rows, void* y_dev,
+                                 int64_t y_stride, void* stream);
+
+/* ---- serving: key/value cache in 8 bits ------------------------------------------------------ */
+
+/* A pool of blocks of block_tokens tokens.  Codes are symmetric int8 in [-127, 127] (Section 2.2, Eq. 10), one scale
+ * per block and key/value head: the real value is code * scale.  Position p of a request lies in block
+ * table[request][p / block_tokens] at offset p % block_tokens; its slot is block * block_tokens + offset.
+ *   k, v          [blocks][kv_heads][block_tokens][head_dim], 16-byte aligned
+ *   k_scale, v_scale [blocks][kv_heads]; scales are at least 2^-100 (an all-zero block; smaller ones count as 2^-100)
+ *   head_dim      64, 128 or 256;  block_tokens a multiple of 16, at most 256                                  */
+typedef struct {
+    int8_t* k_dev;
+    int8_t* v_dev;
+    float* k_scale_dev;
+    float* v_scale_dev;
+    int32_t blocks, kv_heads, block_tokens, head_dim;
+} qtz_kv_cache;
+
+/* Admits one step: requests[r] has cached[r] tokens in the cache and brings added[r] new ones (0 allowed).  Takes the
+ * blocks they need from the end of the free list, request after request, and writes on the device
+ *   table   [requests][table_width]: only the entries of newly taken blocks
+ *   starts  [requests + 1]: row of each request's first new token; starts[requests] is their number
+ *   lens    [requests]: cached + added
+ *   slots   [capacity]: slot of every new token, -1 from starts[requests] on
+ *   report  4 values: blocks left in the free list, new tokens, blocks taken, refused
+ * free list: free_dev[0 .. *free_count_dev - 1]; neither is written, the next step's count is report[0].
+ * All or nothing: with too few free blocks, a request beyond table_width, more than `capacity` new tokens or a negative
+ * length, report[3] = 1, no block is taken, the table is untouched, starts are 0, lens = cached and slots -1.
+ * At most 8192 requests (QTZ_ERR_TOO_LARGE).  Asynchronous; nothing is copied to the host.                          */
+QTZ_API qtz_status qtz_kv_schedule(qtz_handle h, const int32_t* cached_dev, const int32_t* added_dev, int32_t requests,
+                                   int32_t block_tokens, int32_t* table_dev, int32_t table_width, const int32_t* free_dev,
+                                   const int32_t* free_count_dev, int32_t* starts_dev, int32_t* lens_dev, int64_t* slots_dev,
+                                   int64_t capacity, int32_t* report_dev, void* stream);
+/* Quantizes `tokens` new keys and values (rows of head_dim values in `ftype`: QTZ_F16 or QTZ_BF16; strides in elements)
+ * into the slots given; a negative slot is skipped.  Tokens of one block are neighbours in the list, in ascending slots, and
+ * no block appears in two places.  Per block, head and tensor, over the block's new tokens (Section 2.2):
+ *   s = max(max|x| / 127, 2^-100); if the first new token is not at offset 0, s = max(s, old scale) and the codes
+ *   before it become round(code * (old scale / s)); new codes are clamp(round(x / s), -127, 127)
+ * with IEEE fp32 steps and round-half-to-even.  Infinities saturate and do not count in the maximum, NaN takes the lowest
+ * code.  Base pointers 16-byte aligned, strides multiples of 8 elements.  Asynchronous on `stream`.                      */
+QTZ_API qtz_status qtz_kv_append(qtz_handle h, const qtz_kv_cache* cache, const void* k_dev, int64_t k_token_stride,
+                                 int64_t k_head_stride, const void* v_dev, int64_t v_token_stride, int64_t v_head_stride,
+                                 int32_t ftype, const int64_t* slots_dev, int64_t tokens, void* stream);
+/* The reverse: code * scale of the slots given, rounded once to `ftype` (any), as dense [tokens][kv_heads][head_dim];
+ * zeros for a negative slot.  Outputs 16-byte aligned.                                                               */
+QTZ_API qtz_status qtz_kv_read(qtz_handle h, const qtz_kv_cache* cache, const int64_t* slots_dev, int64_t tokens, int32_t ftype,
+                               void* k_out_dev, void* v_out_dev, void* stream);
+
+/* Softmax attention of each request's newest tokens over its cached ones, its own included:
+ *   y[t][h] = sum_p softmax_p(scale * q[t][h] . K[p][g]) V[p][g],     g = h / (q_heads / kv_heads)
+ * Row t of request r (starts[r] <= t < starts[r + 1]) is its token number lens[r] - (starts[r + 1] - starts[r]) + t - starts[r]
+ * and sees that token and the ones before it, with window > 0 only the last `window` of those.  A row that sees nothing
+ * gives zeros and lse = -inf.
+ *   q, y    [tokens][q_heads][head_dim] in `ftype` (QTZ_F16 or QTZ_BF16), strides in elements, bases 16-byte aligned,
+ *           strides multiples of 8.  Rows from starts[requests] on are neither read nor written.
+ *   lse     NULL, or [tokens][q_heads] fp32: natural logarithm of the softmax's sum, for joining with other keys
+ *   tokens  rows of q and y
+ *   workspace  qtz_kv_attention_workspace_bytes(h, cache) bytes, 16-byte aligned, zero-filled once before its first use;
+ *           one stream at a time.  Its size does not depend on lengths.
+ * Keys and queries multiply exactly in fp16 (each row of q scaled by a power of two to its range), probabilities are
+ * rounded to fp16 before they meet the values; every sum, maximum and statistic is fp32.
+ * q_heads a multiple of kv_heads; at most 8192 requests.  Asynchronous; same results whenever repeated.               */
+QTZ_API int64_t qtz_kv_attention_workspace_bytes(qtz_handle h, const qtz_kv_cache* cache);
+QTZ_API qtz_status qtz_kv_attention(qtz_handle h, const qtz_kv_cache* cache, const void* q_dev, int64_t q_token_stride,
+                                    int64_t q_head_stride, int32_t q_heads, int32_t ftype, const int32_t* starts_dev,
+                                    const int32_t* lens_dev, int32_t requests, int64_t tokens, const int32_t* table_dev,
+                                    int32_t table_width, float scale, int32_t window, void* y_dev, int64_t y_token_stride,
+                                    int64_t y_head_stride, float* lse_dev, void* workspace_dev, void* stream);
 
 #ifdef __cplusplus
 }

@@ -83,7 +83,7 @@ extern "C" qtz_status qtz_last_device_status(qtz_handle h, int32_t* site_id, voi
     if (site_id) *site_id = host[1];
     if (host[0] != 0) {
         QTZ_CUDA(h, cudaMemsetAsync(h->status_dev, 0, sizeof(host), st));
-        return QTZ_ERR_DEVICE_TIMEOUT;
+        return host[0];
     }
     return QTZ_OK;
 }

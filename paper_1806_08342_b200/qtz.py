@@ -21,6 +21,8 @@ U8, S8, S4_PACKED, S32, U4_PACKED, U16, S16 = 0, 1, 2, 3, 4, 5, 6
 W_S8_PER_CHANNEL_SYM, W_U8_PER_LAYER_ASYM, W_S4_PACKED_PER_CHANNEL_SYM = 0, 1, 2
 OUT_U8, OUT_S32_RAW = 0, 1
 ACT_NONE, ACT_RELU, ACT_RELU6 = 0, 1, 2
+F32, F16, BF16 = 16, 17, 18
+FTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
 
 QPARAMS = np.dtype([("scale", "<f4"), ("zero_point", "<i4"), ("min_nudged", "<f4"), ("max_nudged", "<f4")])
 
@@ -32,6 +34,15 @@ class ConvDesc(Structure):
 
 class Residual(Structure):
     _fields_ = [(n, c_int32) for n in ("t_zero_point", "t_act_min", "t_act_max", "t_mult", "s_zero_point", "s_mult", "rshift")]
+
+
+class LinearDesc(Structure):
+    _fields_ = [(n, c_int32) for n in ("n", "k", "group", "wdtype", "ftype")]
+
+
+class KvCacheDesc(Structure):
+    _fields_ = [(n, c_void_p) for n in ("k_dev", "v_dev", "k_scale_dev", "v_scale_dev")] + \
+               [(n, c_int32) for n in ("blocks", "kv_heads", "block_tokens", "head_dim")]
 
 
 class QtzError(RuntimeError):
@@ -102,6 +113,17 @@ SIGNATURES = {
                                  c_int32, c_int32, c_int32, c_void_p]),
     "qtz_maxpool_u8": (c_int32, [c_void_p, c_void_p, c_void_p] + [c_int32] * 8 + [c_void_p]),
     "qtz_global_avgpool_u8": (c_int32, [c_void_p, c_void_p, c_int32, c_void_p] + [c_int32] * 7 + [c_void_p]),
+    "qtz_linear_create": (c_int32, [c_void_p, POINTER(LinearDesc), c_void_p, c_void_p, c_void_p, c_void_p, POINTER(c_void_p), c_void_p]),
+    "qtz_linear_destroy": (c_int32, [c_void_p]),
+    "qtz_linear_w4": (c_int32, [c_void_p, c_void_p, c_int64, c_int64, c_void_p, c_int64, c_void_p]),
+    "qtz_kv_schedule": (c_int32, [c_void_p, c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_int32, c_void_p, c_void_p, c_void_p,
+                                  c_void_p, c_void_p, c_int64, c_void_p, c_void_p]),
+    "qtz_kv_append": (c_int32, [c_void_p, POINTER(KvCacheDesc), c_void_p, c_int64, c_int64, c_void_p, c_int64, c_int64, c_int32, c_void_p,
+                                c_int64, c_void_p]),
+    "qtz_kv_read": (c_int32, [c_void_p, POINTER(KvCacheDesc), c_void_p, c_int64, c_int32, c_void_p, c_void_p, c_void_p]),
+    "qtz_kv_attention_workspace_bytes": (c_int64, [c_void_p, POINTER(KvCacheDesc)]),
+    "qtz_kv_attention": (c_int32, [c_void_p, POINTER(KvCacheDesc), c_void_p, c_int64, c_int64, c_int32, c_int32, c_void_p, c_void_p, c_int32,
+                                   c_int64, c_void_p, c_int32, c_float, c_int32, c_void_p, c_int64, c_int64, c_void_p, c_void_p, c_void_p]),
 }
 
 
@@ -144,6 +166,23 @@ def _check_dev(*ts):
     for t in ts:
         if t is not None and (not t.is_cuda or not t.is_contiguous()):
             raise ValueError("expected contiguous CUDA tensors")
+
+
+def _check_on(device, dtype, *ts):
+    for t in ts:
+        if t.dtype != dtype or t.device.type != "cuda" or t.device.index != device:
+            raise ValueError(f"expected {dtype} tensors on cuda:{device}, got {t.dtype} on {t.device}")
+
+
+def _check_flat(device, dtype, *ts):
+    _check_on(device, dtype, *ts)
+    for t in ts:
+        if not t.is_contiguous():
+            raise ValueError("expected contiguous tensors")
+
+
+def _raw_stream(device):
+    return torch._C._cuda_getCurrentRawStream(device)
 
 
 # ---- host-only helpers ------------------------------------------------------------------
@@ -474,6 +513,67 @@ class Handle:
                                            _np(m), _np(r), byref(plan), _stream()), "qtz_conv_create")
         return ConvPlan(self, plan, desc, depthwise)
 
+    # ---- serving: 4-bit linear layers and the 8-bit key/value cache ----
+    def quantize_groups(self, w, group, dtype=torch.bfloat16, symmetric=True):
+        """4-bit codes of w [n][k] (fp32) with one scale per row and `group` columns: (codes, scales, zeros) as
+        linear_create takes them; zeros is None for the symmetric quantizer.  Each scale is rounded to `dtype` before
+        the codes are taken with it, so that the codes belong to the scale that the layer multiplies by."""
+        _check_dev(w)
+        n, k = w.shape
+        groups = -(-k // group)
+        if groups * group != k:                       # a short last group: the zeros that fill it change no range
+            w = torch.nn.functional.pad(w, (0, groups * group - k))
+        w = w.reshape(n * groups, group)
+        params = self.calibrate_minmax(w, axis=0, bits=4, symmetric=symmetric)
+        scales = torch.from_numpy(params["scale"].copy()).to(dtype).clamp(min=torch.finfo(dtype).tiny)
+        params["scale"] = scales.float().numpy()
+        codes = self.quantize_tensor(w, params, axis=0, out_dtype=S4_PACKED if symmetric else U4_PACKED)
+        codes = codes.reshape(n, groups * group // 2)[:, :(k + 1) // 2].contiguous()
+        zeros = None if symmetric else torch.from_numpy(params["zero_point"].astype(np.uint8)).reshape(n, groups).to(w.device)
+        return codes, scales.reshape(n, groups).to(w.device), zeros
+
+    def linear_create(self, codes, scales, k, group, zeros=None, bias=None, signed=None):
+        """Plan of y = x W^T + bias with packed 4-bit codes [n][(k + 1) // 2], scales [n][ceil(k / group)] and, for unsigned
+        codes, zero points of the same shape.  `signed` defaults to whether there are no zero points."""
+        n = codes.shape[0]
+        if k <= 0 or group <= 0:
+            raise ValueError("k and group are positive")
+        _check_flat(self.device, torch.uint8, codes, *(() if zeros is None else (zeros,)))
+        if scales.dtype not in (torch.float16, torch.bfloat16):
+            raise ValueError("scales are float16 or bfloat16: the type of the layer")
+        _check_flat(self.device, scales.dtype, scales, *(() if bias is None else (bias,)))
+        shape = (n, -(-int(k) // int(group)))
+        if codes.shape != (n, (k + 1) // 2) or scales.shape != shape or (zeros is not None and zeros.shape != shape) or \
+                (bias is not None and bias.shape != (n,)):
+            raise ValueError("shapes of codes, scales, zeros and bias do not belong together")
+        signed = zeros is None if signed is None else signed
+        desc = LinearDesc(n, int(k), int(group), S4_PACKED if signed else U4_PACKED, FTYPES[scales.dtype])
+        plan = c_void_p()
+        self._chk(self.lib.qtz_linear_create(self.h, byref(desc), _ptr(codes), _ptr(scales), _ptr(zeros), _ptr(bias), byref(plan),
+                                             _raw_stream(self.device)), "qtz_linear_create")
+        return LinearPlan(self, plan, desc, scales.dtype)
+
+    def kv_schedule(self, cached, added, table, free, free_count, block_tokens, capacity):
+        """qtz_kv_schedule: writes the new blocks into `table` and returns (starts, lens, slots, report)."""
+        _check_flat(self.device, torch.int32, cached, added, table, free, free_count)
+        b = cached.shape[0]
+        if added.shape != (b,) or table.dim() != 2 or table.shape[0] != b:
+            raise ValueError("cached, added and table describe different numbers of requests")
+        out = torch.empty(2 * b + 1 + 4, dtype=torch.int32, device=cached.device)
+        slots = torch.empty(capacity, dtype=torch.int64, device=cached.device)
+        starts, lens, report = out[4:b + 5], out[b + 5:], out[:4]
+        self._chk(self.lib.qtz_kv_schedule(self.h, cached.data_ptr(), added.data_ptr(), b, block_tokens, table.data_ptr(), table.shape[1],
+                                           free.data_ptr(), free_count.data_ptr(), starts.data_ptr(), lens.data_ptr(), slots.data_ptr(),
+                                           capacity, report.data_ptr(), _raw_stream(self.device)), "qtz_kv_schedule")
+        return starts, lens, slots, report
+
+    def kv_cache(self, blocks, kv_heads, block_tokens, head_dim):
+        """A cache whose memory torch owns, every block all zero."""
+        device = f"cuda:{self.device}"
+        k, v = (torch.zeros(blocks, kv_heads, block_tokens, head_dim, dtype=torch.int8, device=device) for _ in range(2))
+        ks, vs = (torch.full((blocks, kv_heads), 2.0 ** -100, device=device) for _ in range(2))
+        return KvCache(self, k, v, ks, vs)
+
     def add_u8(self, a, a_zp, a_mult, b, b_zp, b_mult, rshift, y_zp, act_min, act_max, c, out=None):
         _check_dev(a, b, out)
         pitch = a.shape[-1]
@@ -569,6 +669,120 @@ class ConvPlan:
             self.close()
         except Exception:
             pass
+
+
+class LinearPlan:
+    """Owns a qtz_linear_plan: y = x W^T + bias with 4-bit weights."""
+
+    def __init__(self, handle: Handle, plan, desc: LinearDesc, dtype):
+        self.handle, self.plan, self.desc, self.dtype = handle, plan, desc, dtype
+        self._run = handle.lib.qtz_linear_w4
+
+    def __call__(self, x, out=None):
+        """x [rows][k] (or more leading axes that fold into rows); rows may lie apart by a multiple of 16 bytes."""
+        n, k = self.desc.n, self.desc.k
+        if x.shape[-1] != k or x.stride(-1) != 1:
+            raise ValueError(f"expected rows of {k} neighbouring values, got {tuple(x.shape)} with strides {x.stride()}")
+        _check_on(self.handle.device, self.dtype, x)
+        lead = x.shape[:-1]
+        if x.dim() != 2:
+            x = x.view(-1, k)
+        if out is None:
+            out = torch.empty(lead + (n,), dtype=self.dtype, device=x.device)
+        else:
+            _check_on(self.handle.device, self.dtype, out)
+            if out.shape != lead + (n,) or out.stride(-1) != 1:
+                raise ValueError("out has another shape")
+        y = out if out.dim() == 2 else out.view(-1, n)
+        rows = x.shape[0]
+        # a single row has no stride to keep: torch reports any value for it
+        xs = (k + 7) // 8 * 8 if rows == 1 else x.stride(0)
+        rc = self._run(self.plan, x.data_ptr(), xs, rows, y.data_ptr(), n if rows == 1 else y.stride(0),
+                       _raw_stream(self.handle.device))
+        if rc:
+            self.handle._chk(rc, "qtz_linear_w4")
+        return out
+
+    def close(self):
+        if self.plan:
+            self.handle.lib.qtz_linear_destroy(self.plan)
+            self.plan = c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class KvCache:
+    """A paged 8-bit key/value cache in torch tensors: codes [blocks][kv_heads][block_tokens][head_dim] int8, scales
+    [blocks][kv_heads] fp32.  attention() keeps its workspace here: one stream at a time."""
+
+    def __init__(self, handle: Handle, k, v, k_scale, v_scale):
+        _check_flat(handle.device, torch.int8, k, v)
+        _check_flat(handle.device, torch.float32, k_scale, v_scale)
+        if k.dim() != 4 or v.shape != k.shape or k_scale.shape != k.shape[:2] or v_scale.shape != k.shape[:2]:
+            raise ValueError("shapes of codes and scales do not belong together")
+        self.handle, self.k, self.v, self.k_scale, self.v_scale = handle, k, v, k_scale, v_scale
+        self.blocks, self.kv_heads, self.block_tokens, self.head_dim = k.shape
+        self._desc = KvCacheDesc(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), *k.shape)
+        self._ref = byref(self._desc)
+        self.workspace = None
+
+    def append(self, k, v, slots):
+        """Quantizes new keys and values [tokens][kv_heads][head_dim] (any token and head stride) into `slots`."""
+        dev = self.handle.device
+        _check_on(dev, k.dtype, k, v)
+        _check_flat(dev, torch.int64, slots)
+        shape = (slots.shape[0], self.kv_heads, self.head_dim)
+        if k.shape != shape or v.shape != shape or k.stride(2) != 1 or v.stride(2) != 1 or k.dtype not in FTYPES:
+            raise ValueError(f"expected keys and values of shape {shape}")
+        rc = self.handle.lib.qtz_kv_append(self.handle.h, self._ref, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0),
+                                           v.stride(1), FTYPES[k.dtype], slots.data_ptr(), shape[0], _raw_stream(dev))
+        if rc:
+            self.handle._chk(rc, "qtz_kv_append")
+
+    def read(self, slots, dtype=torch.float32):
+        """Real values of the slots: keys and values [tokens][kv_heads][head_dim]."""
+        dev = self.handle.device
+        _check_flat(dev, torch.int64, slots)
+        k, v = torch.empty((2, slots.shape[0], self.kv_heads, self.head_dim), dtype=dtype, device=slots.device).unbind(0)
+        rc = self.handle.lib.qtz_kv_read(self.handle.h, self._ref, slots.data_ptr(), slots.shape[0], FTYPES.get(dtype, -1), k.data_ptr(),
+                                         v.data_ptr(), _raw_stream(dev))
+        if rc:
+            self.handle._chk(rc, "qtz_kv_read")
+        return k, v
+
+    def attention(self, q, starts, lens, table, scale=None, window=0, out=None, return_lse=False):
+        """q [tokens][q_heads][head_dim] of the requests' newest tokens (rows starts[r] .. starts[r + 1]); returns y, or (y, lse)."""
+        dev = self.handle.device
+        dtype = q.dtype
+        _check_on(dev, dtype, q)
+        _check_flat(dev, torch.int32, starts, lens, table)
+        b = lens.shape[0]
+        if q.dim() != 3 or q.shape[2] != self.head_dim or q.stride(2) != 1 or dtype not in FTYPES:
+            raise ValueError(f"expected queries [tokens][heads][{self.head_dim}]")
+        if starts.shape != (b + 1,) or table.dim() != 2 or table.shape[0] != b:
+            raise ValueError("starts, lens and table describe different numbers of requests")
+        if out is None:
+            out = torch.empty(q.shape, dtype=dtype, device=q.device)
+        else:
+            _check_on(dev, dtype, out)
+            if out.shape != q.shape or out.stride(2) != 1:
+                raise ValueError("out has another shape")
+        lib, h = self.handle.lib, self.handle.h
+        if self.workspace is None:
+            size = lib.qtz_kv_attention_workspace_bytes(h, self._ref)
+            self.workspace = torch.zeros(max(size, 16), dtype=torch.uint8, device=q.device)
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if return_lse else None
+        rc = lib.qtz_kv_attention(h, self._ref, q.data_ptr(), q.stride(0), q.stride(1), q.shape[1], FTYPES[dtype], starts.data_ptr(),
+                                  lens.data_ptr(), b, q.shape[0], table.data_ptr(), table.shape[1],
+                                  self.head_dim ** -0.5 if scale is None else scale, window, out.data_ptr(), out.stride(0), out.stride(1),
+                                  None if lse is None else lse.data_ptr(), self.workspace.data_ptr(), _raw_stream(dev))
+        if rc:
+            self.handle._chk(rc, "qtz_kv_attention")
+        return (out, lse) if return_lse else out
 
 
 def conv_desc(batch, h, w, c, n, kh, kw, stride, pad, wkind=W_S8_PER_CHANNEL_SYM, outkind=OUT_U8,
