@@ -550,8 +550,9 @@ QTZ_API qtz_status qtz_kv_read(qtz_handle h, const qtz_kv_cache* cache, const in
  *   tokens  rows of q and y
  *   workspace  qtz_kv_attention_workspace_bytes(h, cache) bytes, 16-byte aligned, zero-filled once before its first use;
  *           one stream at a time.  Its size does not depend on lengths.
- * Keys and queries multiply exactly in fp16 (each row of q scaled by a power of two to its range), probabilities are
- * rounded to fp16 before they meet the values; every sum, maximum and statistic is fp32.
+ * Codes meet fixed-point queries and weights in exact integer sums: a query keeps 22 bits below its row's largest value, a
+ * softmax weight 22 bits below the largest weight so far; every other sum, maximum and statistic is fp32.  A query row that
+ * holds NaN or an infinity gives NaN.
  * q_heads a multiple of kv_heads; at most 8192 requests.  Asynchronous; same results whenever repeated.               */
 QTZ_API int64_t qtz_kv_attention_workspace_bytes(qtz_handle h, const qtz_kv_cache* cache);
 QTZ_API qtz_status qtz_kv_attention(qtz_handle h, const qtz_kv_cache* cache, const void* q_dev, int64_t q_token_stride,

@@ -1,20 +1,30 @@
-// Attention of new tokens over the paged 8-bit key/value cache.
+// Attention of new tokens over the paged 8-bit key/value cache, on the integer tensor cores.
 //
 // Mathematics.  For one query row q and one block with key scale s_k and value scale s_v the kernel holds, per token p,
 //   t_p = (q . k_p) c log2(e) s_k + log2(s_v),      w_p = 2^(t_p - m),     m = running maximum of t
 // so that w_p = s_v exp(logit_p) 2^-m carries the block's value scale: the sum over values is sum w_p v_p on the codes
-// themselves, and the softmax's denominator is sum w_p / s_v.  Codes become fp16 exactly (a byte placed in the mantissa of
-// 1024 + u, minus the offset), queries keep all their bits in fp16 after each row is scaled by a power of two, so logits are
-// exact products summed in fp32; w_p, at most 1, is the only value rounded to 16 bits (fp16: 2^-11, finer than a bf16 output).
+// themselves, and the softmax's denominator is sum w_p / s_v.
+// Both products have 8-bit codes on one side, which the tensor cores (kind::i8) read straight from the bytes that TMA
+// brings in: nothing is converted.  The other side is split into base-256 digits, one operand column each:
+//   q_row = 2^(e - 21) (d_2 2^16 + d_1 2^8 + d_0)   e = exponent of the row's largest value, d in [-128, 127]: 22 bits
+//   w_p   = 2^-22 (b_2 2^16 + b_1 2^8 + b_0)        b in [0, 255]; the mantissa of w_p + 2
+// Integer sums are exact; a query loses what lies below 2^-22 of its row's largest value and a weight what lies below
+// 2^-23 of the largest weight, both far less than the output's type.  The sums are joined in fp32.
+//
+// One tile is 128 tokens of one key/value head against kRows query rows (heads of the group x new tokens):
+//   S^T [128 tokens x 3 kRows] = K [128 x D] Q^T        a thread owns a token: logits, maximum, weights
+//   O^T [D x 3 kRows]          = V^T [D x 128] W        a thread owns a column of the head: fp32 running sum
+// with V read as it lies (the depth of the product along its rows).
 //
 // What bounds it: one token reads 2 D bytes a head for 4 D flops a query head: HBM, by a factor of 4 to 100 over the tensor
-// cores.  So every byte is read once, and the work is cut for an even stream: the 16-token tiles of all (request, key/value
-// head, 16 query rows) items form one sequence that is dealt out in equal contiguous shares to the warps of a grid of one
-// CTA per SM, whatever the lengths.  Each warp streams its share through a private ring in shared memory (TMA boxes of 16
-// rows, issued by lane 0, several tiles ahead of use, across items).  An item that one warp finishes is written from
-// registers; shares that meet in an item are joined in the CTA, and across CTAs by the last one to arrive, always in the
-// order of the tiles, so that results do not depend on timing.
+// cores.  So every byte is read once, and the work is cut for an even stream: the tiles of all (request, key/value head, row
+// tile) items form one sequence that is dealt out in equal contiguous shares to a grid that fills the GPU once, whatever the
+// lengths.  A producer warp streams a CTA's share through a ring of TMA boxes, several tiles ahead and across items.  Items
+// that lie in more than one share are joined by the last CTA to arrive, in the order of the tiles, so that results do not
+// depend on timing.
 #include <cuda.h>
+
+#include <type_traits>
 
 #include "qtz_half_util.cuh"
 #include "qtz_kv.cuh"
@@ -26,23 +36,14 @@ namespace {
 using namespace qtz_ptx;
 
 constexpr int kMaxRequests = 8192;
-constexpr int kWarps = 8;
-constexpr int kThreads = kWarps * 32;
-constexpr int kTile = 16;          // tokens of a tile: the depth of one matrix instruction
-constexpr int kMaxStages = 8;
-constexpr int kBatch = 32;         // tiles whose addresses and scales a warp looks up together
-constexpr int kMinShare = 8;       // tiles: shorter shares cost more in joining than they save in streaming
-constexpr int kSmemLimit = 227 * 1024;
-
-struct TileInfo {                  // what a warp needs to know about one tile
-    int32_t row;                   // first row of the tile in the [blocks * heads * block_tokens] view
-    float k_scale, v_scale;
-    int32_t pos;                   // position of its first token
-    int32_t request, item;         // item: index within the request (head, row tile)
-    int32_t flags;
-    int32_t pad;
-};
-enum { kValid = 1, kFirst = 2, kLast = 4 };
+constexpr int kTile = 128;                 // tokens of a tile: the rows of one matrix instruction
+constexpr int kComputeWarps = 4;
+constexpr int kComputeThreads = 32 * kComputeWarps;
+constexpr int kThreads = kComputeThreads + 64;   // + one warp for TMA, one for the matrix instructions
+constexpr int kMaxRows = 16;
+constexpr int kMaxStages = 6;
+constexpr int kTmemColumns = 256;          // S (two buffers), O (two halves of a head of 256), 64 columns each
+constexpr int kSmemLimit = 227 * 1024;     // of an SM, each CTA costing 1 KB more than it asks for
 
 struct AttnArgs {
     qtz_kv_cache c;
@@ -53,39 +54,74 @@ struct AttnArgs {
     int32_t requests, tokens;
     const int32_t* table;
     int32_t width;
-    float scale_log2;              // softmax scale * log2(e)
+    float scale_log2;                      // softmax scale * log2(e)
     int32_t window;
     void* y;
     int64_t y_token_stride, y_head_stride;
     float* lse;
-    int32_t* counters;             // [CTAs] arrivals at the item that begins in a CTA and ends in a later one
-    float* warp_parts;             // [CTAs][warps][16 * D]
-    float* cta_parts;              // [CTAs][2][16 * D + 32]
-    int32_t stages;
+    int32_t* counters;                     // [CTAs] arrivals at the item that begins in a CTA and ends in a later one
+    float* parts;                          // [CTAs][2][kMaxRows * D + 2 kMaxRows]: sums, maxima, denominators
+    int32_t stages, box_rows;
     int64_t wait_budget;
     int32_t* status;
 };
 
 struct RequestShape {
-    int first, added;              // rows of q
-    int len, limit;                // tokens; those that the table can hold
-    int row_tiles, lo, hi, tiles;  // items per head; tiles [lo, hi) of the cache; tiles per item (at least one)
+    int first, added;                      // rows of q
+    int len, limit;                        // tokens; those that the table can hold
+    int row_tiles, lo, hi, tiles;          // items per head; tiles [lo, hi) of the cache; tiles per item (at least one)
 };
 
+template <int kRows>
 __device__ __forceinline__ RequestShape shape_of(const AttnArgs& a, int r)
 {
     RequestShape s;
     s.first = min(max(a.starts[r], 0), a.tokens);
     s.added = min(max(a.starts[r + 1], s.first), a.tokens) - s.first;
-    s.len = min(max(a.lens[r], 0), 0x7ffffff0);
+    s.len = min(max(a.lens[r], 0), 0x7fffff00);
     s.limit = static_cast<int>(min(static_cast<int64_t>(s.len), static_cast<int64_t>(a.width) * a.c.block_tokens));
-    s.row_tiles = static_cast<int>((static_cast<int64_t>(s.added) * a.group + 15) / 16);
-    const int64_t begin = static_cast<int64_t>(s.len) - s.added + 1 - a.window;
-    s.lo = a.window > 0 && begin > 0 ? static_cast<int>(begin / kTile) : 0;
+    s.row_tiles = static_cast<int>((static_cast<int64_t>(s.added) * a.group + kRows - 1) / kRows);
+    const int begin = s.len - s.added + 1 - a.window;
+    s.lo = a.window > 0 && begin > 0 ? begin / kTile : 0;
     s.hi = (s.limit + kTile - 1) / kTile;
     s.tiles = max(1, s.hi - s.lo);
     return s;
 }
+
+// A place in the sequence of tiles.
+template <int kRows>
+struct Cursor {
+    RequestShape s;
+    int request, item, k;                  // item: (head, row tile) within the request; k: tile within the item
+    uint32_t begin;                        // index of the item's first tile
+
+    __device__ __forceinline__ void seek(const AttnArgs& a, const uint32_t* prefix, uint32_t tile)
+    {
+        int u = 0, v = a.requests;
+        while (v - u > 1) {
+            const int mid = (u + v) >> 1;
+            if (prefix[mid] <= tile) u = mid; else v = mid;
+        }
+        request = u;
+        s = shape_of<kRows>(a, u);
+        const int off = static_cast<int>(tile - prefix[u]);
+        item = off / s.tiles;
+        k = off - item * s.tiles;
+        begin = tile - k;
+    }
+    __device__ __forceinline__ void next(const AttnArgs& a, const uint32_t* prefix)
+    {
+        if (++k < s.tiles) return;
+        k = 0;
+        begin += s.tiles;
+        if (++item < a.c.kv_heads * s.row_tiles) return;
+        item = 0;
+        do ++request; while (request < a.requests && prefix[request + 1] == prefix[request]);
+        if (request < a.requests) s = shape_of<kRows>(a, request);
+    }
+    __device__ __forceinline__ int head() const { return item / s.row_tiles; }
+    __device__ __forceinline__ int pos() const { return (s.lo + k) * kTile; }
+};
 
 __device__ __forceinline__ float ex2(float v)
 {
@@ -93,7 +129,6 @@ __device__ __forceinline__ float ex2(float v)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-
 __device__ __forceinline__ float lg2(float v)
 {
     float r;
@@ -101,89 +136,97 @@ __device__ __forceinline__ float lg2(float v)
     return r;
 }
 
-// D (16 x 8, fp32) += A (16 x 16, fp16, row major) B (16 x 8, fp16, column major)
-__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+// d_2 65536 + d_1 256 + d_0 for digit sums below 2^22
+__device__ __forceinline__ float join_digits(uint32_t d0, uint32_t d1, uint32_t d2)
 {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    const int hi = static_cast<int>(d2) * 256 + static_cast<int>(d1);
+    return fmaf(static_cast<float>(hi), 256.f, static_cast<float>(static_cast<int>(d0)));
 }
 
-// Bytes (b0, b1) or (b2, b3) of a word of codes with the sign bit flipped, as two fp16 values: 1024 + (code + 128) - 1152.
-template <int kPair>
-__device__ __forceinline__ uint32_t codes_to_half2(uint32_t flipped)
+template <int kN>
+__device__ __forceinline__ void load_columns(uint32_t taddr, uint32_t (&v)[kN])
 {
-    const uint32_t v = __byte_perm(flipped, 0x64646464u, kPair == 0 ? 0x4140 : 0x4342);
-    const uint32_t offset = 0x64806480u;   // 1152
-    const __half2 h = __hsub2(*reinterpret_cast<const __half2*>(&v), *reinterpret_cast<const __half2*>(&offset));
-    return *reinterpret_cast<const uint32_t*>(&h);
+    if constexpr (kN >= 32) {
+        uint32_t x[32];
+        tmem_ld_32x32(taddr, x);
+        if constexpr (kN > 32) {
+            uint32_t y[16];
+            tmem_ld_32x16(taddr + 32, y);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) v[32 + i] = y[i];
+        } else {
+            tmem_ld_wait();
+        }
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = x[i];
+    } else {
+        tmem_ld_32x16(taddr, v);
+        tmem_ld_wait();
+    }
 }
 
-__device__ __forceinline__ uint4 lds128(uint32_t addr)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
-    return v;
-}
-__device__ __forceinline__ uint2 lds64(uint32_t addr)
-{
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
-    return v;
-}
-
-struct WorkerParts {               // the partial results that a warp leaves for its CTA
-    int head, tail;                // 0 / 1
-    int head_begin, head_end, head_request, head_item;
-    int tail_begin, tail_end, tail_request, tail_item;
+// What the compute threads know of an item: two of them, for the one at work and the next.
+struct ItemInfo {
+    float factor[kMaxRows];                // from a digit sum to a logit in base 2
+    int32_t begin[kMaxRows], end[kMaxRows];
+    int64_t out[kMaxRows];                 // offset of the row in y, -1 beyond the request's rows
+    int64_t lse[kMaxRows];
+    int32_t full_lo, full_hi;              // tokens that every row sees
 };
-struct Group {                     // an item's partial results within one CTA
-    int begin, end, request, item, first, count;
-};
 
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreads, 1)
+template <typename T, int D, int kRows>
+__global__ void __launch_bounds__(kThreads, D == 256 ? 1 : 2)
 attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
 {
-    constexpr int kHalves = D > 128 ? D / 128 : 1;     // boxes along a row
+    constexpr int kHalves = D > 128 ? 2 : 1;           // boxes along a row of the cache
     constexpr int kRowBytes = D < 128 ? D : 128;
-    constexpr int kChunks = kRowBytes / 64;            // 16-byte chunks of a key row that a lane holds, per box
-    constexpr int kNt = D / 8;                         // 8-column tiles of the output
-    constexpr int kNtBox = kNt / kHalves;
-    constexpr int kKs = D / 16;                        // matrix instructions along a head
-    constexpr int kBox = kTile * kRowBytes;
+    constexpr int kN = (3 * kRows + 15) / 16 * 16;     // operand columns: digit * kRows + row
+    constexpr int kBox = kTile * kRowBytes;            // K or V of one tile and half
     constexpr int kStage = 2 * kHalves * kBox;
+    constexpr int kPart = kMaxRows * D + 2 * kMaxRows;
+    constexpr uint32_t kMulK = (2u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(kN >> 3) << 17) | (static_cast<uint32_t>(kTile >> 4) << 24);
+    constexpr uint32_t kMulV = (2u << 4) | (1u << 7) | (0u << 10) | (1u << 15) | (static_cast<uint32_t>(kN >> 3) << 17) | (128u >> 4 << 24);
 
     extern __shared__ uint8_t smem_raw[];
-    __shared__ float s_m[kWarps][2][16], s_l[kWarps][2][16];
-    __shared__ WorkerParts s_parts[kWarps];
-    __shared__ Group s_groups[2 * kWarps];
-    __shared__ int s_members[2 * kWarps], s_group_count, s_last;
-    __shared__ uint64_t s_bars[kWarps][kMaxStages];
-    __shared__ uint32_t s_scan[kWarps];
+    __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_sfull[2], s_pfull, s_ofull, s_qfull, s_drain;
+    __shared__ __align__(16) float s_max[2][kMaxRows][kComputeWarps], s_sum[kMaxRows][kComputeWarps];
+    __shared__ __align__(16) ItemInfo s_item[2];
+    __shared__ uint32_t s_scan[kThreads / 32], s_tmem;
+    __shared__ int s_last;
 
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
-    const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    uint8_t* smem = smem_raw + (smem_base - smem_u32(smem_raw));
-    const int ring_bytes = a.stages * kStage;
-    TileInfo* info = reinterpret_cast<TileInfo*>(smem + kWarps * ring_bytes) + warp * 2 * kBatch;
-    uint32_t* prefix = reinterpret_cast<uint32_t*>(smem + kWarps * ring_bytes + kWarps * 2 * kBatch * sizeof(TileInfo));
-    const uint32_t ring = smem_base + warp * ring_bytes;
-    const uint32_t bars = smem_u32(&s_bars[warp][0]);
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* const smem = smem_raw + (base - smem_u32(smem_raw));
+    const uint32_t off_p = a.stages * kStage, off_q = off_p + kN * 128, off_prefix = off_q + kHalves * kN * kRowBytes;
+    uint32_t* const prefix = reinterpret_cast<uint32_t*>(smem + off_prefix);
 
-    if (lane < kMaxStages) mbar_init(bars + 8 * lane, 1);
     if (tid == 0) {
         prefetch_tensormap(&k_map);
         prefetch_tensormap(&v_map);
+        for (int i = 0; i < kMaxStages; ++i) {
+            mbar_init(smem_u32(&s_full[i]), 1);
+            mbar_init(smem_u32(&s_empty[i]), 1);
+        }
+        mbar_init(smem_u32(&s_sfull[0]), 1);
+        mbar_init(smem_u32(&s_sfull[1]), 1);
+        mbar_init(smem_u32(&s_ofull), 1);
+        mbar_init(smem_u32(&s_drain), 1);
+        mbar_init(smem_u32(&s_pfull), kComputeWarps);
+        mbar_init(smem_u32(&s_qfull), kComputeWarps);
+        fence_barrier_init();
     }
-    fence_barrier_init();
+    if (warp == kComputeWarps + 1) {
+        tmem_alloc(smem_u32(&s_tmem), kTmemColumns);
+        tmem_relinquish();
+    }
 
     // ---- tiles before each request: an exclusive prefix sum over the requests ----
     const int per = (a.requests + kThreads - 1) / kThreads;
     const int r_lo = min(tid * per, a.requests), r_hi = min(r_lo + per, a.requests);
     uint32_t mine = 0;
     for (int r = r_lo; r < r_hi; ++r) {
-        const RequestShape s = shape_of(a, r);
+        const RequestShape s = shape_of<kRows>(a, r);
         const uint32_t n = static_cast<uint32_t>(a.c.kv_heads) * s.row_tiles * s.tiles;
         prefix[r] = n;
         mine += n;
@@ -198,7 +241,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
     __syncthreads();
     uint32_t before = scan - mine, total = 0;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
+    for (int w = 0; w < kThreads / 32; ++w) {
         if (w < warp) before += s_scan[w];
         total += s_scan[w];
     }
@@ -208,490 +251,450 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         before += n;
     }
     if (tid == 0) prefix[a.requests] = total;
+    tc_fence_before();
     __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
 
-    const int all = static_cast<int>(total);
-    const int workers = gridDim.x * kWarps;
-    const int share = max((all + workers - 1) / workers, kMinShare);
-    const int cta_share = share * kWarps;
-    const int t0 = min((static_cast<int>(blockIdx.x) * kWarps + warp) * share, all);
-    const int count = min(t0 + share, all) - t0;
+    const int all = static_cast<int>(total), share = (all + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x);
+    const int t0 = min(static_cast<int>(blockIdx.x) * share, all), count = min(t0 + share, all) - t0;
+    auto timed_out = [&]() {
+        if (lane == 0 && atomicCAS(a.status, 0, QTZ_ERR_DEVICE_TIMEOUT) == 0) a.status[1] = QTZ_SITE_KV_ATTENTION;
+    };
+    Cursor<kRows> cur;
+    if (count > 0) cur.seek(a, prefix, t0);
 
-    // ---- tile look-up, a batch at a time: lane i takes tile t0 + batch * kBatch + i ----
-    const int64_t heads = a.c.kv_heads;
-    auto look_up = [&](int batch) {                    // everything but the scales; returns block * heads + head, or -1
-        const int i = batch * kBatch + lane;
-        if (i >= count) return static_cast<int64_t>(-1);
-        const uint32_t tile = t0 + i;
-        int u = 0, v = a.requests;
-        while (v - u > 1) {
-            const int mid = (u + v) >> 1;
-            if (prefix[mid] <= tile) u = mid; else v = mid;
-        }
-        const RequestShape s = shape_of(a, u);
-        const int off = static_cast<int>(tile - prefix[u]);
-        const int item = off / s.tiles, k = off - item * s.tiles;
-        const int pos = (s.lo + k) * kTile, h = item / s.row_tiles;
-        int flags = (k == 0 ? kFirst : 0) | (k == s.tiles - 1 ? kLast : 0);
-        int64_t bh = -1;
-        TileInfo& e = info[(batch & 1) * kBatch + lane];
-        if (s.lo + k < s.hi) {
-            const int id = a.table[static_cast<int64_t>(u) * a.width + pos / a.c.block_tokens];
-            if (id >= 0 && id < a.c.blocks) {
-                flags |= kValid;
-                bh = id * heads + h;
-                e.row = static_cast<int32_t>(bh * a.c.block_tokens + pos % a.c.block_tokens);
-            } else {
-                qtz_dev::report_invalid(a.status, QTZ_SITE_KV_ATTENTION);
+    if (count > 0 && warp == kComputeWarps) {
+        // ======== producer: lane j brings box j (box_rows tokens) of the tile ========
+        const int boxes = kTile / a.box_rows;
+        // row of the box in the [blocks * heads * block_tokens] view, -1 if there is nothing to bring
+        auto look_up = [&](const Cursor<kRows>& c) {
+            const int pos = c.pos() + lane * a.box_rows;
+            if (lane >= boxes || pos >= c.s.limit) return -1;
+            const int id = a.table[static_cast<int64_t>(c.request) * a.width + pos / a.c.block_tokens];
+            if (id < 0 || id >= a.c.blocks) return -1;
+            return static_cast<int>((static_cast<int64_t>(id) * a.c.kv_heads + c.head()) * a.c.block_tokens + pos % a.c.block_tokens);
+        };
+        int row = look_up(cur), i = 0, stage = 0, round = 0;
+        for (; i < count; ++i) {
+            int ahead = -1;
+            if (i + 1 < count) {
+                cur.next(a, prefix);
+                ahead = look_up(cur);                  // in flight while this tile is issued
+            }
+            if (round > 0 && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&s_empty[stage]), (round - 1) & 1, a.wait_budget))) {
+                timed_out();
+                break;
+            }
+            const uint32_t bar = smem_u32(&s_full[stage]), dst = base + stage * kStage;
+            const int have = __popc(__ballot_sync(0xffffffffu, row >= 0));
+            if (lane == 0) mbar_arrive_expect_tx(bar, have * a.box_rows * 2 * D);
+            __syncwarp();
+            if (row >= 0) {
+                const uint32_t at = dst + lane * a.box_rows * kRowBytes;
+#pragma unroll
+                for (int hh = 0; hh < kHalves; ++hh) tma_load_2d(at + hh * kBox, &k_map, bar, hh * 128, row);
+#pragma unroll
+                for (int hh = 0; hh < kHalves; ++hh) tma_load_2d(at + (kHalves + hh) * kBox, &v_map, bar, hh * 128, row);
+            }
+            row = ahead;
+            if (++stage == a.stages) {
+                stage = 0;
+                ++round;
             }
         }
-        e.pos = pos;
-        e.request = u;
-        e.item = item;
-        e.flags = flags;
-        return bh;
-    };
-    // Scales lie in [2^-100, 2^122] here (the least is QTZ_KV_MIN_SCALE; no 16-bit value gives more than 2^121), so that their
-    // logarithms and inverses are ordinary numbers.
-    auto scale_of = [&](const float* p, int64_t bh) { return bh < 0 ? 1.f : fminf(fmaxf(p[bh], QTZ_KV_MIN_SCALE), 5.3169120e36f); };
-
-    int64_t bh = look_up(0);
-    float ks = scale_of(a.c.k_scale_dev, bh), vs = scale_of(a.c.v_scale_dev, bh);
-    auto put_scales = [&](int batch) {
-        info[(batch & 1) * kBatch + lane].k_scale = ks;
-        info[(batch & 1) * kBatch + lane].v_scale = vs;
-    };
-    put_scales(0);
-    __syncwarp();
-
-    bool failed = false;
-    auto issue = [&](int i, int stage) {               // lane 0 only
-        const TileInfo& e = info[((i / kBatch) & 1) * kBatch + i % kBatch];
-        const uint32_t bar = bars + 8 * stage, dst = ring + stage * kStage;
-        if (!(e.flags & kValid)) {
-            mbar_arrive(bar);
-            return;
-        }
-        mbar_arrive_expect_tx(bar, kStage);
+        // nothing may be in flight when the CTA ends
+        for (int j = max(0, i - a.stages); j < i; ++j)
+            if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&s_full[j % a.stages]), (j / a.stages) & 1, a.wait_budget))) timed_out();
+    } else if (count > 0 && warp == kComputeWarps + 1) {
+        // ======== matrix instructions: S of the next tile is issued before O of this one ========
+        int items = 0;
+        bool ok = true;
+        auto multiply_keys = [&](int i, const Cursor<kRows>& c) {
+            const int stage = i % a.stages;
+            if (i == 0 || c.k == 0) {
+                ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_qfull), items & 1, a.wait_budget));
+                ++items;
+            }
+            ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_full[stage]), (i / a.stages) & 1, a.wait_budget));
+            if (!ok) return;
+            tc_fence_after();
+            if (elect_one()) {
 #pragma unroll
-        for (int hh = 0; hh < kHalves; ++hh) {
-            tma_load_2d(dst + hh * kBox, &k_map, bar, hh * 128, e.row);
-            tma_load_2d(dst + (kHalves + hh) * kBox, &v_map, bar, hh * 128, e.row);
-        }
-    };
-    int issued = min(a.stages, count);
-    if (lane == 0)
-        for (int i = 0; i < issued; ++i) issue(i, i);
-
-    // ---- state of the current item ----
-    uint32_t qf[kKs][4];
-    float o[kNt][4], m0 = 0.f, m1 = 0.f, l0 = 0.f, l1 = 0.f, f0 = 0.f, f1 = 0.f;
-    int end0 = 0, end1 = 0, begin0 = 0, begin1 = 0, full_lo = 0, full_hi = 0;
-    int seg_begin = 0;                                 // index in the share where the item's part of this warp begins
-    bool seg_whole = false;
-
-    // A row of a 16-row tile: its token and head, or false beyond the request's rows.
-    auto row_of = [&](const RequestShape& s, int item, int row, int64_t& token, int& head, int& local) {
-        const int h = item / s.row_tiles, index = (item - h * s.row_tiles) * 16 + row;
-        local = index / a.group;
-        head = h * a.group + (index - local * a.group);
-        token = s.first + local;
-        return local < s.added;
-    };
-    auto write_lse = [&](int64_t token, int head, float m, float l) {
-        if (a.lse) a.lse[token * a.q_heads + head] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.693147181f;
-    };
-
-    int stage = 0;
-    uint32_t phase = 0;
-    for (int i = 0; i < count; ++i) {
-        const int in_batch = i % kBatch, batch = i / kBatch;
-        // the next batch's addresses and scales come in three steps, far apart, so that no load is waited for
-        if (in_batch == 0) bh = look_up(batch + 1);
-        else if (in_batch == 8) {
-            ks = scale_of(a.c.k_scale_dev, bh);
-            vs = scale_of(a.c.v_scale_dev, bh);
-        } else if (in_batch == 16) {
-            put_scales(batch + 1);
+                for (int hh = 0; hh < kHalves; ++hh)
+#pragma unroll
+                    for (int j = 0; j < kRowBytes / 32; ++j)
+                        mma_i8(tmem + (i & 1) * 64, make_kmajor_desc(base + stage * kStage + hh * kBox, kRowBytes) + 2 * j,
+                               make_kmajor_desc(base + off_q + hh * kN * kRowBytes, kRowBytes) + 2 * j, kMulK, hh + j > 0);
+                mma_commit(smem_u32(&s_sfull[i & 1]));
+            }
+            __syncwarp();
+        };
+        multiply_keys(0, cur);
+        for (int i = 0; i < count && ok; ++i) {
+            if (i + 1 < count) {
+                cur.next(a, prefix);
+                multiply_keys(i + 1, cur);
+            }
+            ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_pfull), i & 1, a.wait_budget));
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint32_t v = base + (i % a.stages) * kStage + kHalves * kBox;
+#pragma unroll
+                for (int hh = 0; hh < kHalves; ++hh)
+#pragma unroll
+                    for (int j = 0; j < kTile / 32; ++j)
+                        mma_i8(tmem + 128 + hh * 64, make_mnmajor_desc(v + hh * kBox + j * 32 * kRowBytes, kRowBytes),
+                               make_kmajor_desc(base + off_p, 128) + 2 * j, kMulV, j > 0);
+                mma_commit(smem_u32(&s_ofull));
+                mma_commit(smem_u32(&s_empty[i % a.stages]));
+            }
             __syncwarp();
         }
-        const TileInfo e = info[(batch & 1) * kBatch + in_batch];
-
-        if (i == 0 || (e.flags & kFirst)) {            // a new item: its query rows, converted once
-            const RequestShape s = shape_of(a, e.request);
-            seg_begin = i;
-            seg_whole = (e.flags & kFirst) != 0;
-            m0 = m1 = -INFINITY;
-            l0 = l1 = 0.f;
-#pragma unroll
-            for (int n = 0; n < kNt; ++n)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) o[n][c] = 0.f;
-#pragma unroll
-            for (int hi = 0; hi < 2; ++hi) {
-                int64_t token;
-                int head, local;
-                const bool has = row_of(s, e.item, g + 8 * hi, token, head, local);
-                const T* q = static_cast<const T*>(a.q) + token * a.q_token_stride + head * a.q_head_stride;
-                // what the row sees; a row beyond the request's is never written and needs no mask
-                const int own = s.len - s.added + local + 1;
-                (hi ? end1 : end0) = has ? min(own, s.limit) : 0x7fffffff;
-                (hi ? begin1 : begin0) = has && a.window > 0 ? max(0, own - a.window) : 0;
-                uint32_t raw[kKs][2];
+        if (!ok) {                                     // what was issued may still run: give it the same limit, then go
+            timed_out();
+            if (elect_one()) mma_commit(smem_u32(&s_drain));
+            __syncwarp();
+            mbar_wait(smem_u32(&s_drain), 0, a.wait_budget);
+        }
+    } else if (count > 0) {
+        // ======== compute: thread = token of S^T, then column of O^T ========
+        bool ok = true;
+        auto wait = [&](uint64_t& bar, int parity) {   // the warp goes on together
+            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar), parity, a.wait_budget)) && ok;
+        };
+        // Digits of an item's query rows into the operand, and what the softmax has to know of them.
+        auto load_queries = [&](const Cursor<kRows>& c, int which) {
+            ItemInfo& it = s_item[which];
+            constexpr int kPer = D / 32;               // values of a row that a lane holds
+            const int h = c.head(), row0 = (c.item - h * c.s.row_tiles) * kRows;
+            int lo = 0, hi = 0x7fffffff;
+            for (int r = 0; r < kRows; ++r) {
+                const int local = (row0 + r) / a.group, sub = row0 + r - local * a.group;
+                const bool has = local < c.s.added;
+                const int own = c.s.len - c.s.added + local + 1;
+                const int end = has ? min(own, c.s.limit) : 0, begin = has && a.window > 0 ? max(0, own - a.window) : 0;
+                if (has) {
+                    lo = max(lo, begin);
+                    hi = min(hi, end);
+                }
+                if (r % kComputeWarps != warp) continue;
+                const int64_t token = c.s.first + local;
+                const int head = h * a.group + sub;
+                float v[kPer];
                 float top = 0.f;
-#pragma unroll
-                for (int ch = 0; ch < kHalves * kChunks; ++ch) {
-                    const int d0 = (ch / kChunks) * 128 + (kChunks * t4 + ch % kChunks) * 16;
-                    uint4 u = {0, 0, 0, 0}, v = {0, 0, 0, 0};
-                    if (has) {
-                        u = __ldg(reinterpret_cast<const uint4*>(q + d0));
-                        v = __ldg(reinterpret_cast<const uint4*>(q + d0) + 1);
+                bool odd = false;
+                if (has) {
+                    const T* q = static_cast<const T*>(a.q) + token * a.q_token_stride + head * a.q_head_stride + lane * kPer;
+                    uint32_t raw[kPer / 2];
+                    if constexpr (kPer == 2) raw[0] = *reinterpret_cast<const uint32_t*>(q);
+                    else if constexpr (kPer == 4) {
+                        const uint2 u = *reinterpret_cast<const uint2*>(q);
+                        raw[0] = u.x; raw[1] = u.y;
+                    } else {
+                        const uint4 u = *reinterpret_cast<const uint4*>(q);
+                        raw[0] = u.x; raw[1] = u.y; raw[2] = u.z; raw[3] = u.w;
                     }
-                    const uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        raw[ch * 4 + k / 2][k & 1] = w[k];
-                        const float2 f = qtz_dev::unpack2(w[k], T());
-                        top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
+                    for (int j = 0; j < kPer / 2; ++j) {
+                        const float2 f = qtz_dev::unpack2(raw[j], T());
+                        v[2 * j] = f.x;
+                        v[2 * j + 1] = f.y;
                     }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < kPer; ++j) v[j] = 0.f;
                 }
-                // bf16 rows are scaled by a power of two that takes their largest value to [2^14, 2^15): values down to
-                // 2^-28 of it stay exact in fp16.  fp16 rows are taken as they are.
-                float mult = 1.f, back = a.scale_log2;
-                if constexpr (sizeof(T) == 2 && !std::is_same<T, __half>::value) {
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                    const int ex = max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -100);
-                    mult = __uint_as_float(static_cast<uint32_t>(127 + 14 - ex) << 23);
-                    back *= __uint_as_float(static_cast<uint32_t>(127 - 14 + ex) << 23);
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) {
+                    odd = odd || (__float_as_uint(v[j]) & 0x7f800000u) == 0x7f800000u;
+                    top = fmaxf(top, fabsf(v[j]));
                 }
-                (hi ? f1 : f0) = back;
+                top = redux_max(top);
+                odd = __any_sync(0xffffffffu, odd);
+                // rows below 2^-100 count as 2^-100 (their logits are zero either way)
+                const int ex = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -100), 127);
+                const float mult = __uint_as_float(static_cast<uint32_t>(127 + min(21 - ex, 127)) << 23);
+                uint64_t digits[3] = {0, 0, 0};
 #pragma unroll
-                for (int k = 0; k < kKs; ++k)
+                for (int j = 0; j < kPer; ++j) {
+                    const int x = odd ? 0 : __float2int_rn(v[j] * mult);
+                    const int d0 = (x << 24) >> 24, x1 = (x - d0) >> 8, d1 = (x1 << 24) >> 24, d2 = (x1 - d1) >> 8;
+                    digits[0] |= static_cast<uint64_t>(d0 & 0xff) << (8 * j);
+                    digits[1] |= static_cast<uint64_t>(d1 & 0xff) << (8 * j);
+                    digits[2] |= static_cast<uint64_t>(d2 & 0xff) << (8 * j);
+                }
+                const int d = lane * kPer, hh = d / 128, x = d % kRowBytes;
 #pragma unroll
-                    for (int p = 0; p < 2; ++p) {
-                        if constexpr (std::is_same<T, __half>::value) {
-                            qf[k][2 * p + hi] = raw[k][p];
-                        } else {
-                            const float2 f = qtz_dev::unpack2(raw[k][p], T());
-                            qf[k][2 * p + hi] = qtz_dev::pack2(f.x * mult, f.y * mult, __half());
-                        }
-                    }
+                for (int g = 0; g < 3; ++g) {
+                    const int n = g * kRows + r;
+                    const int swz = kRowBytes == 128 ? (n & 7) : ((n >> 1) & 3);
+                    uint8_t* to = smem + off_q + hh * kN * kRowBytes + n * kRowBytes + (((x >> 4) ^ swz) << 4) + (x & 15);
+                    if constexpr (kPer == 2) *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(digits[g]);
+                    else if constexpr (kPer == 4) *reinterpret_cast<uint32_t*>(to) = static_cast<uint32_t>(digits[g]);
+                    else *reinterpret_cast<uint64_t*>(to) = digits[g];
+                }
+                if (lane == 0) {
+                    // a row that holds NaN or infinity gives NaN
+                    it.factor[r] = odd ? __uint_as_float(0x7fc00000u) : a.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 - 21 + ex) << 23);
+                    it.begin[r] = begin;
+                    it.end[r] = end;
+                    it.out[r] = has ? token * a.y_token_stride + head * a.y_head_stride : -1;
+                    it.lse[r] = token * a.q_heads + head;
+                }
             }
-            // tiles inside [full_lo, full_hi) need no mask for any row
-            full_lo = max(begin0, begin1);
-            full_hi = min(end0, end1);
-#pragma unroll
-            for (int off = 4; off < 32; off <<= 1) {
-                full_lo = max(full_lo, __shfl_xor_sync(0xffffffffu, full_lo, off));
-                full_hi = min(full_hi, __shfl_xor_sync(0xffffffffu, full_hi, off));
+            if (tid == 0) {
+                it.full_lo = lo;
+                it.full_hi = hi;
             }
-        }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&s_qfull));
+        };
 
-        // after a wait that gave up nothing more is issued, but what is in flight is still waited for (with the same limit)
-        if (i < issued && !mbar_wait(bars + 8 * stage, phase, a.wait_budget)) {
-            if (lane == 0 && atomicCAS(a.status, 0, QTZ_ERR_DEVICE_TIMEOUT) == 0) a.status[1] = QTZ_SITE_TMA_FULL;
-            failed = true;
-        }
-        failed = __any_sync(0xffffffffu, failed);
+        // block * heads + head of this thread's token, -1 if it has none
+        auto token_block = [&](const Cursor<kRows>& c) {
+            const int pos = c.pos() + tid;
+            if (pos >= c.s.limit) return static_cast<int64_t>(-1);
+            const int id = a.table[static_cast<int64_t>(c.request) * a.width + pos / a.c.block_tokens];
+            if (id < 0 || id >= a.c.blocks) {
+                qtz_dev::report_invalid(a.status, QTZ_SITE_KV_ATTENTION);
+                return static_cast<int64_t>(-1);
+            }
+            return static_cast<int64_t>(id) * a.c.kv_heads + c.head();
+        };
+        // Scales lie in [2^-100, 2^122] here (the least is QTZ_KV_MIN_SCALE; no 16-bit value gives more than 2^121), so
+        // that their logarithms and inverses are ordinary numbers.
+        auto scale_of = [&](const float* p, int64_t bh) { return bh < 0 ? 1.f : fminf(fmaxf(p[bh], QTZ_KV_MIN_SCALE), 5.3169120e36f); };
 
-        if ((e.flags & kValid) && !failed) {
-            const uint32_t kb = ring + stage * kStage, vb = kb + kHalves * kBox;
-            float sa[4] = {}, sb[4] = {};
+        int items = 0;
+        load_queries(cur, 0);
+        int64_t bh = token_block(cur);
+        float ks = scale_of(a.c.k_scale_dev, bh), vs = scale_of(a.c.v_scale_dev, bh);
+        Cursor<kRows> ahead = cur;
+        float m[kRows], l[kRows], acc[kHalves][kRows];
+        int seg_first = cur.k;
+
+        auto reset = [&]() {
 #pragma unroll
-            for (int ch = 0; ch < kHalves * kChunks; ++ch) {
-                const int hh = ch / kChunks;
-                // 16-byte chunk c of row r lies at chunk c ^ (r & 7) of a 128-byte row, c ^ ((r >> 1) & 3) of a 64-byte row
-                const int chunk = kRowBytes == 128 ? ((2 * t4 + ch % kChunks) ^ g) : (t4 ^ (g >> 1));
-                const uint32_t at = kb + hh * kBox + g * kRowBytes + chunk * 16;
-                const uint4 ua = lds128(at), ub = lds128(at + 8 * kRowBytes);
-                const uint32_t wa[4] = {ua.x, ua.y, ua.z, ua.w}, wb[4] = {ub.x, ub.y, ub.z, ub.w};
+            for (int r = 0; r < kRows; ++r) {
+                m[r] = -INFINITY;
+                l[r] = 0.f;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const uint32_t xa = wa[k] ^ 0x80808080u, xb = wb[k] ^ 0x80808080u;
-                    mma(sa, qf[ch * 4 + k], codes_to_half2<0>(xa), codes_to_half2<1>(xa));
-                    mma(sb, qf[ch * 4 + k], codes_to_half2<0>(xb), codes_to_half2<1>(xb));
+                for (int hh = 0; hh < kHalves; ++hh) acc[hh][r] = 0.f;
+            }
+        };
+        reset();
+        auto write_row = [&](const ItemInfo& it, int r, float mm, float ll, const float (&v)[kHalves], int d) {
+            if (it.out[r] < 0) return;
+            const float inv = ll == 0.f ? 0.f : __fdiv_rn(1.f, ll);
+            T* y = static_cast<T*>(a.y) + it.out[r] + d;
+#pragma unroll
+            for (int hh = 0; hh < kHalves; ++hh) y[hh * 128] = qtz_dev::from_f32<T>(v[hh] * inv);
+            if (d == 0 && a.lse) a.lse[it.lse[r]] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.693147181f;
+        };
+
+        for (int i = 0; i < count; ++i) {
+            const ItemInfo& it = s_item[items & 1];
+            const int pos0 = cur.pos(), pos = pos0 + tid;
+            const bool last = cur.k == cur.s.tiles - 1, more = i + 1 < count;
+            // the next tile's block, in flight during this one
+            int64_t bh_next = -1;
+            if (more) {
+                ahead.next(a, prefix);
+                bh_next = token_block(ahead);
+            }
+            if (i == 0 || cur.k == 0) wait(s_qfull, items & 1);
+            wait(s_sfull[i & 1], (i >> 1) & 1);
+            tc_fence_after();
+            float x[kRows];
+            {
+                uint32_t s[kN];
+                load_columns<kN>(tmem + (i & 1) * 64 + (static_cast<uint32_t>(warp) << 21), s);
+                const float lv = lg2(vs);
+#pragma unroll
+                for (int r = 0; r < kRows; ++r)
+                    x[r] = fmaf(join_digits(s[r], s[kRows + r], s[2 * kRows + r]), it.factor[r] * ks, lv);
+            }
+            if (bh < 0) {
+#pragma unroll
+                for (int r = 0; r < kRows; ++r) x[r] = -INFINITY;
+            } else if (pos0 < it.full_lo || pos0 + kTile > it.full_hi) {
+#pragma unroll
+                for (int r = 0; r < kRows; ++r)
+                    if (pos < it.begin[r] || pos >= it.end[r]) x[r] = -INFINITY;
+            }
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                const float top = redux_max(x[r]);
+                if (lane == 0) s_max[i & 1][r][warp] = top;
+            }
+            ok = named_barrier_and(1, kComputeThreads, ok);
+            if (!ok) break;
+            const float inv = __fdividef(1.f, vs);
+            float keep[kRows];
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                const float4 t = *reinterpret_cast<const float4*>(s_max[i & 1][r]);
+                const float top = fmaxf(fmaxf(fmaxf(t.x, t.y), fmaxf(t.z, t.w)), m[r]);
+                const float origin = top == -INFINITY ? 0.f : top;
+                keep[r] = ex2(m[r] - origin);
+                m[r] = top;
+                const float w = ex2(x[r] - origin);
+                l[r] = fmaf(w, inv, l[r] * keep[r]);
+                // w in [0, 1]: the mantissa of w + 2 is w in units of 2^-22, its bytes are the digits
+                const uint32_t bits = __float_as_uint(w + 2.f);
+#pragma unroll
+                for (int g = 0; g < 3; ++g) {
+                    const int n = g * kRows + r;
+                    smem[off_p + n * 128 + (((tid >> 4) ^ (n & 7)) << 4) + (tid & 15)] = static_cast<uint8_t>(bits >> (8 * g));
                 }
             }
-            const float lv = lg2(e.v_scale), k0 = f0 * e.k_scale, k1 = f1 * e.k_scale;
-            float x0[4] = {fmaf(sa[0], k0, lv), fmaf(sa[1], k0, lv), fmaf(sb[0], k0, lv), fmaf(sb[1], k0, lv)};
-            float x1[4] = {fmaf(sa[2], k1, lv), fmaf(sa[3], k1, lv), fmaf(sb[2], k1, lv), fmaf(sb[3], k1, lv)};
-            if (e.pos < full_lo || e.pos + kTile > full_hi) {
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const int p = e.pos + (c >> 1) * 8 + 2 * t4 + (c & 1);
-                    if (p < begin0 || p >= end0) x0[c] = -INFINITY;
-                    if (p < begin1 || p >= end1) x1[c] = -INFINITY;
-                }
-            }
-            float n0 = fmaxf(fmaxf(x0[0], x0[1]), fmaxf(x0[2], x0[3])), n1 = fmaxf(fmaxf(x1[0], x1[1]), fmaxf(x1[2], x1[3]));
-            n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, 1));
-            n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, 1));
-            n0 = fmaxf(n0, __shfl_xor_sync(0xffffffffu, n0, 2));
-            n1 = fmaxf(n1, __shfl_xor_sync(0xffffffffu, n1, 2));
-            n0 = fmaxf(n0, m0);
-            n1 = fmaxf(n1, m1);
-            if (__any_sync(0xffffffffu, n0 > m0 || n1 > m1)) {
-                const float c0 = n0 > m0 ? ex2(m0 - n0) : 1.f, c1 = n1 > m1 ? ex2(m1 - n1) : 1.f;
-                l0 *= c0;
-                l1 *= c1;
-#pragma unroll
-                for (int n = 0; n < kNt; ++n) {
-                    o[n][0] *= c0;
-                    o[n][1] *= c0;
-                    o[n][2] *= c1;
-                    o[n][3] *= c1;
-                }
-                m0 = n0;
-                m1 = n1;
-            }
-            const float b0 = m0 == -INFINITY ? 0.f : m0, b1 = m1 == -INFINITY ? 0.f : m1;
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                x0[c] = ex2(x0[c] - b0);
-                x1[c] = ex2(x1[c] - b1);
-            }
-            const float inv = __fdividef(1.f, e.v_scale);
-            l0 = fmaf((x0[0] + x0[1]) + (x0[2] + x0[3]), inv, l0);
-            l1 = fmaf((x1[0] + x1[1]) + (x1[2] + x1[3]), inv, l1);
-            const uint32_t pf[4] = {qtz_dev::pack2(x0[0], x0[1], __half()), qtz_dev::pack2(x1[0], x1[1], __half()),
-                                    qtz_dev::pack2(x0[2], x0[3], __half()), qtz_dev::pack2(x1[2], x1[3], __half())};
+            tc_fence_before();
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&s_pfull));
+
+            // while O is under way: the next tile's scales, the next item's queries
+            bh = bh_next;
+            ks = scale_of(a.c.k_scale_dev, bh);
+            vs = scale_of(a.c.v_scale_dev, bh);
+            if (last && more) load_queries(ahead, (items + 1) & 1);
+
+            wait(s_ofull, i & 1);
+            tc_fence_after();
 #pragma unroll
             for (int hh = 0; hh < kHalves; ++hh) {
-                uint32_t w[4][4];                      // [token of this lane][word]: tokens 2 t4, 2 t4 + 1, 2 t4 + 8, 2 t4 + 9
+                uint32_t o[kN];
+                load_columns<kN>(tmem + 128 + hh * 64 + (static_cast<uint32_t>(warp) << 21), o);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int row = 2 * t4 + (k & 1) + 8 * (k >> 1);
-                    if constexpr (kRowBytes == 128) {
-                        const uint4 u = lds128(vb + hh * kBox + row * 128 + ((g ^ (row & 7)) << 4));
-                        w[k][0] = u.x; w[k][1] = u.y; w[k][2] = u.z; w[k][3] = u.w;
-                    } else {
-                        const uint2 u = lds64(vb + row * 64 + (((g >> 1) ^ ((row >> 1) & 3)) << 4) + (g & 1) * 8);
-                        w[k][0] = u.x; w[k][1] = u.y; w[k][2] = 0; w[k][3] = 0;
+                for (int r = 0; r < kRows; ++r)
+                    acc[hh][r] = fmaf(acc[hh][r], keep[r], join_digits(o[r], o[kRows + r], o[2 * kRows + r]));
+            }
+
+            if (last || !more) {                       // the end of the item, or of this CTA's part of it
+#pragma unroll
+                for (int r = 0; r < kRows; ++r) {
+#pragma unroll
+                    for (int off = 16; off > 0; off >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], off);
+                    if (lane == 0) s_sum[r][warp] = l[r];
+                }
+                ok = named_barrier_and(1, kComputeThreads, ok);
+                if (!ok) break;
+                const bool whole = seg_first == 0 && last;
+                // slot 0: an item that began in an earlier CTA; slot 1: one that goes on in the next
+                float* part = a.parts + (static_cast<int64_t>(blockIdx.x) * 2 + (seg_first == 0 ? 1 : 0)) * kPart;
+#pragma unroll
+                for (int r = 0; r < kRows; ++r) {
+                    const float4 t = *reinterpret_cast<const float4*>(s_sum[r]);
+                    const float sum = (t.x + t.y) + (t.z + t.w);
+                    float v[kHalves];
+#pragma unroll
+                    for (int hh = 0; hh < kHalves; ++hh) v[hh] = acc[hh][r] * 2.384185791015625e-07f;   // 2^-22
+                    if (D >= 128 || tid < D) {
+                        if (whole) {
+                            write_row(it, r, m[r], sum, v, tid);
+                        } else {
+#pragma unroll
+                            for (int hh = 0; hh < kHalves; ++hh) part[r * D + hh * 128 + tid] = v[hh];
+                        }
+                    }
+                    if (!whole && tid == 0) {
+                        part[kMaxRows * D + r] = m[r];
+                        part[kMaxRows * D + kMaxRows + r] = sum;
                     }
                 }
+                if (!whole) {
+                    const int c0 = static_cast<int>(cur.begin) / share, c1 = static_cast<int>(cur.begin + cur.s.tiles - 1) / share;
+                    __threadfence();
+                    named_barrier(1, kComputeThreads);
+                    if (tid == 0) {
+                        const int arrived = atomicAdd(&a.counters[c0], 1);
+                        s_last = arrived == c1 - c0;
+                        if (s_last) a.counters[c0] = 0;    // ready for the next call
+                    }
+                    named_barrier(1, kComputeThreads);
+                    if (s_last) {
+                        __threadfence();
+                        auto part_of = [&](int cta) { return a.parts + (static_cast<int64_t>(cta) * 2 + (cta == c0 ? 1 : 0)) * kPart; };
+                        if (D >= 128 || tid < D)
+                            for (int r = 0; r < kRows; ++r) {
+                                if (it.out[r] < 0) continue;
+                                float top = -INFINITY;
+#pragma unroll 8
+                                for (int cta = c0; cta <= c1; ++cta) top = fmaxf(top, __ldcg(part_of(cta) + kMaxRows * D + r));
+                                const float origin = top == -INFINITY ? 0.f : top;
+                                float sum = 0.f, v[kHalves] = {};
+#pragma unroll 8
+                                for (int cta = c0; cta <= c1; ++cta) {
+                                    const float* from = part_of(cta);
+                                    const float pm = __ldcg(from + kMaxRows * D + r), pl = __ldcg(from + kMaxRows * D + kMaxRows + r);
+                                    const float wt = pm == -INFINITY && pl == 0.f ? 0.f : ex2(pm - origin);
+                                    sum = fmaf(pl, wt, sum);
 #pragma unroll
-                for (int k = 0; k < kNtBox / 4; ++k) {
-                    // two tokens' bytes side by side: (a0 b0 a1 b1), (a2 b2 a3 b3)
-                    const uint32_t x = __byte_perm(w[0][k], w[1][k], 0x5140) ^ 0x80808080u, y = __byte_perm(w[0][k], w[1][k], 0x7362) ^ 0x80808080u;
-                    const uint32_t u = __byte_perm(w[2][k], w[3][k], 0x5140) ^ 0x80808080u, v = __byte_perm(w[2][k], w[3][k], 0x7362) ^ 0x80808080u;
-                    const int n = hh * kNtBox + 4 * k;
-                    mma(o[n + 0], pf, codes_to_half2<0>(x), codes_to_half2<0>(u));
-                    mma(o[n + 1], pf, codes_to_half2<1>(x), codes_to_half2<1>(u));
-                    mma(o[n + 2], pf, codes_to_half2<0>(y), codes_to_half2<0>(v));
-                    mma(o[n + 3], pf, codes_to_half2<1>(y), codes_to_half2<1>(v));
+                                    for (int hh = 0; hh < kHalves; ++hh) v[hh] = fmaf(__ldcg(from + r * D + hh * 128 + tid), wt, v[hh]);
+                                }
+                                write_row(it, r, top, sum, v, tid);
+                            }
+                        named_barrier(1, kComputeThreads);
+                    }
                 }
+                reset();
+                seg_first = 0;
             }
+            if (last) ++items;
+            cur = ahead;
         }
-        __syncwarp();                                  // every lane has read the stage
-        if (!failed && issued < count) {
-            if (lane == 0) issue(issued, stage);
-            ++issued;
-        }
-        if (++stage == a.stages) {
-            stage = 0;
-            phase ^= 1;
-        }
-
-        if ((e.flags & kLast) || i == count - 1) {     // the end of the item, or of this warp's part of it
-            l0 += __shfl_xor_sync(0xffffffffu, l0, 1);
-            l1 += __shfl_xor_sync(0xffffffffu, l1, 1);
-            l0 += __shfl_xor_sync(0xffffffffu, l0, 2);
-            l1 += __shfl_xor_sync(0xffffffffu, l1, 2);
-            if (seg_whole && (e.flags & kLast)) {
-                const RequestShape s = shape_of(a, e.request);
-#pragma unroll
-                for (int hi = 0; hi < 2; ++hi) {
-                    int64_t token;
-                    int head, local;
-                    if (!row_of(s, e.item, g + 8 * hi, token, head, local)) continue;
-                    const float l = hi ? l1 : l0, r = l == 0.f ? 0.f : __fdiv_rn(1.f, l);
-                    T* y = static_cast<T*>(a.y) + token * a.y_token_stride + head * a.y_head_stride;
-#pragma unroll
-                    for (int n = 0; n < kNt; n += 8)
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            // column 2 t4 + c of the 8-column tiles n .. n + 7 holds eight neighbouring values
-                            const int d = kRowBytes == 128 ? (n / 16) * 128 + 16 * (2 * t4 + c) + (n % 16) : 8 * (2 * t4 + c);
-                            uint4 v;
-                            v.x = qtz_dev::pack2(o[n + 0][2 * hi + c] * r, o[n + 1][2 * hi + c] * r, T());
-                            v.y = qtz_dev::pack2(o[n + 2][2 * hi + c] * r, o[n + 3][2 * hi + c] * r, T());
-                            v.z = qtz_dev::pack2(o[n + 4][2 * hi + c] * r, o[n + 5][2 * hi + c] * r, T());
-                            v.w = qtz_dev::pack2(o[n + 6][2 * hi + c] * r, o[n + 7][2 * hi + c] * r, T());
-                            *reinterpret_cast<uint4*>(y + d) = v;
-                        }
-                    if (t4 == 0) write_lse(token, head, hi ? m1 : m0, l);
-                }
-            } else {
-                // A part that goes on in the next warp is this warp's last work: it may lie in the ring.  One that began in an
-                // earlier warp may be followed by more items: it goes to the workspace.
-                const int slot = seg_whole ? 1 : 0;
-                float* to = slot ? reinterpret_cast<float*>(smem + warp * ring_bytes)
-                                 : a.warp_parts + (static_cast<int64_t>(blockIdx.x) * kWarps + warp) * (16 * D);
-#pragma unroll
-                for (int n = 0; n < kNt; ++n)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) to[(n * 4 + c) * 32 + lane] = o[n][c];
-                if (t4 == 0) {
-                    s_m[warp][slot][g] = m0;
-                    s_m[warp][slot][g + 8] = m1;
-                    s_l[warp][slot][g] = l0;
-                    s_l[warp][slot][g + 8] = l1;
-                }
-            }
-            if (lane == 0) {
-                const RequestShape s = shape_of(a, e.request);
-                const int begin = static_cast<int>(prefix[e.request]) + e.item * s.tiles;
-                WorkerParts& p = s_parts[warp];
-                if (seg_begin == 0) p.head = p.tail = 0;
-                if (!seg_whole) {
-                    p.head = 1;
-                    p.head_begin = begin; p.head_end = begin + s.tiles; p.head_request = e.request; p.head_item = e.item;
-                } else if (!(e.flags & kLast)) {
-                    p.tail = 1;
-                    p.tail_begin = begin; p.tail_end = begin + s.tiles; p.tail_request = e.request; p.tail_item = e.item;
-                }
-            }
-        }
+        if (!ok) timed_out();
     }
-    if (count <= 0 && lane == 0) s_parts[warp].head = s_parts[warp].tail = 0;
+
+    tc_fence_before();
     __syncthreads();
-
-    // ---- joining: first the parts that the warps of this CTA left ----
-    if (tid == 0) {
-        int groups = 0, members = 0;
-        for (int w = 0; w < kWarps; ++w) {
-            const WorkerParts& p = s_parts[w];
-            if (p.head) {
-                if (groups == 0 || s_groups[groups - 1].begin != p.head_begin)
-                    s_groups[groups++] = Group{p.head_begin, p.head_end, p.head_request, p.head_item, members, 0};
-                s_members[members++] = 2 * w;
-                ++s_groups[groups - 1].count;
-            }
-            if (p.tail) {
-                s_groups[groups++] = Group{p.tail_begin, p.tail_end, p.tail_request, p.tail_item, members, 1};
-                s_members[members++] = 2 * w + 1;
-            }
-        }
-        s_group_count = groups;
-    }
-    __syncthreads();
-
-    // A unit is eight neighbouring output values: register column c, tiles n .. n + 7, of one lane's position.
-    constexpr int kUnits = 4 * (kNt / 8) * 32;
-    auto finish = [&](const Group& gr, int unit, const float (&v)[8], float m, float l) {
-        const int ln = unit & 31, c = (unit >> 5) & 3, n = (unit >> 7) * 8;
-        const RequestShape s = shape_of(a, gr.request);
-        int64_t token;
-        int head, local;
-        if (!row_of(s, gr.item, (ln >> 2) + 8 * (c >> 1), token, head, local)) return;
-        const float r = l == 0.f ? 0.f : __fdiv_rn(1.f, l);
-        const int column = 2 * (ln & 3) + (c & 1), d = kRowBytes == 128 ? (n / 16) * 128 + 16 * column + (n % 16) : 8 * column;
-        uint4 u;
-        u.x = qtz_dev::pack2(v[0] * r, v[1] * r, T());
-        u.y = qtz_dev::pack2(v[2] * r, v[3] * r, T());
-        u.z = qtz_dev::pack2(v[4] * r, v[5] * r, T());
-        u.w = qtz_dev::pack2(v[6] * r, v[7] * r, T());
-        *reinterpret_cast<uint4*>(static_cast<T*>(a.y) + token * a.y_token_stride + head * a.y_head_stride + d) = u;
-        if (n == 0 && column == 0) write_lse(token, head, m, l);
-    };
-    auto weight = [](float m, float l, float top) { return m == -INFINITY && l == 0.f ? 0.f : ex2(m - top); };
-
-    const int cta_begin = blockIdx.x * cta_share, cta_end = min(cta_begin + cta_share, all);
-    constexpr int64_t kPart = 16 * D + 32;
-    for (int k = 0; k < s_group_count; ++k) {
-        const Group gr = s_groups[k];
-        const bool complete = gr.begin >= cta_begin && gr.end <= cta_end;
-        float* part = a.cta_parts + (static_cast<int64_t>(blockIdx.x) * 2 + (gr.begin >= cta_begin ? 1 : 0)) * kPart;
-        for (int unit = tid; unit < kUnits; unit += kThreads) {
-            const int ln = unit & 31, c = (unit >> 5) & 3, n = (unit >> 7) * 8, row = (ln >> 2) + 8 * (c >> 1);
-            float top = -INFINITY, l = 0.f, v[8] = {};
-            for (int j = 0; j < gr.count; ++j) {
-                const int mb = s_members[gr.first + j];
-                top = fmaxf(top, s_m[mb >> 1][mb & 1][row]);
-            }
-            const float base = top == -INFINITY ? 0.f : top;
-            for (int j = 0; j < gr.count; ++j) {
-                const int mb = s_members[gr.first + j], w = mb >> 1;
-                const float* from = (mb & 1) ? reinterpret_cast<const float*>(smem + w * ring_bytes)
-                                             : a.warp_parts + (static_cast<int64_t>(blockIdx.x) * kWarps + w) * (16 * D);
-                const float wt = weight(s_m[w][mb & 1][row], s_l[w][mb & 1][row], base);
-                l = fmaf(s_l[w][mb & 1][row], wt, l);
-#pragma unroll
-                for (int x = 0; x < 8; ++x) v[x] = fmaf(from[((n + x) * 4 + c) * 32 + ln], wt, v[x]);
-            }
-            if (complete) {
-                finish(gr, unit, v, top, l);
-            } else {
-#pragma unroll
-                for (int x = 0; x < 8; ++x) part[((n + x) * 4 + c) * 32 + ln] = v[x];
-                if (n == 0 && (c & 1) == 0 && (ln & 3) == 0) {
-                    part[16 * D + row] = top;
-                    part[16 * D + 16 + row] = l;
-                }
-            }
-        }
-    }
-
-    // ---- then the items that lie across CTAs: the last to arrive joins all their parts, in order ----
-    for (int k = 0; k < s_group_count; ++k) {
-        const Group gr = s_groups[k];
-        if (gr.begin >= cta_begin && gr.end <= cta_end) continue;
-        const int c0 = gr.begin / cta_share, c1 = (gr.end - 1) / cta_share;
-        __threadfence();
-        __syncthreads();
-        if (tid == 0) {
-            const int arrived = atomicAdd(&a.counters[c0], 1);
-            s_last = arrived == c1 - c0;
-            if (s_last) a.counters[c0] = 0;            // ready for the next call
-        }
-        __syncthreads();
-        if (!s_last) continue;
-        __threadfence();
-        for (int unit = tid; unit < kUnits; unit += kThreads) {
-            const int ln = unit & 31, c = (unit >> 5) & 3, n = (unit >> 7) * 8, row = (ln >> 2) + 8 * (c >> 1);
-            auto part_of = [&](int cta) { return a.cta_parts + (static_cast<int64_t>(cta) * 2 + (cta == c0 ? 1 : 0)) * kPart; };
-            float top = -INFINITY, l = 0.f, v[8] = {};
-            for (int cta = c0; cta <= c1; ++cta) top = fmaxf(top, __ldcg(part_of(cta) + 16 * D + row));
-            const float base = top == -INFINITY ? 0.f : top;
-            for (int cta = c0; cta <= c1; ++cta) {
-                const float* from = part_of(cta);
-                const float pl = __ldcg(from + 16 * D + 16 + row), wt = weight(__ldcg(from + 16 * D + row), pl, base);
-                l = fmaf(pl, wt, l);
-#pragma unroll
-                for (int x = 0; x < 8; ++x) v[x] = fmaf(__ldcg(from + ((n + x) * 4 + c) * 32 + ln), wt, v[x]);
-            }
-            finish(gr, unit, v, top, l);
-        }
+    if (warp == kComputeWarps + 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, kTmemColumns);
     }
 }
 
-int stage_bytes(int head_dim) { return 2 * kTile * head_dim; }
+int ctas_per_sm(int head_dim) { return head_dim == 256 ? 1 : 2; }
 
-template <typename T, int D>
+template <typename T, int D, int kRows>
 qtz_status launch(qtz_ctx* h, AttnArgs& a, const CUtensorMap& km, const CUtensorMap& vm, cudaStream_t st)
 {
-    const size_t fixed = 1024 + static_cast<size_t>(kWarps) * 2 * kBatch * sizeof(TileInfo) + sizeof(uint32_t) * (a.requests + 1);
-    // static shared memory of the kernel is a few KB; what is left after the look-up tables goes to the rings
-    const size_t room = kSmemLimit - 6 * 1024 - fixed;
-    a.stages = static_cast<int32_t>(room / (kWarps * stage_bytes(D)));
-    if (a.stages > kMaxStages) a.stages = kMaxStages;
-    const size_t smem = fixed + static_cast<size_t>(kWarps) * a.stages * stage_bytes(D);
-    QTZ_CUDA(h, cudaFuncSetAttribute(attention_kernel<T, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
-    attention_kernel<T, D><<<h->num_sms, kThreads, smem, st>>>(a, km, vm);
+    constexpr int kN = (3 * kRows + 15) / 16 * 16, kStage = 2 * kTile * D;
+    const int ctas = ctas_per_sm(D);
+    const int fixed = 1024 + kN * 128 + kN * D + static_cast<int>(sizeof(uint32_t)) * (a.requests + 1);
+    const int room = kSmemLimit / ctas - 1024 - 3 * 1024 - fixed;   // 3 KB: the kernel's static shared memory
+    a.stages = room / kStage < kMaxStages ? room / kStage : kMaxStages;
+    if (a.stages < 2) return QTZ_ERR_TOO_LARGE;
+    const int smem = fixed + a.stages * kStage;
+    QTZ_CUDA(h, cudaFuncSetAttribute(attention_kernel<T, D, kRows>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    attention_kernel<T, D, kRows><<<h->num_sms * ctas, kThreads, smem, st>>>(a, km, vm);
     QTZ_LAUNCH_CHECK(h, "attention_kernel");
     return QTZ_OK;
 }
 
-int64_t counters_bytes(const qtz_ctx* h) { return (static_cast<int64_t>(h->num_sms) * 4 + 255) / 256 * 256; }
+template <typename T, int D>
+qtz_status launch_rows(qtz_ctx* h, AttnArgs& a, const CUtensorMap& km, const CUtensorMap& vm, cudaStream_t st)
+{
+    // Query rows of a (request, key/value head) if all requests bring equally many tokens: the smallest tile that takes them
+    // reads the cache once; larger ones only compute unused columns.
+    const int64_t rows = a.group * ((static_cast<int64_t>(a.tokens) + a.requests - 1) / a.requests);
+    if (rows <= 5) return launch<T, D, 5>(h, a, km, vm, st);
+    if (rows <= 10) return launch<T, D, 10>(h, a, km, vm, st);
+    return launch<T, D, 16>(h, a, km, vm, st);
+}
+
+int64_t counters_bytes(const qtz_ctx* h, int head_dim) { return (static_cast<int64_t>(h->num_sms) * ctas_per_sm(head_dim) * 4 + 255) / 256 * 256; }
 
 }  // namespace
 
 extern "C" int64_t qtz_kv_attention_workspace_bytes(qtz_handle h, const qtz_kv_cache* cache)
 {
     if (!h || qtz_kv_check(cache) != QTZ_OK) return 0;
-    const int64_t part = 16 * static_cast<int64_t>(cache->head_dim);
-    return counters_bytes(h) + 4 * h->num_sms * (kWarps * part + 2 * (part + 32));
+    const int d = cache->head_dim;
+    return counters_bytes(h, d) + static_cast<int64_t>(h->num_sms) * ctas_per_sm(d) * 2 * (kMaxRows * d + 2 * kMaxRows) * 4;
 }
 
 extern "C" qtz_status qtz_kv_attention(qtz_handle h, const qtz_kv_cache* cache, const void* q_dev, int64_t q_token_stride,
@@ -713,30 +716,31 @@ extern "C" qtz_status qtz_kv_attention(qtz_handle h, const qtz_kv_cache* cache, 
         return QTZ_ERR_MISALIGNED;
     // rows of the cache and tiles of the longest possible step are counted in 32 bits
     const int64_t rows = static_cast<int64_t>(cache->blocks) * cache->kv_heads * cache->block_tokens;
-    const int64_t group = q_heads / cache->kv_heads, tiles = static_cast<int64_t>(table_width) * cache->block_tokens / kTile;
-    const double bound = static_cast<double>(cache->kv_heads) * static_cast<double>(tiles) * (static_cast<double>(tokens) * group / 16 + requests);
-    if (rows > 0x7fffffff || bound > 2.0e9 || static_cast<int64_t>(table_width) * cache->block_tokens > 0x7fffffff) return QTZ_ERR_TOO_LARGE;
+    const int64_t reach = static_cast<int64_t>(table_width) * cache->block_tokens, group = q_heads / cache->kv_heads;
+    const double bound = static_cast<double>(cache->kv_heads) * static_cast<double>(reach / kTile + 1) * (static_cast<double>(tokens) * group / 5 + requests);
+    if (rows > 0x7fffffff || reach > 0x7fffffff || bound > 2.0e9) return QTZ_ERR_TOO_LARGE;
     qtz_device_guard guard(h->device);
+    int box_rows = 16;                         // the largest box that divides both a block and a tile
+    while (box_rows < kTile && cache->block_tokens % (2 * box_rows) == 0) box_rows *= 2;
     CUtensorMap km, vm;
     const uint32_t row_bytes = cache->head_dim < 128 ? cache->head_dim : 128;
     const uint64_t dims[2] = {static_cast<uint64_t>(cache->head_dim), static_cast<uint64_t>(rows)};
     const uint64_t strides[1] = {static_cast<uint64_t>(cache->head_dim)};
-    const uint32_t box[2] = {row_bytes, kTile};
+    const uint32_t box[2] = {row_bytes, static_cast<uint32_t>(box_rows)};
     if (!qtz_encode_u8_map(&km, cache->k_dev, 2, dims, strides, box, static_cast<int>(row_bytes)) ||
         !qtz_encode_u8_map(&vm, cache->v_dev, 2, dims, strides, box, static_cast<int>(row_bytes)))
         return qtz_cuda_fail(h, cudaErrorInvalidValue, "tensor map of the cache");
-    const int64_t part = 16 * static_cast<int64_t>(cache->head_dim);
-    float* parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace_dev) + counters_bytes(h));
+    float* parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace_dev) + counters_bytes(h, cache->head_dim));
     AttnArgs a{*cache, q_dev, q_token_stride, q_head_stride, q_heads, static_cast<int32_t>(group), starts_dev, lens_dev, requests,
-               static_cast<int32_t>(tokens), table_dev, table_width, scale * 1.44269504f, window < (1 << 30) ? window : 1 << 30, y_dev, y_token_stride, y_head_stride, lse_dev,
-               static_cast<int32_t*>(workspace_dev), parts, parts + h->num_sms * kWarps * part, 0, h->wait_budget, h->status_dev};
+               static_cast<int32_t>(tokens), table_dev, table_width, scale * 1.44269504f, window < (1 << 30) ? window : 1 << 30, y_dev,
+               y_token_stride, y_head_stride, lse_dev, static_cast<int32_t*>(workspace_dev), parts, 0, box_rows, h->wait_budget, h->status_dev};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (ftype == QTZ_F16) {
-        if (cache->head_dim == 64) return launch<__half, 64>(h, a, km, vm, st);
-        if (cache->head_dim == 128) return launch<__half, 128>(h, a, km, vm, st);
-        return launch<__half, 256>(h, a, km, vm, st);
+        if (cache->head_dim == 64) return launch_rows<__half, 64>(h, a, km, vm, st);
+        if (cache->head_dim == 128) return launch_rows<__half, 128>(h, a, km, vm, st);
+        return launch_rows<__half, 256>(h, a, km, vm, st);
     }
-    if (cache->head_dim == 64) return launch<__nv_bfloat16, 64>(h, a, km, vm, st);
-    if (cache->head_dim == 128) return launch<__nv_bfloat16, 128>(h, a, km, vm, st);
-    return launch<__nv_bfloat16, 256>(h, a, km, vm, st);
+    if (cache->head_dim == 64) return launch_rows<__nv_bfloat16, 64>(h, a, km, vm, st);
+    if (cache->head_dim == 128) return launch_rows<__nv_bfloat16, 128>(h, a, km, vm, st);
+    return launch_rows<__nv_bfloat16, 256>(h, a, km, vm, st);
 }

@@ -360,4 +360,26 @@ __device__ __forceinline__ uint64_t make_sliding_desc(uint32_t smem_addr)
     return d;                                                       // layout field 0: no swizzle
 }
 
+// Descriptor of an operand stored the other way round: `depth` rows (the contraction index) of row_bytes (64 or 128)
+// contiguous bytes along M or N, with the TMA swizzle of the same width.  Eight depth rows form one swizzle atom, the next
+// eight lie 8 * row_bytes bytes on; the leading offset is 0: an operand wider than an atom meets the same atom again.
+__device__ __forceinline__ uint64_t make_mnmajor_desc(uint32_t smem_addr, uint32_t row_bytes)
+{
+    const uint64_t layout = row_bytes == 128 ? 2ull : 4ull;
+    uint64_t d = 0;
+    d |= static_cast<uint64_t>((smem_addr & 0x3ffffu) >> 4);        // start address, 16-byte units
+    d |= static_cast<uint64_t>((8u * row_bytes) >> 4) << 32;        // stride offset between groups of eight depth rows
+    d |= static_cast<uint64_t>(1) << 46;                            // descriptor version of this architecture
+    d |= layout << 61;
+    return d;
+}
+
+// Largest value of a warp's lanes; NaN is passed over.
+__device__ __forceinline__ float redux_max(float v)
+{
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+
 }  // namespace qtz_ptx
