@@ -42,7 +42,8 @@ constexpr int kComputeThreads = 32 * kComputeWarps;
 constexpr int kThreads = kComputeThreads + 64;   // + one warp for TMA, one for the matrix instructions
 constexpr int kMaxRows = 16;
 constexpr int kMaxStages = 6;
-constexpr int kTmemColumns = 256;          // S (two buffers), O (two halves of a head of 256), 64 columns each
+constexpr int kMaxBoxes = 8;
+constexpr int kFanIn = 8;                  // parts that one CTA joins; more are joined in two steps
 constexpr int kSmemLimit = 227 * 1024;     // of an SM, each CTA costing 1 KB more than it asks for
 
 struct AttnArgs {
@@ -59,9 +60,9 @@ struct AttnArgs {
     void* y;
     int64_t y_token_stride, y_head_stride;
     float* lse;
-    int32_t* counters;                     // [CTAs] arrivals at the item that begins in a CTA and ends in a later one
+    int32_t* counters;                     // [CTAs][2] arrivals of parts at a group, [CTAs] of groups at an item (see the joining)
     float* parts;                          // [CTAs][2][kMaxRows * D + 2 kMaxRows]: sums, maxima, denominators
-    int32_t stages, box_rows;
+    int32_t stages, box_shift;             // tokens of a box: 1 << box_shift
     int64_t wait_budget;
     int32_t* status;
 };
@@ -184,21 +185,25 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
     constexpr int kN = (3 * kRows + 15) / 16 * 16;     // operand columns: digit * kRows + row
     constexpr int kBox = kTile * kRowBytes;            // K or V of one tile and half
     constexpr int kStage = 2 * kHalves * kBox;
+    constexpr int kColumns = kN == 48 ? 64 : kN;       // of tensor memory: two buffers of S, two of each half of O
+    constexpr int kTmemColumns = (2 + 2 * kHalves) * kColumns <= 64 ? 64 : (2 + 2 * kHalves) * kColumns <= 128 ? 128 :
+                                 (2 + 2 * kHalves) * kColumns <= 256 ? 256 : 512;
     constexpr int kPart = kMaxRows * D + 2 * kMaxRows;
     constexpr uint32_t kMulK = (2u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(kN >> 3) << 17) | (static_cast<uint32_t>(kTile >> 4) << 24);
     constexpr uint32_t kMulV = (2u << 4) | (1u << 7) | (0u << 10) | (1u << 15) | (static_cast<uint32_t>(kN >> 3) << 17) | (128u >> 4 << 24);
 
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_sfull[2], s_pfull, s_ofull, s_qfull, s_drain;
+    __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_sfull[2], s_pfull[2], s_ofull[2], s_qfull, s_drain;
     __shared__ __align__(16) float s_max[2][kMaxRows][kComputeWarps], s_sum[kMaxRows][kComputeWarps];
     __shared__ __align__(16) ItemInfo s_item[2];
+    __shared__ float2 s_scales[kMaxStages][kMaxBoxes];   // (k, v) of each box; v = 0: there is none
     __shared__ uint32_t s_scan[kThreads / 32], s_tmem;
     __shared__ int s_last;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* const smem = smem_raw + (base - smem_u32(smem_raw));
-    const uint32_t off_p = a.stages * kStage, off_q = off_p + kN * 128, off_prefix = off_q + kHalves * kN * kRowBytes;
+    const uint32_t off_p = a.stages * kStage, off_q = off_p + 2 * kN * 128, off_prefix = off_q + kHalves * kN * kRowBytes;
     uint32_t* const prefix = reinterpret_cast<uint32_t*>(smem + off_prefix);
 
     if (tid == 0) {
@@ -210,9 +215,11 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         }
         mbar_init(smem_u32(&s_sfull[0]), 1);
         mbar_init(smem_u32(&s_sfull[1]), 1);
-        mbar_init(smem_u32(&s_ofull), 1);
+        mbar_init(smem_u32(&s_ofull[0]), 1);
+        mbar_init(smem_u32(&s_ofull[1]), 1);
         mbar_init(smem_u32(&s_drain), 1);
-        mbar_init(smem_u32(&s_pfull), kComputeWarps);
+        mbar_init(smem_u32(&s_pfull[0]), kComputeWarps);
+        mbar_init(smem_u32(&s_pfull[1]), kComputeWarps);
         mbar_init(smem_u32(&s_qfull), kComputeWarps);
         fence_barrier_init();
     }
@@ -265,39 +272,77 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
     if (count > 0) cur.seek(a, prefix, t0);
 
     if (count > 0 && warp == kComputeWarps) {
-        // ======== producer: lane j brings box j (box_rows tokens) of the tile ========
-        const int boxes = kTile / a.box_rows;
-        // row of the box in the [blocks * heads * block_tokens] view, -1 if there is nothing to bring
-        auto look_up = [&](const Cursor<kRows>& c) {
-            const int pos = c.pos() + lane * a.box_rows;
+        // ======== producer: lane j brings box j of the tile, and its scales ========
+        // Three tiles are under way: table entries of tile i + 2, scales of tile i + 1, the copy of tile i, so that no look-up
+        // is waited for.
+        const int box_rows = 1 << a.box_shift, boxes = kTile >> a.box_shift;
+        auto entry_of = [&](const Cursor<kRows>& c, int& head, int& offset) {
+            const int pos = c.pos() + lane * box_rows;
+            head = c.head();
+            offset = 0;
             if (lane >= boxes || pos >= c.s.limit) return -1;
-            const int id = a.table[static_cast<int64_t>(c.request) * a.width + pos / a.c.block_tokens];
-            if (id < 0 || id >= a.c.blocks) return -1;
-            return static_cast<int>((static_cast<int64_t>(id) * a.c.kv_heads + c.head()) * a.c.block_tokens + pos % a.c.block_tokens);
+            const int j = pos / a.c.block_tokens;
+            offset = pos - j * a.c.block_tokens;
+            return a.table[static_cast<int64_t>(c.request) * a.width + j];
         };
-        int row = look_up(cur), i = 0, stage = 0, round = 0;
-        for (; i < count; ++i) {
-            int ahead = -1;
-            if (i + 1 < count) {
-                cur.next(a, prefix);
-                ahead = look_up(cur);                  // in flight while this tile is issued
+        // Scales lie in [2^-100, 2^122] here (the least is QTZ_KV_MIN_SCALE; no 16-bit value gives more than 2^121), so
+        // that their logarithms and inverses are ordinary numbers.
+        auto clamped = [](float v) { return fminf(fmaxf(v, QTZ_KV_MIN_SCALE), 5.3169120e36f); };
+        int id1 = -1, head1 = 0, off1 = 0, id2, head2, off2, row0 = -1, row1 = -1, limit1 = 0, limit2;
+        float ks0 = 0.f, vs0 = 0.f, ks1 = 0.f, vs1 = 0.f;
+        auto resolve = [&](int id, int head, int offset, int wanted, float& ks, float& vs) {
+            if (!wanted) return -1;
+            if (id < 0 || id >= a.c.blocks) {
+                qtz_dev::report_invalid(a.status, QTZ_SITE_KV_ATTENTION);
+                return -1;
             }
+            const int64_t bh = static_cast<int64_t>(id) * a.c.kv_heads + head;
+            ks = a.c.k_scale_dev[bh];
+            vs = a.c.v_scale_dev[bh];
+            return static_cast<int>(bh * a.c.block_tokens + offset);
+        };
+        auto wanted = [&](const Cursor<kRows>& c) { return lane < boxes && c.pos() + lane * box_rows < c.s.limit ? 1 : 0; };
+        id1 = entry_of(cur, head1, off1);
+        row0 = resolve(id1, head1, off1, wanted(cur), ks0, vs0);
+        if (count > 1) {
+            cur.next(a, prefix);
+            id1 = entry_of(cur, head1, off1);
+            limit1 = wanted(cur);
+        }
+        int i = 0, stage = 0, round = 0;
+        for (; i < count; ++i) {
+            id2 = -1, head2 = 0, off2 = 0, limit2 = 0;
+            if (i + 2 < count) {
+                cur.next(a, prefix);
+                id2 = entry_of(cur, head2, off2);
+                limit2 = wanted(cur);
+            }
+            row1 = -1;
+            if (i + 1 < count) row1 = resolve(id1, head1, off1, limit1, ks1, vs1);
             if (round > 0 && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&s_empty[stage]), (round - 1) & 1, a.wait_budget))) {
                 timed_out();
                 break;
             }
             const uint32_t bar = smem_u32(&s_full[stage]), dst = base + stage * kStage;
-            const int have = __popc(__ballot_sync(0xffffffffu, row >= 0));
-            if (lane == 0) mbar_arrive_expect_tx(bar, have * a.box_rows * 2 * D);
+            if (lane < boxes) s_scales[stage][lane] = row0 >= 0 ? make_float2(clamped(ks0), clamped(vs0)) : make_float2(0.f, 0.f);
+            const int have = __popc(__ballot_sync(0xffffffffu, row0 >= 0));
             __syncwarp();
-            if (row >= 0) {
-                const uint32_t at = dst + lane * a.box_rows * kRowBytes;
+            if (lane == 0) mbar_arrive_expect_tx(bar, have * box_rows * 2 * D);
+            __syncwarp();
+            if (row0 >= 0) {
+                const uint32_t at = dst + lane * box_rows * kRowBytes;
 #pragma unroll
-                for (int hh = 0; hh < kHalves; ++hh) tma_load_2d(at + hh * kBox, &k_map, bar, hh * 128, row);
+                for (int hh = 0; hh < kHalves; ++hh) tma_load_2d(at + hh * kBox, &k_map, bar, hh * 128, row0);
 #pragma unroll
-                for (int hh = 0; hh < kHalves; ++hh) tma_load_2d(at + (kHalves + hh) * kBox, &v_map, bar, hh * 128, row);
+                for (int hh = 0; hh < kHalves; ++hh) tma_load_2d(at + (kHalves + hh) * kBox, &v_map, bar, hh * 128, row0);
             }
-            row = ahead;
+            row0 = row1;
+            ks0 = ks1;
+            vs0 = vs1;
+            id1 = id2;
+            head1 = head2;
+            off1 = off2;
+            limit1 = limit2;
             if (++stage == a.stages) {
                 stage = 0;
                 ++round;
@@ -324,7 +369,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                 for (int hh = 0; hh < kHalves; ++hh)
 #pragma unroll
                     for (int j = 0; j < kRowBytes / 32; ++j)
-                        mma_i8(tmem + (i & 1) * 64, make_kmajor_desc(base + stage * kStage + hh * kBox, kRowBytes) + 2 * j,
+                        mma_i8(tmem + (i & 1) * kColumns, make_kmajor_desc(base + stage * kStage + hh * kBox, kRowBytes) + 2 * j,
                                make_kmajor_desc(base + off_q + hh * kN * kRowBytes, kRowBytes) + 2 * j, kMulK, hh + j > 0);
                 mma_commit(smem_u32(&s_sfull[i & 1]));
             }
@@ -336,7 +381,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                 cur.next(a, prefix);
                 multiply_keys(i + 1, cur);
             }
-            ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_pfull), i & 1, a.wait_budget));
+            ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_pfull[i & 1]), (i >> 1) & 1, a.wait_budget));
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
@@ -345,9 +390,9 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                 for (int hh = 0; hh < kHalves; ++hh)
 #pragma unroll
                     for (int j = 0; j < kTile / 32; ++j)
-                        mma_i8(tmem + 128 + hh * 64, make_mnmajor_desc(v + hh * kBox + j * 32 * kRowBytes, kRowBytes),
-                               make_kmajor_desc(base + off_p, 128) + 2 * j, kMulV, j > 0);
-                mma_commit(smem_u32(&s_ofull));
+                        mma_i8(tmem + (2 + (i & 1) * kHalves + hh) * kColumns, make_mnmajor_desc(v + hh * kBox + j * 32 * kRowBytes, kRowBytes),
+                               make_kmajor_desc(base + off_p + (i & 1) * kN * 128, 128) + 2 * j, kMulV, j > 0);
+                mma_commit(smem_u32(&s_ofull[i & 1]));
                 mma_commit(smem_u32(&s_empty[i % a.stages]));
             }
             __syncwarp();
@@ -453,28 +498,11 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
             if (lane == 0) mbar_arrive(smem_u32(&s_qfull));
         };
 
-        // block * heads + head of this thread's token, -1 if it has none
-        auto token_block = [&](const Cursor<kRows>& c) {
-            const int pos = c.pos() + tid;
-            if (pos >= c.s.limit) return static_cast<int64_t>(-1);
-            const int id = a.table[static_cast<int64_t>(c.request) * a.width + pos / a.c.block_tokens];
-            if (id < 0 || id >= a.c.blocks) {
-                qtz_dev::report_invalid(a.status, QTZ_SITE_KV_ATTENTION);
-                return static_cast<int64_t>(-1);
-            }
-            return static_cast<int64_t>(id) * a.c.kv_heads + c.head();
-        };
-        // Scales lie in [2^-100, 2^122] here (the least is QTZ_KV_MIN_SCALE; no 16-bit value gives more than 2^121), so
-        // that their logarithms and inverses are ordinary numbers.
-        auto scale_of = [&](const float* p, int64_t bh) { return bh < 0 ? 1.f : fminf(fmaxf(p[bh], QTZ_KV_MIN_SCALE), 5.3169120e36f); };
-
         int items = 0;
         load_queries(cur, 0);
-        int64_t bh = token_block(cur);
-        float ks = scale_of(a.c.k_scale_dev, bh), vs = scale_of(a.c.v_scale_dev, bh);
-        Cursor<kRows> ahead = cur;
-        float m[kRows], l[kRows], acc[kHalves][kRows];
-        int seg_first = cur.k;
+        float m[kRows], l[kRows], acc[kHalves][kRows], keep[kRows];
+        int seg_first = cur.k, stage = 0, round = 0;
+        bool pending = false;                          // O of the tile before is still to be taken
 
         auto reset = [&]() {
 #pragma unroll
@@ -495,29 +523,42 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
             if (d == 0 && a.lse) a.lse[it.lse[r]] = ll == 0.f ? -INFINITY : (mm + log2f(ll)) * 0.693147181f;
         };
 
+        auto take_sums = [&](int i) {
+            wait(s_ofull[i & 1], (i >> 1) & 1);
+            tc_fence_after();
+#pragma unroll
+            for (int hh = 0; hh < kHalves; ++hh) {
+                uint32_t o[kN];
+                load_columns<kN>(tmem + (2 + (i & 1) * kHalves + hh) * kColumns + (static_cast<uint32_t>(warp) << 21), o);
+#pragma unroll
+                for (int r = 0; r < kRows; ++r)
+                    acc[hh][r] = fmaf(acc[hh][r], keep[r], join_digits(o[r], o[kRows + r], o[2 * kRows + r]));
+            }
+        };
+
         for (int i = 0; i < count; ++i) {
             const ItemInfo& it = s_item[items & 1];
             const int pos0 = cur.pos(), pos = pos0 + tid;
             const bool last = cur.k == cur.s.tiles - 1, more = i + 1 < count;
-            // the next tile's block, in flight during this one
-            int64_t bh_next = -1;
-            if (more) {
-                ahead.next(a, prefix);
-                bh_next = token_block(ahead);
-            }
             if (i == 0 || cur.k == 0) wait(s_qfull, items & 1);
+            wait(s_full[stage], round & 1);
+            const float2 scales = s_scales[stage][tid >> a.box_shift];
+            if (++stage == a.stages) {
+                stage = 0;
+                ++round;
+            }
             wait(s_sfull[i & 1], (i >> 1) & 1);
             tc_fence_after();
             float x[kRows];
             {
                 uint32_t s[kN];
-                load_columns<kN>(tmem + (i & 1) * 64 + (static_cast<uint32_t>(warp) << 21), s);
-                const float lv = lg2(vs);
+                load_columns<kN>(tmem + (i & 1) * kColumns + (static_cast<uint32_t>(warp) << 21), s);
+                const float lv = lg2(scales.y);
 #pragma unroll
                 for (int r = 0; r < kRows; ++r)
-                    x[r] = fmaf(join_digits(s[r], s[kRows + r], s[2 * kRows + r]), it.factor[r] * ks, lv);
+                    x[r] = fmaf(join_digits(s[r], s[kRows + r], s[2 * kRows + r]), it.factor[r] * scales.x, lv);
             }
-            if (bh < 0) {
+            if (scales.y == 0.f) {
 #pragma unroll
                 for (int r = 0; r < kRows; ++r) x[r] = -INFINITY;
             } else if (pos0 < it.full_lo || pos0 + kTile > it.full_hi) {
@@ -532,48 +573,46 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
             }
             ok = named_barrier_and(1, kComputeThreads, ok);
             if (!ok) break;
-            const float inv = __fdividef(1.f, vs);
-            float keep[kRows];
+            const float inv = scales.y == 0.f ? 0.f : __fdividef(1.f, scales.y);
+            float fresh[kRows];
 #pragma unroll
             for (int r = 0; r < kRows; ++r) {
                 const float4 t = *reinterpret_cast<const float4*>(s_max[i & 1][r]);
                 const float top = fmaxf(fmaxf(fmaxf(t.x, t.y), fmaxf(t.z, t.w)), m[r]);
                 const float origin = top == -INFINITY ? 0.f : top;
-                keep[r] = ex2(m[r] - origin);
+                fresh[r] = ex2(m[r] - origin);
                 m[r] = top;
                 const float w = ex2(x[r] - origin);
-                l[r] = fmaf(w, inv, l[r] * keep[r]);
+                l[r] = fmaf(w, inv, l[r] * fresh[r]);
                 // w in [0, 1]: the mantissa of w + 2 is w in units of 2^-22, its bytes are the digits
                 const uint32_t bits = __float_as_uint(w + 2.f);
 #pragma unroll
                 for (int g = 0; g < 3; ++g) {
                     const int n = g * kRows + r;
-                    smem[off_p + n * 128 + (((tid >> 4) ^ (n & 7)) << 4) + (tid & 15)] = static_cast<uint8_t>(bits >> (8 * g));
+                    smem[off_p + (i & 1) * kN * 128 + n * 128 + (((tid >> 4) ^ (n & 7)) << 4) + (tid & 15)] = static_cast<uint8_t>(bits >> (8 * g));
                 }
             }
             tc_fence_before();
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&s_pfull));
+            if (lane == 0) mbar_arrive(smem_u32(&s_pfull[i & 1]));
 
-            // while O is under way: the next tile's scales, the next item's queries
-            bh = bh_next;
-            ks = scale_of(a.c.k_scale_dev, bh);
-            vs = scale_of(a.c.v_scale_dev, bh);
-            if (last && more) load_queries(ahead, (items + 1) & 1);
-
-            wait(s_ofull, i & 1);
-            tc_fence_after();
+            // O of the tile before: its product ran beside this tile's softmax
+            if (pending) take_sums(i - 1);
 #pragma unroll
-            for (int hh = 0; hh < kHalves; ++hh) {
-                uint32_t o[kN];
-                load_columns<kN>(tmem + 128 + hh * 64 + (static_cast<uint32_t>(warp) << 21), o);
-#pragma unroll
-                for (int r = 0; r < kRows; ++r)
-                    acc[hh][r] = fmaf(acc[hh][r], keep[r], join_digits(o[r], o[kRows + r], o[2 * kRows + r]));
-            }
+            for (int r = 0; r < kRows; ++r) keep[r] = fresh[r];
+            pending = true;
 
-            if (last || !more) {                       // the end of the item, or of this CTA's part of it
+            if (!last && more) {
+                ++cur.k;
+            } else {                                   // the end of the item, or of this CTA's part of it
+                Cursor<kRows> ahead = cur;
+                if (more) {
+                    ahead.next(a, prefix);
+                    load_queries(ahead, (items + 1) & 1);
+                }
+                take_sums(i);
+                pending = false;
 #pragma unroll
                 for (int r = 0; r < kRows; ++r) {
 #pragma unroll
@@ -606,45 +645,88 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                     }
                 }
                 if (!whole) {
+                    // Parts of CTAs c0 .. c1.  The last of each group of kFanIn neighbours to arrive joins them into the place of
+                    // the group's first; with several groups, the last of those joins the groups.  Always in the same order.
                     const int c0 = static_cast<int>(cur.begin) / share, c1 = static_cast<int>(cur.begin + cur.s.tiles - 1) / share;
-                    __threadfence();
-                    named_barrier(1, kComputeThreads);
-                    if (tid == 0) {
-                        const int arrived = atomicAdd(&a.counters[c0], 1);
-                        s_last = arrived == c1 - c0;
-                        if (s_last) a.counters[c0] = 0;    // ready for the next call
-                    }
-                    named_barrier(1, kComputeThreads);
-                    if (s_last) {
+                    auto part_of = [&](int cta) { return a.parts + (static_cast<int64_t>(cta) * 2 + (cta == c0 ? 1 : 0)) * kPart; };
+                    auto arrives_last = [&](int32_t* counter, int others) {
                         __threadfence();
-                        auto part_of = [&](int cta) { return a.parts + (static_cast<int64_t>(cta) * 2 + (cta == c0 ? 1 : 0)) * kPart; };
-                        if (D >= 128 || tid < D)
-                            for (int r = 0; r < kRows; ++r) {
-                                if (it.out[r] < 0) continue;
-                                float top = -INFINITY;
-#pragma unroll 8
-                                for (int cta = c0; cta <= c1; ++cta) top = fmaxf(top, __ldcg(part_of(cta) + kMaxRows * D + r));
-                                const float origin = top == -INFINITY ? 0.f : top;
-                                float sum = 0.f, v[kHalves] = {};
-#pragma unroll 8
-                                for (int cta = c0; cta <= c1; ++cta) {
-                                    const float* from = part_of(cta);
-                                    const float pm = __ldcg(from + kMaxRows * D + r), pl = __ldcg(from + kMaxRows * D + kMaxRows + r);
-                                    const float wt = pm == -INFINITY && pl == 0.f ? 0.f : ex2(pm - origin);
-                                    sum = fmaf(pl, wt, sum);
-#pragma unroll
-                                    for (int hh = 0; hh < kHalves; ++hh) v[hh] = fmaf(__ldcg(from + r * D + hh * 128 + tid), wt, v[hh]);
-                                }
-                                write_row(it, r, top, sum, v, tid);
-                            }
                         named_barrier(1, kComputeThreads);
+                        if (tid == 0) {
+                            const int arrived = atomicAdd(counter, 1);
+                            s_last = arrived == others;
+                            if (arrived == others) *counter = 0;           // ready for the next call
+                        }
+                        named_barrier(1, kComputeThreads);
+                        const bool yes = s_last;
+                        __threadfence();
+                        return yes;
+                    };
+                    // joins the parts of CTAs from, from + step, .. (at most kFanIn at a time are in flight)
+                    float sum[kRows];
+                    auto join = [&](int from, int to, int step) {
+#pragma unroll
+                        for (int r = 0; r < kRows; ++r) {
+                            m[r] = -INFINITY;
+                            sum[r] = 0.f;
+#pragma unroll
+                            for (int hh = 0; hh < kHalves; ++hh) acc[hh][r] = 0.f;
+                        }
+                        for (int cta = from; cta <= to; cta += step) {
+                            const float* p = part_of(cta);
+#pragma unroll
+                            for (int r = 0; r < kRows; ++r) m[r] = fmaxf(m[r], __ldcg(p + kMaxRows * D + r));
+                        }
+#pragma unroll 2
+                        for (int cta = from; cta <= to; cta += step) {
+                            const float* p = part_of(cta);
+#pragma unroll
+                            for (int r = 0; r < kRows; ++r) {
+                                const float pm = __ldcg(p + kMaxRows * D + r), pl = __ldcg(p + kMaxRows * D + kMaxRows + r);
+                                const float wt = pm == -INFINITY && pl == 0.f ? 0.f : ex2(pm - (m[r] == -INFINITY ? 0.f : m[r]));
+                                sum[r] = fmaf(pl, wt, sum[r]);
+#pragma unroll
+                                for (int hh = 0; hh < kHalves; ++hh)
+                                    acc[hh][r] = fmaf(D >= 128 || tid < D ? __ldcg(p + r * D + hh * 128 + tid) : 0.f, wt, acc[hh][r]);
+                            }
+                        }
+                    };
+                    const int me = static_cast<int>(blockIdx.x), groups = (c1 - c0) / kFanIn + 1, first = me - (me - c0) % kFanIn;
+                    bool mine = arrives_last(a.counters + 2 * first + (first == c0 ? 1 : 0), min(first + kFanIn - 1, c1) - first);
+                    if (mine) {
+                        join(first, min(first + kFanIn - 1, c1), 1);
+                        if (groups > 1) {
+                            float* to = part_of(first);
+                            named_barrier(1, kComputeThreads);                 // every thread has read the maxima
+#pragma unroll
+                            for (int r = 0; r < kRows; ++r) {
+                                if (D >= 128 || tid < D)
+#pragma unroll
+                                    for (int hh = 0; hh < kHalves; ++hh) to[r * D + hh * 128 + tid] = acc[hh][r];
+                                if (tid == 0) {
+                                    to[kMaxRows * D + r] = m[r];
+                                    to[kMaxRows * D + kMaxRows + r] = sum[r];
+                                }
+                            }
+                            mine = arrives_last(a.counters + 2 * gridDim.x + c0, groups - 1);
+                            if (mine) join(c0, c1, kFanIn);
+                        }
                     }
+                    if (mine && (D >= 128 || tid < D))
+#pragma unroll
+                        for (int r = 0; r < kRows; ++r) {
+                            float v[kHalves];
+#pragma unroll
+                            for (int hh = 0; hh < kHalves; ++hh) v[hh] = acc[hh][r];
+                            write_row(it, r, m[r], sum[r], v, tid);
+                        }
+                    named_barrier(1, kComputeThreads);
                 }
                 reset();
                 seg_first = 0;
+                ++items;
+                cur = ahead;
             }
-            if (last) ++items;
-            cur = ahead;
         }
         if (!ok) timed_out();
     }
@@ -664,7 +746,7 @@ qtz_status launch(qtz_ctx* h, AttnArgs& a, const CUtensorMap& km, const CUtensor
 {
     constexpr int kN = (3 * kRows + 15) / 16 * 16, kStage = 2 * kTile * D;
     const int ctas = ctas_per_sm(D);
-    const int fixed = 1024 + kN * 128 + kN * D + static_cast<int>(sizeof(uint32_t)) * (a.requests + 1);
+    const int fixed = 1024 + 2 * kN * 128 + kN * D + static_cast<int>(sizeof(uint32_t)) * (a.requests + 1);
     const int room = kSmemLimit / ctas - 1024 - 3 * 1024 - fixed;   // 3 KB: the kernel's static shared memory
     a.stages = room / kStage < kMaxStages ? room / kStage : kMaxStages;
     if (a.stages < 2) return QTZ_ERR_TOO_LARGE;
@@ -686,7 +768,7 @@ qtz_status launch_rows(qtz_ctx* h, AttnArgs& a, const CUtensorMap& km, const CUt
     return launch<T, D, 16>(h, a, km, vm, st);
 }
 
-int64_t counters_bytes(const qtz_ctx* h, int head_dim) { return (static_cast<int64_t>(h->num_sms) * ctas_per_sm(head_dim) * 4 + 255) / 256 * 256; }
+int64_t counters_bytes(const qtz_ctx* h, int head_dim) { return (static_cast<int64_t>(h->num_sms) * ctas_per_sm(head_dim) * 3 * 4 + 255) / 256 * 256; }
 
 }  // namespace
 
@@ -720,20 +802,20 @@ extern "C" qtz_status qtz_kv_attention(qtz_handle h, const qtz_kv_cache* cache, 
     const double bound = static_cast<double>(cache->kv_heads) * static_cast<double>(reach / kTile + 1) * (static_cast<double>(tokens) * group / 5 + requests);
     if (rows > 0x7fffffff || reach > 0x7fffffff || bound > 2.0e9) return QTZ_ERR_TOO_LARGE;
     qtz_device_guard guard(h->device);
-    int box_rows = 16;                         // the largest box that divides both a block and a tile
-    while (box_rows < kTile && cache->block_tokens % (2 * box_rows) == 0) box_rows *= 2;
+    int box_shift = 4;                         // the largest box that divides both a block and a tile
+    while ((1 << box_shift) < kTile && cache->block_tokens % (2 << box_shift) == 0) ++box_shift;
     CUtensorMap km, vm;
     const uint32_t row_bytes = cache->head_dim < 128 ? cache->head_dim : 128;
     const uint64_t dims[2] = {static_cast<uint64_t>(cache->head_dim), static_cast<uint64_t>(rows)};
     const uint64_t strides[1] = {static_cast<uint64_t>(cache->head_dim)};
-    const uint32_t box[2] = {row_bytes, static_cast<uint32_t>(box_rows)};
+    const uint32_t box[2] = {row_bytes, 1u << box_shift};
     if (!qtz_encode_u8_map(&km, cache->k_dev, 2, dims, strides, box, static_cast<int>(row_bytes)) ||
         !qtz_encode_u8_map(&vm, cache->v_dev, 2, dims, strides, box, static_cast<int>(row_bytes)))
         return qtz_cuda_fail(h, cudaErrorInvalidValue, "tensor map of the cache");
     float* parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace_dev) + counters_bytes(h, cache->head_dim));
     AttnArgs a{*cache, q_dev, q_token_stride, q_head_stride, q_heads, static_cast<int32_t>(group), starts_dev, lens_dev, requests,
                static_cast<int32_t>(tokens), table_dev, table_width, scale * 1.44269504f, window < (1 << 30) ? window : 1 << 30, y_dev,
-               y_token_stride, y_head_stride, lse_dev, static_cast<int32_t*>(workspace_dev), parts, 0, box_rows, h->wait_budget, h->status_dev};
+               y_token_stride, y_head_stride, lse_dev, static_cast<int32_t*>(workspace_dev), parts, 0, box_shift, h->wait_budget, h->status_dev};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (ftype == QTZ_F16) {
         if (cache->head_dim == 64) return launch_rows<__half, 64>(h, a, km, vm, st);
