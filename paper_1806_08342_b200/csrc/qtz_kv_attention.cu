@@ -137,6 +137,11 @@ __device__ __forceinline__ float lg2(float v)
     return r;
 }
 
+__device__ __forceinline__ void st_shared_u8(uint32_t addr, uint32_t v)
+{
+    asm volatile("st.shared.u8 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
 // d_2 65536 + d_1 256 + d_0 for digit sums below 2^22
 __device__ __forceinline__ float join_digits(uint32_t d0, uint32_t d1, uint32_t d2)
 {
@@ -182,6 +187,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
 {
     constexpr int kHalves = D > 128 ? 2 : 1;           // boxes along a row of the cache
     constexpr int kRowBytes = D < 128 ? D : 128;
+    constexpr int kRowsUp = (kRows + 3) / 4 * 4;
     constexpr int kN = (3 * kRows + 15) / 16 * 16;     // operand columns: digit * kRows + row
     constexpr int kBox = kTile * kRowBytes;            // K or V of one tile and half
     constexpr int kStage = 2 * kHalves * kBox;
@@ -194,7 +200,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
 
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_sfull[2], s_pfull[2], s_ofull[2], s_qfull, s_drain;
-    __shared__ __align__(16) float s_max[2][kMaxRows][kComputeWarps], s_sum[kMaxRows][kComputeWarps];
+    __shared__ __align__(16) float s_max[2][kComputeWarps][kMaxRows], s_sum[kMaxRows][kComputeWarps];
     __shared__ __align__(16) ItemInfo s_item[2];
     __shared__ float2 s_scales[kMaxStages][kMaxBoxes];   // (k, v) of each box; v = 0: there is none
     __shared__ uint32_t s_scan[kThreads / 32], s_tmem;
@@ -566,32 +572,47 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                 for (int r = 0; r < kRows; ++r)
                     if (pos < it.begin[r] || pos >= it.end[r]) x[r] = -INFINITY;
             }
+            float top[kRowsUp];
 #pragma unroll
-            for (int r = 0; r < kRows; ++r) {
-                const float top = redux_max(x[r]);
-                if (lane == 0) s_max[i & 1][r][warp] = top;
-            }
+            for (int r = 0; r < kRowsUp; ++r) top[r] = r < kRows ? redux_max(x[r]) : -INFINITY;
+            if (lane == 0)
+#pragma unroll
+                for (int r = 0; r < kRowsUp; r += 4)
+                    *reinterpret_cast<float4*>(&s_max[i & 1][warp][r]) = make_float4(top[r], top[r + 1], top[r + 2], top[r + 3]);
             ok = named_barrier_and(1, kComputeThreads, ok);
             if (!ok) break;
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) top[r] = m[r];
+#pragma unroll
+            for (int w = 0; w < kComputeWarps; ++w)
+#pragma unroll
+                for (int r = 0; r < kRowsUp; r += 4) {
+                    const float4 t = *reinterpret_cast<const float4*>(&s_max[i & 1][w][r]);
+                    top[r] = fmaxf(top[r], t.x);
+                    top[r + 1] = fmaxf(top[r + 1], t.y);
+                    top[r + 2] = fmaxf(top[r + 2], t.z);
+                    top[r + 3] = fmaxf(top[r + 3], t.w);
+                }
             const float inv = scales.y == 0.f ? 0.f : __fdividef(1.f, scales.y);
             float fresh[kRows];
+            uint32_t bits[kRows];
 #pragma unroll
             for (int r = 0; r < kRows; ++r) {
-                const float4 t = *reinterpret_cast<const float4*>(s_max[i & 1][r]);
-                const float top = fmaxf(fmaxf(fmaxf(t.x, t.y), fmaxf(t.z, t.w)), m[r]);
-                const float origin = top == -INFINITY ? 0.f : top;
+                const float origin = top[r] == -INFINITY ? 0.f : top[r];
                 fresh[r] = ex2(m[r] - origin);
-                m[r] = top;
+                m[r] = top[r];
                 const float w = ex2(x[r] - origin);
                 l[r] = fmaf(w, inv, l[r] * fresh[r]);
-                // w in [0, 1]: the mantissa of w + 2 is w in units of 2^-22, its bytes are the digits
-                const uint32_t bits = __float_as_uint(w + 2.f);
+                bits[r] = __float_as_uint(w + 2.f);    // w in [0, 1]: the mantissa is w in units of 2^-22, its bytes are the digits
+            }
+            const uint32_t to = base + off_p + (i & 1) * kN * 128;
+#pragma unroll
+            for (int r = 0; r < kRows; ++r)
 #pragma unroll
                 for (int g = 0; g < 3; ++g) {
                     const int n = g * kRows + r;
-                    smem[off_p + (i & 1) * kN * 128 + n * 128 + (((tid >> 4) ^ (n & 7)) << 4) + (tid & 15)] = static_cast<uint8_t>(bits >> (8 * g));
+                    st_shared_u8(to + n * 128 + (((tid >> 4) ^ (n & 7)) << 4) + (tid & 15), bits[r] >> (8 * g));
                 }
-            }
             tc_fence_before();
             fence_proxy_async_smem();
             __syncwarp();
