@@ -89,6 +89,13 @@ __device__ __forceinline__ RequestShape shape_of(const AttnArgs& a, int r)
     return s;
 }
 
+// What the warps of a CTA look up again and again: the requests from the one that its share begins in.
+constexpr int kKnown = 16;
+struct KnownRequests {
+    int first;
+    RequestShape s[kKnown];
+};
+
 // A place in the sequence of tiles.
 template <int kRows>
 struct Cursor {
@@ -96,21 +103,16 @@ struct Cursor {
     int request, item, k;                  // item: (head, row tile) within the request; k: tile within the item
     uint32_t begin;                        // index of the item's first tile
 
-    __device__ __forceinline__ void seek(const AttnArgs& a, const uint32_t* prefix, uint32_t tile)
+    __device__ __forceinline__ void seek(const AttnArgs& a, const uint32_t* prefix, const KnownRequests& known, uint32_t tile)
     {
-        int u = 0, v = a.requests;
-        while (v - u > 1) {
-            const int mid = (u + v) >> 1;
-            if (prefix[mid] <= tile) u = mid; else v = mid;
-        }
-        request = u;
-        s = shape_of<kRows>(a, u);
-        const int off = static_cast<int>(tile - prefix[u]);
+        request = known.first;
+        s = known.s[0];
+        const int off = static_cast<int>(tile - prefix[request]);
         item = off / s.tiles;
         k = off - item * s.tiles;
         begin = tile - k;
     }
-    __device__ __forceinline__ void next(const AttnArgs& a, const uint32_t* prefix)
+    __device__ __forceinline__ void next(const AttnArgs& a, const uint32_t* prefix, const KnownRequests& known)
     {
         if (++k < s.tiles) return;
         k = 0;
@@ -118,7 +120,8 @@ struct Cursor {
         if (++item < a.c.kv_heads * s.row_tiles) return;
         item = 0;
         do ++request; while (request < a.requests && prefix[request + 1] == prefix[request]);
-        if (request < a.requests) s = shape_of<kRows>(a, request);
+        if (request - known.first < kKnown) s = known.s[request - known.first];
+        else if (request < a.requests) s = shape_of<kRows>(a, request);
     }
     __device__ __forceinline__ int head() const { return item / s.row_tiles; }
     __device__ __forceinline__ int pos() const { return (s.lo + k) * kTile; }
@@ -202,7 +205,8 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
     __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_sfull[2], s_pfull[2], s_ofull[2], s_qfull, s_drain;
     __shared__ __align__(16) float s_max[2][kComputeWarps][kMaxRows], s_sum[kMaxRows][kComputeWarps];
     __shared__ __align__(16) ItemInfo s_item[2];
-    __shared__ float2 s_scales[kMaxStages][kMaxBoxes];   // (k, v) of each box; v = 0: there is none
+    __shared__ float2 s_scales[kMaxStages][kMaxBoxes];   // (k, v) of each box; negative: there is none
+    __shared__ KnownRequests known;
     __shared__ uint32_t s_scan[kThreads / 32], s_tmem;
     __shared__ int s_last;
 
@@ -216,7 +220,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         prefetch_tensormap(&k_map);
         prefetch_tensormap(&v_map);
         for (int i = 0; i < kMaxStages; ++i) {
-            mbar_init(smem_u32(&s_full[i]), 1);
+            mbar_init(smem_u32(&s_full[i]), 1 + kMaxBoxes);   // the boxes' bytes; the scales of each lane
             mbar_init(smem_u32(&s_empty[i]), 1);
         }
         mbar_init(smem_u32(&s_sfull[0]), 1);
@@ -274,81 +278,86 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
     auto timed_out = [&]() {
         if (lane == 0 && atomicCAS(a.status, 0, QTZ_ERR_DEVICE_TIMEOUT) == 0) a.status[1] = QTZ_SITE_KV_ATTENTION;
     };
+    if (count > 0 && warp == 0) {
+        int u = 0, v = a.requests;                     // the last request that begins at or before the share's first tile
+        while (v - u > 1) {
+            const int mid = (u + v) >> 1;
+            if (prefix[mid] <= static_cast<uint32_t>(t0)) u = mid; else v = mid;
+        }
+        if (lane == 0) known.first = u;
+        if (lane < kKnown && u + lane < a.requests) known.s[lane] = shape_of<kRows>(a, u + lane);
+    }
+    __syncthreads();
     Cursor<kRows> cur;
-    if (count > 0) cur.seek(a, prefix, t0);
+    if (count > 0) cur.seek(a, prefix, known, t0);
 
     if (count > 0 && warp == kComputeWarps) {
         // ======== producer: lane j brings box j of the tile, and its scales ========
-        // Three tiles are under way: table entries of tile i + 2, scales of tile i + 1, the copy of tile i, so that no look-up
-        // is waited for.
+        // Table entries are requested kAhead tiles before they are needed, and the scales travel like the boxes, by asynchronous
+        // copies that the tile's barrier counts: the producer waits for no look-up (under load one takes longer than a tile).
         const int box_rows = 1 << a.box_shift, boxes = kTile >> a.box_shift;
-        auto entry_of = [&](const Cursor<kRows>& c, int& head, int& offset) {
-            const int pos = c.pos() + lane * box_rows;
-            head = c.head();
-            offset = 0;
-            if (lane >= boxes || pos >= c.s.limit) return -1;
+        constexpr int kAhead = 4;
+        int id[kAhead], offset[kAhead], head[kAhead];  // offset: within the block, -1 where there is nothing to bring
+        auto request_entry = [&](int& e, int& o, int& h) {
+            const int pos = cur.pos() + lane * box_rows;
+            e = o = -1;
+            h = cur.head();
+            if (lane >= boxes || pos >= cur.s.limit) return;
             const int j = pos / a.c.block_tokens;
-            offset = pos - j * a.c.block_tokens;
-            return a.table[static_cast<int64_t>(c.request) * a.width + j];
+            o = pos - j * a.c.block_tokens;
+            e = a.table[static_cast<int64_t>(cur.request) * a.width + j];
         };
-        // Scales lie in [2^-100, 2^122] here (the least is QTZ_KV_MIN_SCALE; no 16-bit value gives more than 2^121), so
-        // that their logarithms and inverses are ordinary numbers.
-        auto clamped = [](float v) { return fminf(fmaxf(v, QTZ_KV_MIN_SCALE), 5.3169120e36f); };
-        int id1 = -1, head1 = 0, off1 = 0, id2, head2, off2, row0 = -1, row1 = -1, limit1 = 0, limit2;
-        float ks0 = 0.f, vs0 = 0.f, ks1 = 0.f, vs1 = 0.f;
-        auto resolve = [&](int id, int head, int offset, int wanted, float& ks, float& vs) {
-            if (!wanted) return -1;
-            if (id < 0 || id >= a.c.blocks) {
-                qtz_dev::report_invalid(a.status, QTZ_SITE_KV_ATTENTION);
-                return -1;
-            }
-            const int64_t bh = static_cast<int64_t>(id) * a.c.kv_heads + head;
-            ks = a.c.k_scale_dev[bh];
-            vs = a.c.v_scale_dev[bh];
-            return static_cast<int>(bh * a.c.block_tokens + offset);
-        };
-        auto wanted = [&](const Cursor<kRows>& c) { return lane < boxes && c.pos() + lane * box_rows < c.s.limit ? 1 : 0; };
-        id1 = entry_of(cur, head1, off1);
-        row0 = resolve(id1, head1, off1, wanted(cur), ks0, vs0);
-        if (count > 1) {
-            cur.next(a, prefix);
-            id1 = entry_of(cur, head1, off1);
-            limit1 = wanted(cur);
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            id[j] = offset[j] = -1;
+            head[j] = 0;
+            if (j >= count) continue;
+            if (j > 0) cur.next(a, prefix, known);
+            request_entry(id[j], offset[j], head[j]);
         }
         int i = 0, stage = 0, round = 0;
         for (; i < count; ++i) {
-            id2 = -1, head2 = 0, off2 = 0, limit2 = 0;
-            if (i + 2 < count) {
-                cur.next(a, prefix);
-                id2 = entry_of(cur, head2, off2);
-                limit2 = wanted(cur);
+            int row = -1;
+            int64_t bh = 0;
+            if (offset[0] >= 0) {
+                if (id[0] < 0 || id[0] >= a.c.blocks) {
+                    qtz_dev::report_invalid(a.status, QTZ_SITE_KV_ATTENTION);
+                } else {
+                    bh = static_cast<int64_t>(id[0]) * a.c.kv_heads + head[0];
+                    row = static_cast<int>(bh * a.c.block_tokens + offset[0]);
+                }
             }
-            row1 = -1;
-            if (i + 1 < count) row1 = resolve(id1, head1, off1, limit1, ks1, vs1);
+#pragma unroll
+            for (int j = 0; j + 1 < kAhead; ++j) {
+                id[j] = id[j + 1];
+                offset[j] = offset[j + 1];
+                head[j] = head[j + 1];
+            }
+            id[kAhead - 1] = offset[kAhead - 1] = -1;
+            if (i + kAhead < count) {
+                cur.next(a, prefix, known);
+                request_entry(id[kAhead - 1], offset[kAhead - 1], head[kAhead - 1]);
+            }
             if (round > 0 && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&s_empty[stage]), (round - 1) & 1, a.wait_budget))) {
                 timed_out();
                 break;
             }
             const uint32_t bar = smem_u32(&s_full[stage]), dst = base + stage * kStage;
-            if (lane < boxes) s_scales[stage][lane] = row0 >= 0 ? make_float2(clamped(ks0), clamped(vs0)) : make_float2(0.f, 0.f);
-            const int have = __popc(__ballot_sync(0xffffffffu, row0 >= 0));
+            if (lane < kMaxBoxes && row < 0) s_scales[stage][lane] = make_float2(-1.f, -1.f);
+            const int have = __popc(__ballot_sync(0xffffffffu, row >= 0));
             __syncwarp();
             if (lane == 0) mbar_arrive_expect_tx(bar, have * box_rows * 2 * D);
             __syncwarp();
-            if (row0 >= 0) {
-                const uint32_t at = dst + lane * box_rows * kRowBytes;
+            if (row >= 0) {
+                const uint32_t at = dst + lane * box_rows * kRowBytes, sc = smem_u32(&s_scales[stage][lane]);
 #pragma unroll
-                for (int hh = 0; hh < kHalves; ++hh) tma_load_2d(at + hh * kBox, &k_map, bar, hh * 128, row0);
+                for (int hh = 0; hh < kHalves; ++hh) tma_load_2d(at + hh * kBox, &k_map, bar, hh * 128, row);
 #pragma unroll
-                for (int hh = 0; hh < kHalves; ++hh) tma_load_2d(at + (kHalves + hh) * kBox, &v_map, bar, hh * 128, row0);
+                for (int hh = 0; hh < kHalves; ++hh) tma_load_2d(at + (kHalves + hh) * kBox, &v_map, bar, hh * 128, row);
+                cp_async_4(sc, a.c.k_scale_dev + bh);
+                cp_async_4(sc + 4, a.c.v_scale_dev + bh);
             }
-            row0 = row1;
-            ks0 = ks1;
-            vs0 = vs1;
-            id1 = id2;
-            head1 = head2;
-            off1 = off2;
-            limit1 = limit2;
+            if (lane < kMaxBoxes) cp_async_arrive(bar);
             if (++stage == a.stages) {
                 stage = 0;
                 ++round;
@@ -384,7 +393,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         multiply_keys(0, cur);
         for (int i = 0; i < count && ok; ++i) {
             if (i + 1 < count) {
-                cur.next(a, prefix);
+                cur.next(a, prefix, known);
                 multiply_keys(i + 1, cur);
             }
             ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_pfull[i & 1]), (i >> 1) & 1, a.wait_budget));
@@ -548,7 +557,10 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
             const bool last = cur.k == cur.s.tiles - 1, more = i + 1 < count;
             if (i == 0 || cur.k == 0) wait(s_qfull, items & 1);
             wait(s_full[stage], round & 1);
+            // Scales lie in [2^-100, 2^122] here (the least is QTZ_KV_MIN_SCALE; no 16-bit value gives more than 2^121), so
+            // that their logarithms and inverses are ordinary numbers.
             const float2 scales = s_scales[stage][tid >> a.box_shift];
+            const float ks = fminf(fmaxf(scales.x, QTZ_KV_MIN_SCALE), 5.3169120e36f), vs = fminf(fmaxf(scales.y, QTZ_KV_MIN_SCALE), 5.3169120e36f);
             if (++stage == a.stages) {
                 stage = 0;
                 ++round;
@@ -559,12 +571,12 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
             {
                 uint32_t s[kN];
                 load_columns<kN>(tmem + (i & 1) * kColumns + (static_cast<uint32_t>(warp) << 21), s);
-                const float lv = lg2(scales.y);
+                const float lv = lg2(vs);
 #pragma unroll
                 for (int r = 0; r < kRows; ++r)
-                    x[r] = fmaf(join_digits(s[r], s[kRows + r], s[2 * kRows + r]), it.factor[r] * scales.x, lv);
+                    x[r] = fmaf(join_digits(s[r], s[kRows + r], s[2 * kRows + r]), it.factor[r] * ks, lv);
             }
-            if (scales.y == 0.f) {
+            if (scales.x < 0.f) {
 #pragma unroll
                 for (int r = 0; r < kRows; ++r) x[r] = -INFINITY;
             } else if (pos0 < it.full_lo || pos0 + kTile > it.full_hi) {
@@ -593,7 +605,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                     top[r + 2] = fmaxf(top[r + 2], t.z);
                     top[r + 3] = fmaxf(top[r + 3], t.w);
                 }
-            const float inv = scales.y == 0.f ? 0.f : __fdividef(1.f, scales.y);
+            const float inv = __fdividef(1.f, vs);
             float fresh[kRows];
             uint32_t bits[kRows];
 #pragma unroll
@@ -629,7 +641,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
             } else {                                   // the end of the item, or of this CTA's part of it
                 Cursor<kRows> ahead = cur;
                 if (more) {
-                    ahead.next(a, prefix);
+                    ahead.next(a, prefix, known);
                     load_queries(ahead, (items + 1) & 1);
                 }
                 take_sums(i);
