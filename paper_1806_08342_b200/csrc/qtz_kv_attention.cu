@@ -43,7 +43,7 @@ constexpr int kThreads = kComputeThreads + 64;   // + one warp for TMA, one for 
 constexpr int kMaxRows = 16;
 constexpr int kMaxStages = 6;
 constexpr int kMaxBoxes = 8;
-constexpr int kFanIn = 8;                  // parts that one CTA joins; more are joined in two steps
+constexpr int kFanIn = kComputeThreads / kMaxRows;   // parts that one CTA joins at a time; more are joined in two steps
 constexpr int kSmemLimit = 227 * 1024;     // of an SM, each CTA costing 1 KB more than it asks for
 
 struct AttnArgs {
@@ -203,7 +203,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
 
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_sfull[2], s_pfull[2], s_ofull[2], s_qfull, s_drain;
-    __shared__ __align__(16) float s_max[2][kComputeWarps][kMaxRows], s_sum[kMaxRows][kComputeWarps];
+    __shared__ __align__(16) float s_max[2][kComputeWarps][kMaxRows], s_sum[kMaxRows][kComputeWarps], s_join[2][kFanIn][kMaxRows];
     __shared__ __align__(16) ItemInfo s_item[2];
     __shared__ float2 s_scales[kMaxStages][kMaxBoxes];   // (k, v) of each box; negative: there is none
     __shared__ KnownRequests known;
@@ -428,85 +428,88 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         auto load_queries = [&](const Cursor<kRows>& c, int which) {
             ItemInfo& it = s_item[which];
             constexpr int kPer = D / 32;               // values of a row that a lane holds
-            const int h = c.head(), row0 = (c.item - h * c.s.row_tiles) * kRows;
-            int lo = 0, hi = 0x7fffffff;
-            for (int r = 0; r < kRows; ++r) {
-                const int local = (row0 + r) / a.group, sub = row0 + r - local * a.group;
-                const bool has = local < c.s.added;
-                const int own = c.s.len - c.s.added + local + 1;
-                const int end = has ? min(own, c.s.limit) : 0, begin = has && a.window > 0 ? max(0, own - a.window) : 0;
-                if (has) {
-                    lo = max(lo, begin);
-                    hi = min(hi, end);
-                }
-                if (r % kComputeWarps != warp) continue;
-                const int64_t token = c.s.first + local;
-                const int head = h * a.group + sub;
-                float v[kPer];
-                float top = 0.f;
-                bool odd = false;
-                if (has) {
-                    const T* q = static_cast<const T*>(a.q) + token * a.q_token_stride + head * a.q_head_stride + lane * kPer;
-                    uint32_t raw[kPer / 2];
-                    if constexpr (kPer == 2) raw[0] = *reinterpret_cast<const uint32_t*>(q);
-                    else if constexpr (kPer == 4) {
-                        const uint2 u = *reinterpret_cast<const uint2*>(q);
-                        raw[0] = u.x; raw[1] = u.y;
-                    } else {
-                        const uint4 u = *reinterpret_cast<const uint4*>(q);
-                        raw[0] = u.x; raw[1] = u.y; raw[2] = u.z; raw[3] = u.w;
-                    }
+            constexpr int kMine = (kRows + kComputeWarps - 1) / kComputeWarps;
+            // lane r finds row r
+            const int h = c.head(), index = (c.item - h * c.s.row_tiles) * kRows + lane, local = index / a.group;
+            const int head = h * a.group + (index - local * a.group);
+            const bool has = lane < kRows && local < c.s.added;
+            const int64_t token = c.s.first + local, from = has ? token * a.q_token_stride + head * a.q_head_stride : -1;
+            uint32_t raw[kMine][kPer / 2];
 #pragma unroll
-                    for (int j = 0; j < kPer / 2; ++j) {
-                        const float2 f = qtz_dev::unpack2(raw[j], T());
-                        v[2 * j] = f.x;
-                        v[2 * j + 1] = f.y;
-                    }
+            for (int j = 0; j < kMine; ++j) {
+                const int r = warp + j * kComputeWarps;
+                const int64_t at = __shfl_sync(0xffffffffu, from, r);
+                const T* q = static_cast<const T*>(a.q) + at + lane * kPer;
+#pragma unroll
+                for (int k = 0; k < kPer / 2; ++k) raw[j][k] = 0;
+                if (at < 0) continue;                  // lanes from kRows on hold no row either
+                if constexpr (kPer == 2) {
+                    raw[j][0] = *reinterpret_cast<const uint32_t*>(q);
+                } else if constexpr (kPer == 4) {
+                    const uint2 u = *reinterpret_cast<const uint2*>(q);
+                    raw[j][0] = u.x; raw[j][1] = u.y;
                 } else {
+                    const uint4 u = *reinterpret_cast<const uint4*>(q);
+                    raw[j][0] = u.x; raw[j][1] = u.y; raw[j][2] = u.z; raw[j][3] = u.w;
+                }
+            }
+            if (warp == 0) {
+                const int own = c.s.len - c.s.added + local + 1;   // tokens up to the row's own
+                const int end = has ? min(own, c.s.limit) : 0x7fffffff, begin = has && a.window > 0 ? max(0, own - a.window) : 0;
+                if (lane < kRows) {
+                    it.begin[lane] = begin;
+                    it.end[lane] = end;
+                    it.out[lane] = has ? token * a.y_token_stride + head * a.y_head_stride : -1;
+                    it.lse[lane] = token * a.q_heads + head;
+                }
+                const int lo = __reduce_max_sync(0xffffffffu, begin), hi = __reduce_min_sync(0xffffffffu, end);
+                if (lane == 0) {
+                    it.full_lo = lo;
+                    it.full_hi = hi;
+                }
+            }
 #pragma unroll
-                    for (int j = 0; j < kPer; ++j) v[j] = 0.f;
+            for (int j = 0; j < kMine; ++j) {
+                const int r = warp + j * kComputeWarps;
+                if (r >= kRows) break;
+                float v[kPer], top = 0.f;
+                bool odd = false;
+#pragma unroll
+                for (int k = 0; k < kPer / 2; ++k) {
+                    const float2 f = qtz_dev::unpack2(raw[j][k], T());
+                    v[2 * k] = f.x;
+                    v[2 * k + 1] = f.y;
                 }
 #pragma unroll
-                for (int j = 0; j < kPer; ++j) {
-                    odd = odd || (__float_as_uint(v[j]) & 0x7f800000u) == 0x7f800000u;
-                    top = fmaxf(top, fabsf(v[j]));
+                for (int k = 0; k < kPer; ++k) {
+                    odd = odd || (__float_as_uint(v[k]) & 0x7f800000u) == 0x7f800000u;
+                    top = fmaxf(top, fabsf(v[k]));
                 }
                 top = redux_max(top);
                 odd = __any_sync(0xffffffffu, odd);
                 // rows below 2^-100 count as 2^-100 (their logits are zero either way)
                 const int ex = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -100), 127);
-                const float mult = __uint_as_float(static_cast<uint32_t>(127 + min(21 - ex, 127)) << 23);
+                const float mult = __uint_as_float(static_cast<uint32_t>(127 + 21 - ex) << 23);
                 uint64_t digits[3] = {0, 0, 0};
 #pragma unroll
-                for (int j = 0; j < kPer; ++j) {
-                    const int x = odd ? 0 : __float2int_rn(v[j] * mult);
+                for (int k = 0; k < kPer; ++k) {
+                    const int x = odd ? 0 : __float2int_rn(v[k] * mult);
                     const int d0 = (x << 24) >> 24, x1 = (x - d0) >> 8, d1 = (x1 << 24) >> 24, d2 = (x1 - d1) >> 8;
-                    digits[0] |= static_cast<uint64_t>(d0 & 0xff) << (8 * j);
-                    digits[1] |= static_cast<uint64_t>(d1 & 0xff) << (8 * j);
-                    digits[2] |= static_cast<uint64_t>(d2 & 0xff) << (8 * j);
+                    digits[0] |= static_cast<uint64_t>(d0 & 0xff) << (8 * k);
+                    digits[1] |= static_cast<uint64_t>(d1 & 0xff) << (8 * k);
+                    digits[2] |= static_cast<uint64_t>(d2 & 0xff) << (8 * k);
                 }
                 const int d = lane * kPer, hh = d / 128, x = d % kRowBytes;
 #pragma unroll
                 for (int g = 0; g < 3; ++g) {
-                    const int n = g * kRows + r;
-                    const int swz = kRowBytes == 128 ? (n & 7) : ((n >> 1) & 3);
+                    const int n = g * kRows + r, swz = kRowBytes == 128 ? (n & 7) : ((n >> 1) & 3);
                     uint8_t* to = smem + off_q + hh * kN * kRowBytes + n * kRowBytes + (((x >> 4) ^ swz) << 4) + (x & 15);
                     if constexpr (kPer == 2) *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(digits[g]);
                     else if constexpr (kPer == 4) *reinterpret_cast<uint32_t*>(to) = static_cast<uint32_t>(digits[g]);
                     else *reinterpret_cast<uint64_t*>(to) = digits[g];
                 }
-                if (lane == 0) {
-                    // a row that holds NaN or infinity gives NaN
-                    it.factor[r] = odd ? __uint_as_float(0x7fc00000u) : a.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 - 21 + ex) << 23);
-                    it.begin[r] = begin;
-                    it.end[r] = end;
-                    it.out[r] = has ? token * a.y_token_stride + head * a.y_head_stride : -1;
-                    it.lse[r] = token * a.q_heads + head;
-                }
-            }
-            if (tid == 0) {
-                it.full_lo = lo;
-                it.full_hi = hi;
+                // a row that holds NaN or infinity gives NaN
+                if (lane == 0) it.factor[r] = odd ? __uint_as_float(0x7fc00000u) : a.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 - 21 + ex) << 23);
             }
             fence_proxy_async_smem();
             __syncwarp();
@@ -695,33 +698,49 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                         __threadfence();
                         return yes;
                     };
-                    // joins the parts of CTAs from, from + step, .. (at most kFanIn at a time are in flight)
+                    // Joins the parts of CTAs from, from + step, .. to into acc, m and sum, kFanIn at a time: their maxima and
+                    // denominators come by one load of each thread, and become weights in shared memory.
                     float sum[kRows];
                     auto join = [&](int from, int to, int step) {
-#pragma unroll
-                        for (int r = 0; r < kRows; ++r) {
-                            m[r] = -INFINITY;
-                            sum[r] = 0.f;
-#pragma unroll
-                            for (int hh = 0; hh < kHalves; ++hh) acc[hh][r] = 0.f;
-                        }
-                        for (int cta = from; cta <= to; cta += step) {
-                            const float* p = part_of(cta);
-#pragma unroll
-                            for (int r = 0; r < kRows; ++r) m[r] = fmaxf(m[r], __ldcg(p + kMaxRows * D + r));
-                        }
-#pragma unroll 2
-                        for (int cta = from; cta <= to; cta += step) {
-                            const float* p = part_of(cta);
+                        const int n = (to - from) / step + 1;
+                        for (int done = 0; done < n; done += kFanIn) {
+                            const int part = done + tid / kMaxRows, row = tid % kMaxRows;
+                            float pm = -INFINITY, pl = 0.f;
+                            if (part < n && row < kRows) {
+                                const float* p = part_of(from + part * step) + kMaxRows * D;
+                                pm = __ldcg(p + row);
+                                pl = __ldcg(p + kMaxRows + row);
+                            }
+                            s_join[0][tid / kMaxRows][row] = pm;
+                            s_join[1][tid / kMaxRows][row] = pl;
+                            named_barrier(1, kComputeThreads);
+                            float w[kRows];            // of what has been joined before
 #pragma unroll
                             for (int r = 0; r < kRows; ++r) {
-                                const float pm = __ldcg(p + kMaxRows * D + r), pl = __ldcg(p + kMaxRows * D + kMaxRows + r);
-                                const float wt = pm == -INFINITY && pl == 0.f ? 0.f : ex2(pm - (m[r] == -INFINITY ? 0.f : m[r]));
-                                sum[r] = fmaf(pl, wt, sum[r]);
+                                float top = done > 0 ? m[r] : -INFINITY;
 #pragma unroll
-                                for (int hh = 0; hh < kHalves; ++hh)
-                                    acc[hh][r] = fmaf(D >= 128 || tid < D ? __ldcg(p + r * D + hh * 128 + tid) : 0.f, wt, acc[hh][r]);
+                                for (int j = 0; j < kFanIn; ++j) top = fmaxf(top, s_join[0][j][r]);
+                                const float origin = top == -INFINITY ? 0.f : top;
+                                w[r] = done > 0 && !(m[r] == -INFINITY && sum[r] == 0.f) ? ex2(m[r] - origin) : 0.f;
+                                m[r] = top;
+                                sum[r] = done > 0 ? sum[r] * w[r] : 0.f;
+#pragma unroll
+                                for (int hh = 0; hh < kHalves; ++hh) acc[hh][r] = done > 0 ? acc[hh][r] * w[r] : 0.f;
                             }
+                            const int here = min(kFanIn, n - done);
+#pragma unroll 4
+                            for (int j = 0; j < here; ++j) {
+                                const float* p = part_of(from + (done + j) * step) + (D >= 128 || tid < D ? tid : 0);
+#pragma unroll
+                                for (int r = 0; r < kRows; ++r) {
+                                    const float jm = s_join[0][j][r], jl = s_join[1][j][r];
+                                    const float wt = jm == -INFINITY && jl == 0.f ? 0.f : ex2(jm - (m[r] == -INFINITY ? 0.f : m[r]));
+                                    sum[r] = fmaf(jl, wt, sum[r]);
+#pragma unroll
+                                    for (int hh = 0; hh < kHalves; ++hh) acc[hh][r] = fmaf(__ldcg(p + r * D + hh * 128), wt, acc[hh][r]);
+                                }
+                            }
+                            named_barrier(1, kComputeThreads);
                         }
                     };
                     const int me = static_cast<int>(blockIdx.x), groups = (c1 - c0) / kFanIn + 1, first = me - (me - c0) % kFanIn;
@@ -730,7 +749,6 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                         join(first, min(first + kFanIn - 1, c1), 1);
                         if (groups > 1) {
                             float* to = part_of(first);
-                            named_barrier(1, kComputeThreads);                 // every thread has read the maxima
 #pragma unroll
                             for (int r = 0; r < kRows; ++r) {
                                 if (D >= 128 || tid < D)
