@@ -44,7 +44,7 @@ constexpr int kMaxRows = 16;
 constexpr int kMaxStages = 6;
 constexpr int kMaxBoxes = 8;
 constexpr int kFanIn = kComputeThreads / kMaxRows;   // parts that one CTA joins at a time; more are joined in two steps
-constexpr int kSmemLimit = 227 * 1024;     // of an SM, each CTA costing 1 KB more than it asks for
+constexpr int kSmemLimit = 227 * 1024;     // most that a CTA may ask for; an SM has 1 KB more, and each CTA costs 1 KB more than it asks for
 
 struct AttnArgs {
     qtz_kv_cache c;
@@ -184,6 +184,17 @@ struct ItemInfo {
     int32_t full_lo, full_hi;              // tokens that every row sees
 };
 
+// Shared memory of a CTA beside the ring, the operands and the prefix sums.
+struct Shared {
+    float max[2][kComputeWarps][kMaxRows], sum[kMaxRows][kComputeWarps];
+    ItemInfo item[2];
+    float2 scales[kMaxStages][kMaxBoxes];  // (k, v) of each box; negative: there is none
+    uint64_t full[kMaxStages], empty[kMaxStages], sfull[2], pfull[2], ofull[2], qfull[2], qempty[2], drain;
+    KnownRequests known;
+    uint32_t scan[kThreads / 32], tmem;
+    int last;
+};
+
 template <typename T, int D, int kRows>
 __global__ void __launch_bounds__(kThreads, D == 256 ? 1 : 2)
 attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
@@ -202,39 +213,37 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
     constexpr uint32_t kMulV = (2u << 4) | (1u << 7) | (0u << 10) | (1u << 15) | (static_cast<uint32_t>(kN >> 3) << 17) | (128u >> 4 << 24);
 
     extern __shared__ uint8_t smem_raw[];
-    __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_sfull[2], s_pfull[2], s_ofull[2], s_qfull, s_drain;
-    __shared__ __align__(16) float s_max[2][kComputeWarps][kMaxRows], s_sum[kMaxRows][kComputeWarps], s_join[2][kFanIn][kMaxRows];
-    __shared__ __align__(16) ItemInfo s_item[2];
-    __shared__ float2 s_scales[kMaxStages][kMaxBoxes];   // (k, v) of each box; negative: there is none
-    __shared__ KnownRequests known;
-    __shared__ uint32_t s_scan[kThreads / 32], s_tmem;
-    __shared__ int s_last;
-
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* const smem = smem_raw + (base - smem_u32(smem_raw));
-    const uint32_t off_p = a.stages * kStage, off_q = off_p + 2 * kN * 128, off_prefix = off_q + kHalves * kN * kRowBytes;
+    const uint32_t off_p = a.stages * kStage, off_q = off_p + kN * 128, off_shared = off_q + 2 * kN * D, off_prefix = off_shared + (sizeof(Shared) + 15) / 16 * 16;
     uint32_t* const prefix = reinterpret_cast<uint32_t*>(smem + off_prefix);
+    Shared& sh = *reinterpret_cast<Shared*>(smem + off_shared);
+    KnownRequests& known = sh.known;
+    float (*const join_with)[kFanIn][kMaxRows] = reinterpret_cast<float (*)[kFanIn][kMaxRows]>(smem + off_p);   // while no weights are there
 
     if (tid == 0) {
         prefetch_tensormap(&k_map);
         prefetch_tensormap(&v_map);
         for (int i = 0; i < kMaxStages; ++i) {
-            mbar_init(smem_u32(&s_full[i]), 1 + kMaxBoxes);   // the boxes' bytes; the scales of each lane
-            mbar_init(smem_u32(&s_empty[i]), 1);
+            mbar_init(smem_u32(&sh.full[i]), 1 + kMaxBoxes);   // the boxes' bytes; the scales of each lane
+            mbar_init(smem_u32(&sh.empty[i]), 1);
         }
-        mbar_init(smem_u32(&s_sfull[0]), 1);
-        mbar_init(smem_u32(&s_sfull[1]), 1);
-        mbar_init(smem_u32(&s_ofull[0]), 1);
-        mbar_init(smem_u32(&s_ofull[1]), 1);
-        mbar_init(smem_u32(&s_drain), 1);
-        mbar_init(smem_u32(&s_pfull[0]), kComputeWarps);
-        mbar_init(smem_u32(&s_pfull[1]), kComputeWarps);
-        mbar_init(smem_u32(&s_qfull), kComputeWarps);
+        mbar_init(smem_u32(&sh.sfull[0]), 1);
+        mbar_init(smem_u32(&sh.sfull[1]), 1);
+        mbar_init(smem_u32(&sh.ofull[0]), 1);
+        mbar_init(smem_u32(&sh.ofull[1]), 1);
+        mbar_init(smem_u32(&sh.drain), 1);
+        mbar_init(smem_u32(&sh.pfull[0]), kComputeWarps);
+        mbar_init(smem_u32(&sh.pfull[1]), kComputeWarps);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&sh.qfull[i]), 1);
+            mbar_init(smem_u32(&sh.qempty[i]), kComputeWarps);
+        }
         fence_barrier_init();
     }
     if (warp == kComputeWarps + 1) {
-        tmem_alloc(smem_u32(&s_tmem), kTmemColumns);
+        tmem_alloc(smem_u32(&sh.tmem), kTmemColumns);
         tmem_relinquish();
     }
 
@@ -254,13 +263,13 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         const uint32_t u = __shfl_up_sync(0xffffffffu, scan, off);
         if (lane >= off) scan += u;
     }
-    if (lane == 31) s_scan[warp] = scan;
+    if (lane == 31) sh.scan[warp] = scan;
     __syncthreads();
     uint32_t before = scan - mine, total = 0;
 #pragma unroll
     for (int w = 0; w < kThreads / 32; ++w) {
-        if (w < warp) before += s_scan[w];
-        total += s_scan[w];
+        if (w < warp) before += sh.scan[w];
+        total += sh.scan[w];
     }
     for (int r = r_lo; r < r_hi; ++r) {
         const uint32_t n = prefix[r];
@@ -271,7 +280,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = s_tmem;
+    const uint32_t tmem = sh.tmem;
 
     const int all = static_cast<int>(total), share = (all + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x);
     const int t0 = min(static_cast<int>(blockIdx.x) * share, all), count = min(t0 + share, all) - t0;
@@ -297,6 +306,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         // copies that the tile's barrier counts: the producer waits for no look-up (under load one takes longer than a tile).
         const int box_rows = 1 << a.box_shift, boxes = kTile >> a.box_shift;
         constexpr int kAhead = 4;
+        const Cursor<kRows> first = cur;
         int id[kAhead], offset[kAhead], head[kAhead];  // offset: within the block, -1 where there is nothing to bring
         auto request_entry = [&](int& e, int& o, int& h) {
             const int pos = cur.pos() + lane * box_rows;
@@ -315,145 +325,34 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
             if (j > 0) cur.next(a, prefix, known);
             request_entry(id[j], offset[j], head[j]);
         }
-        int i = 0, stage = 0, round = 0;
-        for (; i < count; ++i) {
-            int row = -1;
-            int64_t bh = 0;
-            if (offset[0] >= 0) {
-                if (id[0] < 0 || id[0] >= a.c.blocks) {
-                    qtz_dev::report_invalid(a.status, QTZ_SITE_KV_ATTENTION);
-                } else {
-                    bh = static_cast<int64_t>(id[0]) * a.c.kv_heads + head[0];
-                    row = static_cast<int>(bh * a.c.block_tokens + offset[0]);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j + 1 < kAhead; ++j) {
-                id[j] = id[j + 1];
-                offset[j] = offset[j + 1];
-                head[j] = head[j + 1];
-            }
-            id[kAhead - 1] = offset[kAhead - 1] = -1;
-            if (i + kAhead < count) {
-                cur.next(a, prefix, known);
-                request_entry(id[kAhead - 1], offset[kAhead - 1], head[kAhead - 1]);
-            }
-            if (round > 0 && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&s_empty[stage]), (round - 1) & 1, a.wait_budget))) {
-                timed_out();
-                break;
-            }
-            const uint32_t bar = smem_u32(&s_full[stage]), dst = base + stage * kStage;
-            if (lane < kMaxBoxes && row < 0) s_scales[stage][lane] = make_float2(-1.f, -1.f);
-            const int have = __popc(__ballot_sync(0xffffffffu, row >= 0));
-            __syncwarp();
-            if (lane == 0) mbar_arrive_expect_tx(bar, have * box_rows * 2 * D);
-            __syncwarp();
-            if (row >= 0) {
-                const uint32_t at = dst + lane * box_rows * kRowBytes, sc = smem_u32(&s_scales[stage][lane]);
-#pragma unroll
-                for (int hh = 0; hh < kHalves; ++hh) tma_load_2d(at + hh * kBox, &k_map, bar, hh * 128, row);
-#pragma unroll
-                for (int hh = 0; hh < kHalves; ++hh) tma_load_2d(at + (kHalves + hh) * kBox, &v_map, bar, hh * 128, row);
-                cp_async_4(sc, a.c.k_scale_dev + bh);
-                cp_async_4(sc + 4, a.c.v_scale_dev + bh);
-            }
-            if (lane < kMaxBoxes) cp_async_arrive(bar);
-            if (++stage == a.stages) {
-                stage = 0;
-                ++round;
-            }
-        }
-        // nothing may be in flight when the CTA ends
-        for (int j = max(0, i - a.stages); j < i; ++j)
-            if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&s_full[j % a.stages]), (j / a.stages) & 1, a.wait_budget))) timed_out();
-    } else if (count > 0 && warp == kComputeWarps + 1) {
-        // ======== matrix instructions: S of the next tile is issued before O of this one ========
-        int items = 0;
-        bool ok = true;
-        auto multiply_keys = [&](int i, const Cursor<kRows>& c) {
-            const int stage = i % a.stages;
-            if (i == 0 || c.k == 0) {
-                ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_qfull), items & 1, a.wait_budget));
-                ++items;
-            }
-            ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_full[stage]), (i / a.stages) & 1, a.wait_budget));
-            if (!ok) return;
-            tc_fence_after();
-            if (elect_one()) {
-#pragma unroll
-                for (int hh = 0; hh < kHalves; ++hh)
-#pragma unroll
-                    for (int j = 0; j < kRowBytes / 32; ++j)
-                        mma_i8(tmem + (i & 1) * kColumns, make_kmajor_desc(base + stage * kStage + hh * kBox, kRowBytes) + 2 * j,
-                               make_kmajor_desc(base + off_q + hh * kN * kRowBytes, kRowBytes) + 2 * j, kMulK, hh + j > 0);
-                mma_commit(smem_u32(&s_sfull[i & 1]));
-            }
-            __syncwarp();
-        };
-        multiply_keys(0, cur);
-        for (int i = 0; i < count && ok; ++i) {
-            if (i + 1 < count) {
-                cur.next(a, prefix, known);
-                multiply_keys(i + 1, cur);
-            }
-            ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_pfull[i & 1]), (i >> 1) & 1, a.wait_budget));
-            if (!ok) break;
-            tc_fence_after();
-            if (elect_one()) {
-                const uint32_t v = base + (i % a.stages) * kStage + kHalves * kBox;
-#pragma unroll
-                for (int hh = 0; hh < kHalves; ++hh)
-#pragma unroll
-                    for (int j = 0; j < kTile / 32; ++j)
-                        mma_i8(tmem + (2 + (i & 1) * kHalves + hh) * kColumns, make_mnmajor_desc(v + hh * kBox + j * 32 * kRowBytes, kRowBytes),
-                               make_kmajor_desc(base + off_p + (i & 1) * kN * 128, 128) + 2 * j, kMulV, j > 0);
-                mma_commit(smem_u32(&s_ofull[i & 1]));
-                mma_commit(smem_u32(&s_empty[i % a.stages]));
-            }
-            __syncwarp();
-        }
-        if (!ok) {                                     // what was issued may still run: give it the same limit, then go
-            timed_out();
-            if (elect_one()) mma_commit(smem_u32(&s_drain));
-            __syncwarp();
-            mbar_wait(smem_u32(&s_drain), 0, a.wait_budget);
-        }
-    } else if (count > 0) {
-        // ======== compute: thread = token of S^T, then column of O^T ========
-        bool ok = true;
-        auto wait = [&](uint64_t& bar, int parity) {   // the warp goes on together
-            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar), parity, a.wait_budget)) && ok;
-        };
         // Digits of an item's query rows into the operand, and what the softmax has to know of them.
         auto load_queries = [&](const Cursor<kRows>& c, int which) {
-            ItemInfo& it = s_item[which];
+            ItemInfo& it = sh.item[which];
             constexpr int kPer = D / 32;               // values of a row that a lane holds
-            constexpr int kMine = (kRows + kComputeWarps - 1) / kComputeWarps;
             // lane r finds row r
             const int h = c.head(), index = (c.item - h * c.s.row_tiles) * kRows + lane, local = index / a.group;
             const int head = h * a.group + (index - local * a.group);
             const bool has = lane < kRows && local < c.s.added;
             const int64_t token = c.s.first + local, from = has ? token * a.q_token_stride + head * a.q_head_stride : -1;
-            uint32_t raw[kMine][kPer / 2];
+            uint32_t raw[kRows][kPer / 2];
 #pragma unroll
-            for (int j = 0; j < kMine; ++j) {
-                const int r = warp + j * kComputeWarps;
+            for (int r = 0; r < kRows; ++r) {
                 const int64_t at = __shfl_sync(0xffffffffu, from, r);
                 const T* q = static_cast<const T*>(a.q) + at + lane * kPer;
 #pragma unroll
-                for (int k = 0; k < kPer / 2; ++k) raw[j][k] = 0;
-                if (at < 0) continue;                  // lanes from kRows on hold no row either
+                for (int k = 0; k < kPer / 2; ++k) raw[r][k] = 0;
+                if (at < 0) continue;
                 if constexpr (kPer == 2) {
-                    raw[j][0] = *reinterpret_cast<const uint32_t*>(q);
+                    raw[r][0] = *reinterpret_cast<const uint32_t*>(q);
                 } else if constexpr (kPer == 4) {
                     const uint2 u = *reinterpret_cast<const uint2*>(q);
-                    raw[j][0] = u.x; raw[j][1] = u.y;
+                    raw[r][0] = u.x; raw[r][1] = u.y;
                 } else {
                     const uint4 u = *reinterpret_cast<const uint4*>(q);
-                    raw[j][0] = u.x; raw[j][1] = u.y; raw[j][2] = u.z; raw[j][3] = u.w;
+                    raw[r][0] = u.x; raw[r][1] = u.y; raw[r][2] = u.z; raw[r][3] = u.w;
                 }
             }
-            if (warp == 0) {
+            {
                 const int own = c.s.len - c.s.added + local + 1;   // tokens up to the row's own
                 const int end = has ? min(own, c.s.limit) : 0x7fffffff, begin = has && a.window > 0 ? max(0, own - a.window) : 0;
                 if (lane < kRows) {
@@ -469,14 +368,12 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                 }
             }
 #pragma unroll
-            for (int j = 0; j < kMine; ++j) {
-                const int r = warp + j * kComputeWarps;
-                if (r >= kRows) break;
+            for (int r = 0; r < kRows; ++r) {
                 float v[kPer], top = 0.f;
                 bool odd = false;
 #pragma unroll
                 for (int k = 0; k < kPer / 2; ++k) {
-                    const float2 f = qtz_dev::unpack2(raw[j][k], T());
+                    const float2 f = qtz_dev::unpack2(raw[r][k], T());
                     v[2 * k] = f.x;
                     v[2 * k + 1] = f.y;
                 }
@@ -503,7 +400,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
 #pragma unroll
                 for (int g = 0; g < 3; ++g) {
                     const int n = g * kRows + r, swz = kRowBytes == 128 ? (n & 7) : ((n >> 1) & 3);
-                    uint8_t* to = smem + off_q + hh * kN * kRowBytes + n * kRowBytes + (((x >> 4) ^ swz) << 4) + (x & 15);
+                    uint8_t* to = smem + off_q + which * kN * D + hh * kN * kRowBytes + n * kRowBytes + (((x >> 4) ^ swz) << 4) + (x & 15);
                     if constexpr (kPer == 2) *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(digits[g]);
                     else if constexpr (kPer == 4) *reinterpret_cast<uint32_t*>(to) = static_cast<uint32_t>(digits[g]);
                     else *reinterpret_cast<uint64_t*>(to) = digits[g];
@@ -513,11 +410,130 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
             }
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&s_qfull));
+            if (lane == 0) mbar_arrive(smem_u32(&sh.qfull[which]));
         };
 
+        Cursor<kRows> now = first;
+        int i = 0, stage = 0, round = 0, items = 0;
+        for (; i < count; ++i) {
+            int row = -1;
+            int64_t bh = 0;
+            if (offset[0] >= 0) {
+                if (id[0] < 0 || id[0] >= a.c.blocks) {
+                    qtz_dev::report_invalid(a.status, QTZ_SITE_KV_ATTENTION);
+                } else {
+                    bh = static_cast<int64_t>(id[0]) * a.c.kv_heads + head[0];
+                    row = static_cast<int>(bh * a.c.block_tokens + offset[0]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j + 1 < kAhead; ++j) {
+                id[j] = id[j + 1];
+                offset[j] = offset[j + 1];
+                head[j] = head[j + 1];
+            }
+            id[kAhead - 1] = offset[kAhead - 1] = -1;
+            if (i + kAhead < count) {
+                cur.next(a, prefix, known);
+                request_entry(id[kAhead - 1], offset[kAhead - 1], head[kAhead - 1]);
+            }
+            if (round > 0 && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.empty[stage]), (round - 1) & 1, a.wait_budget))) {
+                timed_out();
+                break;
+            }
+            const uint32_t bar = smem_u32(&sh.full[stage]), dst = base + stage * kStage;
+            if (lane < kMaxBoxes && row < 0) sh.scales[stage][lane] = make_float2(-1.f, -1.f);
+            const int have = __popc(__ballot_sync(0xffffffffu, row >= 0));
+            __syncwarp();
+            if (lane == 0) mbar_arrive_expect_tx(bar, have * box_rows * 2 * D);
+            __syncwarp();
+            if (row >= 0) {
+                const uint32_t at = dst + lane * box_rows * kRowBytes, sc = smem_u32(&sh.scales[stage][lane]);
+#pragma unroll
+                for (int hh = 0; hh < kHalves; ++hh) tma_load_2d(at + hh * kBox, &k_map, bar, hh * 128, row);
+#pragma unroll
+                for (int hh = 0; hh < kHalves; ++hh) tma_load_2d(at + (kHalves + hh) * kBox, &v_map, bar, hh * 128, row);
+                cp_async_4(sc, a.c.k_scale_dev + bh);
+                cp_async_4(sc + 4, a.c.v_scale_dev + bh);
+            }
+            if (lane < kMaxBoxes) cp_async_arrive(bar);
+            if (i == 0 || now.k == 0) {                // an item's queries, while its first tile is on the way
+                if (items >= 2 && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.qempty[items & 1]), ((items >> 1) - 1) & 1, a.wait_budget))) {
+                    timed_out();
+                    ++i;
+                    break;
+                }
+                load_queries(now, items & 1);
+                ++items;
+            }
+            if (i + 1 < count) now.next(a, prefix, known);
+            if (++stage == a.stages) {
+                stage = 0;
+                ++round;
+            }
+        }
+        // nothing may be in flight when the CTA ends
+        for (int j = max(0, i - a.stages); j < i; ++j)
+            if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.full[j % a.stages]), (j / a.stages) & 1, a.wait_budget))) timed_out();
+    } else if (count > 0 && warp == kComputeWarps + 1) {
+        // ======== matrix instructions: S of the next tile is issued before O of this one ========
         int items = 0;
-        load_queries(cur, 0);
+        bool ok = true;
+        auto multiply_keys = [&](int i, const Cursor<kRows>& c) {
+            const int stage = i % a.stages;
+            if (i == 0 || c.k == 0) {
+                ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.qfull[items & 1]), (items >> 1) & 1, a.wait_budget));
+                ++items;
+            }
+            ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.full[stage]), (i / a.stages) & 1, a.wait_budget));
+            if (!ok) return;
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+                for (int hh = 0; hh < kHalves; ++hh)
+#pragma unroll
+                    for (int j = 0; j < kRowBytes / 32; ++j)
+                        mma_i8(tmem + (i & 1) * kColumns, make_kmajor_desc(base + stage * kStage + hh * kBox, kRowBytes) + 2 * j,
+                               make_kmajor_desc(base + off_q + ((items - 1) & 1) * kN * D + hh * kN * kRowBytes, kRowBytes) + 2 * j, kMulK, hh + j > 0);
+                mma_commit(smem_u32(&sh.sfull[i & 1]));
+            }
+            __syncwarp();
+        };
+        multiply_keys(0, cur);
+        for (int i = 0; i < count && ok; ++i) {
+            if (i + 1 < count) {
+                cur.next(a, prefix, known);
+                multiply_keys(i + 1, cur);
+            }
+            ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.pfull[i & 1]), (i >> 1) & 1, a.wait_budget));
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint32_t v = base + (i % a.stages) * kStage + kHalves * kBox;
+#pragma unroll
+                for (int hh = 0; hh < kHalves; ++hh)
+#pragma unroll
+                    for (int j = 0; j < kTile / 32; ++j)
+                        mma_i8(tmem + (2 + (i & 1) * kHalves + hh) * kColumns, make_mnmajor_desc(v + hh * kBox + j * 32 * kRowBytes, kRowBytes),
+                               make_kmajor_desc(base + off_p, 128) + 2 * j, kMulV, j > 0);
+                mma_commit(smem_u32(&sh.ofull[i & 1]));
+                mma_commit(smem_u32(&sh.empty[i % a.stages]));
+            }
+            __syncwarp();
+        }
+        if (!ok) {                                     // what was issued may still run: give it the same limit, then go
+            timed_out();
+            if (elect_one()) mma_commit(smem_u32(&sh.drain));
+            __syncwarp();
+            mbar_wait(smem_u32(&sh.drain), 0, a.wait_budget);
+        }
+    } else if (count > 0) {
+        // ======== compute: thread = token of S^T, then column of O^T ========
+        bool ok = true;
+        auto wait = [&](uint64_t& bar, int parity) {   // the warp goes on together
+            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar), parity, a.wait_budget)) && ok;
+        };
+        int items = 0;
         float m[kRows], l[kRows], acc[kHalves][kRows], keep[kRows];
         int seg_first = cur.k, stage = 0, round = 0;
         bool pending = false;                          // O of the tile before is still to be taken
@@ -542,7 +558,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         };
 
         auto take_sums = [&](int i) {
-            wait(s_ofull[i & 1], (i >> 1) & 1);
+            wait(sh.ofull[i & 1], (i >> 1) & 1);
             tc_fence_after();
 #pragma unroll
             for (int hh = 0; hh < kHalves; ++hh) {
@@ -555,20 +571,20 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         };
 
         for (int i = 0; i < count; ++i) {
-            const ItemInfo& it = s_item[items & 1];
+            const ItemInfo& it = sh.item[items & 1];
             const int pos0 = cur.pos(), pos = pos0 + tid;
             const bool last = cur.k == cur.s.tiles - 1, more = i + 1 < count;
-            if (i == 0 || cur.k == 0) wait(s_qfull, items & 1);
-            wait(s_full[stage], round & 1);
+            if (i == 0 || cur.k == 0) wait(sh.qfull[items & 1], (items >> 1) & 1);
+            wait(sh.full[stage], round & 1);
             // Scales lie in [2^-100, 2^122] here (the least is QTZ_KV_MIN_SCALE; no 16-bit value gives more than 2^121), so
             // that their logarithms and inverses are ordinary numbers.
-            const float2 scales = s_scales[stage][tid >> a.box_shift];
+            const float2 scales = sh.scales[stage][tid >> a.box_shift];
             const float ks = fminf(fmaxf(scales.x, QTZ_KV_MIN_SCALE), 5.3169120e36f), vs = fminf(fmaxf(scales.y, QTZ_KV_MIN_SCALE), 5.3169120e36f);
             if (++stage == a.stages) {
                 stage = 0;
                 ++round;
             }
-            wait(s_sfull[i & 1], (i >> 1) & 1);
+            wait(sh.sfull[i & 1], (i >> 1) & 1);
             tc_fence_after();
             float x[kRows];
             {
@@ -593,7 +609,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
             if (lane == 0)
 #pragma unroll
                 for (int r = 0; r < kRowsUp; r += 4)
-                    *reinterpret_cast<float4*>(&s_max[i & 1][warp][r]) = make_float4(top[r], top[r + 1], top[r + 2], top[r + 3]);
+                    *reinterpret_cast<float4*>(&sh.max[i & 1][warp][r]) = make_float4(top[r], top[r + 1], top[r + 2], top[r + 3]);
             ok = named_barrier_and(1, kComputeThreads, ok);
             if (!ok) break;
 #pragma unroll
@@ -602,25 +618,27 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
             for (int w = 0; w < kComputeWarps; ++w)
 #pragma unroll
                 for (int r = 0; r < kRowsUp; r += 4) {
-                    const float4 t = *reinterpret_cast<const float4*>(&s_max[i & 1][w][r]);
+                    const float4 t = *reinterpret_cast<const float4*>(&sh.max[i & 1][w][r]);
                     top[r] = fmaxf(top[r], t.x);
                     top[r + 1] = fmaxf(top[r + 1], t.y);
                     top[r + 2] = fmaxf(top[r + 2], t.z);
                     top[r + 3] = fmaxf(top[r + 3], t.w);
                 }
+            // O of the tile before: its product ran beside this tile's logits; after it the weights' place is free
+            if (pending) take_sums(i - 1);
+            pending = true;
             const float inv = __fdividef(1.f, vs);
-            float fresh[kRows];
             uint32_t bits[kRows];
 #pragma unroll
             for (int r = 0; r < kRows; ++r) {
                 const float origin = top[r] == -INFINITY ? 0.f : top[r];
-                fresh[r] = ex2(m[r] - origin);
+                keep[r] = ex2(m[r] - origin);
                 m[r] = top[r];
                 const float w = ex2(x[r] - origin);
-                l[r] = fmaf(w, inv, l[r] * fresh[r]);
+                l[r] = fmaf(w, inv, l[r] * keep[r]);
                 bits[r] = __float_as_uint(w + 2.f);    // w in [0, 1]: the mantissa is w in units of 2^-22, its bytes are the digits
             }
-            const uint32_t to = base + off_p + (i & 1) * kN * 128;
+            const uint32_t to = base + off_p;
 #pragma unroll
             for (int r = 0; r < kRows; ++r)
 #pragma unroll
@@ -631,29 +649,18 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
             tc_fence_before();
             fence_proxy_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&s_pfull[i & 1]));
-
-            // O of the tile before: its product ran beside this tile's softmax
-            if (pending) take_sums(i - 1);
-#pragma unroll
-            for (int r = 0; r < kRows; ++r) keep[r] = fresh[r];
-            pending = true;
+            if (lane == 0) mbar_arrive(smem_u32(&sh.pfull[i & 1]));
 
             if (!last && more) {
                 ++cur.k;
             } else {                                   // the end of the item, or of this CTA's part of it
-                Cursor<kRows> ahead = cur;
-                if (more) {
-                    ahead.next(a, prefix, known);
-                    load_queries(ahead, (items + 1) & 1);
-                }
                 take_sums(i);
                 pending = false;
 #pragma unroll
                 for (int r = 0; r < kRows; ++r) {
 #pragma unroll
                     for (int off = 16; off > 0; off >>= 1) l[r] += __shfl_xor_sync(0xffffffffu, l[r], off);
-                    if (lane == 0) s_sum[r][warp] = l[r];
+                    if (lane == 0) sh.sum[r][warp] = l[r];
                 }
                 ok = named_barrier_and(1, kComputeThreads, ok);
                 if (!ok) break;
@@ -662,7 +669,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                 float* part = a.parts + (static_cast<int64_t>(blockIdx.x) * 2 + (seg_first == 0 ? 1 : 0)) * kPart;
 #pragma unroll
                 for (int r = 0; r < kRows; ++r) {
-                    const float4 t = *reinterpret_cast<const float4*>(s_sum[r]);
+                    const float4 t = *reinterpret_cast<const float4*>(sh.sum[r]);
                     const float sum = (t.x + t.y) + (t.z + t.w);
                     float v[kHalves];
 #pragma unroll
@@ -690,11 +697,11 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                         named_barrier(1, kComputeThreads);
                         if (tid == 0) {
                             const int arrived = atomicAdd(counter, 1);
-                            s_last = arrived == others;
+                            sh.last = arrived == others;
                             if (arrived == others) *counter = 0;           // ready for the next call
                         }
                         named_barrier(1, kComputeThreads);
-                        const bool yes = s_last;
+                        const bool yes = sh.last;
                         __threadfence();
                         return yes;
                     };
@@ -711,15 +718,15 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                                 pm = __ldcg(p + row);
                                 pl = __ldcg(p + kMaxRows + row);
                             }
-                            s_join[0][tid / kMaxRows][row] = pm;
-                            s_join[1][tid / kMaxRows][row] = pl;
+                            join_with[0][tid / kMaxRows][row] = pm;
+                            join_with[1][tid / kMaxRows][row] = pl;
                             named_barrier(1, kComputeThreads);
                             float w[kRows];            // of what has been joined before
 #pragma unroll
                             for (int r = 0; r < kRows; ++r) {
                                 float top = done > 0 ? m[r] : -INFINITY;
 #pragma unroll
-                                for (int j = 0; j < kFanIn; ++j) top = fmaxf(top, s_join[0][j][r]);
+                                for (int j = 0; j < kFanIn; ++j) top = fmaxf(top, join_with[0][j][r]);
                                 const float origin = top == -INFINITY ? 0.f : top;
                                 w[r] = done > 0 && !(m[r] == -INFINITY && sum[r] == 0.f) ? ex2(m[r] - origin) : 0.f;
                                 m[r] = top;
@@ -733,7 +740,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                                 const float* p = part_of(from + (done + j) * step) + (D >= 128 || tid < D ? tid : 0);
 #pragma unroll
                                 for (int r = 0; r < kRows; ++r) {
-                                    const float jm = s_join[0][j][r], jl = s_join[1][j][r];
+                                    const float jm = join_with[0][j][r], jl = join_with[1][j][r];
                                     const float wt = jm == -INFINITY && jl == 0.f ? 0.f : ex2(jm - (m[r] == -INFINITY ? 0.f : m[r]));
                                     sum[r] = fmaf(jl, wt, sum[r]);
 #pragma unroll
@@ -773,10 +780,12 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                         }
                     named_barrier(1, kComputeThreads);
                 }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.qempty[items & 1]));
                 reset();
                 seg_first = 0;
                 ++items;
-                cur = ahead;
+                if (more) cur.next(a, prefix, known);
             }
         }
         if (!ok) timed_out();
@@ -797,8 +806,8 @@ qtz_status launch(qtz_ctx* h, AttnArgs& a, const CUtensorMap& km, const CUtensor
 {
     constexpr int kN = (3 * kRows + 15) / 16 * 16, kStage = 2 * kTile * D;
     const int ctas = ctas_per_sm(D);
-    const int fixed = 1024 + 2 * kN * 128 + kN * D + static_cast<int>(sizeof(uint32_t)) * (a.requests + 1);
-    const int room = kSmemLimit / ctas - 1024 - 3 * 1024 - fixed;   // 3 KB: the kernel's static shared memory
+    const int fixed = 1024 + kN * 128 + 2 * kN * D + static_cast<int>((sizeof(Shared) + 15) / 16 * 16 + sizeof(uint32_t) * (a.requests + 1));
+    const int room = (kSmemLimit + 1024) / ctas - 1024 - fixed;
     a.stages = room / kStage < kMaxStages ? room / kStage : kMaxStages;
     if (a.stages < 2) return QTZ_ERR_TOO_LARGE;
     const int smem = fixed + a.stages * kStage;
