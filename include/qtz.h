@@ -549,7 +549,7 @@ QTZ_API qtz_status qtz_kv_read(qtz_handle h, const qtz_kv_cache* cache, const in
  *   lse     NULL, or [tokens][q_heads] fp32: natural logarithm of the softmax's sum, for joining with other keys
  *   tokens  rows of q and y
  *   workspace  qtz_kv_attention_workspace_bytes(h, cache) bytes, 16-byte aligned, zero-filled once before its first use;
- *           one stream at a time.  Its size does not depend on lengths.
+ *           one stream at a time.  Its size does not depend on lengths.  After QTZ_ERR_DEVICE_TIMEOUT zero it again.
  * Codes meet fixed-point queries and weights in exact integer sums: a query keeps 22 bits below its row's largest value, a
  * softmax weight 22 bits below the largest weight so far; every other sum, maximum and statistic is fp32.  A query row that
  * holds NaN or an infinity gives NaN.

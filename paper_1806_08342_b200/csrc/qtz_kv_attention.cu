@@ -43,7 +43,7 @@ constexpr int kThreads = kComputeThreads + 64;   // + one warp for TMA, one for 
 constexpr int kMaxRows = 16;
 constexpr int kMaxStages = 6;
 constexpr int kMaxBoxes = 8;
-constexpr int kFanIn = kComputeThreads / kMaxRows;   // parts that one CTA joins at a time; more are joined in two steps
+constexpr int kFanIn = 32;                 // most parts that are joined in one step: the square of it covers any grid
 constexpr int kSmemLimit = 227 * 1024;     // most that a CTA may ask for; an SM has 1 KB more, and each CTA costs 1 KB more than it asks for
 
 struct AttnArgs {
@@ -184,6 +184,12 @@ struct ItemInfo {
     int32_t full_lo, full_hi;              // tokens that every row sees
 };
 
+// An item that lies in CTAs c0 .. c1 (c1 < 0: there is none).
+struct OpenItem {
+    int64_t out[kMaxRows], lse[kMaxRows];
+    int c0, c1;
+};
+
 // Shared memory of a CTA beside the ring, the operands and the prefix sums.
 struct Shared {
     float max[2][kComputeWarps][kMaxRows], sum[kMaxRows][kComputeWarps];
@@ -191,8 +197,9 @@ struct Shared {
     float2 scales[kMaxStages][kMaxBoxes];  // (k, v) of each box; negative: there is none
     uint64_t full[kMaxStages], empty[kMaxStages], sfull[2], pfull[2], ofull[2], qfull[2], qempty[2], drain;
     KnownRequests known;
+    OpenItem open[2];                      // begun in an earlier CTA; going on in the next
     uint32_t scan[kThreads / 32], tmem;
-    int last;
+    int last[2], failed;
 };
 
 template <typename T, int D, int kRows>
@@ -220,9 +227,10 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
     uint32_t* const prefix = reinterpret_cast<uint32_t*>(smem + off_prefix);
     Shared& sh = *reinterpret_cast<Shared*>(smem + off_shared);
     KnownRequests& known = sh.known;
-    float (*const join_with)[kFanIn][kMaxRows] = reinterpret_cast<float (*)[kFanIn][kMaxRows]>(smem + off_p);   // while no weights are there
 
     if (tid == 0) {
+        sh.open[0].c1 = sh.open[1].c1 = -1;
+        sh.failed = 0;
         prefetch_tensormap(&k_map);
         prefetch_tensormap(&v_map);
         for (int i = 0; i < kMaxStages; ++i) {
@@ -237,7 +245,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         mbar_init(smem_u32(&sh.pfull[0]), kComputeWarps);
         mbar_init(smem_u32(&sh.pfull[1]), kComputeWarps);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(smem_u32(&sh.qfull[i]), 1);
+            mbar_init(smem_u32(&sh.qfull[i]), kComputeWarps);
             mbar_init(smem_u32(&sh.qempty[i]), kComputeWarps);
         }
         fence_barrier_init();
@@ -300,6 +308,98 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
     Cursor<kRows> cur;
     if (count > 0) cur.seek(a, prefix, known, t0);
 
+            // Digits of an item's query rows into the operand, and what the softmax has to know of them.
+            auto load_queries = [&](auto parts_tag, const Cursor<kRows>& c, int which, int mine) {
+                constexpr int kParts = decltype(parts_tag)::value, kMine = (kRows + kParts - 1) / kParts;   // rows r = mine + j kParts
+                ItemInfo& it = sh.item[which];
+                constexpr int kPer = D / 32;               // values of a row that a lane holds
+                // lane r finds row r
+                const int h = c.head(), index = (c.item - h * c.s.row_tiles) * kRows + lane, local = index / a.group;
+                const int head = h * a.group + (index - local * a.group);
+                const bool has = lane < kRows && local < c.s.added;
+                const int64_t token = c.s.first + local, from = has ? token * a.q_token_stride + head * a.q_head_stride : -1;
+                uint32_t raw[kMine][kPer / 2];
+    #pragma unroll
+                for (int j = 0; j < kMine; ++j) {
+                    const int64_t at = __shfl_sync(0xffffffffu, from, mine + j * kParts);
+                    const T* q = static_cast<const T*>(a.q) + at + lane * kPer;
+    #pragma unroll
+                    for (int k = 0; k < kPer / 2; ++k) raw[j][k] = 0;
+                    if (at < 0) continue;                  // no lane from kRows on holds a row
+                    if constexpr (kPer == 2) {
+                        raw[j][0] = *reinterpret_cast<const uint32_t*>(q);
+                    } else if constexpr (kPer == 4) {
+                        const uint2 u = *reinterpret_cast<const uint2*>(q);
+                        raw[j][0] = u.x; raw[j][1] = u.y;
+                    } else {
+                        const uint4 u = *reinterpret_cast<const uint4*>(q);
+                        raw[j][0] = u.x; raw[j][1] = u.y; raw[j][2] = u.z; raw[j][3] = u.w;
+                    }
+                }
+                if (mine == 0) {
+                    const int own = c.s.len - c.s.added + local + 1;   // tokens up to the row's own
+                    const int end = has ? min(own, c.s.limit) : 0x7fffffff, begin = has && a.window > 0 ? max(0, own - a.window) : 0;
+                    if (lane < kRows) {
+                        it.begin[lane] = begin;
+                        it.end[lane] = end;
+                        it.out[lane] = has ? token * a.y_token_stride + head * a.y_head_stride : -1;
+                        it.lse[lane] = token * a.q_heads + head;
+                    }
+                    const int lo = __reduce_max_sync(0xffffffffu, begin), hi = __reduce_min_sync(0xffffffffu, end);
+                    if (lane == 0) {
+                        it.full_lo = lo;
+                        it.full_hi = hi;
+                    }
+                }
+    #pragma unroll
+                for (int j = 0; j < kMine; ++j) {
+                    const int r = mine + j * kParts;
+                    if (r >= kRows) break;
+                    float v[kPer], top = 0.f;
+                    bool odd = false;
+    #pragma unroll
+                    for (int k = 0; k < kPer / 2; ++k) {
+                        const float2 f = qtz_dev::unpack2(raw[j][k], T());
+                        v[2 * k] = f.x;
+                        v[2 * k + 1] = f.y;
+                    }
+    #pragma unroll
+                    for (int k = 0; k < kPer; ++k) {
+                        odd = odd || (__float_as_uint(v[k]) & 0x7f800000u) == 0x7f800000u;
+                        top = fmaxf(top, fabsf(v[k]));
+                    }
+                    top = redux_max(top);
+                    odd = __any_sync(0xffffffffu, odd);
+                    // rows below 2^-100 count as 2^-100 (their logits are zero either way)
+                    const int ex = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -100), 127);
+                    const float mult = __uint_as_float(static_cast<uint32_t>(127 + 21 - ex) << 23);
+                    uint64_t digits[3] = {0, 0, 0};
+    #pragma unroll
+                    for (int k = 0; k < kPer; ++k) {
+                        const int x = odd ? 0 : __float2int_rn(v[k] * mult);
+                        const int d0 = (x << 24) >> 24, x1 = (x - d0) >> 8, d1 = (x1 << 24) >> 24, d2 = (x1 - d1) >> 8;
+                        digits[0] |= static_cast<uint64_t>(d0 & 0xff) << (8 * k);
+                        digits[1] |= static_cast<uint64_t>(d1 & 0xff) << (8 * k);
+                        digits[2] |= static_cast<uint64_t>(d2 & 0xff) << (8 * k);
+                    }
+                    const int d = lane * kPer, hh = d / 128, x = d % kRowBytes;
+    #pragma unroll
+                    for (int g = 0; g < 3; ++g) {
+                        const int n = g * kRows + r, swz = kRowBytes == 128 ? (n & 7) : ((n >> 1) & 3);
+                        uint8_t* to = smem + off_q + which * kN * D + hh * kN * kRowBytes + n * kRowBytes + (((x >> 4) ^ swz) << 4) + (x & 15);
+                        if constexpr (kPer == 2) *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(digits[g]);
+                        else if constexpr (kPer == 4) *reinterpret_cast<uint32_t*>(to) = static_cast<uint32_t>(digits[g]);
+                        else *reinterpret_cast<uint64_t*>(to) = digits[g];
+                    }
+                    // a row that holds NaN or infinity gives NaN
+                    if (lane == 0) it.factor[r] = odd ? __uint_as_float(0x7fc00000u) : a.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 - 21 + ex) << 23);
+                }
+                fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_n(smem_u32(&sh.qfull[which]), kComputeWarps / kParts);
+            };
+
+
     if (count > 0 && warp == kComputeWarps) {
         // ======== producer: lane j brings box j of the tile, and its scales ========
         // Table entries are requested kAhead tiles before they are needed, and the scales travel like the boxes, by asynchronous
@@ -325,94 +425,6 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
             if (j > 0) cur.next(a, prefix, known);
             request_entry(id[j], offset[j], head[j]);
         }
-        // Digits of an item's query rows into the operand, and what the softmax has to know of them.
-        auto load_queries = [&](const Cursor<kRows>& c, int which) {
-            ItemInfo& it = sh.item[which];
-            constexpr int kPer = D / 32;               // values of a row that a lane holds
-            // lane r finds row r
-            const int h = c.head(), index = (c.item - h * c.s.row_tiles) * kRows + lane, local = index / a.group;
-            const int head = h * a.group + (index - local * a.group);
-            const bool has = lane < kRows && local < c.s.added;
-            const int64_t token = c.s.first + local, from = has ? token * a.q_token_stride + head * a.q_head_stride : -1;
-            uint32_t raw[kRows][kPer / 2];
-#pragma unroll
-            for (int r = 0; r < kRows; ++r) {
-                const int64_t at = __shfl_sync(0xffffffffu, from, r);
-                const T* q = static_cast<const T*>(a.q) + at + lane * kPer;
-#pragma unroll
-                for (int k = 0; k < kPer / 2; ++k) raw[r][k] = 0;
-                if (at < 0) continue;
-                if constexpr (kPer == 2) {
-                    raw[r][0] = *reinterpret_cast<const uint32_t*>(q);
-                } else if constexpr (kPer == 4) {
-                    const uint2 u = *reinterpret_cast<const uint2*>(q);
-                    raw[r][0] = u.x; raw[r][1] = u.y;
-                } else {
-                    const uint4 u = *reinterpret_cast<const uint4*>(q);
-                    raw[r][0] = u.x; raw[r][1] = u.y; raw[r][2] = u.z; raw[r][3] = u.w;
-                }
-            }
-            {
-                const int own = c.s.len - c.s.added + local + 1;   // tokens up to the row's own
-                const int end = has ? min(own, c.s.limit) : 0x7fffffff, begin = has && a.window > 0 ? max(0, own - a.window) : 0;
-                if (lane < kRows) {
-                    it.begin[lane] = begin;
-                    it.end[lane] = end;
-                    it.out[lane] = has ? token * a.y_token_stride + head * a.y_head_stride : -1;
-                    it.lse[lane] = token * a.q_heads + head;
-                }
-                const int lo = __reduce_max_sync(0xffffffffu, begin), hi = __reduce_min_sync(0xffffffffu, end);
-                if (lane == 0) {
-                    it.full_lo = lo;
-                    it.full_hi = hi;
-                }
-            }
-#pragma unroll
-            for (int r = 0; r < kRows; ++r) {
-                float v[kPer], top = 0.f;
-                bool odd = false;
-#pragma unroll
-                for (int k = 0; k < kPer / 2; ++k) {
-                    const float2 f = qtz_dev::unpack2(raw[r][k], T());
-                    v[2 * k] = f.x;
-                    v[2 * k + 1] = f.y;
-                }
-#pragma unroll
-                for (int k = 0; k < kPer; ++k) {
-                    odd = odd || (__float_as_uint(v[k]) & 0x7f800000u) == 0x7f800000u;
-                    top = fmaxf(top, fabsf(v[k]));
-                }
-                top = redux_max(top);
-                odd = __any_sync(0xffffffffu, odd);
-                // rows below 2^-100 count as 2^-100 (their logits are zero either way)
-                const int ex = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -100), 127);
-                const float mult = __uint_as_float(static_cast<uint32_t>(127 + 21 - ex) << 23);
-                uint64_t digits[3] = {0, 0, 0};
-#pragma unroll
-                for (int k = 0; k < kPer; ++k) {
-                    const int x = odd ? 0 : __float2int_rn(v[k] * mult);
-                    const int d0 = (x << 24) >> 24, x1 = (x - d0) >> 8, d1 = (x1 << 24) >> 24, d2 = (x1 - d1) >> 8;
-                    digits[0] |= static_cast<uint64_t>(d0 & 0xff) << (8 * k);
-                    digits[1] |= static_cast<uint64_t>(d1 & 0xff) << (8 * k);
-                    digits[2] |= static_cast<uint64_t>(d2 & 0xff) << (8 * k);
-                }
-                const int d = lane * kPer, hh = d / 128, x = d % kRowBytes;
-#pragma unroll
-                for (int g = 0; g < 3; ++g) {
-                    const int n = g * kRows + r, swz = kRowBytes == 128 ? (n & 7) : ((n >> 1) & 3);
-                    uint8_t* to = smem + off_q + which * kN * D + hh * kN * kRowBytes + n * kRowBytes + (((x >> 4) ^ swz) << 4) + (x & 15);
-                    if constexpr (kPer == 2) *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(digits[g]);
-                    else if constexpr (kPer == 4) *reinterpret_cast<uint32_t*>(to) = static_cast<uint32_t>(digits[g]);
-                    else *reinterpret_cast<uint64_t*>(to) = digits[g];
-                }
-                // a row that holds NaN or infinity gives NaN
-                if (lane == 0) it.factor[r] = odd ? __uint_as_float(0x7fc00000u) : a.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 - 21 + ex) << 23);
-            }
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sh.qfull[which]));
-        };
-
         Cursor<kRows> now = first;
         int i = 0, stage = 0, round = 0, items = 0;
         for (; i < count; ++i) {
@@ -457,13 +469,15 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                 cp_async_4(sc + 4, a.c.v_scale_dev + bh);
             }
             if (lane < kMaxBoxes) cp_async_arrive(bar);
-            if (i == 0 || now.k == 0) {                // an item's queries, while its first tile is on the way
+            // An item's queries, while its first tile is on the way; the compute warps have nothing else to do for the first.
+            if (i == 0) ++items;
+            else if (now.k == 0) {
                 if (items >= 2 && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.qempty[items & 1]), ((items >> 1) - 1) & 1, a.wait_budget))) {
                     timed_out();
                     ++i;
                     break;
                 }
-                load_queries(now, items & 1);
+                load_queries(std::integral_constant<int, 1>(), now, items & 1, 0);
                 ++items;
             }
             if (i + 1 < count) now.next(a, prefix, known);
@@ -533,6 +547,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         auto wait = [&](uint64_t& bar, int parity) {   // the warp goes on together
             ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar), parity, a.wait_budget)) && ok;
         };
+        load_queries(std::integral_constant<int, kComputeWarps>(), cur, 0, warp);
         int items = 0;
         float m[kRows], l[kRows], acc[kHalves][kRows], keep[kRows];
         int seg_first = cur.k, stage = 0, round = 0;
@@ -687,98 +702,16 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                         part[kMaxRows * D + kMaxRows + r] = sum;
                     }
                 }
-                if (!whole) {
-                    // Parts of CTAs c0 .. c1.  The last of each group of kFanIn neighbours to arrive joins them into the place of
-                    // the group's first; with several groups, the last of those joins the groups.  Always in the same order.
-                    const int c0 = static_cast<int>(cur.begin) / share, c1 = static_cast<int>(cur.begin + cur.s.tiles - 1) / share;
-                    auto part_of = [&](int cta) { return a.parts + (static_cast<int64_t>(cta) * 2 + (cta == c0 ? 1 : 0)) * kPart; };
-                    auto arrives_last = [&](int32_t* counter, int others) {
-                        __threadfence();
-                        named_barrier(1, kComputeThreads);
-                        if (tid == 0) {
-                            const int arrived = atomicAdd(counter, 1);
-                            sh.last = arrived == others;
-                            if (arrived == others) *counter = 0;           // ready for the next call
-                        }
-                        named_barrier(1, kComputeThreads);
-                        const bool yes = sh.last;
-                        __threadfence();
-                        return yes;
-                    };
-                    // Joins the parts of CTAs from, from + step, .. to into acc, m and sum, kFanIn at a time: their maxima and
-                    // denominators come by one load of each thread, and become weights in shared memory.
-                    float sum[kRows];
-                    auto join = [&](int from, int to, int step) {
-                        const int n = (to - from) / step + 1;
-                        for (int done = 0; done < n; done += kFanIn) {
-                            const int part = done + tid / kMaxRows, row = tid % kMaxRows;
-                            float pm = -INFINITY, pl = 0.f;
-                            if (part < n && row < kRows) {
-                                const float* p = part_of(from + part * step) + kMaxRows * D;
-                                pm = __ldcg(p + row);
-                                pl = __ldcg(p + kMaxRows + row);
-                            }
-                            join_with[0][tid / kMaxRows][row] = pm;
-                            join_with[1][tid / kMaxRows][row] = pl;
-                            named_barrier(1, kComputeThreads);
-                            float w[kRows];            // of what has been joined before
-#pragma unroll
-                            for (int r = 0; r < kRows; ++r) {
-                                float top = done > 0 ? m[r] : -INFINITY;
-#pragma unroll
-                                for (int j = 0; j < kFanIn; ++j) top = fmaxf(top, join_with[0][j][r]);
-                                const float origin = top == -INFINITY ? 0.f : top;
-                                w[r] = done > 0 && !(m[r] == -INFINITY && sum[r] == 0.f) ? ex2(m[r] - origin) : 0.f;
-                                m[r] = top;
-                                sum[r] = done > 0 ? sum[r] * w[r] : 0.f;
-#pragma unroll
-                                for (int hh = 0; hh < kHalves; ++hh) acc[hh][r] = done > 0 ? acc[hh][r] * w[r] : 0.f;
-                            }
-                            const int here = min(kFanIn, n - done);
-#pragma unroll 4
-                            for (int j = 0; j < here; ++j) {
-                                const float* p = part_of(from + (done + j) * step) + (D >= 128 || tid < D ? tid : 0);
-#pragma unroll
-                                for (int r = 0; r < kRows; ++r) {
-                                    const float jm = join_with[0][j][r], jl = join_with[1][j][r];
-                                    const float wt = jm == -INFINITY && jl == 0.f ? 0.f : ex2(jm - (m[r] == -INFINITY ? 0.f : m[r]));
-                                    sum[r] = fmaf(jl, wt, sum[r]);
-#pragma unroll
-                                    for (int hh = 0; hh < kHalves; ++hh) acc[hh][r] = fmaf(__ldcg(p + r * D + hh * 128), wt, acc[hh][r]);
-                                }
-                            }
-                            named_barrier(1, kComputeThreads);
-                        }
-                    };
-                    const int me = static_cast<int>(blockIdx.x), groups = (c1 - c0) / kFanIn + 1, first = me - (me - c0) % kFanIn;
-                    bool mine = arrives_last(a.counters + 2 * first + (first == c0 ? 1 : 0), min(first + kFanIn - 1, c1) - first);
-                    if (mine) {
-                        join(first, min(first + kFanIn - 1, c1), 1);
-                        if (groups > 1) {
-                            float* to = part_of(first);
-#pragma unroll
-                            for (int r = 0; r < kRows; ++r) {
-                                if (D >= 128 || tid < D)
-#pragma unroll
-                                    for (int hh = 0; hh < kHalves; ++hh) to[r * D + hh * 128 + tid] = acc[hh][r];
-                                if (tid == 0) {
-                                    to[kMaxRows * D + r] = m[r];
-                                    to[kMaxRows * D + kMaxRows + r] = sum[r];
-                                }
-                            }
-                            mine = arrives_last(a.counters + 2 * gridDim.x + c0, groups - 1);
-                            if (mine) join(c0, c1, kFanIn);
-                        }
+                if (!whole) {                          // joined below
+                    OpenItem& open = sh.open[seg_first == 0 ? 1 : 0];
+                    if (tid < kRows) {
+                        open.out[tid] = it.out[tid];
+                        open.lse[tid] = it.lse[tid];
                     }
-                    if (mine && (D >= 128 || tid < D))
-#pragma unroll
-                        for (int r = 0; r < kRows; ++r) {
-                            float v[kHalves];
-#pragma unroll
-                            for (int hh = 0; hh < kHalves; ++hh) v[hh] = acc[hh][r];
-                            write_row(it, r, m[r], sum[r], v, tid);
-                        }
-                    named_barrier(1, kComputeThreads);
+                    if (tid == 0) {
+                        open.c0 = static_cast<int>(cur.begin) / share;
+                        open.c1 = static_cast<int>(cur.begin + cur.s.tiles - 1) / share;
+                    }
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&sh.qempty[items & 1]));
@@ -788,14 +721,114 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                 if (more) cur.next(a, prefix, known);
             }
         }
-        if (!ok) timed_out();
+        if (!ok) {
+            timed_out();
+            sh.failed = 1;
+        }
     }
 
     tc_fence_before();
+    __threadfence();                                   // the parts, before they are counted
     __syncthreads();
     if (warp == kComputeWarps + 1) {
         tc_fence_after();
         tmem_dealloc(tmem, kTmemColumns);
+    }
+
+    // ======== joining: items that lie in several CTAs, c0 .. c1 ========
+    // The last CTA of each group of neighbours to arrive joins the group's parts into the place of its first; with several
+    // groups, the last of those joins the groups.  Always in the order of the tiles.  (After a wait that gave up nothing is
+    // joined: the results are void, and the counters have to be cleared.)
+    if (sh.failed) return;
+    const int me = static_cast<int>(blockIdx.x);
+    auto group_size = [](int n) {                      // about the square root: both steps join at most kFanIn parts
+        int g = 4;
+        while (g * g < n) ++g;
+        return n <= 8 ? n : g;
+    };
+    if (lane == 0 && warp < 2 && sh.open[warp].c1 >= 0) {
+        const OpenItem& open = sh.open[warp];
+        const int size = group_size(open.c1 - open.c0 + 1), first = me - (me - open.c0) % size, others = min(size - 1, open.c1 - first);
+        int32_t* counter = a.counters + 2 * first + (first == open.c0 ? 1 : 0);
+        sh.last[warp] = atomicAdd(counter, 1) == others;
+        if (sh.last[warp]) *counter = 0;               // ready for the next call
+    }
+    __syncthreads();
+    float (*const jm)[kMaxRows] = reinterpret_cast<float (*)[kMaxRows]>(smem), (*const jl)[kMaxRows] = jm + kFanIn, (*const jw)[kMaxRows] = jl + kFanIn;
+    float* const j_top = reinterpret_cast<float*>(jw + kFanIn), * const j_sum = j_top + kMaxRows;
+    for (int slot = 0; slot < 2; ++slot) {
+        const OpenItem& open = sh.open[slot];
+        if (open.c1 < 0 || !sh.last[slot]) continue;
+        __threadfence();
+        const int c0 = open.c0, c1 = open.c1, size = group_size(c1 - c0 + 1), groups = (c1 - c0) / size + 1, first = me - (me - c0) % size;
+        auto part_of = [&](int cta) { return a.parts + (static_cast<int64_t>(cta) * 2 + (cta == c0 ? 1 : 0)) * kPart; };
+        // Joins the n parts of CTAs from, from + step, ..: into `to`, or into the output.
+        auto join = [&](int from, int step, int n, float* to) {
+            for (int i = tid; i < n * kMaxRows; i += kThreads) {
+                const float* p = part_of(from + i / kMaxRows * step) + kMaxRows * D + i % kMaxRows;
+                jm[i / kMaxRows][i % kMaxRows] = __ldcg(p);
+                jl[i / kMaxRows][i % kMaxRows] = __ldcg(p + kMaxRows);
+            }
+            __syncthreads();
+            for (int i = tid; i < n * kMaxRows; i += kThreads) {
+                const int j = i / kMaxRows, r = i % kMaxRows;
+                float top = -INFINITY;
+                for (int x = 0; x < n; ++x) top = fmaxf(top, jm[x][r]);
+                const float mj = jm[j][r], lj = jl[j][r];
+                jw[j][r] = mj == -INFINITY && lj == 0.f ? 0.f : ex2(mj - (top == -INFINITY ? 0.f : top));
+                if (j == 0) j_top[r] = top;
+            }
+            __syncthreads();
+            if (tid < kMaxRows) {
+                float sum = 0.f;
+                for (int x = 0; x < n; ++x) sum = fmaf(jl[x][tid], jw[x][tid], sum);
+                j_sum[tid] = sum;
+            }
+            __syncthreads();
+            for (int u = tid; u < kRows * D / 4; u += kThreads) {
+                const int r = u / (D / 4), d = u % (D / 4) * 4;
+                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 9
+                for (int x = 0; x < n; ++x) {
+                    const float4 p = __ldcg(reinterpret_cast<const float4*>(part_of(from + x * step) + r * D + d));
+                    const float w = jw[x][r];
+                    v.x = fmaf(p.x, w, v.x);
+                    v.y = fmaf(p.y, w, v.y);
+                    v.z = fmaf(p.z, w, v.z);
+                    v.w = fmaf(p.w, w, v.w);
+                }
+                if (to) {
+                    *reinterpret_cast<float4*>(to + r * D + d) = v;
+                    if (d == 0) {
+                        to[kMaxRows * D + r] = j_top[r];
+                        to[kMaxRows * D + kMaxRows + r] = j_sum[r];
+                    }
+                } else if (open.out[r] >= 0) {
+                    const float sum = j_sum[r], inv = sum == 0.f ? 0.f : __fdiv_rn(1.f, sum);
+                    uint2 o;
+                    o.x = qtz_dev::pack2(v.x * inv, v.y * inv, T());
+                    o.y = qtz_dev::pack2(v.z * inv, v.w * inv, T());
+                    *reinterpret_cast<uint2*>(static_cast<T*>(a.y) + open.out[r] + d) = o;
+                    if (d == 0 && a.lse) a.lse[open.lse[r]] = sum == 0.f ? -INFINITY : (j_top[r] + log2f(sum)) * 0.693147181f;
+                }
+            }
+        };
+        join(first, 1, min(size, c1 - first + 1), groups > 1 ? part_of(first) : nullptr);
+        if (groups > 1) {
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) {
+                int32_t* counter = a.counters + 2 * gridDim.x + c0;
+                sh.last[slot] = atomicAdd(counter, 1) == groups - 1;
+                if (sh.last[slot]) *counter = 0;
+            }
+            __syncthreads();
+            if (sh.last[slot]) {
+                __threadfence();
+                join(c0, size, groups, nullptr);
+            }
+        }
+        __syncthreads();
     }
 }
 
