@@ -195,7 +195,7 @@ struct Shared {
     float max[2][kComputeWarps][kMaxRows], sum[kMaxRows][kComputeWarps];
     ItemInfo item[2];
     float2 scales[kMaxStages][kMaxBoxes];  // (k, v) of each box; negative: there is none
-    uint64_t full[kMaxStages], empty[kMaxStages], sfull[2], pfull[2], ofull[2], qfull[2], qempty[2], drain;
+    uint64_t full[kMaxStages], empty[kMaxStages], sfull[2], pfull[2], ofull[2], qfull, drain;
     KnownRequests known;
     OpenItem open[2];                      // begun in an earlier CTA; going on in the next
     uint32_t scan[kThreads / 32], tmem;
@@ -223,7 +223,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* const smem = smem_raw + (base - smem_u32(smem_raw));
-    const uint32_t off_p = a.stages * kStage, off_q = off_p + kN * 128, off_shared = off_q + 2 * kN * D, off_prefix = off_shared + (sizeof(Shared) + 15) / 16 * 16;
+    const uint32_t off_p = a.stages * kStage, off_q = off_p + kN * 128, off_shared = off_q + kN * D, off_prefix = off_shared + (sizeof(Shared) + 15) / 16 * 16;
     uint32_t* const prefix = reinterpret_cast<uint32_t*>(smem + off_prefix);
     Shared& sh = *reinterpret_cast<Shared*>(smem + off_shared);
     KnownRequests& known = sh.known;
@@ -244,10 +244,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         mbar_init(smem_u32(&sh.drain), 1);
         mbar_init(smem_u32(&sh.pfull[0]), kComputeWarps);
         mbar_init(smem_u32(&sh.pfull[1]), kComputeWarps);
-        for (int i = 0; i < 2; ++i) {
-            mbar_init(smem_u32(&sh.qfull[i]), kComputeWarps);
-            mbar_init(smem_u32(&sh.qempty[i]), kComputeWarps);
-        }
+        mbar_init(smem_u32(&sh.qfull), kComputeWarps);
         fence_barrier_init();
     }
     if (warp == kComputeWarps + 1) {
@@ -308,105 +305,12 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
     Cursor<kRows> cur;
     if (count > 0) cur.seek(a, prefix, known, t0);
 
-            // Digits of an item's query rows into the operand, and what the softmax has to know of them.
-            auto load_queries = [&](auto parts_tag, const Cursor<kRows>& c, int which, int mine) {
-                constexpr int kParts = decltype(parts_tag)::value, kMine = (kRows + kParts - 1) / kParts;   // rows r = mine + j kParts
-                ItemInfo& it = sh.item[which];
-                constexpr int kPer = D / 32;               // values of a row that a lane holds
-                // lane r finds row r
-                const int h = c.head(), index = (c.item - h * c.s.row_tiles) * kRows + lane, local = index / a.group;
-                const int head = h * a.group + (index - local * a.group);
-                const bool has = lane < kRows && local < c.s.added;
-                const int64_t token = c.s.first + local, from = has ? token * a.q_token_stride + head * a.q_head_stride : -1;
-                uint32_t raw[kMine][kPer / 2];
-    #pragma unroll
-                for (int j = 0; j < kMine; ++j) {
-                    const int64_t at = __shfl_sync(0xffffffffu, from, mine + j * kParts);
-                    const T* q = static_cast<const T*>(a.q) + at + lane * kPer;
-    #pragma unroll
-                    for (int k = 0; k < kPer / 2; ++k) raw[j][k] = 0;
-                    if (at < 0) continue;                  // no lane from kRows on holds a row
-                    if constexpr (kPer == 2) {
-                        raw[j][0] = *reinterpret_cast<const uint32_t*>(q);
-                    } else if constexpr (kPer == 4) {
-                        const uint2 u = *reinterpret_cast<const uint2*>(q);
-                        raw[j][0] = u.x; raw[j][1] = u.y;
-                    } else {
-                        const uint4 u = *reinterpret_cast<const uint4*>(q);
-                        raw[j][0] = u.x; raw[j][1] = u.y; raw[j][2] = u.z; raw[j][3] = u.w;
-                    }
-                }
-                if (mine == 0) {
-                    const int own = c.s.len - c.s.added + local + 1;   // tokens up to the row's own
-                    const int end = has ? min(own, c.s.limit) : 0x7fffffff, begin = has && a.window > 0 ? max(0, own - a.window) : 0;
-                    if (lane < kRows) {
-                        it.begin[lane] = begin;
-                        it.end[lane] = end;
-                        it.out[lane] = has ? token * a.y_token_stride + head * a.y_head_stride : -1;
-                        it.lse[lane] = token * a.q_heads + head;
-                    }
-                    const int lo = __reduce_max_sync(0xffffffffu, begin), hi = __reduce_min_sync(0xffffffffu, end);
-                    if (lane == 0) {
-                        it.full_lo = lo;
-                        it.full_hi = hi;
-                    }
-                }
-    #pragma unroll
-                for (int j = 0; j < kMine; ++j) {
-                    const int r = mine + j * kParts;
-                    if (r >= kRows) break;
-                    float v[kPer], top = 0.f;
-                    bool odd = false;
-    #pragma unroll
-                    for (int k = 0; k < kPer / 2; ++k) {
-                        const float2 f = qtz_dev::unpack2(raw[j][k], T());
-                        v[2 * k] = f.x;
-                        v[2 * k + 1] = f.y;
-                    }
-    #pragma unroll
-                    for (int k = 0; k < kPer; ++k) {
-                        odd = odd || (__float_as_uint(v[k]) & 0x7f800000u) == 0x7f800000u;
-                        top = fmaxf(top, fabsf(v[k]));
-                    }
-                    top = redux_max(top);
-                    odd = __any_sync(0xffffffffu, odd);
-                    // rows below 2^-100 count as 2^-100 (their logits are zero either way)
-                    const int ex = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -100), 127);
-                    const float mult = __uint_as_float(static_cast<uint32_t>(127 + 21 - ex) << 23);
-                    uint64_t digits[3] = {0, 0, 0};
-    #pragma unroll
-                    for (int k = 0; k < kPer; ++k) {
-                        const int x = odd ? 0 : __float2int_rn(v[k] * mult);
-                        const int d0 = (x << 24) >> 24, x1 = (x - d0) >> 8, d1 = (x1 << 24) >> 24, d2 = (x1 - d1) >> 8;
-                        digits[0] |= static_cast<uint64_t>(d0 & 0xff) << (8 * k);
-                        digits[1] |= static_cast<uint64_t>(d1 & 0xff) << (8 * k);
-                        digits[2] |= static_cast<uint64_t>(d2 & 0xff) << (8 * k);
-                    }
-                    const int d = lane * kPer, hh = d / 128, x = d % kRowBytes;
-    #pragma unroll
-                    for (int g = 0; g < 3; ++g) {
-                        const int n = g * kRows + r, swz = kRowBytes == 128 ? (n & 7) : ((n >> 1) & 3);
-                        uint8_t* to = smem + off_q + which * kN * D + hh * kN * kRowBytes + n * kRowBytes + (((x >> 4) ^ swz) << 4) + (x & 15);
-                        if constexpr (kPer == 2) *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(digits[g]);
-                        else if constexpr (kPer == 4) *reinterpret_cast<uint32_t*>(to) = static_cast<uint32_t>(digits[g]);
-                        else *reinterpret_cast<uint64_t*>(to) = digits[g];
-                    }
-                    // a row that holds NaN or infinity gives NaN
-                    if (lane == 0) it.factor[r] = odd ? __uint_as_float(0x7fc00000u) : a.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 - 21 + ex) << 23);
-                }
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_n(smem_u32(&sh.qfull[which]), kComputeWarps / kParts);
-            };
-
-
-    if (count > 0 && warp == kComputeWarps) {
+            if (count > 0 && warp == kComputeWarps) {
         // ======== producer: lane j brings box j of the tile, and its scales ========
         // Table entries are requested kAhead tiles before they are needed, and the scales travel like the boxes, by asynchronous
         // copies that the tile's barrier counts: the producer waits for no look-up (under load one takes longer than a tile).
         const int box_rows = 1 << a.box_shift, boxes = kTile >> a.box_shift;
         constexpr int kAhead = 4;
-        const Cursor<kRows> first = cur;
         int id[kAhead], offset[kAhead], head[kAhead];  // offset: within the block, -1 where there is nothing to bring
         auto request_entry = [&](int& e, int& o, int& h) {
             const int pos = cur.pos() + lane * box_rows;
@@ -425,8 +329,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
             if (j > 0) cur.next(a, prefix, known);
             request_entry(id[j], offset[j], head[j]);
         }
-        Cursor<kRows> now = first;
-        int i = 0, stage = 0, round = 0, items = 0;
+        int i = 0, stage = 0, round = 0;
         for (; i < count; ++i) {
             int row = -1;
             int64_t bh = 0;
@@ -469,18 +372,6 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                 cp_async_4(sc + 4, a.c.v_scale_dev + bh);
             }
             if (lane < kMaxBoxes) cp_async_arrive(bar);
-            // An item's queries, while its first tile is on the way; the compute warps have nothing else to do for the first.
-            if (i == 0) ++items;
-            else if (now.k == 0) {
-                if (items >= 2 && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.qempty[items & 1]), ((items >> 1) - 1) & 1, a.wait_budget))) {
-                    timed_out();
-                    ++i;
-                    break;
-                }
-                load_queries(std::integral_constant<int, 1>(), now, items & 1, 0);
-                ++items;
-            }
-            if (i + 1 < count) now.next(a, prefix, known);
             if (++stage == a.stages) {
                 stage = 0;
                 ++round;
@@ -496,7 +387,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         auto multiply_keys = [&](int i, const Cursor<kRows>& c) {
             const int stage = i % a.stages;
             if (i == 0 || c.k == 0) {
-                ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.qfull[items & 1]), (items >> 1) & 1, a.wait_budget));
+                ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.qfull), items & 1, a.wait_budget));
                 ++items;
             }
             ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.full[stage]), (i / a.stages) & 1, a.wait_budget));
@@ -508,7 +399,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
 #pragma unroll
                     for (int j = 0; j < kRowBytes / 32; ++j)
                         mma_i8(tmem + (i & 1) * kColumns, make_kmajor_desc(base + stage * kStage + hh * kBox, kRowBytes) + 2 * j,
-                               make_kmajor_desc(base + off_q + ((items - 1) & 1) * kN * D + hh * kN * kRowBytes, kRowBytes) + 2 * j, kMulK, hh + j > 0);
+                               make_kmajor_desc(base + off_q + hh * kN * kRowBytes, kRowBytes) + 2 * j, kMulK, hh + j > 0);
                 mma_commit(smem_u32(&sh.sfull[i & 1]));
             }
             __syncwarp();
@@ -547,7 +438,119 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         auto wait = [&](uint64_t& bar, int parity) {   // the warp goes on together
             ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar), parity, a.wait_budget)) && ok;
         };
-        load_queries(std::integral_constant<int, kComputeWarps>(), cur, 0, warp);
+        // An item's query rows: warp w takes rows w, w + 4, ..  They are fetched a tile before they become the digits of the
+        // operand, which is when the products of the item before are done with its rows.
+        constexpr int kPer = D / 32;                   // values of a row that a lane holds
+        constexpr int kMine = (kRows + kComputeWarps - 1) / kComputeWarps;
+        uint32_t raw[kMine][kPer / 2];
+        struct Row {
+            int64_t token;
+            int head, local;
+            bool has;
+        };
+        auto row_of_lane = [&](const Cursor<kRows>& c) {   // lane r finds row r
+            Row w;
+            const int h = c.head(), index = (c.item - h * c.s.row_tiles) * kRows + lane;
+            w.local = index / a.group;
+            w.head = h * a.group + (index - w.local * a.group);
+            w.has = lane < kRows && w.local < c.s.added;
+            w.token = c.s.first + w.local;
+            return w;
+        };
+        auto fetch_queries = [&](const Cursor<kRows>& c) {
+            const Row w = row_of_lane(c);
+            const int64_t from = w.has ? w.token * a.q_token_stride + w.head * a.q_head_stride : -1;
+#pragma unroll
+            for (int j = 0; j < kMine; ++j) {
+                const int64_t at = __shfl_sync(0xffffffffu, from, warp + j * kComputeWarps);
+                const T* q = static_cast<const T*>(a.q) + at + lane * kPer;
+#pragma unroll
+                for (int k = 0; k < kPer / 2; ++k) raw[j][k] = 0;
+                if (at < 0) continue;                  // no lane from kRows on holds a row
+                if constexpr (kPer == 2) {
+                    raw[j][0] = *reinterpret_cast<const uint32_t*>(q);
+                } else if constexpr (kPer == 4) {
+                    const uint2 u = *reinterpret_cast<const uint2*>(q);
+                    raw[j][0] = u.x; raw[j][1] = u.y;
+                } else {
+                    const uint4 u = *reinterpret_cast<const uint4*>(q);
+                    raw[j][0] = u.x; raw[j][1] = u.y; raw[j][2] = u.z; raw[j][3] = u.w;
+                }
+            }
+        };
+        auto convert_queries = [&](const Cursor<kRows>& c, int which) {
+            ItemInfo& it = sh.item[which];
+            if (warp == 0) {
+                const Row w = row_of_lane(c);
+                const int own = c.s.len - c.s.added + w.local + 1;   // tokens up to the row's own
+                const int end = w.has ? min(own, c.s.limit) : 0x7fffffff, begin = w.has && a.window > 0 ? max(0, own - a.window) : 0;
+                if (lane < kRows) {
+                    it.begin[lane] = begin;
+                    it.end[lane] = end;
+                    it.out[lane] = w.has ? w.token * a.y_token_stride + w.head * a.y_head_stride : -1;
+                    it.lse[lane] = w.token * a.q_heads + w.head;
+                }
+                const int lo = __reduce_max_sync(0xffffffffu, begin), hi = __reduce_min_sync(0xffffffffu, end);
+                if (lane == 0) {
+                    it.full_lo = lo;
+                    it.full_hi = hi;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kMine; ++j) {
+                const int r = warp + j * kComputeWarps;
+                if (r >= kRows) break;
+                float v[kPer], top = 0.f;
+                bool odd = false;
+#pragma unroll
+                for (int k = 0; k < kPer / 2; ++k) {
+                    const float2 f = qtz_dev::unpack2(raw[j][k], T());
+                    v[2 * k] = f.x;
+                    v[2 * k + 1] = f.y;
+                }
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) {
+                    odd = odd || (__float_as_uint(v[k]) & 0x7f800000u) == 0x7f800000u;
+                    top = fmaxf(top, fabsf(v[k]));
+                }
+                top = redux_max(top);
+                odd = __any_sync(0xffffffffu, odd);
+                // rows below 2^-100 count as 2^-100 (their logits are zero either way)
+                const int ex = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -100), 127);
+                const float mult = __uint_as_float(static_cast<uint32_t>(127 + 21 - ex) << 23);
+                uint64_t digits[3] = {0, 0, 0};
+#pragma unroll
+                for (int k = 0; k < kPer; ++k) {
+                    const int x = odd ? 0 : __float2int_rn(v[k] * mult);
+                    const int d0 = (x << 24) >> 24, x1 = (x - d0) >> 8, d1 = (x1 << 24) >> 24, d2 = (x1 - d1) >> 8;
+                    digits[0] |= static_cast<uint64_t>(d0 & 0xff) << (8 * k);
+                    digits[1] |= static_cast<uint64_t>(d1 & 0xff) << (8 * k);
+                    digits[2] |= static_cast<uint64_t>(d2 & 0xff) << (8 * k);
+                }
+                const int d = lane * kPer, hh = d / 128, x = d % kRowBytes;
+#pragma unroll
+                for (int g = 0; g < 3; ++g) {
+                    const int n = g * kRows + r, swz = kRowBytes == 128 ? (n & 7) : ((n >> 1) & 3);
+                    uint8_t* to = smem + off_q + hh * kN * kRowBytes + n * kRowBytes + (((x >> 4) ^ swz) << 4) + (x & 15);
+                    if constexpr (kPer == 2) *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(digits[g]);
+                    else if constexpr (kPer == 4) *reinterpret_cast<uint32_t*>(to) = static_cast<uint32_t>(digits[g]);
+                    else *reinterpret_cast<uint64_t*>(to) = digits[g];
+                }
+                // a row that holds NaN or infinity gives NaN
+                if (lane == 0) it.factor[r] = odd ? __uint_as_float(0x7fc00000u) : a.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 - 21 + ex) << 23);
+            }
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh.qfull));
+        };
+        auto next_item = [&](Cursor<kRows> c) {
+            c.k = c.s.tiles - 1;
+            c.next(a, prefix, known);
+            return c;
+        };
+
+        fetch_queries(cur);
+        convert_queries(cur, 0);
         int items = 0;
         float m[kRows], l[kRows], acc[kHalves][kRows], keep[kRows];
         int seg_first = cur.k, stage = 0, round = 0;
@@ -589,7 +592,10 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
             const ItemInfo& it = sh.item[items & 1];
             const int pos0 = cur.pos(), pos = pos0 + tid;
             const bool last = cur.k == cur.s.tiles - 1, more = i + 1 < count;
-            if (i == 0 || cur.k == 0) wait(sh.qfull[items & 1], (items >> 1) & 1);
+            // the next item's first tile is at most one tile after the next
+            const int to_next = cur.s.tiles - cur.k;
+            if (i + to_next < count && (to_next == 2 || (to_next == 1 && (i == 0 || cur.k == 0)))) fetch_queries(next_item(cur));
+            if (i == 0 || cur.k == 0) wait(sh.qfull, items & 1);
             wait(sh.full[stage], round & 1);
             // Scales lie in [2^-100, 2^122] here (the least is QTZ_KV_MIN_SCALE; no 16-bit value gives more than 2^121), so
             // that their logarithms and inverses are ordinary numbers.
@@ -665,6 +671,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh.pfull[i & 1]));
+            if (last && more) convert_queries(next_item(cur), (items + 1) & 1);
 
             if (!last && more) {
                 ++cur.k;
@@ -713,8 +720,6 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                         open.c1 = static_cast<int>(cur.begin + cur.s.tiles - 1) / share;
                     }
                 }
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&sh.qempty[items & 1]));
                 reset();
                 seg_first = 0;
                 ++items;
@@ -754,23 +759,26 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         if (sh.last[warp]) *counter = 0;               // ready for the next call
     }
     __syncthreads();
-    float (*const jm)[kMaxRows] = reinterpret_cast<float (*)[kMaxRows]>(smem), (*const jl)[kMaxRows] = jm + kFanIn, (*const jw)[kMaxRows] = jl + kFanIn;
+    // three warps for each of the two items
+    constexpr int kHalf = kThreads / 2, kFlight = 8;
+    const int slot = tid / kHalf, ht = tid % kHalf;
+    const OpenItem& open = sh.open[slot];
+    float (*const jm)[kMaxRows] = reinterpret_cast<float (*)[kMaxRows]>(smem + slot * 8192), (*const jl)[kMaxRows] = jm + kFanIn, (*const jw)[kMaxRows] = jl + kFanIn;
     float* const j_top = reinterpret_cast<float*>(jw + kFanIn), * const j_sum = j_top + kMaxRows;
-    for (int slot = 0; slot < 2; ++slot) {
-        const OpenItem& open = sh.open[slot];
-        if (open.c1 < 0 || !sh.last[slot]) continue;
+    auto sync_half = [&]() { named_barrier(2 + slot, kHalf); };
+    if (open.c1 >= 0 && sh.last[slot]) {
         __threadfence();
         const int c0 = open.c0, c1 = open.c1, size = group_size(c1 - c0 + 1), groups = (c1 - c0) / size + 1, first = me - (me - c0) % size;
         auto part_of = [&](int cta) { return a.parts + (static_cast<int64_t>(cta) * 2 + (cta == c0 ? 1 : 0)) * kPart; };
         // Joins the n parts of CTAs from, from + step, ..: into `to`, or into the output.
         auto join = [&](int from, int step, int n, float* to) {
-            for (int i = tid; i < n * kMaxRows; i += kThreads) {
+            for (int i = ht; i < n * kMaxRows; i += kHalf) {
                 const float* p = part_of(from + i / kMaxRows * step) + kMaxRows * D + i % kMaxRows;
                 jm[i / kMaxRows][i % kMaxRows] = __ldcg(p);
                 jl[i / kMaxRows][i % kMaxRows] = __ldcg(p + kMaxRows);
             }
-            __syncthreads();
-            for (int i = tid; i < n * kMaxRows; i += kThreads) {
+            sync_half();
+            for (int i = ht; i < n * kMaxRows; i += kHalf) {
                 const int j = i / kMaxRows, r = i % kMaxRows;
                 float top = -INFINITY;
                 for (int x = 0; x < n; ++x) top = fmaxf(top, jm[x][r]);
@@ -778,24 +786,29 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                 jw[j][r] = mj == -INFINITY && lj == 0.f ? 0.f : ex2(mj - (top == -INFINITY ? 0.f : top));
                 if (j == 0) j_top[r] = top;
             }
-            __syncthreads();
-            if (tid < kMaxRows) {
+            sync_half();
+            if (ht < kMaxRows) {
                 float sum = 0.f;
-                for (int x = 0; x < n; ++x) sum = fmaf(jl[x][tid], jw[x][tid], sum);
-                j_sum[tid] = sum;
+                for (int x = 0; x < n; ++x) sum = fmaf(jl[x][ht], jw[x][ht], sum);
+                j_sum[ht] = sum;
             }
-            __syncthreads();
-            for (int u = tid; u < kRows * D / 4; u += kThreads) {
+            sync_half();
+            for (int u = ht; u < kRows * D / 4; u += kHalf) {
                 const int r = u / (D / 4), d = u % (D / 4) * 4;
                 float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 9
-                for (int x = 0; x < n; ++x) {
-                    const float4 p = __ldcg(reinterpret_cast<const float4*>(part_of(from + x * step) + r * D + d));
-                    const float w = jw[x][r];
-                    v.x = fmaf(p.x, w, v.x);
-                    v.y = fmaf(p.y, w, v.y);
-                    v.z = fmaf(p.z, w, v.z);
-                    v.w = fmaf(p.w, w, v.w);
+                for (int x0 = 0; x0 < n; x0 += kFlight) {
+                    float4 p[kFlight];
+#pragma unroll
+                    for (int x = 0; x < kFlight; ++x)
+                        p[x] = __ldcg(reinterpret_cast<const float4*>(part_of(from + min(x0 + x, n - 1) * step) + r * D + d));
+#pragma unroll
+                    for (int x = 0; x < kFlight; ++x) {
+                        const float w = x0 + x < n ? jw[x0 + x][r] : 0.f;
+                        v.x = fmaf(p[x].x, w, v.x);
+                        v.y = fmaf(p[x].y, w, v.y);
+                        v.z = fmaf(p[x].z, w, v.z);
+                        v.w = fmaf(p[x].w, w, v.w);
+                    }
                 }
                 if (to) {
                     *reinterpret_cast<float4*>(to + r * D + d) = v;
@@ -816,19 +829,18 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         join(first, 1, min(size, c1 - first + 1), groups > 1 ? part_of(first) : nullptr);
         if (groups > 1) {
             __threadfence();
-            __syncthreads();
-            if (tid == 0) {
+            sync_half();
+            if (ht == 0) {
                 int32_t* counter = a.counters + 2 * gridDim.x + c0;
                 sh.last[slot] = atomicAdd(counter, 1) == groups - 1;
                 if (sh.last[slot]) *counter = 0;
             }
-            __syncthreads();
+            sync_half();
             if (sh.last[slot]) {
                 __threadfence();
                 join(c0, size, groups, nullptr);
             }
         }
-        __syncthreads();
     }
 }
 
@@ -839,7 +851,7 @@ qtz_status launch(qtz_ctx* h, AttnArgs& a, const CUtensorMap& km, const CUtensor
 {
     constexpr int kN = (3 * kRows + 15) / 16 * 16, kStage = 2 * kTile * D;
     const int ctas = ctas_per_sm(D);
-    const int fixed = 1024 + kN * 128 + 2 * kN * D + static_cast<int>((sizeof(Shared) + 15) / 16 * 16 + sizeof(uint32_t) * (a.requests + 1));
+    const int fixed = 1024 + kN * 128 + kN * D + static_cast<int>((sizeof(Shared) + 15) / 16 * 16 + sizeof(uint32_t) * (a.requests + 1));
     const int room = (kSmemLimit + 1024) / ctas - 1024 - fixed;
     a.stages = room / kStage < kMaxStages ? room / kStage : kMaxStages;
     if (a.stages < 2) return QTZ_ERR_TOO_LARGE;
