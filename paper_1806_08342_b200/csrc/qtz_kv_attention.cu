@@ -67,10 +67,22 @@ struct AttnArgs {
     int32_t* status;
 };
 
+// The sequence is dealt out by cost: a tile counts two units and the end of an item one (measured at 128 columns and 5 rows:
+// 1.4 us a tile with both CTAs of an SM at work, 0.7 us for the last sums, the output row and the refill behind them).
+constexpr int kTileUnits = 2, kItemUnits = 1;
+
 struct RequestShape {
     int first, added;                      // rows of q
     int len, limit;                        // tokens; those that the table can hold
     int row_tiles, lo, hi, tiles;          // items per head; tiles [lo, hi) of the cache; tiles per item (at least one)
+
+    __device__ __forceinline__ int item_units() const { return kTileUnits * tiles + kItemUnits; }
+    // Tiles of the request's items that begin before unit `off` of the request.
+    __device__ __forceinline__ int tiles_before(int off) const
+    {
+        const int item = off / item_units(), rest = off - item * item_units();
+        return item * tiles + min(tiles, (rest + kTileUnits - 1) / kTileUnits);
+    }
 };
 
 template <int kRows>
@@ -101,22 +113,27 @@ template <int kRows>
 struct Cursor {
     RequestShape s;
     int request, item, k;                  // item: (head, row tile) within the request; k: tile within the item
-    uint32_t begin;                        // index of the item's first tile
+    uint32_t begin;                        // unit that the item's first tile begins at
 
-    __device__ __forceinline__ void seek(const AttnArgs& a, const uint32_t* prefix, const KnownRequests& known, uint32_t tile)
+    // The first tile that begins at or after `unit`, in the first known request.
+    __device__ __forceinline__ void seek(const AttnArgs& a, const uint32_t* prefix, const KnownRequests& known, uint32_t unit)
     {
         request = known.first;
         s = known.s[0];
-        const int off = static_cast<int>(tile - prefix[request]);
-        item = off / s.tiles;
-        k = off - item * s.tiles;
-        begin = tile - k;
+        const int off = static_cast<int>(unit - prefix[request]);
+        item = off / s.item_units();
+        begin = prefix[request] + item * s.item_units();
+        k = (off - item * s.item_units() + kTileUnits - 1) / kTileUnits;
+        if (k >= s.tiles) {
+            k = s.tiles - 1;
+            next(a, prefix, known);
+        }
     }
     __device__ __forceinline__ void next(const AttnArgs& a, const uint32_t* prefix, const KnownRequests& known)
     {
         if (++k < s.tiles) return;
         k = 0;
-        begin += s.tiles;
+        begin += s.item_units();
         if (++item < a.c.kv_heads * s.row_tiles) return;
         item = 0;
         do ++request; while (request < a.requests && prefix[request + 1] == prefix[request]);
@@ -199,7 +216,7 @@ struct Shared {
     KnownRequests known;
     OpenItem open[2];                      // begun in an earlier CTA; going on in the next
     uint32_t scan[kThreads / 32], tmem;
-    int last[2], failed;
+    int last[2], failed, tiles;
 };
 
 template <typename T, int D, int kRows>
@@ -252,13 +269,13 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         tmem_relinquish();
     }
 
-    // ---- tiles before each request: an exclusive prefix sum over the requests ----
+    // ---- units before each request: an exclusive prefix sum over the requests ----
     const int per = (a.requests + kThreads - 1) / kThreads;
     const int r_lo = min(tid * per, a.requests), r_hi = min(r_lo + per, a.requests);
     uint32_t mine = 0;
     for (int r = r_lo; r < r_hi; ++r) {
         const RequestShape s = shape_of<kRows>(a, r);
-        const uint32_t n = static_cast<uint32_t>(a.c.kv_heads) * s.row_tiles * s.tiles;
+        const uint32_t n = static_cast<uint32_t>(a.c.kv_heads) * s.row_tiles * s.item_units();
         prefix[r] = n;
         mine += n;
     }
@@ -287,25 +304,42 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
     tc_fence_after();
     const uint32_t tmem = sh.tmem;
 
-    const int all = static_cast<int>(total), share = (all + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x);
-    const int t0 = min(static_cast<int>(blockIdx.x) * share, all), count = min(t0 + share, all) - t0;
+    // No share is smaller than a tile: every CTA between an item's first and last has a part of it.
+    const int all = static_cast<int>(total);
+    const int share = max((all + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x), kTileUnits);
+    const int u0 = min(static_cast<int>(blockIdx.x) * share, all), u1 = min(u0 + share, all);
     auto timed_out = [&]() {
         if (lane == 0 && atomicCAS(a.status, 0, QTZ_ERR_DEVICE_TIMEOUT) == 0) a.status[1] = QTZ_SITE_KV_ATTENTION;
     };
-    if (count > 0 && warp == 0) {
-        int u = 0, v = a.requests;                     // the last request that begins at or before the share's first tile
-        while (v - u > 1) {
-            const int mid = (u + v) >> 1;
-            if (prefix[mid] <= static_cast<uint32_t>(t0)) u = mid; else v = mid;
+    if (u1 > u0 && warp == 0) {
+        auto request_at = [&](uint32_t unit) {         // the last request that begins at or before the unit
+            int u = 0, v = a.requests;
+            while (v - u > 1) {
+                const int mid = (u + v) >> 1;
+                if (prefix[mid] <= unit) u = mid; else v = mid;
+            }
+            return u;
+        };
+        const int first = request_at(u0), last = request_at(u1 - 1);
+        int tiles = 0;                                 // that begin in [u0, u1)
+        for (int r = first + lane; r <= last; r += 32) {
+            const RequestShape s = shape_of<kRows>(a, r);
+            if (r - first < kKnown) known.s[r - first] = s;
+            const int end = static_cast<int>(min(prefix[r + 1], static_cast<uint32_t>(u1)) - prefix[r]);
+            if (s.row_tiles > 0) tiles += s.tiles_before(end) - (r == first ? s.tiles_before(u0 - static_cast<int>(prefix[r])) : 0);
         }
-        if (lane == 0) known.first = u;
-        if (lane < kKnown && u + lane < a.requests) known.s[lane] = shape_of<kRows>(a, u + lane);
+        tiles = __reduce_add_sync(0xffffffffu, tiles);
+        if (lane == 0) {
+            known.first = first;
+            sh.tiles = tiles;
+        }
     }
     __syncthreads();
+    const int count = u1 > u0 ? sh.tiles : 0;
     Cursor<kRows> cur;
-    if (count > 0) cur.seek(a, prefix, known, t0);
+    if (count > 0) cur.seek(a, prefix, known, u0);
 
-            if (count > 0 && warp == kComputeWarps) {
+    if (count > 0 && warp == kComputeWarps) {
         // ======== producer: lane j brings box j of the tile, and its scales ========
         // Table entries are requested kAhead tiles before they are needed, and the scales travel like the boxes, by asynchronous
         // copies that the tile's barrier counts: the producer waits for no look-up (under load one takes longer than a tile).
@@ -717,7 +751,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                     }
                     if (tid == 0) {
                         open.c0 = static_cast<int>(cur.begin) / share;
-                        open.c1 = static_cast<int>(cur.begin + cur.s.tiles - 1) / share;
+                        open.c1 = static_cast<int>(cur.begin + kTileUnits * (cur.s.tiles - 1)) / share;
                     }
                 }
                 reset();
@@ -760,7 +794,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
     }
     __syncthreads();
     // three warps for each of the two items
-    constexpr int kHalf = kThreads / 2, kFlight = 8;
+    constexpr int kHalf = kThreads / 2, kFlight = kRows <= 5 ? 6 : 9;   // parts in flight: what the registers hold
     const int slot = tid / kHalf, ht = tid % kHalf;
     const OpenItem& open = sh.open[slot];
     float (*const jm)[kMaxRows] = reinterpret_cast<float (*)[kMaxRows]>(smem + slot * 8192), (*const jl)[kMaxRows] = jm + kFanIn, (*const jw)[kMaxRows] = jl + kFanIn;
@@ -793,36 +827,46 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                 j_sum[ht] = sum;
             }
             sync_half();
-            for (int u = ht; u < kRows * D / 4; u += kHalf) {
-                const int r = u / (D / 4), d = u % (D / 4) * 4;
-                float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            constexpr int kQuads = kRows * D / 4;
+            for (int q0 = ht; q0 < kQuads; q0 += 2 * kHalf) {
+                float4 v[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+                const int u2[2] = {q0, min(q0 + kHalf, kQuads - 1)};
                 for (int x0 = 0; x0 < n; x0 += kFlight) {
-                    float4 p[kFlight];
+                    float4 p[2][kFlight];
 #pragma unroll
                     for (int x = 0; x < kFlight; ++x)
-                        p[x] = __ldcg(reinterpret_cast<const float4*>(part_of(from + min(x0 + x, n - 1) * step) + r * D + d));
 #pragma unroll
-                    for (int x = 0; x < kFlight; ++x) {
-                        const float w = x0 + x < n ? jw[x0 + x][r] : 0.f;
-                        v.x = fmaf(p[x].x, w, v.x);
-                        v.y = fmaf(p[x].y, w, v.y);
-                        v.z = fmaf(p[x].z, w, v.z);
-                        v.w = fmaf(p[x].w, w, v.w);
-                    }
+                        for (int j = 0; j < 2; ++j)
+                            p[j][x] = __ldcg(reinterpret_cast<const float4*>(part_of(from + min(x0 + x, n - 1) * step)) + u2[j]);
+#pragma unroll
+                    for (int x = 0; x < kFlight; ++x)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const float w = x0 + x < n ? jw[x0 + x][u2[j] / (D / 4)] : 0.f;
+                            v[j].x = fmaf(p[j][x].x, w, v[j].x);
+                            v[j].y = fmaf(p[j][x].y, w, v[j].y);
+                            v[j].z = fmaf(p[j][x].z, w, v[j].z);
+                            v[j].w = fmaf(p[j][x].w, w, v[j].w);
+                        }
                 }
-                if (to) {
-                    *reinterpret_cast<float4*>(to + r * D + d) = v;
-                    if (d == 0) {
-                        to[kMaxRows * D + r] = j_top[r];
-                        to[kMaxRows * D + kMaxRows + r] = j_sum[r];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    if (q0 + j * kHalf >= kQuads) break;
+                    const int r = u2[j] / (D / 4), d = u2[j] % (D / 4) * 4;
+                    if (to) {
+                        *reinterpret_cast<float4*>(to + r * D + d) = v[j];
+                        if (d == 0) {
+                            to[kMaxRows * D + r] = j_top[r];
+                            to[kMaxRows * D + kMaxRows + r] = j_sum[r];
+                        }
+                    } else if (open.out[r] >= 0) {
+                        const float sum = j_sum[r], inv = sum == 0.f ? 0.f : __fdiv_rn(1.f, sum);
+                        uint2 o;
+                        o.x = qtz_dev::pack2(v[j].x * inv, v[j].y * inv, T());
+                        o.y = qtz_dev::pack2(v[j].z * inv, v[j].w * inv, T());
+                        *reinterpret_cast<uint2*>(static_cast<T*>(a.y) + open.out[r] + d) = o;
+                        if (d == 0 && a.lse) a.lse[open.lse[r]] = sum == 0.f ? -INFINITY : (j_top[r] + log2f(sum)) * 0.693147181f;
                     }
-                } else if (open.out[r] >= 0) {
-                    const float sum = j_sum[r], inv = sum == 0.f ? 0.f : __fdiv_rn(1.f, sum);
-                    uint2 o;
-                    o.x = qtz_dev::pack2(v.x * inv, v.y * inv, T());
-                    o.y = qtz_dev::pack2(v.z * inv, v.w * inv, T());
-                    *reinterpret_cast<uint2*>(static_cast<T*>(a.y) + open.out[r] + d) = o;
-                    if (d == 0 && a.lse) a.lse[open.lse[r]] = sum == 0.f ? -INFINITY : (j_top[r] + log2f(sum)) * 0.693147181f;
                 }
             }
         };
@@ -905,7 +949,7 @@ extern "C" qtz_status qtz_kv_attention(qtz_handle h, const qtz_kv_cache* cache, 
     const int64_t rows = static_cast<int64_t>(cache->blocks) * cache->kv_heads * cache->block_tokens;
     const int64_t reach = static_cast<int64_t>(table_width) * cache->block_tokens, group = q_heads / cache->kv_heads;
     const double bound = static_cast<double>(cache->kv_heads) * static_cast<double>(reach / kTile + 1) * (static_cast<double>(tokens) * group / 5 + requests);
-    if (rows > 0x7fffffff || reach > 0x7fffffff || bound > 2.0e9) return QTZ_ERR_TOO_LARGE;
+    if (rows > 0x7fffffff || reach > 0x7fffffff || 3.0 * bound > 2.0e9) return QTZ_ERR_TOO_LARGE;
     qtz_device_guard guard(h->device);
     int box_shift = 4;                         // the largest box that divides both a block and a tile
     while ((1 << box_shift) < kTile && cache->block_tokens % (2 << box_shift) == 0) ++box_shift;
