@@ -65,6 +65,7 @@ extern "C" qtz_status qtz_destroy(qtz_handle h)
     if (h->params_dev) cudaFree(h->params_dev);
     if (h->reduce_dev) cudaFree(h->reduce_dev);
     if (h->status_dev) cudaFree(h->status_dev);
+    if (h->linear_dev) cudaFree(h->linear_dev);
     if (h->reduce_host) cudaFreeHost(h->reduce_host);
     (void)cudaGetLastError();
     delete h;

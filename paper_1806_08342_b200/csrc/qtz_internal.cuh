@@ -24,6 +24,8 @@ struct qtz_ctx {
     int32_t* status_dev = nullptr;
     float* reduce_host = nullptr;  // pinned
     size_t reduce_host_bytes = 0;
+    void* linear_dev = nullptr;             // parts and counters of linear layers (allocated with the first layer)
+    int32_t* linear_counters = nullptr;     // within it
     bool no_pairs = false;                  // never run layers on CTA pairs (A/B comparisons; set by QTZ_NO_PAIRS=1)
     bool single_row_stems = false;          // row-window layers: one output row per tile (A/B comparisons; QTZ_SINGLE_ROW_STEMS=1)
     long long wait_budget = 2000000000LL;   // cycle budget of every bounded device-side wait (about one second)
@@ -36,7 +38,7 @@ enum qtz_kernel_family { QTZ_K_DIRECT = 0, QTZ_K_TCGEN05 = 1, QTZ_K_DEPTHWISE = 
 enum { QTZ_SITE_TMA_FULL = 1, QTZ_SITE_SMEM_EMPTY = 2, QTZ_SITE_TMEM_FULL = 3,
        QTZ_SITE_TMEM_EMPTY = 4, QTZ_SITE_STORE = 5, QTZ_SITE_OUT_FULL = 6, QTZ_SITE_OUT_EMPTY = 7,
        QTZ_SITE_SELFTEST = 8, QTZ_SITE_PROBE = 9,
-       QTZ_SITE_KV_APPEND = 10, QTZ_SITE_KV_READ = 11, QTZ_SITE_KV_ATTENTION = 12 };
+       QTZ_SITE_KV_APPEND = 10, QTZ_SITE_KV_READ = 11, QTZ_SITE_KV_ATTENTION = 12, QTZ_SITE_LINEAR = 13 };
 
 inline qtz_status qtz_cuda_fail(qtz_ctx* h, cudaError_t e, const char* what)
 {
