@@ -1,16 +1,23 @@
 // Linear layers with 4-bit weights and group scales on few rows of real activations (decoding).
 //
-// Mathematics.  y[r][o] = sum_g s[o][g] sum_{k in g} (q[o][k] - z[o][g]) x[r][k] + b[o].  The inner sum runs on the fp16 / bf16
-// matrix instructions (m16n8k16: 16 output rows x 8 activation rows) with q - z as an exact 16-bit operand and fp32 sums; the
-// scale multiplies the fp32 sum of its group, or of the 64 columns of it that are at hand.  Nothing is rounded before y.
+// Mathematics.  y[r][o] = sum_g s[o][g] sum_{k in g} (q[o][k] - z[o][g]) x[r][k] + b[o].
+//   up to 8 rows   The codes meet the integer matrix instructions (m16n8k32) as they are: eight are cut from a word by three logic
+//                  operations.  Each row's 256 columns at hand are written as 2^(e - 21) (d_2 2^16 + d_1 2^8 + d_0), e the exponent
+//                  of their largest value, d in [-128, 127]: 22 bits below it, more than the 11 or 8 that a value has; one operand
+//                  column for each digit.  Integer sums are exact; scale, digit weight and zero point (through the sum of x over the
+//                  group) multiply them in fp32.
+//   more rows      fp16 / bf16 matrix instructions (m16n8k16) with q - z as an exact operand: two codes are cut from a word by one
+//                  logic operation that also writes the exponent (1024 + q in fp16, 128 + q in bf16), one packed operation takes the
+//                  offset off; the scale multiplies the fp32 sum of its group, or of the 64 columns of it that are at hand.
+// Nothing is rounded to 16 bits before y.
 //
-// What bounds it: half a byte of weight is read for 2 flops an activation row, so up to some 16 rows HBM does (measured copy
-// rate: 46 weights a clock and SM), beyond that the matrix instructions (1024 products a clock and SM: 32 weights at 32 rows).
-// So the weights are read once, in the order of use, as contiguous blocks of 32 rows x 256 columns with their scales and zero
-// points behind the codes; every warp streams its blocks through a ring of its own (bulk copies, several blocks ahead), and a
-// code costs little more than one instruction: two are cut from a word by one logic operation that also writes the exponent
-// (1024 + q in fp16, 128 + q in bf16), one packed operation takes the offset off.  Activations are few and come through L1: the
-// eight warps of a CTA work on the same columns of 256 rows.
+// What bounds it: half a byte of weight is read for 2 flops an activation row.  At the measured copy rate that is 46 weights a clock
+// and SM, for which the SM issues 2.8 operations a weight: the second form needs about 2.3, the first 0.8 for one row and 1.9 for
+// eight, where its matrix instructions (2048 products a clock) still take 85 weights a clock.  With 32 rows the second form's
+// matrix instructions (1024 products a clock) take 32 weights a clock: they bound it.
+// The weights are read once, in the order of use, as contiguous blocks of 32 rows x 256 columns with their scales and zero points
+// behind the codes; every warp streams its blocks through a ring of its own (bulk copies, several blocks ahead).  Activations are
+// few: the eight warps of a CTA work on the same columns of 256 rows and share them in shared memory.
 // The (256 rows, 256 columns) units form one sequence that is dealt out in equal contiguous shares to a grid that fills the GPU
 // once; rows whose columns lie in several CTAs are joined by the last of those to arrive, in the order of the columns.
 #include <new>
@@ -54,8 +61,9 @@ struct PackArgs {
     uint8_t* out;
 };
 
-// One thread per 32-bit word of codes: word (chunk of 64 columns, half of the 32 rows, lane, w) holds eight columns of one row,
-// column pair p at bits 4 p and 16 + 4 p, in the order in which the lanes of a matrix instruction hold their operand.
+// One thread per 32-bit word of codes: word (chunk of 64 columns, half of the 32 rows, lane, w) holds eight columns of one row, in
+// the order in which the lanes of a matrix instruction hold their operand: columns 0 .. 3 in the low nibbles of the four bytes,
+// 4 .. 7 in the high ones.
 __global__ void __launch_bounds__(256)
 pack_kernel(PackArgs a)
 {
@@ -74,7 +82,7 @@ pack_kernel(PackArgs a)
                 const int g = min((k + j) / a.group, a.groups - 1);
                 q = min(static_cast<int>(a.zeros[static_cast<int64_t>(row) * a.groups + g]), 15);
             }
-            v |= q << (4 * (j >> 1) + 16 * (j & 1));
+            v |= q << (8 * (j & 3) + 4 * (j >> 2));
         }
         reinterpret_cast<uint32_t*>(block)[i] = v;
     }
@@ -130,38 +138,43 @@ __device__ __forceinline__ uint32_t cut(uint32_t a, uint32_t mask, uint32_t expo
 template <typename H2> __device__ __forceinline__ H2 as(uint32_t v) { return *reinterpret_cast<const H2*>(&v); }
 template <typename H2> __device__ __forceinline__ uint32_t bits(H2 v) { return *reinterpret_cast<const uint32_t*>(&v); }
 
-// The four pairs of a word as q - z.  fp16: 1024 + q - (1024 + z), and (1024 + 16 q) / 16 - (64 + z) for the pairs at odd nibbles.
-// bf16 has no room for the latter: 128 + q - (128 + z) after a shift each.  `zero`: z as two 16-bit values of T.
+// The pairs of columns (0 2), (4 6), (1 3), (5 7) of a word as q - z; `zero`: z (0..15) in both halves.  fp16: 1024 + q - (1024 + z),
+// and (1024 + 16 q) / 16 - (64 + z) for the pairs in odd nibbles.  bf16 has no room for the latter: 128 + q - (128 + z) after a shift.
 template <typename T>
 __device__ __forceinline__ void unpack_codes(uint32_t w, uint32_t zero, uint32_t (&out)[4])
 {
     if constexpr (std::is_same<T, __half>::value) {
-        const __half2 even = __hadd2(as<__half2>(zero), as<__half2>(0x64006400u));
-        const __half2 odd = __hneg2(__hadd2(as<__half2>(zero), as<__half2>(0x54005400u)));
+        const __half2 even = as<__half2>(0x64006400u | zero), odd = as<__half2>(0xd400d400u | (zero << 4));
         const uint32_t v = w >> 8;
         out[0] = bits(__hsub2(as<__half2>(cut(w, 0x000f000fu, 0x64006400u)), even));
         out[1] = bits(__hfma2(as<__half2>(cut(w, 0x00f000f0u, 0x64006400u)), as<__half2>(0x2c002c00u), odd));
         out[2] = bits(__hsub2(as<__half2>(cut(v, 0x000f000fu, 0x64006400u)), even));
         out[3] = bits(__hfma2(as<__half2>(cut(v, 0x00f000f0u, 0x64006400u)), as<__half2>(0x2c002c00u), odd));
     } else {
-        const __nv_bfloat162 offset = __hadd2(as<__nv_bfloat162>(zero), as<__nv_bfloat162>(0x43004300u));
+        const __nv_bfloat162 offset = as<__nv_bfloat162>(0x43004300u | zero);
 #pragma unroll
         for (int p = 0; p < 4; ++p) out[p] = bits(__hsub2(as<__nv_bfloat162>(cut(w >> (4 * p), 0x000f000fu, 0x43004300u)), offset));
     }
 }
 
-// z (0..15) as two equal values of T
-template <typename T>
-__device__ __forceinline__ uint32_t zero_pair(uint32_t z)
+// D (16 x 8, int32) += A (16 x 32, unsigned bytes) B (32 x 8, signed bytes)
+__device__ __forceinline__ void mma_digits(int (&d)[4], const uint32_t (&a)[4], uint2 b)
 {
-    if constexpr (std::is_same<T, __half>::value) return bits(__half2half2(__ushort2half_rn(static_cast<unsigned short>(z))));
-    else return bits(__bfloat162bfloat162(__ushort2bfloat16_rn(static_cast<unsigned short>(z))));
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y));
 }
 
 __device__ __forceinline__ uint4 lds128(uint32_t addr)
 {
     uint4 v;
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
+    return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t addr)
+{
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr));
     return v;
 }
 __device__ __forceinline__ uint32_t lds32(uint32_t addr)
@@ -177,151 +190,46 @@ __device__ __forceinline__ uint32_t lds16(uint32_t addr)
     return v;
 }
 
-// kNt: blocks of eight activation rows; kFine: groups of 32 columns; kZero: with zero points
-template <typename T, int kNt, bool kFine, bool kZero>
-__global__ void __launch_bounds__(kThreads, kNt <= 2 ? 2 : 1)
-linear_kernel(const __grid_constant__ LinearArgs a)
-{
-    extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ __align__(8) uint64_t s_full[kWarps][kMaxStages];
-    __shared__ int s_last[2], s_failed;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
-    const uint32_t ring = smem_u32(smem) + warp * a.stages * a.block_bytes;
-    if (lane < kMaxStages) mbar_init(smem_u32(&s_full[warp][lane]), 1);
-    if (tid == 0) s_failed = 0;
-    fence_barrier_init();
-    __syncthreads();
+// What both kernels share: a warp's stream of weight blocks, the writing of rows, the joining of parts.  A lane holds eight values
+// of each block of eight activation rows: v[j][c] belongs to output row g + 8 (c >> 1) of half j and activation row 2 t4 + (c & 1).
+struct Stream {
+    const LinearArgs& a;
+    uint32_t ring;
+    uint64_t* full;                        // [kMaxStages] of this warp
+    int u0, u1, warp, lane, issued, stage;
+    uint32_t phase;
 
-    const int u0 = min(static_cast<int>(blockIdx.x) * a.share, a.units), u1 = min(u0 + a.share, a.units);
     // a unit: (rows of x, 256 rows of W, 256 columns), the columns fastest
-    auto tile_of = [&](int unit) { return unit / a.k_blocks % a.row_blocks * kWarps + warp; };
-    auto issue = [&](int unit, int stage) {            // lane 0 only
+    __device__ __forceinline__ int tile_of(int unit) const { return unit / a.k_blocks % a.row_blocks * kWarps + warp; }
+    __device__ __forceinline__ void issue(int unit, int to) const   // lane 0 only
+    {
         const int tile = tile_of(unit);
-        const uint32_t bar = smem_u32(&s_full[warp][stage]);
+        const uint32_t bar = smem_u32(&full[to]);
         if (tile >= a.row_tiles) {                     // no rows for this warp
             mbar_arrive(bar);
             return;
         }
         mbar_arrive_expect_tx(bar, a.block_bytes);
-        bulk_load(ring + stage * a.block_bytes, a.blocks + (static_cast<int64_t>(tile) * a.k_blocks + unit % a.k_blocks) * a.block_bytes, a.block_bytes, bar);
-    };
-    int issued = min(a.stages, u1 - u0);
-    if (lane == 0)
-        for (int i = 0; i < issued; ++i) issue(u0 + i, i);
-
-    float acc[2][kNt][4];
-    auto clear = [&]() {
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int nt = 0; nt < kNt; ++nt)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) acc[j][nt][c] = 0.f;
-    };
-    clear();
-    // rows of y: value c of acc[j][nt] belongs to output row g + 8 (c >> 1) of half j and activation row 2 t4 + (c & 1) of block nt
-    auto write = [&](int unit) {
-        const int o0 = tile_of(unit) * kRowTile + g;
-        const int64_t r0 = static_cast<int64_t>(unit / (a.k_blocks * a.row_blocks)) * (8 * kNt) + 2 * t4;
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int hi = 0; hi < 2; ++hi) {
-                const int o = o0 + 16 * j + 8 * hi;
-                if (o >= a.n) continue;
-                const float b = a.bias ? qtz_dev::to_f32(static_cast<const T*>(a.bias)[o]) : 0.f;
-#pragma unroll
-                for (int nt = 0; nt < kNt; ++nt)
-#pragma unroll
-                    for (int c = 0; c < 2; ++c) {
-                        const int64_t r = r0 + 8 * nt + c;
-                        if (r < a.rows) static_cast<T*>(a.y)[r * a.y_stride + o] = qtz_dev::from_f32<T>(acc[j][nt][2 * hi + c] + b);
-                    }
-            }
-    };
-    constexpr int kPart = kWarps * kRowTile * 8 * kNt;
-    int open[2] = {-1, -1};                            // units whose rows are shared with an earlier / a later CTA
-    bool failed = false;
-    int stage = 0;
-    uint32_t phase = 0;
-    for (int unit = u0; unit < u1; ++unit) {
-        const int kb = unit % a.k_blocks, i = unit - u0;
-        // after a wait that gave up nothing more is issued, but what is in flight is still waited for (with the same limit)
-        if (i < issued && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&s_full[warp][stage]), phase, a.wait_budget))) {
-            if (lane == 0 && atomicCAS(a.status, 0, QTZ_ERR_DEVICE_TIMEOUT) == 0) a.status[1] = QTZ_SITE_LINEAR;
-            failed = true;
-        }
-        if (!failed && tile_of(unit) < a.row_tiles) {
-            const uint32_t block = ring + stage * a.block_bytes, scales = block + kCodeBytes, zeros = scales + a.per_block * kRowTile * 2;
-            const int64_t r0 = static_cast<int64_t>(unit / (a.k_blocks * a.row_blocks)) * (8 * kNt) + g;
-            const uint16_t* xp[kNt];
-#pragma unroll
-            for (int nt = 0; nt < kNt; ++nt)
-                xp[nt] = r0 + 8 * nt < a.rows ? static_cast<const uint16_t*>(a.x) + (r0 + 8 * nt) * a.x_stride + kb * kKBlock + 8 * t4 : nullptr;
-            const int left = a.k - kb * kKBlock - 8 * t4;      // columns from this lane's first one on
-#pragma unroll 1
-            for (int chunk = 0; chunk < 4; ++chunk) {
-                uint32_t w[2][2][2][4];                // [half of the rows][half of the columns][row g, g + 8][pair]
-                float s[2][kFine ? 2 : 1][2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const uint4 q = lds128(block + (chunk * 2 + j) * 512 + lane * 16);
-                    const uint32_t words[2][2] = {{q.x, q.y}, {q.z, q.w}};
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int si = kFine ? 2 * chunk + h : chunk * a.per_block / 4, at = (si * 2 + j) * 8 + g;
-                        uint32_t z0 = zero_pair<T>(8), z1 = z0;
-                        if (kZero) {
-                            const uint32_t z = lds16(zeros + 2 * at);
-                            z0 = zero_pair<T>(z & 0xff);
-                            z1 = zero_pair<T>(z >> 8);
-                        }
-                        if (kFine || h == 0) {
-                            const float2 f = qtz_dev::unpack2(lds32(scales + 4 * at), T());
-                            s[j][kFine ? h : 0][0] = f.x;
-                            s[j][kFine ? h : 0][1] = f.y;
-                        }
-                        unpack_codes<T>(words[h][0], z0, w[j][h][0]);
-                        unpack_codes<T>(words[h][1], z1, w[j][h][1]);
-                    }
-                }
-#pragma unroll
-                for (int nt = 0; nt < kNt; ++nt) {
-                    uint32_t b[2][4];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int k = chunk * 64 + h * 32, have = xp[nt] ? left - k : 0;
-                        uint4 v = make_uint4(0, 0, 0, 0);
-                        if (have > 0) v = __ldg(reinterpret_cast<const uint4*>(xp[nt] + k));
-                        b[h][0] = v.x; b[h][1] = v.y; b[h][2] = v.z; b[h][3] = v.w;
-                        if (have > 0 && have < 8)              // the last columns: what lies behind them is not data
-#pragma unroll
-                            for (int c = 0; c < 4; ++c) b[h][c] = have >= 2 * c + 2 ? b[h][c] : have == 2 * c + 1 ? b[h][c] & 0xffffu : 0u;
-                    }
-                    float part[2][4] = {};
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                        for (int step = 0; step < 2; ++step)
-#pragma unroll
-                            for (int j = 0; j < 2; ++j) {
-                                const uint32_t op[4] = {w[j][h][0][2 * step], w[j][h][1][2 * step], w[j][h][0][2 * step + 1], w[j][h][1][2 * step + 1]};
-                                mma<T>(part[j], op, b[h][2 * step], b[h][2 * step + 1]);
-                            }
-                        if (kFine || h == 1)
-#pragma unroll
-                            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                                for (int c = 0; c < 4; ++c) {
-                                    acc[j][nt][c] = fmaf(part[j][c], s[j][kFine ? h : 0][c >> 1], acc[j][nt][c]);
-                                    part[j][c] = 0.f;
-                                }
-                    }
-                }
-            }
-        }
+        bulk_load(ring + to * a.block_bytes, a.blocks + (static_cast<int64_t>(tile) * a.k_blocks + unit % a.k_blocks) * a.block_bytes, a.block_bytes, bar);
+    }
+    __device__ __forceinline__ void start()
+    {
+        issued = min(a.stages, u1 - u0);
+        stage = 0;
+        phase = 0;
+        if (lane == 0)
+            for (int i = 0; i < issued; ++i) issue(u0 + i, i);
+    }
+    // After a wait that gave up nothing more is issued, but what is in flight is still waited for (with the same limit).
+    __device__ __forceinline__ bool wait(int unit) const
+    {
+        return unit - u0 >= issued || __all_sync(0xffffffffu, mbar_wait(smem_u32(&full[stage]), phase, a.wait_budget));
+    }
+    __device__ __forceinline__ uint32_t block() const { return ring + stage * a.block_bytes; }
+    __device__ __forceinline__ void release(int unit, bool ok)
+    {
         __syncwarp();                                  // every lane has read the stage
-        if (!failed && i + a.stages < u1 - u0) {
+        if (ok && unit + a.stages < u1) {
             if (lane == 0) issue(unit + a.stages, stage);
             ++issued;
         }
@@ -329,94 +237,478 @@ linear_kernel(const __grid_constant__ LinearArgs a)
             stage = 0;
             phase ^= 1;
         }
-        if (kb == a.k_blocks - 1 || unit == u1 - 1) {  // the end of these rows, or of this CTA's columns of them
-            const bool begins = unit - kb >= u0, ends = kb == a.k_blocks - 1;
-            if (begins && ends) {
-                if (tile_of(unit) < a.row_tiles) write(unit);
-            } else {
-                open[begins ? 1 : 0] = unit;
-                float* part = a.parts + (static_cast<int64_t>(blockIdx.x) * 2 + (begins ? 1 : 0)) * kPart + warp * (kRowTile * 8 * kNt) + lane;
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int nt = 0; nt < kNt; ++nt)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) part[((j * kNt + nt) * 4 + c) * 32] = acc[j][nt][c];
-            }
-            clear();
-        }
     }
-    if (failed) s_failed = 1;
+};
 
-    // ---- joining: rows whose columns lie in several CTAs, c0 .. c1 ----
+__device__ __forceinline__ void timed_out(const LinearArgs& a)
+{
+    if ((threadIdx.x & 31) == 0 && atomicCAS(a.status, 0, QTZ_ERR_DEVICE_TIMEOUT) == 0) a.status[1] = QTZ_SITE_LINEAR;
+}
+
+// Rows of y of the warp's tile; `rows` of them at most (an activation block may be narrower than eight).
+template <typename T, int kNt>
+__device__ __forceinline__ void write_rows(const LinearArgs& a, const Stream& s, int unit, const float (&v)[2][kNt][4], int rows)
+{
+    const int t4 = s.lane & 3, o0 = s.tile_of(unit) * kRowTile + (s.lane >> 2);
+    const int64_t r0 = static_cast<int64_t>(unit / (a.k_blocks * a.row_blocks)) * (8 * kNt) + 2 * t4;
+    if (2 * t4 >= rows) return;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int hi = 0; hi < 2; ++hi) {
+            const int o = o0 + 16 * j + 8 * hi;
+            if (o >= a.n) continue;
+            const float b = a.bias ? qtz_dev::to_f32(static_cast<const T*>(a.bias)[o]) : 0.f;
+#pragma unroll
+            for (int nt = 0; nt < kNt; ++nt)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const int64_t r = r0 + 8 * nt + c;
+                    if (r < a.rows) static_cast<T*>(a.y)[r * a.y_stride + o] = qtz_dev::from_f32<T>(v[j][nt][2 * hi + c] + b);
+                }
+        }
+}
+
+// Where the parts of a warp lie: slot 0, rows that began in an earlier CTA; slot 1, rows that go on in a later one.
+template <int kNt>
+__device__ __forceinline__ float* part_of(const LinearArgs& a, const Stream& s, int cta, int slot)
+{
+    return a.parts + ((static_cast<int64_t>(cta) * 2 + slot) * kWarps + s.warp) * (kRowTile * 8 * kNt) + s.lane;
+}
+
+// The end of a row block, or of this CTA's columns of it: y, or a part.
+template <typename T, int kNt>
+__device__ __forceinline__ void finish_rows(const LinearArgs& a, const Stream& s, int unit, const float (&v)[2][kNt][4], int rows, int (&open)[2])
+{
+    const int kb = unit % a.k_blocks;
+    const bool begins = unit - kb >= s.u0, ends = kb == a.k_blocks - 1;
+    if (begins && ends) {
+        if (s.tile_of(unit) < a.row_tiles) write_rows<T, kNt>(a, s, unit, v, rows);
+        return;
+    }
+    open[begins ? 1 : 0] = unit;
+    float* part = part_of<kNt>(a, s, blockIdx.x, begins ? 1 : 0);
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int nt = 0; nt < kNt; ++nt)
+#pragma unroll
+            for (int c = 0; c < 4; ++c) part[((j * kNt + nt) * 4 + c) * 32] = v[j][nt][c];
+}
+
+// Rows whose columns lie in several CTAs, c0 .. c1: the last to arrive joins their parts in order.
+template <typename T, int kNt>
+__device__ __forceinline__ void join_rows(const LinearArgs& a, const Stream& s, const int (&open)[2], int rows, const int& failed, int (&last)[2])
+{
     if (open[0] < 0 && open[1] < 0) return;            // the same for all warps
     __threadfence();
     __syncthreads();
-    if (s_failed) return;                              // the results are void, and the counters have to be cleared
+    if (failed) return;                                // the results are void, and the counters have to be cleared
     auto first_cta = [&](int unit) { return (unit - unit % a.k_blocks) / a.share; };
     auto last_cta = [&](int unit) { return (unit - unit % a.k_blocks + a.k_blocks - 1) / a.share; };
-    if (tid == 0 || tid == 32) {
-        const int which = tid / 32;
-        if (open[which] >= 0) {
-            const int c0 = first_cta(open[which]), c1 = last_cta(open[which]);
-            s_last[which] = atomicAdd(a.counters + c0, 1) == c1 - c0;
-            if (s_last[which]) a.counters[c0] = 0;     // ready for the next call
-        }
+    if (s.lane == 0 && s.warp < 2 && open[s.warp] >= 0) {
+        const int c0 = first_cta(open[s.warp]), c1 = last_cta(open[s.warp]);
+        last[s.warp] = atomicAdd(a.counters + c0, 1) == c1 - c0;
+        if (last[s.warp]) a.counters[c0] = 0;          // ready for the next call
     }
     __syncthreads();
     for (int which = 0; which < 2; ++which) {
-        if (open[which] < 0 || !s_last[which] || tile_of(open[which]) >= a.row_tiles) continue;
+        if (open[which] < 0 || !last[which] || s.tile_of(open[which]) >= a.row_tiles) continue;
         __threadfence();
         const int c0 = first_cta(open[which]), c1 = last_cta(open[which]);
-        clear();
-#pragma unroll 4
-        for (int c = c0; c <= c1; ++c) {
-            const float* part = a.parts + (static_cast<int64_t>(c) * 2 + (c == c0 ? 1 : 0)) * kPart + warp * (kRowTile * 8 * kNt) + lane;
+        constexpr int kFlight = kNt == 1 ? 8 : kNt == 2 ? 4 : 2;       // parts in flight: what the registers hold
+        float v[2][kNt][4] = {};
+        for (int c = c0; c <= c1; c += kFlight) {
+            float p[kFlight][2][kNt][4];
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int x = 0; x < kFlight; ++x) {
+                const float* part = part_of<kNt>(a, s, min(c + x, c1), c + x == c0 ? 1 : 0);
 #pragma unroll
-                for (int nt = 0; nt < kNt; ++nt)
+                for (int i = 0; i < 8 * kNt; ++i) (&p[x][0][0][0])[i] = __ldcg(part + i * 32);
+            }
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) acc[j][nt][v] += __ldcg(part + ((j * kNt + nt) * 4 + v) * 32);
+            for (int x = 0; x < kFlight; ++x)
+#pragma unroll
+                for (int i = 0; i < 8 * kNt; ++i) (&v[0][0][0])[i] += c + x <= c1 ? (&p[x][0][0][0])[i] : 0.f;
         }
-        write(open[which]);
+        write_rows<T, kNt>(a, s, open[which], v, rows);
     }
 }
 
+// ---- up to eight rows: digits of x, integer matrix instructions ----
+constexpr int kDigitBuffers = 3;           // units whose digits are held: the one at work, the next, the one before
+constexpr int kDigitPitch = kKBlock + 32;  // bytes of an operand column: the lanes of a load meet all banks
+
+template <int kTiles>
+struct Digits {                            // of the rows' columns in one unit
+    uint8_t operand[8 * kTiles][kDigitPitch];
+    float factor[8 * kTiles];              // of a column's digit: a power of two, 0 for a column that holds none
+    float sum[8][8 * kTiles];              // per scale of the unit: the sum of x over its columns, at the row's highest digit
+};
+
+// Row r's digit d is operand column: 1 tile (2 rows) 2 d + r; 2 tiles (4 rows) digits 2 i + j at tile i, column 4 j + r; 3 tiles
+// (8 rows) tile d, column r.  A lane so holds a row's digits itself or shares them with the lanes of its quad.
+template <int kTiles>
+__device__ __forceinline__ int digit_column(int d, int r)
+{
+    return kTiles == 1 ? 2 * d + r : kTiles == 2 ? (d >> 1) * 8 + (d & 1) * 4 + r : d * 8 + r;
+}
+
+template <typename T, int kTiles, bool kZero>
+__global__ void __launch_bounds__(kThreads, 2)
+linear_digits_kernel(const __grid_constant__ LinearArgs a)
+{
+    constexpr int kRows = kTiles == 3 ? 8 : 2 * kTiles;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ __align__(8) uint64_t s_full[kWarps][kMaxStages], s_ready[kDigitBuffers], s_free[kDigitBuffers];
+    __shared__ int s_last[2], s_failed;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3, rows = static_cast<int>(a.rows);
+    Digits<kTiles>* const digits = reinterpret_cast<Digits<kTiles>*>(smem);
+    if (lane < kMaxStages) mbar_init(smem_u32(&s_full[warp][lane]), 1);
+    if (tid == 0) {
+        s_failed = 0;
+        for (int i = 0; i < kDigitBuffers; ++i) {
+            mbar_init(smem_u32(&s_ready[i]), rows);
+            mbar_init(smem_u32(&s_free[i]), kWarps);
+        }
+    }
+    for (int i = tid; i < kDigitBuffers * 8 * kTiles; i += kThreads) {   // columns that hold no digit count nothing
+        Digits<kTiles>& d = digits[i / (8 * kTiles)];
+        d.factor[i % (8 * kTiles)] = 0.f;
+        for (int k = 0; k < 8; ++k) d.sum[k][i % (8 * kTiles)] = 0.f;
+    }
+    fence_barrier_init();
+    __syncthreads();
+    const int u0 = min(static_cast<int>(blockIdx.x) * a.share, a.units), u1 = min(u0 + a.share, a.units);
+    Stream s{a, smem_u32(smem) + kDigitBuffers * static_cast<uint32_t>(sizeof(Digits<kTiles>)) + warp * a.stages * a.block_bytes, s_full[warp], u0, u1, warp, lane, 0, 0, 0};
+    s.start();
+    bool ok = true;
+
+    // Rows of x become digits one unit ahead; row r of unit u is the work of warp (u + r) % 8.
+    auto convert = [&](int unit) {
+        const int i = unit - u0, buffer = i % kDigitBuffers, kb = unit % a.k_blocks;
+        Digits<kTiles>& to = digits[buffer];
+        for (int r = (warp - unit) & (kWarps - 1); r < rows; r += kWarps) {
+            const uint16_t* x = static_cast<const uint16_t*>(a.x) + r * a.x_stride + kb * kKBlock + 8 * lane;
+            const int have = a.k - kb * kKBlock - 8 * lane;
+            uint4 raw = make_uint4(0, 0, 0, 0);
+            if (have > 0) raw = __ldg(reinterpret_cast<const uint4*>(x));
+            const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w};
+            float v[8], top = 0.f;
+            bool odd = false;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float2 f = qtz_dev::unpack2(words[k], T());
+                v[2 * k] = 2 * k < have ? f.x : 0.f;   // what lies behind the last column is not data
+                v[2 * k + 1] = 2 * k + 1 < have ? f.y : 0.f;
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                odd = odd || (__float_as_uint(v[k]) & 0x7f800000u) == 0x7f800000u;
+                top = fmaxf(top, fabsf(v[k]));
+            }
+            top = redux_max(top);
+            odd = __any_sync(0xffffffffu, odd);
+            const int ex = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -100), 127);
+            const float mult = __uint_as_float(static_cast<uint32_t>(127 + 21 - ex) << 23);
+            uint64_t d[3] = {0, 0, 0};
+            int sum = 0;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int q = odd ? 0 : __float2int_rn(v[k] * mult);
+                const int d0 = (q << 24) >> 24, q1 = (q - d0) >> 8, d1 = (q1 << 24) >> 24, d2 = (q1 - d1) >> 8;
+                sum += q;
+                d[0] |= static_cast<uint64_t>(d0 & 0xff) << (8 * k);
+                d[1] |= static_cast<uint64_t>(d1 & 0xff) << (8 * k);
+                d[2] |= static_cast<uint64_t>(d2 & 0xff) << (8 * k);
+            }
+            if (i >= kDigitBuffers) {                  // the buffer's unit before has been used by all warps
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_free[buffer]), (i / kDigitBuffers - 1) & 1, a.wait_budget)) && ok;
+            }
+#pragma unroll
+            for (int j = 0; j < 3; ++j) *reinterpret_cast<uint64_t*>(&to.operand[digit_column<kTiles>(j, r)][8 * lane]) = d[j];
+            // sums of 256 / per_block columns: 4, 8, 16 or 32 lanes (|sum| < 2^22 * 256 fits)
+            for (int off = 1; off < 32 / a.per_block; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+            // a row that holds NaN or infinity gives NaN
+            const float unit_of = odd ? __uint_as_float(0x7fc00000u) : __uint_as_float(static_cast<uint32_t>(127 - 21 + ex) << 23);
+            const float minus = kZero ? -1.f : -8.f;
+            if (lane % (32 / a.per_block) == 0)
+                to.sum[lane / (32 / a.per_block)][digit_column<kTiles>(2, r)] = static_cast<float>(sum) * unit_of * minus;
+            if (lane < 3) to.factor[digit_column<kTiles>(lane, r)] = unit_of * (lane == 0 ? 1.f : lane == 1 ? 256.f : 65536.f);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&s_ready[buffer]));
+        }
+    };
+
+    float acc[2][kTiles][4] = {};
+    int open[2] = {-1, -1};                            // units whose rows are shared with an earlier / a later CTA
+    if (u0 < u1) convert(u0);
+    for (int unit = u0; unit < u1; ++unit) {
+        const int i = unit - u0, buffer = i % kDigitBuffers;
+        if (unit + 1 < u1) convert(unit + 1);
+        ok = s.wait(unit) && ok;
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_ready[buffer]), (i / kDigitBuffers) & 1, a.wait_budget)) && ok;
+        if (ok && s.tile_of(unit) < a.row_tiles) {
+            const uint32_t block = s.block(), scales = block + kCodeBytes, zeros = scales + a.per_block * kRowTile * 2;
+            const Digits<kTiles>& dg = digits[buffer];
+            const uint32_t operand = smem_u32(&dg.operand[g][8 * t4]);
+            constexpr int kMagic = 0x4b400000;         // 1.5 * 2^23: an integer sum in the mantissa
+            int part[2][kTiles][4];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int nt = 0; nt < kTiles; ++nt)
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) part[j][nt][c] = kMagic;
+            const int every = 8 / a.per_block;         // steps of 32 columns between two scales
+#pragma unroll 2
+            for (int chunk = 0; chunk < 4; ++chunk) {
+                uint4 q[2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) q[j] = lds128(block + (chunk * 2 + j) * 512 + lane * 16);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int step = 2 * chunk + h;
+                    uint32_t op[2][4];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const uint32_t lo = h ? q[j].z : q[j].x, hi = h ? q[j].w : q[j].y;     // rows g, g + 8
+                        op[j][0] = lo & 0x0f0f0f0fu;
+                        op[j][1] = hi & 0x0f0f0f0fu;
+                        op[j][2] = (lo >> 4) & 0x0f0f0f0fu;
+                        op[j][3] = (hi >> 4) & 0x0f0f0f0fu;
+                    }
+#pragma unroll
+                    for (int nt = 0; nt < kTiles; ++nt) {
+                        const uint2 b = lds64(operand + nt * 8 * kDigitPitch + step * 32);
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) mma_digits(part[j][nt], op[j], b);
+                    }
+                    if ((step + 1) % every == 0) {     // the sums of one scale
+                        const int si = step / every;
+                        float sc[2][2], z[2][2];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const int at = (si * 2 + j) * 8 + g;
+                            const float2 f = qtz_dev::unpack2(lds32(scales + 4 * at), T());
+                            sc[j][0] = f.x;
+                            sc[j][1] = f.y;
+                            if (kZero) {
+                                const uint32_t zz = lds16(zeros + 2 * at);
+                                z[j][0] = static_cast<float>(zz & 0xff);
+                                z[j][1] = static_cast<float>(zz >> 8);
+                            }
+                        }
+#pragma unroll
+                        for (int nt = 0; nt < kTiles; ++nt) {
+                            const float2 f = *reinterpret_cast<const float2*>(&dg.factor[nt * 8 + 2 * t4]), xs = *reinterpret_cast<const float2*>(&dg.sum[si][nt * 8 + 2 * t4]);
+#pragma unroll
+                            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                                for (int c = 0; c < 4; ++c) {
+                                    const float p = __int_as_float(part[j][nt][c]) - 12582912.f, xc = c & 1 ? xs.y : xs.x;
+                                    const float v = fmaf(p, c & 1 ? f.y : f.x, kZero ? z[j][c >> 1] * xc : xc);
+                                    acc[j][nt][c] = fmaf(v, sc[j][c >> 1], acc[j][nt][c]);
+                                    part[j][nt][c] = kMagic;
+                                }
+                        }
+                    }
+                }
+            }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&s_free[buffer]));
+        s.release(unit, ok);
+        if (unit % a.k_blocks == a.k_blocks - 1 || unit == u1 - 1) {
+            float v[2][1][4];                          // the digits of a row together
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    float t = acc[j][0][c];
+                    if (kTiles > 1) t += acc[j][1 % kTiles][c];
+                    if (kTiles > 2) t += acc[j][2 % kTiles][c];
+                    if (kTiles == 1) t += __shfl_xor_sync(0xffffffffu, t, 1);
+                    if (kTiles < 3) t += __shfl_xor_sync(0xffffffffu, t, 2);
+                    v[j][0][c] = t;
+#pragma unroll
+                    for (int nt = 0; nt < kTiles; ++nt) acc[j][nt][c] = 0.f;
+                }
+            finish_rows<T, 1>(a, s, unit, v, kRows, open);
+        }
+    }
+    if (!ok) {
+        timed_out(a);
+        s_failed = 1;
+    }
+    join_rows<T, 1>(a, s, open, kRows, s_failed, s_last);
+}
+
+// ---- more rows: 16-bit matrix instructions; kNt: blocks of eight rows; kFine: groups of 32 columns; kZero: with zero points ----
+constexpr int kRowPitch = 2 * kKBlock + 64;            // bytes of a row of x in shared memory: the lanes of a load meet all banks
+
 template <typename T, int kNt, bool kFine, bool kZero>
-qtz_status launch(qtz_linear* p, LinearArgs& a, cudaStream_t st)
+__global__ void __launch_bounds__(kThreads, 2)
+linear_wide_kernel(const __grid_constant__ LinearArgs a)
+{
+    extern __shared__ __align__(128) uint8_t smem[];   // two units of x, the rings
+    __shared__ __align__(8) uint64_t s_full[kWarps][kMaxStages];
+    __shared__ int s_last[2], s_failed;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
+    if (lane < kMaxStages) mbar_init(smem_u32(&s_full[warp][lane]), 1);
+    if (tid == 0) s_failed = 0;
+    fence_barrier_init();
+    __syncthreads();
+    const int u0 = min(static_cast<int>(blockIdx.x) * a.share, a.units), u1 = min(u0 + a.share, a.units);
+    Stream s{a, smem_u32(smem) + 2 * 8 * kNt * kRowPitch + warp * a.stages * a.block_bytes, s_full[warp], u0, u1, warp, lane, 0, 0, 0};
+    s.start();
+
+    // x of a unit: thread i takes eight columns (i % 32) of rows i / 32, + 8, ..; in the order of the operand (0 2, 4 6, 1 3, 5 7)
+    uint4 held[kNt];
+    auto fetch = [&](int unit) {
+        const int kb = unit % a.k_blocks, have = a.k - kb * kKBlock - 8 * lane;
+        const int64_t r0 = static_cast<int64_t>(unit / (a.k_blocks * a.row_blocks)) * (8 * kNt) + warp;
+#pragma unroll
+        for (int nt = 0; nt < kNt; ++nt) {
+            held[nt] = make_uint4(0, 0, 0, 0);
+            if (r0 + 8 * nt < a.rows && have > 0)
+                held[nt] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.x) + (r0 + 8 * nt) * a.x_stride + kb * kKBlock + 8 * lane));
+        }
+    };
+    auto store = [&](int unit) {
+        const int have = a.k - unit % a.k_blocks * kKBlock - 8 * lane;
+#pragma unroll
+        for (int nt = 0; nt < kNt; ++nt) {
+            uint32_t w[4] = {held[nt].x, held[nt].y, held[nt].z, held[nt].w};
+            if (have > 0 && have < 8)                  // the last columns: what lies behind them is not data
+#pragma unroll
+                for (int c = 0; c < 4; ++c) w[c] = have >= 2 * c + 2 ? w[c] : have == 2 * c + 1 ? w[c] & 0xffffu : 0u;
+            *reinterpret_cast<uint4*>(smem + ((unit - u0) & 1) * (8 * kNt * kRowPitch) + (8 * nt + warp) * kRowPitch + lane * 16) =
+                make_uint4(__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410), __byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632));
+        }
+    };
+
+    float acc[2][kNt][4] = {};
+    int open[2] = {-1, -1};
+    bool ok = true;
+    if (u0 < u1) {
+        fetch(u0);
+        store(u0);
+        __syncthreads();
+    }
+    for (int unit = u0; unit < u1; ++unit) {
+        if (unit + 1 < u1) fetch(unit + 1);
+        ok = s.wait(unit) && ok;
+        if (ok && s.tile_of(unit) < a.row_tiles) {
+            const uint32_t block = s.block(), scales = block + kCodeBytes, zeros = scales + a.per_block * kRowTile * 2;
+            const uint32_t x = smem_u32(smem) + ((unit - u0) & 1) * (8 * kNt * kRowPitch) + g * kRowPitch + t4 * 16;
+#pragma unroll 1
+            for (int chunk = 0; chunk < 4; ++chunk) {
+                uint32_t w[2][2][2][4];                // [half of the rows][half of the columns][row g, g + 8][pair]
+                float sc[2][kFine ? 2 : 1][2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const uint4 q = lds128(block + (chunk * 2 + j) * 512 + lane * 16);
+                    uint32_t z = 0x0808u;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (kFine || h == 0) {
+                            const int si = kFine ? 2 * chunk + h : chunk * a.per_block / 4, at = (si * 2 + j) * 8 + g;
+                            const float2 f = qtz_dev::unpack2(lds32(scales + 4 * at), T());
+                            sc[j][kFine ? h : 0][0] = f.x;
+                            sc[j][kFine ? h : 0][1] = f.y;
+                            if (kZero) z = lds16(zeros + 2 * at);
+                        }
+                        unpack_codes<T>(h ? q.z : q.x, (z & 0xffu) * 0x00010001u, w[j][h][0]);
+                        unpack_codes<T>(h ? q.w : q.y, (z >> 8) * 0x00010001u, w[j][h][1]);
+                    }
+                }
+#pragma unroll
+                for (int nt = 0; nt < kNt; ++nt) {
+                    float part[2][4] = {};
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint4 b = lds128(x + nt * 8 * kRowPitch + chunk * 128 + h * 64);
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const uint32_t first[4] = {w[j][h][0][0], w[j][h][1][0], w[j][h][0][1], w[j][h][1][1]};
+                            mma<T>(part[j], first, b.x, b.y);
+                        }
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const uint32_t second[4] = {w[j][h][0][2], w[j][h][1][2], w[j][h][0][3], w[j][h][1][3]};
+                            mma<T>(part[j], second, b.z, b.w);
+                        }
+                        if (kFine || h == 1)
+#pragma unroll
+                            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                                for (int c = 0; c < 4; ++c) {
+                                    acc[j][nt][c] = fmaf(part[j][c], sc[j][kFine ? h : 0][c >> 1], acc[j][nt][c]);
+                                    part[j][c] = 0.f;
+                                }
+                    }
+                }
+            }
+        }
+        s.release(unit, ok);
+        if (unit + 1 < u1) store(unit + 1);
+        __syncthreads();                               // the next unit's x is there, this one's is free
+        if (unit % a.k_blocks == a.k_blocks - 1 || unit == u1 - 1) {
+            finish_rows<T, kNt>(a, s, unit, acc, 8, open);
+#pragma unroll
+            for (int i = 0; i < 8 * kNt; ++i) (&acc[0][0][0])[i] = 0.f;
+        }
+    }
+    if (!ok) {
+        timed_out(a);
+        s_failed = 1;
+    }
+    join_rows<T, kNt>(a, s, open, 8, s_failed, s_last);
+}
+
+// fixed: shared memory beside the rings; kParts: the most parts that a row block is cut into
+template <typename K>
+qtz_status launch(qtz_linear* p, LinearArgs& a, K kernel, int fixed, int most_parts, cudaStream_t st)
 {
     qtz_ctx* h = p->h;
-    const int ctas = kNt <= 2 ? 2 : 1;
-    const int room = (kSmemLimit + 1024) / ctas - 1024 - 1024;     // 1 KB: the kernel's static shared memory
+    const int room = (kSmemLimit + 1024) / 2 - 1024 - 1024 - fixed;    // two CTAs an SM; 1 KB: the kernels' static shared memory
     a.stages = room / (kWarps * p->block_bytes);
     if (a.stages > kMaxStages) a.stages = kMaxStages;
-    const int smem = kWarps * a.stages * p->block_bytes;
-    const int grid = h->num_sms * ctas;
-    // A share takes in at least 1 / 32 of the columns (1 / 8 for many rows, whose parts are large): joining costs more than it
-    // brings beyond that.
-    const int most = kNt == 1 ? 32 : 8;
+    const int smem = fixed + kWarps * a.stages * p->block_bytes, grid = 2 * h->num_sms;
+    // A share takes in at least 1 / most_parts of the columns: joining costs more than it brings beyond that.
     a.share = (a.units + grid - 1) / grid;
-    if (a.share < (a.k_blocks + most - 1) / most) a.share = (a.k_blocks + most - 1) / most;
-    QTZ_CUDA(h, cudaFuncSetAttribute(linear_kernel<T, kNt, kFine, kZero>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    linear_kernel<T, kNt, kFine, kZero><<<(a.units + a.share - 1) / a.share, kThreads, smem, st>>>(a);
-    QTZ_LAUNCH_CHECK(h, "linear_kernel");
+    if (a.share < (a.k_blocks + most_parts - 1) / most_parts) a.share = (a.k_blocks + most_parts - 1) / most_parts;
+    QTZ_CUDA(h, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    kernel<<<(a.units + a.share - 1) / a.share, kThreads, smem, st>>>(a);
+    QTZ_LAUNCH_CHECK(h, "linear kernel");
     return QTZ_OK;
 }
 
-template <typename T, int kNt>
-qtz_status launch_kind(qtz_linear* p, LinearArgs& a, bool zero, cudaStream_t st)
+template <typename T, int kTiles>
+qtz_status launch_digits(qtz_linear* p, LinearArgs& a, bool zero, cudaStream_t st)
 {
-    if (p->scales == 8) return zero ? launch<T, kNt, true, true>(p, a, st) : launch<T, kNt, true, false>(p, a, st);
-    return zero ? launch<T, kNt, false, true>(p, a, st) : launch<T, kNt, false, false>(p, a, st);
+    constexpr int kFixed = kDigitBuffers * sizeof(Digits<kTiles>);
+    return zero ? launch(p, a, linear_digits_kernel<T, kTiles, true>, kFixed, 32, st) : launch(p, a, linear_digits_kernel<T, kTiles, false>, kFixed, 32, st);
+}
+
+template <typename T, int kNt>
+qtz_status launch_wide(qtz_linear* p, LinearArgs& a, bool zero, cudaStream_t st)
+{
+    constexpr int kFixed = 2 * 8 * kNt * kRowPitch;
+    if (p->scales == 8)
+        return zero ? launch(p, a, linear_wide_kernel<T, kNt, true, true>, kFixed, 8, st) : launch(p, a, linear_wide_kernel<T, kNt, true, false>, kFixed, 8, st);
+    return zero ? launch(p, a, linear_wide_kernel<T, kNt, false, true>, kFixed, 8, st) : launch(p, a, linear_wide_kernel<T, kNt, false, false>, kFixed, 8, st);
 }
 
 template <typename T>
 qtz_status launch_rows(qtz_linear* p, LinearArgs& a, bool zero, cudaStream_t st)
 {
-    if (a.rows <= 8) return launch_kind<T, 1>(p, a, zero, st);
-    if (a.rows <= 16) return launch_kind<T, 2>(p, a, zero, st);
-    return launch_kind<T, 4>(p, a, zero, st);
+    if (a.rows <= 2) return launch_digits<T, 1>(p, a, zero, st);
+    if (a.rows <= 4) return launch_digits<T, 2>(p, a, zero, st);
+    if (a.rows <= 8) return launch_digits<T, 3>(p, a, zero, st);
+    if (a.rows <= 16) return launch_wide<T, 2>(p, a, zero, st);
+    return launch_wide<T, 4>(p, a, zero, st);
 }
 
 // Scratch of the joining, shared by the layers of a handle: parts and counters of a full grid.
@@ -424,8 +716,7 @@ qtz_status ensure_scratch(qtz_ctx* h, cudaStream_t st)
 {
     if (h->linear_dev) return QTZ_OK;
     const int ctas = 2 * h->num_sms;
-    // 16 rows run with two CTAs an SM, 32 with one: the same size
-    const size_t parts = static_cast<size_t>(ctas) * 2 * kWarps * kRowTile * (kMaxTokens / 2) * sizeof(float);
+    const size_t parts = static_cast<size_t>(ctas) * 2 * kWarps * kRowTile * kMaxTokens * sizeof(float);
     QTZ_CUDA(h, cudaMalloc(&h->linear_dev, parts + ctas * sizeof(int32_t)));
     QTZ_CUDA(h, cudaMemsetAsync(static_cast<uint8_t*>(h->linear_dev) + parts, 0, ctas * sizeof(int32_t), st));
     h->linear_counters = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(h->linear_dev) + parts);
