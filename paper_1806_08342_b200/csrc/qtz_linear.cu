@@ -31,7 +31,7 @@ struct qtz_linear {
     qtz_ctx* h = nullptr;
     qtz_linear_desc d{};
     int row_tiles = 0, k_blocks = 0;   // of 32 rows, of 256 columns
-    int scales = 0;                    // scales of a row in a block of 256 columns: 1, 2, 4 or 8
+    int scales = 0;                    // scales of a row in a block of 256 columns: 2, 4 or 8
     int block_bytes = 0;
     uint8_t* blocks = nullptr;         // [row_tiles][k_blocks][block_bytes]: codes, scales, zero points
     void* bias = nullptr;              // [n], behind the blocks in the same allocation; null: none
@@ -157,6 +157,14 @@ __device__ __forceinline__ void unpack_codes(uint32_t w, uint32_t zero, uint32_t
     }
 }
 
+// D = A B + c, the same c everywhere
+__device__ __forceinline__ void mma_digits_from(int (&d)[4], const uint32_t (&a)[4], uint2 b, int c)
+{
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.u8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b.x), "r"(b.y), "r"(c));
+}
+
 // D (16 x 8, int32) += A (16 x 32, unsigned bytes) B (32 x 8, signed bytes)
 __device__ __forceinline__ void mma_digits(int (&d)[4], const uint32_t (&a)[4], uint2 b)
 {
@@ -192,51 +200,77 @@ __device__ __forceinline__ uint32_t lds16(uint32_t addr)
 
 // What both kernels share: a warp's stream of weight blocks, the writing of rows, the joining of parts.  A lane holds eight values
 // of each block of eight activation rows: v[j][c] belongs to output row g + 8 (c >> 1) of half j and activation row 2 t4 + (c & 1).
+struct Place {                             // a unit: (rows of x, 256 rows of W, 256 columns), the columns fastest
+    int kb, rb, pass;
+    __device__ __forceinline__ Place(const LinearArgs& a, int unit)
+    {
+        const int rows = unit / a.k_blocks;
+        kb = unit - rows * a.k_blocks;
+        pass = rows / a.row_blocks;
+        rb = rows - pass * a.row_blocks;
+    }
+    __device__ __forceinline__ void next(const LinearArgs& a)
+    {
+        if (++kb < a.k_blocks) return;
+        kb = 0;
+        if (++rb < a.row_blocks) return;
+        rb = 0;
+        ++pass;
+    }
+};
+
 struct Stream {
     const LinearArgs& a;
     uint32_t ring;
     uint64_t* full;                        // [kMaxStages] of this warp
-    int u0, u1, warp, lane, issued, stage;
+    int u0, u1, warp, lane;
+    Place here, ahead;                     // the unit at work; the next to be issued
+    int unit, issued, stage;
     uint32_t phase;
 
-    // a unit: (rows of x, 256 rows of W, 256 columns), the columns fastest
-    __device__ __forceinline__ int tile_of(int unit) const { return unit / a.k_blocks % a.row_blocks * kWarps + warp; }
-    __device__ __forceinline__ void issue(int unit, int to) const   // lane 0 only
+    __device__ __forceinline__ Stream(const LinearArgs& args, uint32_t ring_, uint64_t* full_)
+        : a(args), ring(ring_), full(full_), u0(min(static_cast<int>(blockIdx.x) * args.share, args.units)), u1(min(u0 + args.share, args.units)),
+          warp(threadIdx.x >> 5), lane(threadIdx.x & 31), here(args, u0), ahead(here), unit(u0), issued(0), stage(0), phase(0)
     {
-        const int tile = tile_of(unit);
-        const uint32_t bar = smem_u32(&full[to]);
-        if (tile >= a.row_tiles) {                     // no rows for this warp
-            mbar_arrive(bar);
-            return;
-        }
-        mbar_arrive_expect_tx(bar, a.block_bytes);
-        bulk_load(ring + to * a.block_bytes, a.blocks + (static_cast<int64_t>(tile) * a.k_blocks + unit % a.k_blocks) * a.block_bytes, a.block_bytes, bar);
+        for (int i = 0; i < min(a.stages, u1 - u0); ++i) issue(i);
     }
-    __device__ __forceinline__ void start()
+    __device__ __forceinline__ int tile(const Place& p) const { return p.rb * kWarps + warp; }
+    __device__ __forceinline__ bool has_rows() const { return tile(here) < a.row_tiles; }
+    __device__ __forceinline__ bool ends() const { return here.kb == a.k_blocks - 1; }
+    __device__ __forceinline__ bool finishes() const { return ends() || unit == u1 - 1; }
+    __device__ __forceinline__ void issue(int to)
     {
-        issued = min(a.stages, u1 - u0);
-        stage = 0;
-        phase = 0;
-        if (lane == 0)
-            for (int i = 0; i < issued; ++i) issue(u0 + i, i);
+        if (lane == 0) {
+            const uint32_t bar = smem_u32(&full[to]);
+            if (tile(ahead) >= a.row_tiles) {          // no rows for this warp
+                mbar_arrive(bar);
+            } else {
+                mbar_arrive_expect_tx(bar, a.block_bytes);
+                bulk_load(ring + to * a.block_bytes, a.blocks + (static_cast<int64_t>(tile(ahead)) * a.k_blocks + ahead.kb) * a.block_bytes, a.block_bytes, bar);
+            }
+        }
+        ahead.next(a);
+        ++issued;
     }
     // After a wait that gave up nothing more is issued, but what is in flight is still waited for (with the same limit).
-    __device__ __forceinline__ bool wait(int unit) const
+    __device__ __forceinline__ bool wait() const
     {
         return unit - u0 >= issued || __all_sync(0xffffffffu, mbar_wait(smem_u32(&full[stage]), phase, a.wait_budget));
     }
     __device__ __forceinline__ uint32_t block() const { return ring + stage * a.block_bytes; }
-    __device__ __forceinline__ void release(int unit, bool ok)
+    __device__ __forceinline__ void release(bool ok)
     {
         __syncwarp();                                  // every lane has read the stage
-        if (ok && unit + a.stages < u1) {
-            if (lane == 0) issue(unit + a.stages, stage);
-            ++issued;
-        }
+        if (ok && issued < u1 - u0) issue(stage);
         if (++stage == a.stages) {
             stage = 0;
             phase ^= 1;
         }
+    }
+    __device__ __forceinline__ void next()
+    {
+        here.next(a);
+        ++unit;
     }
 };
 
@@ -247,10 +281,10 @@ __device__ __forceinline__ void timed_out(const LinearArgs& a)
 
 // Rows of y of the warp's tile; `rows` of them at most (an activation block may be narrower than eight).
 template <typename T, int kNt>
-__device__ __forceinline__ void write_rows(const LinearArgs& a, const Stream& s, int unit, const float (&v)[2][kNt][4], int rows)
+__device__ __forceinline__ void write_rows(const LinearArgs& a, const Stream& s, const Place& at, const float (&v)[2][kNt][4], int rows)
 {
-    const int t4 = s.lane & 3, o0 = s.tile_of(unit) * kRowTile + (s.lane >> 2);
-    const int64_t r0 = static_cast<int64_t>(unit / (a.k_blocks * a.row_blocks)) * (8 * kNt) + 2 * t4;
+    const int t4 = s.lane & 3, o0 = s.tile(at) * kRowTile + (s.lane >> 2);
+    const int64_t r0 = static_cast<int64_t>(at.pass) * (8 * kNt) + 2 * t4;
     if (2 * t4 >= rows) return;
 #pragma unroll
     for (int j = 0; j < 2; ++j)
@@ -278,15 +312,15 @@ __device__ __forceinline__ float* part_of(const LinearArgs& a, const Stream& s, 
 
 // The end of a row block, or of this CTA's columns of it: y, or a part.
 template <typename T, int kNt>
-__device__ __forceinline__ void finish_rows(const LinearArgs& a, const Stream& s, int unit, const float (&v)[2][kNt][4], int rows, int (&open)[2])
+__device__ __forceinline__ void finish_rows(const LinearArgs& a, const Stream& s, const float (&v)[2][kNt][4], int rows, int (&open)[2])
 {
-    const int kb = unit % a.k_blocks;
-    const bool begins = unit - kb >= s.u0, ends = kb == a.k_blocks - 1;
-    if (begins && ends) {
-        if (s.tile_of(unit) < a.row_tiles) write_rows<T, kNt>(a, s, unit, v, rows);
+    const bool begins = s.unit - s.here.kb >= s.u0;
+    if (begins && s.ends()) {
+        if (s.has_rows()) write_rows<T, kNt>(a, s, s.here, v, rows);
         return;
     }
-    open[begins ? 1 : 0] = unit;
+    if (begins) open[1] = s.unit;
+    else open[0] = s.unit;
     float* part = part_of<kNt>(a, s, blockIdx.x, begins ? 1 : 0);
 #pragma unroll
     for (int j = 0; j < 2; ++j)
@@ -304,34 +338,36 @@ __device__ __forceinline__ void join_rows(const LinearArgs& a, const Stream& s, 
     __threadfence();
     __syncthreads();
     if (failed) return;                                // the results are void, and the counters have to be cleared
-    auto first_cta = [&](int unit) { return (unit - unit % a.k_blocks) / a.share; };
-    auto last_cta = [&](int unit) { return (unit - unit % a.k_blocks + a.k_blocks - 1) / a.share; };
-    if (s.lane == 0 && s.warp < 2 && open[s.warp] >= 0) {
-        const int c0 = first_cta(open[s.warp]), c1 = last_cta(open[s.warp]);
-        last[s.warp] = atomicAdd(a.counters + c0, 1) == c1 - c0;
-        if (last[s.warp]) a.counters[c0] = 0;          // ready for the next call
-    }
+    const Place at[2] = {Place(a, max(open[0], 0)), Place(a, max(open[1], 0))};
+    const int c0[2] = {(open[0] - at[0].kb) / a.share, (open[1] - at[1].kb) / a.share};
+    const int c1[2] = {(open[0] - at[0].kb + a.k_blocks - 1) / a.share, (open[1] - at[1].kb + a.k_blocks - 1) / a.share};
+#pragma unroll
+    for (int which = 0; which < 2; ++which)
+        if (threadIdx.x == 32 * which && open[which] >= 0) {
+            last[which] = atomicAdd(a.counters + c0[which], 1) == c1[which] - c0[which];
+            if (last[which]) a.counters[c0[which]] = 0;    // ready for the next call
+        }
     __syncthreads();
+#pragma unroll
     for (int which = 0; which < 2; ++which) {
-        if (open[which] < 0 || !last[which] || s.tile_of(open[which]) >= a.row_tiles) continue;
+        if (open[which] < 0 || !last[which] || s.tile(at[which]) >= a.row_tiles) continue;
         __threadfence();
-        const int c0 = first_cta(open[which]), c1 = last_cta(open[which]);
         constexpr int kFlight = kNt == 1 ? 8 : kNt == 2 ? 4 : 2;       // parts in flight: what the registers hold
         float v[2][kNt][4] = {};
-        for (int c = c0; c <= c1; c += kFlight) {
+        for (int c = c0[which]; c <= c1[which]; c += kFlight) {
             float p[kFlight][2][kNt][4];
 #pragma unroll
             for (int x = 0; x < kFlight; ++x) {
-                const float* part = part_of<kNt>(a, s, min(c + x, c1), c + x == c0 ? 1 : 0);
+                const float* part = part_of<kNt>(a, s, min(c + x, c1[which]), c + x == c0[which] ? 1 : 0);
 #pragma unroll
                 for (int i = 0; i < 8 * kNt; ++i) (&p[x][0][0][0])[i] = __ldcg(part + i * 32);
             }
 #pragma unroll
             for (int x = 0; x < kFlight; ++x)
 #pragma unroll
-                for (int i = 0; i < 8 * kNt; ++i) (&v[0][0][0])[i] += c + x <= c1 ? (&p[x][0][0][0])[i] : 0.f;
+                for (int i = 0; i < 8 * kNt; ++i) (&v[0][0][0])[i] += c + x <= c1[which] ? (&p[x][0][0][0])[i] : 0.f;
         }
-        write_rows<T, kNt>(a, s, open[which], v, rows);
+        write_rows<T, kNt>(a, s, at[which], v, rows);
     }
 }
 
@@ -354,7 +390,8 @@ __device__ __forceinline__ int digit_column(int d, int r)
     return kTiles == 1 ? 2 * d + r : kTiles == 2 ? (d >> 1) * 8 + (d & 1) * 4 + r : d * 8 + r;
 }
 
-template <typename T, int kTiles, bool kZero>
+// kSteps: steps of 32 columns to a scale (1, 2 or 4)
+template <typename T, int kTiles, int kSteps, bool kZero>
 __global__ void __launch_bounds__(kThreads, 2)
 linear_digits_kernel(const __grid_constant__ LinearArgs a)
 {
@@ -379,16 +416,15 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
     }
     fence_barrier_init();
     __syncthreads();
-    const int u0 = min(static_cast<int>(blockIdx.x) * a.share, a.units), u1 = min(u0 + a.share, a.units);
-    Stream s{a, smem_u32(smem) + kDigitBuffers * static_cast<uint32_t>(sizeof(Digits<kTiles>)) + warp * a.stages * a.block_bytes, s_full[warp], u0, u1, warp, lane, 0, 0, 0};
-    s.start();
+    Stream s(a, smem_u32(smem) + kDigitBuffers * static_cast<uint32_t>(sizeof(Digits<kTiles>)) + warp * a.stages * a.block_bytes, s_full[warp]);
     bool ok = true;
 
-    // Rows of x become digits one unit ahead; row r of unit u is the work of warp (u + r) % 8.
-    auto convert = [&](int unit) {
-        const int i = unit - u0, buffer = i % kDigitBuffers, kb = unit % a.k_blocks;
+    // Rows of x become digits one unit ahead; row r of the CTA's unit i is the work of warp (i + r) % 8.  `buffer` and `round`: i
+    // modulo and divided by the number of buffers.
+    auto convert = [&](int i, int kb, int buffer, int round) {
         Digits<kTiles>& to = digits[buffer];
-        for (int r = (warp - unit) & (kWarps - 1); r < rows; r += kWarps) {
+        const int r = (warp - i) & (kWarps - 1);
+        if (r < rows) {
             const uint16_t* x = static_cast<const uint16_t*>(a.x) + r * a.x_stride + kb * kKBlock + 8 * lane;
             const int have = a.k - kb * kKBlock - 8 * lane;
             uint4 raw = make_uint4(0, 0, 0, 0);
@@ -422,18 +458,19 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
                 d[1] |= static_cast<uint64_t>(d1 & 0xff) << (8 * k);
                 d[2] |= static_cast<uint64_t>(d2 & 0xff) << (8 * k);
             }
-            if (i >= kDigitBuffers) {                  // the buffer's unit before has been used by all warps
-                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_free[buffer]), (i / kDigitBuffers - 1) & 1, a.wait_budget)) && ok;
-            }
+            if (round > 0)                             // the buffer's unit before has been used by all warps
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_free[buffer]), (round - 1) & 1, a.wait_budget)) && ok;
 #pragma unroll
             for (int j = 0; j < 3; ++j) *reinterpret_cast<uint64_t*>(&to.operand[digit_column<kTiles>(j, r)][8 * lane]) = d[j];
-            // sums of 256 / per_block columns: 4, 8, 16 or 32 lanes (|sum| < 2^22 * 256 fits)
-            for (int off = 1; off < 32 / a.per_block; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+            // the sum of a scale's columns: |sum| < 2^22 * 128 fits
+            constexpr int kLanes = 4 * kSteps;
+#pragma unroll
+            for (int off = 1; off < kLanes; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
             // a row that holds NaN or infinity gives NaN
             const float unit_of = odd ? __uint_as_float(0x7fc00000u) : __uint_as_float(static_cast<uint32_t>(127 - 21 + ex) << 23);
             const float minus = kZero ? -1.f : -8.f;
-            if (lane % (32 / a.per_block) == 0)
-                to.sum[lane / (32 / a.per_block)][digit_column<kTiles>(2, r)] = static_cast<float>(sum) * unit_of * minus;
+            if (lane % kLanes == 0)
+                to.sum[lane / kLanes][digit_column<kTiles>(2, r)] = static_cast<float>(sum) * unit_of * minus;
             if (lane < 3) to.factor[digit_column<kTiles>(lane, r)] = unit_of * (lane == 0 ? 1.f : lane == 1 ? 256.f : 65536.f);
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&s_ready[buffer]));
@@ -442,32 +479,25 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
 
     float acc[2][kTiles][4] = {};
     int open[2] = {-1, -1};                            // units whose rows are shared with an earlier / a later CTA
-    if (u0 < u1) convert(u0);
-    for (int unit = u0; unit < u1; ++unit) {
-        const int i = unit - u0, buffer = i % kDigitBuffers;
-        if (unit + 1 < u1) convert(unit + 1);
-        ok = s.wait(unit) && ok;
-        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_ready[buffer]), (i / kDigitBuffers) & 1, a.wait_budget)) && ok;
-        if (ok && s.tile_of(unit) < a.row_tiles) {
-            const uint32_t block = s.block(), scales = block + kCodeBytes, zeros = scales + a.per_block * kRowTile * 2;
+    if (s.u0 < s.u1) convert(0, s.here.kb, 0, 0);
+    int buffer = 0, round = 0, buffer_next = 1 % kDigitBuffers, round_next = 0;
+    for (; s.unit < s.u1; s.next()) {
+        if (s.unit + 1 < s.u1) convert(s.unit + 1 - s.u0, s.ends() ? 0 : s.here.kb + 1, buffer_next, round_next);
+        ok = s.wait() && ok;
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_ready[buffer]), round & 1, a.wait_budget)) && ok;
+        if (ok && s.has_rows()) {
+            const uint32_t block = s.block(), scales = block + kCodeBytes, zeros = scales + 8 / kSteps * kRowTile * 2;
             const Digits<kTiles>& dg = digits[buffer];
             const uint32_t operand = smem_u32(&dg.operand[g][8 * t4]);
-            constexpr int kMagic = 0x4b400000;         // 1.5 * 2^23: an integer sum in the mantissa
             int part[2][kTiles][4];
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int nt = 0; nt < kTiles; ++nt)
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) part[j][nt][c] = kMagic;
-            const int every = 8 / a.per_block;         // steps of 32 columns between two scales
-#pragma unroll 2
             for (int chunk = 0; chunk < 4; ++chunk) {
                 uint4 q[2];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) q[j] = lds128(block + (chunk * 2 + j) * 512 + lane * 16);
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
+                    constexpr int kMagic = 0x4b400000; // 1.5 * 2^23: an integer sum in the mantissa
                     const int step = 2 * chunk + h;
                     uint32_t op[2][4];
 #pragma unroll
@@ -482,10 +512,13 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
                     for (int nt = 0; nt < kTiles; ++nt) {
                         const uint2 b = lds64(operand + nt * 8 * kDigitPitch + step * 32);
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) mma_digits(part[j][nt], op[j], b);
+                        for (int j = 0; j < 2; ++j) {
+                            if (step % kSteps == 0) mma_digits_from(part[j][nt], op[j], b, kMagic);
+                            else mma_digits(part[j][nt], op[j], b);
+                        }
                     }
-                    if ((step + 1) % every == 0) {     // the sums of one scale
-                        const int si = step / every;
+                    if ((step + 1) % kSteps == 0) {    // the sums of one scale
+                        const int si = step / kSteps;
                         float sc[2][2], z[2][2];
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
@@ -493,10 +526,10 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
                             const float2 f = qtz_dev::unpack2(lds32(scales + 4 * at), T());
                             sc[j][0] = f.x;
                             sc[j][1] = f.y;
-                            if (kZero) {
+                            if (kZero) {               // 2^23 + z - 2^23
                                 const uint32_t zz = lds16(zeros + 2 * at);
-                                z[j][0] = static_cast<float>(zz & 0xff);
-                                z[j][1] = static_cast<float>(zz >> 8);
+                                z[j][0] = __uint_as_float(__byte_perm(zz, 0x4b000000u, 0x7550)) - 8388608.f;
+                                z[j][1] = __uint_as_float(__byte_perm(zz, 0x4b000000u, 0x7551)) - 8388608.f;
                             }
                         }
 #pragma unroll
@@ -509,7 +542,6 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
                                     const float p = __int_as_float(part[j][nt][c]) - 12582912.f, xc = c & 1 ? xs.y : xs.x;
                                     const float v = fmaf(p, c & 1 ? f.y : f.x, kZero ? z[j][c >> 1] * xc : xc);
                                     acc[j][nt][c] = fmaf(v, sc[j][c >> 1], acc[j][nt][c]);
-                                    part[j][nt][c] = kMagic;
                                 }
                         }
                     }
@@ -518,8 +550,14 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&s_free[buffer]));
-        s.release(unit, ok);
-        if (unit % a.k_blocks == a.k_blocks - 1 || unit == u1 - 1) {
+        s.release(ok);
+        buffer = buffer_next;
+        round = round_next;
+        if (++buffer_next == kDigitBuffers) {
+            buffer_next = 0;
+            ++round_next;
+        }
+        if (s.finishes()) {
             float v[2][1][4];                          // the digits of a row together
 #pragma unroll
             for (int j = 0; j < 2; ++j)
@@ -534,7 +572,7 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
 #pragma unroll
                     for (int nt = 0; nt < kTiles; ++nt) acc[j][nt][c] = 0.f;
                 }
-            finish_rows<T, 1>(a, s, unit, v, kRows, open);
+            finish_rows<T, 1>(a, s, v, kRows, open);
         }
     }
     if (!ok) {
@@ -559,31 +597,29 @@ linear_wide_kernel(const __grid_constant__ LinearArgs a)
     if (tid == 0) s_failed = 0;
     fence_barrier_init();
     __syncthreads();
-    const int u0 = min(static_cast<int>(blockIdx.x) * a.share, a.units), u1 = min(u0 + a.share, a.units);
-    Stream s{a, smem_u32(smem) + 2 * 8 * kNt * kRowPitch + warp * a.stages * a.block_bytes, s_full[warp], u0, u1, warp, lane, 0, 0, 0};
-    s.start();
+    Stream s(a, smem_u32(smem) + 2 * 8 * kNt * kRowPitch + warp * a.stages * a.block_bytes, s_full[warp]);
 
     // x of a unit: thread i takes eight columns (i % 32) of rows i / 32, + 8, ..; in the order of the operand (0 2, 4 6, 1 3, 5 7)
     uint4 held[kNt];
-    auto fetch = [&](int unit) {
-        const int kb = unit % a.k_blocks, have = a.k - kb * kKBlock - 8 * lane;
-        const int64_t r0 = static_cast<int64_t>(unit / (a.k_blocks * a.row_blocks)) * (8 * kNt) + warp;
+    auto fetch = [&](const Place& at) {
+        const int have = a.k - at.kb * kKBlock - 8 * lane;
+        const int64_t r0 = static_cast<int64_t>(at.pass) * (8 * kNt) + warp;
 #pragma unroll
         for (int nt = 0; nt < kNt; ++nt) {
             held[nt] = make_uint4(0, 0, 0, 0);
             if (r0 + 8 * nt < a.rows && have > 0)
-                held[nt] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.x) + (r0 + 8 * nt) * a.x_stride + kb * kKBlock + 8 * lane));
+                held[nt] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.x) + (r0 + 8 * nt) * a.x_stride + at.kb * kKBlock + 8 * lane));
         }
     };
-    auto store = [&](int unit) {
-        const int have = a.k - unit % a.k_blocks * kKBlock - 8 * lane;
+    auto store = [&](const Place& at, int buffer) {
+        const int have = a.k - at.kb * kKBlock - 8 * lane;
 #pragma unroll
         for (int nt = 0; nt < kNt; ++nt) {
             uint32_t w[4] = {held[nt].x, held[nt].y, held[nt].z, held[nt].w};
             if (have > 0 && have < 8)                  // the last columns: what lies behind them is not data
 #pragma unroll
                 for (int c = 0; c < 4; ++c) w[c] = have >= 2 * c + 2 ? w[c] : have == 2 * c + 1 ? w[c] & 0xffffu : 0u;
-            *reinterpret_cast<uint4*>(smem + ((unit - u0) & 1) * (8 * kNt * kRowPitch) + (8 * nt + warp) * kRowPitch + lane * 16) =
+            *reinterpret_cast<uint4*>(smem + buffer * (8 * kNt * kRowPitch) + (8 * nt + warp) * kRowPitch + lane * 16) =
                 make_uint4(__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410), __byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632));
         }
     };
@@ -591,17 +627,20 @@ linear_wide_kernel(const __grid_constant__ LinearArgs a)
     float acc[2][kNt][4] = {};
     int open[2] = {-1, -1};
     bool ok = true;
-    if (u0 < u1) {
-        fetch(u0);
-        store(u0);
+    if (s.u0 < s.u1) {
+        fetch(s.here);
+        store(s.here, 0);
         __syncthreads();
     }
-    for (int unit = u0; unit < u1; ++unit) {
-        if (unit + 1 < u1) fetch(unit + 1);
-        ok = s.wait(unit) && ok;
-        if (ok && s.tile_of(unit) < a.row_tiles) {
+    int buffer = 0;
+    for (; s.unit < s.u1; s.next(), buffer ^= 1) {
+        Place after = s.here;
+        after.next(a);
+        if (s.unit + 1 < s.u1) fetch(after);
+        ok = s.wait() && ok;
+        if (ok && s.has_rows()) {
             const uint32_t block = s.block(), scales = block + kCodeBytes, zeros = scales + a.per_block * kRowTile * 2;
-            const uint32_t x = smem_u32(smem) + ((unit - u0) & 1) * (8 * kNt * kRowPitch) + g * kRowPitch + t4 * 16;
+            const uint32_t x = smem_u32(smem) + buffer * (8 * kNt * kRowPitch) + g * kRowPitch + t4 * 16;
 #pragma unroll 1
             for (int chunk = 0; chunk < 4; ++chunk) {
                 uint32_t w[2][2][2][4];                // [half of the rows][half of the columns][row g, g + 8][pair]
@@ -651,11 +690,11 @@ linear_wide_kernel(const __grid_constant__ LinearArgs a)
                 }
             }
         }
-        s.release(unit, ok);
-        if (unit + 1 < u1) store(unit + 1);
+        s.release(ok);
+        if (s.unit + 1 < s.u1) store(after, buffer ^ 1);
         __syncthreads();                               // the next unit's x is there, this one's is free
-        if (unit % a.k_blocks == a.k_blocks - 1 || unit == u1 - 1) {
-            finish_rows<T, kNt>(a, s, unit, acc, 8, open);
+        if (s.finishes()) {
+            finish_rows<T, kNt>(a, s, acc, 8, open);
 #pragma unroll
             for (int i = 0; i < 8 * kNt; ++i) (&acc[0][0][0])[i] = 0.f;
         }
@@ -689,7 +728,11 @@ template <typename T, int kTiles>
 qtz_status launch_digits(qtz_linear* p, LinearArgs& a, bool zero, cudaStream_t st)
 {
     constexpr int kFixed = kDigitBuffers * sizeof(Digits<kTiles>);
-    return zero ? launch(p, a, linear_digits_kernel<T, kTiles, true>, kFixed, 32, st) : launch(p, a, linear_digits_kernel<T, kTiles, false>, kFixed, 32, st);
+    if (p->scales == 8)
+        return zero ? launch(p, a, linear_digits_kernel<T, kTiles, 1, true>, kFixed, 32, st) : launch(p, a, linear_digits_kernel<T, kTiles, 1, false>, kFixed, 32, st);
+    if (p->scales == 4)
+        return zero ? launch(p, a, linear_digits_kernel<T, kTiles, 2, true>, kFixed, 32, st) : launch(p, a, linear_digits_kernel<T, kTiles, 2, false>, kFixed, 32, st);
+    return zero ? launch(p, a, linear_digits_kernel<T, kTiles, 4, true>, kFixed, 32, st) : launch(p, a, linear_digits_kernel<T, kTiles, 4, false>, kFixed, 32, st);
 }
 
 template <typename T, int kNt>
@@ -758,7 +801,7 @@ extern "C" qtz_status qtz_linear_create(qtz_handle h, const qtz_linear_desc* des
     p->d = d;
     p->row_tiles = static_cast<int>(row_tiles);
     p->k_blocks = static_cast<int>(k_blocks);
-    p->scales = d.group == 32 ? 8 : d.group % 256 == 0 ? 1 : d.group % 128 == 0 ? 2 : 4;
+    p->scales = d.group == 32 ? 8 : d.group % 128 == 0 ? 2 : 4;
     // unsigned codes without zero points are codes with zero points 0: the kernel's constant stands for 8
     const bool zero = d.wdtype == QTZ_U4_PACKED;
     p->block_bytes = kCodeBytes + p->scales * kRowTile * (zero ? 3 : 2);
