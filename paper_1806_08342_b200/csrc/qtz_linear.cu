@@ -127,6 +127,19 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
             : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+template <typename T>
+__device__ __forceinline__ void mma_from_zero(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    if constexpr (std::is_same<T, __half>::value)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+
 // (a & mask) | exponent in one operation
 __device__ __forceinline__ uint32_t cut(uint32_t a, uint32_t mask, uint32_t exponent)
 {
@@ -582,10 +595,10 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
     join_rows<T, 1>(a, s, open, kRows, s_failed, s_last);
 }
 
-// ---- more rows: 16-bit matrix instructions; kNt: blocks of eight rows; kFine: groups of 32 columns; kZero: with zero points ----
+// ---- more rows: 16-bit matrix instructions; kNt: blocks of eight rows; kSteps: steps of 32 columns to a scale (1, 2 or 4) ----
 constexpr int kRowPitch = 2 * kKBlock + 64;            // bytes of a row of x in shared memory: the lanes of a load meet all banks
 
-template <typename T, int kNt, bool kFine, bool kZero>
+template <typename T, int kNt, int kSteps, bool kZero>
 __global__ void __launch_bounds__(kThreads, 2)
 linear_wide_kernel(const __grid_constant__ LinearArgs a)
 {
@@ -639,54 +652,59 @@ linear_wide_kernel(const __grid_constant__ LinearArgs a)
         if (s.unit + 1 < s.u1) fetch(after);
         ok = s.wait() && ok;
         if (ok && s.has_rows()) {
-            const uint32_t block = s.block(), scales = block + kCodeBytes, zeros = scales + a.per_block * kRowTile * 2;
+            const uint32_t block = s.block(), scales = block + kCodeBytes, zeros = scales + 8 / kSteps * kRowTile * 2;
             const uint32_t x = smem_u32(smem) + buffer * (8 * kNt * kRowPitch) + g * kRowPitch + t4 * 16;
+            float part[2][kNt][4];
 #pragma unroll 1
-            for (int chunk = 0; chunk < 4; ++chunk) {
-                uint32_t w[2][2][2][4];                // [half of the rows][half of the columns][row g, g + 8][pair]
-                float sc[2][kFine ? 2 : 1][2];
+            for (int pair = 0; pair < 2; ++pair) {     // 128 columns
+                float sc[2][2];
+                uint32_t z[2] = {0x0808u, 0x0808u};
+                uint4 q[2];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const uint4 q = lds128(block + (chunk * 2 + j) * 512 + lane * 16);
-                    uint32_t z = 0x0808u;
+                for (int i = 0; i < 4; ++i) {          // 32 columns
+                    const int step = 4 * pair + i;
+                    if (i % kSteps == 0)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        if (kFine || h == 0) {
-                            const int si = kFine ? 2 * chunk + h : chunk * a.per_block / 4, at = (si * 2 + j) * 8 + g;
+                        for (int j = 0; j < 2; ++j) {
+                            const int at = (step / kSteps * 2 + j) * 8 + g;
                             const float2 f = qtz_dev::unpack2(lds32(scales + 4 * at), T());
-                            sc[j][kFine ? h : 0][0] = f.x;
-                            sc[j][kFine ? h : 0][1] = f.y;
-                            if (kZero) z = lds16(zeros + 2 * at);
+                            sc[j][0] = f.x;
+                            sc[j][1] = f.y;
+                            if (kZero) z[j] = lds16(zeros + 2 * at);
                         }
-                        unpack_codes<T>(h ? q.z : q.x, (z & 0xffu) * 0x00010001u, w[j][h][0]);
-                        unpack_codes<T>(h ? q.w : q.y, (z >> 8) * 0x00010001u, w[j][h][1]);
+                    uint32_t w[2][2][4];               // [half of the rows][row g, g + 8][pair]
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        if (i % 2 == 0) q[j] = lds128(block + (step / 2 * 2 + j) * 512 + lane * 16);
+                        unpack_codes<T>(i % 2 ? q[j].z : q[j].x, (z[j] & 0xffu) * 0x00010001u, w[j][0]);
+                        unpack_codes<T>(i % 2 ? q[j].w : q[j].y, (z[j] >> 8) * 0x00010001u, w[j][1]);
                     }
-                }
+                    uint4 b[kNt];
 #pragma unroll
-                for (int nt = 0; nt < kNt; ++nt) {
-                    float part[2][4] = {};
+                    for (int nt = 0; nt < kNt; ++nt) b[nt] = lds128(x + nt * 8 * kRowPitch + step * 64);
+                    // neighbouring instructions write different sums
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uint4 b = lds128(x + nt * 8 * kRowPitch + chunk * 128 + h * 64);
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const uint32_t first[4] = {w[j][h][0][0], w[j][h][1][0], w[j][h][0][1], w[j][h][1][1]};
-                            mma<T>(part[j], first, b.x, b.y);
-                        }
+                    for (int nt = 0; nt < kNt; ++nt)
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
-                            const uint32_t second[4] = {w[j][h][0][2], w[j][h][1][2], w[j][h][0][3], w[j][h][1][3]};
-                            mma<T>(part[j], second, b.z, b.w);
+                            const uint32_t op[4] = {w[j][0][0], w[j][1][0], w[j][0][1], w[j][1][1]};
+                            if (i % kSteps == 0) mma_from_zero<T>(part[j][nt], op, b[nt].x, b[nt].y);
+                            else mma<T>(part[j][nt], op, b[nt].x, b[nt].y);
                         }
-                        if (kFine || h == 1)
+#pragma unroll
+                    for (int nt = 0; nt < kNt; ++nt)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const uint32_t op[4] = {w[j][0][2], w[j][1][2], w[j][0][3], w[j][1][3]};
+                            mma<T>(part[j][nt], op, b[nt].z, b[nt].w);
+                        }
+                    if ((i + 1) % kSteps == 0)
+#pragma unroll
+                        for (int nt = 0; nt < kNt; ++nt)
 #pragma unroll
                             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                                for (int c = 0; c < 4; ++c) {
-                                    acc[j][nt][c] = fmaf(part[j][c], sc[j][kFine ? h : 0][c >> 1], acc[j][nt][c]);
-                                    part[j][c] = 0.f;
-                                }
-                    }
+                                for (int c = 0; c < 4; ++c) acc[j][nt][c] = fmaf(part[j][nt][c], sc[j][c >> 1], acc[j][nt][c]);
                 }
             }
         }
@@ -740,8 +758,10 @@ qtz_status launch_wide(qtz_linear* p, LinearArgs& a, bool zero, cudaStream_t st)
 {
     constexpr int kFixed = 2 * 8 * kNt * kRowPitch;
     if (p->scales == 8)
-        return zero ? launch(p, a, linear_wide_kernel<T, kNt, true, true>, kFixed, 8, st) : launch(p, a, linear_wide_kernel<T, kNt, true, false>, kFixed, 8, st);
-    return zero ? launch(p, a, linear_wide_kernel<T, kNt, false, true>, kFixed, 8, st) : launch(p, a, linear_wide_kernel<T, kNt, false, false>, kFixed, 8, st);
+        return zero ? launch(p, a, linear_wide_kernel<T, kNt, 1, true>, kFixed, 8, st) : launch(p, a, linear_wide_kernel<T, kNt, 1, false>, kFixed, 8, st);
+    if (p->scales == 4)
+        return zero ? launch(p, a, linear_wide_kernel<T, kNt, 2, true>, kFixed, 8, st) : launch(p, a, linear_wide_kernel<T, kNt, 2, false>, kFixed, 8, st);
+    return zero ? launch(p, a, linear_wide_kernel<T, kNt, 4, true>, kFixed, 8, st) : launch(p, a, linear_wide_kernel<T, kNt, 4, false>, kFixed, 8, st);
 }
 
 template <typename T>
