@@ -168,17 +168,17 @@ def _check_dev(*ts):
             raise ValueError("expected contiguous CUDA tensors")
 
 
+# The serving calls are short on the GPU: their checks stay cheap (get_device is -1 for a tensor that is not on a GPU).
 def _check_on(device, dtype, *ts):
     for t in ts:
-        if t.dtype != dtype or t.device.type != "cuda" or t.device.index != device:
+        if t.dtype is not dtype or t.get_device() != device:
             raise ValueError(f"expected {dtype} tensors on cuda:{device}, got {t.dtype} on {t.device}")
 
 
 def _check_flat(device, dtype, *ts):
-    _check_on(device, dtype, *ts)
     for t in ts:
-        if not t.is_contiguous():
-            raise ValueError("expected contiguous tensors")
+        if t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+            raise ValueError(f"expected contiguous {dtype} tensors on cuda:{device}, got {t.dtype} on {t.device}")
 
 
 def _raw_stream(device):
@@ -555,16 +555,19 @@ class Handle:
 
     def kv_schedule(self, cached, added, table, free, free_count, block_tokens, capacity):
         """qtz_kv_schedule: writes the new blocks into `table` and returns (starts, lens, slots, report)."""
-        _check_flat(self.device, torch.int32, cached, added, table, free, free_count)
-        b = cached.shape[0]
-        if added.shape != (b,) or table.dim() != 2 or table.shape[0] != b:
+        device = self.device
+        _check_flat(device, torch.int32, cached, added, table, free, free_count)
+        b, (rows, width) = cached.numel(), table.shape
+        if added.numel() != b or rows != b or free_count.numel() != 1:
             raise ValueError("cached, added and table describe different numbers of requests")
-        out = torch.empty(2 * b + 1 + 4, dtype=torch.int32, device=cached.device)
-        slots = torch.empty(capacity, dtype=torch.int64, device=cached.device)
-        starts, lens, report = out[4:b + 5], out[b + 5:], out[:4]
-        self._chk(self.lib.qtz_kv_schedule(self.h, cached.data_ptr(), added.data_ptr(), b, block_tokens, table.data_ptr(), table.shape[1],
-                                           free.data_ptr(), free_count.data_ptr(), starts.data_ptr(), lens.data_ptr(), slots.data_ptr(),
-                                           capacity, report.data_ptr(), _raw_stream(self.device)), "qtz_kv_schedule")
+        slots = cached.new_empty(capacity, dtype=torch.int64)
+        starts, lens, report = cached.new_empty(2 * b + 5).split_with_sizes((b + 1, b, 4))
+        at = starts.data_ptr()
+        rc = self.lib.qtz_kv_schedule(self.h, cached.data_ptr(), added.data_ptr(), b, block_tokens, table.data_ptr(), width, free.data_ptr(),
+                                      free_count.data_ptr(), at, at + 4 * (b + 1), slots.data_ptr(), capacity, at + 4 * (2 * b + 1),
+                                      _raw_stream(device))
+        if rc:
+            self._chk(rc, "qtz_kv_schedule")
         return starts, lens, slots, report
 
     def kv_cache(self, blocks, kv_heads, block_tokens, head_dim):
@@ -675,30 +678,34 @@ class LinearPlan:
     """Owns a qtz_linear_plan: y = x W^T + bias with 4-bit weights."""
 
     def __init__(self, handle: Handle, plan, desc: LinearDesc, dtype):
-        self.handle, self.plan, self.desc, self.dtype = handle, plan, desc, dtype
+        self.handle, self.plan, self.desc, self.dtype, self.device = handle, plan, desc, dtype, handle.device
+        self.n, self.k, self.k_up = desc.n, desc.k, (desc.k + 7) // 8 * 8
         self._run = handle.lib.qtz_linear_w4
 
     def __call__(self, x, out=None):
         """x [rows][k] (or more leading axes that fold into rows); rows may lie apart by a multiple of 16 bytes."""
-        n, k = self.desc.n, self.desc.k
+        n, k, dtype = self.n, self.k, self.dtype
+        lead = x.shape[:-1]
         if x.shape[-1] != k or x.stride(-1) != 1:
             raise ValueError(f"expected rows of {k} neighbouring values, got {tuple(x.shape)} with strides {x.stride()}")
-        _check_on(self.handle.device, self.dtype, x)
-        lead = x.shape[:-1]
-        if x.dim() != 2:
+        if x.dtype is not dtype or x.get_device() != self.device:
+            raise ValueError(f"expected {dtype} on cuda:{self.device}, got {x.dtype} on {x.device}")
+        if len(lead) != 1:
             x = x.view(-1, k)
+        rows = x.shape[0]
         if out is None:
-            out = torch.empty(lead + (n,), dtype=self.dtype, device=x.device)
+            y = x.new_empty((rows, n))
+            out = y if len(lead) == 1 else y.view(*lead, n)
         else:
-            _check_on(self.handle.device, self.dtype, out)
+            _check_on(self.device, dtype, out)
             if out.shape != lead + (n,) or out.stride(-1) != 1:
                 raise ValueError("out has another shape")
-        y = out if out.dim() == 2 else out.view(-1, n)
-        rows = x.shape[0]
+            y = out if len(lead) == 1 else out.view(-1, n)
         # a single row has no stride to keep: torch reports any value for it
-        xs = (k + 7) // 8 * 8 if rows == 1 else x.stride(0)
-        rc = self._run(self.plan, x.data_ptr(), xs, rows, y.data_ptr(), n if rows == 1 else y.stride(0),
-                       _raw_stream(self.handle.device))
+        if rows == 1:
+            rc = self._run(self.plan, x.data_ptr(), self.k_up, 1, y.data_ptr(), n, _raw_stream(self.device))
+        else:
+            rc = self._run(self.plan, x.data_ptr(), x.stride(0), rows, y.data_ptr(), y.stride(0), _raw_stream(self.device))
         if rc:
             self.handle._chk(rc, "qtz_linear_w4")
         return out
@@ -728,58 +735,57 @@ class KvCache:
         self.blocks, self.kv_heads, self.block_tokens, self.head_dim = k.shape
         self._desc = KvCacheDesc(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), *k.shape)
         self._ref = byref(self._desc)
+        self.device, self.lib, self.h, self.scale = handle.device, handle.lib, handle.h, self.head_dim ** -0.5
         self.workspace = None
 
     def append(self, k, v, slots):
         """Quantizes new keys and values [tokens][kv_heads][head_dim] (any token and head stride) into `slots`."""
-        dev = self.handle.device
-        _check_on(dev, k.dtype, k, v)
+        dev, dtype, shape = self.device, k.dtype, (slots.numel(), self.kv_heads, self.head_dim)
         _check_flat(dev, torch.int64, slots)
-        shape = (slots.shape[0], self.kv_heads, self.head_dim)
-        if k.shape != shape or v.shape != shape or k.stride(2) != 1 or v.stride(2) != 1 or k.dtype not in FTYPES:
+        _check_on(dev, dtype, k, v)
+        ks, vs = k.stride(), v.stride()
+        if k.shape != shape or v.shape != shape or ks[2] != 1 or vs[2] != 1 or dtype not in FTYPES:
             raise ValueError(f"expected keys and values of shape {shape}")
-        rc = self.handle.lib.qtz_kv_append(self.handle.h, self._ref, k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0),
-                                           v.stride(1), FTYPES[k.dtype], slots.data_ptr(), shape[0], _raw_stream(dev))
+        rc = self.lib.qtz_kv_append(self.h, self._ref, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], FTYPES[dtype],
+                                    slots.data_ptr(), shape[0], _raw_stream(dev))
         if rc:
             self.handle._chk(rc, "qtz_kv_append")
 
     def read(self, slots, dtype=torch.float32):
         """Real values of the slots: keys and values [tokens][kv_heads][head_dim]."""
-        dev = self.handle.device
+        dev, tokens = self.device, slots.numel()
         _check_flat(dev, torch.int64, slots)
-        k, v = torch.empty((2, slots.shape[0], self.kv_heads, self.head_dim), dtype=dtype, device=slots.device).unbind(0)
-        rc = self.handle.lib.qtz_kv_read(self.handle.h, self._ref, slots.data_ptr(), slots.shape[0], FTYPES.get(dtype, -1), k.data_ptr(),
-                                         v.data_ptr(), _raw_stream(dev))
+        k, v = slots.new_empty((2, tokens, self.kv_heads, self.head_dim), dtype=dtype).unbind(0)
+        rc = self.lib.qtz_kv_read(self.h, self._ref, slots.data_ptr(), tokens, FTYPES.get(dtype, -1), k.data_ptr(), v.data_ptr(),
+                                  _raw_stream(dev))
         if rc:
             self.handle._chk(rc, "qtz_kv_read")
         return k, v
 
     def attention(self, q, starts, lens, table, scale=None, window=0, out=None, return_lse=False):
         """q [tokens][q_heads][head_dim] of the requests' newest tokens (rows starts[r] .. starts[r + 1]); returns y, or (y, lse)."""
-        dev = self.handle.device
-        dtype = q.dtype
+        dev, dtype, shape = self.device, q.dtype, q.shape
         _check_on(dev, dtype, q)
         _check_flat(dev, torch.int32, starts, lens, table)
-        b = lens.shape[0]
-        if q.dim() != 3 or q.shape[2] != self.head_dim or q.stride(2) != 1 or dtype not in FTYPES:
+        b, (rows, width), qs = lens.numel(), table.shape, q.stride()
+        if len(shape) != 3 or shape[2] != self.head_dim or qs[2] != 1 or dtype not in FTYPES:
             raise ValueError(f"expected queries [tokens][heads][{self.head_dim}]")
-        if starts.shape != (b + 1,) or table.dim() != 2 or table.shape[0] != b:
+        if starts.numel() != b + 1 or rows != b:
             raise ValueError("starts, lens and table describe different numbers of requests")
         if out is None:
-            out = torch.empty(q.shape, dtype=dtype, device=q.device)
+            out = q.new_empty(shape)
         else:
             _check_on(dev, dtype, out)
-            if out.shape != q.shape or out.stride(2) != 1:
+            if out.shape != shape or out.stride(2) != 1:
                 raise ValueError("out has another shape")
-        lib, h = self.handle.lib, self.handle.h
         if self.workspace is None:
-            size = lib.qtz_kv_attention_workspace_bytes(h, self._ref)
+            size = self.lib.qtz_kv_attention_workspace_bytes(self.h, self._ref)
             self.workspace = torch.zeros(max(size, 16), dtype=torch.uint8, device=q.device)
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if return_lse else None
-        rc = lib.qtz_kv_attention(h, self._ref, q.data_ptr(), q.stride(0), q.stride(1), q.shape[1], FTYPES[dtype], starts.data_ptr(),
-                                  lens.data_ptr(), b, q.shape[0], table.data_ptr(), table.shape[1],
-                                  self.head_dim ** -0.5 if scale is None else scale, window, out.data_ptr(), out.stride(0), out.stride(1),
-                                  None if lse is None else lse.data_ptr(), self.workspace.data_ptr(), _raw_stream(dev))
+        lse = q.new_empty(shape[:2], dtype=torch.float32) if return_lse else None
+        ys = out.stride()
+        rc = self.lib.qtz_kv_attention(self.h, self._ref, q.data_ptr(), qs[0], qs[1], shape[1], FTYPES[dtype], starts.data_ptr(), lens.data_ptr(), b,
+                                       shape[0], table.data_ptr(), width, self.scale if scale is None else scale, window, out.data_ptr(), ys[0],
+                                       ys[1], lse.data_ptr() if return_lse else None, self.workspace.data_ptr(), _raw_stream(dev))
         if rc:
             self.handle._chk(rc, "qtz_kv_attention")
         return (out, lse) if return_lse else out
