@@ -482,8 +482,8 @@ typedef struct {
     int32_t wdtype; /* QTZ_S4_PACKED or QTZ_U4_PACKED                         */
     int32_t ftype;  /* QTZ_F16 or QTZ_BF16: type of x, y, scales and bias     */
 } qtz_linear_desc;
-/* One-time preparation: copies codes, scales, zero points and bias into the order the kernel reads.  The caller
- * may free or overwrite all inputs once `stream` has passed this call.                                          */
+/* One-time preparation: copies codes, scales, zero points and bias into the order the kernel reads.  BLOCKS until
+ * `stream` has finished; the caller may then free or overwrite all inputs.                                       */
 QTZ_API qtz_status qtz_linear_create(qtz_handle h, const qtz_linear_desc* desc, const void* codes_dev, const void* scales_dev,
                                      const uint8_t* zeros_dev, const void* bias_dev, qtz_linear_plan* out, void* stream);
 QTZ_API qtz_status qtz_linear_destroy(qtz_linear_plan p);

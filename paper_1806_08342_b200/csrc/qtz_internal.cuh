@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include <string>
+#include <utility>
 
 #include "qtz.h"
 
@@ -26,6 +27,8 @@ struct qtz_ctx {
     size_t reduce_host_bytes = 0;
     void* linear_dev = nullptr;             // parts and counters of linear layers (allocated with the first layer)
     int32_t* linear_counters = nullptr;     // within it
+    const void* smem_ready[128] = {};       // kernels that may use all of an SM's shared memory (qtz_allow_smem)
+    int smem_ready_count = 0;
     bool no_pairs = false;                  // never run layers on CTA pairs (A/B comparisons; set by QTZ_NO_PAIRS=1)
     bool single_row_stems = false;          // row-window layers: one output row per tile (A/B comparisons; QTZ_SINGLE_ROW_STEMS=1)
     long long wait_budget = 2000000000LL;   // cycle budget of every bounded device-side wait (about one second)
@@ -74,6 +77,38 @@ struct qtz_device_guard {
     qtz_device_guard(const qtz_device_guard&) = delete;
     qtz_device_guard& operator=(const qtz_device_guard&) = delete;
 };
+
+// Lets a kernel ask for as much dynamic shared memory as a CTA may have; once per kernel and handle.
+template <typename K>
+qtz_status qtz_allow_smem(qtz_ctx* h, K* kernel)
+{
+    const void* id = reinterpret_cast<const void*>(kernel);
+    for (int i = 0; i < h->smem_ready_count; ++i)
+        if (h->smem_ready[i] == id) return QTZ_OK;
+    cudaFuncAttributes at;
+    QTZ_CUDA(h, cudaFuncGetAttributes(&at, id));
+    QTZ_CUDA(h, cudaFuncSetAttribute(id, cudaFuncAttributeMaxDynamicSharedMemorySize, 227 * 1024 - static_cast<int>(at.sharedSizeBytes)));
+    if (h->smem_ready_count < 128) h->smem_ready[h->smem_ready_count++] = id;
+    return QTZ_OK;
+}
+
+// Launch that may begin while the kernel before it in the stream still runs; the kernel calls grid_dependency_wait() before it
+// touches what others read or write.
+template <typename... P, typename... A>
+cudaError_t qtz_launch_dependent(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, A&&... args)
+{
+    cudaLaunchAttribute at;
+    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = &at;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
+}
 
 static inline bool qtz_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 

@@ -269,6 +269,9 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         tmem_relinquish();
     }
 
+    grid_launch_dependents();
+    grid_dependency_wait();                            // everything up to here was this CTA's own
+
     // ---- units before each request: an exclusive prefix sum over the requests ----
     const int per = (a.requests + kThreads - 1) / kThreads;
     const int r_lo = min(tid * per, a.requests), r_hi = min(r_lo + per, a.requests);
@@ -900,9 +903,9 @@ qtz_status launch(qtz_ctx* h, AttnArgs& a, const CUtensorMap& km, const CUtensor
     a.stages = room / kStage < kMaxStages ? room / kStage : kMaxStages;
     if (a.stages < 2) return QTZ_ERR_TOO_LARGE;
     const int smem = fixed + a.stages * kStage;
-    QTZ_CUDA(h, cudaFuncSetAttribute(attention_kernel<T, D, kRows>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    attention_kernel<T, D, kRows><<<h->num_sms * ctas, kThreads, smem, st>>>(a, km, vm);
-    QTZ_LAUNCH_CHECK(h, "attention_kernel");
+    const qtz_status s = qtz_allow_smem(h, attention_kernel<T, D, kRows>);
+    if (s != QTZ_OK) return s;
+    QTZ_CUDA(h, qtz_launch_dependent(attention_kernel<T, D, kRows>, dim3(h->num_sms * ctas), kThreads, smem, st, a, km, vm));
     return QTZ_OK;
 }
 

@@ -3,6 +3,8 @@
 #include "qtz_kv.cuh"
 #include "qtz_ptx.cuh"
 
+using qtz_ptx::grid_dependency_wait;
+using qtz_ptx::grid_launch_dependents;
 using qtz_ptx::redux_max;
 
 namespace {
@@ -34,6 +36,8 @@ __global__ void __launch_bounds__(kSchedThreads)
 schedule_kernel(const __grid_constant__ ScheduleArgs a)
 {
     extern __shared__ int32_t sm[];
+    grid_launch_dependents();
+    grid_dependency_wait();
     int32_t* const tok = sm;                  // [requests + 1]
     int32_t* const blk = sm + a.requests + 1; // [requests + 1]
     __shared__ int64_t w_tok[kSchedThreads / 32], w_blk[kSchedThreads / 32];
@@ -254,6 +258,8 @@ __global__ void __launch_bounds__(kThreads)
 append_kernel(const __grid_constant__ AppendArgs a)
 {
     __shared__ int64_t s_slot[kMaxWindow + 1];
+    grid_launch_dependents();
+    grid_dependency_wait();
     __shared__ int s_start[kMaxWindow], s_count;
     __shared__ float s_top[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, heads = a.c.kv_heads, dim = a.c.head_dim;
@@ -415,7 +421,9 @@ read_kernel(const __grid_constant__ ReadArgs a)
 {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
     const int lane = threadIdx.x & 31;
+    grid_launch_dependents();
     if (i >= a.tokens) return;
+    grid_dependency_wait();
     const int64_t slot = a.slots[i];
     const uint32_t block = a.c.block_tokens;
     const bool bad = slot >= static_cast<int64_t>(a.c.blocks) * block, none = slot < 0 || bad;
@@ -483,11 +491,11 @@ extern "C" qtz_status qtz_kv_schedule(qtz_handle h, const int32_t* cached_dev, c
     const ScheduleArgs a{cached_dev, added_dev, requests, static_cast<uint32_t>(block_tokens), table_width, table_dev, free_dev, free_count_dev,
                          starts_dev, lens_dev, slots_dev, capacity, report_dev};
     const size_t smem = 2 * sizeof(int32_t) * (requests + 1);
-    QTZ_CUDA(h, cudaFuncSetAttribute(schedule_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * sizeof(int32_t) * (kMaxRequests + 1)));
-    const int64_t work = capacity > requests + 1 ? capacity : requests + 1;
-    const int64_t ctas = (work + kSchedThreads - 1) / kSchedThreads;
-    schedule_kernel<<<static_cast<unsigned>(ctas < h->num_sms ? ctas : h->num_sms), kSchedThreads, smem, static_cast<cudaStream_t>(stream)>>>(a);
-    QTZ_LAUNCH_CHECK(h, "schedule_kernel");
+    qtz_status s = qtz_allow_smem(h, schedule_kernel);
+    if (s != QTZ_OK) return s;
+    const int64_t work = capacity > requests + 1 ? capacity : requests + 1, ctas = (work + kSchedThreads - 1) / kSchedThreads;
+    QTZ_CUDA(h, qtz_launch_dependent(schedule_kernel, dim3(static_cast<unsigned>(ctas < h->num_sms ? ctas : h->num_sms)), kSchedThreads, smem,
+                                     static_cast<cudaStream_t>(stream), a));
     return QTZ_OK;
 }
 
@@ -513,9 +521,7 @@ extern "C" qtz_status qtz_kv_append(qtz_handle h, const qtz_kv_cache* cache, con
                        static_cast<int32_t>(window), h->status_dev};
     const dim3 grid(static_cast<unsigned>(ctas), static_cast<unsigned>(cache->kv_heads), 2);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (ftype == QTZ_F16) append_kernel<__half><<<grid, kThreads, 0, st>>>(a);
-    else append_kernel<__nv_bfloat16><<<grid, kThreads, 0, st>>>(a);
-    QTZ_LAUNCH_CHECK(h, "append_kernel");
+    QTZ_CUDA(h, qtz_launch_dependent(ftype == QTZ_F16 ? append_kernel<__half> : append_kernel<__nv_bfloat16>, grid, kThreads, 0, st, a));
     return QTZ_OK;
 }
 
@@ -534,10 +540,7 @@ extern "C" qtz_status qtz_kv_read(qtz_handle h, const qtz_kv_cache* cache, const
     qtz_device_guard guard(h->device);
     const ReadArgs a{*cache, slots_dev, tokens, {k_out_dev, v_out_dev}, h->status_dev};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const unsigned g = static_cast<unsigned>(ctas);
-    if (ftype == QTZ_F16) read_kernel<__half><<<g, kThreads, 0, st>>>(a);
-    else if (ftype == QTZ_BF16) read_kernel<__nv_bfloat16><<<g, kThreads, 0, st>>>(a);
-    else read_kernel<float><<<g, kThreads, 0, st>>>(a);
-    QTZ_LAUNCH_CHECK(h, "read_kernel");
+    QTZ_CUDA(h, qtz_launch_dependent(ftype == QTZ_F16 ? read_kernel<__half> : ftype == QTZ_BF16 ? read_kernel<__nv_bfloat16> : read_kernel<float>,
+                                     dim3(static_cast<unsigned>(ctas)), kThreads, 0, st, a));
     return QTZ_OK;
 }

@@ -245,6 +245,9 @@ struct Stream {
         : a(args), ring(ring_), full(full_), u0(min(static_cast<int>(blockIdx.x) * args.share, args.units)), u1(min(u0 + args.share, args.units)),
           warp(threadIdx.x >> 5), lane(threadIdx.x & 31), here(args, u0), ahead(here), unit(u0), issued(0), stage(0), phase(0)
     {
+    }
+    __device__ __forceinline__ void start()
+    {
         for (int i = 0; i < min(a.stages, u1 - u0); ++i) issue(i);
     }
     __device__ __forceinline__ int tile(const Place& p) const { return p.rb * kWarps + warp; }
@@ -430,6 +433,9 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
     fence_barrier_init();
     __syncthreads();
     Stream s(a, smem_u32(smem) + kDigitBuffers * static_cast<uint32_t>(sizeof(Digits<kTiles>)) + warp * a.stages * a.block_bytes, s_full[warp]);
+    grid_launch_dependents();
+    s.start();                                         // the weights were there when the layer was made; all else is waited for
+    grid_dependency_wait();
     bool ok = true;
 
     // Rows of x become digits one unit ahead; row r of the CTA's unit i is the work of warp (i + r) % 8.  `buffer` and `round`: i
@@ -612,6 +618,10 @@ linear_wide_kernel(const __grid_constant__ LinearArgs a)
     __syncthreads();
     Stream s(a, smem_u32(smem) + 2 * 8 * kNt * kRowPitch + warp * a.stages * a.block_bytes, s_full[warp]);
 
+    grid_launch_dependents();
+    s.start();                                         // the weights were there when the layer was made; all else is waited for
+    grid_dependency_wait();
+
     // x of a unit: thread i takes eight columns (i % 32) of rows i / 32, + 8, ..; in the order of the operand (0 2, 4 6, 1 3, 5 7)
     uint4 held[kNt];
     auto fetch = [&](const Place& at) {
@@ -736,9 +746,9 @@ qtz_status launch(qtz_linear* p, LinearArgs& a, K kernel, int fixed, int most_pa
     // A share takes in at least 1 / most_parts of the columns: joining costs more than it brings beyond that.
     a.share = (a.units + grid - 1) / grid;
     if (a.share < (a.k_blocks + most_parts - 1) / most_parts) a.share = (a.k_blocks + most_parts - 1) / most_parts;
-    QTZ_CUDA(h, cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    kernel<<<(a.units + a.share - 1) / a.share, kThreads, smem, st>>>(a);
-    QTZ_LAUNCH_CHECK(h, "linear kernel");
+    const qtz_status s = qtz_allow_smem(h, kernel);
+    if (s != QTZ_OK) return s;
+    QTZ_CUDA(h, qtz_launch_dependent(kernel, dim3((a.units + a.share - 1) / a.share), kThreads, smem, st, a));
     return QTZ_OK;
 }
 
@@ -842,6 +852,7 @@ extern "C" qtz_status qtz_linear_create(qtz_handle h, const qtz_linear_desc* des
         pack_kernel<<<dim3(static_cast<unsigned>(k_blocks), static_cast<unsigned>(row_tiles)), 256, 0, st>>>(a);
         e = cudaGetLastError();
     }
+    if (e == cudaSuccess) e = cudaStreamSynchronize(st);   // later calls may fetch the blocks before they wait for the stream
     if (e != cudaSuccess) {
         qtz_cuda_fail(h, e, "qtz_linear_create");
         qtz_linear_destroy(p);
