@@ -6,15 +6,15 @@
 //                  of their largest value, d in [-128, 127]: 22 bits below it, more than the 11 or 8 that a value has; one operand
 //                  column for each digit.  Integer sums are exact; scale, digit weight and zero point (through the sum of x over the
 //                  group) multiply them in fp32.
-//   more rows      fp16 / bf16 matrix instructions (m16n8k16) with q - z as an exact operand: two codes are cut from a word by one
-//                  logic operation that also writes the exponent (1024 + q in fp16, 128 + q in bf16), one packed operation takes the
-//                  offset off; the scale multiplies the fp32 sum of its group, or of the 64 columns of it that are at hand.
+//   more rows      fp16 / bf16 tensor cores (tcgen05) with q - z as an exact operand: two codes are cut from a word by one logic
+//                  operation that also writes the exponent (1024 + q in fp16, 128 + q in bf16), one packed operation takes the
+//                  offset off, and the operand goes to tensor memory without touching shared memory; the scale multiplies the fp32
+//                  sum of its group, or of the 128 columns of it that are at hand.
 // Nothing is rounded to 16 bits before y.
 //
 // What bounds it: half a byte of weight is read for 2 flops an activation row.  At the measured copy rate that is 46 weights a clock
-// and SM, for which the SM issues 2.8 operations a weight: the second form needs about 2.3, the first 0.8 for one row and 1.9 for
-// eight, where its matrix instructions (2048 products a clock) still take 85 weights a clock.  With 32 rows the second form's
-// matrix instructions (1024 products a clock) take 32 weights a clock: they bound it.
+// and SM, for which the SM issues 2.8 operations a weight: the first form needs about 1.3 for one row and 1.9 for eight (its matrix
+// instructions, 2048 products a clock, then still take 85 weights a clock), the second 2 with 32 rows.
 // The weights are read once, in the order of use, as contiguous blocks of 32 rows x 256 columns with their scales and zero points
 // behind the codes; every warp streams its blocks through a ring of its own (bulk copies, several blocks ahead).  Activations are
 // few: the eight warps of a CTA work on the same columns of 256 rows and share them in shared memory.
@@ -25,6 +25,7 @@
 
 #include "qtz_half_util.cuh"
 #include "qtz_internal.cuh"
+#include "qtz_plan.cuh"
 #include "qtz_ptx.cuh"
 
 struct qtz_linear {
@@ -46,7 +47,7 @@ constexpr int kThreads = kWarps * 32;
 constexpr int kRowTile = 32, kKBlock = 256;
 constexpr int kCodeBytes = kRowTile * kKBlock / 2;
 constexpr int kMaxStages = 8;
-constexpr int kMaxTokens = 32;             // activation rows of one pass over the weights
+constexpr int kMaxTokens = 64;             // activation rows of one pass over the weights
 constexpr int kSmemLimit = 227 * 1024;
 
 // ------------------------------------------------------------------------------------
@@ -62,8 +63,8 @@ struct PackArgs {
 };
 
 // One thread per 32-bit word of codes: word (chunk of 64 columns, half of the 32 rows, lane, w) holds eight columns of one row, in
-// the order in which the lanes of a matrix instruction hold their operand: columns 0 .. 3 in the low nibbles of the four bytes,
-// 4 .. 7 in the high ones.
+// the order in which the lanes of a matrix instruction hold their operand: the low nibbles of the four bytes are columns 4 t + 0, 2, 1, 3
+// of the 32 at hand (t: the lane's place in its quad), the high ones 16 + 4 t + 0, 2, 1, 3.
 __global__ void __launch_bounds__(256)
 pack_kernel(PackArgs a)
 {
@@ -71,18 +72,19 @@ pack_kernel(PackArgs a)
     const int row0 = blockIdx.y * kRowTile, k0 = blockIdx.x * kKBlock;
     for (int i = threadIdx.x; i < kCodeBytes / 4; i += 256) {
         const int w = i & 3, lane = (i >> 2) & 31, half = (i >> 7) & 1, chunk = i >> 8;
-        const int row = row0 + half * 16 + (lane >> 2) + 8 * (w & 1), k = k0 + chunk * 64 + (w >> 1) * 32 + 8 * (lane & 3);
+        const int row = row0 + half * 16 + (lane >> 2) + 8 * (w & 1), k = k0 + chunk * 64 + (w >> 1) * 32 + 4 * (lane & 3);
         uint32_t v = 0;
-        for (int j = 0; j < 8; ++j) {
+        for (int nibble = 0; nibble < 8; ++nibble) {
+            const int m = nibble >> 1, c = k + 16 * (nibble & 1) + (m == 1 ? 2 : m == 2 ? 1 : m);
             uint32_t q = a.is_signed ? 8 : 0;          // beyond the matrix: the code of zero
-            if (row < a.n && k + j < a.k) {
-                const uint8_t byte = a.codes[static_cast<int64_t>(row) * ((a.k + 1) / 2) + ((k + j) >> 1)];
-                q = ((k + j) & 1 ? byte >> 4 : byte & 15) ^ (a.is_signed ? 8 : 0);
+            if (row < a.n && c < a.k) {
+                const uint8_t byte = a.codes[static_cast<int64_t>(row) * ((a.k + 1) / 2) + (c >> 1)];
+                q = (c & 1 ? byte >> 4 : byte & 15) ^ (a.is_signed ? 8 : 0);
             } else if (row < a.n && a.zeros) {
-                const int g = min((k + j) / a.group, a.groups - 1);
+                const int g = min(c / a.group, a.groups - 1);
                 q = min(static_cast<int>(a.zeros[static_cast<int64_t>(row) * a.groups + g]), 15);
             }
-            v |= q << (8 * (j & 3) + 4 * (j >> 2));
+            v |= q << (4 * nibble);
         }
         reinterpret_cast<uint32_t*>(block)[i] = v;
     }
@@ -114,32 +116,6 @@ struct LinearArgs {
     int32_t* status;
 };
 
-template <typename T>
-__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
-{
-    if constexpr (std::is_same<T, __half>::value)
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    else
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
-template <typename T>
-__device__ __forceinline__ void mma_from_zero(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
-{
-    if constexpr (std::is_same<T, __half>::value)
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
-            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
-    else
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
-            : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
-}
-
 // (a & mask) | exponent in one operation
 __device__ __forceinline__ uint32_t cut(uint32_t a, uint32_t mask, uint32_t exponent)
 {
@@ -148,10 +124,15 @@ __device__ __forceinline__ uint32_t cut(uint32_t a, uint32_t mask, uint32_t expo
     return r;
 }
 
+template <typename T> __device__ __forceinline__ T bits16_as(uint32_t v)
+{
+    const uint16_t u = static_cast<uint16_t>(v);
+    return *reinterpret_cast<const T*>(&u);
+}
 template <typename H2> __device__ __forceinline__ H2 as(uint32_t v) { return *reinterpret_cast<const H2*>(&v); }
 template <typename H2> __device__ __forceinline__ uint32_t bits(H2 v) { return *reinterpret_cast<const uint32_t*>(&v); }
 
-// The pairs of columns (0 2), (4 6), (1 3), (5 7) of a word as q - z; `zero`: z (0..15) in both halves.  fp16: 1024 + q - (1024 + z),
+// The pairs of columns (0 1), (16 17), (2 3), (18 19), from 4 t on, of a word as q - z; `zero`: z (0..15) in both halves.  fp16: 1024 + q - (1024 + z),
 // and (1024 + 16 q) / 16 - (64 + z) for the pairs in odd nibbles.  bf16 has no room for the latter: 128 + q - (128 + z) after a shift.
 template <typename T>
 __device__ __forceinline__ void unpack_codes(uint32_t w, uint32_t zero, uint32_t (&out)[4])
@@ -295,62 +276,34 @@ __device__ __forceinline__ void timed_out(const LinearArgs& a)
     if ((threadIdx.x & 31) == 0 && atomicCAS(a.status, 0, QTZ_ERR_DEVICE_TIMEOUT) == 0) a.status[1] = QTZ_SITE_LINEAR;
 }
 
-// Rows of y of the warp's tile; `rows` of them at most (an activation block may be narrower than eight).
-template <typename T, int kNt>
-__device__ __forceinline__ void write_rows(const LinearArgs& a, const Stream& s, const Place& at, const float (&v)[2][kNt][4], int rows)
-{
-    const int t4 = s.lane & 3, o0 = s.tile(at) * kRowTile + (s.lane >> 2);
-    const int64_t r0 = static_cast<int64_t>(at.pass) * (8 * kNt) + 2 * t4;
-    if (2 * t4 >= rows) return;
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int hi = 0; hi < 2; ++hi) {
-            const int o = o0 + 16 * j + 8 * hi;
-            if (o >= a.n) continue;
-            const float b = a.bias ? qtz_dev::to_f32(static_cast<const T*>(a.bias)[o]) : 0.f;
-#pragma unroll
-            for (int nt = 0; nt < kNt; ++nt)
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const int64_t r = r0 + 8 * nt + c;
-                    if (r < a.rows) static_cast<T*>(a.y)[r * a.y_stride + o] = qtz_dev::from_f32<T>(v[j][nt][2 * hi + c] + b);
-                }
-        }
-}
-
 // Where the parts of a warp lie: slot 0, rows that began in an earlier CTA; slot 1, rows that go on in a later one.
-template <int kNt>
+template <int kValues>
 __device__ __forceinline__ float* part_of(const LinearArgs& a, const Stream& s, int cta, int slot)
 {
-    return a.parts + ((static_cast<int64_t>(cta) * 2 + slot) * kWarps + s.warp) * (kRowTile * 8 * kNt) + s.lane;
+    return a.parts + ((static_cast<int64_t>(cta) * 2 + slot) * kWarps + s.warp) * (32 * kValues) + s.lane;
 }
 
-// The end of a row block, or of this CTA's columns of it: y, or a part.
-template <typename T, int kNt>
-__device__ __forceinline__ void finish_rows(const LinearArgs& a, const Stream& s, const float (&v)[2][kNt][4], int rows, int (&open)[2])
+// The end of a row block, or of this CTA's columns of it: y, or a part.  A lane's values v go to y by `write(place, v)`.
+template <int kValues, typename W>
+__device__ __forceinline__ void finish_rows(const LinearArgs& a, const Stream& s, const float (&v)[kValues], int (&open)[2], const W& write)
 {
     const bool begins = s.unit - s.here.kb >= s.u0;
     if (begins && s.ends()) {
-        if (s.has_rows()) write_rows<T, kNt>(a, s, s.here, v, rows);
+        if (s.has_rows()) write(s.here, v);
         return;
     }
     if (begins) open[1] = s.unit;
     else open[0] = s.unit;
-    float* part = part_of<kNt>(a, s, blockIdx.x, begins ? 1 : 0);
+    float* part = part_of<kValues>(a, s, blockIdx.x, begins ? 1 : 0);
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int nt = 0; nt < kNt; ++nt)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) part[((j * kNt + nt) * 4 + c) * 32] = v[j][nt][c];
+    for (int i = 0; i < kValues; ++i) part[i * 32] = v[i];
 }
 
-// Rows whose columns lie in several CTAs, c0 .. c1: the last to arrive joins their parts in order.
-template <typename T, int kNt>
-__device__ __forceinline__ void join_rows(const LinearArgs& a, const Stream& s, const int (&open)[2], int rows, const int& failed, int (&last)[2])
+// Rows whose columns lie in several CTAs, c0 .. c1: the last to arrive joins their parts in order.  Called by all threads; the first
+// kWarps warps hold the parts.
+template <int kValues, typename W>
+__device__ __forceinline__ void join_rows(const LinearArgs& a, const Stream& s, const int (&open)[2], const int& failed, int (&last)[2], const W& write)
 {
-    if (open[0] < 0 && open[1] < 0) return;            // the same for all warps
     __threadfence();
     __syncthreads();
     if (failed) return;                                // the results are void, and the counters have to be cleared
@@ -364,26 +317,27 @@ __device__ __forceinline__ void join_rows(const LinearArgs& a, const Stream& s, 
             if (last[which]) a.counters[c0[which]] = 0;    // ready for the next call
         }
     __syncthreads();
+    if (s.warp >= kWarps) return;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         if (open[which] < 0 || !last[which] || s.tile(at[which]) >= a.row_tiles) continue;
         __threadfence();
-        constexpr int kFlight = kNt == 1 ? 8 : kNt == 2 ? 4 : 2;       // parts in flight: what the registers hold
-        float v[2][kNt][4] = {};
+        constexpr int kFlight = kValues <= 8 ? 8 : kValues <= 16 ? 4 : 2;     // parts in flight: what the registers hold
+        float v[kValues] = {};
         for (int c = c0[which]; c <= c1[which]; c += kFlight) {
-            float p[kFlight][2][kNt][4];
+            float p[kFlight][kValues];
 #pragma unroll
             for (int x = 0; x < kFlight; ++x) {
-                const float* part = part_of<kNt>(a, s, min(c + x, c1[which]), c + x == c0[which] ? 1 : 0);
+                const float* part = part_of<kValues>(a, s, min(c + x, c1[which]), c + x == c0[which] ? 1 : 0);
 #pragma unroll
-                for (int i = 0; i < 8 * kNt; ++i) (&p[x][0][0][0])[i] = __ldcg(part + i * 32);
+                for (int i = 0; i < kValues; ++i) p[x][i] = __ldcg(part + i * 32);
             }
 #pragma unroll
             for (int x = 0; x < kFlight; ++x)
 #pragma unroll
-                for (int i = 0; i < 8 * kNt; ++i) (&v[0][0][0])[i] += c + x <= c1[which] ? (&p[x][0][0][0])[i] : 0.f;
+                for (int i = 0; i < kValues; ++i) v[i] += c + x <= c1[which] ? p[x][i] : 0.f;
         }
-        write_rows<T, kNt>(a, s, at[which], v, rows);
+        write(at[which], v);
     }
 }
 
@@ -473,14 +427,19 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
                 const int q = odd ? 0 : __float2int_rn(v[k] * mult);
                 const int d0 = (q << 24) >> 24, q1 = (q - d0) >> 8, d1 = (q1 << 24) >> 24, d2 = (q1 - d1) >> 8;
                 sum += q;
-                d[0] |= static_cast<uint64_t>(d0 & 0xff) << (8 * k);
-                d[1] |= static_cast<uint64_t>(d1 & 0xff) << (8 * k);
-                d[2] |= static_cast<uint64_t>(d2 & 0xff) << (8 * k);
+                const int at = 8 * ((k & 4) | (k & 1) << 1 | (k & 2) >> 1);   // columns 0, 2, 1, 3 of four
+                d[0] |= static_cast<uint64_t>(d0 & 0xff) << at;
+                d[1] |= static_cast<uint64_t>(d1 & 0xff) << at;
+                d[2] |= static_cast<uint64_t>(d2 & 0xff) << at;
             }
             if (round > 0)                             // the buffer's unit before has been used by all warps
                 ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_free[buffer]), (round - 1) & 1, a.wait_budget)) && ok;
 #pragma unroll
-            for (int j = 0; j < 3; ++j) *reinterpret_cast<uint64_t*>(&to.operand[digit_column<kTiles>(j, r)][8 * lane]) = d[j];
+            for (int j = 0; j < 3; ++j) {              // columns 4 t .. and 16 + 4 t .. of 32 lie side by side
+                uint8_t* const row = &to.operand[digit_column<kTiles>(j, r)][(lane >> 2) * 32 + (lane & 1) * 16 + (lane & 2) * 2];
+                *reinterpret_cast<uint32_t*>(row) = static_cast<uint32_t>(d[j]);
+                *reinterpret_cast<uint32_t*>(row + 8) = static_cast<uint32_t>(d[j] >> 32);
+            }
             // the sum of a scale's columns: |sum| < 2^22 * 128 fits
             constexpr int kLanes = 4 * kSteps;
 #pragma unroll
@@ -496,6 +455,19 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
         }
     };
 
+    // v[4 j + c]: output row g + 8 (c >> 1) of half j, activation row 2 t4 + (c & 1)
+    auto write = [&](const Place& at, const float (&v)[8]) {
+        if (2 * t4 >= kRows) return;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int o = s.tile(at) * kRowTile + g + 8 * i;
+            if (o >= a.n) continue;
+            const float b = a.bias ? qtz_dev::to_f32(static_cast<const T*>(a.bias)[o]) : 0.f;
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+                if (2 * t4 + c < rows) static_cast<T*>(a.y)[(2 * t4 + c) * a.y_stride + o] = qtz_dev::from_f32<T>(v[2 * i + c] + b);
+        }
+    };
     float acc[2][kTiles][4] = {};
     int open[2] = {-1, -1};                            // units whose rows are shared with an earlier / a later CTA
     if (s.u0 < s.u1) convert(0, s.here.kb, 0, 0);
@@ -577,7 +549,7 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
             ++round_next;
         }
         if (s.finishes()) {
-            float v[2][1][4];                          // the digits of a row together
+            float v[8];                                // the digits of a row together
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -587,168 +559,229 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
                     if (kTiles > 2) t += acc[j][2 % kTiles][c];
                     if (kTiles == 1) t += __shfl_xor_sync(0xffffffffu, t, 1);
                     if (kTiles < 3) t += __shfl_xor_sync(0xffffffffu, t, 2);
-                    v[j][0][c] = t;
+                    v[4 * j + c] = t;
 #pragma unroll
                     for (int nt = 0; nt < kTiles; ++nt) acc[j][nt][c] = 0.f;
                 }
-            finish_rows<T, 1>(a, s, v, kRows, open);
+            finish_rows(a, s, v, open, write);
         }
     }
     if (!ok) {
         timed_out(a);
         s_failed = 1;
     }
-    join_rows<T, 1>(a, s, open, kRows, s_failed, s_last);
+    join_rows<8>(a, s, open, s_failed, s_last, write);
 }
 
-// ---- more rows: 16-bit matrix instructions; kNt: blocks of eight rows; kSteps: steps of 32 columns to a scale (1, 2 or 4) ----
-constexpr int kRowPitch = 2 * kKBlock + 64;            // bytes of a row of x in shared memory: the lanes of a load meet all banks
+// ---- more rows: 16-bit tensor cores (tcgen05) ----
+// Eight warps turn a warp's 32 rows of codes into 16-bit operands, straight into tensor memory: two tiles of 128 rows.  One warp
+// issues the products with kN rows of x, which a last warp brings by TMA.  While the products of one scale's columns run, the eight
+// warps unpack the next; then each thread, which owns a row of W, adds scale * product to its kN sums.  kSteps: steps of 32 columns to
+// a scale (1, 2 or 4).
+constexpr int kWideThreads = kThreads + 64;
 
-template <typename T, int kNt, int kSteps, bool kZero>
-__global__ void __launch_bounds__(kThreads, 2)
-linear_wide_kernel(const __grid_constant__ LinearArgs a)
+template <typename T, int kN, int kSteps, bool kZero>
+__global__ void __launch_bounds__(kWideThreads, 1)
+linear_wide_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap x_map)
 {
-    extern __shared__ __align__(128) uint8_t smem[];   // two units of x, the rings
-    __shared__ __align__(8) uint64_t s_full[kWarps][kMaxStages];
+    constexpr int kXBox = kN * 128;                    // 64 columns of x
+    constexpr int kXUnit = kKBlock / 64 * kXBox;
+    constexpr int kScales = 8 / kSteps;                // of a unit
+    constexpr uint32_t kFormat = std::is_same<T, __half>::value ? 0 : 1;
+    constexpr uint32_t kProduct = (1u << 4) | (kFormat << 7) | (kFormat << 10) | (static_cast<uint32_t>(kN >> 3) << 17) | (128u >> 4 << 24);
+    extern __shared__ uint8_t smem_raw[];              // two units of x, the rings
+    __shared__ __align__(8) uint64_t s_full[kWarps][kMaxStages], s_xfull[2], s_xfree[2], s_operand[2][2], s_product[2][2], s_drain;
     __shared__ int s_last[2], s_failed;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3;
-    if (lane < kMaxStages) mbar_init(smem_u32(&s_full[warp][lane]), 1);
-    if (tid == 0) s_failed = 0;
-    fence_barrier_init();
-    __syncthreads();
-    Stream s(a, smem_u32(smem) + 2 * 8 * kNt * kRowPitch + warp * a.stages * a.block_bytes, s_full[warp]);
-
-    grid_launch_dependents();
-    s.start();                                         // the weights were there when the layer was made; all else is waited for
-    grid_dependency_wait();
-
-    // x of a unit: thread i takes eight columns (i % 32) of rows i / 32, + 8, ..; in the order of the operand (0 2, 4 6, 1 3, 5 7)
-    uint4 held[kNt];
-    auto fetch = [&](const Place& at) {
-        const int have = a.k - at.kb * kKBlock - 8 * lane;
-        const int64_t r0 = static_cast<int64_t>(at.pass) * (8 * kNt) + warp;
-#pragma unroll
-        for (int nt = 0; nt < kNt; ++nt) {
-            held[nt] = make_uint4(0, 0, 0, 0);
-            if (r0 + 8 * nt < a.rows && have > 0)
-                held[nt] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.x) + (r0 + 8 * nt) * a.x_stride + at.kb * kKBlock + 8 * lane));
+    __shared__ uint32_t s_tmem;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    if (warp < kWarps && lane < kMaxStages) mbar_init(smem_u32(&s_full[warp][lane]), 1);
+    if (tid == 0) {
+        s_failed = 0;
+        prefetch_tensormap(&x_map);
+        mbar_init(smem_u32(&s_drain), 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&s_xfull[i]), 1);
+            mbar_init(smem_u32(&s_xfree[i]), 1);
+            for (int j = 0; j < 2; ++j) {
+                mbar_init(smem_u32(&s_operand[i][j]), 4);
+                mbar_init(smem_u32(&s_product[i][j]), 1);
+            }
         }
-    };
-    auto store = [&](const Place& at, int buffer) {
-        const int have = a.k - at.kb * kKBlock - 8 * lane;
-#pragma unroll
-        for (int nt = 0; nt < kNt; ++nt) {
-            uint32_t w[4] = {held[nt].x, held[nt].y, held[nt].z, held[nt].w};
-            if (have > 0 && have < 8)                  // the last columns: what lies behind them is not data
-#pragma unroll
-                for (int c = 0; c < 4; ++c) w[c] = have >= 2 * c + 2 ? w[c] : have == 2 * c + 1 ? w[c] & 0xffffu : 0u;
-            *reinterpret_cast<uint4*>(smem + buffer * (8 * kNt * kRowPitch) + (8 * nt + warp) * kRowPitch + lane * 16) =
-                make_uint4(__byte_perm(w[0], w[1], 0x5410), __byte_perm(w[2], w[3], 0x5410), __byte_perm(w[0], w[1], 0x7632), __byte_perm(w[2], w[3], 0x7632));
-        }
-    };
-
-    float acc[2][kNt][4] = {};
-    int open[2] = {-1, -1};
-    bool ok = true;
-    if (s.u0 < s.u1) {
-        fetch(s.here);
-        store(s.here, 0);
-        __syncthreads();
     }
-    int buffer = 0;
-    for (; s.unit < s.u1; s.next(), buffer ^= 1) {
-        Place after = s.here;
-        after.next(a);
-        if (s.unit + 1 < s.u1) fetch(after);
-        ok = s.wait() && ok;
-        if (ok && s.has_rows()) {
-            const uint32_t block = s.block(), scales = block + kCodeBytes, zeros = scales + 8 / kSteps * kRowTile * 2;
-            const uint32_t x = smem_u32(smem) + buffer * (8 * kNt * kRowPitch) + g * kRowPitch + t4 * 16;
-            float part[2][kNt][4];
-#pragma unroll 1
-            for (int pair = 0; pair < 2; ++pair) {     // 128 columns
-                float sc[2][2];
-                uint32_t z[2] = {0x0808u, 0x0808u};
-                uint4 q[2];
+    if (warp == kWarps + 1) {
+        tmem_alloc(smem_u32(&s_tmem), 512);
+        tmem_relinquish();
+    }
+    fence_barrier_init();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = s_tmem;
+    // columns: operand [tile][buffer], then product [tile][buffer]
+    auto operand_at = [&](int tile, int buffer) { return tmem + (tile * 2 + buffer) * 64; };
+    auto product_at = [&](int tile, int buffer) { return tmem + 256 + (tile * 2 + buffer) * 64; };
+    Stream s(a, base + 2 * kXUnit + (warp < kWarps ? warp : 0) * a.stages * a.block_bytes, s_full[warp < kWarps ? warp : 0]);
+    grid_launch_dependents();
+    if (warp < kWarps) s.start();                      // the weights were there when the layer was made; all else is waited for
+    grid_dependency_wait();
+    int open[2] = {-1, -1};                            // units whose rows are shared with an earlier / a later CTA
+    bool ok = true;
+    // acc[r]: output row `lane` of the tile, activation row r
+    auto write = [&](const Place& at, const float (&v)[kN]) {
+        const int o = s.tile(at) * kRowTile + lane;
+        if (o >= a.n) return;
+        const float b = a.bias ? qtz_dev::to_f32(static_cast<const T*>(a.bias)[o]) : 0.f;
+        const int64_t r0 = static_cast<int64_t>(at.pass) * kN;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {          // 32 columns
-                    const int step = 4 * pair + i;
-                    if (i % kSteps == 0)
+        for (int r = 0; r < kN; ++r)
+            if (r0 + r < a.rows) static_cast<T*>(a.y)[(r0 + r) * a.y_stride + o] = qtz_dev::from_f32<T>(v[r] + b);
+    };
+
+    if (warp == kWarps) {
+        // ======== x: one unit's columns at a time ========
+        int i = 0;
+        for (; s.unit < s.u1; s.next(), ++i) {
+            const int buffer = i & 1;
+            if (i >= 2 && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&s_xfree[buffer]), ((i >> 1) - 1) & 1, a.wait_budget))) {
+                ok = false;
+                break;
+            }
+            if (elect_one()) {
+                const uint32_t bar = smem_u32(&s_xfull[buffer]);
+                mbar_arrive_expect_tx(bar, kXUnit);
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const int at = (step / kSteps * 2 + j) * 8 + g;
-                            const float2 f = qtz_dev::unpack2(lds32(scales + 4 * at), T());
-                            sc[j][0] = f.x;
-                            sc[j][1] = f.y;
-                            if (kZero) z[j] = lds16(zeros + 2 * at);
+                for (int c = 0; c < kKBlock / 64; ++c)
+                    tma_load_2d(base + buffer * kXUnit + c * kXBox, &x_map, bar, (s.here.kb * kKBlock + c * 64) * 2, s.here.pass * kN);
+            }
+            __syncwarp();
+        }
+        for (int j = max(0, i - 2); j < i; ++j)        // nothing may be in flight when the CTA ends
+            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_xfull[j & 1]), (j >> 1) & 1, a.wait_budget)) && ok;
+    } else if (warp == kWarps + 1) {
+        // ======== products ========
+        int step = 0;
+        for (int i = 0; s.unit < s.u1 && ok; s.next(), ++i) {
+            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_xfull[i & 1]), (i >> 1) & 1, a.wait_budget));
+            for (int q = 0; q < kScales && ok; ++q, ++step) {
+                for (int tile = 0; tile < 2 && ok; ++tile) {
+                    ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_operand[tile][step & 1]), (step >> 1) & 1, a.wait_budget));
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+#pragma unroll
+                        for (int k = 0; k < 2 * kSteps; ++k) {         // 16 columns
+                            const int column = q * kSteps * 32 + k * 16;
+                            mma_f16_from_tmem(product_at(tile, step & 1), operand_at(tile, step & 1) + 8 * k,
+                                              make_kmajor_desc(base + (i & 1) * kXUnit + column / 64 * kXBox, 128) + 2 * (column / 16 % 4), kProduct, k > 0);
                         }
-                    uint32_t w[2][2][4];               // [half of the rows][row g, g + 8][pair]
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        if (i % 2 == 0) q[j] = lds128(block + (step / 2 * 2 + j) * 512 + lane * 16);
-                        unpack_codes<T>(i % 2 ? q[j].z : q[j].x, (z[j] & 0xffu) * 0x00010001u, w[j][0]);
-                        unpack_codes<T>(i % 2 ? q[j].w : q[j].y, (z[j] >> 8) * 0x00010001u, w[j][1]);
+                        mma_commit(smem_u32(&s_product[tile][step & 1]));
+                        if (q == kScales - 1 && tile == 1) mma_commit(smem_u32(&s_xfree[i & 1]));
                     }
-                    uint4 b[kNt];
-#pragma unroll
-                    for (int nt = 0; nt < kNt; ++nt) b[nt] = lds128(x + nt * 8 * kRowPitch + step * 64);
-                    // neighbouring instructions write different sums
-#pragma unroll
-                    for (int nt = 0; nt < kNt; ++nt)
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const uint32_t op[4] = {w[j][0][0], w[j][1][0], w[j][0][1], w[j][1][1]};
-                            if (i % kSteps == 0) mma_from_zero<T>(part[j][nt], op, b[nt].x, b[nt].y);
-                            else mma<T>(part[j][nt], op, b[nt].x, b[nt].y);
-                        }
-#pragma unroll
-                    for (int nt = 0; nt < kNt; ++nt)
-#pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const uint32_t op[4] = {w[j][0][2], w[j][1][2], w[j][0][3], w[j][1][3]};
-                            mma<T>(part[j][nt], op, b[nt].z, b[nt].w);
-                        }
-                    if ((i + 1) % kSteps == 0)
-#pragma unroll
-                        for (int nt = 0; nt < kNt; ++nt)
-#pragma unroll
-                            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                                for (int c = 0; c < 4; ++c) acc[j][nt][c] = fmaf(part[j][nt][c], sc[j][c >> 1], acc[j][nt][c]);
+                    __syncwarp();
                 }
             }
         }
-        s.release(ok);
-        if (s.unit + 1 < s.u1) store(after, buffer ^ 1);
-        __syncthreads();                               // the next unit's x is there, this one's is free
-        if (s.finishes()) {
-            finish_rows<T, kNt>(a, s, acc, 8, open);
+        if (!ok) {                                     // what was issued may still run: give it the same limit, then go
+            if (elect_one()) mma_commit(smem_u32(&s_drain));
+            __syncwarp();
+            mbar_wait(smem_u32(&s_drain), 0, a.wait_budget);
+        }
+    } else {
+        // ======== operands, then sums ========
+        const int tile = warp >> 2;
+        const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;
+        float acc[kN];
 #pragma unroll
-            for (int i = 0; i < 8 * kNt; ++i) (&acc[0][0][0])[i] = 0.f;
+        for (int r = 0; r < kN; ++r) acc[r] = 0.f;
+        float scale = 0.f;
+        bool pending = false;                          // the product of the step before is still to be taken
+        // sums of step i (its scale in `scale`)
+        auto take = [&](int i) {
+            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_product[tile][i & 1]), (i >> 1) & 1, a.wait_budget)) && ok;
+            tc_fence_after();
+#pragma unroll
+            for (int r0 = 0; r0 < kN; r0 += 16) {
+                uint32_t v[16];
+                tmem_ld_32x16(product_at(tile, i & 1) + lanes + r0, v);
+                tmem_ld_wait();
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[r0 + r] = fmaf(__uint_as_float(v[r]), scale, acc[r0 + r]);
+            }
+        };
+        int step = 0;
+        for (; s.unit < s.u1; s.next()) {
+            ok = s.wait() && ok;
+            const uint32_t block = s.block(), scales = block + kCodeBytes, zeros = scales + kScales * kRowTile * 2;
+            const bool work = ok && s.has_rows();
+#pragma unroll 1
+            for (int q = 0; q < kScales; ++q, ++step) {
+                float scale_next = 0.f;
+                if (work) {
+                    scale_next = qtz_dev::to_f32(bits16_as<T>(lds16(scales + 2 * (q * 32 + (lane >> 4) * 16 + (lane & 7) * 2 + ((lane >> 3) & 1)))));
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        uint32_t z = 0x0808u;
+                        if (kZero) z = lds16(zeros + 2 * ((q * 2 + j) * 8 + (lane >> 2)));
+                        const uint32_t z0 = (z & 0xffu) * 0x00010001u, z1 = (z >> 8) * 0x00010001u;
+                        const uint32_t to = operand_at(tile, step & 1) + lanes + (static_cast<uint32_t>(16 * j) << 16);
+#pragma unroll
+                        for (int h = 0; h < kSteps; ++h) {     // 32 columns: 16 of tensor memory
+                            const int half = q * kSteps + h;
+                            const uint2 w = lds64(block + ((half >> 1) * 2 + j) * 512 + lane * 16 + (half & 1) * 8);
+                            uint32_t lo[4], hi[4];             // rows g, g + 8
+                            unpack_codes<T>(w.x, z0, lo);
+                            unpack_codes<T>(w.y, z1, hi);
+                            tmem_st_16x256_x2(to + 16 * h, lo[0], lo[2], hi[0], hi[2], lo[1], lo[3], hi[1], hi[3]);
+                        }
+                    }
+                    tmem_st_wait();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&s_operand[tile][step & 1]));
+                if (pending) take(step - 1);
+                pending = true;
+                scale = scale_next;
+            }
+            s.release(ok);
+            if (s.finishes()) {
+                take(step - 1);
+                pending = false;
+                finish_rows(a, s, acc, open, write);
+#pragma unroll
+                for (int r = 0; r < kN; ++r) acc[r] = 0.f;
+            }
         }
     }
     if (!ok) {
         timed_out(a);
         s_failed = 1;
     }
-    join_rows<T, kNt>(a, s, open, 8, s_failed, s_last);
+    tc_fence_before();
+    __syncthreads();
+    if (warp == kWarps + 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+    join_rows<kN>(a, s, open, s_failed, s_last, write);
 }
 
-// fixed: shared memory beside the rings; kParts: the most parts that a row block is cut into
-template <typename K>
-qtz_status launch(qtz_linear* p, LinearArgs& a, K kernel, int fixed, int most_parts, cudaStream_t st)
+// ctas: of an SM; fixed: shared memory beside the rings; most_parts: that a row block is cut into
+template <typename K, typename... X>
+qtz_status launch(qtz_linear* p, LinearArgs& a, K kernel, int threads, int ctas, int fixed, int most_parts, cudaStream_t st, const X&... more)
 {
     qtz_ctx* h = p->h;
-    const int room = (kSmemLimit + 1024) / 2 - 1024 - 1024 - fixed;    // two CTAs an SM; 1 KB: the kernels' static shared memory
+    const int room = (kSmemLimit + 1024) / ctas - 1024 - 1024 - fixed;    // 1 KB: the kernels' static shared memory
     a.stages = room / (kWarps * p->block_bytes);
     if (a.stages > kMaxStages) a.stages = kMaxStages;
-    const int smem = fixed + kWarps * a.stages * p->block_bytes, grid = 2 * h->num_sms;
+    const int smem = fixed + kWarps * a.stages * p->block_bytes, grid = ctas * h->num_sms;
     // A share takes in at least 1 / most_parts of the columns: joining costs more than it brings beyond that.
     a.share = (a.units + grid - 1) / grid;
     if (a.share < (a.k_blocks + most_parts - 1) / most_parts) a.share = (a.k_blocks + most_parts - 1) / most_parts;
     const qtz_status s = qtz_allow_smem(h, kernel);
     if (s != QTZ_OK) return s;
-    QTZ_CUDA(h, qtz_launch_dependent(kernel, dim3((a.units + a.share - 1) / a.share), kThreads, smem, st, a));
+    QTZ_CUDA(h, qtz_launch_dependent(kernel, dim3((a.units + a.share - 1) / a.share), threads, smem, st, a, more...));
     return QTZ_OK;
 }
 
@@ -756,22 +789,24 @@ template <typename T, int kTiles>
 qtz_status launch_digits(qtz_linear* p, LinearArgs& a, bool zero, cudaStream_t st)
 {
     constexpr int kFixed = kDigitBuffers * sizeof(Digits<kTiles>);
-    if (p->scales == 8)
-        return zero ? launch(p, a, linear_digits_kernel<T, kTiles, 1, true>, kFixed, 32, st) : launch(p, a, linear_digits_kernel<T, kTiles, 1, false>, kFixed, 32, st);
-    if (p->scales == 4)
-        return zero ? launch(p, a, linear_digits_kernel<T, kTiles, 2, true>, kFixed, 32, st) : launch(p, a, linear_digits_kernel<T, kTiles, 2, false>, kFixed, 32, st);
-    return zero ? launch(p, a, linear_digits_kernel<T, kTiles, 4, true>, kFixed, 32, st) : launch(p, a, linear_digits_kernel<T, kTiles, 4, false>, kFixed, 32, st);
+    auto go = [&](auto kernel) { return launch(p, a, kernel, kThreads, 2, kFixed, 32, st); };
+    if (p->scales == 8) return zero ? go(linear_digits_kernel<T, kTiles, 1, true>) : go(linear_digits_kernel<T, kTiles, 1, false>);
+    if (p->scales == 4) return zero ? go(linear_digits_kernel<T, kTiles, 2, true>) : go(linear_digits_kernel<T, kTiles, 2, false>);
+    return zero ? go(linear_digits_kernel<T, kTiles, 4, true>) : go(linear_digits_kernel<T, kTiles, 4, false>);
 }
 
-template <typename T, int kNt>
+template <typename T, int kN>
 qtz_status launch_wide(qtz_linear* p, LinearArgs& a, bool zero, cudaStream_t st)
 {
-    constexpr int kFixed = 2 * 8 * kNt * kRowPitch;
-    if (p->scales == 8)
-        return zero ? launch(p, a, linear_wide_kernel<T, kNt, 1, true>, kFixed, 8, st) : launch(p, a, linear_wide_kernel<T, kNt, 1, false>, kFixed, 8, st);
-    if (p->scales == 4)
-        return zero ? launch(p, a, linear_wide_kernel<T, kNt, 2, true>, kFixed, 8, st) : launch(p, a, linear_wide_kernel<T, kNt, 2, false>, kFixed, 8, st);
-    return zero ? launch(p, a, linear_wide_kernel<T, kNt, 4, true>, kFixed, 8, st) : launch(p, a, linear_wide_kernel<T, kNt, 4, false>, kFixed, 8, st);
+    constexpr int kFixed = 1024 + 2 * kKBlock / 64 * kN * 128;
+    CUtensorMap x_map;                                 // bytes: columns beyond k and rows beyond the last read as zero
+    const uint64_t dims[2] = {2 * static_cast<uint64_t>(a.k), static_cast<uint64_t>(a.rows)}, strides[1] = {2 * static_cast<uint64_t>(a.x_stride)};
+    const uint32_t box[2] = {128, kN};
+    if (!qtz_encode_u8_map(&x_map, a.x, 2, dims, strides, box, 128)) return qtz_cuda_fail(p->h, cudaErrorInvalidValue, "tensor map of the activations");
+    auto go = [&](auto kernel) { return launch(p, a, kernel, kWideThreads, 1, kFixed, kN == 16 ? 16 : 8, st, x_map); };
+    if (p->scales == 8) return zero ? go(linear_wide_kernel<T, kN, 1, true>) : go(linear_wide_kernel<T, kN, 1, false>);
+    if (p->scales == 4) return zero ? go(linear_wide_kernel<T, kN, 2, true>) : go(linear_wide_kernel<T, kN, 2, false>);
+    return zero ? go(linear_wide_kernel<T, kN, 4, true>) : go(linear_wide_kernel<T, kN, 4, false>);
 }
 
 template <typename T>
@@ -780,16 +815,17 @@ qtz_status launch_rows(qtz_linear* p, LinearArgs& a, bool zero, cudaStream_t st)
     if (a.rows <= 2) return launch_digits<T, 1>(p, a, zero, st);
     if (a.rows <= 4) return launch_digits<T, 2>(p, a, zero, st);
     if (a.rows <= 8) return launch_digits<T, 3>(p, a, zero, st);
-    if (a.rows <= 16) return launch_wide<T, 2>(p, a, zero, st);
-    return launch_wide<T, 4>(p, a, zero, st);
+    if (a.rows <= 16) return launch_wide<T, 16>(p, a, zero, st);
+    if (a.rows <= 32) return launch_wide<T, 32>(p, a, zero, st);
+    return launch_wide<T, 64>(p, a, zero, st);
 }
 
 // Scratch of the joining, shared by the layers of a handle: parts and counters of a full grid.
 qtz_status ensure_scratch(qtz_ctx* h, cudaStream_t st)
 {
     if (h->linear_dev) return QTZ_OK;
-    const int ctas = 2 * h->num_sms;
-    const size_t parts = static_cast<size_t>(ctas) * 2 * kWarps * kRowTile * kMaxTokens * sizeof(float);
+    const int ctas = 2 * h->num_sms;                   // of up to eight rows; half as many with eight times the rows
+    const size_t parts = static_cast<size_t>(h->num_sms) * 2 * kWarps * kRowTile * kMaxTokens * sizeof(float);
     QTZ_CUDA(h, cudaMalloc(&h->linear_dev, parts + ctas * sizeof(int32_t)));
     QTZ_CUDA(h, cudaMemsetAsync(static_cast<uint8_t*>(h->linear_dev) + parts, 0, ctas * sizeof(int32_t), st));
     h->linear_counters = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(h->linear_dev) + parts);
