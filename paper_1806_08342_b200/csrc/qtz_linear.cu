@@ -278,9 +278,9 @@ __device__ __forceinline__ void timed_out(const LinearArgs& a)
 
 // Where the parts of a warp lie: slot 0, rows that began in an earlier CTA; slot 1, rows that go on in a later one.
 template <int kValues>
-__device__ __forceinline__ float* part_of(const LinearArgs& a, const Stream& s, int cta, int slot)
+__device__ __forceinline__ float* part_of(const LinearArgs& a, int row_tile, int lane, int cta, int slot)
 {
-    return a.parts + ((static_cast<int64_t>(cta) * 2 + slot) * kWarps + s.warp) * (32 * kValues) + s.lane;
+    return a.parts + ((static_cast<int64_t>(cta) * 2 + slot) * kWarps + row_tile) * (32 * kValues) + lane;
 }
 
 // The end of a row block, or of this CTA's columns of it: y, or a part.  A lane's values v go to y by `write(place, v)`.
@@ -294,7 +294,7 @@ __device__ __forceinline__ void finish_rows(const LinearArgs& a, const Stream& s
     }
     if (begins) open[1] = s.unit;
     else open[0] = s.unit;
-    float* part = part_of<kValues>(a, s, blockIdx.x, begins ? 1 : 0);
+    float* part = part_of<kValues>(a, s.warp, s.lane, blockIdx.x, begins ? 1 : 0);
 #pragma unroll
     for (int i = 0; i < kValues; ++i) part[i * 32] = v[i];
 }
@@ -302,7 +302,7 @@ __device__ __forceinline__ void finish_rows(const LinearArgs& a, const Stream& s
 // Rows whose columns lie in several CTAs, c0 .. c1: the last to arrive joins their parts in order.  Called by all threads; the first
 // kWarps warps hold the parts.
 template <int kValues, typename W>
-__device__ __forceinline__ void join_rows(const LinearArgs& a, const Stream& s, const int (&open)[2], const int& failed, int (&last)[2], const W& write)
+__device__ __forceinline__ void join_rows(const LinearArgs& a, int warp, int lane, const int (&open)[2], const int& failed, int (&last)[2], const W& write)
 {
     __threadfence();
     __syncthreads();
@@ -317,18 +317,18 @@ __device__ __forceinline__ void join_rows(const LinearArgs& a, const Stream& s, 
             if (last[which]) a.counters[c0[which]] = 0;    // ready for the next call
         }
     __syncthreads();
-    if (s.warp >= kWarps) return;
+    if (warp >= kWarps) return;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-        if (open[which] < 0 || !last[which] || s.tile(at[which]) >= a.row_tiles) continue;
+        if (open[which] < 0 || !last[which] || at[which].rb * kWarps + warp >= a.row_tiles) continue;
         __threadfence();
-        constexpr int kFlight = kValues <= 8 ? 8 : kValues <= 16 ? 4 : 2;     // parts in flight: what the registers hold
+        constexpr int kFlight = kValues <= 8 ? 8 : kValues <= 16 ? 4 : kValues <= 32 ? 2 : 1;     // parts in flight: what the registers hold
         float v[kValues] = {};
         for (int c = c0[which]; c <= c1[which]; c += kFlight) {
             float p[kFlight][kValues];
 #pragma unroll
             for (int x = 0; x < kFlight; ++x) {
-                const float* part = part_of<kValues>(a, s, min(c + x, c1[which]), c + x == c0[which] ? 1 : 0);
+                const float* part = part_of<kValues>(a, warp, lane, min(c + x, c1[which]), c + x == c0[which] ? 1 : 0);
 #pragma unroll
                 for (int i = 0; i < kValues; ++i) p[x][i] = __ldcg(part + i * 32);
             }
@@ -570,46 +570,57 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
         timed_out(a);
         s_failed = 1;
     }
-    join_rows<8>(a, s, open, s_failed, s_last, write);
+    join_rows<8>(a, warp, lane, open, s_failed, s_last, write);
 }
 
 // ---- more rows: 16-bit tensor cores (tcgen05) ----
-// Eight warps turn a warp's 32 rows of codes into 16-bit operands, straight into tensor memory: two tiles of 128 rows.  One warp
-// issues the products with kN rows of x, which a last warp brings by TMA.  While the products of one scale's columns run, the eight
-// warps unpack the next; then each thread, which owns a row of W, adds scale * product to its kN sums.  kSteps: steps of 32 columns to
-// a scale (1, 2 or 4).
-constexpr int kWideThreads = kThreads + 64;
+// Two groups of eight warps turn 32 rows of codes each into 16-bit operands, straight into tensor memory: two tiles of 128 rows.  One
+// warp issues the products with kN rows of x, which another brings by TMA, like the weights.  The groups take the scales in turn; each
+// hands over at most 64 columns at a time in two operand buffers.  Up to 32 rows a product lies in one of two buffers, too, and each
+// thread, which owns a row of W, adds scale * product to its kN sums while the next one's columns are multiplied (64 rows leave room
+// for one).  The groups' sums meet at the end of the rows.  kSteps: steps of 32 columns to a scale (1, 2 or 4).
+constexpr int kWideThreads = 2 * kThreads + 96;
+constexpr int kExchange = 16;                          // sums of a row that the groups exchange at a time
+template <int kN> constexpr int kXUnitsOf = kN == 64 ? 3 : 4;   // units of x under way: one takes about as long to come as two take to be used
 
 template <typename T, int kN, int kSteps, bool kZero>
 __global__ void __launch_bounds__(kWideThreads, 1)
 linear_wide_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap x_map)
 {
     constexpr int kXBox = kN * 128;                    // 64 columns of x
-    constexpr int kXUnit = kKBlock / 64 * kXBox;
+    constexpr int kXUnit = kKBlock / 64 * kXBox, kXUnits = kXUnitsOf<kN>;
     constexpr int kScales = 8 / kSteps;                // of a unit
+    constexpr int kHand = kSteps < 2 ? kSteps : 2, kHands = kSteps / kHand;    // steps handed over at a time; times to a scale
+    constexpr bool kDefer = kN <= 32;
     constexpr uint32_t kFormat = std::is_same<T, __half>::value ? 0 : 1;
     constexpr uint32_t kProduct = (1u << 4) | (kFormat << 7) | (kFormat << 10) | (static_cast<uint32_t>(kN >> 3) << 17) | (128u >> 4 << 24);
-    extern __shared__ uint8_t smem_raw[];              // two units of x, the rings
-    __shared__ __align__(8) uint64_t s_full[kWarps][kMaxStages], s_xfull[2], s_xfree[2], s_operand[2][2], s_product[2][2], s_drain;
+    extern __shared__ uint8_t smem_raw[];              // units of x, the exchange, the ring
+    __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_xfull[kXUnits], s_xfree[kXUnits], s_operand[8], s_done[8], s_drain[2];   // [tile][group][buffer]
     __shared__ int s_last[2], s_failed;
     __shared__ uint32_t s_tmem;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    if (warp < kWarps && lane < kMaxStages) mbar_init(smem_u32(&s_full[warp][lane]), 1);
+    float* const exchange = reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw)) + kXUnits * kXUnit);
+    const uint32_t ring = base + kXUnits * kXUnit + kThreads * kExchange * 4;
     if (tid == 0) {
         s_failed = 0;
         prefetch_tensormap(&x_map);
-        mbar_init(smem_u32(&s_drain), 1);
-        for (int i = 0; i < 2; ++i) {
+        mbar_init(smem_u32(&s_drain[0]), 1);
+        mbar_init(smem_u32(&s_drain[1]), 1);
+        for (int i = 0; i < a.stages; ++i) {
+            mbar_init(smem_u32(&s_full[i]), 1);
+            mbar_init(smem_u32(&s_empty[i]), 2 * kWarps);
+        }
+        for (int i = 0; i < kXUnits; ++i) {
             mbar_init(smem_u32(&s_xfull[i]), 1);
-            mbar_init(smem_u32(&s_xfree[i]), 1);
-            for (int j = 0; j < 2; ++j) {
-                mbar_init(smem_u32(&s_operand[i][j]), 4);
-                mbar_init(smem_u32(&s_product[i][j]), 1);
-            }
+            mbar_init(smem_u32(&s_xfree[i]), 2);
+        }
+        for (int i = 0; i < 8; ++i) {
+            mbar_init(smem_u32(&s_operand[i]), 4);
+            mbar_init(smem_u32(&s_done[i]), 1);
         }
     }
-    if (warp == kWarps + 1) {
+    if (warp == 2 * kWarps + 1) {
         tmem_alloc(smem_u32(&s_tmem), 512);
         tmem_relinquish();
     }
@@ -617,19 +628,19 @@ linear_wide_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = s_tmem;
-    // columns: operand [tile][buffer], then product [tile][buffer]
-    auto operand_at = [&](int tile, int buffer) { return tmem + (tile * 2 + buffer) * 64; };
-    auto product_at = [&](int tile, int buffer) { return tmem + 256 + (tile * 2 + buffer) * 64; };
-    Stream s(a, base + 2 * kXUnit + (warp < kWarps ? warp : 0) * a.stages * a.block_bytes, s_full[warp < kWarps ? warp : 0]);
-    grid_launch_dependents();
-    if (warp < kWarps) s.start();                      // the weights were there when the layer was made; all else is waited for
-    grid_dependency_wait();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
+    // columns: operand [tile][group][buffer], then product [tile][group] or [tile][group][buffer]
+    auto operand_at = [&](int which) { return tmem + which * 32; };
+    auto product_at = [&](int tile, int group, int turn) { return tmem + 256 + (tile * 2 + group) * 64 + (kDefer ? (turn & 1) * 32 : 0); };
+    const int u0 = min(static_cast<int>(blockIdx.x) * a.share, a.units), count = min(u0 + a.share, a.units) - u0;
+    Place here(a, u0);
     int open[2] = {-1, -1};                            // units whose rows are shared with an earlier / a later CTA
     bool ok = true;
+    auto wait = [&](uint64_t& bar, int parity) { ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar), parity, a.wait_budget)) && ok; };
+    const int row_tile = warp & (kWarps - 1);
     // acc[r]: output row `lane` of the tile, activation row r
     auto write = [&](const Place& at, const float (&v)[kN]) {
-        const int o = s.tile(at) * kRowTile + lane;
+        const int o = (at.rb * kWarps + row_tile) * kRowTile + lane;
         if (o >= a.n) return;
         const float b = a.bias ? qtz_dev::to_f32(static_cast<const T*>(a.bias)[o]) : 0.f;
         const int64_t r0 = static_cast<int64_t>(at.pass) * kN;
@@ -637,121 +648,221 @@ linear_wide_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__
         for (int r = 0; r < kN; ++r)
             if (r0 + r < a.rows) static_cast<T*>(a.y)[(r0 + r) * a.y_stride + o] = qtz_dev::from_f32<T>(v[r] + b);
     };
+    grid_launch_dependents();
 
-    if (warp == kWarps) {
-        // ======== x: one unit's columns at a time ========
-        int i = 0;
-        for (; s.unit < s.u1; s.next(), ++i) {
-            const int buffer = i & 1;
-            if (i >= 2 && !__all_sync(0xffffffffu, mbar_wait(smem_u32(&s_xfree[buffer]), ((i >> 1) - 1) & 1, a.wait_budget))) {
-                ok = false;
-                break;
-            }
+    if (warp == 2 * kWarps) {
+        // ======== loads: weights as many units ahead as the ring holds, x two ========
+        Place ahead = here;
+        int issued = 0;
+        auto issue_weights = [&](int stage) {
+            const uint32_t bar = smem_u32(&s_full[stage]);
+            const int first = ahead.rb * kWarps, tiles = min(kWarps, a.row_tiles - first);
+            if (lane == 0) mbar_arrive_expect_tx(bar, tiles * a.block_bytes);
+            __syncwarp();
+            if (lane < tiles)
+                bulk_load(ring + (stage * kWarps + lane) * a.block_bytes, a.blocks + (static_cast<int64_t>(first + lane) * a.k_blocks + ahead.kb) * a.block_bytes,
+                          a.block_bytes, bar);
+            ahead.next(a);
+            ++issued;
+        };
+        while (issued < min(a.stages, count)) issue_weights(issued);   // the weights were there when the layer was made
+        grid_dependency_wait();                        // all else is waited for
+        int xi = 0, stage = 0, round = 0;              // units of x; the next place of the ring
+        auto issue_x = [&]() {
+            const uint32_t bar = smem_u32(&s_xfull[xi % kXUnits]);
             if (elect_one()) {
-                const uint32_t bar = smem_u32(&s_xfull[buffer]);
                 mbar_arrive_expect_tx(bar, kXUnit);
 #pragma unroll
                 for (int c = 0; c < kKBlock / 64; ++c)
-                    tma_load_2d(base + buffer * kXUnit + c * kXBox, &x_map, bar, (s.here.kb * kKBlock + c * 64) * 2, s.here.pass * kN);
+                    tma_load_2d(base + xi % kXUnits * kXUnit + c * kXBox, &x_map, bar, (here.kb * kKBlock + c * 64) * 2, here.pass * kN);
             }
             __syncwarp();
-        }
-        for (int j = max(0, i - 2); j < i; ++j)        // nothing may be in flight when the CTA ends
-            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_xfull[j & 1]), (j >> 1) & 1, a.wait_budget)) && ok;
-    } else if (warp == kWarps + 1) {
-        // ======== products ========
-        int step = 0;
-        for (int i = 0; s.unit < s.u1 && ok; s.next(), ++i) {
-            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_xfull[i & 1]), (i >> 1) & 1, a.wait_budget));
-            for (int q = 0; q < kScales && ok; ++q, ++step) {
-                for (int tile = 0; tile < 2 && ok; ++tile) {
-                    ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_operand[tile][step & 1]), (step >> 1) & 1, a.wait_budget));
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (elect_one()) {
-#pragma unroll
-                        for (int k = 0; k < 2 * kSteps; ++k) {         // 16 columns
-                            const int column = q * kSteps * 32 + k * 16;
-                            mma_f16_from_tmem(product_at(tile, step & 1), operand_at(tile, step & 1) + 8 * k,
-                                              make_kmajor_desc(base + (i & 1) * kXUnit + column / 64 * kXBox, 128) + 2 * (column / 16 % 4), kProduct, k > 0);
-                        }
-                        mma_commit(smem_u32(&s_product[tile][step & 1]));
-                        if (q == kScales - 1 && tile == 1) mma_commit(smem_u32(&s_xfree[i & 1]));
-                    }
-                    __syncwarp();
+            here.next(a);
+            ++xi;
+        };
+        while (xi < min(kXUnits, count)) issue_x();
+        for (int i = 0; i < count && ok; ++i) {        // as unit i is used up
+            if (issued < count) {
+                wait(s_empty[stage], round & 1);
+                if (!ok) break;
+                issue_weights(stage);
+                if (++stage == a.stages) {
+                    stage = 0;
+                    ++round;
                 }
+            }
+            if (xi < count) {
+                wait(s_xfree[i % kXUnits], (i / kXUnits) & 1);
+                if (ok) issue_x();
+            }
+        }
+        // nothing may be in flight when the CTA ends
+        for (int j = max(0, xi - kXUnits); j < xi; ++j) wait(s_xfull[j % kXUnits], (j / kXUnits) & 1);
+        for (int j = max(0, issued - a.stages); j < issued; ++j) wait(s_full[j % a.stages], (j / a.stages) & 1);
+    } else if (warp > 2 * kWarps) {
+        // ======== products of a group ========
+        const int group = __shfl_sync(0xffffffffu, warp - 2 * kWarps - 1, 0);
+        int hand = 0, turn = 0, x = 0, x_round = 0;
+        for (int i = 0; i < count && ok; ++i) {
+            wait(s_xfull[x], x_round & 1);
+            const uint64_t x_desc = make_kmajor_desc(base + x * kXUnit, 128);
+#pragma unroll
+            for (int q = 0; q < kScales; q += 2) {
+#pragma unroll
+                for (int part = 0; part < kHands; ++part) {
+#pragma unroll
+                    for (int tile = 0; tile < 2; ++tile) {
+                        const int at = (tile * 2 + group) * 2 + (hand & 1);
+                        if (ok) wait(s_operand[at], (hand >> 1) & 1);
+                        if (!ok) break;
+                        tc_fence_after();
+                        const uint32_t to = product_at(tile, group, turn), from = operand_at(at);
+                        // 32 columns of x lie 64 bytes on, 64 a box; a group's step is kSteps of them
+                        const uint64_t desc = x_desc + static_cast<uint64_t>(group) * (kSteps == 1 ? 4 : kSteps == 2 ? kXBox / 16 : 2 * kXBox / 16);
+                        if (elect_one()) {
+#pragma unroll
+                            for (int k = 0; k < 2 * kHand; ++k) {      // 16 columns
+                                constexpr int kStride = kSteps * 32;
+                                const int column = q * kStride + part * kHand * 32 + k * 16;
+                                mma_f16_from_tmem(to, from + 8 * k, desc + column / 64 * (kXBox / 16) + 2 * (column / 16 % 4), kProduct, part + k > 0);
+                            }
+                            mma_commit(smem_u32(&s_done[at]));
+                            if (q + 2 >= kScales && part == kHands - 1 && tile == 1) mma_commit(smem_u32(&s_xfree[x]));
+                        }
+                        __syncwarp();
+                    }
+                    ++hand;
+                }
+                ++turn;
+            }
+            if (++x == kXUnits) {
+                x = 0;
+                ++x_round;
             }
         }
         if (!ok) {                                     // what was issued may still run: give it the same limit, then go
-            if (elect_one()) mma_commit(smem_u32(&s_drain));
+            if (elect_one()) mma_commit(smem_u32(&s_drain[group]));
             __syncwarp();
-            mbar_wait(smem_u32(&s_drain), 0, a.wait_budget);
+            mbar_wait(smem_u32(&s_drain[group]), 0, a.wait_budget);
         }
     } else {
         // ======== operands, then sums ========
-        const int tile = warp >> 2;
+        const int group = warp / kWarps, tile = row_tile >> 2;
         const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;
         float acc[kN];
 #pragma unroll
         for (int r = 0; r < kN; ++r) acc[r] = 0.f;
-        float scale = 0.f;
-        bool pending = false;                          // the product of the step before is still to be taken
-        // sums of step i (its scale in `scale`)
-        auto take = [&](int i) {
-            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_product[tile][i & 1]), (i >> 1) & 1, a.wait_budget)) && ok;
+        int stage = 0, round = 0, hand = 0, turn = 0;
+        float scale = 0.f;                             // of the product that is still to be taken
+        bool pending = false;
+        // the product of a turn
+        auto take = [&](int t) {
             tc_fence_after();
 #pragma unroll
             for (int r0 = 0; r0 < kN; r0 += 16) {
                 uint32_t v[16];
-                tmem_ld_32x16(product_at(tile, i & 1) + lanes + r0, v);
+                tmem_ld_32x16(product_at(tile, group, t) + lanes + r0, v);
                 tmem_ld_wait();
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[r0 + r] = fmaf(__uint_as_float(v[r]), scale, acc[r0 + r]);
             }
         };
-        int step = 0;
-        for (; s.unit < s.u1; s.next()) {
-            ok = s.wait() && ok;
-            const uint32_t block = s.block(), scales = block + kCodeBytes, zeros = scales + kScales * kRowTile * 2;
-            const bool work = ok && s.has_rows();
+        auto wait_done = [&](int h) { wait(s_done[(tile * 2 + group) * 2 + (h & 1)], (h >> 1) & 1); };
+        grid_dependency_wait();
+        for (int i = 0; i < count; ++i) {
+            wait(s_full[stage], round & 1);
+            const uint32_t block = ring + (stage * kWarps + row_tile) * a.block_bytes, scales = block + kCodeBytes, zeros = scales + kScales * kRowTile * 2;
+            const bool work = ok && here.rb * kWarps + row_tile < a.row_tiles;
 #pragma unroll 1
-            for (int q = 0; q < kScales; ++q, ++step) {
-                float scale_next = 0.f;
+            for (int q = group; q < kScales; q += 2, ++turn) {
+                float scale_here = 0.f;
+                uint32_t z[2] = {0x0808u, 0x0808u};
                 if (work) {
-                    scale_next = qtz_dev::to_f32(bits16_as<T>(lds16(scales + 2 * (q * 32 + (lane >> 4) * 16 + (lane & 7) * 2 + ((lane >> 3) & 1)))));
+                    scale_here = qtz_dev::to_f32(bits16_as<T>(lds16(scales + 2 * (q * 32 + (lane >> 4) * 16 + (lane & 7) * 2 + ((lane >> 3) & 1)))));
+                    if (kZero)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        uint32_t z = 0x0808u;
-                        if (kZero) z = lds16(zeros + 2 * ((q * 2 + j) * 8 + (lane >> 2)));
-                        const uint32_t z0 = (z & 0xffu) * 0x00010001u, z1 = (z >> 8) * 0x00010001u;
-                        const uint32_t to = operand_at(tile, step & 1) + lanes + (static_cast<uint32_t>(16 * j) << 16);
-#pragma unroll
-                        for (int h = 0; h < kSteps; ++h) {     // 32 columns: 16 of tensor memory
-                            const int half = q * kSteps + h;
-                            const uint2 w = lds64(block + ((half >> 1) * 2 + j) * 512 + lane * 16 + (half & 1) * 8);
-                            uint32_t lo[4], hi[4];             // rows g, g + 8
-                            unpack_codes<T>(w.x, z0, lo);
-                            unpack_codes<T>(w.y, z1, hi);
-                            tmem_st_16x256_x2(to + 16 * h, lo[0], lo[2], hi[0], hi[2], lo[1], lo[3], hi[1], hi[3]);
-                        }
-                    }
-                    tmem_st_wait();
+                        for (int j = 0; j < 2; ++j) z[j] = lds16(zeros + 2 * ((q * 2 + j) * 8 + (lane >> 2)));
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&s_operand[tile][step & 1]));
-                if (pending) take(step - 1);
-                pending = true;
-                scale = scale_next;
+#pragma unroll
+                for (int part = 0; part < kHands; ++part, ++hand) {
+                    const int at = (tile * 2 + group) * 2 + (hand & 1);
+                    if (hand >= 2) wait_done(hand - 2);        // the buffer's columns before have been multiplied
+                    if (work) {
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const uint32_t z0 = (z[j] & 0xffu) * 0x00010001u, z1 = (z[j] >> 8) * 0x00010001u;
+                            const uint32_t to = operand_at(at) + lanes + (static_cast<uint32_t>(16 * j) << 16);
+#pragma unroll
+                            for (int h = 0; h < kHand; ++h) {  // 32 columns: 16 of tensor memory
+                                const int half = q * kSteps + part * kHand + h;
+                                const uint2 w = lds64(block + ((half >> 1) * 2 + j) * 512 + lane * 16 + (half & 1) * 8);
+                                uint32_t lo[4], hi[4];         // rows g, g + 8
+                                unpack_codes<T>(w.x, z0, lo);
+                                unpack_codes<T>(w.y, z1, hi);
+                                tmem_st_16x256_x2(to + 16 * h, lo[0], lo[2], hi[0], hi[2], lo[1], lo[3], hi[1], hi[3]);
+                            }
+                        }
+                        tmem_st_wait();
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        mbar_arrive(smem_u32(&s_operand[at]));
+                        if (q + 2 >= kScales && part == kHands - 1) mbar_arrive(smem_u32(&s_empty[stage]));   // the unit's codes are taken
+                    }
+                }
+                if (kDefer) {
+                    if (pending) {
+                        // with two hands to a turn, the second has waited for the turn before already
+                        if (kHands == 1) wait_done(hand - 2);
+                        take(turn - 1);
+                    }
+                    scale = scale_here;
+                    pending = true;
+                } else {
+                    scale = scale_here;
+                    wait_done(hand - 1);
+                    take(turn);
+                }
             }
-            s.release(ok);
-            if (s.finishes()) {
-                take(step - 1);
-                pending = false;
-                finish_rows(a, s, acc, open, write);
+            if (++stage == a.stages) {
+                stage = 0;
+                ++round;
+            }
+            const bool ends = here.kb == a.k_blocks - 1;
+            if (ends || i == count - 1) {              // the end of these rows, or of this CTA's columns of them
+                if (pending) {
+                    wait_done(hand - 1);
+                    take(turn - 1);
+                    pending = false;
+                }
+#pragma unroll
+                for (int r0 = 0; r0 < kN; r0 += kExchange) {
+                    if (group == 1)
+#pragma unroll
+                        for (int r = 0; r < kExchange; ++r) exchange[(row_tile * kExchange + r) * 32 + lane] = acc[r0 + r];
+                    named_barrier(1, 2 * kThreads);
+                    if (group == 0)
+#pragma unroll
+                        for (int r = 0; r < kExchange; ++r) acc[r0 + r] += exchange[(row_tile * kExchange + r) * 32 + lane];
+                    named_barrier(1, 2 * kThreads);
+                }
+                const bool begins = i >= here.kb;
+                if (begins && ends) {
+                    if (group == 0 && work) write(here, acc);
+                } else {
+                    if (begins) open[1] = u0 + i;
+                    else open[0] = u0 + i;
+                    if (group == 0) {
+                        float* part = part_of<kN>(a, row_tile, lane, blockIdx.x, begins ? 1 : 0);
+#pragma unroll
+                        for (int r = 0; r < kN; ++r) part[r * 32] = acc[r];
+                    }
+                }
 #pragma unroll
                 for (int r = 0; r < kN; ++r) acc[r] = 0.f;
             }
+            here.next(a);
         }
     }
     if (!ok) {
@@ -760,11 +871,11 @@ linear_wide_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == kWarps + 1) {
+    if (warp == 2 * kWarps + 1) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
-    join_rows<kN>(a, s, open, s_failed, s_last, write);
+    join_rows<kN>(a, warp, lane, open, s_failed, s_last, write);
 }
 
 // ctas: of an SM; fixed: shared memory beside the rings; most_parts: that a row block is cut into
@@ -798,7 +909,7 @@ qtz_status launch_digits(qtz_linear* p, LinearArgs& a, bool zero, cudaStream_t s
 template <typename T, int kN>
 qtz_status launch_wide(qtz_linear* p, LinearArgs& a, bool zero, cudaStream_t st)
 {
-    constexpr int kFixed = 1024 + 2 * kKBlock / 64 * kN * 128;
+    constexpr int kFixed = 1024 + kXUnitsOf<kN> * (kKBlock / 64) * kN * 128 + kThreads * kExchange * 4;
     CUtensorMap x_map;                                 // bytes: columns beyond k and rows beyond the last read as zero
     const uint64_t dims[2] = {2 * static_cast<uint64_t>(a.k), static_cast<uint64_t>(a.rows)}, strides[1] = {2 * static_cast<uint64_t>(a.x_stride)};
     const uint32_t box[2] = {128, kN};
