@@ -144,7 +144,7 @@ constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxWindow = 256;
 constexpr int kShortRun = 4;                  // tokens that one warp takes; longer runs take the CTA
-constexpr int kHeld = 8;                      // 16-byte pieces of a long run that a thread keeps in registers
+constexpr int kHeld = 4;                      // 16-byte pieces of a long run that a thread keeps in registers: 64 tokens of 128 values
 
 struct AppendArgs {
     qtz_kv_cache c;
@@ -153,6 +153,7 @@ struct AppendArgs {
     const int64_t* slots;
     int64_t tokens;
     int32_t window;                           // tokens whose runs a CTA looks after
+    int32_t shift;                            // 16-byte pieces of a token: 1 << shift
     int32_t* status;
 };
 
@@ -202,7 +203,7 @@ __device__ __forceinline__ float max_abs8(uint4 v, float top)
 }
 
 // Codes of eight values.  x * (1/s) is within 2^-21 of the quotient that the definition rounds, so it rounds to the same integer
-// unless it lies within 10^-4 of the middle between two; there, and for NaN and infinity, the definition itself is taken.  The
+// unless it lies within 4 * 10^-5 of the middle between two; there, and for NaN and infinity, the definition itself is taken.  The
 // integer is read from the mantissa after adding 1.5 * 2^23 (round half to even).
 template <typename T>
 __device__ __forceinline__ uint2 quantize8(uint4 v, float s, float r)
@@ -214,7 +215,7 @@ __device__ __forceinline__ uint2 quantize8(uint4 v, float s, float r)
     for (int k = 0; k < 4; ++k) {
         const float2 f = qtz_dev::unpack2(w[k], T());
         const float t0 = f.x * r, t1 = f.y * r, u0 = t0 + 12582912.f, u1 = t1 + 12582912.f;
-        near_tie = near_tie || !(fabsf(t0 - (u0 - 12582912.f)) <= 0.4999f) || !(fabsf(t1 - (u1 - 12582912.f)) <= 0.4999f);
+        near_tie = near_tie || !(fabsf(t0 - (u0 - 12582912.f)) <= 0.49996f) || !(fabsf(t1 - (u1 - 12582912.f)) <= 0.49996f);
         q[2 * k] = __float_as_uint(u0);
         q[2 * k + 1] = __float_as_uint(u1);
     }
@@ -254,17 +255,17 @@ __device__ __forceinline__ uint4 rescale16(uint4 v, float ratio)
 // and the codes.  The window grows with the list, so that a step of single tokens spreads over the GPU and a prompt does not launch a
 // CTA for each of its tokens.  Prompts of 20 200 tokens (8 heads of 128): see the measurements in the design notes.
 template <typename T>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
 append_kernel(const __grid_constant__ AppendArgs a)
 {
     __shared__ int64_t s_slot[kMaxWindow + 1];
+    __shared__ int s_start[kMaxWindow], s_len[kMaxWindow], s_count;
+    __shared__ float s_top[2][kWarps];
     grid_launch_dependents();
     grid_dependency_wait();
-    __shared__ int s_start[kMaxWindow], s_count;
-    __shared__ float s_top[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, heads = a.c.kv_heads, dim = a.c.head_dim;
     const uint32_t block = a.c.block_tokens;
-    const int h = blockIdx.y, which = blockIdx.z;
+    const int h = blockIdx.y, which = blockIdx.z, shift = a.shift;
     const int64_t i0 = static_cast<int64_t>(blockIdx.x) * a.window;
     const int n = static_cast<int>(min(static_cast<int64_t>(a.window), a.tokens - i0));
     const int64_t limit = static_cast<int64_t>(a.c.blocks) * block;
@@ -284,21 +285,11 @@ append_kernel(const __grid_constant__ AppendArgs a)
     }
     __syncthreads();
     const int runs = s_count;
-    const T* const x = static_cast<const T*>(a.x[which]) + h * a.head_stride[which];
     const int64_t ts = a.token_stride[which];
-    const int pieces = dim / 8;               // 16-byte pieces of a token
-    // length of the run that begins at token j of the window: whole warps call it
-    auto length_of = [&](int j, uint32_t b) {
-        int len = 0;
-        while (true) {
-            const int64_t i = i0 + j + len + lane;
-            const int64_t slot = i < a.tokens ? (j + len + lane < n ? s_slot[j + len + lane + 1] : a.slots[i]) : -1;
-            const unsigned same = __ballot_sync(0xffffffffu, slot >= 0 && slot < limit && block_of(slot, block) == b);
-            if (same != 0xffffffffu) return min(len + __ffs(~same) - 1, static_cast<int>(block));
-            len += 32;
-            if (len >= static_cast<int>(block)) return static_cast<int>(block);
-        }
-    };
+    const T* const x = static_cast<const T*>(a.x[which]) + h * a.head_stride[which] + i0 * ts;
+    const int mask = (1 << shift) - 1;
+    // piece p of the run that begins at token j of the window
+    auto value = [&](int j, int p) { return *reinterpret_cast<const uint4*>(x + (j + (p >> shift)) * ts + ((p & mask) << 3)); };
     // The scale of a block after its run, and what its old codes are multiplied by (1: nothing to do).
     auto new_scale = [&](float top, const float* scale, int offset, float& ratio) {
         float s = fmaxf(__fdiv_rn(top, 127.f), QTZ_KV_MIN_SCALE);
@@ -315,13 +306,29 @@ append_kernel(const __grid_constant__ AppendArgs a)
         scale = (which ? a.c.v_scale_dev : a.c.k_scale_dev) + bh;
         codes = (which ? a.c.v_dev : a.c.k_dev) + bh * block * dim;
     };
+    // where piece p of that run goes, within its block
+    auto target = [&](int j, int p, int64_t first) {
+        const int t = j + (p >> shift);
+        const int64_t slot = t < n ? s_slot[t + 1] : a.slots[i0 + t];
+        return static_cast<int>(slot - first) * dim + ((p & mask) << 3);
+    };
 
     bool long_runs = false;
     for (int k = warp; k < runs; k += kWarps) {
         const int j = s_start[k];
         const int64_t slot = s_slot[j + 1];
         const uint32_t b = block_of(slot, block);
-        const int len = length_of(j, b);
+        const int64_t first = static_cast<int64_t>(b) * block;
+        int len = 0;
+        for (bool more = true; more;) {
+            const int t = j + len + lane;
+            const int64_t other = i0 + t < a.tokens ? (t < n ? s_slot[t + 1] : a.slots[i0 + t]) : -1;
+            const unsigned off = ~__ballot_sync(0xffffffffu, other >= first && other < first + block);
+            more = off == 0;
+            len = min(len + (more ? 32 : __ffs(off) - 1), static_cast<int>(block));
+            more = more && len < static_cast<int>(block);
+        }
+        if (lane == 0) s_len[k] = len;
         if (len > kShortRun) {
             long_runs = true;
             continue;
@@ -329,14 +336,13 @@ append_kernel(const __grid_constant__ AppendArgs a)
         float* scale;
         int8_t* codes;
         place(b, scale, codes);
-        const int offset = static_cast<int>(slot - static_cast<int64_t>(b) * block), count = len * pieces;   // at most 4 * 32
+        const int offset = static_cast<int>(slot - first), count = len << shift;     // at most 4 * 32
         uint4 v[kShortRun];
         float top = 0.f;
 #pragma unroll
         for (int q = 0; q < kShortRun; ++q) {
-            const int p = q * 32 + lane;
             v[q] = make_uint4(0, 0, 0, 0);
-            if (p < count) v[q] = *reinterpret_cast<const uint4*>(x + (i0 + j + p / pieces) * ts + p % pieces * 8);
+            if (q * 32 + lane < count) v[q] = value(j, q * 32 + lane);
         }
 #pragma unroll
         for (int q = 0; q < kShortRun; ++q) top = max_abs8<T>(v[q], top);
@@ -350,56 +356,51 @@ append_kernel(const __grid_constant__ AppendArgs a)
 #pragma unroll
         for (int q = 0; q < kShortRun; ++q) {
             const int p = q * 32 + lane;
-            if (p >= count) continue;
-            const int64_t to = j + p / pieces < n ? s_slot[j + p / pieces + 1] : a.slots[i0 + j + p / pieces];
-            *reinterpret_cast<uint2*>(codes + (to - static_cast<int64_t>(b) * block) * dim + p % pieces * 8) = quantize8<T>(v[q], s, r);
+            if (p < count) *reinterpret_cast<uint2*>(codes + target(j, p, first)) = quantize8<T>(v[q], s, r);
         }
     }
     if (!__syncthreads_or(long_runs)) return;
+    int turn = 0;
     for (int k = 0; k < runs; ++k) {
+        const int len = s_len[k];
+        if (len <= kShortRun) continue;
         const int j = s_start[k];
         const int64_t slot = s_slot[j + 1];
         const uint32_t b = block_of(slot, block);
-        const int len = length_of(j, b);
-        if (len <= kShortRun) continue;
+        const int64_t first = static_cast<int64_t>(b) * block;
         float* scale;
         int8_t* codes;
         place(b, scale, codes);
-        const int offset = static_cast<int>(slot - static_cast<int64_t>(b) * block), count = len * pieces;
-        auto value = [&](int p) { return *reinterpret_cast<const uint4*>(x + (i0 + j + p / pieces) * ts + p % pieces * 8); };
+        const int offset = static_cast<int>(slot - first), count = len << shift;
+        const float before = offset > 0 ? *scale : 0.f;    // in flight beside the values
         uint4 held[kHeld];
         float top = 0.f;
 #pragma unroll
         for (int q = 0; q < kHeld; ++q) {
-            const int p = q * kThreads + tid;
             held[q] = make_uint4(0, 0, 0, 0);
-            if (p < count) held[q] = value(p);
+            if (q * kThreads + tid < count) held[q] = value(j, q * kThreads + tid);
         }
 #pragma unroll
         for (int q = 0; q < kHeld; ++q) top = max_abs8<T>(held[q], top);
-        for (int p = kHeld * kThreads + tid; p < count; p += kThreads) top = max_abs8<T>(value(p), top);   // read again below
+        for (int p = kHeld * kThreads + tid; p < count; p += kThreads) top = max_abs8<T>(value(j, p), top);   // read again below
         top = redux_max(top);
-        if (lane == 0) s_top[warp] = top;
-        __syncthreads();
+        float* const tops = s_top[turn ^= 1];          // two places: a run's are read while the next one's are written
+        if (lane == 0) tops[warp] = top;
+        __syncthreads();                               // and every thread has read the old scale
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_top[w]);
+        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, tops[w]);
         float ratio;
-        const float s = new_scale(top, scale, offset, ratio), r = __frcp_rn(s);
-        __syncthreads();                      // every thread has read the old scale and the maxima
+        const float s = new_scale(top, &before, offset, ratio), r = __frcp_rn(s);
         if (tid == 0) *scale = s;
         if (ratio != 1.f)
             for (int p = tid; p < offset * dim / 16; p += kThreads) reinterpret_cast<uint4*>(codes)[p] = rescale16(reinterpret_cast<uint4*>(codes)[p], ratio);
-        auto store = [&](int p, uint4 v) {
-            const int t = p / pieces;
-            const int64_t to = j + t < n ? s_slot[j + t + 1] : a.slots[i0 + j + t];
-            *reinterpret_cast<uint2*>(codes + (to - static_cast<int64_t>(b) * block) * dim + (p - t * pieces) * 8) = quantize8<T>(v, s, r);
-        };
 #pragma unroll
         for (int q = 0; q < kHeld; ++q) {
             const int p = q * kThreads + tid;
-            if (p < count) store(p, held[q]);
+            if (p < count) *reinterpret_cast<uint2*>(codes + target(j, p, first)) = quantize8<T>(held[q], s, r);
         }
-        for (int p = kHeld * kThreads + tid; p < count; p += kThreads) store(p, value(p));
+        for (int p = kHeld * kThreads + tid; p < count; p += kThreads)
+            *reinterpret_cast<uint2*>(codes + target(j, p, first)) = quantize8<T>(value(j, p), s, r);
     }
 }
 
@@ -430,10 +431,10 @@ read_kernel(const __grid_constant__ ReadArgs a)
     if (bad && lane == 0) qtz_dev::report_invalid(a.status, QTZ_SITE_KV_READ);
     const uint32_t b = none ? 0 : block_of(slot, block);
     const int offset = none ? 0 : static_cast<int>(slot - static_cast<int64_t>(b) * block);
-    const int per_head = a.c.head_dim / 16, pieces = a.c.kv_heads * per_head;
+    const int shift = a.c.head_dim == 64 ? 2 : a.c.head_dim == 128 ? 3 : 4, pieces = a.c.kv_heads << shift;   // of 16 codes
 #pragma unroll 4
     for (int p = lane; p < 2 * pieces; p += 32) {
-        const int which = p >= pieces, u = p - which * pieces, h = u / per_head, d = (u - h * per_head) * 16;
+        const int which = p >= pieces, u = p - which * pieces, h = u >> shift, d = (u - (h << shift)) * 16;
         const int64_t bh = static_cast<int64_t>(b) * a.c.kv_heads + h;
         uint4 q = make_uint4(0, 0, 0, 0);
         float s = 0.f;
@@ -518,7 +519,7 @@ extern "C" qtz_status qtz_kv_append(qtz_handle h, const qtz_kv_cache* cache, con
     const int64_t ctas = (tokens + window - 1) / window;
     if (ctas > 0x7fffffff) return QTZ_ERR_TOO_LARGE;
     const AppendArgs a{*cache, {k_dev, v_dev}, {k_token_stride, v_token_stride}, {k_head_stride, v_head_stride}, slots_dev, tokens,
-                       static_cast<int32_t>(window), h->status_dev};
+                       static_cast<int32_t>(window), cache->head_dim == 64 ? 3 : cache->head_dim == 128 ? 4 : 5, h->status_dev};
     const dim3 grid(static_cast<unsigned>(ctas), static_cast<unsigned>(cache->kv_heads), 2);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     QTZ_CUDA(h, qtz_launch_dependent(ftype == QTZ_F16 ? append_kernel<__half> : append_kernel<__nv_bfloat16>, grid, kThreads, 0, st, a));
