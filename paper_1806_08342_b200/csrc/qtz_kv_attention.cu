@@ -247,7 +247,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
 
     if (tid == 0) {
         sh.open[0].c1 = sh.open[1].c1 = -1;
-        sh.failed = 0;
+        sh.failed = sh.tiles = 0;
         prefetch_tensormap(&k_map);
         prefetch_tensormap(&v_map);
         for (int i = 0; i < kMaxStages; ++i) {
@@ -276,9 +276,10 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
     const int per = (a.requests + kThreads - 1) / kThreads;
     const int r_lo = min(tid * per, a.requests), r_hi = min(r_lo + per, a.requests);
     uint32_t mine = 0;
+    RequestShape shape = {};                           // of the last of them: the only one up to kThreads requests
     for (int r = r_lo; r < r_hi; ++r) {
-        const RequestShape s = shape_of<kRows>(a, r);
-        const uint32_t n = static_cast<uint32_t>(a.c.kv_heads) * s.row_tiles * s.item_units();
+        shape = shape_of<kRows>(a, r);
+        const uint32_t n = static_cast<uint32_t>(a.c.kv_heads) * shape.row_tiles * shape.item_units();
         prefix[r] = n;
         mine += n;
     }
@@ -314,31 +315,25 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
     auto timed_out = [&]() {
         if (lane == 0 && atomicCAS(a.status, 0, QTZ_ERR_DEVICE_TIMEOUT) == 0) a.status[1] = QTZ_SITE_KV_ATTENTION;
     };
-    if (u1 > u0 && warp == 0) {
-        auto request_at = [&](uint32_t unit) {         // the last request that begins at or before the unit
-            int u = 0, v = a.requests;
-            while (v - u > 1) {
-                const int mid = (u + v) >> 1;
-                if (prefix[mid] <= unit) u = mid; else v = mid;
-            }
-            return u;
-        };
-        const int first = request_at(u0), last = request_at(u1 - 1);
+    if (u1 > u0) {
+        int u = 0, v = a.requests;                     // the last request that begins at or before the share
+        while (v - u > 1) {
+            const int mid = (u + v) >> 1;
+            if (prefix[mid] <= static_cast<uint32_t>(u0)) u = mid; else v = mid;
+        }
+        if (tid == 0) known.first = u;
         int tiles = 0;                                 // that begin in [u0, u1)
-        for (int r = first + lane; r <= last; r += 32) {
-            const RequestShape s = shape_of<kRows>(a, r);
-            if (r - first < kKnown) known.s[r - first] = s;
+        for (int r = max(r_lo, u); r < r_hi && prefix[r] < static_cast<uint32_t>(u1); ++r) {
+            if (per > 1) shape = shape_of<kRows>(a, r);
+            if (r - u < kKnown) known.s[r - u] = shape;
+            if (shape.row_tiles == 0) continue;
             const int end = static_cast<int>(min(prefix[r + 1], static_cast<uint32_t>(u1)) - prefix[r]);
-            if (s.row_tiles > 0) tiles += s.tiles_before(end) - (r == first ? s.tiles_before(u0 - static_cast<int>(prefix[r])) : 0);
+            tiles += shape.tiles_before(end) - (r == u ? shape.tiles_before(u0 - static_cast<int>(prefix[r])) : 0);
         }
-        tiles = __reduce_add_sync(0xffffffffu, tiles);
-        if (lane == 0) {
-            known.first = first;
-            sh.tiles = tiles;
-        }
+        if (tiles) atomicAdd(&sh.tiles, tiles);
     }
     __syncthreads();
-    const int count = u1 > u0 ? sh.tiles : 0;
+    const int count = sh.tiles;
     Cursor<kRows> cur;
     if (count > 0) cur.seek(a, prefix, known, u0);
 
@@ -796,66 +791,52 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         if (sh.last[warp]) *counter = 0;               // ready for the next call
     }
     __syncthreads();
-    // three warps for each of the two items
-    constexpr int kHalf = kThreads / 2, kFlight = kRows <= 5 ? 6 : 9;   // parts in flight: what the registers hold
-    const int slot = tid / kHalf, ht = tid % kHalf;
+    // Half of the warps for each of the two items, all for one.
+    const bool both = sh.open[0].c1 >= 0 && sh.last[0] && sh.open[1].c1 >= 0 && sh.last[1];
+    const int crew = both ? kThreads / 2 : kThreads, slot = both ? tid / crew : sh.open[1].c1 >= 0 && sh.last[1] ? 1 : 0, ht = tid % crew;
     const OpenItem& open = sh.open[slot];
     float (*const jm)[kMaxRows] = reinterpret_cast<float (*)[kMaxRows]>(smem + slot * 8192), (*const jl)[kMaxRows] = jm + kFanIn, (*const jw)[kMaxRows] = jl + kFanIn;
     float* const j_top = reinterpret_cast<float*>(jw + kFanIn), * const j_sum = j_top + kMaxRows;
-    auto sync_half = [&]() { named_barrier(2 + slot, kHalf); };
+    auto sync_crew = [&]() { named_barrier(2 + slot, crew); };
     if (open.c1 >= 0 && sh.last[slot]) {
         __threadfence();
         const int c0 = open.c0, c1 = open.c1, size = group_size(c1 - c0 + 1), groups = (c1 - c0) / size + 1, first = me - (me - c0) % size;
         auto part_of = [&](int cta) { return a.parts + (static_cast<int64_t>(cta) * 2 + (cta == c0 ? 1 : 0)) * kPart; };
-        // Joins the n parts of CTAs from, from + step, ..: into `to`, or into the output.
-        auto join = [&](int from, int step, int n, float* to) {
-            for (int i = ht; i < n * kMaxRows; i += kHalf) {
-                const float* p = part_of(from + i / kMaxRows * step) + kMaxRows * D + i % kMaxRows;
-                jm[i / kMaxRows][i % kMaxRows] = __ldcg(p);
-                jl[i / kMaxRows][i % kMaxRows] = __ldcg(p + kMaxRows);
-            }
-            sync_half();
-            for (int i = ht; i < n * kMaxRows; i += kHalf) {
-                const int j = i / kMaxRows, r = i % kMaxRows;
-                float top = -INFINITY;
-                for (int x = 0; x < n; ++x) top = fmaxf(top, jm[x][r]);
-                const float mj = jm[j][r], lj = jl[j][r];
-                jw[j][r] = mj == -INFINITY && lj == 0.f ? 0.f : ex2(mj - (top == -INFINITY ? 0.f : top));
-                if (j == 0) j_top[r] = top;
-            }
-            sync_half();
-            if (ht < kMaxRows) {
-                float sum = 0.f;
-                for (int x = 0; x < n; ++x) sum = fmaf(jl[x][ht], jw[x][ht], sum);
-                j_sum[ht] = sum;
-            }
-            sync_half();
-            constexpr int kQuads = kRows * D / 4;
-            for (int q0 = ht; q0 < kQuads; q0 += 2 * kHalf) {
-                float4 v[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-                const int u2[2] = {q0, min(q0 + kHalf, kQuads - 1)};
+        constexpr int kQuads = kRows * D / 4;          // four neighbouring values of a row
+        // Weighted sums over n parts, kFlight parts of kAtOnce quads in flight: a part comes from L2 in half a microsecond.
+        auto add_up = [&](auto flight, auto at_once, int from, int step, int n, float* to) {
+            constexpr int kFlight = decltype(flight)::value, kAtOnce = decltype(at_once)::value;
+            for (int q0 = ht; q0 < kQuads; q0 += kAtOnce * crew) {
+                float4 v[kAtOnce];
+                int quad[kAtOnce];
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j) {
+                    v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    quad[j] = min(q0 + j * crew, kQuads - 1);
+                }
                 for (int x0 = 0; x0 < n; x0 += kFlight) {
-                    float4 p[2][kFlight];
+                    float4 p[kAtOnce][kFlight];
 #pragma unroll
                     for (int x = 0; x < kFlight; ++x)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j)
-                            p[j][x] = __ldcg(reinterpret_cast<const float4*>(part_of(from + min(x0 + x, n - 1) * step)) + u2[j]);
+                        for (int j = 0; j < kAtOnce; ++j)
+                            if (x0 + x < n) p[j][x] = __ldcg(reinterpret_cast<const float4*>(part_of(from + (x0 + x) * step)) + quad[j]);
 #pragma unroll
                     for (int x = 0; x < kFlight; ++x)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const float w = x0 + x < n ? jw[x0 + x][u2[j] / (D / 4)] : 0.f;
-                            v[j].x = fmaf(p[j][x].x, w, v[j].x);
-                            v[j].y = fmaf(p[j][x].y, w, v[j].y);
-                            v[j].z = fmaf(p[j][x].z, w, v[j].z);
-                            v[j].w = fmaf(p[j][x].w, w, v[j].w);
-                        }
+                        for (int j = 0; j < kAtOnce; ++j)
+                            if (x0 + x < n) {
+                                const float w = jw[x0 + x][quad[j] / (D / 4)];
+                                v[j].x = fmaf(p[j][x].x, w, v[j].x);
+                                v[j].y = fmaf(p[j][x].y, w, v[j].y);
+                                v[j].z = fmaf(p[j][x].z, w, v[j].z);
+                                v[j].w = fmaf(p[j][x].w, w, v[j].w);
+                            }
                 }
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    if (q0 + j * kHalf >= kQuads) break;
-                    const int r = u2[j] / (D / 4), d = u2[j] % (D / 4) * 4;
+                for (int j = 0; j < kAtOnce; ++j) {
+                    if (q0 + j * crew >= kQuads) break;
+                    const int r = quad[j] / (D / 4), d = quad[j] % (D / 4) * 4;
                     if (to) {
                         *reinterpret_cast<float4*>(to + r * D + d) = v[j];
                         if (d == 0) {
@@ -873,16 +854,42 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                 }
             }
         };
+        // Joins the n parts of CTAs from, from + step, ..: into `to`, or into the output.
+        auto join = [&](int from, int step, int n, float* to) {
+            for (int i = ht; i < n * kMaxRows; i += crew) {
+                const float* p = part_of(from + i / kMaxRows * step) + kMaxRows * D + i % kMaxRows;
+                jm[i / kMaxRows][i % kMaxRows] = __ldcg(p);
+                jl[i / kMaxRows][i % kMaxRows] = __ldcg(p + kMaxRows);
+            }
+            sync_crew();
+            for (int i = ht; i < n * kMaxRows; i += crew) {
+                const int j = i / kMaxRows, r = i % kMaxRows;
+                float top = -INFINITY;
+                for (int x = 0; x < n; ++x) top = fmaxf(top, jm[x][r]);
+                const float mj = jm[j][r], lj = jl[j][r];
+                jw[j][r] = mj == -INFINITY && lj == 0.f ? 0.f : ex2(mj - (top == -INFINITY ? 0.f : top));
+                if (j == 0) j_top[r] = top;
+            }
+            sync_crew();
+            if (ht < kMaxRows) {
+                float sum = 0.f;
+                for (int x = 0; x < n; ++x) sum = fmaf(jl[x][ht], jw[x][ht], sum);
+                j_sum[ht] = sum;
+            }
+            sync_crew();
+            if (n <= 4) add_up(std::integral_constant<int, 4>(), std::integral_constant<int, 4>(), from, step, n, to);
+            else add_up(std::integral_constant<int, 9>(), std::integral_constant<int, 2>(), from, step, n, to);
+        };
         join(first, 1, min(size, c1 - first + 1), groups > 1 ? part_of(first) : nullptr);
         if (groups > 1) {
             __threadfence();
-            sync_half();
+            sync_crew();
             if (ht == 0) {
                 int32_t* counter = a.counters + 2 * gridDim.x + c0;
                 sh.last[slot] = atomicAdd(counter, 1) == groups - 1;
                 if (sh.last[slot]) *counter = 0;
             }
-            sync_half();
+            sync_crew();
             if (sh.last[slot]) {
                 __threadfence();
                 join(c0, size, groups, nullptr);

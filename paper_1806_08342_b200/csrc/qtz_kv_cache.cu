@@ -261,8 +261,7 @@ append_kernel(const __grid_constant__ AppendArgs a)
     __shared__ int64_t s_slot[kMaxWindow + 1];
     __shared__ int s_start[kMaxWindow], s_len[kMaxWindow], s_count;
     __shared__ float s_top[2][kWarps];
-    grid_launch_dependents();
-    grid_dependency_wait();
+    grid_dependency_wait();                            // the next kernel is not let in early: its waiting CTAs cost this one 3 us of 7
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, heads = a.c.kv_heads, dim = a.c.head_dim;
     const uint32_t block = a.c.block_tokens;
     const int h = blockIdx.y, which = blockIdx.z, shift = a.shift;
@@ -422,7 +421,6 @@ read_kernel(const __grid_constant__ ReadArgs a)
 {
     const int64_t i = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
     const int lane = threadIdx.x & 31;
-    grid_launch_dependents();
     if (i >= a.tokens) return;
     grid_dependency_wait();
     const int64_t slot = a.slots[i];
