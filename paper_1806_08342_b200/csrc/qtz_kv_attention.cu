@@ -310,8 +310,12 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
 
     // No share is smaller than a tile: every CTA between an item's first and last has a part of it.
     const int all = static_cast<int>(total);
-    const int share = max((all + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x), kTileUnits);
-    const int u0 = min(static_cast<int>(blockIdx.x) * share, all), u1 = min(u0 + share, all);
+    // Share c begins at floor(all c / sharing), so that equal items whose number divides the grid begin with a share and need no
+    // change of item within one (one request of 262143 tokens and 4 heads: 58 us against 63 with shares rounded up).
+    const uint32_t sharing = min(gridDim.x, max(total / kTileUnits, 1u)), least = total / sharing, left = total - least * sharing;
+    auto share_begin = [&](uint32_t c) { return c >= sharing ? all : static_cast<int>(c * least + c * left / sharing); };
+    auto share_of = [&](uint32_t unit) { return static_cast<int>((static_cast<uint64_t>(unit + 1) * sharing - 1) / total); };
+    const int u0 = share_begin(blockIdx.x), u1 = share_begin(blockIdx.x + 1);
     auto timed_out = [&]() {
         if (lane == 0 && atomicCAS(a.status, 0, QTZ_ERR_DEVICE_TIMEOUT) == 0) a.status[1] = QTZ_SITE_KV_ATTENTION;
     };
@@ -748,8 +752,8 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                         open.lse[tid] = it.lse[tid];
                     }
                     if (tid == 0) {
-                        open.c0 = static_cast<int>(cur.begin) / share;
-                        open.c1 = static_cast<int>(cur.begin + kTileUnits * (cur.s.tiles - 1)) / share;
+                        open.c0 = share_of(cur.begin);
+                        open.c1 = share_of(cur.begin + kTileUnits * (cur.s.tiles - 1));
                     }
                 }
                 reset();
