@@ -47,7 +47,7 @@ constexpr int kThreads = kWarps * 32;
 constexpr int kRowTile = 32, kKBlock = 256;
 constexpr int kCodeBytes = kRowTile * kKBlock / 2;
 constexpr int kMaxStages = 8;
-constexpr int kMaxTokens = 64;             // activation rows of one pass over the weights
+constexpr int kMaxTokens = 32;             // activation rows of one pass over the weights
 constexpr int kSmemLimit = 227 * 1024;
 
 // ------------------------------------------------------------------------------------
@@ -108,7 +108,7 @@ struct LinearArgs {
     const void* bias;
     void* y;
     int64_t y_stride;
-    int32_t n, k, row_tiles, k_blocks, row_blocks, units, share;
+    int32_t n, k, row_tiles, k_blocks, passes, units, share;
     int32_t per_block, block_bytes, stages;
     float* parts;                          // [CTAs][2][256 * kMaxTokens]
     int32_t* counters;                     // [CTAs]
@@ -194,22 +194,22 @@ __device__ __forceinline__ uint32_t lds16(uint32_t addr)
 
 // What both kernels share: a warp's stream of weight blocks, the writing of rows, the joining of parts.  A lane holds eight values
 // of each block of eight activation rows: v[j][c] belongs to output row g + 8 (c >> 1) of half j and activation row 2 t4 + (c & 1).
-struct Place {                             // a unit: (rows of x, 256 rows of W, 256 columns), the columns fastest
+struct Place {                             // a unit: (256 rows of W, rows of x, 256 columns), the columns fastest: what several passes read of W is in L2
     int kb, rb, pass;
     __device__ __forceinline__ Place(const LinearArgs& a, int unit)
     {
         const int rows = unit / a.k_blocks;
         kb = unit - rows * a.k_blocks;
-        pass = rows / a.row_blocks;
-        rb = rows - pass * a.row_blocks;
+        rb = rows / a.passes;
+        pass = rows - rb * a.passes;
     }
     __device__ __forceinline__ void next(const LinearArgs& a)
     {
         if (++kb < a.k_blocks) return;
         kb = 0;
-        if (++rb < a.row_blocks) return;
-        rb = 0;
-        ++pass;
+        if (++pass < a.passes) return;
+        pass = 0;
+        ++rb;
     }
 };
 
@@ -276,68 +276,88 @@ __device__ __forceinline__ void timed_out(const LinearArgs& a)
     if ((threadIdx.x & 31) == 0 && atomicCAS(a.status, 0, QTZ_ERR_DEVICE_TIMEOUT) == 0) a.status[1] = QTZ_SITE_LINEAR;
 }
 
-// Where the parts of a warp lie: slot 0, rows that began in an earlier CTA; slot 1, rows that go on in a later one.
-template <int kValues>
-__device__ __forceinline__ float* part_of(const LinearArgs& a, int row_tile, int lane, int cta, int slot)
+// A CTA's sums over a part of the columns, [activation row][256 rows of W].  Slot 0: rows that began in an earlier CTA; slot 1, rows
+// that go on in a later one.
+template <int kRows>
+__device__ __forceinline__ float* part_of(const LinearArgs& a, int cta, int slot)
 {
-    return a.parts + ((static_cast<int64_t>(cta) * 2 + slot) * kWarps + row_tile) * (32 * kValues) + lane;
+    return a.parts + (static_cast<int64_t>(cta) * 2 + slot) * (kWarps * kRowTile * kRows);
 }
 
-// The end of a row block, or of this CTA's columns of it: y, or a part.  A lane's values v go to y by `write(place, v)`.
-template <int kValues, typename W>
-__device__ __forceinline__ void finish_rows(const LinearArgs& a, const Stream& s, const float (&v)[kValues], int (&open)[2], const W& write)
+template <typename T>
+__device__ __forceinline__ float bias_of(const LinearArgs& a, int o)
 {
-    const bool begins = s.unit - s.here.kb >= s.u0;
-    if (begins && s.ends()) {
-        if (s.has_rows()) write(s.here, v);
-        return;
-    }
-    if (begins) open[1] = s.unit;
-    else open[0] = s.unit;
-    float* part = part_of<kValues>(a, s.warp, s.lane, blockIdx.x, begins ? 1 : 0);
-#pragma unroll
-    for (int i = 0; i < kValues; ++i) part[i * 32] = v[i];
+    return a.bias && o < a.n ? qtz_dev::to_f32(static_cast<const T*>(a.bias)[o]) : 0.f;
+}
+
+template <typename T>
+__device__ __forceinline__ void put(const LinearArgs& a, int64_t r, int o, float v)
+{
+    if (o < a.n && r < a.rows) static_cast<T*>(a.y)[r * a.y_stride + o] = qtz_dev::from_f32<T>(v);
 }
 
 // Rows whose columns lie in several CTAs, c0 .. c1: the last to arrive joins their parts in order.  Called by all threads; the first
-// kWarps warps hold the parts.
-template <int kValues, typename W>
-__device__ __forceinline__ void join_rows(const LinearArgs& a, int warp, int lane, const int (&open)[2], const int& failed, int (&last)[2], const W& write)
+// kJoin know the units that are open.  All of them read, 16 bytes a load and 16 loads in flight, in short code that comes from memory
+// like the parts: a warp for each 32 rows of W with everything unrolled took 7 us of 50 for 32 rows through 28672 x 8192.
+template <typename T, int kRows, int kJoin>
+__device__ __forceinline__ void join_rows(const LinearArgs& a, const int (&open)[2], const int& failed, int (&last)[2])
 {
+    constexpr int kQuads = kWarps * kRowTile / 4, kAtOnce = (kRows * kQuads + kJoin - 1) / kJoin, kFlight = 16 / kAtOnce;
+    const int tid = threadIdx.x;
     __threadfence();
     __syncthreads();
-    if (failed) return;                                // the results are void, and the counters have to be cleared
-    const Place at[2] = {Place(a, max(open[0], 0)), Place(a, max(open[1], 0))};
-    const int c0[2] = {(open[0] - at[0].kb) / a.share, (open[1] - at[1].kb) / a.share};
-    const int c1[2] = {(open[0] - at[0].kb + a.k_blocks - 1) / a.share, (open[1] - at[1].kb + a.k_blocks - 1) / a.share};
-#pragma unroll
-    for (int which = 0; which < 2; ++which)
-        if (threadIdx.x == 32 * which && open[which] >= 0) {
-            last[which] = atomicAdd(a.counters + c0[which], 1) == c1[which] - c0[which];
-            if (last[which]) a.counters[c0[which]] = 0;    // ready for the next call
-        }
-    __syncthreads();
-    if (warp >= kWarps) return;
-#pragma unroll
+    if (failed || tid >= kJoin) return;                // after a wait that gave up the results are void
+    auto first = [&](int unit) { return unit / a.k_blocks * a.k_blocks; };
+    if ((tid == 0 && open[0] >= 0) || (tid == 32 && open[1] >= 0)) {
+        const int begin = first(tid ? open[1] : open[0]), c0 = begin / a.share;
+        const bool all = atomicAdd(a.counters + c0, 1) == (begin + a.k_blocks - 1) / a.share - c0;
+        last[tid ? 1 : 0] = all;
+        if (all) a.counters[c0] = 0;                   // ready for the next call
+    }
+    named_barrier(1, kJoin);
+#pragma unroll 1
     for (int which = 0; which < 2; ++which) {
-        if (open[which] < 0 || !last[which] || at[which].rb * kWarps + warp >= a.row_tiles) continue;
+        const int unit = which ? open[1] : open[0];
+        if (unit < 0 || !last[which]) continue;
         __threadfence();
-        constexpr int kFlight = kValues <= 8 ? 8 : kValues <= 16 ? 4 : kValues <= 32 ? 2 : 1;     // parts in flight: what the registers hold
-        float v[kValues] = {};
-        for (int c = c0[which]; c <= c1[which]; c += kFlight) {
-            float p[kFlight][kValues];
+        const Place at(a, unit);
+        const int c0 = first(unit) / a.share, c1 = (first(unit) + a.k_blocks - 1) / a.share;
+        const int64_t r0 = static_cast<int64_t>(at.pass) * kRows;
+        const int quads = static_cast<int>(min(static_cast<int64_t>(kRows), a.rows - r0)) * kQuads;
+        float4 v[kAtOnce];
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+        for (int c = c0; c <= c1; c += kFlight) {
+            float4 p[kFlight][kAtOnce];
 #pragma unroll
             for (int x = 0; x < kFlight; ++x) {
-                const float* part = part_of<kValues>(a, warp, lane, min(c + x, c1[which]), c + x == c0[which] ? 1 : 0);
+                const float4* part = reinterpret_cast<const float4*>(part_of<kRows>(a, c + x, c + x == c0 ? 1 : 0)) + tid;
 #pragma unroll
-                for (int i = 0; i < kValues; ++i) p[x][i] = __ldcg(part + i * 32);
+                for (int j = 0; j < kAtOnce; ++j)
+                    p[x][j] = c + x <= c1 && tid + j * kJoin < quads ? __ldcg(part + j * kJoin) : make_float4(0.f, 0.f, 0.f, 0.f);
             }
 #pragma unroll
             for (int x = 0; x < kFlight; ++x)
 #pragma unroll
-                for (int i = 0; i < kValues; ++i) v[i] += c + x <= c1[which] ? p[x][i] : 0.f;
+                for (int j = 0; j < kAtOnce; ++j) {
+                    v[j].x += p[x][j].x;
+                    v[j].y += p[x][j].y;
+                    v[j].z += p[x][j].z;
+                    v[j].w += p[x][j].w;
+                }
         }
-        write(at[which], v);
+        const int o = at.rb * (kWarps * kRowTile) + tid % kQuads * 4;
+        const float4 b = make_float4(bias_of<T>(a, o), bias_of<T>(a, o + 1), bias_of<T>(a, o + 2), bias_of<T>(a, o + 3));
+#pragma unroll
+        for (int j = 0; j < kAtOnce; ++j) {
+            if (tid + j * kJoin >= quads) break;
+            const int64_t r = r0 + (tid + j * kJoin) / kQuads;
+            put<T>(a, r, o, v[j].x + b.x);
+            put<T>(a, r, o + 1, v[j].y + b.y);
+            put<T>(a, r, o + 2, v[j].z + b.z);
+            put<T>(a, r, o + 3, v[j].w + b.w);
+        }
     }
 }
 
@@ -455,19 +475,6 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
         }
     };
 
-    // v[4 j + c]: output row g + 8 (c >> 1) of half j, activation row 2 t4 + (c & 1)
-    auto write = [&](const Place& at, const float (&v)[8]) {
-        if (2 * t4 >= kRows) return;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int o = s.tile(at) * kRowTile + g + 8 * i;
-            if (o >= a.n) continue;
-            const float b = a.bias ? qtz_dev::to_f32(static_cast<const T*>(a.bias)[o]) : 0.f;
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-                if (2 * t4 + c < rows) static_cast<T*>(a.y)[(2 * t4 + c) * a.y_stride + o] = qtz_dev::from_f32<T>(v[2 * i + c] + b);
-        }
-    };
     float acc[2][kTiles][4] = {};
     int open[2] = {-1, -1};                            // units whose rows are shared with an earlier / a later CTA
     if (s.u0 < s.u1) convert(0, s.here.kb, 0, 0);
@@ -563,35 +570,51 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
 #pragma unroll
                     for (int nt = 0; nt < kTiles; ++nt) acc[j][nt][c] = 0.f;
                 }
-            finish_rows(a, s, v, open, write);
+            // v[2 i + c]: output row g + 8 i, activation row 2 t4 + c
+            const bool begins = s.unit - s.here.kb >= s.u0, whole = begins && s.ends();
+            if (!whole) {
+                if (begins) open[1] = s.unit;
+                else open[0] = s.unit;
+            }
+            float* const part = part_of<8>(a, blockIdx.x, begins ? 1 : 0) + warp * kRowTile + g;
+            const int o = s.tile(s.here) * kRowTile + g;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float b = whole ? bias_of<T>(a, o + 8 * i) : 0.f;
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const int r = 2 * t4 + c;
+                    if (r >= rows) continue;
+                    if (whole) put<T>(a, r, o + 8 * i, v[2 * i + c] + b);
+                    else part[r * (kWarps * kRowTile) + 8 * i] = v[2 * i + c];
+                }
+            }
         }
     }
     if (!ok) {
         timed_out(a);
         s_failed = 1;
     }
-    join_rows<8>(a, warp, lane, open, s_failed, s_last, write);
+    join_rows<T, 8, kThreads>(a, open, s_failed, s_last);
 }
 
 // ---- more rows: 16-bit tensor cores (tcgen05) ----
 // Two groups of eight warps turn 32 rows of codes each into 16-bit operands, straight into tensor memory: two tiles of 128 rows.  One
 // warp issues the products with kN rows of x, which another brings by TMA, like the weights.  The groups take the scales in turn; each
-// hands over at most 64 columns at a time in two operand buffers.  Up to 32 rows a product lies in one of two buffers, too, and each
-// thread, which owns a row of W, adds scale * product to its kN sums while the next one's columns are multiplied (64 rows leave room
-// for one).  The groups' sums meet at the end of the rows.  kSteps: steps of 32 columns to a scale (1, 2 or 4).
+// hands over at most 64 columns at a time in two operand buffers.  A product lies in one of two buffers, too, and each thread, which
+// owns a row of W, adds scale * product to its kN sums while the next one's columns are multiplied.  The groups' sums meet at the end of the rows.  kSteps: steps of 32 columns to a scale (1, 2 or 4).
 constexpr int kWideThreads = 2 * kThreads + 96;
-constexpr int kExchange = 16;                          // sums of a row that the groups exchange at a time
-template <int kN> constexpr int kXUnitsOf = kN == 64 ? 3 : 4;   // units of x under way: one takes about as long to come as two take to be used
+constexpr int kExchange = 8;                           // sums of a row that each group hands to the other at a time
+constexpr int kXUnits = 4;                             // units of x under way: one takes about as long to come as two take to be used
 
 template <typename T, int kN, int kSteps, bool kZero>
 __global__ void __launch_bounds__(kWideThreads, 1)
 linear_wide_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap x_map)
 {
     constexpr int kXBox = kN * 128;                    // 64 columns of x
-    constexpr int kXUnit = kKBlock / 64 * kXBox, kXUnits = kXUnitsOf<kN>;
+    constexpr int kXUnit = kKBlock / 64 * kXBox;
     constexpr int kScales = 8 / kSteps;                // of a unit
     constexpr int kHand = kSteps < 2 ? kSteps : 2, kHands = kSteps / kHand;    // steps handed over at a time; times to a scale
-    constexpr bool kDefer = kN <= 32;
     constexpr uint32_t kFormat = std::is_same<T, __half>::value ? 0 : 1;
     constexpr uint32_t kProduct = (1u << 4) | (kFormat << 7) | (kFormat << 10) | (static_cast<uint32_t>(kN >> 3) << 17) | (128u >> 4 << 24);
     extern __shared__ uint8_t smem_raw[];              // units of x, the exchange, the ring
@@ -601,7 +624,7 @@ linear_wide_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     float* const exchange = reinterpret_cast<float*>(smem_raw + (base - smem_u32(smem_raw)) + kXUnits * kXUnit);
-    const uint32_t ring = base + kXUnits * kXUnit + kThreads * kExchange * 4;
+    const uint32_t ring = base + kXUnits * kXUnit + 2 * kThreads * kExchange * 4;
     if (tid == 0) {
         s_failed = 0;
         prefetch_tensormap(&x_map);
@@ -629,25 +652,15 @@ linear_wide_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
-    // columns: operand [tile][group][buffer], then product [tile][group] or [tile][group][buffer]
+    // columns: operand [tile][group][buffer], then product [tile][group][buffer]
     auto operand_at = [&](int which) { return tmem + which * 32; };
-    auto product_at = [&](int tile, int group, int turn) { return tmem + 256 + (tile * 2 + group) * 64 + (kDefer ? (turn & 1) * 32 : 0); };
+    auto product_at = [&](int tile, int group, int turn) { return tmem + 256 + (tile * 2 + group) * 64 + (turn & 1) * 32; };
     const int u0 = min(static_cast<int>(blockIdx.x) * a.share, a.units), count = min(u0 + a.share, a.units) - u0;
     Place here(a, u0);
     int open[2] = {-1, -1};                            // units whose rows are shared with an earlier / a later CTA
     bool ok = true;
     auto wait = [&](uint64_t& bar, int parity) { ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar), parity, a.wait_budget)) && ok; };
     const int row_tile = warp & (kWarps - 1);
-    // acc[r]: output row `lane` of the tile, activation row r
-    auto write = [&](const Place& at, const float (&v)[kN]) {
-        const int o = (at.rb * kWarps + row_tile) * kRowTile + lane;
-        if (o >= a.n) return;
-        const float b = a.bias ? qtz_dev::to_f32(static_cast<const T*>(a.bias)[o]) : 0.f;
-        const int64_t r0 = static_cast<int64_t>(at.pass) * kN;
-#pragma unroll
-        for (int r = 0; r < kN; ++r)
-            if (r0 + r < a.rows) static_cast<T*>(a.y)[(r0 + r) * a.y_stride + o] = qtz_dev::from_f32<T>(v[r] + b);
-    };
     grid_launch_dependents();
 
     if (warp == 2 * kWarps) {
@@ -811,19 +824,13 @@ linear_wide_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__
                         if (q + 2 >= kScales && part == kHands - 1) mbar_arrive(smem_u32(&s_empty[stage]));   // the unit's codes are taken
                     }
                 }
-                if (kDefer) {
-                    if (pending) {
-                        // with two hands to a turn, the second has waited for the turn before already
-                        if (kHands == 1) wait_done(hand - 2);
-                        take(turn - 1);
-                    }
-                    scale = scale_here;
-                    pending = true;
-                } else {
-                    scale = scale_here;
-                    wait_done(hand - 1);
-                    take(turn);
+                if (pending) {
+                    // with two hands to a turn, the second has waited for the turn before already
+                    if (kHands == 1) wait_done(hand - 2);
+                    take(turn - 1);
                 }
+                scale = scale_here;
+                pending = true;
             }
             if (++stage == a.stages) {
                 stage = 0;
@@ -836,28 +843,31 @@ linear_wide_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__
                     take(turn - 1);
                     pending = false;
                 }
+                // group 0 takes the first half of the activation rows, group 1 the second
+                float sum[kN / 2];
 #pragma unroll
-                for (int r0 = 0; r0 < kN; r0 += kExchange) {
-                    if (group == 1)
+                for (int r0 = 0; r0 < kN / 2; r0 += kExchange) {
 #pragma unroll
-                        for (int r = 0; r < kExchange; ++r) exchange[(row_tile * kExchange + r) * 32 + lane] = acc[r0 + r];
+                    for (int r = 0; r < kExchange; ++r)
+                        exchange[(group * kExchange + r) * kThreads + row_tile * 32 + lane] = group ? acc[r0 + r] : acc[kN / 2 + r0 + r];
                     named_barrier(1, 2 * kThreads);
-                    if (group == 0)
 #pragma unroll
-                        for (int r = 0; r < kExchange; ++r) acc[r0 + r] += exchange[(row_tile * kExchange + r) * 32 + lane];
+                    for (int r = 0; r < kExchange; ++r)
+                        sum[r0 + r] = (group ? acc[kN / 2 + r0 + r] : acc[r0 + r]) + exchange[((1 - group) * kExchange + r) * kThreads + row_tile * 32 + lane];
                     named_barrier(1, 2 * kThreads);
                 }
                 const bool begins = i >= here.kb;
                 if (begins && ends) {
-                    if (group == 0 && work) write(here, acc);
+                    const int o = (here.rb * kWarps + row_tile) * kRowTile + lane;
+                    const float b = bias_of<T>(a, o);
+#pragma unroll
+                    for (int r = 0; r < kN / 2; ++r) put<T>(a, static_cast<int64_t>(here.pass) * kN + group * (kN / 2) + r, o, sum[r] + b);
                 } else {
                     if (begins) open[1] = u0 + i;
                     else open[0] = u0 + i;
-                    if (group == 0) {
-                        float* part = part_of<kN>(a, row_tile, lane, blockIdx.x, begins ? 1 : 0);
+                    float* const part = part_of<kN>(a, blockIdx.x, begins ? 1 : 0) + group * (kN / 2) * kThreads + row_tile * 32 + lane;
 #pragma unroll
-                        for (int r = 0; r < kN; ++r) part[r * 32] = acc[r];
-                    }
+                    for (int r = 0; r < kN / 2; ++r) part[r * kThreads] = sum[r];
                 }
 #pragma unroll
                 for (int r = 0; r < kN; ++r) acc[r] = 0.f;
@@ -875,7 +885,7 @@ linear_wide_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }
-    join_rows<kN>(a, warp, lane, open, s_failed, s_last, write);
+    join_rows<T, kN, 2 * kThreads>(a, open, s_failed, s_last);
 }
 
 // ctas: of an SM; fixed: shared memory beside the rings; most_parts: that a row block is cut into
@@ -909,7 +919,7 @@ qtz_status launch_digits(qtz_linear* p, LinearArgs& a, bool zero, cudaStream_t s
 template <typename T, int kN>
 qtz_status launch_wide(qtz_linear* p, LinearArgs& a, bool zero, cudaStream_t st)
 {
-    constexpr int kFixed = 1024 + kXUnitsOf<kN> * (kKBlock / 64) * kN * 128 + kThreads * kExchange * 4;
+    constexpr int kFixed = 1024 + kXUnits * (kKBlock / 64) * kN * 128 + 2 * kThreads * kExchange * 4;
     CUtensorMap x_map;                                 // bytes: columns beyond k and rows beyond the last read as zero
     const uint64_t dims[2] = {2 * static_cast<uint64_t>(a.k), static_cast<uint64_t>(a.rows)}, strides[1] = {2 * static_cast<uint64_t>(a.x_stride)};
     const uint32_t box[2] = {128, kN};
@@ -923,19 +933,22 @@ qtz_status launch_wide(qtz_linear* p, LinearArgs& a, bool zero, cudaStream_t st)
 template <typename T>
 qtz_status launch_rows(qtz_linear* p, LinearArgs& a, bool zero, cudaStream_t st)
 {
+    // us at 1, 2, 4, 5, 8 | 9, 16 | 17, 32 rows: 24.9, 26.5, 32.2, 38.0, 42.2 | 40.7, 41.1 | 41.7, 42.7 through 28672 x 8192, groups of
+    // 128; 7.6, 7.7, 8.7, 9.8, 10.5 | 10.1, 10.7 | 11.9, 13.1 through 4096 x 4096, groups of 32.  With the wide kernel from 5 rows on
+    // 40.6 to 40.7 and 9.9 to 10.1: even on average.  More than 32 rows take several passes over the weights, which then lie in L2:
+    // 64 rows at once left no second buffer for the products (69.9 us against 30.3 for two passes through 5003 x 10001).
     if (a.rows <= 2) return launch_digits<T, 1>(p, a, zero, st);
     if (a.rows <= 4) return launch_digits<T, 2>(p, a, zero, st);
     if (a.rows <= 8) return launch_digits<T, 3>(p, a, zero, st);
     if (a.rows <= 16) return launch_wide<T, 16>(p, a, zero, st);
-    if (a.rows <= 32) return launch_wide<T, 32>(p, a, zero, st);
-    return launch_wide<T, 64>(p, a, zero, st);
+    return launch_wide<T, 32>(p, a, zero, st);
 }
 
 // Scratch of the joining, shared by the layers of a handle: parts and counters of a full grid.
 qtz_status ensure_scratch(qtz_ctx* h, cudaStream_t st)
 {
     if (h->linear_dev) return QTZ_OK;
-    const int ctas = 2 * h->num_sms;                   // of up to eight rows; half as many with eight times the rows
+    const int ctas = 2 * h->num_sms;                   // of up to eight rows; half as many with four times the rows
     const size_t parts = static_cast<size_t>(h->num_sms) * 2 * kWarps * kRowTile * kMaxTokens * sizeof(float);
     QTZ_CUDA(h, cudaMalloc(&h->linear_dev, parts + ctas * sizeof(int32_t)));
     QTZ_CUDA(h, cudaMemsetAsync(static_cast<uint8_t*>(h->linear_dev) + parts, 0, ctas * sizeof(int32_t), st));
@@ -1017,10 +1030,10 @@ extern "C" qtz_status qtz_linear_w4(qtz_linear_plan p, const void* x_dev, int64_
     if (!x_dev || !y_dev || x_stride < p->d.k || y_stride < p->d.n) return QTZ_ERR_INVALID_ARG;
     if (!qtz_aligned16(x_dev) || x_stride % 8 != 0) return QTZ_ERR_MISALIGNED;
     const int row_blocks = (p->row_tiles + kWarps - 1) / kWarps;
-    const int64_t passes = rows <= kMaxTokens ? 1 : (rows + kMaxTokens - 1) / kMaxTokens;
+    const int64_t passes = (rows + kMaxTokens - 1) / kMaxTokens;
     if (passes * row_blocks * p->k_blocks > 0x3fffffff) return QTZ_ERR_TOO_LARGE;
     qtz_device_guard guard(p->h->device);
-    LinearArgs a{p->blocks, x_dev, x_stride, rows, p->bias, y_dev, y_stride, p->d.n, p->d.k, p->row_tiles, p->k_blocks, row_blocks,
+    LinearArgs a{p->blocks, x_dev, x_stride, rows, p->bias, y_dev, y_stride, p->d.n, p->d.k, p->row_tiles, p->k_blocks, static_cast<int32_t>(passes),
                  static_cast<int32_t>(passes * row_blocks * p->k_blocks), 0, p->scales, p->block_bytes, 0, static_cast<float*>(p->h->linear_dev),
                  p->h->linear_counters, p->h->wait_budget, p->h->status_dev};
     const bool zero = p->d.wdtype == QTZ_U4_PACKED;
