@@ -108,7 +108,8 @@ QTZ_API const char* qtz_status_string(qtz_status s);
 QTZ_API const char* qtz_last_error(qtz_handle h);
 /* Status word written by device code: 0; QTZ_ERR_DEVICE_TIMEOUT from a bounded wait that gave up; or
  * QTZ_ERR_INVALID_ARG from a serving call that met a slot or block id outside its cache (and skipped
- * it: site id 10 append, 11 read, 12 attention).  *site_id tells which place.  Synchronises `stream`. */
+ * it: site id 10 append, 11 read, 12 attention).  *site_id tells which place.  Synchronises `stream`.
+ * After a timeout, results of later calls are void until this call has reported it.                 */
 QTZ_API qtz_status qtz_last_device_status(qtz_handle h, int32_t* site_id, void* stream);
 
 /* Cycle budget of every bounded device-side wait of later launches through this handle (default
@@ -483,7 +484,8 @@ typedef struct {
     int32_t ftype;  /* QTZ_F16 or QTZ_BF16: type of x, y, scales and bias     */
 } qtz_linear_desc;
 /* One-time preparation: copies codes, scales, zero points and bias into the order the kernel reads.  BLOCKS until
- * `stream` has finished; the caller may then free or overwrite all inputs.                                       */
+ * `stream` has finished; the caller may then free or overwrite all inputs.  The first layer of a handle makes the
+ * handle allocate scratch that its layers share (10 MB): like all calls of a handle, on one stream at a time.        */
 QTZ_API qtz_status qtz_linear_create(qtz_handle h, const qtz_linear_desc* desc, const void* codes_dev, const void* scales_dev,
                                      const uint8_t* zeros_dev, const void* bias_dev, qtz_linear_plan* out, void* stream);
 QTZ_API qtz_status qtz_linear_destroy(qtz_linear_plan p);

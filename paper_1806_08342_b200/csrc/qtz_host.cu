@@ -84,6 +84,8 @@ extern "C" qtz_status qtz_last_device_status(qtz_handle h, int32_t* site_id, voi
     if (site_id) *site_id = host[1];
     if (host[0] != 0) {
         QTZ_CUDA(h, cudaMemsetAsync(h->status_dev, 0, sizeof(host), st));
+        // a linear layer that gave up may have left its parts counted
+        if (h->linear_counters) QTZ_CUDA(h, cudaMemsetAsync(h->linear_counters, 0, 2 * h->num_sms * sizeof(int32_t), st));
         return host[0];
     }
     return QTZ_OK;
