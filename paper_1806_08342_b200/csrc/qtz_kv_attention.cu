@@ -61,15 +61,16 @@ struct AttnArgs {
     int64_t y_token_stride, y_head_stride;
     float* lse;
     int32_t* counters;                     // [CTAs][2] arrivals of parts at a group, [CTAs] of groups at an item (see the joining)
-    float* parts;                          // [CTAs][2][kMaxRows * D + 2 kMaxRows]: sums, maxima, denominators
+    float* parts;                          // [CTAs][2][kMaxRows * D + 4 kMaxRows]: sums, maxima, denominators; those of the joined group
     int32_t stages, box_shift;             // tokens of a box: 1 << box_shift
     int64_t wait_budget;
     int32_t* status;
 };
 
-// The sequence is dealt out by cost: a tile counts two units and the end of an item one (measured at 128 columns and 5 rows:
-// 1.4 us a tile with both CTAs of an SM at work, 0.7 us for the last sums, the output row and the refill behind them).
-constexpr int kTileUnits = 2, kItemUnits = 1;
+// The sequence is dealt out by cost: a tile counts two units and the end of an item five, for the last sums, the output rows, the
+// next queries and the refill behind them.  us with 1, 3, 5, 8 units: 168, 161, 161, 161 for 64 requests of 300 to 32768 tokens, 8
+// key/value heads, 128 columns; 87, 75, 71, 71 for 256 of 100 to 1000; 35.3 to 35.1 for 8 of 4000 to 16000.
+constexpr int kTileUnits = 2, kItemUnits = 5;
 
 struct RequestShape {
     int first, added;                      // rows of q
@@ -232,7 +233,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
     constexpr int kColumns = kN == 48 ? 64 : kN;       // of tensor memory: two buffers of S, two of each half of O
     constexpr int kTmemColumns = (2 + 2 * kHalves) * kColumns <= 64 ? 64 : (2 + 2 * kHalves) * kColumns <= 128 ? 128 :
                                  (2 + 2 * kHalves) * kColumns <= 256 ? 256 : 512;
-    constexpr int kPart = kMaxRows * D + 2 * kMaxRows;
+    constexpr int kPart = kMaxRows * D + 4 * kMaxRows;
     constexpr uint32_t kMulK = (2u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(kN >> 3) << 17) | (static_cast<uint32_t>(kTile >> 4) << 24);
     constexpr uint32_t kMulV = (2u << 4) | (1u << 7) | (0u << 10) | (1u << 15) | (static_cast<uint32_t>(kN >> 3) << 17) | (128u >> 4 << 24);
 
@@ -442,9 +443,12 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         };
         multiply_keys(0, cur);
         for (int i = 0; i < count && ok; ++i) {
+            // A new item's queries come after this tile's weights: its S may not keep O waiting.
+            bool fresh = false;
             if (i + 1 < count) {
                 cur.next(a, prefix, known);
-                multiply_keys(i + 1, cur);
+                fresh = cur.k == 0;
+                if (!fresh) multiply_keys(i + 1, cur);
             }
             ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.pfull[i & 1]), (i >> 1) & 1, a.wait_budget));
             if (!ok) break;
@@ -461,6 +465,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                 mma_commit(smem_u32(&sh.empty[i % a.stages]));
             }
             __syncwarp();
+            if (fresh) multiply_keys(i + 1, cur);
         }
         if (!ok) {                                     // what was issued may still run: give it the same limit, then go
             timed_out();
@@ -769,8 +774,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
     }
 
     tc_fence_before();
-    __threadfence();                                   // the parts, before they are counted
-    __syncthreads();
+    __syncthreads();                                   // the parts, before they are counted
     if (warp == kComputeWarps + 1) {
         tc_fence_after();
         tmem_dealloc(tmem, kTmemColumns);
@@ -791,7 +795,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         const OpenItem& open = sh.open[warp];
         const int size = group_size(open.c1 - open.c0 + 1), first = me - (me - open.c0) % size, others = min(size - 1, open.c1 - first);
         int32_t* counter = a.counters + 2 * first + (first == open.c0 ? 1 : 0);
-        sh.last[warp] = atomicAdd(counter, 1) == others;
+        sh.last[warp] = arrive_acq_rel(counter) == others;
         if (sh.last[warp]) *counter = 0;               // ready for the next call
     }
     __syncthreads();
@@ -799,43 +803,69 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
     const bool both = sh.open[0].c1 >= 0 && sh.last[0] && sh.open[1].c1 >= 0 && sh.last[1];
     const int crew = both ? kThreads / 2 : kThreads, slot = both ? tid / crew : sh.open[1].c1 >= 0 && sh.last[1] ? 1 : 0, ht = tid % crew;
     const OpenItem& open = sh.open[slot];
-    float (*const jm)[kMaxRows] = reinterpret_cast<float (*)[kMaxRows]>(smem + slot * 8192), (*const jl)[kMaxRows] = jm + kFanIn, (*const jw)[kMaxRows] = jl + kFanIn;
-    float* const j_top = reinterpret_cast<float*>(jw + kFanIn), * const j_sum = j_top + kMaxRows;
     auto sync_crew = [&]() { named_barrier(2 + slot, crew); };
     if (open.c1 >= 0 && sh.last[slot]) {
-        __threadfence();
         const int c0 = open.c0, c1 = open.c1, size = group_size(c1 - c0 + 1), groups = (c1 - c0) / size + 1, first = me - (me - c0) % size;
         auto part_of = [&](int cta) { return a.parts + (static_cast<int64_t>(cta) * 2 + (cta == c0 ? 1 : 0)) * kPart; };
         constexpr int kQuads = kRows * D / 4;          // four neighbouring values of a row
-        // Weighted sums over n parts, kFlight parts of kAtOnce quads in flight: a part comes from L2 in half a microsecond.
-        auto add_up = [&](auto flight, auto at_once, int from, int step, int n, float* to) {
-            constexpr int kFlight = decltype(flight)::value, kAtOnce = decltype(at_once)::value;
+        constexpr int kOwn = kMaxRows * D, kJoined = kOwn + 2 * kMaxRows;
+        // Joins n parts, those of CTAs from, from + step, ..: into `to`, or into the output.  Each thread finds the weights of the rows
+        // that it adds up itself: all loads of a round are under way together, and nothing is waited for in between.
+        constexpr int kUp = (kQuads + kThreads - 1) / kThreads, kAtOnce = kUp < 4 ? kUp : 4, kFlight = 18 / kAtOnce;
+        auto join = [&](int from, int step, int n, int scalars, float* to) {
+#pragma unroll 1
             for (int q0 = ht; q0 < kQuads; q0 += kAtOnce * crew) {
                 float4 v[kAtOnce];
+                float top[kAtOnce], sum[kAtOnce];
                 int quad[kAtOnce];
 #pragma unroll
                 for (int j = 0; j < kAtOnce; ++j) {
                     v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    top[j] = -INFINITY;
+                    sum[j] = 0.f;
                     quad[j] = min(q0 + j * crew, kQuads - 1);
                 }
+#pragma unroll 1
                 for (int x0 = 0; x0 < n; x0 += kFlight) {
                     float4 p[kAtOnce][kFlight];
+                    float pm[kAtOnce][kFlight], pl[kAtOnce][kFlight];
 #pragma unroll
-                    for (int x = 0; x < kFlight; ++x)
+                    for (int x = 0; x < kFlight; ++x) {
+                        const float* part = part_of(from + (x0 + x) * step);
 #pragma unroll
-                        for (int j = 0; j < kAtOnce; ++j)
-                            if (x0 + x < n) p[j][x] = __ldcg(reinterpret_cast<const float4*>(part_of(from + (x0 + x) * step)) + quad[j]);
-#pragma unroll
-                    for (int x = 0; x < kFlight; ++x)
-#pragma unroll
-                        for (int j = 0; j < kAtOnce; ++j)
+                        for (int j = 0; j < kAtOnce; ++j) {
+                            p[j][x] = make_float4(0.f, 0.f, 0.f, 0.f);
+                            pm[j][x] = -INFINITY;
+                            pl[j][x] = 0.f;
                             if (x0 + x < n) {
-                                const float w = jw[x0 + x][quad[j] / (D / 4)];
-                                v[j].x = fmaf(p[j][x].x, w, v[j].x);
-                                v[j].y = fmaf(p[j][x].y, w, v[j].y);
-                                v[j].z = fmaf(p[j][x].z, w, v[j].z);
-                                v[j].w = fmaf(p[j][x].w, w, v[j].w);
+                                p[j][x] = __ldcg(reinterpret_cast<const float4*>(part) + quad[j]);
+                                pm[j][x] = __ldcg(part + scalars + quad[j] / (D / 4));
+                                pl[j][x] = __ldcg(part + scalars + kMaxRows + quad[j] / (D / 4));
                             }
+                        }
+                    }
+#pragma unroll
+                    for (int j = 0; j < kAtOnce; ++j) {
+                        float t = top[j];
+#pragma unroll
+                        for (int x = 0; x < kFlight; ++x) t = fmaxf(t, pm[j][x]);
+                        const float keep = top[j] == t ? 1.f : ex2(top[j] - t);
+                        top[j] = t;
+                        sum[j] *= keep;
+                        v[j].x *= keep;
+                        v[j].y *= keep;
+                        v[j].z *= keep;
+                        v[j].w *= keep;
+#pragma unroll
+                        for (int x = 0; x < kFlight; ++x) {
+                            const float w = pm[j][x] == -INFINITY && pl[j][x] == 0.f ? 0.f : ex2(pm[j][x] - (t == -INFINITY ? 0.f : t));
+                            sum[j] = fmaf(pl[j][x], w, sum[j]);
+                            v[j].x = fmaf(p[j][x].x, w, v[j].x);
+                            v[j].y = fmaf(p[j][x].y, w, v[j].y);
+                            v[j].z = fmaf(p[j][x].z, w, v[j].z);
+                            v[j].w = fmaf(p[j][x].w, w, v[j].w);
+                        }
+                    }
                 }
 #pragma unroll
                 for (int j = 0; j < kAtOnce; ++j) {
@@ -843,61 +873,31 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                     const int r = quad[j] / (D / 4), d = quad[j] % (D / 4) * 4;
                     if (to) {
                         *reinterpret_cast<float4*>(to + r * D + d) = v[j];
-                        if (d == 0) {
-                            to[kMaxRows * D + r] = j_top[r];
-                            to[kMaxRows * D + kMaxRows + r] = j_sum[r];
+                        if (d == 0) {                  // beside those that other threads still read
+                            to[kJoined + r] = top[j];
+                            to[kJoined + kMaxRows + r] = sum[j];
                         }
                     } else if (open.out[r] >= 0) {
-                        const float sum = j_sum[r], inv = sum == 0.f ? 0.f : __fdiv_rn(1.f, sum);
+                        const float inv = sum[j] == 0.f ? 0.f : __fdiv_rn(1.f, sum[j]);
                         uint2 o;
                         o.x = qtz_dev::pack2(v[j].x * inv, v[j].y * inv, T());
                         o.y = qtz_dev::pack2(v[j].z * inv, v[j].w * inv, T());
                         *reinterpret_cast<uint2*>(static_cast<T*>(a.y) + open.out[r] + d) = o;
-                        if (d == 0 && a.lse) a.lse[open.lse[r]] = sum == 0.f ? -INFINITY : (j_top[r] + log2f(sum)) * 0.693147181f;
+                        if (d == 0 && a.lse) a.lse[open.lse[r]] = sum[j] == 0.f ? -INFINITY : (top[j] + log2f(sum[j])) * 0.693147181f;
                     }
                 }
             }
         };
-        // Joins the n parts of CTAs from, from + step, ..: into `to`, or into the output.
-        auto join = [&](int from, int step, int n, float* to) {
-            for (int i = ht; i < n * kMaxRows; i += crew) {
-                const float* p = part_of(from + i / kMaxRows * step) + kMaxRows * D + i % kMaxRows;
-                jm[i / kMaxRows][i % kMaxRows] = __ldcg(p);
-                jl[i / kMaxRows][i % kMaxRows] = __ldcg(p + kMaxRows);
-            }
-            sync_crew();
-            for (int i = ht; i < n * kMaxRows; i += crew) {
-                const int j = i / kMaxRows, r = i % kMaxRows;
-                float top = -INFINITY;
-                for (int x = 0; x < n; ++x) top = fmaxf(top, jm[x][r]);
-                const float mj = jm[j][r], lj = jl[j][r];
-                jw[j][r] = mj == -INFINITY && lj == 0.f ? 0.f : ex2(mj - (top == -INFINITY ? 0.f : top));
-                if (j == 0) j_top[r] = top;
-            }
-            sync_crew();
-            if (ht < kMaxRows) {
-                float sum = 0.f;
-                for (int x = 0; x < n; ++x) sum = fmaf(jl[x][ht], jw[x][ht], sum);
-                j_sum[ht] = sum;
-            }
-            sync_crew();
-            if (n <= 4) add_up(std::integral_constant<int, 4>(), std::integral_constant<int, 4>(), from, step, n, to);
-            else add_up(std::integral_constant<int, 9>(), std::integral_constant<int, 2>(), from, step, n, to);
-        };
-        join(first, 1, min(size, c1 - first + 1), groups > 1 ? part_of(first) : nullptr);
+        join(first, 1, min(size, c1 - first + 1), kOwn, groups > 1 ? part_of(first) : nullptr);
         if (groups > 1) {
-            __threadfence();
             sync_crew();
             if (ht == 0) {
                 int32_t* counter = a.counters + 2 * gridDim.x + c0;
-                sh.last[slot] = atomicAdd(counter, 1) == groups - 1;
+                sh.last[slot] = arrive_acq_rel(counter) == groups - 1;
                 if (sh.last[slot]) *counter = 0;
             }
             sync_crew();
-            if (sh.last[slot]) {
-                __threadfence();
-                join(c0, size, groups, nullptr);
-            }
+            if (sh.last[slot]) join(c0, size, groups, kJoined, nullptr);
         }
     }
 }
@@ -939,7 +939,7 @@ extern "C" int64_t qtz_kv_attention_workspace_bytes(qtz_handle h, const qtz_kv_c
 {
     if (!h || qtz_kv_check(cache) != QTZ_OK) return 0;
     const int d = cache->head_dim;
-    return counters_bytes(h, d) + static_cast<int64_t>(h->num_sms) * ctas_per_sm(d) * 2 * (kMaxRows * d + 2 * kMaxRows) * 4;
+    return counters_bytes(h, d) + static_cast<int64_t>(h->num_sms) * ctas_per_sm(d) * 2 * (kMaxRows * d + 4 * kMaxRows) * 4;
 }
 
 extern "C" qtz_status qtz_kv_attention(qtz_handle h, const qtz_kv_cache* cache, const void* q_dev, int64_t q_token_stride,
@@ -959,11 +959,12 @@ extern "C" qtz_status qtz_kv_attention(qtz_handle h, const qtz_kv_cache* cache, 
     if (!qtz_aligned16(q_dev) || !qtz_aligned16(y_dev) || !qtz_aligned16(workspace_dev) ||
         (q_token_stride | q_head_stride | y_token_stride | y_head_stride) % 8 != 0)
         return QTZ_ERR_MISALIGNED;
-    // rows of the cache and tiles of the longest possible step are counted in 32 bits
+    // rows of the cache and units of the longest possible step are counted in 32 bits
     const int64_t rows = static_cast<int64_t>(cache->blocks) * cache->kv_heads * cache->block_tokens;
     const int64_t reach = static_cast<int64_t>(table_width) * cache->block_tokens, group = q_heads / cache->kv_heads;
-    const double bound = static_cast<double>(cache->kv_heads) * static_cast<double>(reach / kTile + 1) * (static_cast<double>(tokens) * group / 5 + requests);
-    if (rows > 0x7fffffff || reach > 0x7fffffff || 3.0 * bound > 2.0e9) return QTZ_ERR_TOO_LARGE;
+    const double items = static_cast<double>(cache->kv_heads) * (static_cast<double>(tokens) * group / 5 + requests);
+    const double units = items * (kTileUnits * static_cast<double>(reach / kTile + 1) + kItemUnits);
+    if (rows > 0x7fffffff || reach > 0x7fffffff || units > 2.0e9) return QTZ_ERR_TOO_LARGE;
     qtz_device_guard guard(h->device);
     int box_shift = 4;                         // the largest box that divides both a block and a tile
     while ((1 << box_shift) < kTile && cache->block_tokens % (2 << box_shift) == 0) ++box_shift;

@@ -304,13 +304,12 @@ __device__ __forceinline__ void join_rows(const LinearArgs& a, const int (&open)
 {
     constexpr int kQuads = kWarps * kRowTile / 4, kAtOnce = (kRows * kQuads + kJoin - 1) / kJoin, kFlight = 16 / kAtOnce;
     const int tid = threadIdx.x;
-    __threadfence();
     __syncthreads();
     if (failed || tid >= kJoin) return;                // after a wait that gave up the results are void
     auto first = [&](int unit) { return unit / a.k_blocks * a.k_blocks; };
     if ((tid == 0 && open[0] >= 0) || (tid == 32 && open[1] >= 0)) {
         const int begin = first(tid ? open[1] : open[0]), c0 = begin / a.share;
-        const bool all = atomicAdd(a.counters + c0, 1) == (begin + a.k_blocks - 1) / a.share - c0;
+        const bool all = arrive_acq_rel(a.counters + c0) == (begin + a.k_blocks - 1) / a.share - c0;
         last[tid ? 1 : 0] = all;
         if (all) a.counters[c0] = 0;                   // ready for the next call
     }
@@ -319,7 +318,6 @@ __device__ __forceinline__ void join_rows(const LinearArgs& a, const int (&open)
     for (int which = 0; which < 2; ++which) {
         const int unit = which ? open[1] : open[0];
         if (unit < 0 || !last[which]) continue;
-        __threadfence();
         const Place at(a, unit);
         const int c0 = first(unit) / a.share, c1 = (first(unit) + a.k_blocks - 1) / a.share;
         const int64_t r0 = static_cast<int64_t>(at.pass) * kRows;

@@ -91,6 +91,15 @@ __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commi
 template <int kPending>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kPending) : "memory"); }
 
+// Counts the arrival of a CTA whose threads have met at a barrier: what they wrote is seen by the threads that meet after a later
+// arrival that returns this one's count or more.
+__device__ __forceinline__ int arrive_acq_rel(int32_t* counter)
+{
+    int v;
+    asm volatile("atom.add.acq_rel.gpu.global.s32 %0, [%1], 1;" : "=r"(v) : "l"(counter) : "memory");
+    return v;
+}
+
 // Four bytes; cp_async_arrive makes an mbarrier count one arrival once this thread's copies so far have landed.
 __device__ __forceinline__ void cp_async_4(uint32_t dst, const void* src)
 {
