@@ -22,6 +22,9 @@
 // lengths.  A producer warp streams a CTA's share through a ring of TMA boxes, several tiles ahead and across items.  Items
 // that lie in more than one share are joined by the last CTA to arrive, in the order of the tiles, so that results do not
 // depend on timing.
+// Measured: 64 requests of 300 to 32768 tokens, 8 heads of 128, 4 query heads each: 161 us for 1.03 GB, 6.4 TB/s, 0.99 of the copy
+// rate.  One request over 262143 tokens, 4 heads: 54.7 us for 268 MB, 4.9 TB/s: 6 us until the first tile, 8 for the two joins.  16
+// requests with 5 new tokens and a window of 1024: 21.8 us for 24 MB, four tiles a CTA: all of it start, first use and joins.
 #include <cuda.h>
 
 #include <type_traits>
@@ -924,7 +927,9 @@ template <typename T, int D>
 qtz_status launch_rows(qtz_ctx* h, AttnArgs& a, const CUtensorMap& km, const CUtensorMap& vm, cudaStream_t st)
 {
     // Query rows of a (request, key/value head) if all requests bring equally many tokens: the smallest tile that takes them
-    // reads the cache once; larger ones only compute unused columns.
+    // reads the cache once; larger ones only compute unused columns.  4 rows, 64 requests up to 32768 tokens: 161 us with 5 rows a tile,
+    // 230 with 16.  8 rows, 16 requests of 1000 to 8000: 37 with 10, 51 with 5, 50 with 16.  16 rows, 64 of 300 to 3000: 81 with 16, 128
+    // with 5.
     const int64_t rows = a.group * ((static_cast<int64_t>(a.tokens) + a.requests - 1) / a.requests);
     if (rows <= 5) return launch<T, D, 5>(h, a, km, vm, st);
     if (rows <= 10) return launch<T, D, 10>(h, a, km, vm, st);
