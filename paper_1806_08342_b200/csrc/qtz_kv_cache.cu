@@ -143,8 +143,10 @@ schedule_kernel(const __grid_constant__ ScheduleArgs a)
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxWindow = 256;
-// Tokens that one warp takes; longer runs take the CTA (192 single tokens appended and read: 10.5 us against 18.9 with CTAs alone).
-constexpr int kShortRun = 4;
+// Pieces (8 values) that a lane holds of a run that its warp takes, and the most that it takes; longer runs take the CTA.  Appending 7000
+// prompt tokens (8 heads of 128) takes 23 us in blocks of 16, a run of 8 pieces, and 33 if a warp takes 4 at most; in blocks of 32
+// 24, and 41 if it takes 16.  192 single tokens appended and read: 10.5 us, 18.9 with CTAs alone.
+constexpr int kWarpHeld = 4, kWarpPieces = 8;
 constexpr int kHeld = 4;                      // 16-byte pieces of a long run that a thread keeps in registers: 64 tokens of 128 values
 
 struct AppendArgs {
@@ -331,23 +333,24 @@ append_kernel(const __grid_constant__ AppendArgs a)
             more = more && len < static_cast<int>(block);
         }
         if (lane == 0) s_len[k] = len;
-        if (len > kShortRun) {
+        if (len << shift > kWarpPieces * 32) {
             long_runs = true;
             continue;
         }
         float* scale;
         int8_t* codes;
         place(b, scale, codes);
-        const int offset = static_cast<int>(slot - first), count = len << shift;     // at most 4 * 32
-        uint4 v[kShortRun];
+        const int offset = static_cast<int>(slot - first), count = len << shift;
+        uint4 v[kWarpHeld];
         float top = 0.f;
 #pragma unroll
-        for (int q = 0; q < kShortRun; ++q) {
+        for (int q = 0; q < kWarpHeld; ++q) {
             v[q] = make_uint4(0, 0, 0, 0);
             if (q * 32 + lane < count) v[q] = value(j, q * 32 + lane);
         }
 #pragma unroll
-        for (int q = 0; q < kShortRun; ++q) top = max_abs8<T>(v[q], top);
+        for (int q = 0; q < kWarpHeld; ++q) top = max_abs8<T>(v[q], top);
+        for (int p = kWarpHeld * 32 + lane; p < count; p += 32) top = max_abs8<T>(value(j, p), top);   // read again below
         top = redux_max(top);
         float ratio;
         const float s = new_scale(top, scale, offset, ratio), r = __frcp_rn(s);
@@ -356,16 +359,18 @@ append_kernel(const __grid_constant__ AppendArgs a)
         if (ratio != 1.f)
             for (int p = lane; p < offset * dim / 16; p += 32) reinterpret_cast<uint4*>(codes)[p] = rescale16(reinterpret_cast<uint4*>(codes)[p], ratio);
 #pragma unroll
-        for (int q = 0; q < kShortRun; ++q) {
+        for (int q = 0; q < kWarpHeld; ++q) {
             const int p = q * 32 + lane;
             if (p < count) *reinterpret_cast<uint2*>(codes + target(j, p, first)) = quantize8<T>(v[q], s, r);
         }
+        for (int p = kWarpHeld * 32 + lane; p < count; p += 32)
+            *reinterpret_cast<uint2*>(codes + target(j, p, first)) = quantize8<T>(value(j, p), s, r);
     }
     if (!__syncthreads_or(long_runs)) return;
     int turn = 0;
     for (int k = 0; k < runs; ++k) {
         const int len = s_len[k];
-        if (len <= kShortRun) continue;
+        if (len << shift <= kWarpPieces * 32) continue;
         const int j = s_start[k];
         const int64_t slot = s_slot[j + 1];
         const uint32_t b = block_of(slot, block);
@@ -515,9 +520,9 @@ extern "C" qtz_status qtz_kv_append(qtz_handle h, const qtz_kv_cache* cache, con
     if (!qtz_aligned16(k_dev) || !qtz_aligned16(v_dev) || (k_token_stride | k_head_stride | v_token_stride | v_head_stride) % 8 != 0)
         return QTZ_ERR_MISALIGNED;
     qtz_device_guard guard(h->device);
-    // About 16 CTAs an SM, each with at least a token for every warp.  With the smallest window throughout, prompts of 10 800 tokens
-    // take 73 us, read-back included, against 43; with the largest, 192 single tokens take 39 against 10.5.
-    int64_t window = tokens * 2 * cache->kv_heads / (16 * h->num_sms);
+    // About 8 CTAs an SM, each with at least a token for every warp.  Prompts of 10 800 tokens, read-back included: 43 us, with 4 CTAs an SM
+    // 46, with the smallest window throughout 73.  192 single tokens: 10.5, with the largest window 39.
+    int64_t window = (tokens * 2 * cache->kv_heads + 8 * h->num_sms - 1) / (8 * h->num_sms);
     window = window < kWarps ? kWarps : window > kMaxWindow ? kMaxWindow : window;
     const int64_t ctas = (tokens + window - 1) / window;
     if (ctas > 0x7fffffff) return QTZ_ERR_TOO_LARGE;

@@ -144,6 +144,21 @@ def test_append_of_many_tokens(hq):
     codes, scales = check_append(cache, codes, scales, k, v, slots)
 
 
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_append_of_runs_on_either_side_of_what_a_warp_takes(hq, dim):
+    """A lane holds 4 pieces of 8 values and its warp takes 8 at most: runs one token shorter and longer than both, at offset 0 and
+    behind older tokens, side by side."""
+    g = np.random.default_rng(79 + dim)
+    heads, block, most = 2, 64, 256 * 8 // dim
+    lens = [most // 2 - 1, most // 2, most // 2 + 1, most - 1, most, most + 1]
+    cache, codes, scales = random_cache(hq, g, 12, heads, block, dim)
+    order = g.permutation(12)
+    slots = [int(order[2 * i + at]) * block + o for i, n in enumerate(lens) for at, lo in ((0, 0), (1, 3)) for o in range(lo, lo + n)]
+    for _ in range(2):
+        k, v = values(g, torch.float16, len(slots), heads, dim)
+        codes, scales = check_append(cache, codes, scales, k, v, slots)
+
+
 def test_append_of_values_that_are_hard(hq):
     """Zeros, infinities, NaN, the smallest and the largest values, exact ties of the rounding."""
     g = np.random.default_rng(78)
