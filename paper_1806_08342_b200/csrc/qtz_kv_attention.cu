@@ -7,13 +7,14 @@
 // Both products have 8-bit codes on one side, which the tensor cores (kind::i8) read straight from the bytes that TMA
 // brings in: nothing is converted.  The other side is split into base-256 digits, one operand column each:
 //   q_row = 2^(e - 21) (d_2 2^16 + d_1 2^8 + d_0)   e = exponent of the row's largest value, d in [-128, 127]: 22 bits
-//   w_p   = 2^-22 (b_2 2^16 + b_1 2^8 + b_0)        b in [0, 255]; the mantissa of w_p + 2
-// Integer sums are exact; a query loses what lies below 2^-22 of its row's largest value and a weight what lies below
-// 2^-23 of the largest weight, both far less than the output's type.  The sums are joined in fp32.
+//   w_p   = 2^(m' - 31) (b_3 2^24 + b_2 2^16 + b_1 2^8 + b_0)    b in [0, 255]; m' = maximum of t over the tile, not the running one
+// Integer sums are exact; a query loses what lies below 2^-22 of its row's largest value and a weight what lies below 2^-32 of
+// its tile's largest, which is 2^-25 of it for a whole tile.  (Weights count by their sum: with 22 bits below the running maximum
+// a token of large weight and no value took 10^5 others out of y.)  The sums are joined in fp32, a tile's times 2^(m' - m).
 //
 // One tile is 128 tokens of one key/value head against kRows query rows (heads of the group x new tokens):
 //   S^T [128 tokens x 3 kRows] = K [128 x D] Q^T        a thread owns a token: logits, maximum, weights
-//   O^T [D x 3 kRows]          = V^T [D x 128] W        a thread owns a column of the head: fp32 running sum
+//   O^T [D x 4 kRows]          = V^T [D x 128] W        a thread owns a column of the head: fp32 running sum
 // with V read as it lies (the depth of the product along its rows).
 //
 // What bounds it: one token reads 2 D bytes a head for 4 D flops a query head: HBM, by a factor of 4 to 100 over the tensor
@@ -46,7 +47,6 @@ constexpr int kThreads = kComputeThreads + 64;   // + one warp for TMA, one for 
 constexpr int kMaxRows = 16;
 constexpr int kMaxStages = 6;
 constexpr int kMaxBoxes = 8;
-constexpr int kFanIn = 32;                 // most parts that are joined in one step: the square of it covers any grid
 constexpr int kSmemLimit = 227 * 1024;     // most that a CTA may ask for; an SM has 1 KB more, and each CTA costs 1 KB more than it asks for
 
 struct AttnArgs {
@@ -173,6 +173,13 @@ __device__ __forceinline__ float join_digits(uint32_t d0, uint32_t d1, uint32_t 
     return fmaf(static_cast<float>(hi), 256.f, static_cast<float>(static_cast<int>(d0)));
 }
 
+// The four digits' sums over 128 codes, each below 2^22
+__device__ __forceinline__ float join_digits(uint32_t d0, uint32_t d1, uint32_t d2, uint32_t d3)
+{
+    const int hi = static_cast<int>(d3) * 256 + static_cast<int>(d2), lo = static_cast<int>(d1) * 256 + static_cast<int>(d0);
+    return fmaf(static_cast<float>(hi), 65536.f, static_cast<float>(lo));
+}
+
 template <int kN>
 __device__ __forceinline__ void load_columns(uint32_t taddr, uint32_t (&v)[kN])
 {
@@ -214,6 +221,8 @@ struct OpenItem {
 // Shared memory of a CTA beside the ring, the operands and the prefix sums.
 struct Shared {
     float max[2][kComputeWarps][kMaxRows], sum[kMaxRows][kComputeWarps];
+    // of each row, for each warp: the tile's maximum (0 for none), and what the sums so far and the tile's are multiplied by
+    float origin[kComputeWarps][kMaxRows], keep[2][kComputeWarps][kMaxRows], gain[2][kComputeWarps][kMaxRows];
     ItemInfo item[2];
     float2 scales[kMaxStages][kMaxBoxes];  // (k, v) of each box; negative: there is none
     uint64_t full[kMaxStages], empty[kMaxStages], sfull[2], pfull[2], ofull[2], qfull, drain;
@@ -229,22 +238,21 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
 {
     constexpr int kHalves = D > 128 ? 2 : 1;           // boxes along a row of the cache
     constexpr int kRowBytes = D < 128 ? D : 128;
+    constexpr int kN = (3 * kRows + 15) / 16 * 16;     // operand columns of the queries: digit * kRows + row
+    constexpr int kNw = (4 * kRows + 15) / 16 * 16;    // of the weights: 4 row + digit
     constexpr int kRowsUp = (kRows + 3) / 4 * 4;
-    constexpr int kN = (3 * kRows + 15) / 16 * 16;     // operand columns: digit * kRows + row
     constexpr int kBox = kTile * kRowBytes;            // K or V of one tile and half
     constexpr int kStage = 2 * kHalves * kBox;
-    constexpr int kColumns = kN == 48 ? 64 : kN;       // of tensor memory: two buffers of S, two of each half of O
-    constexpr int kTmemColumns = (2 + 2 * kHalves) * kColumns <= 64 ? 64 : (2 + 2 * kHalves) * kColumns <= 128 ? 128 :
-                                 (2 + 2 * kHalves) * kColumns <= 256 ? 256 : 512;
+    constexpr int kColumns = kN == 48 ? 64 : kN, kColumnsO = kNw == 48 ? 64 : kNw;   // of tensor memory: two buffers of S, two of each half of O
+    constexpr int kUsed = 2 * kColumns + 2 * kHalves * kColumnsO, kTmemColumns = kUsed <= 64 ? 64 : kUsed <= 128 ? 128 : kUsed <= 256 ? 256 : 512;
     constexpr int kPart = kMaxRows * D + 4 * kMaxRows;
     constexpr uint32_t kMulK = (2u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(kN >> 3) << 17) | (static_cast<uint32_t>(kTile >> 4) << 24);
-    constexpr uint32_t kMulV = (2u << 4) | (1u << 7) | (0u << 10) | (1u << 15) | (static_cast<uint32_t>(kN >> 3) << 17) | (128u >> 4 << 24);
+    constexpr uint32_t kMulV = (2u << 4) | (1u << 7) | (0u << 10) | (1u << 15) | (static_cast<uint32_t>(kNw >> 3) << 17) | (128u >> 4 << 24);
 
-    extern __shared__ uint8_t smem_raw[];
+    extern __shared__ __align__(1024) uint8_t smem[];  // the swizzle counts from multiples of 1 KB; nothing static lies before it
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    uint8_t* const smem = smem_raw + (base - smem_u32(smem_raw));
-    const uint32_t off_p = a.stages * kStage, off_q = off_p + kN * 128, off_shared = off_q + kN * D, off_prefix = off_shared + (sizeof(Shared) + 15) / 16 * 16;
+    const uint32_t base = smem_u32(smem);
+    const uint32_t off_p = a.stages * kStage, off_q = off_p + kNw * 128, off_shared = off_q + kN * D, off_prefix = off_shared + (sizeof(Shared) + 15) / 16 * 16;
     uint32_t* const prefix = reinterpret_cast<uint32_t*>(smem + off_prefix);
     Shared& sh = *reinterpret_cast<Shared*>(smem + off_shared);
     KnownRequests& known = sh.known;
@@ -462,7 +470,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                 for (int hh = 0; hh < kHalves; ++hh)
 #pragma unroll
                     for (int j = 0; j < kTile / 32; ++j)
-                        mma_i8(tmem + (2 + (i & 1) * kHalves + hh) * kColumns, make_mnmajor_desc(v + hh * kBox + j * 32 * kRowBytes, kRowBytes),
+                        mma_i8(tmem + 2 * kColumns + ((i & 1) * kHalves + hh) * kColumnsO, make_mnmajor_desc(v + hh * kBox + j * 32 * kRowBytes, kRowBytes),
                                make_kmajor_desc(base + off_p, 128) + 2 * j, kMulV, j > 0);
                 mma_commit(smem_u32(&sh.ofull[i & 1]));
                 mma_commit(smem_u32(&sh.empty[i % a.stages]));
@@ -596,14 +604,14 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         fetch_queries(cur);
         convert_queries(cur, 0);
         int items = 0;
-        float m[kRows], l[kRows], acc[kHalves][kRows], keep[kRows];
+        float m = -INFINITY, l[kRows], acc[kHalves][kRows];   // m: of row `lane`
         int seg_first = cur.k, stage = 0, round = 0;
         bool pending = false;                          // O of the tile before is still to be taken
 
         auto reset = [&]() {
+            m = -INFINITY;
 #pragma unroll
             for (int r = 0; r < kRows; ++r) {
-                m[r] = -INFINITY;
                 l[r] = 0.f;
 #pragma unroll
                 for (int hh = 0; hh < kHalves; ++hh) acc[hh][r] = 0.f;
@@ -623,13 +631,21 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
             wait(sh.ofull[i & 1], (i >> 1) & 1);
             tc_fence_after();
 #pragma unroll
-            for (int hh = 0; hh < kHalves; ++hh) {
-                uint32_t o[kN];
-                load_columns<kN>(tmem + (2 + (i & 1) * kHalves + hh) * kColumns + (static_cast<uint32_t>(warp) << 21), o);
+            for (int hh = 0; hh < kHalves; ++hh)
 #pragma unroll
-                for (int r = 0; r < kRows; ++r)
-                    acc[hh][r] = fmaf(acc[hh][r], keep[r], join_digits(o[r], o[kRows + r], o[2 * kRows + r]));
-            }
+                for (int r0 = 0; r0 < kRows; r0 += 4) {
+                    constexpr int kLeft = kRows % 4;
+                    uint32_t o[16];
+                    const uint32_t from = tmem + 2 * kColumns + ((i & 1) * kHalves + hh) * kColumnsO + 4 * r0 + (static_cast<uint32_t>(warp) << 21);
+                    if (kLeft == 1 && r0 + 4 > kRows) tmem_ld_32x4(from, o);
+                    else if (kLeft == 2 && r0 + 4 > kRows) tmem_ld_32x8(from, o);
+                    else tmem_ld_32x16(from, o);
+                    const float4 keep = *reinterpret_cast<const float4*>(&sh.keep[i & 1][warp][r0]), gain = *reinterpret_cast<const float4*>(&sh.gain[i & 1][warp][r0]);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int r = 0; r < 4 && r0 + r < kRows; ++r)
+                        acc[hh][r0 + r] = fmaf(join_digits(o[4 * r], o[4 * r + 1], o[4 * r + 2], o[4 * r + 3]), (&gain.x)[r], acc[hh][r0 + r] * (&keep.x)[r]);
+                }
         };
 
         for (int i = 0; i < count; ++i) {
@@ -677,38 +693,41 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                     *reinterpret_cast<float4*>(&sh.max[i & 1][warp][r]) = make_float4(top[r], top[r + 1], top[r + 2], top[r + 3]);
             ok = named_barrier_and(1, kComputeThreads, ok);
             if (!ok) break;
+            // lane r finds what all threads need of row r
+            if (lane < kRows) {
+                float t = -INFINITY;
 #pragma unroll
-            for (int r = 0; r < kRows; ++r) top[r] = m[r];
-#pragma unroll
-            for (int w = 0; w < kComputeWarps; ++w)
-#pragma unroll
-                for (int r = 0; r < kRowsUp; r += 4) {
-                    const float4 t = *reinterpret_cast<const float4*>(&sh.max[i & 1][w][r]);
-                    top[r] = fmaxf(top[r], t.x);
-                    top[r + 1] = fmaxf(top[r + 1], t.y);
-                    top[r + 2] = fmaxf(top[r + 2], t.z);
-                    top[r + 3] = fmaxf(top[r + 3], t.w);
-                }
+                for (int w = 0; w < kComputeWarps; ++w) t = fmaxf(t, sh.max[i & 1][w][lane]);
+                const float now = fmaxf(m, t), origin = now == -INFINITY ? 0.f : now;   // subtracted from -inf without giving NaN
+                sh.origin[warp][lane] = t == -INFINITY ? 0.f : t;
+                sh.keep[i & 1][warp][lane] = ex2(m - origin);
+                sh.gain[i & 1][warp][lane] = ex2(t - origin);
+                m = now;
+            }
+            __syncwarp();
             // O of the tile before: its product ran beside this tile's logits; after it the weights' place is free
             if (pending) take_sums(i - 1);
             pending = true;
             const float inv = __fdividef(1.f, vs);
             uint32_t bits[kRows];
 #pragma unroll
-            for (int r = 0; r < kRows; ++r) {
-                const float origin = top[r] == -INFINITY ? 0.f : top[r];
-                keep[r] = ex2(m[r] - origin);
-                m[r] = top[r];
-                const float w = ex2(x[r] - origin);
-                l[r] = fmaf(w, inv, l[r] * keep[r]);
-                bits[r] = __float_as_uint(w + 2.f);    // w in [0, 1]: the mantissa is w in units of 2^-22, its bytes are the digits
+            for (int r0 = 0; r0 < kRows; r0 += 4) {
+                const float4 origin = *reinterpret_cast<const float4*>(&sh.origin[warp][r0]), keep = *reinterpret_cast<const float4*>(&sh.keep[i & 1][warp][r0]),
+                             gain = *reinterpret_cast<const float4*>(&sh.gain[i & 1][warp][r0]);
+#pragma unroll
+                for (int j = 0; j < 4 && r0 + j < kRows; ++j) {
+                    const int r = r0 + j;
+                    const float w = ex2(x[r] - (&origin.x)[j]);
+                    l[r] = fmaf(w * (&gain.x)[j], inv, l[r] * (&keep.x)[j]);
+                    bits[r] = __float2uint_rn(w * 2147483648.f);   // units of 2^-31
+                }
             }
             const uint32_t to = base + off_p;
 #pragma unroll
             for (int r = 0; r < kRows; ++r)
 #pragma unroll
-                for (int g = 0; g < 3; ++g) {
-                    const int n = g * kRows + r;
+                for (int g = 0; g < 4; ++g) {
+                    const int n = 4 * r + g;
                     st_shared_u8(to + n * 128 + (((tid >> 4) ^ (n & 7)) << 4) + (tid & 15), bits[r] >> (8 * g));
                 }
             tc_fence_before();
@@ -736,20 +755,20 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
 #pragma unroll
                 for (int r = 0; r < kRows; ++r) {
                     const float4 t = *reinterpret_cast<const float4*>(sh.sum[r]);
-                    const float sum = (t.x + t.y) + (t.z + t.w);
+                    const float sum = (t.x + t.y) + (t.z + t.w), top = __shfl_sync(0xffffffffu, m, r);
                     float v[kHalves];
 #pragma unroll
-                    for (int hh = 0; hh < kHalves; ++hh) v[hh] = acc[hh][r] * 2.384185791015625e-07f;   // 2^-22
+                    for (int hh = 0; hh < kHalves; ++hh) v[hh] = acc[hh][r] * 4.656612873077393e-10f;   // 2^-31
                     if (D >= 128 || tid < D) {
                         if (whole) {
-                            write_row(it, r, m[r], sum, v, tid);
+                            write_row(it, r, top, sum, v, tid);
                         } else {
 #pragma unroll
                             for (int hh = 0; hh < kHalves; ++hh) part[r * D + hh * 128 + tid] = v[hh];
                         }
                     }
                     if (!whole && tid == 0) {
-                        part[kMaxRows * D + r] = m[r];
+                        part[kMaxRows * D + r] = top;
                         part[kMaxRows * D + kMaxRows + r] = sum;
                     }
                 }
@@ -789,7 +808,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
     // joined: the results are void, and the counters have to be cleared.)
     if (sh.failed) return;
     const int me = static_cast<int>(blockIdx.x);
-    auto group_size = [](int n) {                      // about the square root: both steps join at most kFanIn parts
+    auto group_size = [](int n) {                      // about the square root: both steps join about equally many parts
         int g = 4;
         while (g * g < n) ++g;
         return n <= 8 ? n : g;
@@ -910,9 +929,9 @@ int ctas_per_sm(int head_dim) { return head_dim == 256 ? 1 : 2; }
 template <typename T, int D, int kRows>
 qtz_status launch(qtz_ctx* h, AttnArgs& a, const CUtensorMap& km, const CUtensorMap& vm, cudaStream_t st)
 {
-    constexpr int kN = (3 * kRows + 15) / 16 * 16, kStage = 2 * kTile * D;
+    constexpr int kN = (3 * kRows + 15) / 16 * 16, kNw = (4 * kRows + 15) / 16 * 16, kStage = 2 * kTile * D;
     const int ctas = ctas_per_sm(D);
-    const int fixed = 1024 + kN * 128 + kN * D + static_cast<int>((sizeof(Shared) + 15) / 16 * 16 + sizeof(uint32_t) * (a.requests + 1));
+    const int fixed = kNw * 128 + kN * D + static_cast<int>((sizeof(Shared) + 15) / 16 * 16 + sizeof(uint32_t) * (a.requests + 1));
     const int room = (kSmemLimit + 1024) / ctas - 1024 - fixed;
     a.stages = room / kStage < kMaxStages ? room / kStage : kMaxStages;
     if (a.stages < 2) return QTZ_ERR_TOO_LARGE;
@@ -927,12 +946,15 @@ template <typename T, int D>
 qtz_status launch_rows(qtz_ctx* h, AttnArgs& a, const CUtensorMap& km, const CUtensorMap& vm, cudaStream_t st)
 {
     // Query rows of a (request, key/value head) if all requests bring equally many tokens: the smallest tile that takes them
-    // reads the cache once; larger ones only compute unused columns.  4 rows, 64 requests up to 32768 tokens: 161 us with 5 rows a tile,
-    // 230 with 16.  8 rows, 16 requests of 1000 to 8000: 37 with 10, 51 with 5, 50 with 16.  16 rows, 64 of 300 to 3000: 81 with 16, 128
-    // with 5.
+    // reads the cache once; larger ones only compute unused columns.  16 requests of 1000 to 8000 tokens, us: 4 rows 34.5; 5 rows 35.4
+    // in a tile of 5, 36.6 in one of 8 (heads of 64: 28.4, 32.0); 8 rows 36.7; 10 rows 38.1 in a tile of 10, 40.5 in one of 12, 48.7 in one
+    // of 16; 12 rows 40.4 in a tile of 12, 48.9 in one of 16; 16 rows 49.3.
     const int64_t rows = a.group * ((static_cast<int64_t>(a.tokens) + a.requests - 1) / a.requests);
+    if (rows <= 4) return launch<T, D, 4>(h, a, km, vm, st);
     if (rows <= 5) return launch<T, D, 5>(h, a, km, vm, st);
+    if (rows <= 8) return launch<T, D, 8>(h, a, km, vm, st);
     if (rows <= 10) return launch<T, D, 10>(h, a, km, vm, st);
+    if (rows <= 12) return launch<T, D, 12>(h, a, km, vm, st);
     return launch<T, D, 16>(h, a, km, vm, st);
 }
 
