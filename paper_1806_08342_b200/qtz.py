@@ -736,7 +736,9 @@ class KvCache:
         self._desc = KvCacheDesc(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), *k.shape)
         self._ref = byref(self._desc)
         self.device, self.lib, self.h, self.scale = handle.device, handle.lib, handle.h, self.head_dim ** -0.5
-        self.workspace = None
+        # zero-filled here, not by the first call of attention(), whose fill a graph that captures it would keep for itself
+        size = self.lib.qtz_kv_attention_workspace_bytes(self.h, self._ref)
+        self.workspace = torch.zeros(max(size, 16), dtype=torch.uint8, device=k.device)
 
     def append(self, k, v, slots):
         """Quantizes new keys and values [tokens][kv_heads][head_dim] (any token and head stride) into `slots`."""
@@ -778,9 +780,6 @@ class KvCache:
             _check_on(dev, dtype, out)
             if out.shape != shape or out.stride(2) != 1:
                 raise ValueError("out has another shape")
-        if self.workspace is None:
-            size = self.lib.qtz_kv_attention_workspace_bytes(self.h, self._ref)
-            self.workspace = torch.zeros(max(size, 16), dtype=torch.uint8, device=q.device)
         lse = q.new_empty(shape[:2], dtype=torch.float32) if return_lse else None
         ys = out.stride()
         rc = self.lib.qtz_kv_attention(self.h, self._ref, q.data_ptr(), qs[0], qs[1], shape[1], FTYPES[dtype], starts.data_ptr(), lens.data_ptr(), b,

@@ -1,0 +1,51 @@
+"""How the attention over the 8-bit cache is called: captures, stored scales, wide tables, strides of single rows."""
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import hq  # noqa: F401
+from paper_1806_08342_b200 import qtz
+
+pytestmark = pytest.mark.gpu
+
+
+def ints(values, dtype=torch.int32):
+    return torch.tensor(values, dtype=dtype, device="cuda")
+
+
+def make(hq, seed, lens, added, kv_heads, group, dim, block, dtype=torch.bfloat16):
+    """(cache, codes, scales, q, starts, lens, table) with everything on the device but codes and scales."""
+    g = np.random.default_rng(seed)
+    need = [-(-v // block) for v in lens]
+    blocks = sum(need) + 1
+    codes = [g.integers(-127, 128, (blocks, kv_heads, block, dim)).astype(np.int8) for _ in range(2)]
+    scales = [g.uniform(0.005, 0.03, (blocks, kv_heads)).astype(np.float32) for _ in range(2)]
+    table, at = np.zeros((len(lens), max(need)), np.int32), 0
+    for r, n in enumerate(need):
+        table[r, :n] = np.arange(at, at + n)
+        at += n
+    starts = np.concatenate(([0], np.cumsum(added)))
+    q = torch.from_numpy(g.normal(size=(int(starts[-1]), kv_heads * group, dim))).to(dtype)
+    cache = qtz.KvCache(hq, *(torch.from_numpy(c).cuda() for c in codes), *(torch.from_numpy(s).cuda() for s in scales))
+    return cache, codes, scales, q.cuda(), ints(starts.tolist()), ints(lens), torch.from_numpy(table).cuda()
+
+
+def test_first_call_of_a_cache_inside_a_capture(hq):
+    """What a call needs is there before it is captured: a plain call before the first replay gives the same as after it, even if the
+    memory that the capture is given holds something."""
+    cache, codes, scales, q, starts, lens, table = make(hq, 1, [9000, 4100], [1, 1], 2, 4, 128, 32)
+    want = qtz.KvCache(hq, cache.k, cache.v, cache.k_scale, cache.v_scale).attention(q, starts, lens, table)
+    pool, junk, graph, out = torch.cuda.graph_pool_handle(), torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph(), torch.zeros_like(q)
+    with torch.cuda.graph(junk, pool=pool):
+        held = [torch.full((8 << 20,), 77, dtype=torch.int32, device="cuda") for _ in range(2)]
+    junk.replay()
+    torch.cuda.synchronize()
+    del held                                                                # the pool hands this memory out again
+    with torch.cuda.graph(graph, pool=pool):
+        cache.attention(q, starts, lens, table, out=out)
+    for _ in range(3):
+        assert torch.equal(cache.attention(q, starts, lens, table), want)
+    for _ in range(2):
+        graph.replay()
+        assert torch.equal(out, want)
+        assert torch.equal(cache.attention(q, starts, lens, table), want)
