@@ -106,10 +106,12 @@ QTZ_API qtz_status qtz_destroy(qtz_handle h);
 QTZ_API const char* qtz_status_string(qtz_status s);
 /* Text of the last CUDA error seen through this handle ("" if none).  Host only.          */
 QTZ_API const char* qtz_last_error(qtz_handle h);
-/* Status word written by device code: 0; QTZ_ERR_DEVICE_TIMEOUT from a bounded wait that gave up; or
+/* What device code has recorded: 0; QTZ_ERR_DEVICE_TIMEOUT from a bounded wait that gave up; or
  * QTZ_ERR_INVALID_ARG from a serving call that met a slot or block id outside its cache (and skipped
  * it: site id 10 append, 11 read, 12 attention).  *site_id tells which place.  Synchronises `stream`.
- * After a timeout, results of later calls are void until this call has reported it.                 */
+ * The first of each kind is kept; a timeout is reported first, an id by the next call.  A report is
+ * cleared by reading it.  After a timeout, results of later calls are void until this call has
+ * reported it and, for attention, until the workspace is zero-filled again.                         */
 QTZ_API qtz_status qtz_last_device_status(qtz_handle h, int32_t* site_id, void* stream);
 
 /* Cycle budget of every bounded device-side wait of later launches through this handle (default
@@ -551,7 +553,8 @@ QTZ_API qtz_status qtz_kv_read(qtz_handle h, const qtz_kv_cache* cache, const in
  *   lse     NULL, or [tokens][q_heads] fp32: natural logarithm of the softmax's sum, for joining with other keys
  *   tokens  rows of q and y
  *   workspace  qtz_kv_attention_workspace_bytes(h, cache) bytes, 16-byte aligned, zero-filled once before its first use;
- *           one stream at a time.  Its size does not depend on lengths.  After QTZ_ERR_DEVICE_TIMEOUT zero it again.
+ *           one stream at a time.  Its size does not depend on lengths.  After QTZ_ERR_DEVICE_TIMEOUT zero it again, once
+ *           qtz_last_device_status has reported it.
  * Codes meet fixed-point queries and weights in exact integer sums: a query keeps 22 bits below its row's largest value, a
  * softmax weight 31 bits below the largest of its 128 tokens (both rounded to nearest); every other sum, maximum and statistic is fp32.  A query row that
  * holds NaN or an infinity gives NaN.

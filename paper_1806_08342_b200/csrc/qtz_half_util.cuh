@@ -35,10 +35,11 @@ __device__ __forceinline__ uint32_t pack2(float a, float b, __nv_bfloat16)
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// Records the first misuse that device code met (an id outside its cache).
+// Records the first misuse that device code met (an id outside its cache), beside the pair of words that timeouts are recorded in:
+// neither hides the other.
 __device__ __forceinline__ void report_invalid(int32_t* status, int site)
 {
-    if (atomicCAS(status, 0, QTZ_ERR_INVALID_ARG) == 0) status[1] = site;
+    if (atomicCAS(status + 2, 0, QTZ_ERR_INVALID_ARG) == 0) status[3] = site;
 }
 
 }  // namespace qtz_dev

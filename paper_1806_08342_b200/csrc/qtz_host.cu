@@ -40,8 +40,8 @@ extern "C" qtz_status qtz_create(qtz_handle* out, int device)
     if (const char* v = std::getenv("QTZ_SINGLE_ROW_STEMS")) h->single_row_stems = v[0] == '1';
     cudaError_t e = cudaSetDevice(device);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&h->num_sms, cudaDevAttrMultiProcessorCount, device);
-    if (e == cudaSuccess) e = cudaMalloc(&h->status_dev, 2 * sizeof(int32_t));
-    if (e == cudaSuccess) e = cudaMemset(h->status_dev, 0, 2 * sizeof(int32_t));
+    if (e == cudaSuccess) e = cudaMalloc(&h->status_dev, 4 * sizeof(int32_t));
+    if (e == cudaSuccess) e = cudaMemset(h->status_dev, 0, 4 * sizeof(int32_t));
     if (e != cudaSuccess) {
         (void)cudaGetLastError();
         delete h;
@@ -77,18 +77,16 @@ extern "C" const char* qtz_last_error(qtz_handle h) { return h ? h->last_error.c
 extern "C" qtz_status qtz_last_device_status(qtz_handle h, int32_t* site_id, void* stream)
 {
     if (!h) return QTZ_ERR_INVALID_ARG;
-    int32_t host[2] = {0, 0};
+    int32_t host[4] = {0, 0, 0, 0};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     QTZ_CUDA(h, cudaMemcpyAsync(host, h->status_dev, sizeof(host), cudaMemcpyDeviceToHost, st));
     QTZ_CUDA(h, cudaStreamSynchronize(st));
-    if (site_id) *site_id = host[1];
-    if (host[0] != 0) {
-        QTZ_CUDA(h, cudaMemsetAsync(h->status_dev, 0, sizeof(host), st));
-        // a linear layer that gave up may have left its parts counted
-        if (h->linear_counters) QTZ_CUDA(h, cudaMemsetAsync(h->linear_counters, 0, 2 * h->num_sms * sizeof(int32_t), st));
-        return host[0];
-    }
-    return QTZ_OK;
+    const int at = host[0] != 0 ? 0 : 2;
+    if (site_id) *site_id = host[at + 1];
+    if (host[at] != 0) QTZ_CUDA(h, cudaMemsetAsync(h->status_dev + at, 0, 2 * sizeof(int32_t), st));
+    // a linear layer that gave up may have left its parts counted
+    if (host[0] != 0 && h->linear_counters) QTZ_CUDA(h, cudaMemsetAsync(h->linear_counters, 0, 2 * h->num_sms * sizeof(int32_t), st));
+    return host[at];
 }
 
 qtz_status qtz_ensure_params(qtz_ctx* h, size_t bytes)

@@ -22,7 +22,7 @@ struct qtz_ctx {
     size_t params_bytes = 0;
     float* reduce_dev = nullptr;
     size_t reduce_bytes = 0;
-    int32_t* status_dev = nullptr;
+    int32_t* status_dev = nullptr;          // (status, site) of the first timeout, then of the first id outside a cache
     float* reduce_host = nullptr;  // pinned
     size_t reduce_host_bytes = 0;
     void* linear_dev = nullptr;             // parts and counters of linear layers (allocated with the first layer)
