@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import weakref
 from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_float, c_int32, c_int64, c_void_p
 
 import numpy as np
@@ -22,6 +23,7 @@ W_S8_PER_CHANNEL_SYM, W_U8_PER_LAYER_ASYM, W_S4_PACKED_PER_CHANNEL_SYM = 0, 1, 2
 OUT_U8, OUT_S32_RAW = 0, 1
 ACT_NONE, ACT_RELU, ACT_RELU6 = 0, 1, 2
 F32, F16, BF16 = 16, 17, 18
+DEVICE_TIMEOUT = -7
 FTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
 
 QPARAMS = np.dtype([("scale", "<f4"), ("zero_point", "<i4"), ("min_nudged", "<f4"), ("max_nudged", "<f4")])
@@ -306,6 +308,7 @@ class Handle:
         self.lib = load_library()
         self.h = c_void_p()
         self.device = device
+        self._caches = weakref.WeakSet()
         rc = self.lib.qtz_create(byref(self.h), device)
         if rc:
             raise QtzError(rc, "qtz_create", self.lib.qtz_status_string(rc).decode())
@@ -329,8 +332,13 @@ class Handle:
             raise QtzError(rc, what, detail)
 
     def device_status(self):
+        """(status, site) of what device code has recorded, (0, 0) for nothing.  After a timeout the workspaces of this handle's
+        caches are made ready for the next call."""
         site = c_int32()
         rc = self.lib.qtz_last_device_status(self.h, byref(site), _stream())
+        if rc == DEVICE_TIMEOUT:
+            for cache in list(self._caches):
+                cache.reset_workspace()
         return rc, site.value
 
     def set_wait_budget(self, cycles):
@@ -739,6 +747,12 @@ class KvCache:
         # zero-filled here, not by the first call of attention(), whose fill a graph that captures it would keep for itself
         size = self.lib.qtz_kv_attention_workspace_bytes(self.h, self._ref)
         self.workspace = torch.zeros(max(size, 16), dtype=torch.uint8, device=k.device)
+        handle._caches.add(self)
+
+    def reset_workspace(self):
+        """Zero-fills the workspace of attention() on the current stream: a call that gave up may have left parts counted in it.
+        Handle.device_status() does so when it reports a timeout."""
+        self.workspace.zero_()
 
     def append(self, k, v, slots):
         """Quantizes new keys and values [tokens][kv_heads][head_dim] (any token and head stride) into `slots`."""

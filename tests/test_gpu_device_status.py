@@ -1,4 +1,4 @@
-"""What device code records and the host reads: neither kind of report hides the other."""
+"""What device code records and the host reads: neither kind of report hides the other, and what a caller does after a timeout."""
 import pytest
 import torch
 
@@ -30,3 +30,25 @@ def test_a_timeout_is_reported_over_an_id_outside_the_cache(handle):
     cache.read(outside)                                                # the first of the skipped ones is kept
     assert handle.device_status() == (-1, 10)
     assert handle.device_status() == (0, 0)
+
+
+def test_attention_after_a_reported_timeout(handle):
+    """A call that gave up leaves parts counted in the workspace of its cache: reporting the timeout makes it ready again."""
+    g = torch.Generator("cuda").manual_seed(3)
+    cache = handle.kv_cache(600, 1, 16, 64)
+    cache.k.random_(-127, 128, generator=g)
+    cache.v.random_(-127, 128, generator=g)
+    cache.k_scale.fill_(0.02)
+    cache.v_scale.fill_(0.02)
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
+    q = torch.randn(1, 4, 64, device="cuda", generator=g).bfloat16()
+    call = lambda: cache.attention(q, ints(0, 1), ints(9000), torch.arange(600, dtype=torch.int32, device="cuda")[None])  # noqa: E731
+    want = call()
+    assert bool(want.any())
+    cache.workspace.fill_(1)                                           # as a call would leave it that gave up on the way
+    handle.selftest_wait_timeout(20000)
+    assert handle.device_status() == (-7, 8)
+    assert torch.equal(call(), want)
+    cache.workspace.fill_(1)
+    cache.reset_workspace()
+    assert torch.equal(call(), want)
