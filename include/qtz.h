@@ -116,7 +116,8 @@ QTZ_API qtz_status qtz_last_device_status(qtz_handle h, int32_t* site_id, void* 
 
 /* Cycle budget of every bounded device-side wait of later launches through this handle (default
  * 2e9, about one second of SM clocks; at least 1000).  When a wait runs out the kernel records
- * QTZ_ERR_DEVICE_TIMEOUT and returns; qtz_last_device_status reports it.                        */
+ * QTZ_ERR_DEVICE_TIMEOUT and returns; qtz_last_device_status reports it.  The serving kernels first
+ * wait, up to 2e9 cycles whatever the budget, for the copies and products that they have under way. */
 QTZ_API qtz_status qtz_set_wait_budget(qtz_handle h, int64_t cycles);
 /* Self-test of that mechanism: launches one small CTA that waits, for at most budget_cycles
  * (1 .. 1e8), on a barrier nothing ever signals.  The wait gives up by itself and the kernel

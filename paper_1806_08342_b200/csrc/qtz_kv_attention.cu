@@ -427,7 +427,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         }
         // nothing may be in flight when the CTA ends
         for (int j = max(0, i - a.stages); j < i; ++j)
-            if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.full[j % a.stages]), (j / a.stages) & 1, a.wait_budget))) timed_out();
+            if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.full[j % a.stages]), (j / a.stages) & 1, kDrainBudget))) timed_out();
     } else if (count > 0 && warp == kComputeWarps + 1) {
         // ======== matrix instructions: S of the next tile is issued before O of this one ========
         int items = 0;
@@ -478,12 +478,10 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
             __syncwarp();
             if (fresh) multiply_keys(i + 1, cur);
         }
-        if (!ok) {                                     // what was issued may still run: give it the same limit, then go
-            timed_out();
-            if (elect_one()) mma_commit(smem_u32(&sh.drain));
-            __syncwarp();
-            mbar_wait(smem_u32(&sh.drain), 0, a.wait_budget);
-        }
+        if (!ok) timed_out();
+        if (elect_one()) mma_commit(smem_u32(&sh.drain));   // the compute warps may have given up on what is still running
+        __syncwarp();
+        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&sh.drain), 0, kDrainBudget))) timed_out();
     } else if (count > 0) {
         // ======== compute: thread = token of S^T, then column of O^T ========
         bool ok = true;

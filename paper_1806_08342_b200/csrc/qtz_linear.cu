@@ -252,16 +252,23 @@ struct Stream {
         ahead.next(a);
         ++issued;
     }
-    // After a wait that gave up nothing more is issued, but what is in flight is still waited for (with the same limit).
-    __device__ __forceinline__ bool wait() const
+    __device__ __forceinline__ bool wait() const { return __all_sync(0xffffffffu, mbar_wait(smem_u32(&full[stage]), phase, a.wait_budget)); }
+    // After a wait that gave up: nothing may be in flight when the CTA ends.
+    __device__ __forceinline__ void drain()
     {
-        return unit - u0 >= issued || __all_sync(0xffffffffu, mbar_wait(smem_u32(&full[stage]), phase, a.wait_budget));
+        for (int j = unit - u0; j < issued; ++j) {
+            __all_sync(0xffffffffu, mbar_wait(smem_u32(&full[stage]), phase, kDrainBudget));
+            if (++stage == a.stages) {
+                stage = 0;
+                phase ^= 1;
+            }
+        }
     }
     __device__ __forceinline__ uint32_t block() const { return ring + stage * a.block_bytes; }
-    __device__ __forceinline__ void release(bool ok)
+    __device__ __forceinline__ void release()
     {
         __syncwarp();                                  // every lane has read the stage
-        if (ok && issued < u1 - u0) issue(stage);
+        if (issued < u1 - u0) issue(stage);
         if (++stage == a.stages) {
             stage = 0;
             phase ^= 1;
@@ -454,7 +461,7 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
                 d[2] |= static_cast<uint64_t>(d2 & 0xff) << at;
             }
             if (round > 0)                             // the buffer's unit before has been used by all warps
-                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_free[buffer]), (round - 1) & 1, a.wait_budget)) && ok;
+                ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_free[buffer]), (round - 1) & 1, a.wait_budget));
 #pragma unroll
             for (int j = 0; j < 3; ++j) {              // columns 4 t .. and 16 + 4 t .. of 32 lie side by side
                 uint8_t* const row = &to.operand[digit_column<kTiles>(j, r)][(lane >> 2) * 32 + (lane & 1) * 16 + (lane & 2) * 2];
@@ -482,9 +489,10 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
     int buffer = 0, round = 0, buffer_next = 1 % kDigitBuffers, round_next = 0;
     for (; s.unit < s.u1; s.next()) {
         if (s.unit + 1 < s.u1) convert(s.unit + 1 - s.u0, s.ends() ? 0 : s.here.kb + 1, buffer_next, round_next);
-        ok = s.wait() && ok;
-        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_ready[buffer]), round & 1, a.wait_budget)) && ok;
-        if (ok && s.has_rows()) {
+        ok = ok && s.wait();
+        ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_ready[buffer]), round & 1, a.wait_budget));
+        if (!ok) break;
+        if (s.has_rows()) {
             const uint32_t block = s.block(), scales = block + kCodeBytes, zeros = scales + 8 / kSteps * kRowTile * 2;
             const Digits<kTiles>& dg = digits[buffer];
             const uint32_t operand = smem_u32(&dg.operand[g][8 * t4]);
@@ -549,7 +557,7 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&s_free[buffer]));
-        s.release(ok);
+        s.release();
         buffer = buffer_next;
         round = round_next;
         if (++buffer_next == kDigitBuffers) {
@@ -595,6 +603,7 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
     if (!ok) {
         timed_out(a);
         s_failed = 1;
+        s.drain();
     }
     join_rows<T, 8, kThreads>(a, open, s_failed, s_last);
 }
@@ -711,8 +720,9 @@ linear_wide_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__
             }
         }
         // nothing may be in flight when the CTA ends
-        for (int j = max(0, xi - kXUnits); j < xi; ++j) wait(s_xfull[j % kXUnits], (j / kXUnits) & 1);
-        for (int j = max(0, issued - a.stages); j < issued; ++j) wait(s_full[j % a.stages], (j / a.stages) & 1);
+        auto drain = [&](uint64_t& bar, int parity) { ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar), parity, kDrainBudget)) && ok; };
+        for (int j = max(0, xi - kXUnits); j < xi; ++j) drain(s_xfull[j % kXUnits], (j / kXUnits) & 1);
+        for (int j = max(0, issued - a.stages); j < issued; ++j) drain(s_full[j % a.stages], (j / a.stages) & 1);
     } else if (warp > 2 * kWarps) {
         // ======== products of a group ========
         const int group = __shfl_sync(0xffffffffu, warp - 2 * kWarps - 1, 0);
@@ -754,11 +764,9 @@ linear_wide_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__
                 ++x_round;
             }
         }
-        if (!ok) {                                     // what was issued may still run: give it the same limit, then go
-            if (elect_one()) mma_commit(smem_u32(&s_drain[group]));
-            __syncwarp();
-            mbar_wait(smem_u32(&s_drain[group]), 0, a.wait_budget);
-        }
+        if (elect_one()) mma_commit(smem_u32(&s_drain[group]));   // the operands' warps may have given up on what is still running
+        __syncwarp();
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_drain[group]), 0, kDrainBudget)) && ok;
     } else {
         // ======== operands, then sums ========
         const int group = warp / kWarps, tile = row_tile >> 2;

@@ -64,6 +64,10 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, long lo
     return true;
 }
 
+// Limit, in cycles, of the waits for a CTA's own copies and products before it ends: apart from the budget of the other waits, which a
+// caller may set to very little, because shared and tensor memory must not go to the next CTA while something is on its way there.
+constexpr long long kDrainBudget = 2000000000LL;
+
 // True in exactly one lane of a converged warp (the same lane every time).
 __device__ __forceinline__ bool elect_one()
 {
