@@ -486,7 +486,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
         // ======== compute: thread = token of S^T, then column of O^T ========
         bool ok = true;
         auto wait = [&](uint64_t& bar, int parity) {   // the warp goes on together
-            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar), parity, a.wait_budget)) && ok;
+            ok = mbar_wait_warp(smem_u32(&bar), parity, a.wait_budget, ok);
         };
         // An item's query rows: warp w takes rows w, w + 4, ..  They are fetched a tile before they become the digits of the
         // operand, which is when the products of the item before are done with its rows.

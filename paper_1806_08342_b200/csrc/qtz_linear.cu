@@ -252,23 +252,22 @@ struct Stream {
         ahead.next(a);
         ++issued;
     }
-    __device__ __forceinline__ bool wait() const { return __all_sync(0xffffffffu, mbar_wait(smem_u32(&full[stage]), phase, a.wait_budget)); }
-    // After a wait that gave up: nothing may be in flight when the CTA ends.
-    __device__ __forceinline__ void drain()
+    // After a wait that gave up nothing more is issued.
+    __device__ __forceinline__ bool wait(bool ok) const
     {
-        for (int j = unit - u0; j < issued; ++j) {
-            __all_sync(0xffffffffu, mbar_wait(smem_u32(&full[stage]), phase, kDrainBudget));
-            if (++stage == a.stages) {
-                stage = 0;
-                phase ^= 1;
-            }
-        }
+        return unit - u0 >= issued ? ok : mbar_wait_warp(smem_u32(&full[stage]), phase, a.wait_budget, ok);
+    }
+    // After one that gave up: nothing may be in flight when the CTA ends.
+    __device__ __forceinline__ void drain() const
+    {
+        for (int j = max(0, issued - a.stages); j < issued; ++j)
+            __all_sync(0xffffffffu, mbar_wait(smem_u32(&full[j % a.stages]), (j / a.stages) & 1, kDrainBudget));
     }
     __device__ __forceinline__ uint32_t block() const { return ring + stage * a.block_bytes; }
-    __device__ __forceinline__ void release()
+    __device__ __forceinline__ void release(bool ok)
     {
         __syncwarp();                                  // every lane has read the stage
-        if (issued < u1 - u0) issue(stage);
+        if (ok && issued < u1 - u0) issue(stage);
         if (++stage == a.stages) {
             stage = 0;
             phase ^= 1;
@@ -461,7 +460,7 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
                 d[2] |= static_cast<uint64_t>(d2 & 0xff) << at;
             }
             if (round > 0)                             // the buffer's unit before has been used by all warps
-                ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_free[buffer]), (round - 1) & 1, a.wait_budget));
+                ok = mbar_wait_warp(smem_u32(&s_free[buffer]), (round - 1) & 1, a.wait_budget, ok);
 #pragma unroll
             for (int j = 0; j < 3; ++j) {              // columns 4 t .. and 16 + 4 t .. of 32 lie side by side
                 uint8_t* const row = &to.operand[digit_column<kTiles>(j, r)][(lane >> 2) * 32 + (lane & 1) * 16 + (lane & 2) * 2];
@@ -489,10 +488,9 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
     int buffer = 0, round = 0, buffer_next = 1 % kDigitBuffers, round_next = 0;
     for (; s.unit < s.u1; s.next()) {
         if (s.unit + 1 < s.u1) convert(s.unit + 1 - s.u0, s.ends() ? 0 : s.here.kb + 1, buffer_next, round_next);
-        ok = ok && s.wait();
-        ok = ok && __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_ready[buffer]), round & 1, a.wait_budget));
-        if (!ok) break;
-        if (s.has_rows()) {
+        ok = s.wait(ok);
+        ok = mbar_wait_warp(smem_u32(&s_ready[buffer]), round & 1, a.wait_budget, ok);
+        if (ok && s.has_rows()) {
             const uint32_t block = s.block(), scales = block + kCodeBytes, zeros = scales + 8 / kSteps * kRowTile * 2;
             const Digits<kTiles>& dg = digits[buffer];
             const uint32_t operand = smem_u32(&dg.operand[g][8 * t4]);
@@ -557,7 +555,7 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&s_free[buffer]));
-        s.release();
+        s.release(ok);
         buffer = buffer_next;
         round = round_next;
         if (++buffer_next == kDigitBuffers) {
@@ -669,7 +667,7 @@ linear_wide_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__
     Place here(a, u0);
     int open[2] = {-1, -1};                            // units whose rows are shared with an earlier / a later CTA
     bool ok = true;
-    auto wait = [&](uint64_t& bar, int parity) { ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar), parity, a.wait_budget)) && ok; };
+    auto wait = [&](uint64_t& bar, int parity) { ok = mbar_wait_warp(smem_u32(&bar), parity, a.wait_budget, ok); };
     const int row_tile = warp & (kWarps - 1);
     grid_launch_dependents();
 

@@ -68,6 +68,16 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, long lo
 // caller may set to very little, because shared and tensor memory must not go to the next CTA while something is on its way there.
 constexpr long long kDrainBudget = 2000000000LL;
 
+// A warp's wait, with what its lanes agree on: false as soon as one of its waits, this or an earlier one (`ok` false), has given up.
+// After one that gave up there is a single poll and no limit to sit out again.  Asked behind the poll: a branch before it cost
+// the linear layers 2 %.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, long long budget, bool ok)
+{
+    bool done = mbar_try_wait(bar, parity);
+    if (!done && ok) done = mbar_wait(bar, parity, budget);
+    return __all_sync(0xffffffffu, done) && ok;
+}
+
 // True in exactly one lane of a converged warp (the same lane every time).
 __device__ __forceinline__ bool elect_one()
 {
