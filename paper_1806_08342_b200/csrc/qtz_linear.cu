@@ -428,7 +428,8 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
             const uint16_t* x = static_cast<const uint16_t*>(a.x) + r * a.x_stride + kb * kKBlock + 8 * lane;
             const int have = a.k - kb * kKBlock - 8 * lane;
             uint4 raw = make_uint4(0, 0, 0, 0);
-            if (have > 0) raw = __ldg(reinterpret_cast<const uint4*>(x));
+            // an ordinary load: the call before may have written x while this CTA was up already
+            if (have > 0) raw = *reinterpret_cast<const uint4*>(x);
             const uint32_t words[4] = {raw.x, raw.y, raw.z, raw.w};
             float v[8], top = 0.f;
             bool odd = false;
