@@ -504,7 +504,8 @@ QTZ_API qtz_status qtz_linear_w4(qtz_linear_plan p, const void* x_dev, int64_t x
  * per block and key/value head: the real value is code * scale.  Position p of a request lies in block
  * table[request][p / block_tokens] at offset p % block_tokens; its slot is block * block_tokens + offset.
  *   k, v          [blocks][kv_heads][block_tokens][head_dim], 16-byte aligned
- *   k_scale, v_scale [blocks][kv_heads]; scales are at least 2^-100 (an all-zero block; smaller ones count as 2^-100)
+ *   k_scale, v_scale [blocks][kv_heads]; scales are at least 2^-100 (an all-zero block; smaller ones and NaN count as
+ *                 2^-100, for attention larger ones than 2^122 as that: append writes at most 2^121)
  *   head_dim      64, 128 or 256;  block_tokens a multiple of 16, at most 256                                  */
 typedef struct {
     int8_t* k_dev;

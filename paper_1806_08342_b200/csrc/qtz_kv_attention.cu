@@ -47,6 +47,7 @@ constexpr int kThreads = kComputeThreads + 64;   // + one warp for TMA, one for 
 constexpr int kMaxRows = 16;
 constexpr int kMaxStages = 6;
 constexpr int kMaxBoxes = 8;
+constexpr uint32_t kNoBox = 0xffffffffu;   // in the place of a scale: a NaN that no arithmetic gives
 constexpr int kSmemLimit = 227 * 1024;     // most that a CTA may ask for; an SM has 1 KB more, and each CTA costs 1 KB more than it asks for
 
 struct AttnArgs {
@@ -224,7 +225,7 @@ struct Shared {
     // of each row, for each warp: the tile's maximum (0 for none), and what the sums so far and the tile's are multiplied by
     float origin[kComputeWarps][kMaxRows], keep[2][kComputeWarps][kMaxRows], gain[2][kComputeWarps][kMaxRows];
     ItemInfo item[2];
-    float2 scales[kMaxStages][kMaxBoxes];  // (k, v) of each box; negative: there is none
+    float2 scales[kMaxStages][kMaxBoxes];  // (k, v) of each box; kNoBox: there is none
     uint64_t full[kMaxStages], empty[kMaxStages], sfull[2], pfull[2], ofull[2], qfull, drain;
     KnownRequests known;
     OpenItem open[2];                      // begun in an earlier CTA; going on in the next
@@ -405,7 +406,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                 break;
             }
             const uint32_t bar = smem_u32(&sh.full[stage]), dst = base + stage * kStage;
-            if (lane < kMaxBoxes && row < 0) sh.scales[stage][lane] = make_float2(-1.f, -1.f);
+            if (lane < kMaxBoxes && row < 0) sh.scales[stage][lane] = make_float2(__uint_as_float(kNoBox), 0.f);
             const int have = __popc(__ballot_sync(0xffffffffu, row >= 0));
             __syncwarp();
             if (lane == 0) mbar_arrive_expect_tx(bar, have * box_rows * 2 * D);
@@ -674,7 +675,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                 for (int r = 0; r < kRows; ++r)
                     x[r] = fmaf(join_digits(s[r], s[kRows + r], s[2 * kRows + r]), it.factor[r] * ks, lv);
             }
-            if (scales.x < 0.f) {
+            if (__float_as_uint(scales.x) == kNoBox) {
 #pragma unroll
                 for (int r = 0; r < kRows; ++r) x[r] = -INFINITY;
             } else if (pos0 < it.full_lo || pos0 + kTile > it.full_hi) {

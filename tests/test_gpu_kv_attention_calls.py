@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from gpu_util import hq  # noqa: F401
+from oracle import serving
 from paper_1806_08342_b200 import qtz
 
 pytestmark = pytest.mark.gpu
@@ -49,3 +50,16 @@ def test_first_call_of_a_cache_inside_a_capture(hq):
         graph.replay()
         assert torch.equal(out, want)
         assert torch.equal(cache.attention(q, starts, lens, table), want)
+
+
+def test_stored_scales_below_the_least_one_count_as_it(hq):
+    """Zero, negative and NaN scales, which append never writes, count as 2^-100 in either tensor, as in the read-back."""
+    for at, value in ((0, -0.02), (1, -1e30), (0, 0.0), (1, 0.0), (0, -float("inf")), (0, float("nan"))):
+        cache, codes, scales, q, starts, lens, table = make(hq, 2, [200, 64], [1, 2], 2, 2, 64, 16)
+        (cache.k_scale, cache.v_scale)[at][1::2] = value
+        scales[at][1::2] = 2.0 ** -100
+        y, lse = cache.attention(q, starts, lens, table, return_lse=True)
+        want, want_lse = serving.attention(q.double().cpu().numpy(), codes[0], scales[0], codes[1], scales[1], starts.tolist(), lens.tolist(),
+                                           table.cpu().numpy(), 64 ** -0.5)
+        assert np.allclose(lse.double().cpu().numpy(), want_lse, rtol=0, atol=2e-4), (at, value)
+        assert np.allclose(y.double().cpu().numpy(), want, rtol=2.0 ** -8, atol=2e-3), (at, value)
