@@ -536,7 +536,8 @@ QTZ_API qtz_status qtz_kv_schedule(qtz_handle h, const int32_t* cached_dev, cons
  *   s = max(max|x| / 127, 2^-100); if the first new token is not at offset 0, s = max(s, old scale) and the codes
  *   before it become round(code * (old scale / s)); new codes are clamp(round(x / s), -127, 127)
  * with IEEE fp32 steps and round-half-to-even.  Infinities saturate and do not count in the maximum, NaN takes the lowest
- * code.  Base pointers 16-byte aligned, strides multiples of 8 elements.  Asynchronous on `stream`.                      */
+ * code.  Base pointers 16-byte aligned, strides multiples of 8 elements (that of an axis of one element does not matter).  Asynchronous on
+ * `stream`.                      */
 QTZ_API qtz_status qtz_kv_append(qtz_handle h, const qtz_kv_cache* cache, const void* k_dev, int64_t k_token_stride,
                                  int64_t k_head_stride, const void* v_dev, int64_t v_token_stride, int64_t v_head_stride,
                                  int32_t ftype, const int64_t* slots_dev, int64_t tokens, void* stream);
@@ -551,7 +552,7 @@ QTZ_API qtz_status qtz_kv_read(qtz_handle h, const qtz_kv_cache* cache, const in
  * and sees that token and the ones before it, with window > 0 only the last `window` of those.  A row that sees nothing
  * gives zeros and lse = -inf.
  *   q, y    [tokens][q_heads][head_dim] in `ftype` (QTZ_F16 or QTZ_BF16), strides in elements, bases 16-byte aligned,
- *           strides multiples of 8.  Rows from starts[requests] on are neither read nor written.
+ *           strides multiples of 8 (that of an axis of one element does not matter).  Rows from starts[requests] on are neither read nor written.
  *   lse     NULL, or [tokens][q_heads] fp32: natural logarithm of the softmax's sum, for joining with other keys
  *   tokens  rows of q and y
  *   workspace  qtz_kv_attention_workspace_bytes(h, cache) bytes, 16-byte aligned, zero-filled once before its first use;

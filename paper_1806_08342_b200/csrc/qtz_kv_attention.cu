@@ -983,7 +983,7 @@ extern "C" qtz_status qtz_kv_attention(qtz_handle h, const qtz_kv_cache* cache, 
     if (tokens == 0) return QTZ_OK;
     if (!q_dev || !y_dev || !starts_dev || !lens_dev || !table_dev || !workspace_dev) return QTZ_ERR_INVALID_ARG;
     if (!qtz_aligned16(q_dev) || !qtz_aligned16(y_dev) || !qtz_aligned16(workspace_dev) ||
-        (q_token_stride | q_head_stride | y_token_stride | y_head_stride) % 8 != 0)
+        !qtz_kv_strides_ok(tokens, q_token_stride, q_heads, q_head_stride) || !qtz_kv_strides_ok(tokens, y_token_stride, q_heads, y_head_stride))
         return QTZ_ERR_MISALIGNED;
     // rows of the cache and units of the longest possible step are counted in 32 bits
     const int64_t rows = static_cast<int64_t>(cache->blocks) * cache->kv_heads * cache->block_tokens;

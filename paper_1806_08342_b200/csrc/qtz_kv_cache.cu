@@ -517,7 +517,8 @@ extern "C" qtz_status qtz_kv_append(qtz_handle h, const qtz_kv_cache* cache, con
     if (ftype != QTZ_F16 && ftype != QTZ_BF16) return QTZ_ERR_INVALID_ARG;
     if (tokens == 0) return QTZ_OK;
     if (!k_dev || !v_dev || !slots_dev) return QTZ_ERR_INVALID_ARG;
-    if (!qtz_aligned16(k_dev) || !qtz_aligned16(v_dev) || (k_token_stride | k_head_stride | v_token_stride | v_head_stride) % 8 != 0)
+    if (!qtz_aligned16(k_dev) || !qtz_aligned16(v_dev) || !qtz_kv_strides_ok(tokens, k_token_stride, cache->kv_heads, k_head_stride) ||
+        !qtz_kv_strides_ok(tokens, v_token_stride, cache->kv_heads, v_head_stride))
         return QTZ_ERR_MISALIGNED;
     qtz_device_guard guard(h->device);
     // About 8 CTAs an SM, each with at least a token for every warp.  Prompts of 10 800 tokens, read-back included: 43 us, with 4 CTAs an SM

@@ -63,3 +63,20 @@ def test_stored_scales_below_the_least_one_count_as_it(hq):
                                            table.cpu().numpy(), 64 ** -0.5)
         assert np.allclose(lse.double().cpu().numpy(), want_lse, rtol=0, atol=2e-4), (at, value)
         assert np.allclose(y.double().cpu().numpy(), want, rtol=2.0 ** -8, atol=2e-3), (at, value)
+
+
+def test_strides_of_single_rows_and_heads_do_not_matter(hq):
+    """An axis of one element has no stride: a row of a matrix of odd pitch, one head of a single-head cache."""
+    cache, codes, scales, q, starts, lens, table = make(hq, 4, [100], [1], 1, 4, 64, 16)
+    want = cache.attention(q, starts, lens, table)
+    row = lambda t: torch.zeros(1024, dtype=q.dtype, device="cuda").as_strided((1, 4, 64), (261, 64, 1)).copy_(t)  # noqa: E731
+    assert torch.equal(cache.attention(row(q), starts, lens, table, out=row(want)), want)
+    cache, codes, scales, q, starts, lens, table = make(hq, 5, [100, 50], [1, 1], 1, 1, 64, 16)
+    want = cache.attention(q, starts, lens, table)
+    head = lambda t: torch.zeros(1024, dtype=q.dtype, device="cuda").as_strided((2, 1, 64), (64, 77, 1)).copy_(t)  # noqa: E731
+    assert torch.equal(cache.attention(head(q), starts, lens, table, out=head(want)), want)
+    got, same = hq.kv_cache(2, 1, 16, 64), hq.kv_cache(2, 1, 16, 64)
+    for c, k in ((got, head(q)), (same, q)):
+        c.append(k, k, ints([3, 4], torch.int64))
+        c.append(k[:1].as_strided((1, 1, 64), (13, 13, 1)), k[:1], ints([5], torch.int64))
+    assert torch.equal(got.k, same.k) and torch.equal(got.v_scale, same.v_scale) and bool(same.k.any())
