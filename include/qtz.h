@@ -561,7 +561,11 @@ QTZ_API qtz_status qtz_kv_read(qtz_handle h, const qtz_kv_cache* cache, const in
  * Codes meet fixed-point queries and weights in exact integer sums: a query keeps 22 bits below its row's largest value, a
  * softmax weight 31 bits below the largest of its 128 tokens (both rounded to nearest); every other sum, maximum and statistic is fp32.  A query row that
  * holds NaN or an infinity gives NaN.
- * q_heads a multiple of kv_heads; at most 8192 requests.  Asynchronous; same results whenever repeated.               */
+ * q_heads a multiple of kv_heads; at most 8192 requests.  Asynchronous; same results whenever repeated.
+ * Work is counted in 32 bits: QTZ_ERR_TOO_LARGE where the longest step that the arguments allow, kv_heads * (tokens * group / R +
+ * requests) * (table_width * block_tokens / 64 + 7), passes 2e9, whatever the lengths; group = q_heads / kv_heads, and R, the query
+ * rows of a tile, is the least of 4, 5, 8, 10, 12, 16 that takes group * ceil(tokens / requests), 16 beyond.  The same where
+ * table_width * block_tokens or blocks * kv_heads * block_tokens passes 2^31 - 1.                                             */
 QTZ_API int64_t qtz_kv_attention_workspace_bytes(qtz_handle h, const qtz_kv_cache* cache);
 QTZ_API qtz_status qtz_kv_attention(qtz_handle h, const qtz_kv_cache* cache, const void* q_dev, int64_t q_token_stride,
                                     int64_t q_head_stride, int32_t q_heads, int32_t ftype, const int32_t* starts_dev,

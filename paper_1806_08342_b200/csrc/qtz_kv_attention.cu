@@ -941,20 +941,27 @@ qtz_status launch(qtz_ctx* h, AttnArgs& a, const CUtensorMap& km, const CUtensor
     return QTZ_OK;
 }
 
-template <typename T, int D>
-qtz_status launch_rows(qtz_ctx* h, AttnArgs& a, const CUtensorMap& km, const CUtensorMap& vm, cudaStream_t st)
+int rows_of_tile(int64_t group, int64_t tokens, int64_t requests)
 {
     // Query rows of a (request, key/value head) if all requests bring equally many tokens: the smallest tile that takes them
     // reads the cache once; larger ones only compute unused columns.  16 requests of 1000 to 8000 tokens, us: 4 rows 34.5; 5 rows 35.4
     // in a tile of 5, 36.6 in one of 8 (heads of 64: 28.4, 32.0); 8 rows 36.7; 10 rows 38.1 in a tile of 10, 40.5 in one of 12, 48.7 in one
     // of 16; 12 rows 40.4 in a tile of 12, 48.9 in one of 16; 16 rows 49.3.
-    const int64_t rows = a.group * ((static_cast<int64_t>(a.tokens) + a.requests - 1) / a.requests);
-    if (rows <= 4) return launch<T, D, 4>(h, a, km, vm, st);
-    if (rows <= 5) return launch<T, D, 5>(h, a, km, vm, st);
-    if (rows <= 8) return launch<T, D, 8>(h, a, km, vm, st);
-    if (rows <= 10) return launch<T, D, 10>(h, a, km, vm, st);
-    if (rows <= 12) return launch<T, D, 12>(h, a, km, vm, st);
-    return launch<T, D, 16>(h, a, km, vm, st);
+    const int64_t rows = group * ((tokens + requests - 1) / requests);
+    return rows <= 4 ? 4 : rows <= 5 ? 5 : rows <= 8 ? 8 : rows <= 10 ? 10 : rows <= 12 ? 12 : 16;
+}
+
+template <typename T, int D>
+qtz_status launch_rows(qtz_ctx* h, AttnArgs& a, int rows, const CUtensorMap& km, const CUtensorMap& vm, cudaStream_t st)
+{
+    switch (rows) {
+        case 4: return launch<T, D, 4>(h, a, km, vm, st);
+        case 5: return launch<T, D, 5>(h, a, km, vm, st);
+        case 8: return launch<T, D, 8>(h, a, km, vm, st);
+        case 10: return launch<T, D, 10>(h, a, km, vm, st);
+        case 12: return launch<T, D, 12>(h, a, km, vm, st);
+        default: return launch<T, D, 16>(h, a, km, vm, st);
+    }
 }
 
 int64_t counters_bytes(const qtz_ctx* h, int head_dim) { return (static_cast<int64_t>(h->num_sms) * ctas_per_sm(head_dim) * 3 * 4 + 255) / 256 * 256; }
@@ -988,7 +995,8 @@ extern "C" qtz_status qtz_kv_attention(qtz_handle h, const qtz_kv_cache* cache, 
     // rows of the cache and units of the longest possible step are counted in 32 bits
     const int64_t rows = static_cast<int64_t>(cache->blocks) * cache->kv_heads * cache->block_tokens;
     const int64_t reach = static_cast<int64_t>(table_width) * cache->block_tokens, group = q_heads / cache->kv_heads;
-    const double items = static_cast<double>(cache->kv_heads) * (static_cast<double>(tokens) * group / 5 + requests);
+    const int tile_rows = rows_of_tile(group, tokens, requests);
+    const double items = static_cast<double>(cache->kv_heads) * (static_cast<double>(tokens) * group / tile_rows + requests);
     const double units = items * (kTileUnits * static_cast<double>(reach / kTile + 1) + kItemUnits);
     if (rows > 0x7fffffff || reach > 0x7fffffff || units > 2.0e9) return QTZ_ERR_TOO_LARGE;
     qtz_device_guard guard(h->device);
@@ -1008,11 +1016,11 @@ extern "C" qtz_status qtz_kv_attention(qtz_handle h, const qtz_kv_cache* cache, 
                y_token_stride, y_head_stride, lse_dev, static_cast<int32_t*>(workspace_dev), parts, 0, box_shift, h->wait_budget, h->status_dev};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (ftype == QTZ_F16) {
-        if (cache->head_dim == 64) return launch_rows<__half, 64>(h, a, km, vm, st);
-        if (cache->head_dim == 128) return launch_rows<__half, 128>(h, a, km, vm, st);
-        return launch_rows<__half, 256>(h, a, km, vm, st);
+        if (cache->head_dim == 64) return launch_rows<__half, 64>(h, a, tile_rows, km, vm, st);
+        if (cache->head_dim == 128) return launch_rows<__half, 128>(h, a, tile_rows, km, vm, st);
+        return launch_rows<__half, 256>(h, a, tile_rows, km, vm, st);
     }
-    if (cache->head_dim == 64) return launch_rows<__nv_bfloat16, 64>(h, a, km, vm, st);
-    if (cache->head_dim == 128) return launch_rows<__nv_bfloat16, 128>(h, a, km, vm, st);
-    return launch_rows<__nv_bfloat16, 256>(h, a, km, vm, st);
+    if (cache->head_dim == 64) return launch_rows<__nv_bfloat16, 64>(h, a, tile_rows, km, vm, st);
+    if (cache->head_dim == 128) return launch_rows<__nv_bfloat16, 128>(h, a, tile_rows, km, vm, st);
+    return launch_rows<__nv_bfloat16, 256>(h, a, tile_rows, km, vm, st);
 }

@@ -80,3 +80,15 @@ def test_strides_of_single_rows_and_heads_do_not_matter(hq):
         c.append(k, k, ints([3, 4], torch.int64))
         c.append(k[:1].as_strided((1, 1, 64), (13, 13, 1)), k[:1], ints([5], torch.int64))
     assert torch.equal(got.k, same.k) and torch.equal(got.v_scale, same.v_scale) and bool(same.k.any())
+
+
+def test_many_rows_beside_a_wide_table(hq):
+    """A long step on a table for long requests: what counts is the lengths, and most of these rows are padding."""
+    cache, codes, scales, q, starts, lens, table = make(hq, 3, [300, 20], [30, 20], 8, 8, 64, 256)
+    wide = torch.zeros(2, 1024, dtype=torch.int32, device="cuda")
+    wide[:, :table.shape[1]] = table
+    many = torch.zeros(65536, 64, 64, dtype=q.dtype, device="cuda")
+    many[:50] = q
+    y, out = cache.attention(q, starts, lens, table), torch.full_like(many, 3.0)
+    cache.attention(many, starts, lens, wide, out=out)
+    assert torch.allclose(out[:50].float(), y.float(), rtol=2.0 ** -7, atol=1e-5) and bool((out[50:] == 3.0).all())
