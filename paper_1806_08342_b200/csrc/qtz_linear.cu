@@ -305,7 +305,7 @@ __device__ __forceinline__ void put(const LinearArgs& a, int64_t r, int o, float
     if (o < a.n && r < a.rows) static_cast<T*>(a.y)[r * a.y_stride + o] = qtz_dev::from_f32<T>(v);
 }
 
-// Rows whose columns lie in several CTAs, c0 .. c1: the last to arrive joins their parts in order.  Called by all threads; the first
+// Rows whose columns lie in several CTAs, c0 .. c1: the last to arrive joins their parts in order.  Called by all threads behind a barrier; the first
 // kJoin know the units that are open.  All of them read, 16 bytes a load and 16 loads in flight, in short code that comes from memory
 // like the parts: a warp for each 32 rows of W with everything unrolled took 7 us of 50 for 32 rows through 28672 x 8192.
 template <typename T, int kRows, int kJoin>
@@ -313,7 +313,6 @@ __device__ __forceinline__ void join_rows(const LinearArgs& a, const int (&open)
 {
     constexpr int kQuads = kWarps * kRowTile / 4, kAtOnce = (kRows * kQuads + kJoin - 1) / kJoin, kFlight = 16 / kAtOnce;
     const int tid = threadIdx.x;
-    __syncthreads();
     if (failed || tid >= kJoin) return;                // after a wait that gave up the results are void
     auto first = [&](int unit) { return unit / a.k_blocks * a.k_blocks; };
     if ((tid == 0 && open[0] >= 0) || (tid == 32 && open[1] >= 0)) {
@@ -387,6 +386,50 @@ __device__ __forceinline__ int digit_column(int d, int r)
     return kTiles == 1 ? 2 * d + r : kTiles == 2 ? (d >> 1) * 8 + (d & 1) * 4 + r : d * 8 + r;
 }
 
+// Takes this warp's sums of the activation rows in `odd` again, over all units of the CTA, in fp32 straight from the formula: rows that
+// hold infinities or NaN have no digits.  A lane owns a row of W.  Rolled up, since it hardly ever runs, and in place: as a function
+// that is called it cost all layers of up to eight rows 2 %.
+template <typename T, int kSteps, bool kZero>
+__device__ __forceinline__ void redo_rows(const LinearArgs& a, uint32_t odd, int u0, int u1)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int half = lane >> 4, g = lane & 7, upper = (lane >> 3) & 1;     // as pack_kernel lays them out
+#pragma unroll 1
+    for (int unit = u0; unit < u1;) {
+        const Place at(a, unit);
+        const int end = min(a.k_blocks, at.kb + u1 - unit), tile = at.rb * kWarps + warp, o = tile * kRowTile + lane;
+        for (int r = 0; r < 8 && tile < a.row_tiles; ++r) {
+            if (!(odd >> r & 1)) continue;
+            const T* const x = static_cast<const T*>(a.x) + r * a.x_stride;
+            float sum = 0.f;
+#pragma unroll 1
+            for (int kb = at.kb; kb < end; ++kb) {
+                const uint8_t* block = a.blocks + (static_cast<int64_t>(tile) * a.k_blocks + kb) * a.block_bytes;
+#pragma unroll 1
+                for (int step = 0; step < 8; step += kSteps) {
+                    const int place = step / kSteps * kRowTile + half * 16 + g * 2 + upper;
+                    const float scale = qtz_dev::to_f32(reinterpret_cast<const T*>(block + kCodeBytes)[place]);
+                    const float zero = kZero ? block[kCodeBytes + 8 / kSteps * kRowTile * 2 + place] : 8;
+                    float t = 0.f;
+#pragma unroll 1
+                    for (int i = 0; i < 4 * kSteps; ++i) {                 // words of eight columns
+                        const int s = step + i / 4, l = i % 4;
+                        const uint32_t w = reinterpret_cast<const uint32_t*>(block)[(((s >> 1) * 2 + half) * 32 + g * 4 + l) * 4 + (s & 1) * 2 + upper];
+                        for (int j = 0; j < 8; ++j) {
+                            const int m = j >> 1, c = kb * kKBlock + s * 32 + 4 * l + 16 * (j & 1) + (m == 1 ? 2 : m == 2 ? 1 : m);
+                            if (c < a.k) t += qtz_dev::to_f32(x[c]) * (static_cast<float>(w >> (4 * j) & 15) - zero);
+                        }
+                    }
+                    sum += t * scale;
+                }
+            }
+            if (at.kb == 0 && end == a.k_blocks) put<T>(a, r, o, sum + bias_of<T>(a, o));
+            else part_of<8>(a, blockIdx.x, at.kb == 0 ? 1 : 0)[r * (kWarps * kRowTile) + warp * kRowTile + lane] = sum;
+        }
+        unit += end - at.kb;
+    }
+}
+
 // kSteps: steps of 32 columns to a scale (1, 2 or 4)
 template <typename T, int kTiles, int kSteps, bool kZero>
 __global__ void __launch_bounds__(kThreads, 2)
@@ -396,11 +439,13 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(8) uint64_t s_full[kWarps][kMaxStages], s_ready[kDigitBuffers], s_free[kDigitBuffers];
     __shared__ int s_last[2], s_failed;
+    __shared__ uint32_t s_odd;                         // activation rows with values that are not finite
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t4 = lane & 3, rows = static_cast<int>(a.rows);
     Digits<kTiles>* const digits = reinterpret_cast<Digits<kTiles>*>(smem);
     if (lane < kMaxStages) mbar_init(smem_u32(&s_full[warp][lane]), 1);
     if (tid == 0) {
         s_failed = 0;
+        s_odd = 0;
         for (int i = 0; i < kDigitBuffers; ++i) {
             mbar_init(smem_u32(&s_ready[i]), rows);
             mbar_init(smem_u32(&s_free[i]), kWarps);
@@ -472,7 +517,8 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
             constexpr int kLanes = 4 * kSteps;
 #pragma unroll
             for (int off = 1; off < kLanes; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-            // a row that holds NaN or infinity gives NaN
+            // a row that holds NaN or infinity gives NaN, and its sums are taken again at the end
+            if (odd && lane == 0) atomicOr(&s_odd, 1u << r);
             const float unit_of = odd ? __uint_as_float(0x7fc00000u) : __uint_as_float(static_cast<uint32_t>(127 - 21 + ex) << 23);
             const float minus = kZero ? -1.f : -8.f;
             if (lane % kLanes == 0)
@@ -603,6 +649,11 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
         timed_out(a);
         s_failed = 1;
         s.drain();
+    }
+    __syncthreads();
+    if (s_odd && !s_failed) {                          // the same for all threads
+        redo_rows<T, kSteps, kZero>(a, s_odd, s.u0, s.u1);
+        __syncthreads();
     }
     join_rows<T, 8, kThreads>(a, open, s_failed, s_last);
 }
