@@ -33,6 +33,7 @@
 
 struct qtz_linear {
     qtz_ctx* h = nullptr;
+    int device = 0;                    // a plan may be destroyed after its handle
     qtz_linear_desc d{};
     int row_tiles = 0, k_blocks = 0;   // of 32 rows, of 256 columns
     int scales = 0;                    // scales of a row in a block of 256 columns: 2, 4 or 8
@@ -1021,7 +1022,7 @@ qtz_status ensure_scratch(qtz_ctx* h, cudaStream_t st)
 extern "C" qtz_status qtz_linear_destroy(qtz_linear_plan p)
 {
     if (!p) return QTZ_ERR_INVALID_ARG;
-    qtz_device_guard guard(p->h->device);
+    qtz_device_guard guard(p->device);
     if (p->blocks) cudaFree(p->blocks);
     (void)cudaGetLastError();
     delete p;
@@ -1048,6 +1049,7 @@ extern "C" qtz_status qtz_linear_create(qtz_handle h, const qtz_linear_desc* des
     qtz_linear* p = new (std::nothrow) qtz_linear();
     if (!p) return QTZ_ERR_INVALID_ARG;
     p->h = h;
+    p->device = h->device;
     p->d = d;
     p->row_tiles = static_cast<int>(row_tiles);
     p->k_blocks = static_cast<int>(k_blocks);

@@ -709,6 +709,8 @@ class LinearPlan:
             if out.shape != lead + (n,) or out.stride(-1) != 1:
                 raise ValueError("out has another shape")
             y = out if len(lead) == 1 else out.view(-1, n)
+        if not self.handle.h:
+            raise ValueError("the handle of this plan is closed")
         # a single row has no stride to keep: torch reports any value for it
         if rows == 1:
             rc = self._run(self.plan, x.data_ptr(), self.k_up, 1, y.data_ptr(), n, _raw_stream(self.device))
@@ -743,9 +745,9 @@ class KvCache:
         self.blocks, self.kv_heads, self.block_tokens, self.head_dim = k.shape
         self._desc = KvCacheDesc(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), *k.shape)
         self._ref = byref(self._desc)
-        self.device, self.lib, self.h, self.scale = handle.device, handle.lib, handle.h, self.head_dim ** -0.5
+        self.device, self.lib, self.scale = handle.device, handle.lib, self.head_dim ** -0.5
         # zero-filled here, not by the first call of attention(), whose fill a graph that captures it would keep for itself
-        size = self.lib.qtz_kv_attention_workspace_bytes(self.h, self._ref)
+        size = self.lib.qtz_kv_attention_workspace_bytes(handle.h, self._ref)
         self.workspace = torch.zeros(max(size, 16), dtype=torch.uint8, device=k.device)
         handle._caches.add(self)
 
@@ -762,7 +764,7 @@ class KvCache:
         ks, vs = k.stride(), v.stride()
         if k.shape != shape or v.shape != shape or ks[2] != 1 or vs[2] != 1 or dtype not in FTYPES:
             raise ValueError(f"expected keys and values of shape {shape}")
-        rc = self.lib.qtz_kv_append(self.h, self._ref, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], FTYPES[dtype],
+        rc = self.lib.qtz_kv_append(self.handle.h, self._ref, k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1], FTYPES[dtype],
                                     slots.data_ptr(), shape[0], _raw_stream(dev))
         if rc:
             self.handle._chk(rc, "qtz_kv_append")
@@ -772,7 +774,7 @@ class KvCache:
         dev, tokens = self.device, slots.numel()
         _check_flat(dev, torch.int64, slots)
         k, v = slots.new_empty((2, tokens, self.kv_heads, self.head_dim), dtype=dtype).unbind(0)
-        rc = self.lib.qtz_kv_read(self.h, self._ref, slots.data_ptr(), tokens, FTYPES.get(dtype, -1), k.data_ptr(), v.data_ptr(),
+        rc = self.lib.qtz_kv_read(self.handle.h, self._ref, slots.data_ptr(), tokens, FTYPES.get(dtype, -1), k.data_ptr(), v.data_ptr(),
                                   _raw_stream(dev))
         if rc:
             self.handle._chk(rc, "qtz_kv_read")
@@ -796,7 +798,7 @@ class KvCache:
                 raise ValueError("out has another shape")
         lse = q.new_empty(shape[:2], dtype=torch.float32) if return_lse else None
         ys = out.stride()
-        rc = self.lib.qtz_kv_attention(self.h, self._ref, q.data_ptr(), qs[0], qs[1], shape[1], FTYPES[dtype], starts.data_ptr(), lens.data_ptr(), b,
+        rc = self.lib.qtz_kv_attention(self.handle.h, self._ref, q.data_ptr(), qs[0], qs[1], shape[1], FTYPES[dtype], starts.data_ptr(), lens.data_ptr(), b,
                                        shape[0], table.data_ptr(), width, self.scale if scale is None else scale, window, out.data_ptr(), ys[0],
                                        ys[1], lse.data_ptr() if return_lse else None, self.workspace.data_ptr(), _raw_stream(dev))
         if rc:
