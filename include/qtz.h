@@ -475,7 +475,7 @@ QTZ_API qtz_status qtz_global_avgpool_u8(qtz_handle h, const uint8_t* x_dev, int
  * The affine quantizer of Section 2.1 (U4 codes with zero points) or the symmetric one of Section 2.2 (S4
  * codes, z = 0) at a finer granularity than Section 2.6's channels: `group` neighbouring columns of a row share
  * one scale.  Activations stay real.  Sums are held in fp32 and y is rounded once.  Products
- * are exact for more than eight rows; up to eight rows of x meet the codes as integers, which keep 22 bits below the largest of the 256
+ * are exact for more than four rows; up to four rows of x meet the codes as integers, which keep 30 bits below the largest of the 256
  * neighbouring values at hand (columns 256 i to 256 i + 255), rounded to nearest.  Infinities and NaN give what the formula gives.
  *   codes   [n][(k + 1) / 2] two 4-bit codes per byte, element 2i of a row in the low nibble (what
  *           qtz_quantize_tensor writes for QTZ_S4_PACKED / QTZ_U4_PACKED when `inner` is a row or, with k a

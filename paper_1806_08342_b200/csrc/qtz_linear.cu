@@ -1,11 +1,14 @@
 // Linear layers with 4-bit weights and group scales on few rows of real activations (decoding).
 //
 // Mathematics.  y[r][o] = sum_g s[o][g] sum_{k in g} (q[o][k] - z[o][g]) x[r][k] + b[o].
-//   up to 8 rows   The codes meet the integer matrix instructions (m16n8k32) as they are: eight are cut from a word by three logic
-//                  operations.  Each row's 256 columns at hand are written as 2^(e - 21) (d_2 2^16 + d_1 2^8 + d_0), e the exponent
-//                  of their largest value, d in [-128, 127]: 22 bits below it, more than the 11 or 8 that a value has; one operand
-//                  column for each digit.  Integer sums are exact; scale, digit weight and zero point (through the sum of x over the
-//                  group) multiply them in fp32.
+//   up to 4 rows   The codes meet the integer matrix instructions (m16n8k32) as they are: eight are cut from a word by three logic
+//                  operations.  Each row's 256 columns at hand are written as 2^(e - 29) (d_3 2^24 + d_2 2^16 + d_1 2^8 + d_0), e
+//                  the exponent of their largest value, d in [-128, 127], one operand column for each digit: 30 bits below that
+//                  value, so that fp16 and bf16 values are exact down to 2^-19 and 2^-22 of it, and what smaller ones lose is 2^-29 of it
+//                  at most.  (22 bits were not enough: where a strong value meets a weight of zero, the others are all that
+//                  counts.)  Integer sums are exact, the zero point's part (through the sums of the digits over the group) among
+//                  them; scale and digit weight multiply them in fp32.  Rows with infinities or NaN have no digits and are summed
+//                  from the formula in fp32.
 //   more rows      fp16 / bf16 tensor cores (tcgen05) with q - z as an exact operand: two codes are cut from a word by one logic
 //                  operation that also writes the exponent (1024 + q in fp16, 128 + q in bf16), one packed operation takes the
 //                  offset off, and the operand goes to tensor memory without touching shared memory; the scale multiplies the fp32
@@ -368,7 +371,7 @@ __device__ __forceinline__ void join_rows(const LinearArgs& a, const int (&open)
     }
 }
 
-// ---- up to eight rows: digits of x, integer matrix instructions ----
+// ---- up to four rows: digits of x, integer matrix instructions ----
 constexpr int kDigitBuffers = 3;           // units whose digits are held: the one at work, the next, the one before
 constexpr int kDigitPitch = kKBlock + 32;  // bytes of an operand column: the lanes of a load meet all banks
 
@@ -376,20 +379,20 @@ template <int kTiles>
 struct Digits {                            // of the rows' columns in one unit
     uint8_t operand[8 * kTiles][kDigitPitch];
     float factor[8 * kTiles];              // of a column's digit: a power of two, 0 for a column that holds none
-    float sum[8][8 * kTiles];              // per scale of the unit: the sum of x over its columns, at the row's highest digit
+    float sum[8][8 * kTiles];              // per scale of the unit: minus the sum of the column's digits times its factor (times 8 without zero points)
 };
 
-// Row r's digit d is operand column: 1 tile (2 rows) 2 d + r; 2 tiles (4 rows) digits 2 i + j at tile i, column 4 j + r; 3 tiles
-// (8 rows) tile d, column r.  A lane so holds a row's digits itself or shares them with the lanes of its quad.
+// Row r's digit d is operand column: 1 tile (2 rows) 2 d + r; 2 tiles (4 rows) digits 2 i + j at tile i, column 4 j + r.  A lane so
+// shares a row's digits with the lanes of its quad.
 template <int kTiles>
 __device__ __forceinline__ int digit_column(int d, int r)
 {
-    return kTiles == 1 ? 2 * d + r : kTiles == 2 ? (d >> 1) * 8 + (d & 1) * 4 + r : d * 8 + r;
+    return kTiles == 1 ? 2 * d + r : (d >> 1) * 8 + (d & 1) * 4 + r;
 }
 
 // Takes this warp's sums of the activation rows in `odd` again, over all units of the CTA, in fp32 straight from the formula: rows that
 // hold infinities or NaN have no digits.  A lane owns a row of W.  Rolled up, since it hardly ever runs, and in place: as a function
-// that is called it cost all layers of up to eight rows 2 %.
+// that is called it cost all layers of few rows 2 %.
 template <typename T, int kSteps, bool kZero>
 __device__ __forceinline__ void redo_rows(const LinearArgs& a, uint32_t odd, int u0, int u1)
 {
@@ -399,7 +402,7 @@ __device__ __forceinline__ void redo_rows(const LinearArgs& a, uint32_t odd, int
     for (int unit = u0; unit < u1;) {
         const Place at(a, unit);
         const int end = min(a.k_blocks, at.kb + u1 - unit), tile = at.rb * kWarps + warp, o = tile * kRowTile + lane;
-        for (int r = 0; r < 8 && tile < a.row_tiles; ++r) {
+        for (int r = 0; r < 4 && tile < a.row_tiles; ++r) {
             if (!(odd >> r & 1)) continue;
             const T* const x = static_cast<const T*>(a.x) + r * a.x_stride;
             float sum = 0.f;
@@ -425,7 +428,7 @@ __device__ __forceinline__ void redo_rows(const LinearArgs& a, uint32_t odd, int
                 }
             }
             if (at.kb == 0 && end == a.k_blocks) put<T>(a, r, o, sum + bias_of<T>(a, o));
-            else part_of<8>(a, blockIdx.x, at.kb == 0 ? 1 : 0)[r * (kWarps * kRowTile) + warp * kRowTile + lane] = sum;
+            else part_of<4>(a, blockIdx.x, at.kb == 0 ? 1 : 0)[r * (kWarps * kRowTile) + warp * kRowTile + lane] = sum;
         }
         unit += end - at.kb;
     }
@@ -436,7 +439,6 @@ template <typename T, int kTiles, int kSteps, bool kZero>
 __global__ void __launch_bounds__(kThreads, 2)
 linear_digits_kernel(const __grid_constant__ LinearArgs a)
 {
-    constexpr int kRows = kTiles == 3 ? 8 : 2 * kTiles;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ __align__(8) uint64_t s_full[kWarps][kMaxStages], s_ready[kDigitBuffers], s_free[kDigitBuffers];
     __shared__ int s_last[2], s_failed;
@@ -492,39 +494,51 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
             }
             top = redux_max(top);
             odd = __any_sync(0xffffffffu, odd);
-            const int ex = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -100), 127);
-            const float mult = __uint_as_float(static_cast<uint32_t>(127 + 21 - ex) << 23);
-            uint64_t d[3] = {0, 0, 0};
-            int sum = 0;
+            const int ex = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -97), 127);   // below, the unit is no normal number
+            const float mult = __uint_as_float(static_cast<uint32_t>(127 + 29 - ex) << 23);
+            uint32_t d[4][2];                          // digit, columns 0, 2, 1, 3 of the lane's first and second four
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int q = odd ? 0 : __float2int_rn(v[k] * mult);
-                const int d0 = (q << 24) >> 24, q1 = (q - d0) >> 8, d1 = (q1 << 24) >> 24, d2 = (q1 - d1) >> 8;
-                sum += q;
-                const int at = 8 * ((k & 4) | (k & 1) << 1 | (k & 2) >> 1);   // columns 0, 2, 1, 3 of four
-                d[0] |= static_cast<uint64_t>(d0 & 0xff) << at;
-                d[1] |= static_cast<uint64_t>(d1 & 0xff) << at;
-                d[2] |= static_cast<uint64_t>(d2 & 0xff) << at;
+            for (int k = 0; k < 8; k += 4) {
+                auto bytes_of = [&](float f) {         // of a number, the lower three as signed digits
+                    return (static_cast<uint32_t>(odd ? 0 : __float2int_rn(f * mult)) + 0x00808080u) ^ 0x00808080u;
+                };
+                const uint32_t q0 = bytes_of(v[k]), q1 = bytes_of(v[k + 2]), q2 = bytes_of(v[k + 1]), q3 = bytes_of(v[k + 3]);
+                const uint32_t lo01 = __byte_perm(q0, q1, 0x5140), hi01 = __byte_perm(q0, q1, 0x7362), lo23 = __byte_perm(q2, q3, 0x5140), hi23 = __byte_perm(q2, q3, 0x7362);
+                d[0][k / 4] = __byte_perm(lo01, lo23, 0x5410);
+                d[1][k / 4] = __byte_perm(lo01, lo23, 0x7632);
+                d[2][k / 4] = __byte_perm(hi01, hi23, 0x5410);
+                d[3][k / 4] = __byte_perm(hi01, hi23, 0x7632);
             }
             if (round > 0)                             // the buffer's unit before has been used by all warps
                 ok = mbar_wait_warp(smem_u32(&s_free[buffer]), (round - 1) & 1, a.wait_budget, ok);
 #pragma unroll
-            for (int j = 0; j < 3; ++j) {              // columns 4 t .. and 16 + 4 t .. of 32 lie side by side
+            for (int j = 0; j < 4; ++j) {              // columns 4 t .. and 16 + 4 t .. of 32 lie side by side
                 uint8_t* const row = &to.operand[digit_column<kTiles>(j, r)][(lane >> 2) * 32 + (lane & 1) * 16 + (lane & 2) * 2];
-                *reinterpret_cast<uint32_t*>(row) = static_cast<uint32_t>(d[j]);
-                *reinterpret_cast<uint32_t*>(row + 8) = static_cast<uint32_t>(d[j] >> 32);
+                *reinterpret_cast<uint32_t*>(row) = d[j][0];
+                *reinterpret_cast<uint32_t*>(row + 8) = d[j][1];
             }
-            // the sum of a scale's columns: |sum| < 2^22 * 128 fits
+            // the sums of the digits over a scale's columns, two to a register: 128 times 128 fits 16 bits
             constexpr int kLanes = 4 * kSteps;
+            auto digits_of = [&](int j) { return __dp4a(static_cast<int>(d[j][0]), 0x01010101, __dp4a(static_cast<int>(d[j][1]), 0x01010101, 0)); };
+            int low = digits_of(0) + (digits_of(1) << 16), high = digits_of(2) + (digits_of(3) << 16);
 #pragma unroll
-            for (int off = 1; off < kLanes; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+            for (int off = 1; off < kLanes; off <<= 1) {
+                low += __shfl_xor_sync(0xffffffffu, low, off);
+                high += __shfl_xor_sync(0xffffffffu, high, off);
+            }
             // a row that holds NaN or infinity gives NaN, and its sums are taken again at the end
             if (odd && lane == 0) atomicOr(&s_odd, 1u << r);
-            const float unit_of = odd ? __uint_as_float(0x7fc00000u) : __uint_as_float(static_cast<uint32_t>(127 - 21 + ex) << 23);
+            const float unit_of = odd ? __uint_as_float(0x7fc00000u) : __uint_as_float(static_cast<uint32_t>(127 - 29 + ex) << 23);
             const float minus = kZero ? -1.f : -8.f;
-            if (lane % kLanes == 0)
-                to.sum[lane / kLanes][digit_column<kTiles>(2, r)] = static_cast<float>(sum) * unit_of * minus;
-            if (lane < 3) to.factor[digit_column<kTiles>(lane, r)] = unit_of * (lane == 0 ? 1.f : lane == 1 ? 256.f : 65536.f);
+            if (lane % kLanes == 0) {
+                const int s0 = (low << 16) >> 16, s2 = (high << 16) >> 16;
+                float* const sums = to.sum[lane / kLanes];
+                sums[digit_column<kTiles>(0, r)] = static_cast<float>(s0) * unit_of * minus;
+                sums[digit_column<kTiles>(1, r)] = static_cast<float>((low - s0) >> 16) * (unit_of * 256.f) * minus;
+                sums[digit_column<kTiles>(2, r)] = static_cast<float>(s2) * (unit_of * 65536.f) * minus;
+                sums[digit_column<kTiles>(3, r)] = static_cast<float>((high - s2) >> 16) * (unit_of * 16777216.f) * minus;
+            }
+            if (lane < 4) to.factor[digit_column<kTiles>(lane, r)] = unit_of * static_cast<float>(1 << (8 * lane));
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&s_ready[buffer]));
         }
@@ -618,9 +632,8 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
                 for (int c = 0; c < 4; ++c) {
                     float t = acc[j][0][c];
                     if (kTiles > 1) t += acc[j][1 % kTiles][c];
-                    if (kTiles > 2) t += acc[j][2 % kTiles][c];
                     if (kTiles == 1) t += __shfl_xor_sync(0xffffffffu, t, 1);
-                    if (kTiles < 3) t += __shfl_xor_sync(0xffffffffu, t, 2);
+                    t += __shfl_xor_sync(0xffffffffu, t, 2);
                     v[4 * j + c] = t;
 #pragma unroll
                     for (int nt = 0; nt < kTiles; ++nt) acc[j][nt][c] = 0.f;
@@ -631,7 +644,7 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
                 if (begins) open[1] = s.unit;
                 else open[0] = s.unit;
             }
-            float* const part = part_of<8>(a, blockIdx.x, begins ? 1 : 0) + warp * kRowTile + g;
+            float* const part = part_of<4>(a, blockIdx.x, begins ? 1 : 0) + warp * kRowTile + g;
             const int o = s.tile(s.here) * kRowTile + g;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -656,7 +669,7 @@ linear_digits_kernel(const __grid_constant__ LinearArgs a)
         redo_rows<T, kSteps, kZero>(a, s_odd, s.u0, s.u1);
         __syncthreads();
     }
-    join_rows<T, 8, kThreads>(a, open, s_failed, s_last);
+    join_rows<T, 4, kThreads>(a, open, s_failed, s_last);
 }
 
 // ---- more rows: 16-bit tensor cores (tcgen05) ----
@@ -958,7 +971,7 @@ qtz_status launch(qtz_linear* p, LinearArgs& a, K kernel, int threads, int ctas,
     if (a.stages > kMaxStages) a.stages = kMaxStages;
     const int smem = fixed + kWarps * a.stages * p->block_bytes, grid = ctas * h->num_sms;
     // A share takes in at least 1 / most_parts of the columns: joining 16 or 32 rows costs more than it brings beyond that (1024 x 8192:
-    // 9.7 and 12.5 us against 10.9 and 16.3 without a limit; up to eight rows the limit changes nothing and there is none).
+    // 9.7 and 12.5 us against 10.9 and 16.3 without a limit; with few rows the limit changes nothing and there is none).
     a.share = (a.units + grid - 1) / grid;
     if (most_parts && a.share < (a.k_blocks + most_parts - 1) / most_parts) a.share = (a.k_blocks + most_parts - 1) / most_parts;
     const qtz_status s = qtz_allow_smem(h, kernel);
@@ -994,13 +1007,12 @@ qtz_status launch_wide(qtz_linear* p, LinearArgs& a, bool zero, cudaStream_t st)
 template <typename T>
 qtz_status launch_rows(qtz_linear* p, LinearArgs& a, bool zero, cudaStream_t st)
 {
-    // us at 1, 2, 4, 5, 8 | 9, 16 | 17, 32 rows: 24.9, 26.5, 32.2, 38.0, 42.2 | 40.7, 41.1 | 41.7, 42.7 through 28672 x 8192, groups of
-    // 128; 7.6, 7.7, 8.7, 9.8, 10.5 | 10.1, 10.7 | 11.9, 13.1 through 4096 x 4096, groups of 32.  With the wide kernel from 5 rows on
-    // 40.6 to 40.7 and 9.9 to 10.1: even on average.  More than 32 rows take several passes over the weights, which then lie in L2:
+    // us at 1, 2, 4 | 5 to 8, 12, 16 | 32 rows: 24.4, 26.2, 31.6 | 40.0, 40.1, 40.3 | 41.8 through 28672 x 8192, groups of 128; 6.2, 6.3, 7.3 |
+    // 9.3, 9.4, 9.7 | 12.4 through 4096 x 4096, groups of 32; 4.7, 4.8, 5.2 | 6.4, 6.5, 6.9 | 8.4 through 1000 x 1024.  Digits for five to
+    // eight rows would take 32 operand columns; with 24, three digits a row, eight rows took 42.8, 9.0 and 6.0.  More than 32 rows take several passes over the weights, which then lie in L2:
     // 64 rows at once left no second buffer for the products (69.9 us against 30.3 for two passes through 5003 x 10001).
     if (a.rows <= 2) return launch_digits<T, 1>(p, a, zero, st);
     if (a.rows <= 4) return launch_digits<T, 2>(p, a, zero, st);
-    if (a.rows <= 8) return launch_digits<T, 3>(p, a, zero, st);
     if (a.rows <= 16) return launch_wide<T, 16>(p, a, zero, st);
     return launch_wide<T, 32>(p, a, zero, st);
 }
@@ -1009,7 +1021,7 @@ qtz_status launch_rows(qtz_linear* p, LinearArgs& a, bool zero, cudaStream_t st)
 qtz_status ensure_scratch(qtz_ctx* h, cudaStream_t st)
 {
     if (h->linear_dev) return QTZ_OK;
-    const int ctas = 2 * h->num_sms;                   // of up to eight rows; half as many with four times the rows
+    const int ctas = 2 * h->num_sms;                   // of up to four rows; half as many with more
     const size_t parts = static_cast<size_t>(h->num_sms) * 2 * kWarps * kRowTile * kMaxTokens * sizeof(float);
     QTZ_CUDA(h, cudaMalloc(&h->linear_dev, parts + ctas * sizeof(int32_t)));
     QTZ_CUDA(h, cudaMemsetAsync(static_cast<uint8_t*>(h->linear_dev) + parts, 0, ctas * sizeof(int32_t), st));

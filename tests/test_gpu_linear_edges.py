@@ -51,3 +51,32 @@ def test_infinities_and_nan_as_in_the_definition(hq, n, k, group, zeros, rows, d
     tol = 2 * (k + 8) * 2.0 ** -24 * size
     tol = tol + torch.finfo(dtype).eps / 2 * (np.abs(np.where(odd, 0, want)) + tol) + 2.0 ** -25
     assert (np.abs(got[~odd] - want[~odd]) <= tol[~odd]).all()
+
+
+@pytest.mark.parametrize("dtype,strong", [(torch.float16, 2.0 ** 15), (torch.bfloat16, 2.0 ** 20)])
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 8, 12])
+@pytest.mark.parametrize("n,k,group,zeros", [(300, 512, 64, False), (70, 777, 32, True), (64, 256, 128, False)])
+def test_strong_values_that_meet_weights_of_zero(hq, n, k, group, zeros, rows, dtype, strong):
+    """One value of each row lies far above the others, and half of the weights that it meets are zero: there the others are all that
+    counts.  Bound: that of fp32 sums, 2 (k + 8) 2^-24 sum |x w|, half of 2^-29 of the strong value for each column of a block of 256
+    (no sum is off by more), and the rounding to the output's type."""
+    g = torch.Generator().manual_seed(n + rows)
+    at = 5
+    codes = torch.randint(0, 256, (n, (k + 1) // 2), generator=g, dtype=torch.uint8)
+    scales = (torch.rand(n, -(-k // group), generator=g) + 0.1).to(dtype)
+    z = torch.randint(1, 15, (n, -(-k // group)), generator=g, dtype=torch.uint8) if zeros else None
+    none = z[::2, at // group] if zeros else torch.zeros((n + 1) // 2, dtype=torch.uint8)
+    codes[::2, at // 2] = (codes[::2, at // 2] & 15) | (none << 4)             # column 5 is a high nibble
+    q = torch.stack((codes & 15, codes >> 4), -1).flatten(1)[:, :k].double()
+    cols = torch.arange(k) // group
+    w = (q - z[:, cols].double() if zeros else torch.where(q > 7, q - 16, q)) * scales.double()[:, cols]
+    assert not w[::2, at].any()
+    x = torch.randn(rows, -(-k // 8) * 8, generator=g).to(dtype)
+    x[:, at] = strong
+    got = hq.linear_create(codes.cuda(), scales.cuda(), k, group, zeros=None if z is None else z.cuda())(x.cuda()[:, :k]).double().cpu()
+    x = x[:, :k].double()
+    want = x @ w.T
+    tol = 2 * (k + 8) * 2.0 ** -24 * (x.abs() @ w.abs().T) + 2.0 ** -30 * strong * w[:, :256].abs().sum(1)
+    tol = tol + torch.finfo(dtype).eps / 2 * (want.abs() + tol) + 2.0 ** -25
+    worst = ((got - want).abs() / tol)[torch.isfinite(got)].max().item()
+    assert worst <= 1.0 and bool(torch.isfinite(got[:, ::2]).all()), worst
