@@ -560,7 +560,7 @@ QTZ_API qtz_status qtz_kv_read(qtz_handle h, const qtz_kv_cache* cache, const in
  *   workspace  qtz_kv_attention_workspace_bytes(h, cache) bytes, 16-byte aligned, zero-filled once before its first use;
  *           one stream at a time.  Its size does not depend on lengths.  After QTZ_ERR_DEVICE_TIMEOUT zero it again, once
  *           qtz_last_device_status has reported it.
- * Codes meet fixed-point queries and weights in exact integer sums: a query keeps 22 bits below its row's largest value, a
+ * Codes meet fixed-point queries and weights in exact integer sums: a query keeps 30 bits below its row's largest value, a
  * softmax weight 31 bits below the largest of its 128 tokens (both rounded to nearest); every other sum, maximum and statistic is fp32.  A query row that
  * holds NaN or an infinity gives NaN.
  * q_heads a multiple of kv_heads; at most 8192 requests.  Asynchronous; same results whenever repeated.

@@ -6,14 +6,15 @@
 // themselves, and the softmax's denominator is sum w_p / s_v.
 // Both products have 8-bit codes on one side, which the tensor cores (kind::i8) read straight from the bytes that TMA
 // brings in: nothing is converted.  The other side is split into base-256 digits, one operand column each:
-//   q_row = 2^(e - 21) (d_2 2^16 + d_1 2^8 + d_0)   e = exponent of the row's largest value, d in [-128, 127]: 22 bits
+//   q_row = 2^(e - 29) (d_3 2^24 + d_2 2^16 + d_1 2^8 + d_0)     e = exponent of the row's largest value, d in [-128, 127]
 //   w_p   = 2^(m' - 31) (b_3 2^24 + b_2 2^16 + b_1 2^8 + b_0)    b in [0, 255]; m' = maximum of t over the tile, not the running one
-// Integer sums are exact; a query loses what lies below 2^-22 of its row's largest value and a weight what lies below 2^-32 of
-// its tile's largest, which is 2^-25 of it for a whole tile.  (Weights count by their sum: with 22 bits below the running maximum
-// a token of large weight and no value took 10^5 others out of y.)  The sums are joined in fp32, a tile's times 2^(m' - m).
+// Integer sums are exact; a query's values lose 2^-29 of the row's largest at most (fp16 and bf16 are exact down to 2^-19 and 2^-22 of
+// it), a weight 2^-32 of its tile's largest, which is 2^-25 of it for a whole tile.  Three digits, 22 bits, were not enough: a strong
+// value of a query can meet codes of zero, so that the others decide, and weights count by their sum: a token of large weight and no
+// value took 10^5 others out of y.  The sums are joined in fp32, a tile's times 2^(m' - m).
 //
 // One tile is 128 tokens of one key/value head against kRows query rows (heads of the group x new tokens):
-//   S^T [128 tokens x 3 kRows] = K [128 x D] Q^T        a thread owns a token: logits, maximum, weights
+//   S^T [128 tokens x 4 kRows] = K [128 x D] Q^T        a thread owns a token: logits, maximum, weights
 //   O^T [D x 4 kRows]          = V^T [D x 128] W        a thread owns a column of the head: fp32 running sum
 // with V read as it lies (the depth of the product along its rows).
 //
@@ -167,13 +168,6 @@ __device__ __forceinline__ void st_shared_u8(uint32_t addr, uint32_t v)
     asm volatile("st.shared.u8 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
 
-// d_2 65536 + d_1 256 + d_0 for digit sums below 2^22
-__device__ __forceinline__ float join_digits(uint32_t d0, uint32_t d1, uint32_t d2)
-{
-    const int hi = static_cast<int>(d2) * 256 + static_cast<int>(d1);
-    return fmaf(static_cast<float>(hi), 256.f, static_cast<float>(static_cast<int>(d0)));
-}
-
 // The four digits' sums over 128 codes, each below 2^22
 __device__ __forceinline__ float join_digits(uint32_t d0, uint32_t d1, uint32_t d2, uint32_t d3)
 {
@@ -181,27 +175,13 @@ __device__ __forceinline__ float join_digits(uint32_t d0, uint32_t d1, uint32_t 
     return fmaf(static_cast<float>(hi), 65536.f, static_cast<float>(lo));
 }
 
-template <int kN>
-__device__ __forceinline__ void load_columns(uint32_t taddr, uint32_t (&v)[kN])
+// The digits' sums of rows r0 to r0 + 3, as far as there are any.
+template <int kRows>
+__device__ __forceinline__ void load_digits(uint32_t taddr, int r0, uint32_t (&v)[16])
 {
-    if constexpr (kN >= 32) {
-        uint32_t x[32];
-        tmem_ld_32x32(taddr, x);
-        if constexpr (kN > 32) {
-            uint32_t y[16];
-            tmem_ld_32x16(taddr + 32, y);
-            tmem_ld_wait();
-#pragma unroll
-            for (int i = 0; i < 16; ++i) v[32 + i] = y[i];
-        } else {
-            tmem_ld_wait();
-        }
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = x[i];
-    } else {
-        tmem_ld_32x16(taddr, v);
-        tmem_ld_wait();
-    }
+    if (kRows % 4 == 1 && r0 + 4 > kRows) tmem_ld_32x4(taddr + 4 * r0, v);
+    else if (kRows % 4 == 2 && r0 + 4 > kRows) tmem_ld_32x8(taddr + 4 * r0, v);
+    else tmem_ld_32x16(taddr + 4 * r0, v);
 }
 
 // What the compute threads know of an item: two of them, for the one at work and the next.
@@ -239,21 +219,20 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
 {
     constexpr int kHalves = D > 128 ? 2 : 1;           // boxes along a row of the cache
     constexpr int kRowBytes = D < 128 ? D : 128;
-    constexpr int kN = (3 * kRows + 15) / 16 * 16;     // operand columns of the queries: digit * kRows + row
-    constexpr int kNw = (4 * kRows + 15) / 16 * 16;    // of the weights: 4 row + digit
+    constexpr int kN = (4 * kRows + 15) / 16 * 16;     // operand columns: 4 row + digit
     constexpr int kRowsUp = (kRows + 3) / 4 * 4;
     constexpr int kBox = kTile * kRowBytes;            // K or V of one tile and half
     constexpr int kStage = 2 * kHalves * kBox;
-    constexpr int kColumns = kN == 48 ? 64 : kN, kColumnsO = kNw == 48 ? 64 : kNw;   // of tensor memory: two buffers of S, two of each half of O
-    constexpr int kUsed = 2 * kColumns + 2 * kHalves * kColumnsO, kTmemColumns = kUsed <= 64 ? 64 : kUsed <= 128 ? 128 : kUsed <= 256 ? 256 : 512;
+    constexpr int kColumns = kN == 48 ? 64 : kN;       // of tensor memory: two buffers of S, two of each half of O
+    constexpr int kUsed = (2 + 2 * kHalves) * kColumns, kTmemColumns = kUsed <= 64 ? 64 : kUsed <= 128 ? 128 : kUsed <= 256 ? 256 : 512;
     constexpr int kPart = kMaxRows * D + 4 * kMaxRows;
     constexpr uint32_t kMulK = (2u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(kN >> 3) << 17) | (static_cast<uint32_t>(kTile >> 4) << 24);
-    constexpr uint32_t kMulV = (2u << 4) | (1u << 7) | (0u << 10) | (1u << 15) | (static_cast<uint32_t>(kNw >> 3) << 17) | (128u >> 4 << 24);
+    constexpr uint32_t kMulV = (2u << 4) | (1u << 7) | (0u << 10) | (1u << 15) | (static_cast<uint32_t>(kN >> 3) << 17) | (128u >> 4 << 24);
 
     extern __shared__ __align__(1024) uint8_t smem[];  // the swizzle counts from multiples of 1 KB; nothing static lies before it
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t base = smem_u32(smem);
-    const uint32_t off_p = a.stages * kStage, off_q = off_p + kNw * 128, off_shared = off_q + kN * D, off_prefix = off_shared + (sizeof(Shared) + 15) / 16 * 16;
+    const uint32_t off_p = a.stages * kStage, off_q = off_p + kN * 128, off_shared = off_q + kN * D, off_prefix = off_shared + (sizeof(Shared) + 15) / 16 * 16;
     uint32_t* const prefix = reinterpret_cast<uint32_t*>(smem + off_prefix);
     Shared& sh = *reinterpret_cast<Shared*>(smem + off_shared);
     KnownRequests& known = sh.known;
@@ -471,7 +450,7 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                 for (int hh = 0; hh < kHalves; ++hh)
 #pragma unroll
                     for (int j = 0; j < kTile / 32; ++j)
-                        mma_i8(tmem + 2 * kColumns + ((i & 1) * kHalves + hh) * kColumnsO, make_mnmajor_desc(v + hh * kBox + j * 32 * kRowBytes, kRowBytes),
+                        mma_i8(tmem + (2 + (i & 1) * kHalves + hh) * kColumns, make_mnmajor_desc(v + hh * kBox + j * 32 * kRowBytes, kRowBytes),
                                make_kmajor_desc(base + off_p, 128) + 2 * j, kMulV, j > 0);
                 mma_commit(smem_u32(&sh.ofull[i & 1]));
                 mma_commit(smem_u32(&sh.empty[i % a.stages]));
@@ -566,29 +545,24 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
                 }
                 top = redux_max(top);
                 odd = __any_sync(0xffffffffu, odd);
-                // rows below 2^-100 count as 2^-100 (their logits are zero either way)
-                const int ex = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -100), 127);
-                const float mult = __uint_as_float(static_cast<uint32_t>(127 + 21 - ex) << 23);
-                uint64_t digits[3] = {0, 0, 0};
+                // rows below 2^-97 count as 2^-97 (their logits are zero either way)
+                const int ex = min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127, -97), 127);
+                const float mult = __uint_as_float(static_cast<uint32_t>(127 + 29 - ex) << 23);
+                uint32_t bytes[kPer];                  // of a number, the lower three as signed digits
 #pragma unroll
-                for (int k = 0; k < kPer; ++k) {
-                    const int x = odd ? 0 : __float2int_rn(v[k] * mult);
-                    const int d0 = (x << 24) >> 24, x1 = (x - d0) >> 8, d1 = (x1 << 24) >> 24, d2 = (x1 - d1) >> 8;
-                    digits[0] |= static_cast<uint64_t>(d0 & 0xff) << (8 * k);
-                    digits[1] |= static_cast<uint64_t>(d1 & 0xff) << (8 * k);
-                    digits[2] |= static_cast<uint64_t>(d2 & 0xff) << (8 * k);
-                }
+                for (int k = 0; k < kPer; ++k) bytes[k] = (static_cast<uint32_t>(odd ? 0 : __float2int_rn(v[k] * mult)) + 0x00808080u) ^ 0x00808080u;
                 const int d = lane * kPer, hh = d / 128, x = d % kRowBytes;
 #pragma unroll
-                for (int g = 0; g < 3; ++g) {
-                    const int n = g * kRows + r, swz = kRowBytes == 128 ? (n & 7) : ((n >> 1) & 3);
+                for (int g = 0; g < 4; ++g) {
+                    const int n = 4 * r + g, swz = kRowBytes == 128 ? (n & 7) : ((n >> 1) & 3);
                     uint8_t* to = smem + off_q + hh * kN * kRowBytes + n * kRowBytes + (((x >> 4) ^ swz) << 4) + (x & 15);
-                    if constexpr (kPer == 2) *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(digits[g]);
-                    else if constexpr (kPer == 4) *reinterpret_cast<uint32_t*>(to) = static_cast<uint32_t>(digits[g]);
-                    else *reinterpret_cast<uint64_t*>(to) = digits[g];
+                    auto pair = [&](int k) { return __byte_perm(bytes[k], bytes[k + 1], g | (4 + g) << 4); };
+                    if constexpr (kPer == 2) *reinterpret_cast<uint16_t*>(to) = static_cast<uint16_t>(pair(0));
+                    else if constexpr (kPer == 4) *reinterpret_cast<uint32_t*>(to) = __byte_perm(pair(0), pair(2), 0x5410);
+                    else *reinterpret_cast<uint2*>(to) = make_uint2(__byte_perm(pair(0), pair(2), 0x5410), __byte_perm(pair(4), pair(6), 0x5410));
                 }
                 // a row that holds NaN or infinity gives NaN
-                if (lane == 0) it.factor[r] = odd ? __uint_as_float(0x7fc00000u) : a.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 - 21 + ex) << 23);
+                if (lane == 0) it.factor[r] = odd ? __uint_as_float(0x7fc00000u) : a.scale_log2 * __uint_as_float(static_cast<uint32_t>(127 - 29 + ex) << 23);
             }
             fence_proxy_async_smem();
             __syncwarp();
@@ -633,12 +607,8 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
             for (int hh = 0; hh < kHalves; ++hh)
 #pragma unroll
                 for (int r0 = 0; r0 < kRows; r0 += 4) {
-                    constexpr int kLeft = kRows % 4;
                     uint32_t o[16];
-                    const uint32_t from = tmem + 2 * kColumns + ((i & 1) * kHalves + hh) * kColumnsO + 4 * r0 + (static_cast<uint32_t>(warp) << 21);
-                    if (kLeft == 1 && r0 + 4 > kRows) tmem_ld_32x4(from, o);
-                    else if (kLeft == 2 && r0 + 4 > kRows) tmem_ld_32x8(from, o);
-                    else tmem_ld_32x16(from, o);
+                    load_digits<kRows>(tmem + (2 + (i & 1) * kHalves + hh) * kColumns + (static_cast<uint32_t>(warp) << 21), r0, o);
                     const float4 keep = *reinterpret_cast<const float4*>(&sh.keep[i & 1][warp][r0]), gain = *reinterpret_cast<const float4*>(&sh.gain[i & 1][warp][r0]);
                     tmem_ld_wait();
 #pragma unroll
@@ -668,12 +638,16 @@ attention_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ CUt
             tc_fence_after();
             float x[kRows];
             {
-                uint32_t s[kN];
-                load_columns<kN>(tmem + (i & 1) * kColumns + (static_cast<uint32_t>(warp) << 21), s);
                 const float lv = lg2(vs);
 #pragma unroll
-                for (int r = 0; r < kRows; ++r)
-                    x[r] = fmaf(join_digits(s[r], s[kRows + r], s[2 * kRows + r]), it.factor[r] * ks, lv);
+                for (int r0 = 0; r0 < kRows; r0 += 4) {
+                    uint32_t s[16];
+                    load_digits<kRows>(tmem + (i & 1) * kColumns + (static_cast<uint32_t>(warp) << 21), r0, s);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int r = 0; r < 4 && r0 + r < kRows; ++r)
+                        x[r0 + r] = fmaf(join_digits(s[4 * r], s[4 * r + 1], s[4 * r + 2], s[4 * r + 3]), it.factor[r0 + r] * ks, lv);
+                }
             }
             if (__float_as_uint(scales.x) == kNoBox) {
 #pragma unroll
@@ -928,9 +902,9 @@ int ctas_per_sm(int head_dim) { return head_dim == 256 ? 1 : 2; }
 template <typename T, int D, int kRows>
 qtz_status launch(qtz_ctx* h, AttnArgs& a, const CUtensorMap& km, const CUtensorMap& vm, cudaStream_t st)
 {
-    constexpr int kN = (3 * kRows + 15) / 16 * 16, kNw = (4 * kRows + 15) / 16 * 16, kStage = 2 * kTile * D;
+    constexpr int kN = (4 * kRows + 15) / 16 * 16, kStage = 2 * kTile * D;
     const int ctas = ctas_per_sm(D);
-    const int fixed = kNw * 128 + kN * D + static_cast<int>((sizeof(Shared) + 15) / 16 * 16 + sizeof(uint32_t) * (a.requests + 1));
+    const int fixed = kN * 128 + kN * D + static_cast<int>((sizeof(Shared) + 15) / 16 * 16 + sizeof(uint32_t) * (a.requests + 1));
     const int room = (kSmemLimit + 1024) / ctas - 1024 - fixed;
     a.stages = room / kStage < kMaxStages ? room / kStage : kMaxStages;
     if (a.stages < 2) return QTZ_ERR_TOO_LARGE;

@@ -96,3 +96,30 @@ def test_strong_token_last_and_in_a_window(hq):
     made = strong_token(5, [5000, 4100], [2, 2], 2, 4, 128, 16, torch.bfloat16, 15, 4097)
     check(hq, made)
     check(hq, made, window=3000)
+
+
+@pytest.mark.parametrize("dtype,strong", [(torch.float16, 2.0 ** 15), (torch.bfloat16, 2.0 ** 20)])
+@pytest.mark.parametrize("dim,group,new", [(64, 1, 1), (64, 5, 1), (128, 8, 1), (128, 5, 2), (128, 4, 3), (256, 16, 1)])
+def test_strong_query_values_that_meet_codes_of_zero(hq, dim, group, new, dtype, strong):
+    """One value of each query lies far above the others and meets nothing but zeros in the keys: the logits come from the others.
+    A query loses half of 2^-29 of its largest value: a logit is off by c 2^-30 max|q| sum |k| beside the fp32 sums' part."""
+    requests = 3
+    codes, scales, table, starts, lens, q, scale = strong_token(dim + group, [260, 131, 70], [new] * requests, 2, group, dim, 16, dtype, 2, 0)
+    at = 7
+    codes[0][..., at] = 0
+    q[:, :, at] = strong
+    cache = qtz.KvCache(hq, *(torch.from_numpy(c).cuda() for c in codes), *(torch.from_numpy(s).cuda() for s in scales))
+    dev = lambda a: torch.from_numpy(a).cuda()  # noqa: E731
+    y, lse = cache.attention(q.cuda(), dev(starts), dev(lens), dev(table), scale=scale, return_lse=True)
+    qn = q.double().numpy()
+    args = (scales[1], starts, lens, table, scale)
+    want, want_lse = serving.attention(qn, codes[0], scales[0], codes[1], *args)
+    size, _ = serving.attention(qn, codes[0], scales[0], np.abs(codes[1]), *args)
+    rest = qn.copy()
+    rest[..., at] = 0
+    k = np.abs(codes[0].astype(np.float64)).sum(-1).max() * scales[0].max()                # sum |k| of a token, at most
+    d = scale * (2 * (dim + 8) * 2.0 ** -24 * np.abs(rest).max() * k + 2.0 ** -30 * strong * k)
+    tol = (2 * d + 2.0 ** -18) * size + 2.0 ** -24 * 127 * scales[1].max()
+    tol = tol + UNIT[dtype] * (np.abs(want) + tol) + 2.0 ** -25
+    assert (np.abs(y.double().cpu().numpy() - want) <= tol).all()
+    assert np.abs(lse.double().cpu().numpy() - want_lse).max() <= d + 2.0 ** -18 * (1 + np.abs(want_lse).max())
