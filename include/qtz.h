@@ -495,7 +495,7 @@ QTZ_API qtz_status qtz_linear_create(qtz_handle h, const qtz_linear_desc* desc, 
                                      const uint8_t* zeros_dev, const void* bias_dev, qtz_linear_plan* out, void* stream);
 QTZ_API qtz_status qtz_linear_destroy(qtz_linear_plan p);
 /* x: `rows` rows of k values, x_stride elements apart; base and x_stride * 2 bytes multiples of 16, x_stride >= k.
- * Values past k in a row are never used.  y: rows of n values, y_stride >= n elements apart, no alignment rule.
+ * Values past k in a row are never used, but the 16 bytes that hold the last one are read whole, also of the last row.  y: rows of n values, y_stride >= n elements apart, no alignment rule.
  * rows == 0 does nothing.  Asynchronous on `stream`.                                                            */
 QTZ_API qtz_status qtz_linear_w4(qtz_linear_plan p, const void* x_dev, int64_t x_stride, int64_t rows, void* y_dev,
                                  int64_t y_stride, void* stream);
@@ -534,7 +534,7 @@ QTZ_API qtz_status qtz_kv_schedule(qtz_handle h, const int32_t* cached_dev, cons
                                    int64_t capacity, int32_t* report_dev, void* stream);
 /* Quantizes `tokens` new keys and values (rows of head_dim values in `ftype`: QTZ_F16 or QTZ_BF16; strides in elements)
  * into the slots given; a negative slot is skipped.  Tokens of one block are neighbours in the list, in ascending slots, and
- * no block appears in two places.  Per block, head and tensor, over the block's new tokens (Section 2.2):
+ * no block appears in two places; where that does not hold, what those blocks then contain is undefined.  Per block, head and tensor, over the block's new tokens (Section 2.2):
  *   s = max(max|x| / 127, 2^-100); if the first new token is not at offset 0, s = max(s, old scale) and the codes
  *   before it become round(code * (old scale / s)); new codes are clamp(round(x / s), -127, 127)
  * with IEEE fp32 steps and round-half-to-even.  Infinities saturate and do not count in the maximum, NaN takes the lowest
@@ -552,7 +552,7 @@ QTZ_API qtz_status qtz_kv_read(qtz_handle h, const qtz_kv_cache* cache, const in
  *   y[t][h] = sum_p softmax_p(scale * q[t][h] . K[p][g]) V[p][g],     g = h / (q_heads / kv_heads)
  * Row t of request r (starts[r] <= t < starts[r + 1]) is its token number lens[r] - (starts[r + 1] - starts[r]) + t - starts[r]
  * and sees that token and the ones before it, with window > 0 only the last `window` of those.  A row that sees nothing
- * gives zeros and lse = -inf.
+ * gives zeros and lse = -inf.  Of a length beyond table_width * block_tokens the tokens past the table are not seen.
  *   q, y    [tokens][q_heads][head_dim] in `ftype` (QTZ_F16 or QTZ_BF16), strides in elements, bases 16-byte aligned,
  *           strides multiples of 8 (that of an axis of one element does not matter).  Rows from starts[requests] on are neither read nor written.
  *   lse     NULL, or [tokens][q_heads] fp32: natural logarithm of the softmax's sum, for joining with other keys

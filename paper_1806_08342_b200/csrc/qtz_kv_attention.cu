@@ -24,9 +24,11 @@
 // lengths.  A producer warp streams a CTA's share through a ring of TMA boxes, several tiles ahead and across items.  Items
 // that lie in more than one share are joined by the last CTA to arrive, in the order of the tiles, so that results do not
 // depend on timing.
-// Measured: 64 requests of 300 to 32768 tokens, 8 heads of 128, 4 query heads each: 161 us for 1.03 GB, 6.4 TB/s, 0.99 of the copy
+// Measured: 64 requests of 300 to 32768 tokens, 8 heads of 128, 4 query heads each: 160 us for 1.03 GB, 6.4 TB/s, 0.99 of the copy
 // rate.  One request over 262143 tokens, 4 heads: 54.7 us for 268 MB, 4.9 TB/s: 6 us until the first tile, 8 for the two joins.  16
-// requests with 5 new tokens and a window of 1024: 21.8 us for 24 MB, four tiles a CTA: all of it start, first use and joins.
+// requests with 5 new tokens and a window of 1024: 22.0 us for 24 MB, four tiles a CTA: all of it start, first use and joins.  Many new
+// tokens a request are not what it is made for: 16 rows a pass over the keys, and all row tiles of a request go over the same tiles,
+// masked ones included (4 requests of 500 to 900 tokens, 100 of them new: 83 us).
 #include <cuda.h>
 
 #include <type_traits>
@@ -73,8 +75,9 @@ struct AttnArgs {
 };
 
 // The sequence is dealt out by cost: a tile counts two units and the end of an item five, for the last sums, the output rows, the
-// next queries and the refill behind them.  us with 1, 3, 5, 8 units: 168, 161, 161, 161 for 64 requests of 300 to 32768 tokens, 8
-// key/value heads, 128 columns; 87, 75, 71, 71 for 256 of 100 to 1000; 35.3 to 35.1 for 8 of 4000 to 16000.
+// next queries and the refill behind them.  us with 1, 3, 5, 8 units, measured with row tiles of 5: 168, 161, 161, 161 for 64 requests of
+// 300 to 32768 tokens, 8 key/value heads, 128 columns; 87, 75, 71, 71 for 256 of 100 to 1000 (62 with tiles of 4); 35.3 to 35.1 for 8 of
+// 4000 to 16000.
 constexpr int kTileUnits = 2, kItemUnits = 5;
 
 struct RequestShape {

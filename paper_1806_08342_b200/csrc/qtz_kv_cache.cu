@@ -30,8 +30,8 @@ struct ScheduleArgs {
 
 // Exclusive prefix sums of (new tokens, new blocks) over the requests, recomputed by every CTA in shared memory: the lengths are a
 // few KB that all CTAs read from L2, which is cheaper than a second launch or a grid barrier.  Bound by latency: 3.4 us for 96
-// requests with a token each, 5.8 us for 1501 with 0 to 83 tokens, where 0.04 us would do for the 257 KB that have to move.  Each thread then finds the request of its token, or
-// of its new block, by bisection, and writes the slot or the table entry.
+// requests with a token each, 5.8 us for 1501 with 0 to 83 tokens, where 0.04 us would do for the 257 KB that have to move.  Each thread
+// then finds the request of its token, or of its new block, by bisection, and writes the slot or the table entry.
 __global__ void __launch_bounds__(kSchedThreads)
 schedule_kernel(const __grid_constant__ ScheduleArgs a)
 {
@@ -205,9 +205,9 @@ __device__ __forceinline__ float max_abs8(uint4 v, float top)
     return fmaxf(top, fmaxf(f.x, f.y));
 }
 
-// Codes of eight values.  x * (1/s) is within 2^-21 of the quotient that the definition rounds, so it rounds to the same integer
-// unless it lies within 4 * 10^-5 of the middle between two; there, and for NaN and infinity, the definition itself is taken.  The
-// integer is read from the mantissa after adding 1.5 * 2^23 (round half to even).
+// Codes of eight values.  x * (1/s) is off from the quotient that the definition rounds by three roundings, 1.5 * 2^-23 of it: 2.3 * 10^-5
+// at a code of 127.  It rounds to the same integer unless it lies within 4 * 10^-5 of the middle between two; there, and for NaN and
+// infinity, the definition itself is taken.  The integer is read from the mantissa after adding 1.5 * 2^23 (round half to even).
 template <typename T>
 __device__ __forceinline__ uint2 quantize8(uint4 v, float s, float r)
 {
@@ -257,8 +257,9 @@ __device__ __forceinline__ uint4 rescale16(uint4 v, float ratio)
 // tensor.  Short runs take a warp each, long ones the CTA, whose threads keep the run's values in registers between the maximum
 // and the codes.  The window grows with the list, so that a step of single tokens spreads over the GPU and a prompt does not launch a
 // CTA for each of its tokens.  Prompts of 10 800 tokens (8 heads of 128): 27 us for 66 MB, 2.5 TB/s, with the issue slots 59 % busy:
-// loads, maxima and codes of one window do not overlap, and four CTAs an SM fill the gaps only in part.  192 single tokens: about
-// 6 us, of which 3 the chain slot, value, old scale, code.
+// loads, maxima and codes of a run follow one another with nothing of the next run under way (shared memory, which has the room for
+// it, is not used), and four CTAs an SM fill the gaps only in part.  192 single tokens: about 6 us, of which 3 the chain slot, value,
+// old scale, code.
 template <typename T>
 __global__ void __launch_bounds__(kThreads, 4)
 append_kernel(const __grid_constant__ AppendArgs a)
@@ -422,8 +423,8 @@ struct ReadArgs {
     int32_t* status;
 };
 
-// One warp per token: lanes take sixteen codes at a time of all heads of both tensors.  Bound by HBM: one byte in, two or four out
-// (10 800 tokens of 8 heads of 128 to bf16: 16 us for 66 MB, 4.1 TB/s).
+// One warp per token: lanes take sixteen codes at a time of all heads of both tensors.  One byte in, two or four out.  10 800 tokens of 8
+// heads of 128 to bf16: 16 us for 66 MB, 4.1 TB/s, 0.64 of the copy rate: a warp has one token's loads under way, behind its look-up.
 template <typename T>
 __global__ void __launch_bounds__(kThreads)
 read_kernel(const __grid_constant__ ReadArgs a)

@@ -16,14 +16,16 @@
 // Nothing is rounded to 16 bits before y.
 //
 // What bounds it: half a byte of weight is read for 2 flops an activation row.  At the measured copy rate that is 46 weights a clock
-// and SM, for which the SM issues 2.8 operations a weight: the first form needs about 1.3 for one row and 1.9 for eight (its matrix
-// instructions, 2048 products a clock, then still take 85 weights a clock), the second 2 with 32 rows.
+// and SM, for which the SM issues 2.8 operations a weight: the first form needs about 1.3 for one row (its matrix instructions, 2048
+// products a clock, take 128 weights a clock with four rows), the second less than 2 with 32 rows, by the source.
 // The weights are read once, in the order of use, as contiguous blocks of 32 rows x 256 columns with their scales and zero points
 // behind the codes; every warp streams its blocks through a ring of its own (bulk copies, several blocks ahead).  Activations are
 // few: the eight warps of a CTA work on the same columns of 256 rows and share them in shared memory.
-// Measured: one row through 32768 x 8192 26.3 us, 5.3 TB/s of weights, 0.83 of the copy rate; 32 rows through 28672 x 8192 41.7 us,
-// 3.0 TB/s and 0.36 PFLOP/s, the issue slots 63 % busy and the tensor pipe 17 %: unpacking bounds it, 3.7 operations a weight with all
-// waits counted; one row through 1000 x 1024 4.6 us, where 2 are the launch.
+// Measured: one row through 32768 x 8192 27.1 us, 5.2 TB/s of weights, 0.81 of the copy rate; four through 28672 x 8192 31.6 us, where the
+// fp32 work for each scale grows with the digit columns; 32 rows through 28672 x 8192 41.8 us, 2.9 TB/s and 0.36 PFLOP/s, the issue slots
+// 64 % busy and the tensor pipe 17 %: 3.7 operations a weight are issued, about half of them polls, because a thread waits for each 16
+// sums of a product right after it has asked for them and holds too many (32) to have others under way; one row through 1000 x 1024
+// 4.7 us, where 2 are the launch.
 // The (256 rows, 256 columns) units form one sequence that is dealt out in equal contiguous shares to a grid that fills the GPU
 // once; rows whose columns lie in several CTAs are joined by the last of those to arrive, in the order of the columns.
 #include <new>
