@@ -1011,8 +1011,9 @@ qtz_status launch_rows(qtz_linear* p, LinearArgs& a, bool zero, cudaStream_t st)
 {
     // us at 1, 2, 4 | 5 to 8, 12, 16 | 32 rows: 24.4, 26.2, 31.6 | 40.0, 40.1, 40.3 | 41.8 through 28672 x 8192, groups of 128; 6.2, 6.3, 7.3 |
     // 9.3, 9.4, 9.7 | 12.4 through 4096 x 4096, groups of 32; 4.7, 4.8, 5.2 | 6.4, 6.5, 6.9 | 8.4 through 1000 x 1024.  Digits for five to
-    // eight rows would take 32 operand columns; with 24, three digits a row, eight rows took 42.8, 9.0 and 6.0.  More than 32 rows take several passes over the weights, which then lie in L2:
-    // 64 rows at once left no second buffer for the products (69.9 us against 30.3 for two passes through 5003 x 10001).
+    // eight rows would take 32 operand columns; with 24, three digits a row, eight rows took 42.8, 9.0 and 6.0.  More than 32 rows take
+    // several passes over the weights, which then lie in L2: 64 rows at once left no second buffer for the products (69.9 us against
+    // 30.3 for two passes through 5003 x 10001).
     if (a.rows <= 2) return launch_digits<T, 1>(p, a, zero, st);
     if (a.rows <= 4) return launch_digits<T, 2>(p, a, zero, st);
     if (a.rows <= 16) return launch_wide<T, 16>(p, a, zero, st);
