@@ -57,6 +57,7 @@ typedef int32_t qtz_status;
 typedef struct qtz_ctx* qtz_handle;     /* library-owned, opaque */
 typedef struct qtz_plan* qtz_conv_plan; /* library-owned: prepacked weights and tables */
 typedef struct qtz_linear* qtz_linear_plan; /* library-owned: prepacked 4-bit weights   */
+typedef struct qtz_f8_layer* qtz_f8_linear_plan;  /* library-owned: prepacked e4m3 weights */
 
 /* Scale, zero point and the nudged real range of one quantizer (Section 2.1). */
 typedef struct {
@@ -499,6 +500,57 @@ QTZ_API qtz_status qtz_linear_destroy(qtz_linear_plan p);
  * rows == 0 does nothing.  Asynchronous on `stream`.                                                            */
 QTZ_API qtz_status qtz_linear_w4(qtz_linear_plan p, const void* x_dev, int64_t x_stride, int64_t rows, void* y_dev,
                                  int64_t y_stride, void* stream);
+
+/* ---- serving: linear layers in 8-bit floating point ------------------------------------------- */
+
+/* Codes are e4m3 (one sign, four exponent, three mantissa bits, no infinities; one byte each): the real value is code * scale.
+ * Activations have one scale for each row and 128 neighbouring columns, weights one for each block of 128 rows and 128 columns: Section
+ * 2.2's symmetric quantizer with a floating-point code in the integer's place, at a finer granularity than Section 2.6's channels.  The
+ * last blocks of a row or a column may be short.  For a block whose largest finite magnitude is m:
+ *   s = max(m / 448, 2^-100),  code = e4m3(v * (1 / s)) with fp32 steps, rounded to nearest even.
+ * Infinities saturate and do not count in m; NaN becomes the code NaN.
+ *
+ * qtz_f8_rmsnorm: root-mean-square norm of rows of k values with the residual's addition before it,
+ *   h = x + residual;  sum = h;  v = h / sqrt(mean(h^2) + eps) * gain;  values = v;  (codes, scales) of v
+ * h, v and the mean in fp32, each output rounded once from them (the norm goes on with the unrounded h).  A row that holds an
+ * infinity gives NaN there and zeros elsewhere, as the formula does; one that holds NaN gives NaN.
+ *   x, residual, gain, sum, values   of type `ftype` (QTZ_F32, QTZ_F16, QTZ_BF16); residual, sum and values may be NULL
+ *   codes, scales                    NULL (then values is not), or [rows][k] and [rows][ceil(k / 128)]
+ *   eps                              at least 1e-30
+ * Strides are in elements; bases and rows start on 16 bytes (the stride of a single row does not matter; scales have no alignment
+ * rule), and a row's values lie next to each other.  sum and values may be x or residual themselves; otherwise nothing overlaps.
+ * Bytes past k in a row are neither read nor written.  At most 32768 columns (QTZ_ERR_TOO_LARGE).  Asynchronous on `stream`; rows == 0
+ * does nothing.                                                                                                   */
+QTZ_API qtz_status qtz_f8_rmsnorm(qtz_handle h, const void* x_dev, int64_t x_stride, const void* residual_dev, int64_t residual_stride,
+                                  const void* gain_dev, float eps, int64_t rows, int32_t k, int32_t ftype, void* sum_dev, int64_t sum_stride,
+                                  void* values_dev, int64_t values_stride, uint8_t* codes_dev, int64_t codes_stride, float* scales_dev,
+                                  int64_t scales_stride, void* stream);
+/* Codes and scales of v = x, or with gate of v = gate / (1 + exp(-gate)) * x in fp32 (the gate's factor is 0 where exp(-gate) passes
+ * fp32, below -88.7).  Types, strides and alignment as above; at most 2^30 columns.                                */
+QTZ_API qtz_status qtz_f8_quantize(qtz_handle h, const void* x_dev, int64_t x_stride, const void* gate_dev, int64_t gate_stride, int64_t rows,
+                                   int32_t k, int32_t ftype, uint8_t* codes_dev, int64_t codes_stride, float* scales_dev, int64_t scales_stride,
+                                   void* stream);
+/* Weights w [n][k] (any `ftype`, rows w_stride elements apart, no alignment rule): codes [n][k] dense, scales
+ * [ceil(n / 128)][ceil(k / 128)].  Asynchronous on `stream`.                                                         */
+QTZ_API qtz_status qtz_f8_quantize_weights(qtz_handle h, const void* w_dev, int64_t w_stride, int32_t n, int32_t k, int32_t ftype,
+                                           uint8_t* codes_dev, float* scales_dev, void* stream);
+
+/* y[r][o] = sum_b x_scale[r][b] w_scale[o / 128][b] sum_{k in b} x[r][k] w[o][k] + bias[o]
+ * Products of codes are exact, their sum over a block of 128 columns and the sum over blocks are held in fp32, and y is rounded once.
+ * A NaN code gives NaN in its row (of x) or column (of w).  Scales are finite, and so are the products of two that meet.
+ *
+ * One-time preparation: copies codes (rows codes_stride bytes apart, no alignment rule), scales and bias (n values of type
+ * bias_ftype, or NULL) into the order the kernels read.  BLOCKS until `stream` has finished; the caller may then free or overwrite
+ * all inputs.                                                                                                     */
+QTZ_API qtz_status qtz_f8_linear_create(qtz_handle h, int32_t n, int32_t k, const uint8_t* codes_dev, int64_t codes_stride, const float* scales_dev,
+                                        const void* bias_dev, int32_t bias_ftype, qtz_f8_linear_plan* out, void* stream);
+QTZ_API qtz_status qtz_f8_linear_destroy(qtz_f8_linear_plan p);
+/* x: `rows` rows of k codes, codes_stride bytes apart, base and stride multiples of 16 (the stride of a single row does not matter);
+ * scales: element (r, b) at r * scales_row_stride + b * scales_block_stride; y: rows of n values of type `ftype` (QTZ_F32, QTZ_F16 or
+ * QTZ_BF16), y_stride elements apart, no alignment rule.  rows == 0 does nothing.  Asynchronous on `stream`.         */
+QTZ_API qtz_status qtz_f8_linear(qtz_f8_linear_plan p, const uint8_t* codes_dev, int64_t codes_stride, const float* scales_dev,
+                                 int64_t scales_row_stride, int64_t scales_block_stride, int64_t rows, void* y_dev, int64_t y_stride,
+                                 int32_t ftype, void* stream);
 
 /* ---- serving: key/value cache in 8 bits ------------------------------------------------------ */
 

@@ -25,6 +25,7 @@ ACT_NONE, ACT_RELU, ACT_RELU6 = 0, 1, 2
 F32, F16, BF16 = 16, 17, 18
 DEVICE_TIMEOUT = -7
 FTYPES = {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16}
+E4M3 = torch.float8_e4m3fn
 
 QPARAMS = np.dtype([("scale", "<f4"), ("zero_point", "<i4"), ("min_nudged", "<f4"), ("max_nudged", "<f4")])
 
@@ -118,6 +119,14 @@ SIGNATURES = {
     "qtz_linear_create": (c_int32, [c_void_p, POINTER(LinearDesc), c_void_p, c_void_p, c_void_p, c_void_p, POINTER(c_void_p), c_void_p]),
     "qtz_linear_destroy": (c_int32, [c_void_p]),
     "qtz_linear_w4": (c_int32, [c_void_p, c_void_p, c_int64, c_int64, c_void_p, c_int64, c_void_p]),
+    "qtz_f8_rmsnorm": (c_int32, [c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_float, c_int64, c_int32, c_int32, c_void_p, c_int64,
+                                 c_void_p, c_int64, c_void_p, c_int64, c_void_p, c_int64, c_void_p]),
+    "qtz_f8_quantize": (c_int32, [c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_int64, c_int32, c_int32, c_void_p, c_int64, c_void_p, c_int64,
+                                  c_void_p]),
+    "qtz_f8_quantize_weights": (c_int32, [c_void_p, c_void_p, c_int64, c_int32, c_int32, c_int32, c_void_p, c_void_p, c_void_p]),
+    "qtz_f8_linear_create": (c_int32, [c_void_p, c_int32, c_int32, c_void_p, c_int64, c_void_p, c_void_p, c_int32, POINTER(c_void_p), c_void_p]),
+    "qtz_f8_linear_destroy": (c_int32, [c_void_p]),
+    "qtz_f8_linear": (c_int32, [c_void_p, c_void_p, c_int64, c_void_p, c_int64, c_int64, c_int64, c_void_p, c_int64, c_int32, c_void_p]),
     "qtz_kv_schedule": (c_int32, [c_void_p, c_void_p, c_void_p, c_int32, c_int32, c_void_p, c_int32, c_void_p, c_void_p, c_void_p,
                                   c_void_p, c_void_p, c_int64, c_void_p, c_void_p]),
     "qtz_kv_append": (c_int32, [c_void_p, POINTER(KvCacheDesc), c_void_p, c_int64, c_int64, c_void_p, c_int64, c_int64, c_int32, c_void_p,
@@ -561,6 +570,88 @@ class Handle:
                                              _raw_stream(self.device)), "qtz_linear_create")
         return LinearPlan(self, plan, desc, scales.dtype)
 
+    # ---- serving: 8-bit floating point, scales for blocks of 128 ----
+    def _f8_empty(self, rows, k):
+        """Codes [rows][k] whose rows start on 16 bytes, and scales [rows][ceil(k / 128)]."""
+        device, pitch = f"cuda:{self.device}", (k + 15) // 16 * 16
+        codes = torch.empty((rows, pitch), dtype=E4M3, device=device)
+        return codes if pitch == k else codes[:, :k], torch.empty((rows, (k + 127) // 128), dtype=torch.float32, device=device)
+
+    def _f8_rows(self, dtype, shape, *ts):
+        for t in ts:
+            if t is not None and (t.dtype is not dtype or t.get_device() != self.device or t.shape != shape or (t.stride(1) != 1 and shape[1] > 1)):
+                raise ValueError(f"expected rows of {dtype} values of shape {tuple(shape)} on cuda:{self.device}, got {t.dtype}, {tuple(t.shape)}, "
+                                 f"strides {t.stride()} on {t.device}")
+
+    def f8_rmsnorm(self, x, gain, eps=1e-6, residual=None, codes=True, values=False, sum_out=None):
+        """Root-mean-square norm of the rows of x (+ residual) [rows][k]: (codes, scales, values, sum).  codes and scales (e4m3
+        [rows][k], fp32 [rows][ceil(k / 128)]) are None unless `codes`, values (the type of x) unless `values`, sum (x + residual)
+        without a residual.  `sum_out` may be `residual` itself."""
+        dtype, shape = x.dtype, x.shape
+        if len(shape) != 2 or dtype not in FTYPES:
+            raise ValueError("expected rows of float32, float16 or bfloat16 values")
+        rows, k = shape
+        total = None
+        if residual is not None:
+            total = x.new_empty((rows, (k + 7) // 8 * 8))[:, :k] if sum_out is None else sum_out
+        elif sum_out is not None:
+            raise ValueError("sum_out belongs to a residual")
+        self._f8_rows(dtype, shape, x, residual, total)
+        if gain.dtype is not dtype or gain.shape != (k,) or gain.get_device() != self.device or not gain.is_contiguous():
+            raise ValueError(f"expected a gain of {k} {dtype} values on cuda:{self.device}")
+        out = x.new_empty((rows, (k + 7) // 8 * 8))[:, :k] if values else None
+        q, s = self._f8_empty(rows, k) if codes else (None, None)
+        at = lambda t: (None, 0) if t is None else (t.data_ptr(), t.stride(0))  # noqa: E731
+        rc = self.lib.qtz_f8_rmsnorm(self.h, *at(x), *at(residual), gain.data_ptr(), eps, rows, k, FTYPES[dtype], *at(total), *at(out), *at(q), *at(s),
+                                     _raw_stream(self.device))
+        if rc:
+            self._chk(rc, "qtz_f8_rmsnorm")
+        return q, s, out, total
+
+    def f8_quantize(self, x, gate=None):
+        """Codes (e4m3 [rows][k]) and scales (fp32 [rows][ceil(k / 128)]) of x [rows][k], or of silu(gate) * x."""
+        dtype, shape = x.dtype, x.shape
+        if len(shape) != 2 or dtype not in FTYPES:
+            raise ValueError("expected rows of float32, float16 or bfloat16 values")
+        self._f8_rows(dtype, shape, x, gate)
+        rows, k = shape
+        q, s = self._f8_empty(rows, k)
+        rc = self.lib.qtz_f8_quantize(self.h, x.data_ptr(), x.stride(0), None if gate is None else gate.data_ptr(), 0 if gate is None else gate.stride(0),
+                                      rows, k, FTYPES[dtype], q.data_ptr(), q.stride(0), s.data_ptr(), s.stride(0), _raw_stream(self.device))
+        if rc:
+            self._chk(rc, "qtz_f8_quantize")
+        return q, s
+
+    def f8_quantize_weights(self, w):
+        """Codes (e4m3 [n][k]) and scales (fp32 [ceil(n / 128)][ceil(k / 128)]) of weights w [n][k], as f8_linear_create takes them."""
+        if w.dim() != 2 or w.dtype not in FTYPES:
+            raise ValueError("expected a matrix of float32, float16 or bfloat16 values")
+        self._f8_rows(w.dtype, w.shape, w)
+        n, k = w.shape
+        codes = torch.empty((n, k), dtype=E4M3, device=w.device)
+        scales = torch.empty((-(-n // 128), -(-k // 128)), dtype=torch.float32, device=w.device)
+        self._chk(self.lib.qtz_f8_quantize_weights(self.h, _ptr(w), w.stride(0), n, k, FTYPES[w.dtype], _ptr(codes), _ptr(scales),
+                                                   _raw_stream(self.device)), "qtz_f8_quantize_weights")
+        return codes, scales
+
+    def f8_linear_create(self, codes, scales, bias=None):
+        """Plan of y = x W^T + bias with e4m3 codes of W [n][k] and fp32 scales [ceil(n / 128)][ceil(k / 128)]."""
+        if codes.dim() != 2:
+            raise ValueError("expected codes [n][k]")
+        n, k = codes.shape
+        self._f8_rows(E4M3, codes.shape, codes)
+        _check_flat(self.device, torch.float32, scales)
+        if scales.shape != (-(-n // 128), -(-k // 128)):
+            raise ValueError(f"expected a scale for each 128 x 128 block of [{n}][{k}], got {tuple(scales.shape)}")
+        if bias is not None:
+            _check_flat(self.device, bias.dtype, bias)
+            if bias.shape != (n,) or bias.dtype not in FTYPES:
+                raise ValueError(f"expected a bias of {n} values")
+        plan = c_void_p()
+        self._chk(self.lib.qtz_f8_linear_create(self.h, n, k, _ptr(codes), codes.stride(0), _ptr(scales), _ptr(bias),
+                                                F32 if bias is None else FTYPES[bias.dtype], byref(plan), _raw_stream(self.device)), "qtz_f8_linear_create")
+        return F8LinearPlan(self, plan, n, k)
+
     def kv_schedule(self, cached, added, table, free, free_count, block_tokens, capacity):
         """qtz_kv_schedule: writes the new blocks into `table` and returns (starts, lens, slots, report)."""
         device = self.device
@@ -723,6 +814,48 @@ class LinearPlan:
     def close(self):
         if self.plan:
             self.handle.lib.qtz_linear_destroy(self.plan)
+            self.plan = c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class F8LinearPlan:
+    """Owns a qtz_f8_linear_plan: y = x W^T + bias with e4m3 activations and weights."""
+
+    def __init__(self, handle: Handle, plan, n, k):
+        self.handle, self.plan, self.n, self.k, self.device, self.blocks = handle, plan, n, k, handle.device, -(-k // 128)
+        self._run = handle.lib.qtz_f8_linear
+
+    def __call__(self, codes, scales, dtype=torch.bfloat16, out=None):
+        """codes [rows][k] in e4m3 (rows a multiple of 16 bytes apart), scales [rows][ceil(k / 128)] in fp32 with any strides."""
+        device, n = self.device, self.n
+        if codes.dtype is not E4M3 or codes.get_device() != device or scales.dtype is not torch.float32 or scales.get_device() != device:
+            raise ValueError(f"expected {E4M3} codes and float32 scales on cuda:{device}, got {codes.dtype} on {codes.device}, {scales.dtype} on {scales.device}")
+        rows = codes.shape[0]
+        if codes.shape != (rows, self.k) or (codes.stride(1) != 1 and self.k > 1) or scales.shape != (rows, self.blocks):
+            raise ValueError(f"expected rows of {self.k} neighbouring codes and {self.blocks} scales, got {tuple(codes.shape)} with strides "
+                             f"{codes.stride()} and {tuple(scales.shape)}")
+        if out is None:
+            if dtype not in FTYPES:
+                raise ValueError("y is float32, float16 or bfloat16")
+            out = torch.empty((rows, n), dtype=dtype, device=codes.device)
+        elif out.shape != (rows, n) or (out.stride(1) != 1 and n > 1) or out.dtype not in FTYPES or out.get_device() != device:
+            raise ValueError(f"expected out of shape {(rows, n)} on cuda:{device}")
+        if not self.handle.h:
+            raise ValueError("the handle of this plan is closed")
+        rc = self._run(self.plan, codes.data_ptr(), codes.stride(0), scales.data_ptr(), scales.stride(0), scales.stride(1), rows, out.data_ptr(),
+                       out.stride(0), FTYPES[out.dtype], _raw_stream(device))
+        if rc:
+            self.handle._chk(rc, "qtz_f8_linear")
+        return out
+
+    def close(self):
+        if self.plan:
+            self.handle.lib.qtz_f8_linear_destroy(self.plan)
             self.plan = c_void_p()
 
     def __del__(self):
