@@ -2,8 +2,6 @@
 // block of 128 x 128.
 //
 // Mathematics.  y[r][o] = sum_b x_scale[r][b] w_scale[o / 128][b] sum_{k in b} x[r][k] w[o][k] + bias[o].
-#include <cuda_fp8.h>
-
 #include <new>
 
 #include "qtz_f8.cuh"
@@ -18,9 +16,12 @@ struct qtz_f8_layer {
     uint8_t* tiles = nullptr;          // [n_tiles][k_blocks][128][128] codes, zeros beyond n and k
     float* scales = nullptr;           // [n_tiles][k_blocks], behind the tiles in the same allocation
     float* bias = nullptr;             // [n], behind the scales; null: none
+    CUtensorMap w_map{};               // the tiles as rows of 128 bytes, 128 rows at a time
 };
 
 namespace {
+
+using namespace qtz_ptx;
 
 struct PackArgs {
     const uint8_t* codes;
@@ -47,57 +48,605 @@ __global__ void bias_kernel(const void* bias, int32_t ftype, float* out, int32_t
 }
 
 struct LinearArgs {
-    const uint8_t *tiles, *x;
     const float *w_scales, *bias, *x_scales;
-    int64_t x_stride, row_stride, block_stride, rows, y_stride;
+    int64_t row_stride, block_stride, rows, y_stride;
     void* y;
-    int32_t n, k, n_tiles, k_blocks;
-    int32_t ftype;
+    int32_t n, n_tiles, k_blocks, ftype;
+    int32_t vector;            // rows of y start on 16 bytes
+    int32_t row_tiles;         // tiles of activation rows
+    int32_t units, share;      // few rows: tiles x blocks of 128 columns, and how many of them a CTA takes
+    float* parts;              // few rows: what tiles that lie in several shares are joined from
+    int32_t* counters;
+    long long wait_budget;
+    int32_t* status;
 };
 
-__device__ __forceinline__ float e4m3_f32(uint8_t v)
+constexpr int kTileBytes = kF8Block * kF8Block;
+constexpr int kSmemLimit = 227 * 1024;
+constexpr int kMaxStages = 12;
+// Descriptor of the products: fp32 sums of e4m3 x e4m3, kN columns, kM rows.
+template <int kM, int kN>
+constexpr uint32_t kProduct = (1u << 4) | (static_cast<uint32_t>(kN >> 3) << 17) | (static_cast<uint32_t>(kM >> 4) << 24);
+
+__device__ __forceinline__ void timed_out(const LinearArgs& a)
 {
-    __nv_fp8_e4m3 t;
-    t.__x = v;
-    return static_cast<float>(t);
+    if (atomicCAS(a.status, 0, QTZ_ERR_DEVICE_TIMEOUT) == 0) a.status[1] = QTZ_SITE_F8_LINEAR;
 }
 
-// 32 rows of x, 32 of W; a thread four sums of one row of x.
-__global__ void __launch_bounds__(256) linear_kernel(const __grid_constant__ LinearArgs a)
+__device__ __forceinline__ void put(const LinearArgs& a, int64_t at, float v)
 {
-    __shared__ float s_x[32][33], s_w[32][33];
-    const int tid = threadIdx.x, tx = tid & 31, ty = tid >> 5;
-    const int o0 = blockIdx.x * 32;
-    for (int64_t r0 = static_cast<int64_t>(blockIdx.y) * 32; r0 < a.rows; r0 += static_cast<int64_t>(gridDim.y) * 32) {
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int b = 0; b < a.k_blocks; ++b) {
-            float part[4] = {0.f, 0.f, 0.f, 0.f};
-            const uint8_t* tile = a.tiles + (static_cast<int64_t>(o0 / kF8Block) * a.k_blocks + b) * (kF8Block * kF8Block);
-            for (int c = 0; c < kF8Block; c += 32) {
-                __syncthreads();
-                for (int i = ty; i < 32; i += 8) {
-                    const int col = b * kF8Block + c + tx;
-                    s_x[i][tx] = r0 + i < a.rows && col < a.k ? e4m3_f32(a.x[(r0 + i) * a.x_stride + col]) : 0.f;
-                    s_w[i][tx] = e4m3_f32(tile[(o0 % kF8Block + i) * kF8Block + c + tx]);
-                }
-                __syncthreads();
-                for (int i = 0; i < 32; ++i)
-                    for (int j = 0; j < 4; ++j) part[j] = fmaf(s_x[ty * 4 + j][i], s_w[tx][i], part[j]);
-            }
-            const float ws = a.w_scales[static_cast<int64_t>(o0 / kF8Block) * a.k_blocks + b];
-            for (int j = 0; j < 4; ++j)
-                if (r0 + ty * 4 + j < a.rows) sum[j] = fmaf(part[j], a.x_scales[(r0 + ty * 4 + j) * a.row_stride + b * a.block_stride] * ws, sum[j]);
-        }
-        const int o = o0 + tx;
-        for (int j = 0; j < 4; ++j) {
-            const int64_t r = r0 + ty * 4 + j, at = r * a.y_stride + o;
-            if (r >= a.rows || o >= a.n) continue;
-            const float y = sum[j] + (a.bias ? a.bias[o] : 0.f);
-            if (a.ftype == QTZ_F32) static_cast<float*>(a.y)[at] = y;
-            else if (a.ftype == QTZ_F16) static_cast<__half*>(a.y)[at] = __float2half_rn(y);
-            else static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(y);
+    if (a.ftype == QTZ_BF16) static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(v);
+    else if (a.ftype == QTZ_F16) static_cast<__half*>(a.y)[at] = __float2half_rn(v);
+    else static_cast<float*>(a.y)[at] = v;
+}
+
+// Eight neighbouring values of a row, of which `valid` exist.
+__device__ __forceinline__ void put8(const LinearArgs& a, int64_t at, int valid, const float* v)
+{
+    if (valid < 8 || !a.vector) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < valid) put(a, at + i, v[i]);
+    } else if (a.ftype == QTZ_F32) {
+        float4* const to = reinterpret_cast<float4*>(static_cast<float*>(a.y) + at);
+        to[0] = make_float4(v[0], v[1], v[2], v[3]);
+        to[1] = make_float4(v[4], v[5], v[6], v[7]);
+    } else if (a.ftype == QTZ_F16) {
+        using qtz_dev::pack2;
+        *reinterpret_cast<uint4*>(static_cast<__half*>(a.y) + at) =
+            make_uint4(pack2(v[0], v[1], __half()), pack2(v[2], v[3], __half()), pack2(v[4], v[5], __half()), pack2(v[6], v[7], __half()));
+    } else {
+        using qtz_dev::pack2;
+        using B = __nv_bfloat16;
+        *reinterpret_cast<uint4*>(static_cast<B*>(a.y) + at) = make_uint4(pack2(v[0], v[1], B()), pack2(v[2], v[3], B()), pack2(v[4], v[5], B()), pack2(v[6], v[7], B()));
+    }
+}
+
+__device__ __forceinline__ float bias_of(const LinearArgs& a, int o) { return a.bias && o < a.n ? __ldg(a.bias + o) : 0.f; }
+
+// ---- few rows: the weights stream past kN rows of x ----
+// The 128 weights of a tile are the rows of the product, the rows of x its columns.  Units (tile, block of 128 columns) form one
+// sequence that is dealt out in equal contiguous shares; a tile that lies in several shares is joined by the last CTA to arrive.
+constexpr int kSlots = 8;              // units whose scales are under way
+
+template <int kN>
+struct Stream {
+    static constexpr int kEpiWarps = kN == 128 ? 8 : 4, kCols = kN * 4 / kEpiWarps;   // columns of a warp
+    static constexpr int kThreads = 128 + 32 * kEpiWarps;
+    static constexpr int kStage = kTileBytes + kN * kF8Block;
+    static constexpr int kBuffers = kN <= 64 ? 8 : 4;                                 // of kN columns of tensor memory
+    static constexpr int kColumns = kN * kBuffers < 32 ? 32 : kN * kBuffers;
+    static constexpr int kStages = (kSmemLimit - 1024 - kSlots * kN * 4 - 1024) / kStage < kMaxStages ? (kSmemLimit - 1024 - kSlots * kN * 4 - 1024) / kStage : kMaxStages;
+};
+
+struct Unit {
+    int tile, kb;
+    __device__ Unit(const LinearArgs& a, int u) : tile(u / a.k_blocks), kb(u % a.k_blocks) {}
+    __device__ void next(const LinearArgs& a)
+    {
+        if (++kb == a.k_blocks) {
+            kb = 0;
+            ++tile;
         }
     }
+};
+
+template <int kN>
+__device__ __forceinline__ float* part_of(const LinearArgs& a, int cta, int which) { return a.parts + (static_cast<int64_t>(cta) * 2 + which) * (kN * kF8Block); }
+
+// After a CTA's last unit: counts its arrival at the tiles that it shares with others, and sums those at which it is the last, in the
+// order of the columns.  Called by all `threads` threads, behind a barrier of the CTA.
+template <int kN>
+__device__ __forceinline__ void join_tiles(const LinearArgs& a, const int (&open)[2], int tid, int threads, int (&last)[2])
+{
+    auto first = [&](int unit) { return unit / a.k_blocks * a.k_blocks; };
+    if ((tid == 0 && open[0] >= 0) || (tid == 32 && open[1] >= 0)) {
+        const int begin = first(tid ? open[1] : open[0]), c0 = begin / a.share;
+        const bool all = arrive_acq_rel(a.counters + c0) == (begin + a.k_blocks - 1) / a.share - c0;
+        last[tid ? 1 : 0] = all;
+        if (all) a.counters[c0] = 0;                   // ready for the next call
+    }
+    named_barrier(1, threads);
+#pragma unroll 1
+    for (int which = 0; which < 2; ++which) {
+        const int unit = open[which];
+        if (unit < 0 || !last[which]) continue;
+        const int begin = first(unit), c0 = begin / a.share, c1 = (begin + a.k_blocks - 1) / a.share, tile = unit / a.k_blocks;
+        const int64_t r0 = static_cast<int64_t>(tile % a.row_tiles) * kN;
+        const int quads = static_cast<int>(min(static_cast<int64_t>(kN), a.rows - r0)) * (kF8Block / 4);
+        constexpr int kAtOnce = 4;
+#pragma unroll 1
+        for (int q0 = tid; q0 < quads; q0 += kAtOnce * threads) {
+            float4 v[kAtOnce];
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+            for (int c = c0; c <= c1; ++c) {
+                const float4* const part = reinterpret_cast<const float4*>(part_of<kN>(a, c, c == c0 ? 1 : 0)) + q0;
+                float4 p[kAtOnce];
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j) p[j] = q0 + j * threads < quads ? __ldcg(part + j * threads) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int j = 0; j < kAtOnce; ++j) {
+                    v[j].x += p[j].x;
+                    v[j].y += p[j].y;
+                    v[j].z += p[j].z;
+                    v[j].w += p[j].w;
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                const int q = q0 + j * threads;
+                if (q >= quads) break;
+                const int o = tile / a.row_tiles * kF8Block + q % (kF8Block / 4) * 4;
+                const int64_t at = (r0 + q / (kF8Block / 4)) * a.y_stride + o;
+                if (o < a.n) put(a, at, v[j].x + bias_of(a, o));
+                if (o + 1 < a.n) put(a, at + 1, v[j].y + bias_of(a, o + 1));
+                if (o + 2 < a.n) put(a, at + 2, v[j].z + bias_of(a, o + 2));
+                if (o + 3 < a.n) put(a, at + 3, v[j].w + bias_of(a, o + 3));
+            }
+        }
+    }
+}
+
+template <int kN>
+__global__ void __launch_bounds__(Stream<kN>::kThreads, 1)
+stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map)
+{
+    using S = Stream<kN>;
+    extern __shared__ uint8_t smem_raw[];              // the ring: a tile of weights, kN rows of x
+    __shared__ __align__(16) float s_scales[kSlots][kN];
+    __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_done[S::kBuffers], s_free[S::kBuffers], s_scaled[kSlots], s_slot[kSlots], s_drain;
+    __shared__ int s_open[2], s_last[2], s_failed;     // s_open: units whose tiles are shared with an earlier / a later CTA
+    __shared__ uint32_t s_tmem;
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    if (tid == 0) {
+        s_failed = 0;
+        s_open[0] = s_open[1] = -1;
+        prefetch_tensormap(&w_map);
+        prefetch_tensormap(&x_map);
+        for (int i = 0; i < S::kStages; ++i) {
+            mbar_init(smem_u32(&s_full[i]), 1);
+            mbar_init(smem_u32(&s_empty[i]), 1);
+        }
+        for (int i = 0; i < S::kBuffers; ++i) {
+            mbar_init(smem_u32(&s_done[i]), 1);
+            mbar_init(smem_u32(&s_free[i]), S::kEpiWarps);
+        }
+        for (int i = 0; i < kSlots; ++i) {
+            mbar_init(smem_u32(&s_scaled[i]), 32);
+            mbar_init(smem_u32(&s_slot[i]), S::kEpiWarps);
+        }
+        mbar_init(smem_u32(&s_drain), 1);
+    }
+    if (warp == 1) {
+        tmem_alloc(smem_u32(&s_tmem), S::kColumns);
+        tmem_relinquish();
+    }
+    fence_barrier_init();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
+    const int u0 = blockIdx.x * a.share, count = min(u0 + a.share, a.units) - u0;
+    bool ok = true;
+    auto wait = [&](uint64_t& bar, int parity) { ok = mbar_wait_warp(smem_u32(&bar), parity, a.wait_budget, ok); };
+    grid_launch_dependents();
+
+    if (warp == 0) {
+        // ======== loads ========
+        Unit here(a, u0), ahead = here;
+        auto weights = [&](int stage) {
+            if (elect_one()) {
+                const uint32_t bar = smem_u32(&s_full[stage]);
+                mbar_arrive_expect_tx(bar, S::kStage);
+                tma_load_2d(base + stage * S::kStage, &w_map, bar, 0, (ahead.tile / a.row_tiles * a.k_blocks + ahead.kb) * kF8Block);
+            }
+            __syncwarp();
+            ahead.next(a);
+        };
+        auto rows = [&](int stage) {
+            if (elect_one())
+                tma_load_2d(base + stage * S::kStage + kTileBytes, &x_map, smem_u32(&s_full[stage]), here.kb * kF8Block, here.tile % a.row_tiles * kN);
+            __syncwarp();
+            here.next(a);
+        };
+        const int early = min(S::kStages, count);
+        for (int i = 0; i < early; ++i) weights(i);    // they were there when the layer was made
+        grid_dependency_wait();                        // all else is waited for
+        for (int i = 0; i < early; ++i) rows(i);
+        int issued = early, stage = 0, round = 0;
+        for (; issued < count; ++issued) {
+            wait(s_empty[stage], round & 1);
+            if (!ok) break;
+            weights(stage);
+            rows(stage);
+            if (++stage == S::kStages) {
+                stage = 0;
+                ++round;
+            }
+        }
+        // nothing may be in flight when the CTA ends
+        for (int j = max(0, issued - S::kStages); j < issued; ++j) ok = mbar_wait_warp(smem_u32(&s_full[j % S::kStages]), (j / S::kStages) & 1, kDrainBudget, ok);
+    } else if (warp == 1) {
+        // ======== products ========
+        int stage = 0, round = 0, buffer = 0, turn = 0;
+        for (int i = 0; i < count; ++i) {
+            if (i >= S::kBuffers) wait(s_free[buffer], (turn & 1) ^ 1);
+            if (ok) wait(s_full[stage], round & 1);
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+                const uint64_t w = make_kmajor_desc(base + stage * S::kStage, 128), x = make_kmajor_desc(base + stage * S::kStage + kTileBytes, 128);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) mma_f8(tmem + buffer * kN, w + 2 * k, x + 2 * k, kProduct<128, kN>, k > 0);
+                mma_commit(smem_u32(&s_empty[stage]));
+                mma_commit(smem_u32(&s_done[buffer]));
+            }
+            __syncwarp();
+            if (++stage == S::kStages) {
+                stage = 0;
+                ++round;
+            }
+            if (++buffer == S::kBuffers) {
+                buffer = 0;
+                ++turn;
+            }
+        }
+        if (elect_one()) mma_commit(smem_u32(&s_drain));   // the others may have given up on what is still running
+        __syncwarp();
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_drain), 0, kDrainBudget)) && ok;
+    } else if (warp == 2) {
+        // ======== scales of x ========
+        grid_dependency_wait();
+        Unit here(a, u0);
+        for (int i = 0; i < count; ++i) {
+            const int slot = i % kSlots;
+            if (i >= kSlots) wait(s_slot[slot], (i / kSlots & 1) ^ 1);
+            if (!ok) break;
+            const int64_t r0 = static_cast<int64_t>(here.tile % a.row_tiles) * kN;
+            for (int r = lane; r < kN; r += 32)
+                cp_async_4(smem_u32(&s_scales[slot][r]), a.x_scales + min(r0 + r, a.rows - 1) * a.row_stride + here.kb * a.block_stride);
+            cp_async_arrive(smem_u32(&s_scaled[slot]));
+            here.next(a);
+        }
+        cp_async_commit();
+        cp_async_wait<0>();
+    } else if (warp >= 4) {
+        // ======== sums ========
+        const int part = (warp - 4) >> 2, o_lane = (warp & 3) * 32 + lane;
+        const uint32_t from = tmem + (static_cast<uint32_t>(warp & 3) << 21) + part * S::kCols;
+        float acc[S::kCols];
+#pragma unroll
+        for (int c = 0; c < S::kCols; ++c) acc[c] = 0.f;
+        grid_dependency_wait();                        // y may be what the kernel before reads
+        Unit here(a, u0);
+        int buffer = 0, turn = 0;
+        for (int i = 0; i < count; ++i) {
+            const int slot = i % kSlots, n_tile = here.tile / a.row_tiles;
+            const float w_scale = __ldg(a.w_scales + static_cast<int64_t>(n_tile) * a.k_blocks + here.kb);
+            wait(s_scaled[slot], i / kSlots & 1);
+            if (ok) wait(s_done[buffer], turn & 1);
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll
+            for (int c0 = 0; c0 < S::kCols; c0 += 16) {
+                uint32_t v[16];
+                tmem_ld_32x16(from + buffer * kN + c0, v);
+                tmem_ld_wait_for(v);
+#pragma unroll
+                for (int c = 0; c < 16; c += 4) {
+                    const float4 s = *reinterpret_cast<const float4*>(&s_scales[slot][part * S::kCols + c0 + c]);
+                    acc[c0 + c] = fmaf(__uint_as_float(v[c]), s.x * w_scale, acc[c0 + c]);
+                    acc[c0 + c + 1] = fmaf(__uint_as_float(v[c + 1]), s.y * w_scale, acc[c0 + c + 1]);
+                    acc[c0 + c + 2] = fmaf(__uint_as_float(v[c + 2]), s.z * w_scale, acc[c0 + c + 2]);
+                    acc[c0 + c + 3] = fmaf(__uint_as_float(v[c + 3]), s.w * w_scale, acc[c0 + c + 3]);
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                mbar_arrive(smem_u32(&s_free[buffer]));
+                mbar_arrive(smem_u32(&s_slot[slot]));
+            }
+            if (++buffer == S::kBuffers) {
+                buffer = 0;
+                ++turn;
+            }
+            const bool ends = here.kb == a.k_blocks - 1;
+            if (ends || i == count - 1) {              // the end of this tile, or of this CTA's columns of it
+                const bool begins = i >= here.kb;
+                if (begins && ends) {
+                    const int o = n_tile * kF8Block + o_lane;
+                    const int64_t r0 = static_cast<int64_t>(here.tile % a.row_tiles) * kN + part * S::kCols;
+                    const float b = bias_of(a, o);
+                    if (o < a.n) {
+#pragma unroll
+                        for (int c = 0; c < S::kCols; ++c)
+                            if (r0 + c < a.rows) put(a, (r0 + c) * a.y_stride + o, acc[c] + b);
+                    }
+                } else {
+                    if (tid == 128) s_open[begins ? 1 : 0] = u0 + i;
+                    float* const to = part_of<kN>(a, blockIdx.x, begins ? 1 : 0) + part * S::kCols * kF8Block + o_lane;
+#pragma unroll
+                    for (int c = 0; c < S::kCols; ++c) to[c * kF8Block] = acc[c];
+                }
+#pragma unroll
+                for (int c = 0; c < S::kCols; ++c) acc[c] = 0.f;
+            }
+            here.next(a);
+        }
+    }
+    if (!ok) {
+        timed_out(a);
+        s_failed = 1;
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, S::kColumns);
+    }
+    if (!s_failed) join_tiles<kN>(a, s_open, tid, S::kThreads, s_last);   // after a wait that gave up the results are void
+}
+
+// ---- many rows: CTA pairs on tiles of 256 rows of x and 256 weights ----
+// Each CTA of a pair holds 128 of the rows and 128 of the weights; its half of the product, 128 rows x 256 columns, lies in its own
+// tensor memory, twice, so that one block of 128 columns is multiplied while the sums of the one before are taken.  A thread owns a row
+// of x and half of the columns, which share a scale of the weights: one factor a thread and block.
+constexpr int kPairThreads = 384;      // four warps that load, multiply and fetch scales, eight for the sums
+constexpr int kPairLaunch = 168, kPairFew = 56, kPairMany = 224;   // registers of a thread: at launch, then of either
+static_assert(4 * 32 * kPairFew + 8 * 32 * kPairMany <= kPairThreads * kPairLaunch, "more registers than the CTA was launched with");
+constexpr int kPairStage = 2 * kTileBytes;
+constexpr int kPairStages = (kSmemLimit - 1024 - 1024 - kSlots * 130 * 4) / kPairStage;
+constexpr int kBand = 16;              // row tiles that the pairs work on side by side, for the L2
+
+struct PairTile {
+    int row, col;                      // in tiles of 256
+    __device__ PairTile(const LinearArgs& a, int tile)
+    {
+        const int cols = (a.n_tiles + 1) / 2, band = tile / (kBand * cols), rest = tile - band * kBand * cols;
+        const int tall = min(kBand, a.row_tiles - band * kBand);
+        col = rest / tall;
+        row = band * kBand + rest % tall;
+    }
+};
+
+__global__ void __launch_bounds__(kPairThreads, 1)
+pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map)
+{
+    extern __shared__ uint8_t smem_raw[];              // the ring: a tile of x, a tile of weights
+    __shared__ float s_x[kSlots][kF8Block], s_w[kSlots][2];            // scales
+    __shared__ __align__(8) uint64_t s_full[kPairStages], s_empty[kPairStages], s_done[2], s_free[2], s_scaled[kSlots], s_slot[kSlots], s_drain;
+    __shared__ uint32_t s_tmem;
+    const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, rank = cluster_ctarank();
+    if (tid == 0) {
+        prefetch_tensormap(&w_map);
+        prefetch_tensormap(&x_map);
+        for (int i = 0; i < kPairStages; ++i) {
+            mbar_init(smem_u32(&s_full[i]), 1);
+            mbar_init(smem_u32(&s_empty[i]), 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&s_done[i]), 1);
+            mbar_init(smem_u32(&s_free[i]), 16);
+        }
+        for (int i = 0; i < kSlots; ++i) {
+            mbar_init(smem_u32(&s_scaled[i]), 32);
+            mbar_init(smem_u32(&s_slot[i]), 8);
+        }
+        mbar_init(smem_u32(&s_drain), 1);
+    }
+    if (warp == 1) {
+        tmem_alloc_pair(smem_u32(&s_tmem), 512);
+        tmem_relinquish_pair();
+    }
+    fence_barrier_init();
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync();                                    // both CTAs' barriers are there
+    tc_fence_after();
+    const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
+    const int tile0 = blockIdx.x / 2, step = gridDim.x / 2, tiles = a.units;
+    bool ok = true;
+    grid_launch_dependents();
+
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPairFew));
+        if (warp == 0) {
+            // ======== loads: both CTAs' are counted on the first one's barrier ========
+            grid_dependency_wait();
+            int stage = 0, round = 0, issued = 0;
+            for (int tile = tile0; ok && tile < tiles; tile += step) {
+                const PairTile at(a, tile);
+                const int w_tile = min(2 * at.col + static_cast<int>(rank), a.n_tiles - 1), x_row = (2 * at.row + static_cast<int>(rank)) * kF8Block;
+                for (int kb = 0; kb < a.k_blocks; ++kb) {
+                    if (issued >= kPairStages) ok = mbar_wait_warp(smem_u32(&s_empty[stage]), (round & 1) ^ 1, a.wait_budget, ok);
+                    if (!ok) break;
+                    if (elect_one()) {
+                        const uint32_t own = smem_u32(&s_full[stage]), to = base + stage * kPairStage;
+                        if (rank == 0) mbar_arrive_expect_tx(own, 2 * kPairStage);
+                        const uint32_t bar = mapa_shared(own, 0u);
+                        tma_load_2d_pair(to, &x_map, bar, kb * kF8Block, x_row);
+                        tma_load_2d_pair(to + kTileBytes, &w_map, bar, 0, (w_tile * a.k_blocks + kb) * kF8Block);
+                    }
+                    __syncwarp();
+                    ++issued;
+                    if (++stage == kPairStages) {
+                        stage = 0;
+                        ++round;
+                    }
+                }
+            }
+            // nothing may be in flight when the CTAs end
+            if (rank == 0)
+                for (int j = max(0, issued - kPairStages); j < issued; ++j)
+                    ok = mbar_wait_warp(smem_u32(&s_full[j % kPairStages]), (j / kPairStages) & 1, kDrainBudget, ok);
+        } else if (warp == 1 && rank == 0) {
+            // ======== products ========
+            int stage = 0, round = 0, block = 0;
+            for (int tile = tile0; ok && tile < tiles; tile += step) {
+                for (int kb = 0; kb < a.k_blocks; ++kb, ++block) {
+                    if (block >= 2) ok = __all_sync(0xffffffffu, mbar_wait_cluster(smem_u32(&s_free[block & 1]), (block >> 1 & 1) ^ 1, a.wait_budget));
+                    if (ok) ok = __all_sync(0xffffffffu, mbar_wait_cluster(smem_u32(&s_full[stage]), round & 1, a.wait_budget));
+                    if (!ok) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint64_t x = make_kmajor_desc(base + stage * kPairStage, 128), w = make_kmajor_desc(base + stage * kPairStage + kTileBytes, 128);
+    #pragma unroll
+                        for (int k = 0; k < 4; ++k) mma_f8_pair(tmem + (block & 1) * 256, x + 2 * k, w + 2 * k, kProduct<256, 256>, k > 0);
+                        mma_commit_pair(smem_u32(&s_empty[stage]));
+                        mma_commit_pair(smem_u32(&s_done[block & 1]));
+                    }
+                    __syncwarp();
+                    if (++stage == kPairStages) {
+                        stage = 0;
+                        ++round;
+                    }
+                }
+            }
+            if (elect_one()) mma_commit_pair(smem_u32(&s_drain));
+            __syncwarp();
+        } else if (warp == 2) {
+            // ======== scales ========
+            grid_dependency_wait();
+            int block = 0;
+            for (int tile = tile0; ok && tile < tiles; tile += step) {
+                const PairTile at(a, tile);
+                const int64_t row0 = (2 * static_cast<int64_t>(at.row) + rank) * kF8Block + lane;
+                const float* from[5];                      // four rows of x; lanes 0 and 1: a tile of weights
+    #pragma unroll
+                for (int j = 0; j < 4; ++j) from[j] = a.x_scales + min(row0 + 32 * j, a.rows - 1) * a.row_stride;
+                from[4] = a.w_scales + static_cast<int64_t>(min(2 * at.col + (lane & 1), a.n_tiles - 1)) * a.k_blocks;
+                for (int kb = 0; kb < a.k_blocks; ++kb, ++block) {
+                    const int slot = block % kSlots;
+                    if (block >= kSlots) ok = mbar_wait_warp(smem_u32(&s_slot[slot]), (block / kSlots & 1) ^ 1, a.wait_budget, ok);
+                    if (!ok) break;
+    #pragma unroll
+                    for (int j = 0; j < 4; ++j) cp_async_4(smem_u32(&s_x[slot][32 * j + lane]), from[j] + kb * a.block_stride);
+                    if (lane < 2) cp_async_4(smem_u32(&s_w[slot][lane]), from[4] + kb);
+                    cp_async_arrive(smem_u32(&s_scaled[slot]));
+                }
+            }
+            cp_async_commit();
+            cp_async_wait<0>();
+        }
+    } else {
+        // ======== sums ========
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPairMany));
+        const int half = (warp - 4) >> 2, row_lane = (warp & 3) * 32 + lane;
+        const uint32_t from = tmem + (static_cast<uint32_t>(warp & 3) << 21) + half * 128;
+        grid_dependency_wait();
+        int block = 0;
+        for (int tile = tile0; ok && tile < tiles; tile += step) {
+            float acc[128];
+#pragma unroll
+            for (int c = 0; c < 128; ++c) acc[c] = 0.f;
+#pragma unroll 1
+            for (int kb = 0; kb < a.k_blocks; ++kb, ++block) {
+                const int slot = block % kSlots;
+                ok = mbar_wait_warp(smem_u32(&s_scaled[slot]), block / kSlots & 1, a.wait_budget, ok);
+                const float s = s_x[slot][row_lane] * s_w[slot][half];
+                ok = mbar_wait_warp(smem_u32(&s_done[block & 1]), block >> 1 & 1, a.wait_budget, ok);
+                if (!ok) break;
+                tc_fence_after();
+                uint32_t v[2][32];
+                tmem_ld_32x32(from + (block & 1) * 256, v[0]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    tmem_ld_wait_for(v[j & 1]);
+                    if (j < 3) {
+                        tmem_ld_32x32(from + (block & 1) * 256 + 32 * (j + 1), v[(j + 1) & 1]);
+                    } else {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) {
+                            mbar_arrive_remote(smem_u32(&s_free[block & 1]), 0u);
+                            mbar_arrive(smem_u32(&s_slot[slot]));
+                        }
+                    }
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) acc[32 * j + c] = fmaf(__uint_as_float(v[j & 1][c]), s, acc[32 * j + c]);
+                }
+            }
+            if (!ok) break;
+            const PairTile at(a, tile);
+            const int64_t row = (2 * static_cast<int64_t>(at.row) + rank) * kF8Block + row_lane;
+            const int o = (2 * at.col + half) * kF8Block;
+            if (a.bias) {
+#pragma unroll
+                for (int c = 0; c < 128; ++c) acc[c] += bias_of(a, o + c);
+            }
+            if (row < a.rows) {
+#pragma unroll
+                for (int c = 0; c < 128; c += 8) put8(a, row * a.y_stride + o + c, a.n - o - c, acc + c);
+            }
+        }
+    }
+    if (!ok) timed_out(a);
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) (void)mbar_wait(smem_u32(&s_drain), 0, kDrainBudget);   // the products that the first CTA issued are done
+    __syncthreads();
+    cluster_sync();                                    // and no arrival of the other CTA is under way
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc_pair(tmem, 512);
+    }
+}
+
+// Scratch of the joining, shared by the layers of a handle: parts and counters of a full grid.
+qtz_status ensure_scratch(qtz_ctx* h, cudaStream_t st)
+{
+    if (h->f8_dev) return QTZ_OK;
+    cudaFuncAttributes at;
+    QTZ_CUDA(h, cudaFuncGetAttributes(&at, reinterpret_cast<const void*>(pair_kernel)));
+    if (at.numRegs < kPairLaunch) return QTZ_ERR_UNSUPPORTED;      // its warps would wait for registers that nobody gives back
+    const size_t parts = static_cast<size_t>(h->num_sms) * 2 * kF8Block * 128 * sizeof(float);
+    QTZ_CUDA(h, cudaMalloc(&h->f8_dev, parts + h->num_sms * sizeof(int32_t)));
+    QTZ_CUDA(h, cudaMemsetAsync(static_cast<uint8_t*>(h->f8_dev) + parts, 0, h->num_sms * sizeof(int32_t), st));
+    h->f8_counters = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(h->f8_dev) + parts);
+    return QTZ_OK;
+}
+
+template <int kN>
+qtz_status launch_stream(qtz_f8_layer* p, LinearArgs& a, const CUtensorMap& x_map, cudaStream_t st)
+{
+    qtz_ctx* h = p->h;
+    a.row_tiles = static_cast<int32_t>((a.rows + kN - 1) / kN);
+    a.units = a.row_tiles * a.n_tiles * a.k_blocks;
+    a.share = (a.units + h->num_sms - 1) / h->num_sms;
+    const qtz_status s = qtz_allow_smem(h, stream_kernel<kN>);
+    if (s != QTZ_OK) return s;
+    QTZ_CUDA(h, qtz_launch_dependent(stream_kernel<kN>, dim3((a.units + a.share - 1) / a.share), Stream<kN>::kThreads,
+                                     1024 + Stream<kN>::kStages * Stream<kN>::kStage, st, a, p->w_map, x_map));
+    return QTZ_OK;
+}
+
+qtz_status launch_pair(qtz_f8_layer* p, LinearArgs& a, const CUtensorMap& x_map, cudaStream_t st)
+{
+    qtz_ctx* h = p->h;
+    a.row_tiles = static_cast<int32_t>((a.rows + 255) / 256);
+    a.units = a.row_tiles * ((a.n_tiles + 1) / 2);
+    const qtz_status s = qtz_allow_smem(h, pair_kernel);
+    if (s != QTZ_OK) return s;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = 2;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2 * (a.units < h->num_sms / 2 ? a.units : h->num_sms / 2));
+    cfg.blockDim = dim3(kPairThreads);
+    cfg.dynamicSmemBytes = 1024 + kPairStages * kPairStage;
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    QTZ_CUDA(h, cudaLaunchKernelEx(&cfg, pair_kernel, a, p->w_map, x_map));
+    return QTZ_OK;
 }
 
 }  // namespace
@@ -122,6 +671,8 @@ extern "C" qtz_status qtz_f8_linear_create(qtz_handle h, int32_t n, int32_t k, c
     if (n_tiles > 65535 || n_tiles * k_blocks > (1 << 23)) return QTZ_ERR_TOO_LARGE;
     qtz_device_guard guard(h->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const qtz_status s = ensure_scratch(h, st);
+    if (s != QTZ_OK) return s;
     qtz_f8_layer* p = new (std::nothrow) qtz_f8_layer();
     if (!p) return QTZ_ERR_INVALID_ARG;
     p->h = h;
@@ -147,6 +698,9 @@ extern "C" qtz_status qtz_f8_linear_create(qtz_handle h, int32_t n, int32_t k, c
         e = cudaGetLastError();
     }
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);   // later calls may fetch the tiles before they wait for the stream
+    const uint64_t dims[2] = {kF8Block, blocks * kF8Block}, strides[1] = {kF8Block};
+    const uint32_t box[2] = {kF8Block, kF8Block};
+    if (e == cudaSuccess && !qtz_encode_u8_map(&p->w_map, p->tiles, 2, dims, strides, box, 128)) e = cudaErrorInvalidValue;
     if (e != cudaSuccess) {
         qtz_cuda_fail(h, e, "qtz_f8_linear_create");
         qtz_f8_linear_destroy(p);
@@ -164,12 +718,26 @@ extern "C" qtz_status qtz_f8_linear(qtz_f8_linear_plan p, const uint8_t* codes_d
     if (rows == 0) return QTZ_OK;
     if (!codes_dev || !scales_dev || !y_dev || (rows > 1 && (codes_stride < p->k || y_stride < p->n))) return QTZ_ERR_INVALID_ARG;
     if (!qtz_aligned16(codes_dev) || (rows > 1 && codes_stride % 16 != 0)) return QTZ_ERR_MISALIGNED;
+    // tiles of at least 16 rows of x, of 128 weights and of 128 columns are counted in 32 bits
+    if (rows > 0x7fffff00 || (rows + 127) / 128 * p->n_tiles * p->k_blocks > 0x3fffffff) return QTZ_ERR_TOO_LARGE;
     qtz_ctx* h = p->h;
     qtz_device_guard guard(h->device);
-    const LinearArgs a{p->tiles, codes_dev, p->scales, p->bias, scales_dev, codes_stride, scales_row_stride, scales_block_stride, rows, y_stride,
-                       y_dev, p->n, p->k, p->n_tiles, p->k_blocks, ftype};
-    const int64_t down = (rows + 31) / 32;
-    linear_kernel<<<dim3(static_cast<unsigned>((p->n + 31) / 32), static_cast<unsigned>(down < 65535 ? down : 65535)), 256, 0, static_cast<cudaStream_t>(stream)>>>(a);
-    QTZ_LAUNCH_CHECK(h, "linear_kernel");
-    return QTZ_OK;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    LinearArgs a{p->scales, p->bias, scales_dev, scales_row_stride, scales_block_stride, rows, y_stride, y_dev, p->n, p->n_tiles, p->k_blocks, ftype,
+                 qtz_aligned16(y_dev) && (rows <= 1 || y_stride * (ftype == QTZ_F32 ? 4 : 2) % 16 == 0), 0, 0, 0,
+                 static_cast<float*>(h->f8_dev), h->f8_counters, h->wait_budget, h->status_dev};
+    const bool pair = rows > 512;
+    const int box_rows = pair ? 128 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
+    CUtensorMap x_map;                                 // columns beyond k and rows beyond the last read as zero
+    const int64_t pitch = rows > 1 ? codes_stride : (p->k + 15) / 16 * 16;
+    const uint64_t dims[2] = {static_cast<uint64_t>(p->k), static_cast<uint64_t>(rows)}, strides[1] = {static_cast<uint64_t>(pitch)};
+    const uint32_t box[2] = {kF8Block, static_cast<uint32_t>(box_rows)};
+    if (!qtz_encode_u8_map(&x_map, codes_dev, 2, dims, strides, box, 128)) return qtz_cuda_fail(h, cudaErrorInvalidValue, "tensor map of the activations");
+    if (pair) return launch_pair(p, a, x_map, st);
+    switch (box_rows) {
+    case 16: return launch_stream<16>(p, a, x_map, st);
+    case 32: return launch_stream<32>(p, a, x_map, st);
+    case 64: return launch_stream<64>(p, a, x_map, st);
+    default: return launch_stream<128>(p, a, x_map, st);
+    }
 }

@@ -27,6 +27,8 @@ struct qtz_ctx {
     size_t reduce_host_bytes = 0;
     void* linear_dev = nullptr;             // parts and counters of linear layers (allocated with the first layer)
     int32_t* linear_counters = nullptr;     // within it
+    void* f8_dev = nullptr;                 // the same of 8-bit floating-point layers
+    int32_t* f8_counters = nullptr;
     const void* smem_ready[128] = {};       // kernels that may use all of an SM's shared memory (qtz_allow_smem)
     int smem_ready_count = 0;
     bool no_pairs = false;                  // never run layers on CTA pairs (A/B comparisons; set by QTZ_NO_PAIRS=1)
@@ -41,7 +43,8 @@ enum qtz_kernel_family { QTZ_K_DIRECT = 0, QTZ_K_TCGEN05 = 1, QTZ_K_DEPTHWISE = 
 enum { QTZ_SITE_TMA_FULL = 1, QTZ_SITE_SMEM_EMPTY = 2, QTZ_SITE_TMEM_FULL = 3,
        QTZ_SITE_TMEM_EMPTY = 4, QTZ_SITE_STORE = 5, QTZ_SITE_OUT_FULL = 6, QTZ_SITE_OUT_EMPTY = 7,
        QTZ_SITE_SELFTEST = 8, QTZ_SITE_PROBE = 9,
-       QTZ_SITE_KV_APPEND = 10, QTZ_SITE_KV_READ = 11, QTZ_SITE_KV_ATTENTION = 12, QTZ_SITE_LINEAR = 13 };
+       QTZ_SITE_KV_APPEND = 10, QTZ_SITE_KV_READ = 11, QTZ_SITE_KV_ATTENTION = 12, QTZ_SITE_LINEAR = 13,
+       QTZ_SITE_F8_LINEAR = 14 };
 
 inline qtz_status qtz_cuda_fail(qtz_ctx* h, cudaError_t e, const char* what)
 {
