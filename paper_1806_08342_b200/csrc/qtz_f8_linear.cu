@@ -22,7 +22,6 @@ struct qtz_f8_layer {
 namespace {
 
 using namespace qtz_ptx;
-
 struct PackArgs {
     const uint8_t* codes;
     int64_t stride;
@@ -80,26 +79,15 @@ __device__ __forceinline__ void put(const LinearArgs& a, int64_t at, float v)
     else static_cast<float*>(a.y)[at] = v;
 }
 
-// Eight neighbouring values of a row, of which `valid` exist.
-__device__ __forceinline__ void put8(const LinearArgs& a, int64_t at, int valid, const float* v)
+// (x, y) += (u, v) * (s, t), two fp32 sums in one operation.
+__device__ __forceinline__ void fma2(float& x, float& y, float u, float v, float s, float t)
 {
-    if (valid < 8 || !a.vector) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < valid) put(a, at + i, v[i]);
-    } else if (a.ftype == QTZ_F32) {
-        float4* const to = reinterpret_cast<float4*>(static_cast<float*>(a.y) + at);
-        to[0] = make_float4(v[0], v[1], v[2], v[3]);
-        to[1] = make_float4(v[4], v[5], v[6], v[7]);
-    } else if (a.ftype == QTZ_F16) {
-        using qtz_dev::pack2;
-        *reinterpret_cast<uint4*>(static_cast<__half*>(a.y) + at) =
-            make_uint4(pack2(v[0], v[1], __half()), pack2(v[2], v[3], __half()), pack2(v[4], v[5], __half()), pack2(v[6], v[7], __half()));
-    } else {
-        using qtz_dev::pack2;
-        using B = __nv_bfloat16;
-        *reinterpret_cast<uint4*>(static_cast<B*>(a.y) + at) = make_uint4(pack2(v[0], v[1], B()), pack2(v[2], v[3], B()), pack2(v[4], v[5], B()), pack2(v[6], v[7], B()));
-    }
+    unsigned long long sums, values, factors;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(sums) : "f"(x), "f"(y));
+    asm("mov.b64 %0, {%1, %2};" : "=l"(values) : "f"(u), "f"(v));
+    asm("mov.b64 %0, {%1, %2};" : "=l"(factors) : "f"(s), "f"(t));
+    asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(sums) : "l"(values), "l"(factors));
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(sums));
 }
 
 __device__ __forceinline__ float bias_of(const LinearArgs& a, int o) { return a.bias && o < a.n ? __ldg(a.bias + o) : 0.f; }
@@ -107,7 +95,10 @@ __device__ __forceinline__ float bias_of(const LinearArgs& a, int o) { return a.
 // ---- few rows: the weights stream past kN rows of x ----
 // The 128 weights of a tile are the rows of the product, the rows of x its columns.  Units (tile, block of 128 columns) form one
 // sequence that is dealt out in equal contiguous shares; a tile that lies in several shares is joined by the last CTA to arrive.
-constexpr int kSlots = 8;              // units whose scales are under way
+constexpr int kSlots = 8, kAhead = 4;  // places for the scales of units, and how many units ahead they are asked for
+
+__device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t (&v)[16]) { tmem_ld_32x16(taddr, v); }
+__device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t (&v)[32]) { tmem_ld_32x32(taddr, v); }
 
 template <int kN>
 struct Stream {
@@ -116,18 +107,19 @@ struct Stream {
     static constexpr int kStage = kTileBytes + kN * kF8Block;
     static constexpr int kBuffers = kN <= 64 ? 8 : 4;                                 // of kN columns of tensor memory
     static constexpr int kColumns = kN * kBuffers < 32 ? 32 : kN * kBuffers;
-    static constexpr int kStages = (kSmemLimit - 1024 - kSlots * kN * 4 - 1024) / kStage < kMaxStages ? (kSmemLimit - 1024 - kSlots * kN * 4 - 1024) / kStage : kMaxStages;
+    static constexpr int kRoom = (kSmemLimit - 1024 - kSlots * (kN + 1) * 4 - 1024) / kStage, kStages = kRoom < kMaxStages ? kRoom : kMaxStages;
 };
 
-struct Unit {
-    int tile, kb;
-    __device__ Unit(const LinearArgs& a, int u) : tile(u / a.k_blocks), kb(u % a.k_blocks) {}
+struct Unit {                          // 128 weights, kN rows of x, 128 columns; row tiles of the same weights follow each other
+    int n_tile, row_tile, kb;
+    __device__ Unit(const LinearArgs& a, int u) : n_tile(u / a.k_blocks / a.row_tiles), row_tile(u / a.k_blocks % a.row_tiles), kb(u % a.k_blocks) {}
     __device__ void next(const LinearArgs& a)
     {
-        if (++kb == a.k_blocks) {
-            kb = 0;
-            ++tile;
-        }
+        if (++kb < a.k_blocks) return;
+        kb = 0;
+        if (++row_tile < a.row_tiles) return;
+        row_tile = 0;
+        ++n_tile;
     }
 };
 
@@ -195,8 +187,9 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
 {
     using S = Stream<kN>;
     extern __shared__ uint8_t smem_raw[];              // the ring: a tile of weights, kN rows of x
-    __shared__ __align__(16) float s_scales[kSlots][kN];
-    __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_done[S::kBuffers], s_free[S::kBuffers], s_scaled[kSlots], s_slot[kSlots], s_drain;
+    __shared__ __align__(16) float s_x[kSlots][kN];    // scales
+    __shared__ float s_w[kSlots];
+    __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_done[S::kBuffers], s_free[S::kBuffers], s_drain;
     __shared__ int s_open[2], s_last[2], s_failed;     // s_open: units whose tiles are shared with an earlier / a later CTA
     __shared__ uint32_t s_tmem;
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -211,12 +204,8 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
             mbar_init(smem_u32(&s_empty[i]), 1);
         }
         for (int i = 0; i < S::kBuffers; ++i) {
-            mbar_init(smem_u32(&s_done[i]), 1);
+            mbar_init(smem_u32(&s_done[i]), 2);        // the product and its scales
             mbar_init(smem_u32(&s_free[i]), S::kEpiWarps);
-        }
-        for (int i = 0; i < kSlots; ++i) {
-            mbar_init(smem_u32(&s_scaled[i]), 32);
-            mbar_init(smem_u32(&s_slot[i]), S::kEpiWarps);
         }
         mbar_init(smem_u32(&s_drain), 1);
     }
@@ -241,14 +230,13 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
             if (elect_one()) {
                 const uint32_t bar = smem_u32(&s_full[stage]);
                 mbar_arrive_expect_tx(bar, S::kStage);
-                tma_load_2d(base + stage * S::kStage, &w_map, bar, 0, (ahead.tile / a.row_tiles * a.k_blocks + ahead.kb) * kF8Block);
+                tma_load_2d(base + stage * S::kStage, &w_map, bar, 0, (ahead.n_tile * a.k_blocks + ahead.kb) * kF8Block);
             }
             __syncwarp();
             ahead.next(a);
         };
         auto rows = [&](int stage) {
-            if (elect_one())
-                tma_load_2d(base + stage * S::kStage + kTileBytes, &x_map, smem_u32(&s_full[stage]), here.kb * kF8Block, here.tile % a.row_tiles * kN);
+            if (elect_one()) tma_load_2d(base + stage * S::kStage + kTileBytes, &x_map, smem_u32(&s_full[stage]), here.kb * kF8Block, here.row_tile * kN);
             __syncwarp();
             here.next(a);
         };
@@ -271,47 +259,57 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
         for (int j = max(0, issued - S::kStages); j < issued; ++j) ok = mbar_wait_warp(smem_u32(&s_full[j % S::kStages]), (j / S::kStages) & 1, kDrainBudget, ok);
     } else if (warp == 1) {
         // ======== products ========
-        int stage = 0, round = 0, buffer = 0, turn = 0;
+        int stage = 0, round = 0;
         for (int i = 0; i < count; ++i) {
-            if (i >= S::kBuffers) wait(s_free[buffer], (turn & 1) ^ 1);
-            if (ok) wait(s_full[stage], round & 1);
+            const int buffer = i % S::kBuffers;
+            wait(s_full[stage], round & 1);
+            if (i >= S::kBuffers) wait(s_free[buffer], (i / S::kBuffers & 1) ^ 1);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
                 const uint64_t w = make_kmajor_desc(base + stage * S::kStage, 128), x = make_kmajor_desc(base + stage * S::kStage + kTileBytes, 128);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) mma_f8(tmem + buffer * kN, w + 2 * k, x + 2 * k, kProduct<128, kN>, k > 0);
-                mma_commit(smem_u32(&s_empty[stage]));
                 mma_commit(smem_u32(&s_done[buffer]));
+                mma_commit(smem_u32(&s_empty[stage]));
             }
             __syncwarp();
             if (++stage == S::kStages) {
                 stage = 0;
                 ++round;
             }
-            if (++buffer == S::kBuffers) {
-                buffer = 0;
-                ++turn;
-            }
         }
         if (elect_one()) mma_commit(smem_u32(&s_drain));   // the others may have given up on what is still running
         __syncwarp();
         ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_drain), 0, kDrainBudget)) && ok;
     } else if (warp == 2) {
-        // ======== scales of x ========
+        // ======== scales: on their way kAhead units ahead, counted with the unit's product ========
         grid_dependency_wait();
         Unit here(a, u0);
-        for (int i = 0; i < count; ++i) {
-            const int slot = i % kSlots;
-            if (i >= kSlots) wait(s_slot[slot], (i / kSlots & 1) ^ 1);
-            if (!ok) break;
-            const int64_t r0 = static_cast<int64_t>(here.tile % a.row_tiles) * kN;
-            for (int r = lane; r < kN; r += 32)
-                cp_async_4(smem_u32(&s_scales[slot][r]), a.x_scales + min(r0 + r, a.rows - 1) * a.row_stride + here.kb * a.block_stride);
-            cp_async_arrive(smem_u32(&s_scaled[slot]));
-            here.next(a);
+        for (int i = 0; i < count + kAhead; ++i) {
+            const int now = i - kAhead;
+            if (now >= 0) {
+                cp_async_wait<kAhead - 1>();
+                __syncwarp();
+                if (now >= S::kBuffers) wait(s_done[now % S::kBuffers], (now / S::kBuffers & 1) ^ 1);
+                if (!ok) break;
+                if (lane == 0) mbar_arrive(smem_u32(&s_done[now % S::kBuffers]));
+            }
+            if (i < count) {
+                // the place's unit, kSlots before, has been used up where the one after it has been read
+                const int next = i - kSlots + 1;
+                if (next >= 1) wait(s_free[next % S::kBuffers], next / S::kBuffers & 1);
+                if (!ok) break;
+                const int slot = i % kSlots;
+                const int64_t r0 = static_cast<int64_t>(here.row_tile) * kN;
+#pragma unroll
+                for (int r = lane; r < kN; r += 32)
+                    cp_async_4(smem_u32(&s_x[slot][r]), a.x_scales + min(r0 + r, a.rows - 1) * a.row_stride + here.kb * a.block_stride);
+                if (lane == 0) cp_async_4(smem_u32(&s_w[slot]), a.w_scales + static_cast<int64_t>(here.n_tile) * a.k_blocks + here.kb);
+                here.next(a);
+            }
+            cp_async_commit();
         }
-        cp_async_commit();
         cp_async_wait<0>();
     } else if (warp >= 4) {
         // ======== sums ========
@@ -322,44 +320,34 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
         for (int c = 0; c < S::kCols; ++c) acc[c] = 0.f;
         grid_dependency_wait();                        // y may be what the kernel before reads
         Unit here(a, u0);
-        int buffer = 0, turn = 0;
         for (int i = 0; i < count; ++i) {
-            const int slot = i % kSlots, n_tile = here.tile / a.row_tiles;
-            const float w_scale = __ldg(a.w_scales + static_cast<int64_t>(n_tile) * a.k_blocks + here.kb);
-            wait(s_scaled[slot], i / kSlots & 1);
-            if (ok) wait(s_done[buffer], turn & 1);
+            const int slot = i % kSlots, buffer = i % S::kBuffers;
+            wait(s_done[buffer], i / S::kBuffers & 1);
             if (!ok) break;
             tc_fence_after();
+            constexpr int kPiece = S::kCols < 32 ? 16 : 32;
+            uint32_t v[S::kCols / kPiece][kPiece];
 #pragma unroll
-            for (int c0 = 0; c0 < S::kCols; c0 += 16) {
-                uint32_t v[16];
-                tmem_ld_32x16(from + buffer * kN + c0, v);
-                tmem_ld_wait_for(v);
-#pragma unroll
-                for (int c = 0; c < 16; c += 4) {
-                    const float4 s = *reinterpret_cast<const float4*>(&s_scales[slot][part * S::kCols + c0 + c]);
-                    acc[c0 + c] = fmaf(__uint_as_float(v[c]), s.x * w_scale, acc[c0 + c]);
-                    acc[c0 + c + 1] = fmaf(__uint_as_float(v[c + 1]), s.y * w_scale, acc[c0 + c + 1]);
-                    acc[c0 + c + 2] = fmaf(__uint_as_float(v[c + 2]), s.z * w_scale, acc[c0 + c + 2]);
-                    acc[c0 + c + 3] = fmaf(__uint_as_float(v[c + 3]), s.w * w_scale, acc[c0 + c + 3]);
-                }
-            }
+            for (int p = 0; p < S::kCols / kPiece; ++p) tmem_load(from + buffer * kN + p * kPiece, v[p]);
+            tmem_ld_wait_for(v[0]);
+            if constexpr (S::kCols == 64) tmem_ld_tie(v[1]);
             tc_fence_before();
             __syncwarp();
-            if (lane == 0) {
-                mbar_arrive(smem_u32(&s_free[buffer]));
-                mbar_arrive(smem_u32(&s_slot[slot]));
-            }
-            if (++buffer == S::kBuffers) {
-                buffer = 0;
-                ++turn;
+            if (lane == 0) mbar_arrive(smem_u32(&s_free[buffer]));
+            const float w_scale = s_w[slot];
+#pragma unroll
+            for (int c = 0; c < S::kCols; c += 4) {
+                const float4 s = *reinterpret_cast<const float4*>(&s_x[slot][part * S::kCols + c]);
+                const uint32_t* const p = v[c / kPiece] + c % kPiece;
+                fma2(acc[c], acc[c + 1], __uint_as_float(p[0]), __uint_as_float(p[1]), s.x * w_scale, s.y * w_scale);
+                fma2(acc[c + 2], acc[c + 3], __uint_as_float(p[2]), __uint_as_float(p[3]), s.z * w_scale, s.w * w_scale);
             }
             const bool ends = here.kb == a.k_blocks - 1;
             if (ends || i == count - 1) {              // the end of this tile, or of this CTA's columns of it
                 const bool begins = i >= here.kb;
                 if (begins && ends) {
-                    const int o = n_tile * kF8Block + o_lane;
-                    const int64_t r0 = static_cast<int64_t>(here.tile % a.row_tiles) * kN + part * S::kCols;
+                    const int o = here.n_tile * kF8Block + o_lane;
+                    const int64_t r0 = static_cast<int64_t>(here.row_tile) * kN + part * S::kCols;
                     const float b = bias_of(a, o);
                     if (o < a.n) {
 #pragma unroll
@@ -396,10 +384,11 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
 // tensor memory, twice, so that one block of 128 columns is multiplied while the sums of the one before are taken.  A thread owns a row
 // of x and half of the columns, which share a scale of the weights: one factor a thread and block.
 constexpr int kPairThreads = 384;      // four warps that load, multiply and fetch scales, eight for the sums
-constexpr int kPairLaunch = 168, kPairFew = 56, kPairMany = 224;   // registers of a thread: at launch, then of either
+constexpr int kPairLaunch = 168, kPairFew = 80, kPairMany = 208;   // registers of a thread: at launch, then of either
 static_assert(4 * 32 * kPairFew + 8 * 32 * kPairMany <= kPairThreads * kPairLaunch, "more registers than the CTA was launched with");
 constexpr int kPairStage = 2 * kTileBytes;
-constexpr int kPairStages = (kSmemLimit - 1024 - 1024 - kSlots * 130 * 4) / kPairStage;
+constexpr int kPairStages = 6;          // what the rows on their way to y leave room for
+constexpr int kPairOut = 2048;         // bytes of a warp on their way to y: 32 rows of 64
 constexpr int kBand = 16;              // row tiles that the pairs work on side by side, for the L2
 
 struct PairTile {
@@ -413,12 +402,56 @@ struct PairTile {
     }
 };
 
+template <typename T>
+__device__ __forceinline__ uint4 pack16(const float* v)
+{
+    if constexpr (sizeof(T) == 4) return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    else return make_uint4(qtz_dev::pack2(v[0], v[1], T()), qtz_dev::pack2(v[2], v[3], T()), qtz_dev::pack2(v[4], v[5], T()), qtz_dev::pack2(v[6], v[7], T()));
+}
+
+// A warp's 32 rows of y (from row0 on) of 128 columns (from o on); lane l holds row l.  64 bytes of each row at a time cross through `out` so
+// that neighbouring lanes write neighbouring values; pieces of 16 bytes are shifted by row, for the banks.
+template <typename T>
+__device__ __forceinline__ void put_rows(const LinearArgs& a, uint4* out, const float (&acc)[128], int64_t row0, int o)
+{
+    constexpr int kPer = 16 / sizeof(T), kCols = 64 / sizeof(T);
+    const int lane = threadIdx.x & 31, rows = static_cast<int>(min(static_cast<int64_t>(32), a.rows - row0));
+    T* const y = static_cast<T*>(a.y);
+#pragma unroll
+    for (int c0 = 0; c0 < 128; c0 += kCols) {
+        const int cols = min(kCols, a.n - o - c0);
+        __syncwarp();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) out[lane * 4 + (q ^ (lane >> 1 & 3))] = pack16<T>(acc + c0 + q * kPer);
+        __syncwarp();
+        if (a.vector) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = i * 8 + (lane >> 2), q = lane & 3;
+                const uint4 v = out[r * 4 + (q ^ (r >> 1 & 3))];
+                T* const to = y + (row0 + r) * a.y_stride + o + c0 + q * kPer;
+                if (r < rows && q * kPer + kPer <= cols) {
+                    *reinterpret_cast<uint4*>(to) = v;
+                } else if (r < rows) {
+                    const T* const one = reinterpret_cast<const T*>(out + r * 4 + (q ^ (r >> 1 & 3)));
+                    for (int e = 0; e < cols - q * kPer; ++e) to[e] = one[e];
+                }
+            }
+        } else {
+            for (int at = lane; at < 32 * kCols; at += 32) {
+                const int r = at / kCols, e = at % kCols;
+                if (r < rows && e < cols) y[(row0 + r) * a.y_stride + o + c0 + e] = reinterpret_cast<const T*>(out + r * 4 + (e / kPer ^ (r >> 1 & 3)))[e % kPer];
+            }
+        }
+    }
+}
+
 __global__ void __launch_bounds__(kPairThreads, 1)
 pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map)
 {
     extern __shared__ uint8_t smem_raw[];              // the ring: a tile of x, a tile of weights
     __shared__ float s_x[kSlots][kF8Block], s_w[kSlots][2];            // scales
-    __shared__ __align__(8) uint64_t s_full[kPairStages], s_empty[kPairStages], s_done[2], s_free[2], s_scaled[kSlots], s_slot[kSlots], s_drain;
+    __shared__ __align__(8) uint64_t s_full[kPairStages], s_empty[kPairStages], s_done[2], s_free[2], s_drain;
     __shared__ uint32_t s_tmem;
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, rank = cluster_ctarank();
@@ -430,14 +463,10 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
             mbar_init(smem_u32(&s_empty[i]), 1);
         }
         for (int i = 0; i < 2; ++i) {
-            mbar_init(smem_u32(&s_done[i]), 1);
+            mbar_init(smem_u32(&s_done[i]), 2);
             mbar_init(smem_u32(&s_free[i]), 16);
         }
-        for (int i = 0; i < kSlots; ++i) {
-            mbar_init(smem_u32(&s_scaled[i]), 32);
-            mbar_init(smem_u32(&s_slot[i]), 8);
-        }
-        mbar_init(smem_u32(&s_drain), 1);
+        mbar_init(smem_u32(&s_drain), 2);
     }
     if (warp == 1) {
         tmem_alloc_pair(smem_u32(&s_tmem), 512);
@@ -484,53 +513,65 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
             if (rank == 0)
                 for (int j = max(0, issued - kPairStages); j < issued; ++j)
                     ok = mbar_wait_warp(smem_u32(&s_full[j % kPairStages]), (j / kPairStages) & 1, kDrainBudget, ok);
-        } else if (warp == 1 && rank == 0) {
-            // ======== products ========
-            int stage = 0, round = 0, block = 0;
-            for (int tile = tile0; ok && tile < tiles; tile += step) {
-                for (int kb = 0; kb < a.k_blocks; ++kb, ++block) {
-                    if (block >= 2) ok = __all_sync(0xffffffffu, mbar_wait_cluster(smem_u32(&s_free[block & 1]), (block >> 1 & 1) ^ 1, a.wait_budget));
-                    if (ok) ok = __all_sync(0xffffffffu, mbar_wait_cluster(smem_u32(&s_full[stage]), round & 1, a.wait_budget));
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (elect_one()) {
-                        const uint64_t x = make_kmajor_desc(base + stage * kPairStage, 128), w = make_kmajor_desc(base + stage * kPairStage + kTileBytes, 128);
-    #pragma unroll
-                        for (int k = 0; k < 4; ++k) mma_f8_pair(tmem + (block & 1) * 256, x + 2 * k, w + 2 * k, kProduct<256, 256>, k > 0);
-                        mma_commit_pair(smem_u32(&s_empty[stage]));
-                        mma_commit_pair(smem_u32(&s_done[block & 1]));
-                    }
-                    __syncwarp();
-                    if (++stage == kPairStages) {
-                        stage = 0;
-                        ++round;
-                    }
+        } else if (warp != 2) {
+            // ======== products: a warp for the even blocks, one for the odd ones ========
+            const int blocks = rank == 0 ? (tiles - tile0 + step - 1) / step * a.k_blocks : 0, buffer = warp >> 1;
+            int stage = buffer, round = 0;
+            for (int block = buffer; block < blocks; block += 2) {
+                ok = mbar_wait_warp(smem_u32(&s_full[stage]), round & 1, a.wait_budget, ok);
+                if (block >= 2) ok = mbar_wait_warp(smem_u32(&s_free[buffer]), (block >> 1 & 1) ^ 1, a.wait_budget, ok);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint64_t x = make_kmajor_desc(base + stage * kPairStage, 128), w = make_kmajor_desc(base + stage * kPairStage + kTileBytes, 128);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) mma_f8_pair(tmem + buffer * 256, x + 2 * k, w + 2 * k, kProduct<256, 256>, k > 0);
+                    mma_commit_pair(smem_u32(&s_done[buffer]));
+                    mma_commit_pair(smem_u32(&s_empty[stage]));
+                }
+                __syncwarp();
+                stage += 2;
+                if (stage >= kPairStages) {
+                    stage -= kPairStages;
+                    ++round;
                 }
             }
-            if (elect_one()) mma_commit_pair(smem_u32(&s_drain));
+            if (rank == 0 && elect_one()) mma_commit_pair(smem_u32(&s_drain));
             __syncwarp();
         } else if (warp == 2) {
-            // ======== scales ========
+            // ======== scales: on their way four blocks ahead, counted with the products of the block ========
             grid_dependency_wait();
-            int block = 0;
-            for (int tile = tile0; ok && tile < tiles; tile += step) {
-                const PairTile at(a, tile);
-                const int64_t row0 = (2 * static_cast<int64_t>(at.row) + rank) * kF8Block + lane;
-                const float* from[5];                      // four rows of x; lanes 0 and 1: a tile of weights
-    #pragma unroll
-                for (int j = 0; j < 4; ++j) from[j] = a.x_scales + min(row0 + 32 * j, a.rows - 1) * a.row_stride;
-                from[4] = a.w_scales + static_cast<int64_t>(min(2 * at.col + (lane & 1), a.n_tiles - 1)) * a.k_blocks;
-                for (int kb = 0; kb < a.k_blocks; ++kb, ++block) {
-                    const int slot = block % kSlots;
-                    if (block >= kSlots) ok = mbar_wait_warp(smem_u32(&s_slot[slot]), (block / kSlots & 1) ^ 1, a.wait_budget, ok);
+            const int blocks = (tiles - tile0 + step - 1) / step * a.k_blocks;
+            int tile = tile0, kb = 0;
+            const float* from[5];                      // four rows of x; lanes 0 and 1: a tile of weights
+            for (int block = 0; block < blocks + kAhead; ++block) {
+                const int now = block - kAhead;
+                if (now >= 0) {
+                    cp_async_wait<kAhead - 2>();
+                    __syncwarp();
+                    if (now >= 2) ok = mbar_wait_warp(smem_u32(&s_done[now & 1]), (now >> 1 & 1) ^ 1, a.wait_budget, ok);
                     if (!ok) break;
-    #pragma unroll
+                    if (lane == 0) mbar_arrive(smem_u32(&s_done[now & 1]));
+                }
+                if (block < blocks) {
+                    if (kb == 0) {
+                        const PairTile at(a, tile);
+                        const int64_t row0 = (2 * static_cast<int64_t>(at.row) + rank) * kF8Block + lane;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) from[j] = a.x_scales + min(row0 + 32 * j, a.rows - 1) * a.row_stride;
+                        from[4] = a.w_scales + static_cast<int64_t>(min(2 * at.col + (lane & 1), a.n_tiles - 1)) * a.k_blocks;
+                    }
+                    const int slot = block % kSlots;   // of the block eight before, which the sums are through with: the product four before is done
+#pragma unroll
                     for (int j = 0; j < 4; ++j) cp_async_4(smem_u32(&s_x[slot][32 * j + lane]), from[j] + kb * a.block_stride);
                     if (lane < 2) cp_async_4(smem_u32(&s_w[slot][lane]), from[4] + kb);
-                    cp_async_arrive(smem_u32(&s_scaled[slot]));
+                    if (++kb == a.k_blocks) {
+                        kb = 0;
+                        tile += step;
+                    }
                 }
+                cp_async_commit();
             }
-            cp_async_commit();
             cp_async_wait<0>();
         }
     } else {
@@ -538,8 +579,10 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPairMany));
         const int half = (warp - 4) >> 2, row_lane = (warp & 3) * 32 + lane;
         const uint32_t from = tmem + (static_cast<uint32_t>(warp & 3) << 21) + half * 128;
+        uint4* const out = reinterpret_cast<uint4*>(smem_raw + (base - smem_u32(smem_raw)) + kPairStages * kPairStage + (warp - 4) * kPairOut);
         grid_dependency_wait();
         int block = 0;
+        float s_next = 0.f;                            // the next block's factor: its scales are there with this block's
         for (int tile = tile0; ok && tile < tiles; tile += step) {
             float acc[128];
 #pragma unroll
@@ -547,29 +590,32 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
 #pragma unroll 1
             for (int kb = 0; kb < a.k_blocks; ++kb, ++block) {
                 const int slot = block % kSlots;
-                ok = mbar_wait_warp(smem_u32(&s_scaled[slot]), block / kSlots & 1, a.wait_budget, ok);
-                const float s = s_x[slot][row_lane] * s_w[slot][half];
                 ok = mbar_wait_warp(smem_u32(&s_done[block & 1]), block >> 1 & 1, a.wait_budget, ok);
                 if (!ok) break;
                 tc_fence_after();
-                uint32_t v[2][32];
-                tmem_ld_32x32(from + (block & 1) * 256, v[0]);
+                const float s = block ? s_next : s_x[0][row_lane] * s_w[0][half];
+                s_next = s_x[(slot + 1) % kSlots][row_lane] * s_w[(slot + 1) % kSlots][half];
+                uint32_t v0[32], v1[32];
+                const uint32_t here = from + (block & 1) * 256;
+                auto take = [&](const uint32_t (&v)[32], int at) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    tmem_ld_wait_for(v[j & 1]);
-                    if (j < 3) {
-                        tmem_ld_32x32(from + (block & 1) * 256 + 32 * (j + 1), v[(j + 1) & 1]);
-                    } else {
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) {
-                            mbar_arrive_remote(smem_u32(&s_free[block & 1]), 0u);
-                            mbar_arrive(smem_u32(&s_slot[slot]));
-                        }
-                    }
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) acc[32 * j + c] = fmaf(__uint_as_float(v[j & 1][c]), s, acc[32 * j + c]);
-                }
+                    for (int c = 0; c < 32; c += 2) fma2(acc[at + c], acc[at + c + 1], __uint_as_float(v[c]), __uint_as_float(v[c + 1]), s, s);
+                };
+                tmem_ld_32x32(here, v0);
+                tmem_ld_32x32(here + 32, v1);
+                tmem_ld_wait_for(v0);
+                tmem_ld_tie(v1);
+                take(v0, 0);
+                tmem_ld_32x32(here + 64, v0);
+                take(v1, 32);
+                tmem_ld_32x32(here + 96, v1);
+                tmem_ld_wait_for(v0);
+                tmem_ld_tie(v1);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_remote_relaxed(smem_u32(&s_free[block & 1]), 0u);
+                take(v0, 64);
+                take(v1, 96);
             }
             if (!ok) break;
             const PairTile at(a, tile);
@@ -579,10 +625,10 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
 #pragma unroll
                 for (int c = 0; c < 128; ++c) acc[c] += bias_of(a, o + c);
             }
-            if (row < a.rows) {
-#pragma unroll
-                for (int c = 0; c < 128; c += 8) put8(a, row * a.y_stride + o + c, a.n - o - c, acc + c);
-            }
+            const int64_t row0 = row - lane;
+            if (a.ftype == QTZ_BF16) put_rows<__nv_bfloat16>(a, out, acc, row0, o);
+            else if (a.ftype == QTZ_F16) put_rows<__half>(a, out, acc, row0, o);
+            else put_rows<float>(a, out, acc, row0, o);
         }
     }
     if (!ok) timed_out(a);
@@ -641,7 +687,7 @@ qtz_status launch_pair(qtz_f8_layer* p, LinearArgs& a, const CUtensorMap& x_map,
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * (a.units < h->num_sms / 2 ? a.units : h->num_sms / 2));
     cfg.blockDim = dim3(kPairThreads);
-    cfg.dynamicSmemBytes = 1024 + kPairStages * kPairStage;
+    cfg.dynamicSmemBytes = 1024 + kPairStages * kPairStage + 8 * kPairOut;
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = 2;
