@@ -92,25 +92,83 @@ __device__ __forceinline__ void fma2(float& x, float& y, float u, float v, float
 
 __device__ __forceinline__ float bias_of(const LinearArgs& a, int o) { return a.bias && o < a.n ? __ldg(a.bias + o) : 0.f; }
 
-// ---- few rows: the weights stream past kN rows of x ----
-// The 128 weights of a tile are the rows of the product, the rows of x its columns.  Units (tile, block of 128 columns) form one
-// sequence that is dealt out in equal contiguous shares; a tile that lies in several shares is joined by the last CTA to arrive.
-constexpr int kSlots = 8, kAhead = 4;  // places for the scales of units, and how many units ahead they are asked for
+template <typename T>
+__device__ __forceinline__ uint4 pack16(const float* v)
+{
+    if constexpr (sizeof(T) == 4) return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    else return make_uint4(qtz_dev::pack2(v[0], v[1], T()), qtz_dev::pack2(v[2], v[3], T()), qtz_dev::pack2(v[4], v[5], T()), qtz_dev::pack2(v[6], v[7], T()));
+}
 
-__device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t (&v)[16]) { tmem_ld_32x16(taddr, v); }
-__device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t (&v)[32]) { tmem_ld_32x32(taddr, v); }
+constexpr int kOutBytes = 2048;        // of a warp's values on their way out: 32 rows of 64 bytes
 
-template <int kN>
+// A warp's `rows` (at most 32) rows of kCols columns, of which `cols` exist; lane l holds row l, row r goes to to + r * stride.  64 bytes of
+// each row at a time cross through `out`, so that neighbouring lanes write neighbouring values; pieces of 16 bytes are shifted by row, for
+// the banks.  vector: rows start on 16 bytes.
+template <typename T, int kCols>
+__device__ __forceinline__ void put_rows(T* to, int64_t stride, int rows, int cols, bool vector, uint4* out, const float (&acc)[kCols])
+{
+    constexpr int kPer = 16 / sizeof(T), kStep = 64 / sizeof(T);
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int c0 = 0; c0 < kCols; c0 += kStep) {
+        const int here = min(kStep, cols - c0);
+        __syncwarp();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) out[lane * 4 + (q ^ (lane >> 1 & 3))] = pack16<T>(acc + c0 + q * kPer);
+        __syncwarp();
+        if (vector) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int r = i * 8 + (lane >> 2), q = lane & 3;
+                const uint4* const from = out + r * 4 + (q ^ (r >> 1 & 3));
+                T* const at = to + r * stride + c0 + q * kPer;
+                if (r < rows && q * kPer + kPer <= here) *reinterpret_cast<uint4*>(at) = *from;
+                else if (r < rows)
+                    for (int e = 0; e < here - q * kPer; ++e) at[e] = reinterpret_cast<const T*>(from)[e];
+            }
+        } else {
+            for (int at = lane; at < rows * kStep; at += 32) {
+                const int r = at / kStep, e = at % kStep;
+                if (e < here) to[r * stride + c0 + e] = reinterpret_cast<const T*>(out + r * 4 + (e / kPer ^ (r >> 1 & 3)))[e % kPer];
+            }
+        }
+    }
+}
+
+// The same into y, from (row, o) on, with the bias.
+template <int kCols>
+__device__ __forceinline__ void put_y(const LinearArgs& a, int64_t row, int o, uint4* out, float (&acc)[kCols])
+{
+    const int rows = static_cast<int>(min(static_cast<int64_t>(32), a.rows - row)), cols = a.n - o;
+    if (a.bias) {
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) acc[c] += bias_of(a, o + c);
+    }
+    const int64_t at = row * a.y_stride + o;
+    if (a.ftype == QTZ_BF16) put_rows(static_cast<__nv_bfloat16*>(a.y) + at, a.y_stride, rows, cols, a.vector, out, acc);
+    else if (a.ftype == QTZ_F16) put_rows(static_cast<__half*>(a.y) + at, a.y_stride, rows, cols, a.vector, out, acc);
+    else put_rows(static_cast<float*>(a.y) + at, a.y_stride, rows, cols, a.vector, out, acc);
+}
+
+// Places for the scales of blocks, and how many blocks ahead they are asked for.  A thread of the sums reads its block's factor a block
+// early, so that the loads of a block's scales are counted with the product of the block before.
+constexpr int kSlots = 8, kAhead = 4;
+
+// ---- few rows: the weights stream past a tile of rows ----
+// A tile is 128 rows of x, of which kRows are loaded (what the other rows of the product hold is not looked at), and 128 weights.  Units
+// (tile, block of 128 columns) form one sequence that is dealt out in equal contiguous shares; a tile that lies in several shares is
+// joined by the last CTA to arrive.  A thread owns a row of x and half of the weights: one factor a thread and unit.
+constexpr int kStreamThreads = 384;    // loads, products (two warps), scales, eight warps for the sums
+constexpr int kBuffers = 4;            // of 128 columns of tensor memory
+
+template <int kRows>
 struct Stream {
-    static constexpr int kEpiWarps = kN == 128 ? 8 : 4, kCols = kN * 4 / kEpiWarps;   // columns of a warp
-    static constexpr int kThreads = 128 + 32 * kEpiWarps;
-    static constexpr int kStage = kTileBytes + kN * kF8Block;
-    static constexpr int kBuffers = kN <= 64 ? 8 : 4;                                 // of kN columns of tensor memory
-    static constexpr int kColumns = kN * kBuffers < 32 ? 32 : kN * kBuffers;
-    static constexpr int kRoom = (kSmemLimit - 1024 - kSlots * (kN + 1) * 4 - 1024) / kStage, kStages = kRoom < kMaxStages ? kRoom : kMaxStages;
+    static constexpr int kStage = kTileBytes + kRows * kF8Block;
+    static constexpr int kRoom = (kSmemLimit - 1024 - 8 * kOutBytes - kSlots * (kRows + 1) * 4 - 1024) / kStage, kStages = kRoom < kMaxStages ? kRoom / 2 * 2 : kMaxStages;
+    static constexpr int kSmem = 1024 + kStages * kStage + 8 * kOutBytes;
 };
 
-struct Unit {                          // 128 weights, kN rows of x, 128 columns; row tiles of the same weights follow each other
+struct Unit {                          // row tiles of the same weights follow each other
     int n_tile, row_tile, kb;
     __device__ Unit(const LinearArgs& a, int u) : n_tile(u / a.k_blocks / a.row_tiles), row_tile(u / a.k_blocks % a.row_tiles), kb(u % a.k_blocks) {}
     __device__ void next(const LinearArgs& a)
@@ -123,14 +181,13 @@ struct Unit {                          // 128 weights, kN rows of x, 128 columns
     }
 };
 
-template <int kN>
-__device__ __forceinline__ float* part_of(const LinearArgs& a, int cta, int which) { return a.parts + (static_cast<int64_t>(cta) * 2 + which) * (kN * kF8Block); }
+__device__ __forceinline__ float* part_of(const LinearArgs& a, int cta, int which) { return a.parts + (static_cast<int64_t>(cta) * 2 + which) * (kF8Block * kF8Block); }
 
 // After a CTA's last unit: counts its arrival at the tiles that it shares with others, and sums those at which it is the last, in the
-// order of the columns.  Called by all `threads` threads, behind a barrier of the CTA.
-template <int kN>
-__device__ __forceinline__ void join_tiles(const LinearArgs& a, const int (&open)[2], int tid, int threads, int (&last)[2])
+// order of the columns.  Called by all threads, behind a barrier of the CTA.
+__device__ __forceinline__ void join_tiles(const LinearArgs& a, const int (&open)[2], int (&last)[2])
 {
+    const int tid = threadIdx.x;
     auto first = [&](int unit) { return unit / a.k_blocks * a.k_blocks; };
     if ((tid == 0 && open[0] >= 0) || (tid == 32 && open[1] >= 0)) {
         const int begin = first(tid ? open[1] : open[0]), c0 = begin / a.share;
@@ -138,26 +195,27 @@ __device__ __forceinline__ void join_tiles(const LinearArgs& a, const int (&open
         last[tid ? 1 : 0] = all;
         if (all) a.counters[c0] = 0;                   // ready for the next call
     }
-    named_barrier(1, threads);
+    __syncthreads();
 #pragma unroll 1
     for (int which = 0; which < 2; ++which) {
         const int unit = open[which];
         if (unit < 0 || !last[which]) continue;
-        const int begin = first(unit), c0 = begin / a.share, c1 = (begin + a.k_blocks - 1) / a.share, tile = unit / a.k_blocks;
-        const int64_t r0 = static_cast<int64_t>(tile % a.row_tiles) * kN;
-        const int quads = static_cast<int>(min(static_cast<int64_t>(kN), a.rows - r0)) * (kF8Block / 4);
+        const int begin = first(unit), c0 = begin / a.share, c1 = (begin + a.k_blocks - 1) / a.share;
+        const Unit at(a, unit);
+        const int64_t r0 = static_cast<int64_t>(at.row_tile) * kF8Block;
+        const int quads = static_cast<int>(min(static_cast<int64_t>(kF8Block), a.rows - r0)) * (kF8Block / 4);
         constexpr int kAtOnce = 4;
 #pragma unroll 1
-        for (int q0 = tid; q0 < quads; q0 += kAtOnce * threads) {
+        for (int q0 = tid; q0 < quads; q0 += kAtOnce * kStreamThreads) {
             float4 v[kAtOnce];
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j) v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 2
             for (int c = c0; c <= c1; ++c) {
-                const float4* const part = reinterpret_cast<const float4*>(part_of<kN>(a, c, c == c0 ? 1 : 0)) + q0;
+                const float4* const part = reinterpret_cast<const float4*>(part_of(a, c, c == c0 ? 1 : 0)) + q0;
                 float4 p[kAtOnce];
 #pragma unroll
-                for (int j = 0; j < kAtOnce; ++j) p[j] = q0 + j * threads < quads ? __ldcg(part + j * threads) : make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int j = 0; j < kAtOnce; ++j) p[j] = q0 + j * kStreamThreads < quads ? __ldcg(part + j * kStreamThreads) : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int j = 0; j < kAtOnce; ++j) {
                     v[j].x += p[j].x;
@@ -168,32 +226,40 @@ __device__ __forceinline__ void join_tiles(const LinearArgs& a, const int (&open
             }
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j) {
-                const int q = q0 + j * threads;
+                const int q = q0 + j * kStreamThreads;
                 if (q >= quads) break;
-                const int o = tile / a.row_tiles * kF8Block + q % (kF8Block / 4) * 4;
-                const int64_t at = (r0 + q / (kF8Block / 4)) * a.y_stride + o;
-                if (o < a.n) put(a, at, v[j].x + bias_of(a, o));
-                if (o + 1 < a.n) put(a, at + 1, v[j].y + bias_of(a, o + 1));
-                if (o + 2 < a.n) put(a, at + 2, v[j].z + bias_of(a, o + 2));
-                if (o + 3 < a.n) put(a, at + 3, v[j].w + bias_of(a, o + 3));
+                const int o = at.n_tile * kF8Block + q % (kF8Block / 4) * 4;
+                const int64_t to = (r0 + q / (kF8Block / 4)) * a.y_stride + o;
+                const float y[4] = {v[j].x + bias_of(a, o), v[j].y + bias_of(a, o + 1), v[j].z + bias_of(a, o + 2), v[j].w + bias_of(a, o + 3)};
+                if (a.vector && o + 4 <= a.n) {
+                    using qtz_dev::pack2;
+                    if (a.ftype == QTZ_F32) *reinterpret_cast<float4*>(static_cast<float*>(a.y) + to) = make_float4(y[0], y[1], y[2], y[3]);
+                    else if (a.ftype == QTZ_F16) *reinterpret_cast<uint2*>(static_cast<__half*>(a.y) + to) = make_uint2(pack2(y[0], y[1], __half()), pack2(y[2], y[3], __half()));
+                    else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.y) + to) = make_uint2(pack2(y[0], y[1], __nv_bfloat16()), pack2(y[2], y[3], __nv_bfloat16()));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (o + e < a.n) put(a, to + e, y[e]);
+                }
             }
         }
     }
 }
 
-template <int kN>
-__global__ void __launch_bounds__(Stream<kN>::kThreads, 1)
+template <int kRows>
+__global__ void __launch_bounds__(kStreamThreads, 1)
 stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map)
 {
-    using S = Stream<kN>;
-    extern __shared__ uint8_t smem_raw[];              // the ring: a tile of weights, kN rows of x
-    __shared__ __align__(16) float s_x[kSlots][kN];    // scales
-    __shared__ float s_w[kSlots];
-    __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_done[S::kBuffers], s_free[S::kBuffers], s_drain;
+    using S = Stream<kRows>;
+    extern __shared__ uint8_t smem_raw[];              // the ring: kRows rows of x, a tile of weights; then values on their way out
+    __shared__ float s_x[kSlots][kRows], s_w[kSlots];  // scales
+    __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_done[kBuffers], s_free[kBuffers], s_drain;
     __shared__ int s_open[2], s_last[2], s_failed;     // s_open: units whose tiles are shared with an earlier / a later CTA
     __shared__ uint32_t s_tmem;
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    // warps of the sums whose rows exist: those of a quarter of tensor memory take 32 rows
+    const int quarters = static_cast<int>(min(static_cast<int64_t>(4), (a.rows + 31) / 32));
     if (tid == 0) {
         s_failed = 0;
         s_open[0] = s_open[1] = -1;
@@ -203,14 +269,14 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
             mbar_init(smem_u32(&s_full[i]), 1);
             mbar_init(smem_u32(&s_empty[i]), 1);
         }
-        for (int i = 0; i < S::kBuffers; ++i) {
-            mbar_init(smem_u32(&s_done[i]), 2);        // the product and its scales
-            mbar_init(smem_u32(&s_free[i]), S::kEpiWarps);
+        for (int i = 0; i < kBuffers; ++i) {
+            mbar_init(smem_u32(&s_done[i]), 2);        // the product; scales
+            mbar_init(smem_u32(&s_free[i]), 2 * quarters);
         }
-        mbar_init(smem_u32(&s_drain), 1);
+        mbar_init(smem_u32(&s_drain), 2);
     }
     if (warp == 1) {
-        tmem_alloc(smem_u32(&s_tmem), S::kColumns);
+        tmem_alloc(smem_u32(&s_tmem), kBuffers * 128);
         tmem_relinquish();
     }
     fence_barrier_init();
@@ -230,13 +296,13 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
             if (elect_one()) {
                 const uint32_t bar = smem_u32(&s_full[stage]);
                 mbar_arrive_expect_tx(bar, S::kStage);
-                tma_load_2d(base + stage * S::kStage, &w_map, bar, 0, (ahead.n_tile * a.k_blocks + ahead.kb) * kF8Block);
+                tma_load_2d(base + stage * S::kStage + kRows * kF8Block, &w_map, bar, 0, (ahead.n_tile * a.k_blocks + ahead.kb) * kF8Block);
             }
             __syncwarp();
             ahead.next(a);
         };
         auto rows = [&](int stage) {
-            if (elect_one()) tma_load_2d(base + stage * S::kStage + kTileBytes, &x_map, smem_u32(&s_full[stage]), here.kb * kF8Block, here.row_tile * kN);
+            if (elect_one()) tma_load_2d(base + stage * S::kStage, &x_map, smem_u32(&s_full[stage]), here.kb * kF8Block, here.row_tile * kF8Block);
             __syncwarp();
             here.next(a);
         };
@@ -257,53 +323,53 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
         }
         // nothing may be in flight when the CTA ends
         for (int j = max(0, issued - S::kStages); j < issued; ++j) ok = mbar_wait_warp(smem_u32(&s_full[j % S::kStages]), (j / S::kStages) & 1, kDrainBudget, ok);
-    } else if (warp == 1) {
-        // ======== products ========
-        int stage = 0, round = 0;
-        for (int i = 0; i < count; ++i) {
-            const int buffer = i % S::kBuffers;
+    } else if (warp == 1 || warp == 3) {
+        // ======== products: a warp for the even units, one for the odd ones ========
+        const int odd = warp >> 1;
+        int stage = odd, round = 0;
+        for (int i = odd; i < count; i += 2) {
+            const int buffer = i % kBuffers;
             wait(s_full[stage], round & 1);
-            if (i >= S::kBuffers) wait(s_free[buffer], (i / S::kBuffers & 1) ^ 1);
+            if (i >= kBuffers) wait(s_free[buffer], (i / kBuffers & 1) ^ 1);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
-                const uint64_t w = make_kmajor_desc(base + stage * S::kStage, 128), x = make_kmajor_desc(base + stage * S::kStage + kTileBytes, 128);
+                const uint64_t x = make_kmajor_desc(base + stage * S::kStage, 128), w = make_kmajor_desc(base + stage * S::kStage + kRows * kF8Block, 128);
 #pragma unroll
-                for (int k = 0; k < 4; ++k) mma_f8(tmem + buffer * kN, w + 2 * k, x + 2 * k, kProduct<128, kN>, k > 0);
+                for (int k = 0; k < 4; ++k) mma_f8(tmem + buffer * 128, x + 2 * k, w + 2 * k, kProduct<128, 128>, k > 0);
                 mma_commit(smem_u32(&s_done[buffer]));
                 mma_commit(smem_u32(&s_empty[stage]));
             }
             __syncwarp();
-            if (++stage == S::kStages) {
-                stage = 0;
+            stage += 2;                                // the number of stages is even
+            if (stage >= S::kStages) {
+                stage -= S::kStages;
                 ++round;
             }
         }
         if (elect_one()) mma_commit(smem_u32(&s_drain));   // the others may have given up on what is still running
         __syncwarp();
-        ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&s_drain), 0, kDrainBudget)) && ok;
     } else if (warp == 2) {
-        // ======== scales: on their way kAhead units ahead, counted with the unit's product ========
+        // ======== scales ========
         grid_dependency_wait();
         Unit here(a, u0);
         for (int i = 0; i < count + kAhead; ++i) {
             const int now = i - kAhead;
             if (now >= 0) {
-                cp_async_wait<kAhead - 1>();
+                cp_async_wait<kAhead - 2>();           // the unit's scales and the next one's
                 __syncwarp();
-                if (now >= S::kBuffers) wait(s_done[now % S::kBuffers], (now / S::kBuffers & 1) ^ 1);
-                if (!ok) break;
-                if (lane == 0) mbar_arrive(smem_u32(&s_done[now % S::kBuffers]));
+                if (lane == 0) mbar_arrive(smem_u32(&s_done[now % kBuffers]));
             }
+            // What the place held, kSlots units ago, has been used up where the unit after it has been read out; that also says that the
+            // product that was counted kBuffers units before the next one is done.
+            const int read = now - kAhead + 1;
+            if (read >= 0) wait(s_free[read % kBuffers], read / kBuffers & 1);
+            if (!ok) break;
             if (i < count) {
-                // the place's unit, kSlots before, has been used up where the one after it has been read
-                const int next = i - kSlots + 1;
-                if (next >= 1) wait(s_free[next % S::kBuffers], next / S::kBuffers & 1);
-                if (!ok) break;
                 const int slot = i % kSlots;
-                const int64_t r0 = static_cast<int64_t>(here.row_tile) * kN;
+                const int64_t r0 = static_cast<int64_t>(here.row_tile) * kF8Block;
 #pragma unroll
-                for (int r = lane; r < kN; r += 32)
+                for (int r = lane; r < kRows; r += 32)
                     cp_async_4(smem_u32(&s_x[slot][r]), a.x_scales + min(r0 + r, a.rows - 1) * a.row_stride + here.kb * a.block_stride);
                 if (lane == 0) cp_async_4(smem_u32(&s_w[slot]), a.w_scales + static_cast<int64_t>(here.n_tile) * a.k_blocks + here.kb);
                 here.next(a);
@@ -311,57 +377,49 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
             cp_async_commit();
         }
         cp_async_wait<0>();
-    } else if (warp >= 4) {
+    } else if ((warp & 3) < quarters) {
         // ======== sums ========
-        const int part = (warp - 4) >> 2, o_lane = (warp & 3) * 32 + lane;
-        const uint32_t from = tmem + (static_cast<uint32_t>(warp & 3) << 21) + part * S::kCols;
-        float acc[S::kCols];
+        const int half = (warp - 4) >> 2, row_warp = (warp & 3) * 32, row_lane = min(row_warp + lane, kRows - 1);
+        const uint32_t from = tmem + (static_cast<uint32_t>(warp & 3) << 21) + half * 64;
+        uint4* const out = reinterpret_cast<uint4*>(smem_raw + (base - smem_u32(smem_raw)) + S::kStages * S::kStage + (warp - 4) * kOutBytes);
+        float acc[64];
 #pragma unroll
-        for (int c = 0; c < S::kCols; ++c) acc[c] = 0.f;
+        for (int c = 0; c < 64; ++c) acc[c] = 0.f;
         grid_dependency_wait();                        // y may be what the kernel before reads
         Unit here(a, u0);
+        float s_next = 0.f;
         for (int i = 0; i < count; ++i) {
-            const int slot = i % kSlots, buffer = i % S::kBuffers;
-            wait(s_done[buffer], i / S::kBuffers & 1);
+            const int buffer = i % kBuffers, after = (i + 1) % kSlots;
+            wait(s_done[buffer], i / kBuffers & 1);
             if (!ok) break;
             tc_fence_after();
-            constexpr int kPiece = S::kCols < 32 ? 16 : 32;
-            uint32_t v[S::kCols / kPiece][kPiece];
-#pragma unroll
-            for (int p = 0; p < S::kCols / kPiece; ++p) tmem_load(from + buffer * kN + p * kPiece, v[p]);
-            tmem_ld_wait_for(v[0]);
-            if constexpr (S::kCols == 64) tmem_ld_tie(v[1]);
+            uint32_t v0[32], v1[32];
+            tmem_ld_32x32(from + buffer * 128, v0);
+            tmem_ld_32x32(from + buffer * 128 + 32, v1);
+            const float s = i ? s_next : s_x[0][row_lane] * s_w[0];
+            s_next = s_x[after][row_lane] * s_w[after];
+            tmem_ld_wait_for(v0);
+            tmem_ld_tie(v1);
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&s_free[buffer]));
-            const float w_scale = s_w[slot];
 #pragma unroll
-            for (int c = 0; c < S::kCols; c += 4) {
-                const float4 s = *reinterpret_cast<const float4*>(&s_x[slot][part * S::kCols + c]);
-                const uint32_t* const p = v[c / kPiece] + c % kPiece;
-                fma2(acc[c], acc[c + 1], __uint_as_float(p[0]), __uint_as_float(p[1]), s.x * w_scale, s.y * w_scale);
-                fma2(acc[c + 2], acc[c + 3], __uint_as_float(p[2]), __uint_as_float(p[3]), s.z * w_scale, s.w * w_scale);
-            }
+            for (int c = 0; c < 32; c += 2) fma2(acc[c], acc[c + 1], __uint_as_float(v0[c]), __uint_as_float(v0[c + 1]), s, s);
+#pragma unroll
+            for (int c = 0; c < 32; c += 2) fma2(acc[32 + c], acc[33 + c], __uint_as_float(v1[c]), __uint_as_float(v1[c + 1]), s, s);
             const bool ends = here.kb == a.k_blocks - 1;
             if (ends || i == count - 1) {              // the end of this tile, or of this CTA's columns of it
                 const bool begins = i >= here.kb;
+                const int64_t row = static_cast<int64_t>(here.row_tile) * kF8Block + row_warp;
                 if (begins && ends) {
-                    const int o = here.n_tile * kF8Block + o_lane;
-                    const int64_t r0 = static_cast<int64_t>(here.row_tile) * kN + part * S::kCols;
-                    const float b = bias_of(a, o);
-                    if (o < a.n) {
-#pragma unroll
-                        for (int c = 0; c < S::kCols; ++c)
-                            if (r0 + c < a.rows) put(a, (r0 + c) * a.y_stride + o, acc[c] + b);
-                    }
+                    put_y(a, row, here.n_tile * kF8Block + half * 64, out, acc);
                 } else {
-                    if (tid == 128) s_open[begins ? 1 : 0] = u0 + i;
-                    float* const to = part_of<kN>(a, blockIdx.x, begins ? 1 : 0) + part * S::kCols * kF8Block + o_lane;
-#pragma unroll
-                    for (int c = 0; c < S::kCols; ++c) to[c * kF8Block] = acc[c];
+                    if (lane == 0) s_open[begins ? 1 : 0] = u0 + i;
+                    put_rows(part_of(a, blockIdx.x, begins ? 1 : 0) + row_warp * kF8Block + half * 64, kF8Block, static_cast<int>(min(static_cast<int64_t>(32), a.rows - row)), 64,
+                             true, out, acc);
                 }
 #pragma unroll
-                for (int c = 0; c < S::kCols; ++c) acc[c] = 0.f;
+                for (int c = 0; c < 64; ++c) acc[c] = 0.f;
             }
             here.next(a);
         }
@@ -373,10 +431,12 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
     tc_fence_before();
     __syncthreads();
     if (warp == 1) {
+        (void)mbar_wait(smem_u32(&s_drain), 0, kDrainBudget);
+        __syncwarp();
         tc_fence_after();
-        tmem_dealloc(tmem, S::kColumns);
+        tmem_dealloc(tmem, kBuffers * 128);
     }
-    if (!s_failed) join_tiles<kN>(a, s_open, tid, S::kThreads, s_last);   // after a wait that gave up the results are void
+    if (!s_failed) join_tiles(a, s_open, s_last);      // after a wait that gave up the results are void
 }
 
 // ---- many rows: CTA pairs on tiles of 256 rows of x and 256 weights ----
@@ -388,7 +448,6 @@ constexpr int kPairLaunch = 168, kPairFew = 80, kPairMany = 208;   // registers 
 static_assert(4 * 32 * kPairFew + 8 * 32 * kPairMany <= kPairThreads * kPairLaunch, "more registers than the CTA was launched with");
 constexpr int kPairStage = 2 * kTileBytes;
 constexpr int kPairStages = 6;          // what the rows on their way to y leave room for
-constexpr int kPairOut = 2048;         // bytes of a warp on their way to y: 32 rows of 64
 constexpr int kBand = 16;              // row tiles that the pairs work on side by side, for the L2
 
 struct PairTile {
@@ -401,50 +460,6 @@ struct PairTile {
         row = band * kBand + rest % tall;
     }
 };
-
-template <typename T>
-__device__ __forceinline__ uint4 pack16(const float* v)
-{
-    if constexpr (sizeof(T) == 4) return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-    else return make_uint4(qtz_dev::pack2(v[0], v[1], T()), qtz_dev::pack2(v[2], v[3], T()), qtz_dev::pack2(v[4], v[5], T()), qtz_dev::pack2(v[6], v[7], T()));
-}
-
-// A warp's 32 rows of y (from row0 on) of 128 columns (from o on); lane l holds row l.  64 bytes of each row at a time cross through `out` so
-// that neighbouring lanes write neighbouring values; pieces of 16 bytes are shifted by row, for the banks.
-template <typename T>
-__device__ __forceinline__ void put_rows(const LinearArgs& a, uint4* out, const float (&acc)[128], int64_t row0, int o)
-{
-    constexpr int kPer = 16 / sizeof(T), kCols = 64 / sizeof(T);
-    const int lane = threadIdx.x & 31, rows = static_cast<int>(min(static_cast<int64_t>(32), a.rows - row0));
-    T* const y = static_cast<T*>(a.y);
-#pragma unroll
-    for (int c0 = 0; c0 < 128; c0 += kCols) {
-        const int cols = min(kCols, a.n - o - c0);
-        __syncwarp();
-#pragma unroll
-        for (int q = 0; q < 4; ++q) out[lane * 4 + (q ^ (lane >> 1 & 3))] = pack16<T>(acc + c0 + q * kPer);
-        __syncwarp();
-        if (a.vector) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = i * 8 + (lane >> 2), q = lane & 3;
-                const uint4 v = out[r * 4 + (q ^ (r >> 1 & 3))];
-                T* const to = y + (row0 + r) * a.y_stride + o + c0 + q * kPer;
-                if (r < rows && q * kPer + kPer <= cols) {
-                    *reinterpret_cast<uint4*>(to) = v;
-                } else if (r < rows) {
-                    const T* const one = reinterpret_cast<const T*>(out + r * 4 + (q ^ (r >> 1 & 3)));
-                    for (int e = 0; e < cols - q * kPer; ++e) to[e] = one[e];
-                }
-            }
-        } else {
-            for (int at = lane; at < 32 * kCols; at += 32) {
-                const int r = at / kCols, e = at % kCols;
-                if (r < rows && e < cols) y[(row0 + r) * a.y_stride + o + c0 + e] = reinterpret_cast<const T*>(out + r * 4 + (e / kPer ^ (r >> 1 & 3)))[e % kPer];
-            }
-        }
-    }
-}
 
 __global__ void __launch_bounds__(kPairThreads, 1)
 pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map)
@@ -579,7 +594,7 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPairMany));
         const int half = (warp - 4) >> 2, row_lane = (warp & 3) * 32 + lane;
         const uint32_t from = tmem + (static_cast<uint32_t>(warp & 3) << 21) + half * 128;
-        uint4* const out = reinterpret_cast<uint4*>(smem_raw + (base - smem_u32(smem_raw)) + kPairStages * kPairStage + (warp - 4) * kPairOut);
+        uint4* const out = reinterpret_cast<uint4*>(smem_raw + (base - smem_u32(smem_raw)) + kPairStages * kPairStage + (warp - 4) * kOutBytes);
         grid_dependency_wait();
         int block = 0;
         float s_next = 0.f;                            // the next block's factor: its scales are there with this block's
@@ -619,16 +634,7 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
             }
             if (!ok) break;
             const PairTile at(a, tile);
-            const int64_t row = (2 * static_cast<int64_t>(at.row) + rank) * kF8Block + row_lane;
-            const int o = (2 * at.col + half) * kF8Block;
-            if (a.bias) {
-#pragma unroll
-                for (int c = 0; c < 128; ++c) acc[c] += bias_of(a, o + c);
-            }
-            const int64_t row0 = row - lane;
-            if (a.ftype == QTZ_BF16) put_rows<__nv_bfloat16>(a, out, acc, row0, o);
-            else if (a.ftype == QTZ_F16) put_rows<__half>(a, out, acc, row0, o);
-            else put_rows<float>(a, out, acc, row0, o);
+            put_y(a, (2 * static_cast<int64_t>(at.row) + rank) * kF8Block + row_lane - lane, (2 * at.col + half) * kF8Block, out, acc);
         }
     }
     if (!ok) timed_out(a);
@@ -657,17 +663,16 @@ qtz_status ensure_scratch(qtz_ctx* h, cudaStream_t st)
     return QTZ_OK;
 }
 
-template <int kN>
+template <int kRows>
 qtz_status launch_stream(qtz_f8_layer* p, LinearArgs& a, const CUtensorMap& x_map, cudaStream_t st)
 {
     qtz_ctx* h = p->h;
-    a.row_tiles = static_cast<int32_t>((a.rows + kN - 1) / kN);
+    a.row_tiles = static_cast<int32_t>((a.rows + kF8Block - 1) / kF8Block);
     a.units = a.row_tiles * a.n_tiles * a.k_blocks;
     a.share = (a.units + h->num_sms - 1) / h->num_sms;
-    const qtz_status s = qtz_allow_smem(h, stream_kernel<kN>);
+    const qtz_status s = qtz_allow_smem(h, stream_kernel<kRows>);
     if (s != QTZ_OK) return s;
-    QTZ_CUDA(h, qtz_launch_dependent(stream_kernel<kN>, dim3((a.units + a.share - 1) / a.share), Stream<kN>::kThreads,
-                                     1024 + Stream<kN>::kStages * Stream<kN>::kStage, st, a, p->w_map, x_map));
+    QTZ_CUDA(h, qtz_launch_dependent(stream_kernel<kRows>, dim3((a.units + a.share - 1) / a.share), kStreamThreads, Stream<kRows>::kSmem, st, a, p->w_map, x_map));
     return QTZ_OK;
 }
 
@@ -687,7 +692,7 @@ qtz_status launch_pair(qtz_f8_layer* p, LinearArgs& a, const CUtensorMap& x_map,
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * (a.units < h->num_sms / 2 ? a.units : h->num_sms / 2));
     cfg.blockDim = dim3(kPairThreads);
-    cfg.dynamicSmemBytes = 1024 + kPairStages * kPairStage + 8 * kPairOut;
+    cfg.dynamicSmemBytes = 1024 + kPairStages * kPairStage + 8 * kOutBytes;
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = 2;
