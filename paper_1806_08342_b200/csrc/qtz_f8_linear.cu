@@ -53,7 +53,8 @@ struct LinearArgs {
     int32_t n, n_tiles, k_blocks, ftype;
     int32_t vector;            // rows of y start on 16 bytes
     int32_t row_tiles;         // tiles of activation rows
-    int32_t units, share;      // few rows: tiles x blocks of 128 columns, and how many of them a CTA takes
+    int32_t split;             // few rows: CTAs (of a cluster) that share the columns of a tile; 0: shares of the sequence of units
+    int32_t units, share;      // tiles x blocks of 128 columns, and how many of them a CTA takes
     float* parts;              // few rows: what tiles that lie in several shares are joined from
     int32_t* counters;
     long long wait_budget;
@@ -155,11 +156,13 @@ __device__ __forceinline__ void put_y(const LinearArgs& a, int64_t row, int o, u
 constexpr int kSlots = 8, kAhead = 4;
 
 // ---- few rows: the weights stream past a tile of rows ----
-// A tile is 128 rows of x, of which kRows are loaded (what the other rows of the product hold is not looked at), and 128 weights.  Units
-// (tile, block of 128 columns) form one sequence that is dealt out in equal contiguous shares; a tile that lies in several shares is
-// joined by the last CTA to arrive.  A thread owns a row of x and half of the weights: one factor a thread and unit.
+// A tile is 128 rows of x, of which kRows are loaded (what the other rows of the product hold is not looked at), and 128 weights.  Where
+// there are fewer tiles than SMs, the CTAs of a cluster take equal parts of a tile's columns and join their sums through each other's shared
+// memory.  Where there are more, units (tile, block of 128 columns) form one sequence that is dealt out in equal contiguous shares; a tile
+// that lies in several shares is joined by the last CTA to arrive.  A thread owns a row of x and half of the weights: one factor a thread and unit.
 constexpr int kStreamThreads = 384;    // loads, products (two warps), scales, eight warps for the sums
 constexpr int kBuffers = 4;            // of 128 columns of tensor memory
+constexpr int kMaxSplit = 8;           // CTAs of a cluster
 
 template <int kRows>
 struct Stream {
@@ -183,6 +186,47 @@ struct Unit {                          // row tiles of the same weights follow e
 
 __device__ __forceinline__ float* part_of(const LinearArgs& a, int cta, int which) { return a.parts + (static_cast<int64_t>(cta) * 2 + which) * (kF8Block * kF8Block); }
 
+// Four neighbouring sums.
+__device__ __forceinline__ void put_quad(const LinearArgs& a, int64_t row, int o, float4 v)
+{
+    using qtz_dev::pack2;
+    const int64_t to = row * a.y_stride + o;
+    const float y[4] = {v.x + bias_of(a, o), v.y + bias_of(a, o + 1), v.z + bias_of(a, o + 2), v.w + bias_of(a, o + 3)};
+    if (a.vector && o + 4 <= a.n) {
+        if (a.ftype == QTZ_F32) *reinterpret_cast<float4*>(static_cast<float*>(a.y) + to) = make_float4(y[0], y[1], y[2], y[3]);
+        else if (a.ftype == QTZ_F16) *reinterpret_cast<uint2*>(static_cast<__half*>(a.y) + to) = make_uint2(pack2(y[0], y[1], __half()), pack2(y[2], y[3], __half()));
+        else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.y) + to) = make_uint2(pack2(y[0], y[1], __nv_bfloat16()), pack2(y[2], y[3], __nv_bfloat16()));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (o + e < a.n) put(a, to + e, y[e]);
+    }
+}
+
+// Sums of a tile that the CTAs of a cluster hold in shared memory, [row][32 quads of columns], a quad at its number ^ (row % 32) (for the
+// banks): each CTA takes an equal part of the quads and adds them up in the order of the columns.
+__device__ __forceinline__ uint32_t quad_at(uint32_t base, int row, int quad) { return base + (row * 32 + (quad ^ (row & 31))) * 16; }
+
+__device__ __forceinline__ void join_cluster(const LinearArgs& a, const Unit& tile, uint32_t base)
+{
+    const int64_t r0 = static_cast<int64_t>(tile.row_tile) * kF8Block;
+    const int quads = static_cast<int>(min(static_cast<int64_t>(kF8Block), a.rows - r0)) * 32, rank = static_cast<int>(cluster_ctarank());
+    const int end = (rank + 1) * quads / a.split;
+    for (int q = rank * quads / a.split + threadIdx.x; q < end; q += kStreamThreads) {
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+        const uint32_t own = quad_at(base, q >> 5, q & 31);
+#pragma unroll 4
+        for (int c = 0; c < a.split; ++c) {
+            const float4 p = lds_cluster(mapa_shared(own, c));
+            v.x += p.x;
+            v.y += p.y;
+            v.z += p.z;
+            v.w += p.w;
+        }
+        put_quad(a, r0 + (q >> 5), tile.n_tile * kF8Block + (q & 31) * 4, v);
+    }
+}
+
 // After a CTA's last unit: counts its arrival at the tiles that it shares with others, and sums those at which it is the last, in the
 // order of the columns.  Called by all threads, behind a barrier of the CTA.
 __device__ __forceinline__ void join_tiles(const LinearArgs& a, const int (&open)[2], int (&last)[2])
@@ -204,43 +248,37 @@ __device__ __forceinline__ void join_tiles(const LinearArgs& a, const int (&open
         const Unit at(a, unit);
         const int64_t r0 = static_cast<int64_t>(at.row_tile) * kF8Block;
         const int quads = static_cast<int>(min(static_cast<int64_t>(kF8Block), a.rows - r0)) * (kF8Block / 4);
-        constexpr int kAtOnce = 4;
+        constexpr int kAtOnce = 6, kParts = 4;         // loads under way: of a pass over all rows there are two
 #pragma unroll 1
         for (int q0 = tid; q0 < quads; q0 += kAtOnce * kStreamThreads) {
             float4 v[kAtOnce];
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j) v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-            for (int c = c0; c <= c1; ++c) {
-                const float4* const part = reinterpret_cast<const float4*>(part_of(a, c, c == c0 ? 1 : 0)) + q0;
-                float4 p[kAtOnce];
+#pragma unroll 1
+            for (int c = c0; c <= c1; c += kParts) {
+                float4 p[kParts][kAtOnce];
 #pragma unroll
-                for (int j = 0; j < kAtOnce; ++j) p[j] = q0 + j * kStreamThreads < quads ? __ldcg(part + j * kStreamThreads) : make_float4(0.f, 0.f, 0.f, 0.f);
+                for (int x = 0; x < kParts; ++x) {
+                    const float4* const part = reinterpret_cast<const float4*>(part_of(a, c + x, c + x == c0 ? 1 : 0)) + q0;
 #pragma unroll
-                for (int j = 0; j < kAtOnce; ++j) {
-                    v[j].x += p[j].x;
-                    v[j].y += p[j].y;
-                    v[j].z += p[j].z;
-                    v[j].w += p[j].w;
+                    for (int j = 0; j < kAtOnce; ++j)
+                        p[x][j] = c + x <= c1 && q0 + j * kStreamThreads < quads ? __ldcg(part + j * kStreamThreads) : make_float4(0.f, 0.f, 0.f, 0.f);
                 }
+#pragma unroll
+                for (int x = 0; x < kParts; ++x)
+#pragma unroll
+                    for (int j = 0; j < kAtOnce; ++j) {
+                        v[j].x += p[x][j].x;
+                        v[j].y += p[x][j].y;
+                        v[j].z += p[x][j].z;
+                        v[j].w += p[x][j].w;
+                    }
             }
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j) {
                 const int q = q0 + j * kStreamThreads;
                 if (q >= quads) break;
-                const int o = at.n_tile * kF8Block + q % (kF8Block / 4) * 4;
-                const int64_t to = (r0 + q / (kF8Block / 4)) * a.y_stride + o;
-                const float y[4] = {v[j].x + bias_of(a, o), v[j].y + bias_of(a, o + 1), v[j].z + bias_of(a, o + 2), v[j].w + bias_of(a, o + 3)};
-                if (a.vector && o + 4 <= a.n) {
-                    using qtz_dev::pack2;
-                    if (a.ftype == QTZ_F32) *reinterpret_cast<float4*>(static_cast<float*>(a.y) + to) = make_float4(y[0], y[1], y[2], y[3]);
-                    else if (a.ftype == QTZ_F16) *reinterpret_cast<uint2*>(static_cast<__half*>(a.y) + to) = make_uint2(pack2(y[0], y[1], __half()), pack2(y[2], y[3], __half()));
-                    else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.y) + to) = make_uint2(pack2(y[0], y[1], __nv_bfloat16()), pack2(y[2], y[3], __nv_bfloat16()));
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (o + e < a.n) put(a, to + e, y[e]);
-                }
+                put_quad(a, r0 + q / (kF8Block / 4), at.n_tile * kF8Block + q % (kF8Block / 4) * 4, v[j]);
             }
         }
     }
@@ -284,7 +322,12 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
-    const int u0 = blockIdx.x * a.share, count = min(u0 + a.share, a.units) - u0;
+    int u0 = blockIdx.x * a.share, count = min(u0 + a.share, a.units) - u0;
+    if (a.split) {
+        const int tile = blockIdx.x / a.split, part = blockIdx.x % a.split, first = part * a.k_blocks / a.split;
+        u0 = tile * a.k_blocks + first;
+        count = (part + 1) * a.k_blocks / a.split - first;
+    }
     bool ok = true;
     auto wait = [&](uint64_t& bar, int parity) { ok = mbar_wait_warp(smem_u32(&bar), parity, a.wait_budget, ok); };
     grid_launch_dependents();
@@ -411,7 +454,12 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
             if (ends || i == count - 1) {              // the end of this tile, or of this CTA's columns of it
                 const bool begins = i >= here.kb;
                 const int64_t row = static_cast<int64_t>(here.row_tile) * kF8Block + row_warp;
-                if (begins && ends) {
+                if (a.split > 1) {
+                    // the ring is free: all its products are done
+#pragma unroll
+                    for (int c = 0; c < 64; c += 4)
+                        if (row_warp + lane < kRows) sts128(quad_at(base, row_warp + lane, (half * 64 + c) / 4), make_float4(acc[c], acc[c + 1], acc[c + 2], acc[c + 3]));
+                } else if (begins && ends) {
                     put_y(a, row, here.n_tile * kF8Block + half * 64, out, acc);
                 } else {
                     if (lane == 0) s_open[begins ? 1 : 0] = u0 + i;
@@ -436,7 +484,13 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
         tc_fence_after();
         tmem_dealloc(tmem, kBuffers * 128);
     }
-    if (!s_failed) join_tiles(a, s_open, s_last);      // after a wait that gave up the results are void
+    if (a.split > 1) {
+        cluster_sync();                                // the cluster's sums are there
+        join_cluster(a, Unit(a, u0), base);
+        cluster_sync();                                // and have been read
+    } else if (!s_failed) {
+        join_tiles(a, s_open, s_last);                 // after a wait that gave up the results are void
+    }
 }
 
 // ---- many rows: CTA pairs on tiles of 256 rows of x and 256 weights ----
@@ -656,6 +710,21 @@ qtz_status ensure_scratch(qtz_ctx* h, cudaStream_t st)
     cudaFuncAttributes at;
     QTZ_CUDA(h, cudaFuncGetAttributes(&at, reinterpret_cast<const void*>(pair_kernel)));
     if (at.numRegs < kPairLaunch) return QTZ_ERR_UNSUPPORTED;      // its warps would wait for registers that nobody gives back
+    const qtz_status s = qtz_allow_smem(h, stream_kernel<kF8Block>);
+    if (s != QTZ_OK) return s;
+    for (int c = 2; c <= kMaxSplit; ++c) {             // clusters that run at once: an SM holds one CTA of any of the stream kernels
+        cudaLaunchAttribute size;
+        size.id = cudaLaunchAttributeClusterDimension;
+        size.val.clusterDim.x = c;
+        size.val.clusterDim.y = size.val.clusterDim.z = 1;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(c);
+        cfg.blockDim = dim3(kStreamThreads);
+        cfg.dynamicSmemBytes = Stream<kF8Block>::kSmem;
+        cfg.attrs = &size;
+        cfg.numAttrs = 1;
+        QTZ_CUDA(h, cudaOccupancyMaxActiveClusters(&h->f8_clusters[c], stream_kernel<kF8Block>, &cfg));
+    }
     const size_t parts = static_cast<size_t>(h->num_sms) * 2 * kF8Block * 128 * sizeof(float);
     QTZ_CUDA(h, cudaMalloc(&h->f8_dev, parts + h->num_sms * sizeof(int32_t)));
     QTZ_CUDA(h, cudaMemsetAsync(static_cast<uint8_t*>(h->f8_dev) + parts, 0, h->num_sms * sizeof(int32_t), st));
@@ -669,10 +738,31 @@ qtz_status launch_stream(qtz_f8_layer* p, LinearArgs& a, const CUtensorMap& x_ma
     qtz_ctx* h = p->h;
     a.row_tiles = static_cast<int32_t>((a.rows + kF8Block - 1) / kF8Block);
     a.units = a.row_tiles * a.n_tiles * a.k_blocks;
-    a.share = (a.units + h->num_sms - 1) / h->num_sms;
+    const int tiles = a.row_tiles * a.n_tiles;
     const qtz_status s = qtz_allow_smem(h, stream_kernel<kRows>);
     if (s != QTZ_OK) return s;
-    QTZ_CUDA(h, qtz_launch_dependent(stream_kernel<kRows>, dim3((a.units + a.share - 1) / a.share), kStreamThreads, Stream<kRows>::kSmem, st, a, p->w_map, x_map));
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    if (tiles <= h->num_sms) {
+        a.split = 1;
+        for (int c = 2; c <= kMaxSplit && c <= a.k_blocks; ++c)
+            if (tiles <= h->f8_clusters[c]) a.split = c;
+        at[1].val.clusterDim.x = a.split;
+        cfg.gridDim = dim3(tiles * a.split);
+    } else {
+        a.share = (a.units + h->num_sms - 1) / h->num_sms;
+        cfg.gridDim = dim3((a.units + a.share - 1) / a.share);
+    }
+    cfg.blockDim = dim3(kStreamThreads);
+    cfg.dynamicSmemBytes = Stream<kRows>::kSmem;
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    QTZ_CUDA(h, cudaLaunchKernelEx(&cfg, stream_kernel<kRows>, a, p->w_map, x_map));
     return QTZ_OK;
 }
 
@@ -775,7 +865,7 @@ extern "C" qtz_status qtz_f8_linear(qtz_f8_linear_plan p, const uint8_t* codes_d
     qtz_device_guard guard(h->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     LinearArgs a{p->scales, p->bias, scales_dev, scales_row_stride, scales_block_stride, rows, y_stride, y_dev, p->n, p->n_tiles, p->k_blocks, ftype,
-                 qtz_aligned16(y_dev) && (rows <= 1 || y_stride * (ftype == QTZ_F32 ? 4 : 2) % 16 == 0), 0, 0, 0,
+                 qtz_aligned16(y_dev) && (rows <= 1 || y_stride * (ftype == QTZ_F32 ? 4 : 2) % 16 == 0), 0, 0, 0, 0,
                  static_cast<float*>(h->f8_dev), h->f8_counters, h->wait_budget, h->status_dev};
     const bool pair = rows > 512;
     const int box_rows = pair ? 128 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
