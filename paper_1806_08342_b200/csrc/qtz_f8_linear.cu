@@ -13,7 +13,7 @@ struct qtz_f8_layer {
     int device = 0;                    // a plan may be destroyed after its handle
     int32_t n = 0, k = 0;
     int32_t n_tiles = 0, k_blocks = 0; // of 128 rows, of 128 columns
-    uint8_t* tiles = nullptr;          // [n_tiles][k_blocks][128][128] codes, zeros beyond n and k
+    uint8_t* tiles = nullptr;          // [n_tiles / 2, rounded up][k_blocks][256][128] codes, zeros beyond k; what lies beyond n is not used
     float* scales = nullptr;           // [n_tiles][k_blocks], behind the tiles in the same allocation
     float* bias = nullptr;             // [n], behind the scales; null: none
     CUtensorMap w_map{};               // the tiles as rows of 128 bytes, 128 rows at a time
@@ -29,10 +29,11 @@ struct PackArgs {
     uint8_t* tiles;
 };
 
-// A CTA a tile.
+// A CTA a block of 128 x 128.
 __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackArgs a)
 {
-    uint8_t* const tile = a.tiles + (static_cast<int64_t>(blockIdx.y) * a.k_blocks + blockIdx.x) * (kF8Block * kF8Block);
+    const int64_t place = (static_cast<int64_t>(blockIdx.y / 2) * a.k_blocks + blockIdx.x) * 2 + blockIdx.y % 2;
+    uint8_t* const tile = a.tiles + place * (kF8Block * kF8Block);
     for (int i = threadIdx.x; i < kF8Block * kF8Block; i += 256) {
         const int64_t row = static_cast<int64_t>(blockIdx.y) * kF8Block + i / kF8Block;
         const int col = blockIdx.x * kF8Block + i % kF8Block;
@@ -61,6 +62,9 @@ struct LinearArgs {
     int32_t* status;
 };
 
+constexpr int kThreads = 384, kSumThreads = 256;         // loads, products (two warps), scales; eight warps for the sums
+constexpr int kLaunchRegs = 168, kFew = 80, kMany = 208;   // registers of a thread: at launch, of the first four warps, of the others
+static_assert(4 * 32 * kFew + 8 * 32 * kMany <= kThreads * kLaunchRegs, "more registers than the CTA was launched with");
 constexpr int kTileBytes = kF8Block * kF8Block;
 constexpr int kSmemLimit = 227 * 1024;
 constexpr int kMaxStages = 12;
@@ -151,40 +155,70 @@ __device__ __forceinline__ void put_y(const LinearArgs& a, int64_t row, int o, u
     else put_rows(static_cast<float*>(a.y) + at, a.y_stride, rows, cols, a.vector, out, acc);
 }
 
+// First row, among the packed tiles' rows, of half a tile of 256 weights.
+__device__ __forceinline__ int w_row(const LinearArgs& a, int col, int kb, int half) { return ((col * a.k_blocks + kb) * 2 + half) * kF8Block; }
+
+// Adds a block's products, 128 columns from `from` of tensor memory on, times s; `read` is called once they have been read out, before the
+// last of them are added.  What is held at a time is what the registers allow.
+template <typename Read>
+__device__ __forceinline__ void add_block(float (&acc)[128], uint32_t from, float s, Read read)
+{
+    uint32_t v0[32], v1[32];
+    auto take = [&](const uint32_t (&v)[32], int at) {
+#pragma unroll
+        for (int c = 0; c < 32; c += 2) fma2(acc[at + c], acc[at + c + 1], __uint_as_float(v[c]), __uint_as_float(v[c + 1]), s, s);
+    };
+    tmem_ld_32x32(from, v0);
+    tmem_ld_32x32(from + 32, v1);
+    tmem_ld_wait_for(v0);
+    tmem_ld_tie(v1);
+    take(v0, 0);
+    tmem_ld_32x32(from + 64, v0);
+    take(v1, 32);
+    tmem_ld_32x32(from + 96, v1);
+    tmem_ld_wait_for(v0);
+    tmem_ld_tie(v1);
+    tc_fence_before();
+    __syncwarp();
+    read();
+    take(v0, 64);
+    take(v1, 96);
+}
+
 // Places for the scales of blocks, and how many blocks ahead they are asked for.  A thread of the sums reads its block's factor a block
 // early, so that the loads of a block's scales are counted with the product of the block before.
 constexpr int kSlots = 8, kAhead = 4;
 
 // ---- few rows: the weights stream past a tile of rows ----
-// A tile is 128 rows of x, of which kRows are loaded (what the other rows of the product hold is not looked at), and 128 weights.  Where
+// A tile is 128 rows of x, of which kRows are loaded (what the other rows of the product hold is not looked at), and 256 weights.  Where
 // there are fewer tiles than SMs, the CTAs of a cluster take equal parts of a tile's columns and join their sums through each other's shared
 // memory.  Where there are more, units (tile, block of 128 columns) form one sequence that is dealt out in equal contiguous shares; a tile
-// that lies in several shares is joined by the last CTA to arrive.  A thread owns a row of x and half of the weights: one factor a thread and unit.
-constexpr int kStreamThreads = 384;    // loads, products (two warps), scales, eight warps for the sums
-constexpr int kBuffers = 4;            // of 128 columns of tensor memory
+// that lies in several shares is joined by the last CTA to arrive.  A thread owns a row of x and half of the weights, which share a scale:
+// one factor a thread and unit.
 constexpr int kMaxSplit = 8;           // CTAs of a cluster
+constexpr int kTileCols = 256, kQuads = kTileCols / 4;
 
 template <int kRows>
 struct Stream {
-    static constexpr int kStage = kTileBytes + kRows * kF8Block;
-    static constexpr int kRoom = (kSmemLimit - 1024 - 8 * kOutBytes - kSlots * (kRows + 1) * 4 - 1024) / kStage, kStages = kRoom < kMaxStages ? kRoom / 2 * 2 : kMaxStages;
+    static constexpr int kStage = 2 * kTileBytes + kRows * kF8Block;
+    static constexpr int kRoom = (kSmemLimit - 1024 - 8 * kOutBytes - kSlots * (kRows + 2) * 4 - 1024) / kStage, kStages = kRoom < kMaxStages ? kRoom : kMaxStages;
     static constexpr int kSmem = 1024 + kStages * kStage + 8 * kOutBytes;
 };
 
-struct Unit {                          // row tiles of the same weights follow each other
-    int n_tile, row_tile, kb;
-    __device__ Unit(const LinearArgs& a, int u) : n_tile(u / a.k_blocks / a.row_tiles), row_tile(u / a.k_blocks % a.row_tiles), kb(u % a.k_blocks) {}
+struct Unit {                          // row tiles of the same 256 weights follow each other
+    int col, row_tile, kb;
+    __device__ Unit(const LinearArgs& a, int u) : col(u / a.k_blocks / a.row_tiles), row_tile(u / a.k_blocks % a.row_tiles), kb(u % a.k_blocks) {}
     __device__ void next(const LinearArgs& a)
     {
         if (++kb < a.k_blocks) return;
         kb = 0;
         if (++row_tile < a.row_tiles) return;
         row_tile = 0;
-        ++n_tile;
+        ++col;
     }
 };
 
-__device__ __forceinline__ float* part_of(const LinearArgs& a, int cta, int which) { return a.parts + (static_cast<int64_t>(cta) * 2 + which) * (kF8Block * kF8Block); }
+__device__ __forceinline__ float* part_of(const LinearArgs& a, int cta, int which) { return a.parts + (static_cast<int64_t>(cta) * 2 + which) * (kF8Block * kTileCols); }
 
 // Four neighbouring sums.
 __device__ __forceinline__ void put_quad(const LinearArgs& a, int64_t row, int o, float4 v)
@@ -203,18 +237,18 @@ __device__ __forceinline__ void put_quad(const LinearArgs& a, int64_t row, int o
     }
 }
 
-// Sums of a tile that the CTAs of a cluster hold in shared memory, [row][32 quads of columns], a quad at its number ^ (row % 32) (for the
+// Sums of a tile that the CTAs of a cluster hold in shared memory, [row][64 quads of columns], a quad at its number ^ (row % 32) (for the
 // banks): each CTA takes an equal part of the quads and adds them up in the order of the columns.
-__device__ __forceinline__ uint32_t quad_at(uint32_t base, int row, int quad) { return base + (row * 32 + (quad ^ (row & 31))) * 16; }
+__device__ __forceinline__ uint32_t quad_at(uint32_t base, int row, int quad) { return base + (row * kQuads + (quad ^ (row & 31))) * 16; }
 
 __device__ __forceinline__ void join_cluster(const LinearArgs& a, const Unit& tile, uint32_t base)
 {
     const int64_t r0 = static_cast<int64_t>(tile.row_tile) * kF8Block;
-    const int quads = static_cast<int>(min(static_cast<int64_t>(kF8Block), a.rows - r0)) * 32, rank = static_cast<int>(cluster_ctarank());
+    const int quads = static_cast<int>(min(static_cast<int64_t>(kF8Block), a.rows - r0)) * kQuads, rank = static_cast<int>(cluster_ctarank());
     const int end = (rank + 1) * quads / a.split;
-    for (int q = rank * quads / a.split + threadIdx.x; q < end; q += kStreamThreads) {
+    for (int q = rank * quads / a.split + threadIdx.x; q < end; q += kThreads) {
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        const uint32_t own = quad_at(base, q >> 5, q & 31);
+        const uint32_t own = quad_at(base, q / kQuads, q % kQuads);
 #pragma unroll 4
         for (int c = 0; c < a.split; ++c) {
             const float4 p = lds_cluster(mapa_shared(own, c));
@@ -223,15 +257,15 @@ __device__ __forceinline__ void join_cluster(const LinearArgs& a, const Unit& ti
             v.z += p.z;
             v.w += p.w;
         }
-        put_quad(a, r0 + (q >> 5), tile.n_tile * kF8Block + (q & 31) * 4, v);
+        put_quad(a, r0 + q / kQuads, tile.col * kTileCols + q % kQuads * 4, v);
     }
 }
 
 // After a CTA's last unit: counts its arrival at the tiles that it shares with others, and sums those at which it is the last, in the
-// order of the columns.  Called by all threads, behind a barrier of the CTA.
+// order of the columns.  Called by the warps of the sums, behind a barrier of theirs.
 __device__ __forceinline__ void join_tiles(const LinearArgs& a, const int (&open)[2], int (&last)[2])
 {
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x - (kThreads - kSumThreads);
     auto first = [&](int unit) { return unit / a.k_blocks * a.k_blocks; };
     if ((tid == 0 && open[0] >= 0) || (tid == 32 && open[1] >= 0)) {
         const int begin = first(tid ? open[1] : open[0]), c0 = begin / a.share;
@@ -239,7 +273,7 @@ __device__ __forceinline__ void join_tiles(const LinearArgs& a, const int (&open
         last[tid ? 1 : 0] = all;
         if (all) a.counters[c0] = 0;                   // ready for the next call
     }
-    __syncthreads();
+    named_barrier(1, kSumThreads);
 #pragma unroll 1
     for (int which = 0; which < 2; ++which) {
         const int unit = open[which];
@@ -247,10 +281,10 @@ __device__ __forceinline__ void join_tiles(const LinearArgs& a, const int (&open
         const int begin = first(unit), c0 = begin / a.share, c1 = (begin + a.k_blocks - 1) / a.share;
         const Unit at(a, unit);
         const int64_t r0 = static_cast<int64_t>(at.row_tile) * kF8Block;
-        const int quads = static_cast<int>(min(static_cast<int64_t>(kF8Block), a.rows - r0)) * (kF8Block / 4);
+        const int quads = static_cast<int>(min(static_cast<int64_t>(kF8Block), a.rows - r0)) * kQuads;
         constexpr int kAtOnce = 6, kParts = 4;         // loads under way: of a pass over all rows there are two
 #pragma unroll 1
-        for (int q0 = tid; q0 < quads; q0 += kAtOnce * kStreamThreads) {
+        for (int q0 = tid; q0 < quads; q0 += kAtOnce * kSumThreads) {
             float4 v[kAtOnce];
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j) v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -262,7 +296,7 @@ __device__ __forceinline__ void join_tiles(const LinearArgs& a, const int (&open
                     const float4* const part = reinterpret_cast<const float4*>(part_of(a, c + x, c + x == c0 ? 1 : 0)) + q0;
 #pragma unroll
                     for (int j = 0; j < kAtOnce; ++j)
-                        p[x][j] = c + x <= c1 && q0 + j * kStreamThreads < quads ? __ldcg(part + j * kStreamThreads) : make_float4(0.f, 0.f, 0.f, 0.f);
+                        p[x][j] = c + x <= c1 && q0 + j * kSumThreads < quads ? __ldcg(part + j * kSumThreads) : make_float4(0.f, 0.f, 0.f, 0.f);
                 }
 #pragma unroll
                 for (int x = 0; x < kParts; ++x)
@@ -276,30 +310,29 @@ __device__ __forceinline__ void join_tiles(const LinearArgs& a, const int (&open
             }
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j) {
-                const int q = q0 + j * kStreamThreads;
+                const int q = q0 + j * kSumThreads;
                 if (q >= quads) break;
-                put_quad(a, r0 + q / (kF8Block / 4), at.n_tile * kF8Block + q % (kF8Block / 4) * 4, v[j]);
+                put_quad(a, r0 + q / kQuads, at.col * kTileCols + q % kQuads * 4, v[j]);
             }
         }
     }
 }
 
 template <int kRows>
-__global__ void __launch_bounds__(kStreamThreads, 1)
+__global__ void __launch_bounds__(kThreads, 1)
 stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map)
 {
     using S = Stream<kRows>;
     extern __shared__ uint8_t smem_raw[];              // the ring: kRows rows of x, a tile of weights; then values on their way out
-    __shared__ float s_x[kSlots][kRows], s_w[kSlots];  // scales
-    __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_done[kBuffers], s_free[kBuffers], s_drain;
-    __shared__ int s_open[2], s_last[2], s_failed;     // s_open: units whose tiles are shared with an earlier / a later CTA
+    __shared__ float s_x[kSlots][kRows], s_w[kSlots][2];               // scales
+    __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_done[2], s_free[2], s_drain;
+    __shared__ int s_open[2], s_last[2];               // s_open: units whose tiles are shared with an earlier / a later CTA
     __shared__ uint32_t s_tmem;
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     // warps of the sums whose rows exist: those of a quarter of tensor memory take 32 rows
     const int quarters = static_cast<int>(min(static_cast<int64_t>(4), (a.rows + 31) / 32));
     if (tid == 0) {
-        s_failed = 0;
         s_open[0] = s_open[1] = -1;
         prefetch_tensormap(&w_map);
         prefetch_tensormap(&x_map);
@@ -307,14 +340,14 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
             mbar_init(smem_u32(&s_full[i]), 1);
             mbar_init(smem_u32(&s_empty[i]), 1);
         }
-        for (int i = 0; i < kBuffers; ++i) {
+        for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&s_done[i]), 2);        // the product; scales
             mbar_init(smem_u32(&s_free[i]), 2 * quarters);
         }
         mbar_init(smem_u32(&s_drain), 2);
     }
     if (warp == 1) {
-        tmem_alloc(smem_u32(&s_tmem), kBuffers * 128);
+        tmem_alloc(smem_u32(&s_tmem), 512);
         tmem_relinquish();
     }
     fence_barrier_init();
@@ -332,164 +365,158 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
     auto wait = [&](uint64_t& bar, int parity) { ok = mbar_wait_warp(smem_u32(&bar), parity, a.wait_budget, ok); };
     grid_launch_dependents();
 
-    if (warp == 0) {
-        // ======== loads ========
-        Unit here(a, u0), ahead = here;
-        auto weights = [&](int stage) {
-            if (elect_one()) {
-                const uint32_t bar = smem_u32(&s_full[stage]);
-                mbar_arrive_expect_tx(bar, S::kStage);
-                tma_load_2d(base + stage * S::kStage + kRows * kF8Block, &w_map, bar, 0, (ahead.n_tile * a.k_blocks + ahead.kb) * kF8Block);
-            }
-            __syncwarp();
-            ahead.next(a);
-        };
-        auto rows = [&](int stage) {
-            if (elect_one()) tma_load_2d(base + stage * S::kStage, &x_map, smem_u32(&s_full[stage]), here.kb * kF8Block, here.row_tile * kF8Block);
-            __syncwarp();
-            here.next(a);
-        };
-        const int early = min(S::kStages, count);
-        for (int i = 0; i < early; ++i) weights(i);    // they were there when the layer was made
-        grid_dependency_wait();                        // all else is waited for
-        for (int i = 0; i < early; ++i) rows(i);
-        int issued = early, stage = 0, round = 0;
-        for (; issued < count; ++issued) {
-            wait(s_empty[stage], round & 1);
-            if (!ok) break;
-            weights(stage);
-            rows(stage);
-            if (++stage == S::kStages) {
-                stage = 0;
-                ++round;
-            }
-        }
-        // nothing may be in flight when the CTA ends
-        for (int j = max(0, issued - S::kStages); j < issued; ++j) ok = mbar_wait_warp(smem_u32(&s_full[j % S::kStages]), (j / S::kStages) & 1, kDrainBudget, ok);
-    } else if (warp == 1 || warp == 3) {
-        // ======== products: a warp for the even units, one for the odd ones ========
-        const int odd = warp >> 1;
-        int stage = odd, round = 0;
-        for (int i = odd; i < count; i += 2) {
-            const int buffer = i % kBuffers;
-            wait(s_full[stage], round & 1);
-            if (i >= kBuffers) wait(s_free[buffer], (i / kBuffers & 1) ^ 1);
-            if (!ok) break;
-            tc_fence_after();
-            if (elect_one()) {
-                const uint64_t x = make_kmajor_desc(base + stage * S::kStage, 128), w = make_kmajor_desc(base + stage * S::kStage + kRows * kF8Block, 128);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) mma_f8(tmem + buffer * 128, x + 2 * k, w + 2 * k, kProduct<128, 128>, k > 0);
-                mma_commit(smem_u32(&s_done[buffer]));
-                mma_commit(smem_u32(&s_empty[stage]));
-            }
-            __syncwarp();
-            stage += 2;                                // the number of stages is even
-            if (stage >= S::kStages) {
-                stage -= S::kStages;
-                ++round;
-            }
-        }
-        if (elect_one()) mma_commit(smem_u32(&s_drain));   // the others may have given up on what is still running
-        __syncwarp();
-    } else if (warp == 2) {
-        // ======== scales ========
-        grid_dependency_wait();
-        Unit here(a, u0);
-        for (int i = 0; i < count + kAhead; ++i) {
-            const int now = i - kAhead;
-            if (now >= 0) {
-                cp_async_wait<kAhead - 2>();           // the unit's scales and the next one's
+    if (warp < 4) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFew));
+        if (warp == 0) {
+            // ======== loads ========
+            Unit here(a, u0), ahead = here;
+            auto weights = [&](int stage) {
+                if (elect_one()) {
+                    const uint32_t bar = smem_u32(&s_full[stage]), to = base + stage * S::kStage + kRows * kF8Block;
+                    const bool both = 2 * ahead.col + 1 < a.n_tiles;
+                    mbar_arrive_expect_tx(bar, both ? S::kStage : S::kStage - kTileBytes);
+                    tma_load_2d(to, &w_map, bar, 0, w_row(a, ahead.col, ahead.kb, 0));
+                    if (both) tma_load_2d(to + kTileBytes, &w_map, bar, 0, w_row(a, ahead.col, ahead.kb, 1));
+                }
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&s_done[now % kBuffers]));
-            }
-            // What the place held, kSlots units ago, has been used up where the unit after it has been read out; that also says that the
-            // product that was counted kBuffers units before the next one is done.
-            const int read = now - kAhead + 1;
-            if (read >= 0) wait(s_free[read % kBuffers], read / kBuffers & 1);
-            if (!ok) break;
-            if (i < count) {
-                const int slot = i % kSlots;
-                const int64_t r0 = static_cast<int64_t>(here.row_tile) * kF8Block;
-#pragma unroll
-                for (int r = lane; r < kRows; r += 32)
-                    cp_async_4(smem_u32(&s_x[slot][r]), a.x_scales + min(r0 + r, a.rows - 1) * a.row_stride + here.kb * a.block_stride);
-                if (lane == 0) cp_async_4(smem_u32(&s_w[slot]), a.w_scales + static_cast<int64_t>(here.n_tile) * a.k_blocks + here.kb);
+                ahead.next(a);
+            };
+            auto rows = [&](int stage) {
+                if (elect_one()) tma_load_2d(base + stage * S::kStage, &x_map, smem_u32(&s_full[stage]), here.kb * kF8Block, here.row_tile * kF8Block);
+                __syncwarp();
                 here.next(a);
+            };
+            const int early = min(S::kStages, count);
+            for (int i = 0; i < early; ++i) weights(i);    // they were there when the layer was made
+            grid_dependency_wait();                        // all else is waited for
+            for (int i = 0; i < early; ++i) rows(i);
+            int issued = early, stage = 0, round = 0;
+            for (; issued < count; ++issued) {
+                wait(s_empty[stage], round & 1);
+                if (!ok) break;
+                weights(stage);
+                rows(stage);
+                if (++stage == S::kStages) {
+                    stage = 0;
+                    ++round;
+                }
             }
-            cp_async_commit();
-        }
-        cp_async_wait<0>();
-    } else if ((warp & 3) < quarters) {
-        // ======== sums ========
-        const int half = (warp - 4) >> 2, row_warp = (warp & 3) * 32, row_lane = min(row_warp + lane, kRows - 1);
-        const uint32_t from = tmem + (static_cast<uint32_t>(warp & 3) << 21) + half * 64;
-        uint4* const out = reinterpret_cast<uint4*>(smem_raw + (base - smem_u32(smem_raw)) + S::kStages * S::kStage + (warp - 4) * kOutBytes);
-        float acc[64];
+            // nothing may be in flight when the CTA ends
+            for (int j = max(0, issued - S::kStages); j < issued; ++j) ok = mbar_wait_warp(smem_u32(&s_full[j % S::kStages]), (j / S::kStages) & 1, kDrainBudget, ok);
+        } else if (warp == 1 || warp == 3) {
+            // ======== products: a warp for the even units, one for the odd ones ========
+            const int buffer = warp >> 1;
+            int stage = buffer, round = 0;
+            for (int i = buffer; i < count; i += 2) {
+                wait(s_full[stage], round & 1);
+                if (i >= 2) wait(s_free[buffer], (i >> 1 & 1) ^ 1);
+                if (!ok) break;
+                tc_fence_after();
+                if (elect_one()) {
+                    const uint64_t x = make_kmajor_desc(base + stage * S::kStage, 128), w = make_kmajor_desc(base + stage * S::kStage + kRows * kF8Block, 128);
 #pragma unroll
-        for (int c = 0; c < 64; ++c) acc[c] = 0.f;
-        grid_dependency_wait();                        // y may be what the kernel before reads
-        Unit here(a, u0);
-        float s_next = 0.f;
-        for (int i = 0; i < count; ++i) {
-            const int buffer = i % kBuffers, after = (i + 1) % kSlots;
-            wait(s_done[buffer], i / kBuffers & 1);
-            if (!ok) break;
-            tc_fence_after();
-            uint32_t v0[32], v1[32];
-            tmem_ld_32x32(from + buffer * 128, v0);
-            tmem_ld_32x32(from + buffer * 128 + 32, v1);
-            const float s = i ? s_next : s_x[0][row_lane] * s_w[0];
-            s_next = s_x[after][row_lane] * s_w[after];
-            tmem_ld_wait_for(v0);
-            tmem_ld_tie(v1);
-            tc_fence_before();
+                    for (int k = 0; k < 4; ++k) mma_f8(tmem + buffer * 256, x + 2 * k, w + 2 * k, kProduct<128, 256>, k > 0);
+                    mma_commit(smem_u32(&s_done[buffer]));
+                    mma_commit(smem_u32(&s_empty[stage]));
+                }
+                __syncwarp();
+                stage += 2;
+                if (stage >= S::kStages) {
+                    stage -= S::kStages;
+                    ++round;
+                }
+            }
+            if (elect_one()) mma_commit(smem_u32(&s_drain));   // the others may have given up on what is still running
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&s_free[buffer]));
+        } else if (warp == 2) {
+            // ======== scales ========
+            grid_dependency_wait();
+            Unit here(a, u0);
+            for (int i = 0; i < count + kAhead; ++i) {
+                const int now = i - kAhead;
+                if (now >= 0) {
+                    cp_async_wait<kAhead - 2>();       // the unit's scales and the next one's
+                    __syncwarp();
+                    if (now >= 2) wait(s_done[now & 1], (now >> 1 & 1) ^ 1);
+                    if (!ok) break;
+                    if (lane == 0) mbar_arrive(smem_u32(&s_done[now & 1]));
+                }
+                // The place held the scales of eight units ago, which have been used: the product of the unit two behind them, which waited for
+                // that, is done.
+                if (i < count) {
+                    const int slot = i % kSlots;
+                    const int64_t r0 = static_cast<int64_t>(here.row_tile) * kF8Block;
 #pragma unroll
-            for (int c = 0; c < 32; c += 2) fma2(acc[c], acc[c + 1], __uint_as_float(v0[c]), __uint_as_float(v0[c + 1]), s, s);
+                    for (int r = lane; r < kRows; r += 32)
+                        cp_async_4(smem_u32(&s_x[slot][r]), a.x_scales + min(r0 + r, a.rows - 1) * a.row_stride + here.kb * a.block_stride);
+                    if (lane < 2) cp_async_4(smem_u32(&s_w[slot][lane]), a.w_scales + static_cast<int64_t>(min(2 * here.col + lane, a.n_tiles - 1)) * a.k_blocks + here.kb);
+                    here.next(a);
+                }
+                cp_async_commit();
+            }
+            cp_async_wait<0>();
+        }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kMany));
+        if ((warp & 3) < quarters) {
+            // ======== sums ========
+            const int half = (warp - 4) >> 2, row_warp = (warp & 3) * 32, row_lane = min(row_warp + lane, kRows - 1);
+            const uint32_t from = tmem + (static_cast<uint32_t>(warp & 3) << 21) + half * 128;
+            uint4* const out = reinterpret_cast<uint4*>(smem_raw + (base - smem_u32(smem_raw)) + S::kStages * S::kStage + (warp - 4) * kOutBytes);
+            grid_dependency_wait();                    // y may be what the kernel before reads
+            float acc[128];
+            float s_next = 0.f;                        // the next unit's factor: its scales are there with this unit's
+            Unit here(a, u0);
+            for (int i = 0; ok && i < count;) {            // a tile, or what this CTA has of it
 #pragma unroll
-            for (int c = 0; c < 32; c += 2) fma2(acc[32 + c], acc[33 + c], __uint_as_float(v1[c]), __uint_as_float(v1[c + 1]), s, s);
-            const bool ends = here.kb == a.k_blocks - 1;
-            if (ends || i == count - 1) {              // the end of this tile, or of this CTA's columns of it
-                const bool begins = i >= here.kb;
+                for (int c = 0; c < 128; ++c) acc[c] = 0.f;
+                const bool begins = here.kb == 0, ends = i + a.k_blocks - here.kb <= count;
+                const int last = ends ? i + a.k_blocks - here.kb : count;
+#pragma unroll 1
+                for (; i < last; ++i) {
+                    const int slot = i % kSlots, after = (i + 1) % kSlots;
+                    wait(s_done[i & 1], i >> 1 & 1);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const float s = i ? s_next : s_x[slot][row_lane] * s_w[slot][half];
+                    s_next = s_x[after][row_lane] * s_w[after][half];
+                    add_block(acc, from + (i & 1) * 256, s, [&]() {
+                        if (lane == 0) mbar_arrive(smem_u32(&s_free[i & 1]));
+                    });
+                }
+                if (!ok) break;
                 const int64_t row = static_cast<int64_t>(here.row_tile) * kF8Block + row_warp;
                 if (a.split > 1) {
                     // the ring is free: all its products are done
 #pragma unroll
-                    for (int c = 0; c < 64; c += 4)
-                        if (row_warp + lane < kRows) sts128(quad_at(base, row_warp + lane, (half * 64 + c) / 4), make_float4(acc[c], acc[c + 1], acc[c + 2], acc[c + 3]));
+                    for (int c = 0; c < 128; c += 4)
+                        if (row_warp + lane < kRows) sts128(quad_at(base, row_warp + lane, (half * 128 + c) / 4), make_float4(acc[c], acc[c + 1], acc[c + 2], acc[c + 3]));
                 } else if (begins && ends) {
-                    put_y(a, row, here.n_tile * kF8Block + half * 64, out, acc);
+                    put_y(a, row, here.col * kTileCols + half * 128, out, acc);
                 } else {
-                    if (lane == 0) s_open[begins ? 1 : 0] = u0 + i;
-                    put_rows(part_of(a, blockIdx.x, begins ? 1 : 0) + row_warp * kF8Block + half * 64, kF8Block, static_cast<int>(min(static_cast<int64_t>(32), a.rows - row)), 64,
+                    if (lane == 0) s_open[begins ? 1 : 0] = u0 + i - 1;
+                    put_rows(part_of(a, blockIdx.x, begins ? 1 : 0) + row_warp * kTileCols + half * 128, kTileCols, static_cast<int>(min(static_cast<int64_t>(32), a.rows - row)), 128,
                              true, out, acc);
                 }
-#pragma unroll
-                for (int c = 0; c < 64; ++c) acc[c] = 0.f;
+                here.kb = a.k_blocks - 1;
+                here.next(a);
             }
-            here.next(a);
         }
+        if (!a.split && named_barrier_and(1, kSumThreads, ok)) join_tiles(a, s_open, s_last);   // after a wait that gave up the results are void
     }
-    if (!ok) {
-        timed_out(a);
-        s_failed = 1;
-    }
+    if (!ok) timed_out(a);
     tc_fence_before();
     __syncthreads();
     if (warp == 1) {
         (void)mbar_wait(smem_u32(&s_drain), 0, kDrainBudget);
         __syncwarp();
         tc_fence_after();
-        tmem_dealloc(tmem, kBuffers * 128);
+        tmem_dealloc(tmem, 512);
     }
     if (a.split > 1) {
         cluster_sync();                                // the cluster's sums are there
         join_cluster(a, Unit(a, u0), base);
         cluster_sync();                                // and have been read
-    } else if (!s_failed) {
-        join_tiles(a, s_open, s_last);                 // after a wait that gave up the results are void
     }
 }
 
@@ -497,9 +524,6 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
 // Each CTA of a pair holds 128 of the rows and 128 of the weights; its half of the product, 128 rows x 256 columns, lies in its own
 // tensor memory, twice, so that one block of 128 columns is multiplied while the sums of the one before are taken.  A thread owns a row
 // of x and half of the columns, which share a scale of the weights: one factor a thread and block.
-constexpr int kPairThreads = 384;      // four warps that load, multiply and fetch scales, eight for the sums
-constexpr int kPairLaunch = 168, kPairFew = 80, kPairMany = 208;   // registers of a thread: at launch, then of either
-static_assert(4 * 32 * kPairFew + 8 * 32 * kPairMany <= kPairThreads * kPairLaunch, "more registers than the CTA was launched with");
 constexpr int kPairStage = 2 * kTileBytes;
 constexpr int kPairStages = 6;          // what the rows on their way to y leave room for
 constexpr int kBand = 16;              // row tiles that the pairs work on side by side, for the L2
@@ -515,7 +539,7 @@ struct PairTile {
     }
 };
 
-__global__ void __launch_bounds__(kPairThreads, 1)
+__global__ void __launch_bounds__(kThreads, 1)
 pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map)
 {
     extern __shared__ uint8_t smem_raw[];              // the ring: a tile of x, a tile of weights
@@ -552,14 +576,14 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
     grid_launch_dependents();
 
     if (warp < 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPairFew));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFew));
         if (warp == 0) {
             // ======== loads: both CTAs' are counted on the first one's barrier ========
             grid_dependency_wait();
             int stage = 0, round = 0, issued = 0;
             for (int tile = tile0; ok && tile < tiles; tile += step) {
                 const PairTile at(a, tile);
-                const int w_tile = min(2 * at.col + static_cast<int>(rank), a.n_tiles - 1), x_row = (2 * at.row + static_cast<int>(rank)) * kF8Block;
+                const int w_half = min(static_cast<int>(rank), a.n_tiles - 1 - 2 * at.col), x_row = (2 * at.row + static_cast<int>(rank)) * kF8Block;
                 for (int kb = 0; kb < a.k_blocks; ++kb) {
                     if (issued >= kPairStages) ok = mbar_wait_warp(smem_u32(&s_empty[stage]), (round & 1) ^ 1, a.wait_budget, ok);
                     if (!ok) break;
@@ -568,7 +592,7 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
                         if (rank == 0) mbar_arrive_expect_tx(own, 2 * kPairStage);
                         const uint32_t bar = mapa_shared(own, 0u);
                         tma_load_2d_pair(to, &x_map, bar, kb * kF8Block, x_row);
-                        tma_load_2d_pair(to + kTileBytes, &w_map, bar, 0, (w_tile * a.k_blocks + kb) * kF8Block);
+                        tma_load_2d_pair(to + kTileBytes, &w_map, bar, 0, w_row(a, at.col, kb, w_half));
                     }
                     __syncwarp();
                     ++issued;
@@ -645,7 +669,7 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
         }
     } else {
         // ======== sums ========
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPairMany));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kMany));
         const int half = (warp - 4) >> 2, row_lane = (warp & 3) * 32 + lane;
         const uint32_t from = tmem + (static_cast<uint32_t>(warp & 3) << 21) + half * 128;
         uint4* const out = reinterpret_cast<uint4*>(smem_raw + (base - smem_u32(smem_raw)) + kPairStages * kPairStage + (warp - 4) * kOutBytes);
@@ -664,27 +688,9 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
                 tc_fence_after();
                 const float s = block ? s_next : s_x[0][row_lane] * s_w[0][half];
                 s_next = s_x[(slot + 1) % kSlots][row_lane] * s_w[(slot + 1) % kSlots][half];
-                uint32_t v0[32], v1[32];
-                const uint32_t here = from + (block & 1) * 256;
-                auto take = [&](const uint32_t (&v)[32], int at) {
-#pragma unroll
-                    for (int c = 0; c < 32; c += 2) fma2(acc[at + c], acc[at + c + 1], __uint_as_float(v[c]), __uint_as_float(v[c + 1]), s, s);
-                };
-                tmem_ld_32x32(here, v0);
-                tmem_ld_32x32(here + 32, v1);
-                tmem_ld_wait_for(v0);
-                tmem_ld_tie(v1);
-                take(v0, 0);
-                tmem_ld_32x32(here + 64, v0);
-                take(v1, 32);
-                tmem_ld_32x32(here + 96, v1);
-                tmem_ld_wait_for(v0);
-                tmem_ld_tie(v1);
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_remote_relaxed(smem_u32(&s_free[block & 1]), 0u);
-                take(v0, 64);
-                take(v1, 96);
+                add_block(acc, from + (block & 1) * 256, s, [&]() {
+                    if (lane == 0) mbar_arrive_remote_relaxed(smem_u32(&s_free[block & 1]), 0u);
+                });
             }
             if (!ok) break;
             const PairTile at(a, tile);
@@ -707,9 +713,12 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
 qtz_status ensure_scratch(qtz_ctx* h, cudaStream_t st)
 {
     if (h->f8_dev) return QTZ_OK;
-    cudaFuncAttributes at;
-    QTZ_CUDA(h, cudaFuncGetAttributes(&at, reinterpret_cast<const void*>(pair_kernel)));
-    if (at.numRegs < kPairLaunch) return QTZ_ERR_UNSUPPORTED;      // its warps would wait for registers that nobody gives back
+    for (const void* kernel : {reinterpret_cast<const void*>(pair_kernel), reinterpret_cast<const void*>(stream_kernel<16>), reinterpret_cast<const void*>(stream_kernel<32>),
+                               reinterpret_cast<const void*>(stream_kernel<64>), reinterpret_cast<const void*>(stream_kernel<128>)}) {
+        cudaFuncAttributes at;
+        QTZ_CUDA(h, cudaFuncGetAttributes(&at, kernel));
+        if (at.numRegs < kLaunchRegs) return QTZ_ERR_UNSUPPORTED;  // its warps would wait for registers that nobody gives back
+    }
     const qtz_status s = qtz_allow_smem(h, stream_kernel<kF8Block>);
     if (s != QTZ_OK) return s;
     for (int c = 2; c <= kMaxSplit; ++c) {             // clusters that run at once: an SM holds one CTA of any of the stream kernels
@@ -719,13 +728,13 @@ qtz_status ensure_scratch(qtz_ctx* h, cudaStream_t st)
         size.val.clusterDim.y = size.val.clusterDim.z = 1;
         cudaLaunchConfig_t cfg = {};
         cfg.gridDim = dim3(c);
-        cfg.blockDim = dim3(kStreamThreads);
+        cfg.blockDim = dim3(kThreads);
         cfg.dynamicSmemBytes = Stream<kF8Block>::kSmem;
         cfg.attrs = &size;
         cfg.numAttrs = 1;
         QTZ_CUDA(h, cudaOccupancyMaxActiveClusters(&h->f8_clusters[c], stream_kernel<kF8Block>, &cfg));
     }
-    const size_t parts = static_cast<size_t>(h->num_sms) * 2 * kF8Block * 128 * sizeof(float);
+    const size_t parts = static_cast<size_t>(h->num_sms) * 2 * kF8Block * kTileCols * sizeof(float);
     QTZ_CUDA(h, cudaMalloc(&h->f8_dev, parts + h->num_sms * sizeof(int32_t)));
     QTZ_CUDA(h, cudaMemsetAsync(static_cast<uint8_t*>(h->f8_dev) + parts, 0, h->num_sms * sizeof(int32_t), st));
     h->f8_counters = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(h->f8_dev) + parts);
@@ -737,8 +746,8 @@ qtz_status launch_stream(qtz_f8_layer* p, LinearArgs& a, const CUtensorMap& x_ma
 {
     qtz_ctx* h = p->h;
     a.row_tiles = static_cast<int32_t>((a.rows + kF8Block - 1) / kF8Block);
-    a.units = a.row_tiles * a.n_tiles * a.k_blocks;
-    const int tiles = a.row_tiles * a.n_tiles;
+    const int tiles = a.row_tiles * ((a.n_tiles + 1) / 2);
+    a.units = tiles * a.k_blocks;
     const qtz_status s = qtz_allow_smem(h, stream_kernel<kRows>);
     if (s != QTZ_OK) return s;
     cudaLaunchAttribute at[2];
@@ -757,7 +766,7 @@ qtz_status launch_stream(qtz_f8_layer* p, LinearArgs& a, const CUtensorMap& x_ma
         a.share = (a.units + h->num_sms - 1) / h->num_sms;
         cfg.gridDim = dim3((a.units + a.share - 1) / a.share);
     }
-    cfg.blockDim = dim3(kStreamThreads);
+    cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = Stream<kRows>::kSmem;
     cfg.stream = st;
     cfg.attrs = at;
@@ -781,7 +790,7 @@ qtz_status launch_pair(qtz_f8_layer* p, LinearArgs& a, const CUtensorMap& x_map,
     at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * (a.units < h->num_sms / 2 ? a.units : h->num_sms / 2));
-    cfg.blockDim = dim3(kPairThreads);
+    cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = 1024 + kPairStages * kPairStage + 8 * kOutBytes;
     cfg.stream = st;
     cfg.attrs = at;
@@ -822,7 +831,7 @@ extern "C" qtz_status qtz_f8_linear_create(qtz_handle h, int32_t n, int32_t k, c
     p->k = k;
     p->n_tiles = static_cast<int32_t>(n_tiles);
     p->k_blocks = static_cast<int32_t>(k_blocks);
-    const size_t blocks = static_cast<size_t>(n_tiles) * k_blocks, tile_bytes = blocks * kF8Block * kF8Block;
+    const size_t blocks = static_cast<size_t>(n_tiles) * k_blocks, places = (static_cast<size_t>(n_tiles) + 1) / 2 * 2 * k_blocks, tile_bytes = places * kF8Block * kF8Block;
     cudaError_t e = cudaMalloc(reinterpret_cast<void**>(&p->tiles), tile_bytes + (blocks + n) * sizeof(float));
     if (e == cudaSuccess) {
         p->scales = reinterpret_cast<float*>(p->tiles + tile_bytes);
@@ -839,7 +848,7 @@ extern "C" qtz_status qtz_f8_linear_create(qtz_handle h, int32_t n, int32_t k, c
         e = cudaGetLastError();
     }
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);   // later calls may fetch the tiles before they wait for the stream
-    const uint64_t dims[2] = {kF8Block, blocks * kF8Block}, strides[1] = {kF8Block};
+    const uint64_t dims[2] = {kF8Block, places * kF8Block}, strides[1] = {kF8Block};
     const uint32_t box[2] = {kF8Block, kF8Block};
     if (e == cudaSuccess && !qtz_encode_u8_map(&p->w_map, p->tiles, 2, dims, strides, box, 128)) e = cudaErrorInvalidValue;
     if (e != cudaSuccess) {
