@@ -238,27 +238,32 @@ __device__ __forceinline__ void put_quad(const LinearArgs& a, int64_t row, int o
 }
 
 // Sums of a tile that the CTAs of a cluster hold in shared memory, [row][64 quads of columns], a quad at its number ^ (row % 32) (for the
-// banks): each CTA takes an equal part of the quads and adds them up in the order of the columns.
+// banks): each CTA takes an equal part of the quads and adds them up in the order of the columns.  Called by the warps of the sums.
 __device__ __forceinline__ uint32_t quad_at(uint32_t base, int row, int quad) { return base + (row * kQuads + (quad ^ (row & 31))) * 16; }
 
-__device__ __forceinline__ void join_cluster(const LinearArgs& a, const Unit& tile, uint32_t base)
+__device__ __forceinline__ void join_cluster(const LinearArgs& a, int64_t row0, int col, uint32_t base, int part, int rank0, int rank_step)
 {
-    const int64_t r0 = static_cast<int64_t>(tile.row_tile) * kF8Block;
-    const int quads = static_cast<int>(min(static_cast<int64_t>(kF8Block), a.rows - r0)) * kQuads, rank = static_cast<int>(cluster_ctarank());
-    const int end = (rank + 1) * quads / a.split;
-    for (int q = rank * quads / a.split + threadIdx.x; q < end; q += kThreads) {
-        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-        const uint32_t own = quad_at(base, q / kQuads, q % kQuads);
-#pragma unroll 4
-        for (int c = 0; c < a.split; ++c) {
-            const float4 p = lds_cluster(mapa_shared(own, c));
-            v.x += p.x;
-            v.y += p.y;
-            v.z += p.z;
-            v.w += p.w;
-        }
-        put_quad(a, r0 + q / kQuads, tile.col * kTileCols + q % kQuads * 4, v);
+    const int quads = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(kF8Block), a.rows - row0))) * kQuads, end = (part + 1) * quads / a.split;
+    // all of a quad's parts are on their way together
+    for (int q = part * quads / a.split + static_cast<int>(threadIdx.x) - (kThreads - kSumThreads); q < end; q += kSumThreads) {
+        const uint32_t at = quad_at(base, q / kQuads, q % kQuads);
+        float4 p[kMaxSplit];
+#pragma unroll
+        for (int c = 0; c < kMaxSplit; ++c)
+            if (c < a.split) p[c] = lds_cluster(mapa_shared(at, rank0 + c * rank_step));
+        float4 v = p[0];
+#pragma unroll
+        for (int c = 1; c < kMaxSplit; ++c)
+            if (c < a.split) v = make_float4(v.x + p[c].x, v.y + p[c].y, v.z + p[c].z, v.w + p[c].w);
+        put_quad(a, row0 + q / kQuads, col * kTileCols + q % kQuads * 4, v);
     }
+}
+
+// A thread's 128 sums, of row `row` and columns half * 128 on, into that place.
+__device__ __forceinline__ void keep_sums(const float (&acc)[128], uint32_t base, int row, int half)
+{
+#pragma unroll
+    for (int c = 0; c < 128; c += 4) sts128(quad_at(base, row, half * 32 + c / 4), make_float4(acc[c], acc[c + 1], acc[c + 2], acc[c + 3]));
 }
 
 // After a CTA's last unit: counts its arrival at the tiles that it shares with others, and sums those at which it is the last, in the
@@ -456,6 +461,10 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
             }
             cp_async_wait<0>();
         }
+        if (a.split > 1) {
+            cluster_sync();
+            cluster_sync();
+        }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kMany));
         if ((warp & 3) < quarters) {
@@ -488,9 +497,7 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
                 const int64_t row = static_cast<int64_t>(here.row_tile) * kF8Block + row_warp;
                 if (a.split > 1) {
                     // the ring is free: all its products are done
-#pragma unroll
-                    for (int c = 0; c < 128; c += 4)
-                        if (row_warp + lane < kRows) sts128(quad_at(base, row_warp + lane, (half * 128 + c) / 4), make_float4(acc[c], acc[c + 1], acc[c + 2], acc[c + 3]));
+                    if (row_warp + lane < kRows) keep_sums(acc, base, row_warp + lane, half);
                 } else if (begins && ends) {
                     put_y(a, row, here.col * kTileCols + half * 128, out, acc);
                 } else {
@@ -502,7 +509,14 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
                 here.next(a);
             }
         }
-        if (!a.split && named_barrier_and(1, kSumThreads, ok)) join_tiles(a, s_open, s_last);   // after a wait that gave up the results are void
+        if (a.split > 1) {
+            const Unit tile(a, u0);
+            cluster_sync();                            // the cluster's sums are there
+            join_cluster(a, static_cast<int64_t>(tile.row_tile) * kF8Block, tile.col, base, static_cast<int>(cluster_ctarank()), 0, 1);
+            cluster_sync();                            // and have been read
+        } else if (!a.split && named_barrier_and(1, kSumThreads, ok)) {
+            join_tiles(a, s_open, s_last);             // after a wait that gave up the results are void
+        }
     }
     if (!ok) timed_out(a);
     tc_fence_before();
@@ -512,11 +526,6 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
         __syncwarp();
         tc_fence_after();
         tmem_dealloc(tmem, 512);
-    }
-    if (a.split > 1) {
-        cluster_sync();                                // the cluster's sums are there
-        join_cluster(a, Unit(a, u0), base);
-        cluster_sync();                                // and have been read
     }
 }
 
@@ -547,7 +556,7 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
     __shared__ __align__(8) uint64_t s_full[kPairStages], s_empty[kPairStages], s_done[2], s_free[2], s_drain;
     __shared__ uint32_t s_tmem;
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
-    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, rank = cluster_ctarank();
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u, rank = cluster_ctarank(), side = rank & 1, first = rank & ~1u;
     if (tid == 0) {
         prefetch_tensormap(&w_map);
         prefetch_tensormap(&x_map);
@@ -571,7 +580,9 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
     cluster_sync();                                    // both CTAs' barriers are there
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
-    const int tile0 = blockIdx.x / 2, step = gridDim.x / 2, tiles = a.units;
+    // the pairs of a cluster share the columns of a tile
+    const int tile0 = blockIdx.x / (2 * a.split), step = gridDim.x / (2 * a.split), tiles = a.units, part = rank >> 1;
+    const int kb0 = part * a.k_blocks / a.split, kbs = (part + 1) * a.k_blocks / a.split - kb0;
     bool ok = true;
     grid_launch_dependents();
 
@@ -583,14 +594,14 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
             int stage = 0, round = 0, issued = 0;
             for (int tile = tile0; ok && tile < tiles; tile += step) {
                 const PairTile at(a, tile);
-                const int w_half = min(static_cast<int>(rank), a.n_tiles - 1 - 2 * at.col), x_row = (2 * at.row + static_cast<int>(rank)) * kF8Block;
-                for (int kb = 0; kb < a.k_blocks; ++kb) {
+                const int w_half = min(static_cast<int>(side), a.n_tiles - 1 - 2 * at.col), x_row = (2 * at.row + static_cast<int>(side)) * kF8Block;
+                for (int kb = kb0; kb < kb0 + kbs; ++kb) {
                     if (issued >= kPairStages) ok = mbar_wait_warp(smem_u32(&s_empty[stage]), (round & 1) ^ 1, a.wait_budget, ok);
                     if (!ok) break;
                     if (elect_one()) {
                         const uint32_t own = smem_u32(&s_full[stage]), to = base + stage * kPairStage;
-                        if (rank == 0) mbar_arrive_expect_tx(own, 2 * kPairStage);
-                        const uint32_t bar = mapa_shared(own, 0u);
+                        if (side == 0) mbar_arrive_expect_tx(own, 2 * kPairStage);
+                        const uint32_t bar = mapa_shared(own, first);
                         tma_load_2d_pair(to, &x_map, bar, kb * kF8Block, x_row);
                         tma_load_2d_pair(to + kTileBytes, &w_map, bar, 0, w_row(a, at.col, kb, w_half));
                     }
@@ -603,12 +614,12 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
                 }
             }
             // nothing may be in flight when the CTAs end
-            if (rank == 0)
+            if (side == 0)
                 for (int j = max(0, issued - kPairStages); j < issued; ++j)
                     ok = mbar_wait_warp(smem_u32(&s_full[j % kPairStages]), (j / kPairStages) & 1, kDrainBudget, ok);
         } else if (warp != 2) {
             // ======== products: a warp for the even blocks, one for the odd ones ========
-            const int blocks = rank == 0 ? (tiles - tile0 + step - 1) / step * a.k_blocks : 0, buffer = warp >> 1;
+            const int blocks = side == 0 ? (tiles - tile0 + step - 1) / step * kbs : 0, buffer = warp >> 1;
             int stage = buffer, round = 0;
             for (int block = buffer; block < blocks; block += 2) {
                 ok = mbar_wait_warp(smem_u32(&s_full[stage]), round & 1, a.wait_budget, ok);
@@ -619,8 +630,8 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
                     const uint64_t x = make_kmajor_desc(base + stage * kPairStage, 128), w = make_kmajor_desc(base + stage * kPairStage + kTileBytes, 128);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) mma_f8_pair(tmem + buffer * 256, x + 2 * k, w + 2 * k, kProduct<256, 256>, k > 0);
-                    mma_commit_pair(smem_u32(&s_done[buffer]));
-                    mma_commit_pair(smem_u32(&s_empty[stage]));
+                    mma_commit_pair(smem_u32(&s_done[buffer]), first);
+                    mma_commit_pair(smem_u32(&s_empty[stage]), first);
                 }
                 __syncwarp();
                 stage += 2;
@@ -629,12 +640,12 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
                     ++round;
                 }
             }
-            if (rank == 0 && elect_one()) mma_commit_pair(smem_u32(&s_drain));
+            if (side == 0 && elect_one()) mma_commit_pair(smem_u32(&s_drain), first);
             __syncwarp();
         } else if (warp == 2) {
             // ======== scales: on their way four blocks ahead, counted with the products of the block ========
             grid_dependency_wait();
-            const int blocks = (tiles - tile0 + step - 1) / step * a.k_blocks;
+            const int blocks = (tiles - tile0 + step - 1) / step * kbs;
             int tile = tile0, kb = 0;
             const float* from[5];                      // four rows of x; lanes 0 and 1: a tile of weights
             for (int block = 0; block < blocks + kAhead; ++block) {
@@ -649,16 +660,16 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
                 if (block < blocks) {
                     if (kb == 0) {
                         const PairTile at(a, tile);
-                        const int64_t row0 = (2 * static_cast<int64_t>(at.row) + rank) * kF8Block + lane;
+                        const int64_t row0 = (2 * static_cast<int64_t>(at.row) + side) * kF8Block + lane;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) from[j] = a.x_scales + min(row0 + 32 * j, a.rows - 1) * a.row_stride;
-                        from[4] = a.w_scales + static_cast<int64_t>(min(2 * at.col + (lane & 1), a.n_tiles - 1)) * a.k_blocks;
+                        for (int j = 0; j < 4; ++j) from[j] = a.x_scales + min(row0 + 32 * j, a.rows - 1) * a.row_stride + kb0 * a.block_stride;
+                        from[4] = a.w_scales + static_cast<int64_t>(min(2 * at.col + (lane & 1), a.n_tiles - 1)) * a.k_blocks + kb0;
                     }
                     const int slot = block % kSlots;   // of the block eight before, which the sums are through with: the product four before is done
 #pragma unroll
                     for (int j = 0; j < 4; ++j) cp_async_4(smem_u32(&s_x[slot][32 * j + lane]), from[j] + kb * a.block_stride);
                     if (lane < 2) cp_async_4(smem_u32(&s_w[slot][lane]), from[4] + kb);
-                    if (++kb == a.k_blocks) {
+                    if (++kb == kbs) {
                         kb = 0;
                         tile += step;
                     }
@@ -666,6 +677,10 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
                 cp_async_commit();
             }
             cp_async_wait<0>();
+        }
+        if (a.split > 1) {
+            cluster_sync();
+            cluster_sync();
         }
     } else {
         // ======== sums ========
@@ -681,7 +696,7 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
 #pragma unroll
             for (int c = 0; c < 128; ++c) acc[c] = 0.f;
 #pragma unroll 1
-            for (int kb = 0; kb < a.k_blocks; ++kb, ++block) {
+            for (int kb = 0; kb < kbs; ++kb, ++block) {
                 const int slot = block % kSlots;
                 ok = mbar_wait_warp(smem_u32(&s_done[block & 1]), block >> 1 & 1, a.wait_budget, ok);
                 if (!ok) break;
@@ -689,12 +704,19 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
                 const float s = block ? s_next : s_x[0][row_lane] * s_w[0][half];
                 s_next = s_x[(slot + 1) % kSlots][row_lane] * s_w[(slot + 1) % kSlots][half];
                 add_block(acc, from + (block & 1) * 256, s, [&]() {
-                    if (lane == 0) mbar_arrive_remote_relaxed(smem_u32(&s_free[block & 1]), 0u);
+                    if (lane == 0) mbar_arrive_remote_relaxed(smem_u32(&s_free[block & 1]), first);
                 });
             }
             if (!ok) break;
             const PairTile at(a, tile);
-            put_y(a, (2 * static_cast<int64_t>(at.row) + rank) * kF8Block + row_lane - lane, (2 * at.col + half) * kF8Block, out, acc);
+            if (a.split > 1) keep_sums(acc, base, row_lane, half);   // the ring is free: the cluster's only tile is done
+            else put_y(a, (2 * static_cast<int64_t>(at.row) + side) * kF8Block + row_lane - lane, (2 * at.col + half) * kF8Block, out, acc);
+        }
+        if (a.split > 1) {
+            const PairTile at(a, tile0);
+            cluster_sync();                            // the cluster's sums are there
+            join_cluster(a, (2 * static_cast<int64_t>(at.row) + side) * kF8Block, at.col, base, part, side, 2);
+            cluster_sync();                            // and have been read
         }
     }
     if (!ok) timed_out(a);
@@ -741,6 +763,28 @@ qtz_status ensure_scratch(qtz_ctx* h, cudaStream_t st)
     return QTZ_OK;
 }
 
+template <typename K>
+qtz_status launch(qtz_ctx* h, K* kernel, const LinearArgs& a, int cluster, int ctas, int smem, cudaStream_t st, const CUtensorMap& w_map, const CUtensorMap& x_map)
+{
+    const qtz_status s = qtz_allow_smem(h, kernel);
+    if (s != QTZ_OK) return s;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = cluster;
+    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 2;
+    QTZ_CUDA(h, cudaLaunchKernelEx(&cfg, kernel, a, w_map, x_map));
+    return QTZ_OK;
+}
+
 template <int kRows>
 qtz_status launch_stream(qtz_f8_layer* p, LinearArgs& a, const CUtensorMap& x_map, cudaStream_t st)
 {
@@ -748,31 +792,17 @@ qtz_status launch_stream(qtz_f8_layer* p, LinearArgs& a, const CUtensorMap& x_ma
     a.row_tiles = static_cast<int32_t>((a.rows + kF8Block - 1) / kF8Block);
     const int tiles = a.row_tiles * ((a.n_tiles + 1) / 2);
     a.units = tiles * a.k_blocks;
-    const qtz_status s = qtz_allow_smem(h, stream_kernel<kRows>);
-    if (s != QTZ_OK) return s;
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    if (tiles <= h->num_sms) {
-        a.split = 1;
-        for (int c = 2; c <= kMaxSplit && c <= a.k_blocks; ++c)
-            if (tiles <= h->f8_clusters[c]) a.split = c;
-        at[1].val.clusterDim.x = a.split;
-        cfg.gridDim = dim3(tiles * a.split);
-    } else {
-        a.share = (a.units + h->num_sms - 1) / h->num_sms;
-        cfg.gridDim = dim3((a.units + a.share - 1) / a.share);
-    }
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = Stream<kRows>::kSmem;
-    cfg.stream = st;
-    cfg.attrs = at;
-    cfg.numAttrs = 2;
-    QTZ_CUDA(h, cudaLaunchKernelEx(&cfg, stream_kernel<kRows>, a, p->w_map, x_map));
-    return QTZ_OK;
+    if (!a.split) a.share = (a.units + h->num_sms - 1) / h->num_sms;
+    return launch(h, stream_kernel<kRows>, a, a.split ? a.split : 1, a.split ? tiles * a.split : (a.units + a.share - 1) / a.share, Stream<kRows>::kSmem, st, p->w_map, x_map);
+}
+
+// How many clusters' CTAs (times `each`) can take parts of a tile's columns with all tiles at work at once; 0: not even one.
+int most_split(const qtz_ctx* h, int64_t tiles, int each, int k_blocks)
+{
+    int split = tiles * each <= h->num_sms ? 1 : 0;
+    for (int c = 2; split && c * each <= kMaxSplit && c <= k_blocks; ++c)
+        if (tiles <= h->f8_clusters[c * each]) split = c;
+    return split;
 }
 
 qtz_status launch_pair(qtz_f8_layer* p, LinearArgs& a, const CUtensorMap& x_map, cudaStream_t st)
@@ -780,23 +810,8 @@ qtz_status launch_pair(qtz_f8_layer* p, LinearArgs& a, const CUtensorMap& x_map,
     qtz_ctx* h = p->h;
     a.row_tiles = static_cast<int32_t>((a.rows + 255) / 256);
     a.units = a.row_tiles * ((a.n_tiles + 1) / 2);
-    const qtz_status s = qtz_allow_smem(h, pair_kernel);
-    if (s != QTZ_OK) return s;
-    cudaLaunchAttribute at[2];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    at[1].id = cudaLaunchAttributeClusterDimension;
-    at[1].val.clusterDim.x = 2;
-    at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(2 * (a.units < h->num_sms / 2 ? a.units : h->num_sms / 2));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = 1024 + kPairStages * kPairStage + 8 * kOutBytes;
-    cfg.stream = st;
-    cfg.attrs = at;
-    cfg.numAttrs = 2;
-    QTZ_CUDA(h, cudaLaunchKernelEx(&cfg, pair_kernel, a, p->w_map, x_map));
-    return QTZ_OK;
+    const int pairs = h->num_sms / 2;
+    return launch(h, pair_kernel, a, 2 * a.split, 2 * a.split * (a.split > 1 || a.units < pairs ? a.units : pairs), 1024 + kPairStages * kPairStage + 8 * kOutBytes, st, p->w_map, x_map);
 }
 
 }  // namespace
@@ -876,7 +891,13 @@ extern "C" qtz_status qtz_f8_linear(qtz_f8_linear_plan p, const uint8_t* codes_d
     LinearArgs a{p->scales, p->bias, scales_dev, scales_row_stride, scales_block_stride, rows, y_stride, y_dev, p->n, p->n_tiles, p->k_blocks, ftype,
                  qtz_aligned16(y_dev) && (rows <= 1 || y_stride * (ftype == QTZ_F32 ? 4 : 2) % 16 == 0), 0, 0, 0, 0,
                  static_cast<float*>(h->f8_dev), h->f8_counters, h->wait_budget, h->status_dev};
-    const bool pair = rows > 512;
+    // More than 128 rows: a tile's block of 128 columns takes a pair about 10 and a CTA about 13 units of time; single CTAs only where each
+    // has at most one tile.
+    const int64_t cols = (p->n_tiles + 1) / 2, pair_tiles = (rows + 255) / 256 * cols, tiles = (rows + 127) / 128 * cols;
+    const int pair_split = most_split(h, pair_tiles, 2, p->k_blocks), split = most_split(h, tiles, 1, p->k_blocks);
+    const int64_t pair_cost = 10 * (pair_split ? (p->k_blocks + pair_split - 1) / pair_split : (pair_tiles + h->num_sms / 2 - 1) / (h->num_sms / 2) * p->k_blocks);
+    const bool pair = rows > 128 && (!split || pair_cost < 13 * ((p->k_blocks + split - 1) / split));
+    a.split = pair ? (pair_split ? pair_split : 1) : split;
     const int box_rows = pair ? 128 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
     CUtensorMap x_map;                                 // columns beyond k and rows beyond the last read as zero
     const int64_t pitch = rows > 1 ? codes_stride : (p->k + 15) / 16 * 16;

@@ -319,11 +319,12 @@ __device__ __forceinline__ void mma_i8_pair(uint32_t d_tmem, uint64_t a_desc, ui
         : "memory");
 }
 
-// Arrives, once the pair's MMAs issued so far are done, on the mbarrier at this offset in both CTAs of the pair.
-__device__ __forceinline__ void mma_commit_pair(uint32_t bar)
+// Arrives, once the pair's MMAs issued so far are done, on the mbarrier at this offset in both CTAs of the pair; `first` is the rank of
+// the pair's first CTA in the cluster.
+__device__ __forceinline__ void mma_commit_pair(uint32_t bar, uint32_t first = 0)
 {
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(bar), "h"(static_cast<uint16_t>(3))
+                 ::"r"(bar), "h"(static_cast<uint16_t>(3u << first))
                  : "memory");
 }
 
