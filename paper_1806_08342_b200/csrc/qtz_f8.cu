@@ -6,8 +6,8 @@
 // norm goes on with is not.
 //
 // What bounds them: bytes.  Every value is read once, kept in registers between the row's sum of squares, the block's maximum and the
-// code, and written once.  A thread holds eight neighbouring columns, so that the 16 lanes of a half warp hold a block and its maximum
-// takes four shuffles.
+// code, and written once.  A thread holds 32 bytes of neighbouring columns, so that 8 or 16 lanes hold a block and its maximum takes three or
+// four shuffles; warps and CTAs go over several rows and have the next row's values on their way while they work on one.
 #include "qtz_f8.cuh"
 #include "qtz_ptx.cuh"
 
@@ -15,102 +15,126 @@ namespace {
 
 using namespace qtz_ptx;
 
-constexpr int kNormChunks = 4;             // of eight columns that a thread of the norm holds at most
-constexpr int kNormThreads = 1024;
-constexpr int kQuantThreads = 128;
-constexpr int kQuantRows = 4;              // that a thread of the quantizer has under way
-
-// Eight neighbouring values of a row of which `valid` exist; zeros behind them.
+// Neighbouring columns of a thread: two loads of 16 bytes.
 template <typename T>
-__device__ __forceinline__ void load8(const T* p, int valid, float (&v)[8])
-{
-    if (valid >= 8) {
-        if constexpr (sizeof(T) == 2) {
-            const uint4 w = *reinterpret_cast<const uint4*>(p);
-            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+constexpr int kColsOf = 32 / sizeof(T);
+constexpr int kNormThreads = 1024, kWideThreads = 512; // of the norm: with 32 bytes of a row each, with more
+constexpr int kMostColumns = 32768;
+constexpr int kQuantWarps = 4, kQuantWarpsPerSm = 32;  // of a CTA of the quantizer; at work at once
+
+// The columns of a thread, of which `valid` exist, as they are stored: words, and half a word at the end of a row of an odd number of
+// 16-bit values.
+template <typename T>
+struct Raw {
+    static constexpr int kCols = kColsOf<T>, kPer = 4 / sizeof(T);   // values of a word
+    uint32_t w[8];
+
+    // zeros behind the last
+    __device__ __forceinline__ void load(const T* p, int valid)
+    {
+        if (valid >= kCols) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 f = qtz_dev::unpack2(u[i], T());
-                v[2 * i] = f.x;
-                v[2 * i + 1] = f.y;
+            for (int i = 0; i < 8; i += 4) {
+                const uint4 v = *reinterpret_cast<const uint4*>(p + i * kPer);
+                w[i] = v.x;
+                w[i + 1] = v.y;
+                w[i + 2] = v.z;
+                w[i + 3] = v.w;
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const float4 f = reinterpret_cast<const float4*>(p)[i];
-                v[4 * i] = f.x;
-                v[4 * i + 1] = f.y;
-                v[4 * i + 2] = f.z;
-                v[4 * i + 3] = f.w;
+            for (int i = 0; i < 8; ++i) {
+                w[i] = 0;
+                if (i * kPer + kPer <= valid) w[i] = *reinterpret_cast<const uint32_t*>(p + i * kPer);
+                else if (i * kPer < valid) w[i] = *reinterpret_cast<const uint16_t*>(p + i * kPer);
             }
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < valid ? qtz_dev::to_f32(p[i]) : 0.f;
     }
-}
-
-template <typename T>
-__device__ __forceinline__ void store8(T* p, int valid, const float (&v)[8])
-{
-    if (valid >= 8) {
-        if constexpr (sizeof(T) == 2) {
-            *reinterpret_cast<uint4*>(p) = make_uint4(qtz_dev::pack2(v[0], v[1], T()), qtz_dev::pack2(v[2], v[3], T()),
-                                                      qtz_dev::pack2(v[4], v[5], T()), qtz_dev::pack2(v[6], v[7], T()));
+    __device__ __forceinline__ void store(T* p, int valid) const
+    {
+        if (valid >= kCols) {
+#pragma unroll
+            for (int i = 0; i < 8; i += 4) *reinterpret_cast<uint4*>(p + i * kPer) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
         } else {
-            reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (i * kPer + kPer <= valid) *reinterpret_cast<uint32_t*>(p + i * kPer) = w[i];
+                else if (i * kPer < valid) *reinterpret_cast<uint16_t*>(p + i * kPer) = static_cast<uint16_t>(w[i]);
+            }
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < valid) p[i] = qtz_dev::from_f32<T>(v[i]);
     }
-}
+    __device__ __forceinline__ void get(float (&v)[kCols]) const
+    {
+#pragma unroll
+        for (int i = 0; i < kCols; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                v[i] = __uint_as_float(w[i]);
+            } else {
+                const float2 f = qtz_dev::unpack2(w[i / 2], T());
+                v[i] = i % 2 ? f.y : f.x;
+            }
+        }
+    }
+    __device__ __forceinline__ void set(const float (&v)[kCols])
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(v[i]);
+            else w[i] = qtz_dev::pack2(v[2 * i], v[2 * i + 1], T());
+        }
+    }
+};
 
-__device__ __forceinline__ float finite_top(const float (&v)[8])
+// Largest of the neighbouring lanes that share a block.
+template <int kLanes>
+__device__ __forceinline__ float block_max(float top)
 {
-    float top = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float m = fabsf(v[i]);
-        top = fmaxf(top, m < INFINITY ? m : 0.f);
-    }
+    for (int off = kLanes / 2; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
     return top;
 }
 
-// The codes and the scale of a block that the 16 lanes of a half warp hold; all lanes of the warp take part.  `codes` is where this
-// lane's eight go, `valid` of them exist.
-__device__ __forceinline__ void put_block(const float (&v)[8], int valid, uint8_t* codes, float* scale)
+// The codes and the scale of a block that 128 / kCols lanes hold; all lanes of the warp take part.  `codes` is where this lane's go, `valid`
+// of them exist.
+template <int kCols>
+__device__ __forceinline__ void put_block(const float (&v)[kCols], int valid, uint8_t* codes, float* scale)
 {
+    constexpr int kLanes = kF8Block / kCols;
     float top = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(v[i]));
-#pragma unroll
-    for (int off = 8; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    for (int i = 0; i < kCols; ++i) top = fmaxf(top, fabsf(v[i]));
+    top = block_max<kLanes>(top);
     if (__any_sync(0xffffffffu, top == INFINITY)) {     // infinities do not count
-        top = finite_top(v);
+        top = 0.f;
 #pragma unroll
-        for (int off = 8; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+        for (int i = 0; i < kCols; ++i) top = fmaxf(top, fabsf(v[i]) < INFINITY ? fabsf(v[i]) : 0.f);
+        top = block_max<kLanes>(top);
     }
     if (valid <= 0) return;
     const float s = qtz_dev::f8_scale(top), inverse = 1.f / s;
-    if ((threadIdx.x & 15) == 0) *scale = s;
-    uint32_t w[4];
+    if (threadIdx.x % kLanes == 0) *scale = s;
+    uint32_t w[kCols / 4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = qtz_dev::e4m3x2(v[2 * i] * inverse, v[2 * i + 1] * inverse);
-    if (valid >= 8) {
-        *reinterpret_cast<uint2*>(codes) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
+    for (int i = 0; i < kCols / 4; ++i)
+        w[i] = qtz_dev::e4m3x2(v[4 * i] * inverse, v[4 * i + 1] * inverse) | qtz_dev::e4m3x2(v[4 * i + 2] * inverse, v[4 * i + 3] * inverse) << 16;
+    if (valid >= kCols) {
+        if constexpr (kCols == 16) *reinterpret_cast<uint4*>(codes) = make_uint4(w[0], w[1], w[2], w[3]);
+        else *reinterpret_cast<uint2*>(codes) = make_uint2(w[0], w[1]);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < valid) codes[i] = static_cast<uint8_t>(w[i >> 1] >> (8 * (i & 1)));
+        for (int i = 0; i < kCols / 4; ++i) {
+            if (4 * i + 4 <= valid) *reinterpret_cast<uint32_t*>(codes + 4 * i) = w[i];
+            else
+#pragma unroll
+                for (int j = 0; j < 3; ++j)
+                    if (4 * i + j < valid) codes[4 * i + j] = static_cast<uint8_t>(w[i] >> (8 * j));
+        }
     }
 }
 
 struct NormArgs {
     const void *x, *residual, *gain;
-    int64_t x_stride, residual_stride, sum_stride, values_stride, codes_stride, scales_stride;
+    int64_t x_stride, residual_stride, sum_stride, values_stride, codes_stride, scales_stride, rows;
     void *sum, *values;
     uint8_t* codes;
     float* scales;
@@ -118,79 +142,95 @@ struct NormArgs {
     int32_t k;
 };
 
-// Sum of the squares of what the CTA's threads hold, in all threads.
-template <int kChunks>
-__device__ __forceinline__ float sum_of_squares(const float (&h)[kChunks][8], float* s_part)
+// Sum of the squares of what the CTA's threads hold, in all threads.  `part`: a place for each warp, not the one of the call before.
+template <int kChunks, int kCols>
+__device__ __forceinline__ float sum_of_squares(const float (&h)[kChunks][kCols], float* part)
 {
     float v = 0.f;
 #pragma unroll
     for (int j = 0; j < kChunks; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v = fmaf(h[j][i], h[j][i], v);
+        for (int i = 0; i < kCols; ++i) v = fmaf(h[j][i], h[j][i], v);
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
     const int warps = blockDim.x >> 5, lane = threadIdx.x & 31;
-    __syncthreads();                                   // an earlier call's parts have been read
-    if (lane == 0) s_part[threadIdx.x >> 5] = v;
+    if (lane == 0) part[threadIdx.x >> 5] = v;
     __syncthreads();
-    v = lane < warps ? s_part[lane] : 0.f;
+    v = lane < warps ? part[lane] : 0.f;
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) v += __shfl_xor_sync(0xffffffffu, v, off);
     return v;
 }
 
-// A CTA a row; thread t holds chunks t, t + blockDim, ... of eight columns.
+// A CTA goes over rows blockIdx.x, blockIdx.x + gridDim.x, ...; thread t holds chunks t, t + blockDim, ... of their columns.
 template <typename T, int kChunks>
-__global__ void __launch_bounds__(kNormThreads) norm_kernel(const __grid_constant__ NormArgs a)
+__global__ void __launch_bounds__(kChunks == 1 ? kNormThreads : kWideThreads) norm_kernel(const __grid_constant__ NormArgs a)
 {
-    __shared__ float s_part[kNormThreads / 32];
+    __shared__ float s_part[2][kNormThreads / 32];
+    constexpr int kCols = kColsOf<T>;
+    constexpr bool kEarly = kChunks == 1;              // the next row's values are asked for before this row's are used: as registers allow
     grid_dependency_wait();
     grid_launch_dependents();
-    const int64_t row = blockIdx.x;
-    const T* const x = static_cast<const T*>(a.x) + row * a.x_stride;
-    const T* const residual = a.residual ? static_cast<const T*>(a.residual) + row * a.residual_stride : nullptr;
-    float h[kChunks][8];
-#pragma unroll
-    for (int j = 0; j < kChunks; ++j) {
-        const int col = (j * blockDim.x + threadIdx.x) * 8;
-        load8<T>(x + col, a.k - col, h[j]);
-    }
-    if (residual) {
-#pragma unroll
-        for (int j = 0; j < kChunks; ++j) {
-            const int col = (j * blockDim.x + threadIdx.x) * 8;
-            float r[8];
-            load8<T>(residual + col, a.k - col, r);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) h[j][i] += r[i];
-        }
-    }
-    if (a.sum) {
+    Raw<T> x, residual;
+    auto load = [&](int64_t row, int j) {
+        const int col = (j * blockDim.x + threadIdx.x) * kCols;
+        x.load(static_cast<const T*>(a.x) + row * a.x_stride + col, a.k - col);
+        if (a.residual) residual.load(static_cast<const T*>(a.residual) + row * a.residual_stride + col, a.k - col);
+    };
+    if (kEarly) load(blockIdx.x, 0);
+    int turn = 0;
+#pragma unroll 1
+    for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        float h[kChunks][kCols];
 #pragma unroll
         for (int j = 0; j < kChunks; ++j) {
-            const int col = (j * blockDim.x + threadIdx.x) * 8;
-            if (a.k > col) store8<T>(static_cast<T*>(a.sum) + row * a.sum_stride + col, a.k - col, h[j]);
+            if (!kEarly) load(row, j);
+            x.get(h[j]);
+            if (a.residual) {
+                float r[kCols];
+                residual.get(r);
+#pragma unroll
+                for (int i = 0; i < kCols; ++i) h[j][i] += r[i];
+            }
         }
-    }
-    float squares = sum_of_squares(h, s_part), eps = a.eps;
-    if (squares == INFINITY) {                         // too large to be squared in fp32 (eps is nothing beside it), or infinite
+        if (kEarly && row + gridDim.x < a.rows) load(row + gridDim.x, 0);
+        if (a.sum) {
 #pragma unroll
-        for (int j = 0; j < kChunks; ++j)
+            for (int j = 0; j < kChunks; ++j) {
+                const int col = (j * blockDim.x + threadIdx.x) * kCols;
+                Raw<T> sum;
+                sum.set(h[j]);
+                sum.store(static_cast<T*>(a.sum) + row * a.sum_stride + col, a.k - col);
+            }
+        }
+        float squares, eps = a.eps;
+#pragma unroll 1
+        for (;;) {
+            squares = sum_of_squares(h, s_part[turn]);
+            turn ^= 1;
+            if (squares != INFINITY || eps == 0.f) break;
+            eps = 0.f;                                 // too large to be squared in fp32 (eps is nothing beside it), or infinite
 #pragma unroll
-            for (int i = 0; i < 8; ++i) h[j][i] *= kF8MinScale;
-        squares = sum_of_squares(h, s_part);
-        eps = 0.f;
-    }
-    const float factor = 1.f / sqrtf(squares / static_cast<float>(a.k) + eps);
+            for (int j = 0; j < kChunks; ++j)
 #pragma unroll
-    for (int j = 0; j < kChunks; ++j) {
-        const int col = (j * blockDim.x + threadIdx.x) * 8, valid = a.k - col;
-        float g[8], v[8];
-        load8<T>(static_cast<const T*>(a.gain) + col, valid, g);
+                for (int i = 0; i < kCols; ++i) h[j][i] *= kF8MinScale;
+        }
+        const float factor = 1.f / sqrtf(squares / static_cast<float>(a.k) + eps);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = h[j][i] * factor * g[i];
-        if (a.values && valid > 0) store8<T>(static_cast<T*>(a.values) + row * a.values_stride + col, valid, v);
-        if (a.codes) put_block(v, valid, a.codes + row * a.codes_stride + col, a.scales + row * a.scales_stride + col / kF8Block);
+        for (int j = 0; j < kChunks; ++j) {
+            const int col = (j * blockDim.x + threadIdx.x) * kCols, valid = a.k - col;
+            Raw<T> gain;
+            float v[kCols];
+            gain.load(static_cast<const T*>(a.gain) + col, valid);
+            gain.get(v);
+#pragma unroll
+            for (int i = 0; i < kCols; ++i) v[i] *= h[j][i] * factor;
+            if (a.values) {
+                gain.set(v);
+                gain.store(static_cast<T*>(a.values) + row * a.values_stride + col, valid);
+            }
+            if (a.codes) put_block(v, valid, a.codes + row * a.codes_stride + col, a.scales + row * a.scales_stride + col / kF8Block);
+        }
     }
 }
 
@@ -200,34 +240,64 @@ struct QuantArgs {
     uint8_t* codes;
     float* scales;
     int32_t k;
+    int32_t pieces, per;       // of a row; rows that a warp takes together
 };
 
-// gate / (1 + exp(-gate)).  The fast division takes divisors below 2^126 only: a sixteenth of it is, wherever the exponential is finite.
-__device__ __forceinline__ float silu(float g) { return __fdividef(g, (1.f + __expf(-g)) * 0.0625f) * 0.0625f; }
-
-// A CTA takes 1024 columns of kQuantRows rows at a time, gridDim.y rows apart.
-template <typename T, bool kGate>
-__global__ void __launch_bounds__(kQuantThreads) quantize_kernel(const __grid_constant__ QuantArgs a)
+// gate / (1 + exp(-gate)).  A sixteenth of the divisor is inverted, so that the result is not below fp32 wherever the exponential is finite;
+// the exponential is off by 2^-17 of itself at a gate of -88 and by less nearer to 0.
+__device__ __forceinline__ float silu(float g)
 {
+    float e, r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(g * -1.4426950408889634f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(fmaf(e, 0.0625f, 0.0625f)));
+    return g * (r * 0.0625f);
+}
+
+// A warp takes a piece (1 KB) of one or two rows at a time.  Pieces are dealt out so that each warp meets all places of a row: the last
+// one may be slower.
+template <typename T, bool kGate>
+__global__ void __launch_bounds__(kQuantWarps * 32) quantize_kernel(const __grid_constant__ QuantArgs a)
+{
+    constexpr int kCols = kColsOf<T>;
     grid_dependency_wait();
     grid_launch_dependents();
-    const int col = (blockIdx.x * kQuantThreads + threadIdx.x) * 8, valid = a.k - col;
-    for (int64_t row0 = blockIdx.y; row0 < a.rows; row0 += static_cast<int64_t>(gridDim.y) * kQuantRows) {
-        float v[kQuantRows][8], g[kQuantRows][8];
+    const int warps = gridDim.x * kQuantWarps, unit = blockIdx.x * kQuantWarps + threadIdx.x / 32;
+    int64_t row = unit / a.pieces;
+    int piece = unit % a.pieces;
+    const int rows_on = warps / a.pieces, pieces_on = warps % a.pieces;
+#pragma unroll 1
+    for (row *= a.per; row < a.rows;) {
+        const int col = (piece * 32 + (threadIdx.x & 31)) * kCols, valid = a.k - col;
+        const int count = static_cast<int>(min(static_cast<int64_t>(a.per), a.rows - row));
+        const T* const x = static_cast<const T*>(a.x) + row * a.x_stride + col;
+        const T* const gate = kGate ? static_cast<const T*>(a.gate) + row * a.gate_stride + col : nullptr;
+        Raw<T> v[2], g[2];
 #pragma unroll
-        for (int r = 0; r < kQuantRows; ++r) {
-            const int64_t row = row0 + static_cast<int64_t>(r) * gridDim.y;
-            load8<T>(static_cast<const T*>(a.x) + row * a.x_stride + col, row < a.rows ? valid : 0, v[r]);
-            if constexpr (kGate) load8<T>(static_cast<const T*>(a.gate) + row * a.gate_stride + col, row < a.rows ? valid : 0, g[r]);
+        for (int r = 0; r < 2; ++r) {
+            if (r >= count) break;
+            v[r].load(x + r * a.x_stride, valid);
+            if constexpr (kGate) g[r].load(gate + r * a.gate_stride, valid);
         }
+        uint8_t* const codes = a.codes + row * a.codes_stride + col;
+        float* const scales = a.scales + row * a.scales_stride + col / kF8Block;
 #pragma unroll
-        for (int r = 0; r < kQuantRows; ++r) {
-            const int64_t row = row0 + static_cast<int64_t>(r) * gridDim.y;
-            if (row >= a.rows) break;
-            if constexpr (kGate)
+        for (int r = 0; r < 2; ++r) {
+            if (r >= count) break;
+            float f[kCols];
+            v[r].get(f);
+            if constexpr (kGate) {
+                float s[kCols];
+                g[r].get(s);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[r][i] *= silu(g[r][i]);
-            put_block(v[r], valid, a.codes + row * a.codes_stride + col, a.scales + row * a.scales_stride + col / kF8Block);
+                for (int i = 0; i < kCols; ++i) f[i] *= silu(s[i]);
+            }
+            put_block(f, valid, codes + r * a.codes_stride, scales + r * a.scales_stride);
+        }
+        row += static_cast<int64_t>(rows_on) * a.per;
+        piece += pieces_on;
+        if (piece >= a.pieces) {
+            piece -= a.pieces;
+            row += a.per;
         }
     }
 }
@@ -284,31 +354,31 @@ qtz_status check_codes(const uint8_t* codes, int64_t codes_stride, const float* 
 }
 
 template <typename T>
-cudaError_t launch_norm(const NormArgs& a, int64_t rows, int num_sms, cudaStream_t st)
+cudaError_t launch_norm(const NormArgs& a, int num_sms, cudaStream_t st)
 {
-    // Few rows: a chunk a thread, since the row's latency counts.  Many: four, so that each thread has 64 or 128 bytes under way.
-    const int chunks = (a.k + 7) / 8, least = (chunks + kNormThreads - 1) / kNormThreads;
-    const int want = rows <= 2 * num_sms ? least : kNormChunks, per = want < least ? least : want;
-    int threads = ((chunks + per - 1) / per + 31) / 32 * 32;
-    const int hold = (chunks + threads - 1) / threads;
-    auto go = [&](auto kernel) { return qtz_launch_dependent(kernel, dim3(static_cast<unsigned>(rows)), threads, 0, st, a); };
-    switch (hold) {
-    case 1: return go(norm_kernel<T, 1>);
-    case 2: return go(norm_kernel<T, 2>);
-    case 3: return go(norm_kernel<T, 3>);
-    default: return go(norm_kernel<T, 4>);
-    }
+    constexpr int kMost = kMostColumns / kWideThreads / kColsOf<T>;
+    const int chunks = (a.k + kColsOf<T> - 1) / kColsOf<T>, per = chunks <= kNormThreads ? 1 : chunks <= 4 * kWideThreads ? 4 : kMost;
+    const int threads = ((chunks + per - 1) / per + 31) / 32 * 32;
+    // A thousand threads an SM, what their registers allow, each CTA with a row at work and a row on its way.
+    const int64_t at_once = static_cast<int64_t>(num_sms) * (threads >= 1024 ? 1 : 1024 / threads);
+    const dim3 grid(static_cast<unsigned>(a.rows < at_once ? a.rows : at_once));
+    auto go = [&](auto kernel) { return qtz_launch_dependent(kernel, grid, threads, 0, st, a); };
+    if (per == 1) return go(norm_kernel<T, 1>);
+    if (per == 4) return go(norm_kernel<T, 4>);
+    return go(norm_kernel<T, kMost>);
 }
 
 template <typename T>
-cudaError_t launch_quantize(const QuantArgs& a, int num_sms, cudaStream_t st)
+cudaError_t launch_quantize(QuantArgs& a, int num_sms, cudaStream_t st)
 {
-    const unsigned slabs = static_cast<unsigned>((a.k + kQuantThreads * 8 - 1) / (kQuantThreads * 8));
-    int64_t groups = (a.rows + kQuantRows - 1) / kQuantRows;
-    if (a.rows * slabs <= 8 * num_sms) groups = a.rows;          // few rows: one each, for the least latency
-    const dim3 grid(slabs, static_cast<unsigned>(groups < 65535 ? groups : 65535));
-    if (a.gate) return qtz_launch_dependent(quantize_kernel<T, true>, grid, kQuantThreads, 0, st, a);
-    return qtz_launch_dependent(quantize_kernel<T, false>, grid, kQuantThreads, 0, st, a);
+    a.pieces = (a.k + 32 * kColsOf<T> - 1) / (32 * kColsOf<T>);
+    // Two rows a warp where the warps that the registers allow at once have enough to do, one for the least latency where they do not.
+    const int64_t most = static_cast<int64_t>(num_sms) * kQuantWarpsPerSm;
+    a.per = a.rows * a.pieces <= 4 * most ? 1 : 2;
+    const int64_t units = (a.rows + a.per - 1) / a.per * a.pieces, warps = units < most ? units : most;
+    const dim3 grid(static_cast<unsigned>((warps + kQuantWarps - 1) / kQuantWarps));
+    if (a.gate) return qtz_launch_dependent(quantize_kernel<T, true>, grid, kQuantWarps * 32, 0, st, a);
+    return qtz_launch_dependent(quantize_kernel<T, false>, grid, kQuantWarps * 32, 0, st, a);
 }
 
 }  // namespace
@@ -319,7 +389,7 @@ extern "C" qtz_status qtz_f8_rmsnorm(qtz_handle h, const void* x_dev, int64_t x_
                                      int64_t scales_stride, void* stream)
 {
     if (!h || rows < 0 || k <= 0 || !qtz_is_real(ftype) || !(eps >= 1e-30f && eps < INFINITY)) return QTZ_ERR_INVALID_ARG;
-    if (k > kNormThreads * kNormChunks * 8 || rows > 0x7fffffff) return QTZ_ERR_TOO_LARGE;
+    if (k > kMostColumns || rows > 0x7fffffff) return QTZ_ERR_TOO_LARGE;
     if (rows == 0) return QTZ_OK;
     if (!codes_dev && !values_dev) return QTZ_ERR_INVALID_ARG;
     const int size = ftype == QTZ_F32 ? 4 : 2;
@@ -331,11 +401,11 @@ extern "C" qtz_status qtz_f8_rmsnorm(qtz_handle h, const void* x_dev, int64_t x_
     if (s == QTZ_OK && codes_dev) s = check_codes(codes_dev, codes_stride, scales_dev, scales_stride, rows, k);
     if (s != QTZ_OK) return s;
     qtz_device_guard guard(h->device);
-    const NormArgs a{x_dev, residual_dev, gain_dev, x_stride, residual_stride, sum_stride, values_stride, codes_stride, scales_stride,
+    const NormArgs a{x_dev, residual_dev, gain_dev, x_stride, residual_stride, sum_stride, values_stride, codes_stride, scales_stride, rows,
                      sum_dev, values_dev, codes_dev, scales_dev, eps, k};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    QTZ_CUDA(h, ftype == QTZ_F32 ? launch_norm<float>(a, rows, h->num_sms, st)
-              : ftype == QTZ_F16 ? launch_norm<__half>(a, rows, h->num_sms, st) : launch_norm<__nv_bfloat16>(a, rows, h->num_sms, st));
+    QTZ_CUDA(h, ftype == QTZ_F32 ? launch_norm<float>(a, h->num_sms, st)
+              : ftype == QTZ_F16 ? launch_norm<__half>(a, h->num_sms, st) : launch_norm<__nv_bfloat16>(a, h->num_sms, st));
     return QTZ_OK;
 }
 
@@ -352,7 +422,7 @@ extern "C" qtz_status qtz_f8_quantize(qtz_handle h, const void* x_dev, int64_t x
     if (s == QTZ_OK) s = check_codes(codes_dev, codes_stride, scales_dev, scales_stride, rows, k);
     if (s != QTZ_OK) return s;
     qtz_device_guard guard(h->device);
-    const QuantArgs a{x_dev, gate_dev, x_stride, gate_stride, rows, codes_stride, scales_stride, codes_dev, scales_dev, k};
+    QuantArgs a{x_dev, gate_dev, x_stride, gate_stride, rows, codes_stride, scales_stride, codes_dev, scales_dev, k, 0, 0};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     QTZ_CUDA(h, ftype == QTZ_F32 ? launch_quantize<float>(a, h->num_sms, st)
               : ftype == QTZ_F16 ? launch_quantize<__half>(a, h->num_sms, st) : launch_quantize<__nv_bfloat16>(a, h->num_sms, st));
