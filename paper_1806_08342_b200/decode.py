@@ -7,7 +7,9 @@ copied to the host between the steps, so that a step can be captured in a CUDA g
 
     python -m paper_1806_08342_b200.decode --requests 16 --prompt 500 --steps 64
 
-admits prompts of ragged lengths, then decodes one token a request and step, with seeded random weights and activations.
+admits prompts of ragged lengths, then decodes one token a request and step, with seeded random weights and activations.  With
+`--ffn 5504` each layer is a whole block: norms of the residual stream (`qtz_f8_rmsnorm`) before the attention and before a gated
+feed-forward part whose products run in 8-bit floating point (`qtz_f8_quantize`, `qtz_f8_linear`).
 """
 from __future__ import annotations
 
@@ -78,10 +80,42 @@ class AttentionLayer:
         return self.out(y.view(x.shape[0], -1))
 
 
+class FeedForward:
+    """x' = W_down (silu(W_gate n) * W_up n), n = norm(x + residual) * gain, with e4m3 weights and activations."""
+
+    def __init__(self, handle: qtz.Handle, gain, w_gate_up, w_down, eps: float = 1e-6):
+        """w_gate_up [2 width][hidden], the gate's rows first, and w_down [hidden][width] in any of the three types on the device; width a
+        multiple of 8; gain [hidden] in the layer's type."""
+        self.handle, self.gain, self.eps, self.width = handle, gain, eps, w_down.shape[1]
+        if w_gate_up.shape != (2 * self.width, w_down.shape[0]) or self.width % 8:
+            raise ValueError("expected weights [2 width][hidden] and [hidden][width], width a multiple of 8")
+        self.gate_up, self.down = (handle.f8_linear_create(*handle.f8_quantize_weights(w)) for w in (w_gate_up, w_down))
+
+    def __call__(self, x, residual=None):
+        """(x', x + residual) of x [tokens][hidden]; without a residual the second is x."""
+        codes, scales, _, total = self.handle.f8_rmsnorm(x, self.gain, self.eps, residual=residual)
+        both = self.gate_up(codes, scales, dtype=x.dtype)
+        codes, scales = self.handle.f8_quantize(both[:, self.width:], gate=both[:, :self.width])
+        return self.down(codes, scales, dtype=x.dtype), x if residual is None else total
+
+
+class Block:
+    """An attention layer and a feed-forward part, each behind a norm of the residual stream."""
+
+    def __init__(self, attention: AttentionLayer, gain, feed_forward: FeedForward):
+        self.attention, self.gain, self.feed_forward = attention, gain, feed_forward
+
+    def __call__(self, x, residual, starts, lens, slots, table):
+        """(x', residual') of x [tokens][hidden] and the residual stream, None before the first block."""
+        ff = self.feed_forward
+        _, _, values, total = ff.handle.f8_rmsnorm(x, self.gain, ff.eps, residual=residual, codes=False, values=True)
+        return ff(self.attention(values, starts, lens, slots, table), x if residual is None else total)
+
+
 def main(argv=None) -> dict:
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     for name, value in (("requests", 16), ("prompt", 500), ("steps", 64), ("layers", 4), ("hidden", 2048), ("q-heads", 16),
-                        ("kv-heads", 4), ("head-dim", 128), ("block-tokens", 32), ("group", 128), ("window", 0), ("seed", 0)):
+                        ("kv-heads", 4), ("head-dim", 128), ("block-tokens", 32), ("group", 128), ("window", 0), ("seed", 0), ("ffn", 0)):
         ap.add_argument("--" + name, type=int, default=value)
     o = ap.parse_args(argv)
     h = qtz.Handle(0)
@@ -98,11 +132,18 @@ def main(argv=None) -> dict:
     layers = [AttentionLayer(h, randn(width, o.hidden) * o.hidden ** -0.5, randn(o.hidden, o.q_heads * o.head_dim) * (o.q_heads * o.head_dim) ** -0.5,
                              o.q_heads, o.kv_heads, o.head_dim, blocks, o.block_tokens, o.group, window=o.window)
               for _ in range(o.layers)]
+    if o.ffn:
+        layers = [Block(layer, randn(o.hidden).bfloat16(), FeedForward(h, randn(o.hidden).bfloat16(), randn(2 * o.ffn, o.hidden) * o.hidden ** -0.5,
+                                                                       randn(o.hidden, o.ffn) * o.ffn ** -0.5)) for layer in layers]
 
     def step(x, added):
         plan = requests.admit(added, x.shape[0])
+        residual = None
         for layer in layers:
-            x = layer(x, *plan, requests.table)
+            if o.ffn:
+                x, residual = layer(x, residual, *plan, requests.table)
+            else:
+                x = layer(x, *plan, requests.table)
         return x
 
     lengths = [max(1, o.prompt * (r + 1) // o.requests) for r in range(o.requests)]      # ragged prompts
@@ -131,7 +172,7 @@ def main(argv=None) -> dict:
     if rc:
         raise RuntimeError(f"device status {rc} at {site}")
     us = start.elapsed_time(stop) * 1e3 / o.steps
-    print(f"{o.layers} attention layers, {o.requests} requests, {sum(lengths)} prompt tokens: {us:.1f} us a step, "
+    print(f"{o.layers} {'blocks' if o.ffn else 'attention layers'}, {o.requests} requests, {sum(lengths)} prompt tokens: {us:.1f} us a step, "
           f"{o.requests / us * 1e6:.0f} tokens/s")
     return {"us_per_step": us, "lens": requests.cached.tolist()}
 

@@ -571,13 +571,8 @@ class Handle:
         return LinearPlan(self, plan, desc, scales.dtype)
 
     # ---- serving: 8-bit floating point, scales for blocks of 128 ----
-    def _f8_empty(self, rows, k):
-        """Codes [rows][k] whose rows start on 32 bytes (16 are asked for; whole sectors are written faster), and scales [rows][ceil(k / 128)]."""
-        device, pitch = f"cuda:{self.device}", (k + 31) // 32 * 32
-        codes = torch.empty((rows, pitch), dtype=E4M3, device=device)
-        return codes if pitch == k else codes[:, :k], torch.empty((rows, (k + 127) // 128), dtype=torch.float32, device=device)
-
-    def _f8_rows(self, dtype, shape, *ts):
+    def _f8_refuse(self, dtype, shape, *ts):
+        """Raises for the first tensor that is not rows of neighbouring values of that type and shape on this device."""
         for t in ts:
             if t is not None and (t.dtype is not dtype or t.get_device() != self.device or t.shape != shape or (t.stride(1) != 1 and shape[1] > 1)):
                 raise ValueError(f"expected rows of {dtype} values of shape {tuple(shape)} on cuda:{self.device}, got {t.dtype}, {tuple(t.shape)}, "
@@ -587,46 +582,67 @@ class Handle:
         """Root-mean-square norm of the rows of x (+ residual) [rows][k]: (codes, scales, values, sum).  codes and scales (e4m3
         [rows][k], fp32 [rows][ceil(k / 128)]) are None unless `codes`, values (the type of x) unless `values`, sum (x + residual)
         without a residual.  `sum_out` may be `residual` itself."""
-        dtype, shape = x.dtype, x.shape
-        if len(shape) != 2 or dtype not in FTYPES:
+        dtype, shape, device = x.dtype, x.shape, self.device
+        ftype = FTYPES.get(dtype)
+        if ftype is None or len(shape) != 2:
             raise ValueError("expected rows of float32, float16 or bfloat16 values")
         rows, k = shape
-        total = None
+        total, r_at, r_stride, t_at, t_stride = None, None, 0, None, 0
         if residual is not None:
-            total = x.new_empty((rows, (k + 15) // 16 * 16))[:, :k] if sum_out is None else sum_out
-        elif sum_out is not None:
-            raise ValueError("sum_out belongs to a residual")
-        self._f8_rows(dtype, shape, x, residual, total)
-        if gain.dtype is not dtype or gain.shape != (k,) or gain.get_device() != self.device or not gain.is_contiguous():
-            raise ValueError(f"expected a gain of {k} {dtype} values on cuda:{self.device}")
-        out = x.new_empty((rows, (k + 15) // 16 * 16))[:, :k] if values else None
-        q, s = self._f8_empty(rows, k) if codes else (None, None)
-        at = lambda t: (None, 0) if t is None else (t.data_ptr(), t.stride(0))  # noqa: E731
-        rc = self.lib.qtz_f8_rmsnorm(self.h, *at(x), *at(residual), gain.data_ptr(), eps, rows, k, FTYPES[dtype], *at(total), *at(out), *at(q), *at(s),
-                                     _raw_stream(self.device))
+            total = sum_out
+            if total is None:
+                t_stride = (k + 15) // 16 * 16
+                total = x.new_empty_strided(shape, (t_stride, 1))
+                self._f8_refuse(dtype, shape, x, residual)
+            else:
+                self._f8_refuse(dtype, shape, x, residual, total)
+                t_stride = total.stride(0)
+            r_at, r_stride, t_at = residual.data_ptr(), residual.stride(0), total.data_ptr()
+        else:
+            if sum_out is not None:
+                raise ValueError("sum_out belongs to a residual")
+            self._f8_refuse(dtype, shape, x)
+        if gain.dtype is not dtype or gain.shape != (k,) or gain.get_device() != device or not gain.is_contiguous():
+            raise ValueError(f"expected a gain of {k} {dtype} values on cuda:{device}")
+        out = q = scales = None
+        v_at, v_stride, q_at, q_stride, s_at = None, 0, None, 0, None
+        blocks = (k + 127) // 128
+        if values:
+            v_stride = (k + 15) // 16 * 16
+            out = x.new_empty_strided(shape, (v_stride, 1))
+            v_at = out.data_ptr()
+        if codes:
+            q_stride = (k + 31) // 32 * 32                # 16 bytes are asked for; whole sectors are written faster
+            q, scales = x.new_empty_strided(shape, (q_stride, 1), dtype=E4M3), x.new_empty((rows, blocks), dtype=torch.float32)
+            q_at, s_at = q.data_ptr(), scales.data_ptr()
+        rc = self.lib.qtz_f8_rmsnorm(self.h, x.data_ptr(), x.stride(0), r_at, r_stride, gain.data_ptr(), eps, rows, k, ftype, t_at, t_stride, v_at, v_stride,
+                                     q_at, q_stride, s_at, blocks, _raw_stream(device))
         if rc:
             self._chk(rc, "qtz_f8_rmsnorm")
-        return q, s, out, total
+        return q, scales, out, total
 
     def f8_quantize(self, x, gate=None):
         """Codes (e4m3 [rows][k]) and scales (fp32 [rows][ceil(k / 128)]) of x [rows][k], or of silu(gate) * x."""
         dtype, shape = x.dtype, x.shape
-        if len(shape) != 2 or dtype not in FTYPES:
+        ftype = FTYPES.get(dtype)
+        if ftype is None or len(shape) != 2:
             raise ValueError("expected rows of float32, float16 or bfloat16 values")
-        self._f8_rows(dtype, shape, x, gate)
+        self._f8_refuse(dtype, shape, x, gate)
         rows, k = shape
-        q, s = self._f8_empty(rows, k)
-        rc = self.lib.qtz_f8_quantize(self.h, x.data_ptr(), x.stride(0), None if gate is None else gate.data_ptr(), 0 if gate is None else gate.stride(0),
-                                      rows, k, FTYPES[dtype], q.data_ptr(), q.stride(0), s.data_ptr(), s.stride(0), _raw_stream(self.device))
+        pitch, blocks = (k + 31) // 32 * 32, (k + 127) // 128
+        q, scales = x.new_empty_strided(shape, (pitch, 1), dtype=E4M3), x.new_empty((rows, blocks), dtype=torch.float32)
+        g_at, g_stride = (None, 0) if gate is None else (gate.data_ptr(), gate.stride(0))
+        rc = self.lib.qtz_f8_quantize(self.h, x.data_ptr(), x.stride(0), g_at, g_stride, rows, k, ftype, q.data_ptr(), pitch, scales.data_ptr(), blocks,
+                                      _raw_stream(self.device))
         if rc:
             self._chk(rc, "qtz_f8_quantize")
-        return q, s
+        return q, scales
 
     def f8_quantize_weights(self, w):
         """Codes (e4m3 [n][k]) and scales (fp32 [ceil(n / 128)][ceil(k / 128)]) of weights w [n][k], as f8_linear_create takes them."""
         if w.dim() != 2 or w.dtype not in FTYPES:
             raise ValueError("expected a matrix of float32, float16 or bfloat16 values")
-        self._f8_rows(w.dtype, w.shape, w)
+        self._f8_refuse(w.dtype, w.shape, w)
         n, k = w.shape
         codes = torch.empty((n, k), dtype=E4M3, device=w.device)
         scales = torch.empty((-(-n // 128), -(-k // 128)), dtype=torch.float32, device=w.device)
@@ -639,7 +655,7 @@ class Handle:
         if codes.dim() != 2:
             raise ValueError("expected codes [n][k]")
         n, k = codes.shape
-        self._f8_rows(E4M3, codes.shape, codes)
+        self._f8_refuse(E4M3, codes.shape, codes)
         _check_flat(self.device, torch.float32, scales)
         if scales.shape != (-(-n // 128), -(-k // 128)):
             raise ValueError(f"expected a scale for each 128 x 128 block of [{n}][{k}], got {tuple(scales.shape)}")
@@ -832,23 +848,27 @@ class F8LinearPlan:
 
     def __call__(self, codes, scales, dtype=torch.bfloat16, out=None):
         """codes [rows][k] in e4m3 (rows a multiple of 16 bytes apart), scales [rows][ceil(k / 128)] in fp32 with any strides."""
-        device, n = self.device, self.n
+        device, n, shape, (stride, next_to), (row_stride, block_stride) = self.device, self.n, codes.shape, codes.stride(), scales.stride()
         if codes.dtype is not E4M3 or codes.get_device() != device or scales.dtype is not torch.float32 or scales.get_device() != device:
             raise ValueError(f"expected {E4M3} codes and float32 scales on cuda:{device}, got {codes.dtype} on {codes.device}, {scales.dtype} on {scales.device}")
-        rows = codes.shape[0]
-        if codes.shape != (rows, self.k) or (codes.stride(1) != 1 and self.k > 1) or scales.shape != (rows, self.blocks):
-            raise ValueError(f"expected rows of {self.k} neighbouring codes and {self.blocks} scales, got {tuple(codes.shape)} with strides "
-                             f"{codes.stride()} and {tuple(scales.shape)}")
+        rows, k = shape
+        if k != self.k or (next_to != 1 and k > 1) or scales.shape != (rows, self.blocks):
+            raise ValueError(f"expected rows of {self.k} neighbouring codes and {self.blocks} scales, got {tuple(shape)} with strides {codes.stride()} "
+                             f"and {tuple(scales.shape)}")
         if out is None:
-            if dtype not in FTYPES:
+            ftype, y_stride = FTYPES.get(dtype), n
+            if ftype is None:
                 raise ValueError("y is float32, float16 or bfloat16")
-            out = torch.empty((rows, n), dtype=dtype, device=codes.device)
-        elif out.shape != (rows, n) or (out.stride(1) != 1 and n > 1) or out.dtype not in FTYPES or out.get_device() != device:
-            raise ValueError(f"expected out of shape {(rows, n)} on cuda:{device}")
+            out = codes.new_empty((rows, n), dtype=dtype)
+        else:
+            ftype = FTYPES.get(out.dtype)
+            if ftype is None or out.shape != (rows, n) or (out.stride(1) != 1 and n > 1) or out.get_device() != device:
+                raise ValueError(f"expected out of shape {(rows, n)} on cuda:{device}")
+            y_stride = out.stride(0)
         if not self.handle.h:
             raise ValueError("the handle of this plan is closed")
-        rc = self._run(self.plan, codes.data_ptr(), codes.stride(0), scales.data_ptr(), scales.stride(0), scales.stride(1), rows, out.data_ptr(),
-                       out.stride(0), FTYPES[out.dtype], _raw_stream(device))
+        rc = self._run(self.plan, codes.data_ptr(), stride, scales.data_ptr(), row_stride, block_stride, rows, out.data_ptr(), y_stride, ftype,
+                       _raw_stream(device))
         if rc:
             self.handle._chk(rc, "qtz_f8_linear")
         return out
