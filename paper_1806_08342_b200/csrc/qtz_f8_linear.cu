@@ -54,10 +54,8 @@ struct LinearArgs {
     int32_t n, n_tiles, k_blocks, ftype;
     int32_t vector;            // rows of y start on 16 bytes
     int32_t row_tiles;         // tiles of activation rows
-    int32_t split;             // few rows: CTAs (of a cluster) that share the columns of a tile; 0: shares of the sequence of units
-    int32_t units, share;      // tiles x blocks of 128 columns, and how many of them a CTA takes
-    float* parts;              // few rows: what tiles that lie in several shares are joined from
-    int32_t* counters;
+    int32_t tiles;             // in all
+    int32_t split;             // CTAs or pairs of a cluster, which share the columns of a tile
     long long wait_budget;
     int32_t* status;
 };
@@ -190,11 +188,9 @@ __device__ __forceinline__ void add_block(float (&acc)[128], uint32_t from, floa
 constexpr int kSlots = 8, kAhead = 4;
 
 // ---- few rows: the weights stream past a tile of rows ----
-// A tile is 128 rows of x, of which kRows are loaded (what the other rows of the product hold is not looked at), and 256 weights.  Where
-// there are fewer tiles than SMs, the CTAs of a cluster take equal parts of a tile's columns and join their sums through each other's shared
-// memory.  Where there are more, units (tile, block of 128 columns) form one sequence that is dealt out in equal contiguous shares; a tile
-// that lies in several shares is joined by the last CTA to arrive.  A thread owns a row of x and half of the weights, which share a scale:
-// one factor a thread and unit.
+// A tile is 128 rows of x, of which kRows are loaded (what the other rows of the product hold is not looked at), and 256 weights.  The CTAs
+// of a cluster take equal parts of a tile's columns and join their sums through each other's shared memory.  A thread owns a row of x and
+// half of the weights, which share a scale: one factor a thread and block of 128 columns.
 constexpr int kMaxSplit = 8;           // CTAs of a cluster
 constexpr int kTileCols = 256, kQuads = kTileCols / 4;
 
@@ -204,21 +200,6 @@ struct Stream {
     static constexpr int kRoom = (kSmemLimit - 1024 - 8 * kOutBytes - kSlots * (kRows + 2) * 4 - 1024) / kStage, kStages = kRoom < kMaxStages ? kRoom : kMaxStages;
     static constexpr int kSmem = 1024 + kStages * kStage + 8 * kOutBytes;
 };
-
-struct Unit {                          // row tiles of the same 256 weights follow each other
-    int col, row_tile, kb;
-    __device__ Unit(const LinearArgs& a, int u) : col(u / a.k_blocks / a.row_tiles), row_tile(u / a.k_blocks % a.row_tiles), kb(u % a.k_blocks) {}
-    __device__ void next(const LinearArgs& a)
-    {
-        if (++kb < a.k_blocks) return;
-        kb = 0;
-        if (++row_tile < a.row_tiles) return;
-        row_tile = 0;
-        ++col;
-    }
-};
-
-__device__ __forceinline__ float* part_of(const LinearArgs& a, int cta, int which) { return a.parts + (static_cast<int64_t>(cta) * 2 + which) * (kF8Block * kTileCols); }
 
 // Four neighbouring sums.
 __device__ __forceinline__ void put_quad(const LinearArgs& a, int64_t row, int o, float4 v)
@@ -266,62 +247,10 @@ __device__ __forceinline__ void keep_sums(const float (&acc)[128], uint32_t base
     for (int c = 0; c < 128; c += 4) sts128(quad_at(base, row, half * 32 + c / 4), make_float4(acc[c], acc[c + 1], acc[c + 2], acc[c + 3]));
 }
 
-// After a CTA's last unit: counts its arrival at the tiles that it shares with others, and sums those at which it is the last, in the
-// order of the columns.  Called by the warps of the sums, behind a barrier of theirs.
-__device__ __forceinline__ void join_tiles(const LinearArgs& a, const int (&open)[2], int (&last)[2])
-{
-    const int tid = threadIdx.x - (kThreads - kSumThreads);
-    auto first = [&](int unit) { return unit / a.k_blocks * a.k_blocks; };
-    if ((tid == 0 && open[0] >= 0) || (tid == 32 && open[1] >= 0)) {
-        const int begin = first(tid ? open[1] : open[0]), c0 = begin / a.share;
-        const bool all = arrive_acq_rel(a.counters + c0) == (begin + a.k_blocks - 1) / a.share - c0;
-        last[tid ? 1 : 0] = all;
-        if (all) a.counters[c0] = 0;                   // ready for the next call
-    }
-    named_barrier(1, kSumThreads);
-#pragma unroll 1
-    for (int which = 0; which < 2; ++which) {
-        const int unit = open[which];
-        if (unit < 0 || !last[which]) continue;
-        const int begin = first(unit), c0 = begin / a.share, c1 = (begin + a.k_blocks - 1) / a.share;
-        const Unit at(a, unit);
-        const int64_t r0 = static_cast<int64_t>(at.row_tile) * kF8Block;
-        const int quads = static_cast<int>(min(static_cast<int64_t>(kF8Block), a.rows - r0)) * kQuads;
-        constexpr int kAtOnce = 6, kParts = 4;         // loads under way: of a pass over all rows there are two
-#pragma unroll 1
-        for (int q0 = tid; q0 < quads; q0 += kAtOnce * kSumThreads) {
-            float4 v[kAtOnce];
-#pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) v[j] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-            for (int c = c0; c <= c1; c += kParts) {
-                float4 p[kParts][kAtOnce];
-#pragma unroll
-                for (int x = 0; x < kParts; ++x) {
-                    const float4* const part = reinterpret_cast<const float4*>(part_of(a, c + x, c + x == c0 ? 1 : 0)) + q0;
-#pragma unroll
-                    for (int j = 0; j < kAtOnce; ++j)
-                        p[x][j] = c + x <= c1 && q0 + j * kSumThreads < quads ? __ldcg(part + j * kSumThreads) : make_float4(0.f, 0.f, 0.f, 0.f);
-                }
-#pragma unroll
-                for (int x = 0; x < kParts; ++x)
-#pragma unroll
-                    for (int j = 0; j < kAtOnce; ++j) {
-                        v[j].x += p[x][j].x;
-                        v[j].y += p[x][j].y;
-                        v[j].z += p[x][j].z;
-                        v[j].w += p[x][j].w;
-                    }
-            }
-#pragma unroll
-            for (int j = 0; j < kAtOnce; ++j) {
-                const int q = q0 + j * kSumThreads;
-                if (q >= quads) break;
-                put_quad(a, r0 + q / kQuads, at.col * kTileCols + q % kQuads * 4, v[j]);
-            }
-        }
-    }
-}
+struct StreamTile {                    // row tiles of the same 256 weights follow each other
+    int row, col;
+    __device__ StreamTile(const LinearArgs& a, int tile) : row(tile % a.row_tiles), col(tile / a.row_tiles) {}
+};
 
 template <int kRows>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -331,14 +260,12 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
     extern __shared__ uint8_t smem_raw[];              // the ring: kRows rows of x, a tile of weights; then values on their way out
     __shared__ float s_x[kSlots][kRows], s_w[kSlots][2];               // scales
     __shared__ __align__(8) uint64_t s_full[kMaxStages], s_empty[kMaxStages], s_done[2], s_free[2], s_drain;
-    __shared__ int s_open[2], s_last[2];               // s_open: units whose tiles are shared with an earlier / a later CTA
     __shared__ uint32_t s_tmem;
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     // warps of the sums whose rows exist: those of a quarter of tensor memory take 32 rows
     const int quarters = static_cast<int>(min(static_cast<int64_t>(4), (a.rows + 31) / 32));
     if (tid == 0) {
-        s_open[0] = s_open[1] = -1;
         prefetch_tensormap(&w_map);
         prefetch_tensormap(&x_map);
         for (int i = 0; i < S::kStages; ++i) {
@@ -360,12 +287,8 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
-    int u0 = blockIdx.x * a.share, count = min(u0 + a.share, a.units) - u0;
-    if (a.split) {
-        const int tile = blockIdx.x / a.split, part = blockIdx.x % a.split, first = part * a.k_blocks / a.split;
-        u0 = tile * a.k_blocks + first;
-        count = (part + 1) * a.k_blocks / a.split - first;
-    }
+    const int tile0 = blockIdx.x / a.split, step = gridDim.x / a.split, part = blockIdx.x % a.split;
+    const int kb0 = part * a.k_blocks / a.split, kbs = (part + 1) * a.k_blocks / a.split - kb0, count = (a.tiles - 1 - tile0) / step * kbs + kbs;   // blocks
     bool ok = true;
     auto wait = [&](uint64_t& bar, int parity) { ok = mbar_wait_warp(smem_u32(&bar), parity, a.wait_budget, ok); };
     grid_launch_dependents();
@@ -374,42 +297,39 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFew));
         if (warp == 0) {
             // ======== loads ========
-            Unit here(a, u0), ahead = here;
-            auto weights = [&](int stage) {
+            // Weights were there when the layer was made: a ring of them is asked for before all else is waited for.
+            int stage = 0, round = 0, issued = 0;
+            auto weights = [&](int col, int kb, int to_stage) {
                 if (elect_one()) {
-                    const uint32_t bar = smem_u32(&s_full[stage]), to = base + stage * S::kStage + kRows * kF8Block;
-                    const bool both = 2 * ahead.col + 1 < a.n_tiles;
+                    const uint32_t bar = smem_u32(&s_full[to_stage]), to = base + to_stage * S::kStage + kRows * kF8Block;
+                    const bool both = 2 * col + 1 < a.n_tiles;
                     mbar_arrive_expect_tx(bar, both ? S::kStage : S::kStage - kTileBytes);
-                    tma_load_2d(to, &w_map, bar, 0, w_row(a, ahead.col, ahead.kb, 0));
-                    if (both) tma_load_2d(to + kTileBytes, &w_map, bar, 0, w_row(a, ahead.col, ahead.kb, 1));
+                    tma_load_2d(to, &w_map, bar, 0, w_row(a, col, kb, 0));
+                    if (both) tma_load_2d(to + kTileBytes, &w_map, bar, 0, w_row(a, col, kb, 1));
                 }
                 __syncwarp();
-                ahead.next(a);
             };
-            auto rows = [&](int stage) {
-                if (elect_one()) tma_load_2d(base + stage * S::kStage, &x_map, smem_u32(&s_full[stage]), here.kb * kF8Block, here.row_tile * kF8Block);
-                __syncwarp();
-                here.next(a);
-            };
-            const int early = min(S::kStages, count);
-            for (int i = 0; i < early; ++i) weights(i);    // they were there when the layer was made
-            grid_dependency_wait();                        // all else is waited for
-            for (int i = 0; i < early; ++i) rows(i);
-            int issued = early, stage = 0, round = 0;
-            for (; issued < count; ++issued) {
-                wait(s_empty[stage], round & 1);
-                if (!ok) break;
-                weights(stage);
-                rows(stage);
-                if (++stage == S::kStages) {
-                    stage = 0;
-                    ++round;
+            const int early = min(S::kStages, kbs);
+            for (int i = 0; i < early; ++i) weights(StreamTile(a, tile0).col, kb0 + i, i);
+            grid_dependency_wait();
+            for (int tile = tile0; ok && tile < a.tiles; tile += step) {
+                const StreamTile at(a, tile);
+                for (int kb = kb0; kb < kb0 + kbs; ++kb, ++issued) {
+                    if (issued >= S::kStages) wait(s_empty[stage], (round & 1) ^ 1);
+                    if (!ok) break;
+                    if (issued >= early) weights(at.col, kb, stage);
+                    if (elect_one()) tma_load_2d(base + stage * S::kStage, &x_map, smem_u32(&s_full[stage]), kb * kF8Block, at.row * kF8Block);
+                    __syncwarp();
+                    if (++stage == S::kStages) {
+                        stage = 0;
+                        ++round;
+                    }
                 }
             }
             // nothing may be in flight when the CTA ends
             for (int j = max(0, issued - S::kStages); j < issued; ++j) ok = mbar_wait_warp(smem_u32(&s_full[j % S::kStages]), (j / S::kStages) & 1, kDrainBudget, ok);
         } else if (warp == 1 || warp == 3) {
-            // ======== products: a warp for the even units, one for the odd ones ========
+            // ======== products: a warp for the even blocks, one for the odd ones ========
             const int buffer = warp >> 1;
             int stage = buffer, round = 0;
             for (int i = buffer; i < count; i += 2) {
@@ -436,26 +356,37 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
         } else if (warp == 2) {
             // ======== scales ========
             grid_dependency_wait();
-            Unit here(a, u0);
+            constexpr int kEach = (kRows + 31) / 32;
+            int tile = tile0, kb = 0;
+            const float* from[kEach + 1];              // rows of x; lanes 0 and 1: 128 weights
             for (int i = 0; i < count + kAhead; ++i) {
                 const int now = i - kAhead;
                 if (now >= 0) {
-                    cp_async_wait<kAhead - 2>();       // the unit's scales and the next one's
+                    cp_async_wait<kAhead - 2>();       // the block's scales and the next one's
                     __syncwarp();
                     if (now >= 2) wait(s_done[now & 1], (now >> 1 & 1) ^ 1);
                     if (!ok) break;
                     if (lane == 0) mbar_arrive(smem_u32(&s_done[now & 1]));
                 }
-                // The place held the scales of eight units ago, which have been used: the product of the unit two behind them, which waited for
-                // that, is done.
                 if (i < count) {
-                    const int slot = i % kSlots;
-                    const int64_t r0 = static_cast<int64_t>(here.row_tile) * kF8Block;
+                    if (kb == 0) {
+                        const StreamTile at(a, tile);
+                        const int64_t row0 = static_cast<int64_t>(at.row) * kF8Block + lane;
 #pragma unroll
-                    for (int r = lane; r < kRows; r += 32)
-                        cp_async_4(smem_u32(&s_x[slot][r]), a.x_scales + min(r0 + r, a.rows - 1) * a.row_stride + here.kb * a.block_stride);
-                    if (lane < 2) cp_async_4(smem_u32(&s_w[slot][lane]), a.w_scales + static_cast<int64_t>(min(2 * here.col + lane, a.n_tiles - 1)) * a.k_blocks + here.kb);
-                    here.next(a);
+                        for (int j = 0; j < kEach; ++j) from[j] = a.x_scales + min(row0 + 32 * j, a.rows - 1) * a.row_stride + kb0 * a.block_stride;
+                        from[kEach] = a.w_scales + static_cast<int64_t>(min(2 * at.col + (lane & 1), a.n_tiles - 1)) * a.k_blocks + kb0;
+                    }
+                    // The place held the scales of eight blocks ago, which have been used: the product of the block two behind that one, which
+                    // waited for it, is done.
+                    const int slot = i % kSlots;
+#pragma unroll
+                    for (int j = 0; j < kEach; ++j)
+                        if (32 * j + lane < kRows) cp_async_4(smem_u32(&s_x[slot][32 * j + lane]), from[j] + kb * a.block_stride);
+                    if (lane < 2) cp_async_4(smem_u32(&s_w[slot][lane]), from[kEach] + kb);
+                    if (++kb == kbs) {
+                        kb = 0;
+                        tile += step;
+                    }
                 }
                 cp_async_commit();
             }
@@ -474,48 +405,34 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
             uint4* const out = reinterpret_cast<uint4*>(smem_raw + (base - smem_u32(smem_raw)) + S::kStages * S::kStage + (warp - 4) * kOutBytes);
             grid_dependency_wait();                    // y may be what the kernel before reads
             float acc[128];
-            float s_next = 0.f;                        // the next unit's factor: its scales are there with this unit's
-            Unit here(a, u0);
-            for (int i = 0; ok && i < count;) {            // a tile, or what this CTA has of it
+            float s_next = 0.f;                        // the next block's factor: its scales are there with this block's
+            int i = 0;
+            for (int tile = tile0; ok && tile < a.tiles; tile += step) {
 #pragma unroll
                 for (int c = 0; c < 128; ++c) acc[c] = 0.f;
-                const bool begins = here.kb == 0, ends = i + a.k_blocks - here.kb <= count;
-                const int last = ends ? i + a.k_blocks - here.kb : count;
 #pragma unroll 1
-                for (; i < last; ++i) {
-                    const int slot = i % kSlots, after = (i + 1) % kSlots;
+                for (int kb = 0; kb < kbs; ++kb, ++i) {
+                    const int after = (i + 1) % kSlots;
                     wait(s_done[i & 1], i >> 1 & 1);
                     if (!ok) break;
                     tc_fence_after();
-                    const float s = i ? s_next : s_x[slot][row_lane] * s_w[slot][half];
+                    const float s = i ? s_next : s_x[0][row_lane] * s_w[0][half];
                     s_next = s_x[after][row_lane] * s_w[after][half];
                     add_block(acc, from + (i & 1) * 256, s, [&]() {
                         if (lane == 0) mbar_arrive(smem_u32(&s_free[i & 1]));
                     });
                 }
                 if (!ok) break;
-                const int64_t row = static_cast<int64_t>(here.row_tile) * kF8Block + row_warp;
-                if (a.split > 1) {
-                    // the ring is free: all its products are done
-                    if (row_warp + lane < kRows) keep_sums(acc, base, row_warp + lane, half);
-                } else if (begins && ends) {
-                    put_y(a, row, here.col * kTileCols + half * 128, out, acc);
-                } else {
-                    if (lane == 0) s_open[begins ? 1 : 0] = u0 + i - 1;
-                    put_rows(part_of(a, blockIdx.x, begins ? 1 : 0) + row_warp * kTileCols + half * 128, kTileCols, static_cast<int>(min(static_cast<int64_t>(32), a.rows - row)), 128,
-                             true, out, acc);
-                }
-                here.kb = a.k_blocks - 1;
-                here.next(a);
+                const StreamTile at(a, tile);
+                if (a.split == 1) put_y(a, static_cast<int64_t>(at.row) * kF8Block + row_warp, at.col * kTileCols + half * 128, out, acc);
+                else if (row_warp + lane < kRows) keep_sums(acc, base, row_warp + lane, half);   // the ring is free: the cluster's only tile is done
             }
         }
         if (a.split > 1) {
-            const Unit tile(a, u0);
+            const StreamTile at(a, tile0);
             cluster_sync();                            // the cluster's sums are there
-            join_cluster(a, static_cast<int64_t>(tile.row_tile) * kF8Block, tile.col, base, static_cast<int>(cluster_ctarank()), 0, 1);
+            join_cluster(a, static_cast<int64_t>(at.row) * kF8Block, at.col, base, part, 0, 1);
             cluster_sync();                            // and have been read
-        } else if (!a.split && named_barrier_and(1, kSumThreads, ok)) {
-            join_tiles(a, s_open, s_last);             // after a wait that gave up the results are void
         }
     }
     if (!ok) timed_out(a);
@@ -581,7 +498,7 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
     tc_fence_after();
     const uint32_t tmem = __shfl_sync(0xffffffffu, s_tmem, 0);
     // the pairs of a cluster share the columns of a tile
-    const int tile0 = blockIdx.x / (2 * a.split), step = gridDim.x / (2 * a.split), tiles = a.units, part = rank >> 1;
+    const int tile0 = blockIdx.x / (2 * a.split), step = gridDim.x / (2 * a.split), part = rank >> 1;
     const int kb0 = part * a.k_blocks / a.split, kbs = (part + 1) * a.k_blocks / a.split - kb0;
     bool ok = true;
     grid_launch_dependents();
@@ -592,7 +509,7 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
             // ======== loads: both CTAs' are counted on the first one's barrier ========
             grid_dependency_wait();
             int stage = 0, round = 0, issued = 0;
-            for (int tile = tile0; ok && tile < tiles; tile += step) {
+            for (int tile = tile0; ok && tile < a.tiles; tile += step) {
                 const PairTile at(a, tile);
                 const int w_half = min(static_cast<int>(side), a.n_tiles - 1 - 2 * at.col), x_row = (2 * at.row + static_cast<int>(side)) * kF8Block;
                 for (int kb = kb0; kb < kb0 + kbs; ++kb) {
@@ -619,7 +536,7 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
                     ok = mbar_wait_warp(smem_u32(&s_full[j % kPairStages]), (j / kPairStages) & 1, kDrainBudget, ok);
         } else if (warp != 2) {
             // ======== products: a warp for the even blocks, one for the odd ones ========
-            const int blocks = side == 0 ? (tiles - tile0 + step - 1) / step * kbs : 0, buffer = warp >> 1;
+            const int blocks = side == 0 ? (a.tiles - 1 - tile0) / step * kbs + kbs : 0, buffer = warp >> 1;
             int stage = buffer, round = 0;
             for (int block = buffer; block < blocks; block += 2) {
                 ok = mbar_wait_warp(smem_u32(&s_full[stage]), round & 1, a.wait_budget, ok);
@@ -645,7 +562,7 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
         } else if (warp == 2) {
             // ======== scales: on their way four blocks ahead, counted with the products of the block ========
             grid_dependency_wait();
-            const int blocks = (tiles - tile0 + step - 1) / step * kbs;
+            const int blocks = (a.tiles - 1 - tile0) / step * kbs + kbs;
             int tile = tile0, kb = 0;
             const float* from[5];                      // four rows of x; lanes 0 and 1: a tile of weights
             for (int block = 0; block < blocks + kAhead; ++block) {
@@ -691,7 +608,7 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
         grid_dependency_wait();
         int block = 0;
         float s_next = 0.f;                            // the next block's factor: its scales are there with this block's
-        for (int tile = tile0; ok && tile < tiles; tile += step) {
+        for (int tile = tile0; ok && tile < a.tiles; tile += step) {
             float acc[128];
 #pragma unroll
             for (int c = 0; c < 128; ++c) acc[c] = 0.f;
@@ -731,10 +648,10 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
     }
 }
 
-// Scratch of the joining, shared by the layers of a handle: parts and counters of a full grid.
-qtz_status ensure_scratch(qtz_ctx* h, cudaStream_t st)
+// Asked for once a handle: how many clusters run at once.
+qtz_status learn_clusters(qtz_ctx* h)
 {
-    if (h->f8_dev) return QTZ_OK;
+    if (h->f8_clusters[1]) return QTZ_OK;
     for (const void* kernel : {reinterpret_cast<const void*>(pair_kernel), reinterpret_cast<const void*>(stream_kernel<16>), reinterpret_cast<const void*>(stream_kernel<32>),
                                reinterpret_cast<const void*>(stream_kernel<64>), reinterpret_cast<const void*>(stream_kernel<128>)}) {
         cudaFuncAttributes at;
@@ -743,7 +660,7 @@ qtz_status ensure_scratch(qtz_ctx* h, cudaStream_t st)
     }
     const qtz_status s = qtz_allow_smem(h, stream_kernel<kF8Block>);
     if (s != QTZ_OK) return s;
-    for (int c = 2; c <= kMaxSplit; ++c) {             // clusters that run at once: an SM holds one CTA of any of the stream kernels
+    for (int c = 2; c <= kMaxSplit; ++c) {             // an SM holds one CTA of any of these kernels
         cudaLaunchAttribute size;
         size.id = cudaLaunchAttributeClusterDimension;
         size.val.clusterDim.x = c;
@@ -756,10 +673,7 @@ qtz_status ensure_scratch(qtz_ctx* h, cudaStream_t st)
         cfg.numAttrs = 1;
         QTZ_CUDA(h, cudaOccupancyMaxActiveClusters(&h->f8_clusters[c], stream_kernel<kF8Block>, &cfg));
     }
-    const size_t parts = static_cast<size_t>(h->num_sms) * 2 * kF8Block * kTileCols * sizeof(float);
-    QTZ_CUDA(h, cudaMalloc(&h->f8_dev, parts + h->num_sms * sizeof(int32_t)));
-    QTZ_CUDA(h, cudaMemsetAsync(static_cast<uint8_t*>(h->f8_dev) + parts, 0, h->num_sms * sizeof(int32_t), st));
-    h->f8_counters = reinterpret_cast<int32_t*>(static_cast<uint8_t*>(h->f8_dev) + parts);
+    h->f8_clusters[1] = h->num_sms;
     return QTZ_OK;
 }
 
@@ -790,17 +704,15 @@ qtz_status launch_stream(qtz_f8_layer* p, LinearArgs& a, const CUtensorMap& x_ma
 {
     qtz_ctx* h = p->h;
     a.row_tiles = static_cast<int32_t>((a.rows + kF8Block - 1) / kF8Block);
-    const int tiles = a.row_tiles * ((a.n_tiles + 1) / 2);
-    a.units = tiles * a.k_blocks;
-    if (!a.split) a.share = (a.units + h->num_sms - 1) / h->num_sms;
-    return launch(h, stream_kernel<kRows>, a, a.split ? a.split : 1, a.split ? tiles * a.split : (a.units + a.share - 1) / a.share, Stream<kRows>::kSmem, st, p->w_map, x_map);
+    a.tiles = a.row_tiles * ((a.n_tiles + 1) / 2);
+    return launch(h, stream_kernel<kRows>, a, a.split, a.split * (a.split > 1 || a.tiles < h->num_sms ? a.tiles : h->num_sms), Stream<kRows>::kSmem, st, p->w_map, x_map);
 }
 
-// How many clusters' CTAs (times `each`) can take parts of a tile's columns with all tiles at work at once; 0: not even one.
+// How many CTAs (pairs, with each = 2) of a cluster can share a tile's columns with all tiles at work at once; 1 where there are more tiles.
 int most_split(const qtz_ctx* h, int64_t tiles, int each, int k_blocks)
 {
-    int split = tiles * each <= h->num_sms ? 1 : 0;
-    for (int c = 2; split && c * each <= kMaxSplit && c <= k_blocks; ++c)
+    int split = 1;
+    for (int c = 2; c * each <= kMaxSplit && c <= k_blocks; ++c)
         if (tiles <= h->f8_clusters[c * each]) split = c;
     return split;
 }
@@ -809,9 +721,9 @@ qtz_status launch_pair(qtz_f8_layer* p, LinearArgs& a, const CUtensorMap& x_map,
 {
     qtz_ctx* h = p->h;
     a.row_tiles = static_cast<int32_t>((a.rows + 255) / 256);
-    a.units = a.row_tiles * ((a.n_tiles + 1) / 2);
+    a.tiles = a.row_tiles * ((a.n_tiles + 1) / 2);
     const int pairs = h->num_sms / 2;
-    return launch(h, pair_kernel, a, 2 * a.split, 2 * a.split * (a.split > 1 || a.units < pairs ? a.units : pairs), 1024 + kPairStages * kPairStage + 8 * kOutBytes, st, p->w_map, x_map);
+    return launch(h, pair_kernel, a, 2 * a.split, 2 * a.split * (a.split > 1 || a.tiles < pairs ? a.tiles : pairs), 1024 + kPairStages * kPairStage + 8 * kOutBytes, st, p->w_map, x_map);
 }
 
 }  // namespace
@@ -836,7 +748,7 @@ extern "C" qtz_status qtz_f8_linear_create(qtz_handle h, int32_t n, int32_t k, c
     if (n_tiles > 65535 || n_tiles * k_blocks > (1 << 23)) return QTZ_ERR_TOO_LARGE;
     qtz_device_guard guard(h->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const qtz_status s = ensure_scratch(h, st);
+    const qtz_status s = learn_clusters(h);
     if (s != QTZ_OK) return s;
     qtz_f8_layer* p = new (std::nothrow) qtz_f8_layer();
     if (!p) return QTZ_ERR_INVALID_ARG;
@@ -883,21 +795,20 @@ extern "C" qtz_status qtz_f8_linear(qtz_f8_linear_plan p, const uint8_t* codes_d
     if (rows == 0) return QTZ_OK;
     if (!codes_dev || !scales_dev || !y_dev || (rows > 1 && (codes_stride < p->k || y_stride < p->n))) return QTZ_ERR_INVALID_ARG;
     if (!qtz_aligned16(codes_dev) || (rows > 1 && codes_stride % 16 != 0)) return QTZ_ERR_MISALIGNED;
-    // tiles of at least 16 rows of x, of 128 weights and of 128 columns are counted in 32 bits
-    if (rows > 0x7fffff00 || (rows + 127) / 128 * p->n_tiles * p->k_blocks > 0x3fffffff) return QTZ_ERR_TOO_LARGE;
+    if (rows > 0x7fffff00 || (rows + 127) / 128 * p->n_tiles * p->k_blocks > 0x3fffffff) return QTZ_ERR_TOO_LARGE;   // counted in 32 bits
     qtz_ctx* h = p->h;
     qtz_device_guard guard(h->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     LinearArgs a{p->scales, p->bias, scales_dev, scales_row_stride, scales_block_stride, rows, y_stride, y_dev, p->n, p->n_tiles, p->k_blocks, ftype,
-                 qtz_aligned16(y_dev) && (rows <= 1 || y_stride * (ftype == QTZ_F32 ? 4 : 2) % 16 == 0), 0, 0, 0, 0,
-                 static_cast<float*>(h->f8_dev), h->f8_counters, h->wait_budget, h->status_dev};
-    // More than 128 rows: a tile's block of 128 columns takes a pair about 10 and a CTA about 13 units of time; single CTAs only where each
-    // has at most one tile.
-    const int64_t cols = (p->n_tiles + 1) / 2, pair_tiles = (rows + 255) / 256 * cols, tiles = (rows + 127) / 128 * cols;
+                 qtz_aligned16(y_dev) && (rows <= 1 || y_stride * (ftype == QTZ_F32 ? 4 : 2) % 16 == 0), 0, 0, 0, h->wait_budget, h->status_dev};
+    // Up to 128 rows single CTAs, whose tiles those are.  More: a tile's block of 128 columns takes a pair 10 and a CTA about 13 units of time,
+    // and the longest of either has so many of them (us, CTAs | pairs: 160 x 4096 -> 4096 13.8 | 14.8, 160 x 8192 -> 10240 42 | 33,
+    // 800 x 10001 -> 5003 51 | 82, 512 x 4096 -> 6144 23 | 20); CTAs that take several tiles are slower than that (1777 x 4096 -> 4096 63 | 35).
+    const int64_t cols = (p->n_tiles + 1) / 2, pair_tiles = (rows + 255) / 256 * cols, tiles = (rows + 127) / 128 * cols, pairs = h->num_sms / 2;
     const int pair_split = most_split(h, pair_tiles, 2, p->k_blocks), split = most_split(h, tiles, 1, p->k_blocks);
-    const int64_t pair_cost = 10 * (pair_split ? (p->k_blocks + pair_split - 1) / pair_split : (pair_tiles + h->num_sms / 2 - 1) / (h->num_sms / 2) * p->k_blocks);
-    const bool pair = rows > 128 && (!split || pair_cost < 13 * ((p->k_blocks + split - 1) / split));
-    a.split = pair ? (pair_split ? pair_split : 1) : split;
+    const int64_t pair_blocks = (pair_tiles + pairs - 1) / pairs * ((p->k_blocks + pair_split - 1) / pair_split), blocks = (p->k_blocks + split - 1) / split;
+    const bool pair = rows > 128 && (tiles > h->num_sms || 10 * pair_blocks < 13 * blocks);
+    a.split = pair ? pair_split : split;
     const int box_rows = pair ? 128 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
     CUtensorMap x_map;                                 // columns beyond k and rows beyond the last read as zero
     const int64_t pitch = rows > 1 ? codes_stride : (p->k + 15) / 16 * 16;

@@ -66,7 +66,6 @@ extern "C" qtz_status qtz_destroy(qtz_handle h)
     if (h->reduce_dev) cudaFree(h->reduce_dev);
     if (h->status_dev) cudaFree(h->status_dev);
     if (h->linear_dev) cudaFree(h->linear_dev);
-    if (h->f8_dev) cudaFree(h->f8_dev);
     if (h->reduce_host) cudaFreeHost(h->reduce_host);
     (void)cudaGetLastError();
     delete h;
@@ -87,7 +86,6 @@ extern "C" qtz_status qtz_last_device_status(qtz_handle h, int32_t* site_id, voi
     if (host[at] != 0) QTZ_CUDA(h, cudaMemsetAsync(h->status_dev + at, 0, 2 * sizeof(int32_t), st));
     // a linear layer that gave up may have left its parts counted
     if (host[0] != 0 && h->linear_counters) QTZ_CUDA(h, cudaMemsetAsync(h->linear_counters, 0, 2 * h->num_sms * sizeof(int32_t), st));
-    if (host[0] != 0 && h->f8_counters) QTZ_CUDA(h, cudaMemsetAsync(h->f8_counters, 0, h->num_sms * sizeof(int32_t), st));
     return host[at];
 }
 

@@ -27,9 +27,7 @@ struct qtz_ctx {
     size_t reduce_host_bytes = 0;
     void* linear_dev = nullptr;             // parts and counters of linear layers (allocated with the first layer)
     int32_t* linear_counters = nullptr;     // within it
-    void* f8_dev = nullptr;                 // the same of 8-bit floating-point layers
-    int32_t* f8_counters = nullptr;
-    int f8_clusters[9] = {};                // clusters of so many of their CTAs that run at once
+    int f8_clusters[9] = {};                // clusters of so many CTAs of 8-bit floating-point layers that run at once (asked for with the first layer)
     const void* smem_ready[128] = {};       // kernels that may use all of an SM's shared memory (qtz_allow_smem)
     int smem_ready_count = 0;
     bool no_pairs = false;                  // never run layers on CTA pairs (A/B comparisons; set by QTZ_NO_PAIRS=1)
