@@ -156,32 +156,59 @@ __device__ __forceinline__ void put_y(const LinearArgs& a, int64_t row, int o, u
 // First row, among the packed tiles' rows, of half a tile of 256 weights.
 __device__ __forceinline__ int w_row(const LinearArgs& a, int col, int kb, int half) { return ((col * a.k_blocks + kb) * 2 + half) * kF8Block; }
 
-// Adds a block's products, 128 columns from `from` of tensor memory on, times s; `read` is called once they have been read out, before the
-// last of them are added.  What is held at a time is what the registers allow.
-template <typename Read>
-__device__ __forceinline__ void add_block(float (&acc)[128], uint32_t from, float s, Read read)
-{
-    uint32_t v0[32], v1[32];
-    auto take = [&](const uint32_t (&v)[32], int at) {
+// The sums of a thread: a row of x and 128 weights.  Blocks' products are read from tensor memory 64 columns at a time, what registers
+// allow, and added times the block's factor.  A block's buffer is given back before the last half is added, and the first half of the next
+// block, whose barrier was polled meanwhile, is on its way before that is done.
+struct Sums {
+    float acc[128];
+    uint32_t v0[32], v1[32];           // columns on their way
+
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int c = 0; c < 128; ++c) acc[c] = 0.f;
+    }
+    __device__ __forceinline__ void add(const uint32_t (&v)[32], int at, float s)
+    {
 #pragma unroll
         for (int c = 0; c < 32; c += 2) fma2(acc[at + c], acc[at + c + 1], __uint_as_float(v[c]), __uint_as_float(v[c + 1]), s, s);
-    };
-    tmem_ld_32x32(from, v0);
-    tmem_ld_32x32(from + 32, v1);
-    tmem_ld_wait_for(v0);
-    tmem_ld_tie(v1);
-    take(v0, 0);
-    tmem_ld_32x32(from + 64, v0);
-    take(v1, 32);
-    tmem_ld_32x32(from + 96, v1);
-    tmem_ld_wait_for(v0);
-    tmem_ld_tie(v1);
-    tc_fence_before();
-    __syncwarp();
-    read();
-    take(v0, 64);
-    take(v1, 96);
-}
+    }
+    __device__ __forceinline__ void landed()
+    {
+        tmem_ld_wait_for(v0);
+        tmem_ld_tie(v1);
+    }
+    __device__ __forceinline__ void begin(uint32_t from)
+    {
+        tmem_ld_32x32(from, v0);
+        tmem_ld_32x32(from + 32, v1);
+    }
+    // The block at `from`, whose first half was asked for.  read() gives its buffer back; where `more` holds, the next block's barrier is
+    // polled with poll() and waited for with wait(answer), and its first half asked for at `next`.  False: that wait gave up.
+    template <typename Read, typename Poll, typename Wait>
+    __device__ __forceinline__ bool block(uint32_t from, float s, bool more, uint32_t next, Read read, Poll poll, Wait wait)
+    {
+        landed();
+        add(v0, 0, s);
+        tmem_ld_32x32(from + 64, v0);
+        add(v1, 32, s);
+        tmem_ld_32x32(from + 96, v1);
+        landed();
+        tc_fence_before();
+        __syncwarp();
+        read();
+        const bool answer = more && poll();
+        add(v0, 64, s);
+        if (more) {
+            if (!wait(answer)) return false;
+            tc_fence_after();
+            tmem_ld_32x32(next, v0);
+        }
+        add(v1, 96, s);
+        if (more) tmem_ld_32x32(next + 32, v1);
+        return true;
+    }
+};
 
 // Places for the scales of blocks, and how many blocks ahead they are asked for.  A thread of the sums reads its block's factor a block
 // early, so that the loads of a block's scales are counted with the product of the block before.
@@ -404,28 +431,30 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
             const uint32_t from = tmem + (static_cast<uint32_t>(warp & 3) << 21) + half * 128;
             uint4* const out = reinterpret_cast<uint4*>(smem_raw + (base - smem_u32(smem_raw)) + S::kStages * S::kStage + (warp - 4) * kOutBytes);
             grid_dependency_wait();                    // y may be what the kernel before reads
-            float acc[128];
+            Sums sums;
             float s_next = 0.f;                        // the next block's factor: its scales are there with this block's
             int i = 0;
             for (int tile = tile0; ok && tile < a.tiles; tile += step) {
-#pragma unroll
-                for (int c = 0; c < 128; ++c) acc[c] = 0.f;
+                wait(s_done[i & 1], i >> 1 & 1);
+                if (!ok) break;
+                tc_fence_after();
+                sums.begin(from + (i & 1) * 256);
+                sums.clear();
 #pragma unroll 1
                 for (int kb = 0; kb < kbs; ++kb, ++i) {
-                    const int after = (i + 1) % kSlots;
-                    wait(s_done[i & 1], i >> 1 & 1);
-                    if (!ok) break;
-                    tc_fence_after();
                     const float s = i ? s_next : s_x[0][row_lane] * s_w[0][half];
-                    s_next = s_x[after][row_lane] * s_w[after][half];
-                    add_block(acc, from + (i & 1) * 256, s, [&]() {
-                        if (lane == 0) mbar_arrive(smem_u32(&s_free[i & 1]));
-                    });
+                    s_next = s_x[(i + 1) % kSlots][row_lane] * s_w[(i + 1) % kSlots][half];
+                    const uint32_t next_done = smem_u32(&s_done[(i + 1) & 1]), next_parity = (i + 1) >> 1 & 1;
+                    ok = sums.block(from + (i & 1) * 256, s, kb + 1 < kbs, from + ((i + 1) & 1) * 256,
+                                    [&]() { if (lane == 0) mbar_arrive(smem_u32(&s_free[i & 1])); },
+                                    [&]() { return mbar_try_wait(next_done, next_parity); },
+                                    [&](bool answer) { return mbar_wait_warp_polled(answer, next_done, next_parity, a.wait_budget, true); });
+                    if (!ok) break;
                 }
                 if (!ok) break;
                 const StreamTile at(a, tile);
-                if (a.split == 1) put_y(a, static_cast<int64_t>(at.row) * kF8Block + row_warp, at.col * kTileCols + half * 128, out, acc);
-                else if (row_warp + lane < kRows) keep_sums(acc, base, row_warp + lane, half);   // the ring is free: the cluster's only tile is done
+                if (a.split == 1) put_y(a, static_cast<int64_t>(at.row) * kF8Block + row_warp, at.col * kTileCols + half * 128, out, sums.acc);
+                else if (row_warp + lane < kRows) keep_sums(sums.acc, base, row_warp + lane, half);   // the ring is free: the cluster's only tile is done
             }
         }
         if (a.split > 1) {
@@ -606,28 +635,30 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
         const uint32_t from = tmem + (static_cast<uint32_t>(warp & 3) << 21) + half * 128;
         uint4* const out = reinterpret_cast<uint4*>(smem_raw + (base - smem_u32(smem_raw)) + kPairStages * kPairStage + (warp - 4) * kOutBytes);
         grid_dependency_wait();
+        Sums sums;
         int block = 0;
         float s_next = 0.f;                            // the next block's factor: its scales are there with this block's
         for (int tile = tile0; ok && tile < a.tiles; tile += step) {
-            float acc[128];
-#pragma unroll
-            for (int c = 0; c < 128; ++c) acc[c] = 0.f;
+            ok = mbar_wait_warp(smem_u32(&s_done[block & 1]), block >> 1 & 1, a.wait_budget, ok);
+            if (!ok) break;
+            tc_fence_after();
+            sums.begin(from + (block & 1) * 256);
+            sums.clear();
 #pragma unroll 1
             for (int kb = 0; kb < kbs; ++kb, ++block) {
-                const int slot = block % kSlots;
-                ok = mbar_wait_warp(smem_u32(&s_done[block & 1]), block >> 1 & 1, a.wait_budget, ok);
-                if (!ok) break;
-                tc_fence_after();
                 const float s = block ? s_next : s_x[0][row_lane] * s_w[0][half];
-                s_next = s_x[(slot + 1) % kSlots][row_lane] * s_w[(slot + 1) % kSlots][half];
-                add_block(acc, from + (block & 1) * 256, s, [&]() {
-                    if (lane == 0) mbar_arrive_remote_relaxed(smem_u32(&s_free[block & 1]), first);
-                });
+                s_next = s_x[(block + 1) % kSlots][row_lane] * s_w[(block + 1) % kSlots][half];
+                const uint32_t next_done = smem_u32(&s_done[(block + 1) & 1]), next_parity = (block + 1) >> 1 & 1;
+                ok = sums.block(from + (block & 1) * 256, s, kb + 1 < kbs, from + ((block + 1) & 1) * 256,
+                                [&]() { if (lane == 0) mbar_arrive_remote_relaxed(smem_u32(&s_free[block & 1]), first); },
+                                [&]() { return mbar_try_wait(next_done, next_parity); },
+                                [&](bool answer) { return mbar_wait_warp_polled(answer, next_done, next_parity, a.wait_budget, true); });
+                if (!ok) break;
             }
             if (!ok) break;
             const PairTile at(a, tile);
-            if (a.split > 1) keep_sums(acc, base, row_lane, half);   // the ring is free: the cluster's only tile is done
-            else put_y(a, (2 * static_cast<int64_t>(at.row) + side) * kF8Block + row_lane - lane, (2 * at.col + half) * kF8Block, out, acc);
+            if (a.split > 1) keep_sums(sums.acc, base, row_lane, half);   // the ring is free: the cluster's only tile is done
+            else put_y(a, (2 * static_cast<int64_t>(at.row) + side) * kF8Block + row_lane - lane, (2 * at.col + half) * kF8Block, out, sums.acc);
         }
         if (a.split > 1) {
             const PairTile at(a, tile0);

@@ -78,6 +78,13 @@ __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, lo
     return __all_sync(0xffffffffu, done) && ok;
 }
 
+// The same where the poll (`done`) was made earlier, with other work between: its answer takes about 100 cycles.
+__device__ __forceinline__ bool mbar_wait_warp_polled(bool done, uint32_t bar, uint32_t parity, long long budget, bool ok)
+{
+    if (!done && ok) done = mbar_wait(bar, parity, budget);
+    return __all_sync(0xffffffffu, done) && ok;
+}
+
 // True in exactly one lane of a converged warp (the same lane every time).
 __device__ __forceinline__ bool elect_one()
 {
