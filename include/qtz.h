@@ -536,7 +536,9 @@ QTZ_API qtz_status qtz_f8_quantize_weights(qtz_handle h, const void* w_dev, int6
                                            uint8_t* codes_dev, float* scales_dev, void* stream);
 
 /* y[r][o] = sum_b x_scale[r][b] w_scale[o / 128][b] sum_{k in b} x[r][k] w[o][k] + bias[o]
- * Products of codes are exact, their sum over a block of 128 columns and the sum over blocks are held in fp32, and y is rounded once.
+ * Products of codes are exact, their sum over a block of 128 columns and the sum over blocks are held in fp32 (of 32 columns that are
+ * summed together, what lies 2^-25 below the largest product is cut off), and y is rounded once.  Results are the same whenever
+ * repeated; a row's do not depend on the other rows, but may differ in the last places with the number of rows in the call.
  * A NaN code gives NaN in its row (of x) or column (of w).  Scales are finite, and so are the products of two that meet.
  *
  * One-time preparation: copies codes (rows codes_stride bytes apart, no alignment rule), scales and bias (n values of type
@@ -547,7 +549,9 @@ QTZ_API qtz_status qtz_f8_linear_create(qtz_handle h, int32_t n, int32_t k, cons
 QTZ_API qtz_status qtz_f8_linear_destroy(qtz_f8_linear_plan p);
 /* x: `rows` rows of k codes, codes_stride bytes apart, base and stride multiples of 16 (the stride of a single row does not matter);
  * scales: element (r, b) at r * scales_row_stride + b * scales_block_stride; y: rows of n values of type `ftype` (QTZ_F32, QTZ_F16 or
- * QTZ_BF16), y_stride elements apart, no alignment rule.  rows == 0 does nothing.  Asynchronous on `stream`.         */
+ * QTZ_BF16), y_stride elements apart, no alignment rule (rows that start on 16 bytes are written faster).  rows == 0 does nothing.
+ * Asynchronous on `stream`; a layer has no scratch, so that several streams may use it at once.  QTZ_ERR_TOO_LARGE where rows * n * k
+ * passes 2^51.                                                                                                     */
 QTZ_API qtz_status qtz_f8_linear(qtz_f8_linear_plan p, const uint8_t* codes_dev, int64_t codes_stride, const float* scales_dev,
                                  int64_t scales_row_stride, int64_t scales_block_stride, int64_t rows, void* y_dev, int64_t y_stride,
                                  int32_t ftype, void* stream);

@@ -8,6 +8,9 @@
 // What bounds them: bytes.  Every value is read once, kept in registers between the row's sum of squares, the block's maximum and the
 // code, and written once.  A thread holds 32 bytes of neighbouring columns, so that 8 or 16 lanes hold a block and its maximum takes three or
 // four shuffles; warps and CTAs go over several rows and have the next row's values on their way while they work on one.
+// Measured: norm of 16384 rows of 8192 with residual, bf16, 144 us, 6.5 TB/s, the copy rate (with nothing on its way behind the row at work
+// 248); gated quantizer 8192 x 28672 180 us, 6.5 TB/s (with 32 instructions a value instead of about 16 409), plain 111; 8192 x 10001
+// gated 72 us, 5.7 TB/s; one row of 2048 1.9 us.
 #include "qtz_f8.cuh"
 #include "qtz_ptx.cuh"
 

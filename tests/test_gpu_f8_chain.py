@@ -115,6 +115,23 @@ def test_rows_of_a_batch_do_not_depend_on_each_other(handle):
     assert torch.equal(got[:40], want[:40]) and bool(got[40:].isnan().all())
 
 
+@pytest.mark.parametrize("rows", [2, 90, 400])
+def test_a_layer_on_two_streams_at_once(handle, rows):
+    g = torch.Generator("cuda").manual_seed(rows)
+    plan = handle.f8_linear_create(*handle.f8_quantize_weights(torch.randn(2000, 1500, device="cuda", generator=g)))
+    inputs = [handle.f8_quantize(torch.randn(rows, 1500, device="cuda", generator=g)[:, :1500]) for _ in range(2)]
+    want = [plan(*i) for i in inputs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in inputs]
+    got = [[], []]
+    for _ in range(20):
+        for i, (stream, one) in enumerate(zip(streams, inputs)):
+            with torch.cuda.stream(stream):
+                got[i].append(plan(*one))
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, want[i]) for i in range(2) for y in got[i])
+
+
 def test_blocks_of_the_example():
     got = decode.main(["--requests", "4", "--prompt", "150", "--steps", "4", "--layers", "2", "--hidden", "512", "--q-heads", "8", "--kv-heads", "2",
                        "--head-dim", "64", "--ffn", "1376"])
