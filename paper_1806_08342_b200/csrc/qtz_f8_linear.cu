@@ -10,15 +10,17 @@
 // What bounds it.  Few rows: the weights' bytes.  Many: the tensor cores take 512 cycles for a block of a pair's 256 x 256 tile, reading
 // it from tensor memory and adding it takes the eight warps of a CTA about as long, half of the fp32 pipe's time, and the two work on
 // alternate buffers.  Measured, in cycles a block: products and loads alone 520, with the reading 548, with the sums 700 to 800 (the
-// buffer comes back after the first half has been added: registers hold no more), stores of y 75; the tensor pipe is 64 % busy.  Steps
+// buffer comes back after the first half has been added: registers hold no more); the tensor pipe is 64 % busy.  Steps
 // that counted: arrivals at the other CTA without release order (the fence took 1000 cycles a block); one warp to load, one for scales,
 // two for products, so that no wait stands behind another; scales counted on the product's own barrier; the next block's barrier polled
-// and its first half asked for behind this block's sums; rows of y written through shared memory; fp32 operations in pairs.  Tried and
+// and its first half asked for behind this block's sums; rows of y that leave shared memory by copies while the next tile begins (stores by
+// the threads: 8192 rows 1585 us instead of 1535, 2048 rows through 8192 x 512 18.8 instead of 15.9); fp32 operations in pairs.  Tried and
 // left: halves of 128 columns with four buffers (the same), single CTAs of 128 x 256 (1090 cycles: shared memory brings and reads 192
-// bytes a clock), tiles dealt out block by block with parts in global memory (128 KB a part: 33 -> 55 us for 256 x 8192 -> 10240).
-// Measured, device time: 8192 rows through 28672 x 8192 1.59 to 1.64 ms, 2.4 PFLOP/s, at 1.5 GHz under the power cap; 1777 rows
-// through 6144 x 4096 48.4 us (three rounds of 74 pairs for 2.3 of tiles); 256 rows through 10240 x 8192 33 us (40 tiles for 74 pairs);
-// 45 rows through 5003 x 10001 12.2 us; one row through 28672 x 8192 36.8 us, 6.4 TB/s; one row through 1000 x 1024 4.1 us.
+// bytes a clock), tiles dealt out block by block with parts in global memory (128 KB a part: 33 -> 55 us for 256 x 8192 -> 10240),
+// a launch of clusters for the tiles beyond whole rounds (a launch and a join cost 10 us: 777 rows through 11008 x 4096 49.8 -> 53.0).
+// Measured, device time: 8192 rows through 28672 x 8192 1.53 ms, 2.5 PFLOP/s, under the power cap (1.8 ms in a long run); 1777 rows
+// through 6144 x 4096 46.6 us (three rounds of 74 pairs for 2.3 of tiles); 256 rows through 10240 x 8192 32 us (40 tiles for 74 pairs);
+// 45 rows through 5003 x 10001 12.1 us; one row through 28672 x 8192 36.8 us, 6.4 TB/s; one row through 1000 x 1024 4.1 us.
 #include <new>
 
 #include "qtz_f8.cuh"
@@ -121,16 +123,16 @@ __device__ __forceinline__ uint4 pack16(const float* v)
 
 constexpr int kOutBytes = 2048;        // of a warp's values on their way out: 32 rows of 64 bytes
 
-// A warp's `rows` (at most 32) rows of kCols columns, of which `cols` exist; lane l holds row l, row r goes to to + r * stride.  64 bytes of
+// A warp's `rows` (at most 32) rows of 128 columns, of which `cols` exist; lane l holds row l, row r goes to to + r * stride.  64 bytes of
 // each row at a time cross through `out`, so that neighbouring lanes write neighbouring values; pieces of 16 bytes are shifted by row, for
 // the banks.  vector: rows start on 16 bytes.
-template <typename T, int kCols>
-__device__ __forceinline__ void put_rows(T* to, int64_t stride, int rows, int cols, bool vector, uint4* out, const float (&acc)[kCols])
+template <typename T>
+__device__ __forceinline__ void put_rows(T* to, int64_t stride, int rows, int cols, bool vector, uint4* out, const float (&acc)[128])
 {
     constexpr int kPer = 16 / sizeof(T), kStep = 64 / sizeof(T);
     const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int c0 = 0; c0 < kCols; c0 += kStep) {
+    for (int c0 = 0; c0 < 128; c0 += kStep) {
         const int here = min(kStep, cols - c0);
         __syncwarp();
 #pragma unroll
@@ -155,19 +157,45 @@ __device__ __forceinline__ void put_rows(T* to, int64_t stride, int rows, int co
     }
 }
 
-// The same into y, from (row, o) on, with the bias.
-template <int kCols>
-__device__ __forceinline__ void put_y(const LinearArgs& a, int64_t row, int o, uint4* out, float (&acc)[kCols])
+__device__ __forceinline__ void add_bias(const LinearArgs& a, int o, float (&acc)[128])
+{
+    if (!a.bias) return;
+#pragma unroll
+    for (int c = 0; c < 128; ++c) acc[c] += bias_of(a, o + c);
+}
+
+// The same into y, from (row, o) on.
+__device__ __forceinline__ void put_y(const LinearArgs& a, int64_t row, int o, uint4* out, const float (&acc)[128])
 {
     const int rows = static_cast<int>(min(static_cast<int64_t>(32), a.rows - row)), cols = a.n - o;
-    if (a.bias) {
-#pragma unroll
-        for (int c = 0; c < kCols; ++c) acc[c] += bias_of(a, o + c);
-    }
     const int64_t at = row * a.y_stride + o;
     if (a.ftype == QTZ_BF16) put_rows(static_cast<__nv_bfloat16*>(a.y) + at, a.y_stride, rows, cols, a.vector, out, acc);
     else if (a.ftype == QTZ_F16) put_rows(static_cast<__half*>(a.y) + at, a.y_stride, rows, cols, a.vector, out, acc);
     else put_rows(static_cast<float*>(a.y) + at, a.y_stride, rows, cols, a.vector, out, acc);
+}
+
+// 32 rows of 128 columns where rows of y start on 16 bytes, by copies that run on behind the caller: 64 bytes of each row at a time in the
+// order of a 64-byte swizzle, in two places of `out` in turn.  Rows beyond the last the tensor map leaves out; of columns it would write whole
+// pieces of 16 bytes.
+template <typename T>
+__device__ __forceinline__ void send_rows(const CUtensorMap& y_map, int64_t row, int o, uint32_t out, const float (&acc)[128])
+{
+    constexpr int kPer = 16 / sizeof(T), kStep = 64 / sizeof(T);
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int c0 = 0; c0 < 128; c0 += kStep) {
+        const uint32_t to = out + c0 / kStep % 2 * kOutBytes;
+        if (lane == 0) tma_store_wait_read_n<1>();
+        __syncwarp();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) sts128(to + lane * 64 + (q ^ (lane >> 1 & 3)) * 16, pack16<T>(acc + c0 + q * kPer));
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+            tma_store_2d(&y_map, to, (o + c0) * static_cast<int>(sizeof(T)), static_cast<int>(row));
+            tma_store_commit();
+        }
+    }
 }
 
 // First row, among the packed tiles' rows, of half a tile of 256 weights.
@@ -471,8 +499,11 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
                 }
                 if (!ok) break;
                 const StreamTile at(a, tile);
-                if (a.split == 1) put_y(a, static_cast<int64_t>(at.row) * kF8Block + row_warp, at.col * kTileCols + half * 128, out, sums.acc);
-                else if (row_warp + lane < kRows) keep_sums(sums.acc, base, row_warp + lane, half);   // the ring is free: the cluster's only tile is done
+                if (a.split == 1) {
+                    const int o = at.col * kTileCols + half * 128;
+                    add_bias(a, o, sums.acc);
+                    put_y(a, static_cast<int64_t>(at.row) * kF8Block + row_warp, o, out, sums.acc);
+                } else if (row_warp + lane < kRows) keep_sums(sums.acc, base, row_warp + lane, half);   // the ring is free: the cluster's only tile is done
             }
         }
         if (a.split > 1) {
@@ -498,7 +529,7 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
 // tensor memory, twice, so that one block of 128 columns is multiplied while the sums of the one before are taken.  A thread owns a row
 // of x and half of the columns, which share a scale of the weights: one factor a thread and block.
 constexpr int kPairStage = 2 * kTileBytes;
-constexpr int kPairStages = 6;          // what the rows on their way to y leave room for
+constexpr int kPairStages = 5;          // what the rows on their way to y leave room for; six are no faster
 constexpr int kBand = 16;              // row tiles that the pairs work on side by side, for the L2
 
 struct PairTile {
@@ -513,7 +544,8 @@ struct PairTile {
 };
 
 __global__ void __launch_bounds__(kThreads, 1)
-pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map)
+pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map,
+            const __grid_constant__ CUtensorMap y_map)
 {
     extern __shared__ uint8_t smem_raw[];              // the ring: a tile of x, a tile of weights
     __shared__ float s_x[kSlots][kF8Block], s_w[kSlots][2];            // scales
@@ -524,6 +556,7 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
     if (tid == 0) {
         prefetch_tensormap(&w_map);
         prefetch_tensormap(&x_map);
+        if (a.vector) prefetch_tensormap(&y_map);
         for (int i = 0; i < kPairStages; ++i) {
             mbar_init(smem_u32(&s_full[i]), 1);
             mbar_init(smem_u32(&s_empty[i]), 1);
@@ -652,7 +685,7 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kMany));
         const int half = (warp - 4) >> 2, row_lane = (warp & 3) * 32 + lane;
         const uint32_t from = tmem + (static_cast<uint32_t>(warp & 3) << 21) + half * 128;
-        uint4* const out = reinterpret_cast<uint4*>(smem_raw + (base - smem_u32(smem_raw)) + kPairStages * kPairStage + (warp - 4) * kOutBytes);
+        uint4* const out = reinterpret_cast<uint4*>(smem_raw + (base - smem_u32(smem_raw)) + kPairStages * kPairStage + (warp - 4) * 2 * kOutBytes);
         grid_dependency_wait();
         Sums sums;
         int block = 0;
@@ -676,9 +709,27 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
             }
             if (!ok) break;
             const PairTile at(a, tile);
-            if (a.split > 1) keep_sums(sums.acc, base, row_lane, half);   // the ring is free: the cluster's only tile is done
-            else put_y(a, (2 * static_cast<int64_t>(at.row) + side) * kF8Block + row_lane - lane, (2 * at.col + half) * kF8Block, out, sums.acc);
+            if (a.split > 1) {
+                keep_sums(sums.acc, base, row_lane, half);     // the ring is free: the cluster's only tile is done
+            } else {
+                const int64_t row = (2 * static_cast<int64_t>(at.row) + side) * kF8Block + row_lane - lane;
+                const int o = (2 * at.col + half) * kF8Block;
+                if (row >= a.rows || o >= a.n) continue;
+                add_bias(a, o, sums.acc);
+                if (!a.vector || o + kF8Block > a.n) {
+                    if (lane == 0) tma_store_wait_read();
+                    put_y(a, row, o, out, sums.acc);
+                } else if (a.ftype == QTZ_BF16) {
+                    send_rows<__nv_bfloat16>(y_map, row, o, smem_u32(out), sums.acc);
+                } else if (a.ftype == QTZ_F16) {
+                    send_rows<__half>(y_map, row, o, smem_u32(out), sums.acc);
+                } else {
+                    send_rows<float>(y_map, row, o, smem_u32(out), sums.acc);
+                }
+            }
         }
+        if (lane == 0) tma_store_wait_all();
+        __syncwarp();
         if (a.split > 1) {
             const PairTile at(a, tile0);
             cluster_sync();                            // the cluster's sums are there
@@ -727,8 +778,8 @@ qtz_status learn_clusters(qtz_ctx* h)
     return QTZ_OK;
 }
 
-template <typename K>
-qtz_status launch(qtz_ctx* h, K* kernel, const LinearArgs& a, int cluster, int ctas, int smem, cudaStream_t st, const CUtensorMap& w_map, const CUtensorMap& x_map)
+template <typename K, typename... M>
+qtz_status launch(qtz_ctx* h, K* kernel, const LinearArgs& a, int cluster, int ctas, int smem, cudaStream_t st, const M&... maps)
 {
     const qtz_status s = qtz_allow_smem(h, kernel);
     if (s != QTZ_OK) return s;
@@ -745,7 +796,7 @@ qtz_status launch(qtz_ctx* h, K* kernel, const LinearArgs& a, int cluster, int c
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = 2;
-    QTZ_CUDA(h, cudaLaunchKernelEx(&cfg, kernel, a, w_map, x_map));
+    QTZ_CUDA(h, cudaLaunchKernelEx(&cfg, kernel, a, maps...));
     return QTZ_OK;
 }
 
@@ -769,11 +820,16 @@ int most_split(const qtz_ctx* h, int64_t tiles, int each, int k_blocks)
 
 qtz_status launch_pair(qtz_f8_layer* p, LinearArgs& a, const CUtensorMap& x_map, cudaStream_t st)
 {
+    const int size = a.ftype == QTZ_F32 ? 4 : 2;
+    const uint64_t dims[2] = {static_cast<uint64_t>(a.n) * size, static_cast<uint64_t>(a.rows)}, strides[1] = {static_cast<uint64_t>(a.y_stride) * size};
+    const uint32_t box[2] = {64, 32};
+    CUtensorMap y_map{};
+    if (a.vector && !qtz_encode_u8_map(&y_map, a.y, 2, dims, strides, box, 64)) a.vector = 0;   // rows too far apart for one
     qtz_ctx* h = p->h;
     a.row_tiles = static_cast<int32_t>((a.rows + 255) / 256);
     a.tiles = a.row_tiles * ((a.n_tiles + 1) / 2);
     const int pairs = h->num_sms / 2;
-    return launch(h, pair_kernel, a, 2 * a.split, 2 * a.split * (a.split > 1 || a.tiles < pairs ? a.tiles : pairs), 1024 + kPairStages * kPairStage + 8 * kOutBytes, st, p->w_map, x_map);
+    return launch(h, pair_kernel, a, 2 * a.split, 2 * a.split * (a.split > 1 || a.tiles < pairs ? a.tiles : pairs), 1024 + kPairStages * kPairStage + 8 * 2 * kOutBytes, st, p->w_map, x_map, y_map);
 }
 
 }  // namespace

@@ -259,6 +259,10 @@ __device__ __forceinline__ void sts128(uint32_t to, float4 v)
 {
     asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(to), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
+__device__ __forceinline__ void sts128(uint32_t to, uint4 v)
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
 __device__ __forceinline__ float4 lds_cluster(uint32_t from)
 {
     float4 v;
@@ -441,13 +445,6 @@ __device__ __forceinline__ void tmem_ld_32x4(uint32_t taddr, uint32_t (&v)[16])
 }
 
 // Waits for this thread's loads; what the last one brought is not touched before it.
-__device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&v)[16])
-{
-    asm volatile("tcgen05.wait::ld.sync.aligned;"
-                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
-                   "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
-                 :: "memory");
-}
 __device__ __forceinline__ void tmem_ld_wait_for(uint32_t (&v)[32])
 {
     asm volatile("tcgen05.wait::ld.sync.aligned;"

@@ -50,3 +50,22 @@ def test_codes_beyond_32_bits(hq):
     plan = hq.f8_linear_create(w, ws)
     assert torch.equal(plan(x.view(qtz.E4M3), xs), plan(small, xs))
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("rows,n,k", [(300, 77, 100), (2305, 2087, 260), (4999, 1288, 128), (1290, 5003, 640)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("pad", [0, 16])
+def test_whole_tiles_leave_what_lies_beside_y(hq, rows, n, k, dtype, pad):
+    """Pairs with a tile or several each; rows of y that start on 16 bytes and end anywhere, and rows that do not."""
+    x, xs, w, ws, bias = make(rows, n, k, n)
+    plan = hq.f8_linear_create(w, ws, bias=bias)
+    around = torch.full((rows + 2, -(-n // 8) * 8 + pad + (0 if pad else 1)), 7.0, device="cuda", dtype=dtype)
+    y = around[1:-1, pad // 2:pad // 2 + n]
+    plan(x, xs, out=y)
+    check(y, x, xs, w, ws, bias, rows=[0, 31, 127, 128, 255, 256, rows // 2, rows - 2, rows - 1])
+    few = torch.cat([plan(x[r:r + 100], xs[r:r + 100], dtype=dtype) for r in range(0, rows, 100)])
+    off = (y.double() - few.double()).abs()
+    assert bool((off <= 2.0 ** -7 * few.double().abs() + 1e-3 * few.double().abs().max()).all())   # every row is in its place
+    y.fill_(7)
+    assert bool((around == 7).all())                                            # nothing beside y was written
+    assert hq.device_status() == (0, 0)
