@@ -44,19 +44,28 @@ using namespace qtz_ptx;
 struct PackArgs {
     const uint8_t* codes;
     int64_t stride;
-    int32_t n, k, k_blocks;
+    int32_t n, k, k_blocks, vector;
     uint8_t* tiles;
 };
 
-// A CTA a block of 128 x 128.
+// A CTA a block of 128 x 128; rows that start on 16 bytes (`vector`) are read so.
 __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackArgs a)
 {
     const int64_t place = (static_cast<int64_t>(blockIdx.y / 2) * a.k_blocks + blockIdx.x) * 2 + blockIdx.y % 2;
-    uint8_t* const tile = a.tiles + place * (kF8Block * kF8Block);
-    for (int i = threadIdx.x; i < kF8Block * kF8Block; i += 256) {
-        const int64_t row = static_cast<int64_t>(blockIdx.y) * kF8Block + i / kF8Block;
-        const int col = blockIdx.x * kF8Block + i % kF8Block;
-        tile[i] = row < a.n && col < a.k ? a.codes[row * a.stride + col] : 0;
+    uint4* const tile = reinterpret_cast<uint4*>(a.tiles + place * (kF8Block * kF8Block));
+    for (int i = threadIdx.x; i < kF8Block * kF8Block / 16; i += 256) {
+        const int64_t row = static_cast<int64_t>(blockIdx.y) * kF8Block + i / 8;
+        const int col = blockIdx.x * kF8Block + i % 8 * 16, valid = row < a.n ? a.k - col : 0;
+        const uint8_t* const from = a.codes + row * a.stride + col;
+        uint32_t w[4] = {};
+        if (a.vector && valid >= 16) {
+            tile[i] = *reinterpret_cast<const uint4*>(from);
+            continue;
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            if (e < valid) w[e / 4] |= static_cast<uint32_t>(from[e]) << (e % 4 * 8);
+        tile[i] = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 
@@ -876,7 +885,7 @@ extern "C" qtz_status qtz_f8_linear_create(qtz_handle h, int32_t n, int32_t k, c
         e = cudaGetLastError();
     }
     if (e == cudaSuccess) {
-        const PackArgs a{codes_dev, codes_stride, n, k, p->k_blocks, p->tiles};
+        const PackArgs a{codes_dev, codes_stride, n, k, p->k_blocks, qtz_aligned16(codes_dev) && (n == 1 || codes_stride % 16 == 0), p->tiles};
         pack_kernel<<<dim3(static_cast<unsigned>(k_blocks), static_cast<unsigned>(n_tiles)), 256, 0, st>>>(a);
         e = cudaGetLastError();
     }
