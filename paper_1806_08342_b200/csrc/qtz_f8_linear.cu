@@ -10,7 +10,7 @@
 // What bounds it.  Few rows: the weights' bytes.  Many: the tensor cores take 512 cycles for a block of a pair's 256 x 256 tile, reading
 // it from tensor memory and adding it takes the eight warps of a CTA about as long, half of the fp32 pipe's time, and the two work on
 // alternate buffers.  Measured, in cycles a block: products and loads alone 520, with the reading 548, with the sums 700 to 800 (the
-// buffer comes back after the first half has been added: registers hold no more); the tensor pipe is 64 % busy.  Steps
+// buffer comes back after the first half has been added: registers hold no more); the tensor pipe is 68 % busy.  Steps
 // that counted: arrivals at the other CTA without release order (the fence took 1000 cycles a block); one warp to load, one for scales,
 // two for products, so that no wait stands behind another; scales counted on the product's own barrier; the next block's barrier polled
 // and its first half asked for behind this block's sums; rows of y that leave shared memory by copies while the next tile begins (stores by
