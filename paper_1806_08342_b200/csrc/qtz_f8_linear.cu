@@ -19,8 +19,8 @@
 // bytes a clock), tiles dealt out block by block with parts in global memory (128 KB a part: 33 -> 55 us for 256 x 8192 -> 10240),
 // a launch of clusters for the tiles beyond whole rounds (a launch and a join cost 10 us: 777 rows through 11008 x 4096 49.8 -> 53.0).
 // Measured, device time: 8192 rows through 28672 x 8192 1.53 ms, 2.5 PFLOP/s, under the power cap (1.8 ms in a long run); 1777 rows
-// through 6144 x 4096 46.6 us (three rounds of 74 pairs for 2.3 of tiles); 256 rows through 10240 x 8192 32 us (40 tiles for 74 pairs);
-// 45 rows through 5003 x 10001 12.1 us; one row through 28672 x 8192 36.8 us, 6.4 TB/s; one row through 1000 x 1024 4.1 us.
+// through 6144 x 4096 46.6 us (three rounds of 74 pairs for 2.3 of tiles); 256 rows through 10240 x 8192 28 us (54 tiles of 192
+// weights for 74 pairs); 45 rows through 5003 x 10001 12.1 us; one row through 28672 x 8192 36.8 us, 6.4 TB/s; one row through 1000 x 1024 4.1 us.
 #include <new>
 
 #include "qtz_f8.cuh"
@@ -35,7 +35,7 @@ struct qtz_f8_layer {
     uint8_t* tiles = nullptr;          // [n_tiles / 2, rounded up][k_blocks][256][128] codes, zeros beyond k; what lies beyond n is not used
     float* scales = nullptr;           // [n_tiles][k_blocks], behind the tiles in the same allocation
     float* bias = nullptr;             // [n], behind the scales; null: none
-    CUtensorMap w_map{};               // the tiles as rows of 128 bytes, 128 rows at a time
+    CUtensorMap w_map{}, w_map_32{};   // the tiles as rows of 128 bytes, 128 and 32 rows at a time
 };
 
 namespace {
@@ -132,16 +132,16 @@ __device__ __forceinline__ uint4 pack16(const float* v)
 
 constexpr int kOutBytes = 2048;        // of a warp's values on their way out: 32 rows of 64 bytes
 
-// A warp's `rows` (at most 32) rows of 128 columns, of which `cols` exist; lane l holds row l, row r goes to to + r * stride.  64 bytes of
+// A warp's `rows` (at most 32) rows of kCols columns, of which `cols` exist; lane l holds row l, row r goes to to + r * stride.  64 bytes of
 // each row at a time cross through `out`, so that neighbouring lanes write neighbouring values; pieces of 16 bytes are shifted by row, for
 // the banks.  vector: rows start on 16 bytes.
-template <typename T>
-__device__ __forceinline__ void put_rows(T* to, int64_t stride, int rows, int cols, bool vector, uint4* out, const float (&acc)[128])
+template <typename T, int kCols>
+__device__ __forceinline__ void put_rows(T* to, int64_t stride, int rows, int cols, bool vector, uint4* out, const float (&acc)[kCols])
 {
     constexpr int kPer = 16 / sizeof(T), kStep = 64 / sizeof(T);
     const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int c0 = 0; c0 < 128; c0 += kStep) {
+    for (int c0 = 0; c0 < kCols; c0 += kStep) {
         const int here = min(kStep, cols - c0);
         __syncwarp();
 #pragma unroll
@@ -166,15 +166,17 @@ __device__ __forceinline__ void put_rows(T* to, int64_t stride, int rows, int co
     }
 }
 
-__device__ __forceinline__ void add_bias(const LinearArgs& a, int o, float (&acc)[128])
+template <int kCols>
+__device__ __forceinline__ void add_bias(const LinearArgs& a, int o, float (&acc)[kCols])
 {
     if (!a.bias) return;
 #pragma unroll
-    for (int c = 0; c < 128; ++c) acc[c] += bias_of(a, o + c);
+    for (int c = 0; c < kCols; ++c) acc[c] += bias_of(a, o + c);
 }
 
 // The same into y, from (row, o) on.
-__device__ __forceinline__ void put_y(const LinearArgs& a, int64_t row, int o, uint4* out, const float (&acc)[128])
+template <int kCols>
+__device__ __forceinline__ void put_y(const LinearArgs& a, int64_t row, int o, uint4* out, const float (&acc)[kCols])
 {
     const int rows = static_cast<int>(min(static_cast<int64_t>(32), a.rows - row)), cols = a.n - o;
     const int64_t at = row * a.y_stride + o;
@@ -183,16 +185,16 @@ __device__ __forceinline__ void put_y(const LinearArgs& a, int64_t row, int o, u
     else put_rows(static_cast<float*>(a.y) + at, a.y_stride, rows, cols, a.vector, out, acc);
 }
 
-// 32 rows of 128 columns where rows of y start on 16 bytes, by copies that run on behind the caller: 64 bytes of each row at a time in the
+// 32 rows of kCols columns where rows of y start on 16 bytes, by copies that run on behind the caller: 64 bytes of each row at a time in the
 // order of a 64-byte swizzle, in two places of `out` in turn.  Rows beyond the last the tensor map leaves out; of columns it would write whole
 // pieces of 16 bytes.
-template <typename T>
-__device__ __forceinline__ void send_rows(const CUtensorMap& y_map, int64_t row, int o, uint32_t out, const float (&acc)[128])
+template <typename T, int kCols>
+__device__ __forceinline__ void send_rows(const CUtensorMap& y_map, int64_t row, int o, uint32_t out, const float (&acc)[kCols])
 {
     constexpr int kPer = 16 / sizeof(T), kStep = 64 / sizeof(T);
     const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int c0 = 0; c0 < 128; c0 += kStep) {
+    for (int c0 = 0; c0 < kCols; c0 += kStep) {
         const uint32_t to = out + c0 / kStep % 2 * kOutBytes;
         if (lane == 0) tma_store_wait_read_n<1>();
         __syncwarp();
@@ -210,17 +212,20 @@ __device__ __forceinline__ void send_rows(const CUtensorMap& y_map, int64_t row,
 // First row, among the packed tiles' rows, of half a tile of 256 weights.
 __device__ __forceinline__ int w_row(const LinearArgs& a, int col, int kb, int half) { return ((col * a.k_blocks + kb) * 2 + half) * kF8Block; }
 
-// The sums of a thread: a row of x and 128 weights.  Blocks' products are read from tensor memory 64 columns at a time, what registers
-// allow, and added times the block's factor.  A block's buffer is given back before the last half is added, and the first half of the next
-// block, whose barrier was polled meanwhile, is on its way before that is done.
+// The sums of a thread: a row of x and kCols weights.  Blocks' products are read from tensor memory as far as registers allow, 96 columns
+// at once or 128 in halves, and added times the block's factor.  A block's buffer is given back when the last of them have been read, and the
+// next block's first columns, whose barrier was polled meanwhile, are on their way before those are added.
+template <int kCols>
 struct Sums {
-    float acc[128];
-    uint32_t v0[32], v1[32];           // columns on their way
+    static_assert(kCols == 96 || kCols == 128, "");
+    static constexpr int kLate = kCols == 128 ? 64 : 0;                // the first columns that are added after the buffer was given back
+    float acc[kCols];
+    uint32_t v0[32], v1[32], v2[kCols == 96 ? 32 : 1];                 // columns on their way
 
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
-        for (int c = 0; c < 128; ++c) acc[c] = 0.f;
+        for (int c = 0; c < kCols; ++c) acc[c] = 0.f;
     }
     __device__ __forceinline__ void add(const uint32_t (&v)[32], int at, float s)
     {
@@ -231,35 +236,44 @@ struct Sums {
     {
         tmem_ld_wait_for(v0);
         tmem_ld_tie(v1);
+        if constexpr (kCols == 96) tmem_ld_tie(v2);
     }
     __device__ __forceinline__ void begin(uint32_t from)
     {
         tmem_ld_32x32(from, v0);
         tmem_ld_32x32(from + 32, v1);
+        if constexpr (kCols == 96) tmem_ld_32x32(from + 64, v2);
     }
-    // The block at `from`, whose first half was asked for.  read() gives its buffer back; where `more` holds, the next block's barrier is
-    // polled with poll() and waited for with wait(answer), and its first half asked for at `next`.  False: that wait gave up.
-    template <typename Read, typename Poll, typename Wait>
-    __device__ __forceinline__ bool block(uint32_t from, float s, bool more, uint32_t next, Read read, Poll poll, Wait wait)
+    // The block at `from`, whose first columns were asked for; factor(g): of columns 32 g on.  read() gives its buffer back; where `more`
+    // holds, the next block's barrier is polled with poll() and waited for with wait(answer), and its first columns asked for at `next`.
+    // False: that wait gave up.
+    template <typename Factor, typename Read, typename Poll, typename Wait>
+    __device__ __forceinline__ bool block(uint32_t from, Factor factor, bool more, uint32_t next, Read read, Poll poll, Wait wait)
     {
         landed();
-        add(v0, 0, s);
-        tmem_ld_32x32(from + 64, v0);
-        add(v1, 32, s);
-        tmem_ld_32x32(from + 96, v1);
-        landed();
+        if constexpr (kLate > 0) {
+            add(v0, 0, factor(0));
+            tmem_ld_32x32(from + 64, v0);
+            add(v1, 32, factor(1));
+            tmem_ld_32x32(from + 96, v1);
+            landed();
+        }
         tc_fence_before();
         __syncwarp();
         read();
         const bool answer = more && poll();
-        add(v0, 64, s);
+        add(v0, kLate, factor(kLate / 32));
         if (more) {
             if (!wait(answer)) return false;
             tc_fence_after();
             tmem_ld_32x32(next, v0);
         }
-        add(v1, 96, s);
+        add(v1, kLate + 32, factor(kLate / 32 + 1));
         if (more) tmem_ld_32x32(next + 32, v1);
+        if constexpr (kCols == 96) {
+            add(v2, 64, factor(2));
+            if (more) tmem_ld_32x32(next + 64, v2);
+        }
         return true;
     }
 };
@@ -486,7 +500,7 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
             const uint32_t from = tmem + (static_cast<uint32_t>(warp & 3) << 21) + half * 128;
             uint4* const out = reinterpret_cast<uint4*>(smem_raw + (base - smem_u32(smem_raw)) + S::kStages * S::kStage + (warp - 4) * kOutBytes);
             grid_dependency_wait();                    // y may be what the kernel before reads
-            Sums sums;
+            Sums<128> sums;
             float s_next = 0.f;                        // the next block's factor: its scales are there with this block's
             int i = 0;
             for (int tile = tile0; ok && tile < a.tiles; tile += step) {
@@ -500,7 +514,7 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
                     const float s = i ? s_next : s_x[0][row_lane] * s_w[0][half];
                     s_next = s_x[(i + 1) % kSlots][row_lane] * s_w[(i + 1) % kSlots][half];
                     const uint32_t next_done = smem_u32(&s_done[(i + 1) & 1]), next_parity = (i + 1) >> 1 & 1;
-                    ok = sums.block(from + (i & 1) * 256, s, kb + 1 < kbs, from + ((i + 1) & 1) * 256,
+                    ok = sums.block(from + (i & 1) * 256, [&](int) { return s; }, kb + 1 < kbs, from + ((i + 1) & 1) * 256,
                                     [&]() { if (lane == 0) mbar_arrive(smem_u32(&s_free[i & 1])); },
                                     [&]() { return mbar_try_wait(next_done, next_parity); },
                                     [&](bool answer) { return mbar_wait_warp_polled(answer, next_done, next_parity, a.wait_budget, true); });
@@ -533,30 +547,41 @@ stream_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUte
     }
 }
 
-// ---- many rows: CTA pairs on tiles of 256 rows of x and 256 weights ----
-// Each CTA of a pair holds 128 of the rows and 128 of the weights; its half of the product, 128 rows x 256 columns, lies in its own
+// ---- many rows: CTA pairs on tiles of 256 rows of x and kCols weights ----
+// Each CTA of a pair holds 128 of the rows and half of the weights; its half of the product, 128 rows x kCols columns, lies in its own
 // tensor memory, twice, so that one block of 128 columns is multiplied while the sums of the one before are taken.  A thread owns a row
-// of x and half of the columns, which share a scale of the weights: one factor a thread and block.
-constexpr int kPairStage = 2 * kTileBytes;
-constexpr int kPairStages = 5;          // what the rows on their way to y leave room for; six are no faster
+// of x and half of the columns.  Of 256 these share a scale of the weights: one factor a thread and block.  A tile of 192 begins with a
+// scale or in the middle of one, and meets two.
+template <int kCols>
+struct Pair {
+    static constexpr int kHalf = kCols / 2, kStage = kTileBytes + kHalf * kF8Block;
+    static constexpr int kStages = kCols == 256 ? 5 : 6;              // what the rows on their way to y leave room for
+    static constexpr int kSmem = 1024 + kStages * kStage + 8 * 2 * kOutBytes;
+    // registers of a thread; those of 96 columns are all read at once
+    static constexpr int kFewRegs = kCols == 256 ? kFew : 56, kManyRegs = kCols == 256 ? kMany : 224;
+    static_assert(4 * 32 * kFewRegs + 8 * 32 * kManyRegs <= kThreads * kLaunchRegs, "more registers than the CTA was launched with");
+};
 constexpr int kBand = 16;              // row tiles that the pairs work on side by side, for the L2
 
 struct PairTile {
-    int row, col;                      // in tiles of 256
+    int row, col;                      // in tiles
     __device__ PairTile(const LinearArgs& a, int tile)
     {
-        const int cols = (a.n_tiles + 1) / 2, band = tile / (kBand * cols), rest = tile - band * kBand * cols;
+        const int cols = a.tiles / a.row_tiles, band = tile / (kBand * cols), rest = tile - band * kBand * cols;
         const int tall = min(kBand, a.row_tiles - band * kBand);
         col = rest / tall;
         row = band * kBand + rest % tall;
     }
 };
 
+template <int kCols>
 __global__ void __launch_bounds__(kThreads, 1)
 pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map,
             const __grid_constant__ CUtensorMap y_map)
 {
-    extern __shared__ uint8_t smem_raw[];              // the ring: a tile of x, a tile of weights
+    using P = Pair<kCols>;
+    constexpr int kHalf = P::kHalf, kPairStage = P::kStage, kPairStages = P::kStages;
+    extern __shared__ uint8_t smem_raw[];              // the ring: a tile of x, half a tile of weights; then values on their way out
     __shared__ float s_x[kSlots][kF8Block], s_w[kSlots][2];            // scales
     __shared__ __align__(8) uint64_t s_full[kPairStages], s_empty[kPairStages], s_done[2], s_free[2], s_drain;
     __shared__ uint32_t s_tmem;
@@ -593,26 +618,38 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
     grid_launch_dependents();
 
     if (warp < 4) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFew));
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(P::kFewRegs));
         if (warp == 0) {
             // ======== loads: both CTAs' are counted on the first one's barrier ========
-            grid_dependency_wait();
             int stage = 0, round = 0, issued = 0;
+            auto weights = [&](int col, int kb, int to_stage) {
+                if (elect_one()) {
+                    const uint32_t own = smem_u32(&s_full[to_stage]), bar = mapa_shared(own, first), to = base + to_stage * kPairStage + kTileBytes;
+                    if (side == 0) mbar_arrive_expect_tx(own, 2 * kPairStage);
+                    if constexpr (kCols == 256) {
+                        tma_load_2d_pair(to, &w_map, bar, 0, w_row(a, col, kb, min(static_cast<int>(side), a.n_tiles - 1 - 2 * col)));
+                    } else {                           // 32 weights lie in one packed tile; beyond the last tile they read as zero
+#pragma unroll
+                        for (int i = 0; i < kHalf; i += 32) {
+                            const int o = col * kCols + static_cast<int>(side) * kHalf + i;
+                            tma_load_2d_pair(to + i * kF8Block, &w_map, bar, 0, w_row(a, o / 256, kb, 0) + o % 256);
+                        }
+                    }
+                }
+                __syncwarp();
+            };
+            const int early = min(kPairStages, kbs);
+            for (int i = 0; i < early; ++i) weights(PairTile(a, tile0).col, kb0 + i, i);
+            grid_dependency_wait();
             for (int tile = tile0; ok && tile < a.tiles; tile += step) {
                 const PairTile at(a, tile);
-                const int w_half = min(static_cast<int>(side), a.n_tiles - 1 - 2 * at.col), x_row = (2 * at.row + static_cast<int>(side)) * kF8Block;
-                for (int kb = kb0; kb < kb0 + kbs; ++kb) {
+                const int x_row = (2 * at.row + static_cast<int>(side)) * kF8Block;
+                for (int kb = kb0; kb < kb0 + kbs; ++kb, ++issued) {
                     if (issued >= kPairStages) ok = mbar_wait_warp(smem_u32(&s_empty[stage]), (round & 1) ^ 1, a.wait_budget, ok);
                     if (!ok) break;
-                    if (elect_one()) {
-                        const uint32_t own = smem_u32(&s_full[stage]), to = base + stage * kPairStage;
-                        if (side == 0) mbar_arrive_expect_tx(own, 2 * kPairStage);
-                        const uint32_t bar = mapa_shared(own, first);
-                        tma_load_2d_pair(to, &x_map, bar, kb * kF8Block, x_row);
-                        tma_load_2d_pair(to + kTileBytes, &w_map, bar, 0, w_row(a, at.col, kb, w_half));
-                    }
+                    if (issued >= early) weights(at.col, kb, stage);
+                    if (elect_one()) tma_load_2d_pair(base + stage * kPairStage, &x_map, mapa_shared(smem_u32(&s_full[stage]), first), kb * kF8Block, x_row);
                     __syncwarp();
-                    ++issued;
                     if (++stage == kPairStages) {
                         stage = 0;
                         ++round;
@@ -636,7 +673,7 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
                 if (elect_one()) {
                     const uint64_t x = make_kmajor_desc(base + stage * kPairStage, 128), w = make_kmajor_desc(base + stage * kPairStage + kTileBytes, 128);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) mma_f8_pair(tmem + buffer * 256, x + 2 * k, w + 2 * k, kProduct<256, 256>, k > 0);
+                    for (int k = 0; k < 4; ++k) mma_f8_pair(tmem + buffer * 256, x + 2 * k, w + 2 * k, kProduct<256, kCols>, k > 0);
                     mma_commit_pair(smem_u32(&s_done[buffer]), first);
                     mma_commit_pair(smem_u32(&s_empty[stage]), first);
                 }
@@ -670,7 +707,7 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
                         const int64_t row0 = (2 * static_cast<int64_t>(at.row) + side) * kF8Block + lane;
 #pragma unroll
                         for (int j = 0; j < 4; ++j) from[j] = a.x_scales + min(row0 + 32 * j, a.rows - 1) * a.row_stride + kb0 * a.block_stride;
-                        from[4] = a.w_scales + static_cast<int64_t>(min(2 * at.col + (lane & 1), a.n_tiles - 1)) * a.k_blocks + kb0;
+                        from[4] = a.w_scales + static_cast<int64_t>(min(at.col * kCols / kF8Block + (lane & 1), a.n_tiles - 1)) * a.k_blocks + kb0;
                     }
                     const int slot = block % kSlots;   // of the block eight before, which the sums are through with: the product four before is done
 #pragma unroll
@@ -685,32 +722,47 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
             }
             cp_async_wait<0>();
         }
-        if (a.split > 1) {
+        if (kCols == 256 && a.split > 1) {
             cluster_sync();
             cluster_sync();
         }
     } else {
         // ======== sums ========
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kMany));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(P::kManyRegs));
         const int half = (warp - 4) >> 2, row_lane = (warp & 3) * 32 + lane;
-        const uint32_t from = tmem + (static_cast<uint32_t>(warp & 3) << 21) + half * 128;
+        const uint32_t from = tmem + (static_cast<uint32_t>(warp & 3) << 21) + half * kHalf;
         uint4* const out = reinterpret_cast<uint4*>(smem_raw + (base - smem_u32(smem_raw)) + kPairStages * kPairStage + (warp - 4) * 2 * kOutBytes);
         grid_dependency_wait();
-        Sums sums;
+        Sums<kHalf> sums;
         int block = 0;
-        float s_next = 0.f;                            // the next block's factor: its scales are there with this block's
+        // the next block's factors, of the scales that this thread's weights may meet: they are there with this block's
+        constexpr int kFactors = kCols == 256 ? 1 : 2;
+        float next[kFactors] = {};
+        auto ask = [&](int slot) {
+            const float x = s_x[slot][row_lane];
+            if constexpr (kCols == 256) next[0] = x * s_w[slot][half];
+            else {
+                next[0] = x * s_w[slot][0];
+                next[1] = x * s_w[slot][1];
+            }
+        };
         for (int tile = tile0; ok && tile < a.tiles; tile += step) {
             ok = mbar_wait_warp(smem_u32(&s_done[block & 1]), block >> 1 & 1, a.wait_budget, ok);
             if (!ok) break;
             tc_fence_after();
             sums.begin(from + (block & 1) * 256);
             sums.clear();
+            // which of 32 weights each: the second scale of a tile of 192 begins after 128 of an even tile and 64 of an odd one
+            const int col = PairTile(a, tile).col, second = (kF8Block - col * kCols % kF8Block - half * kHalf) / 32;
+            if (block == 0) ask(0);
 #pragma unroll 1
             for (int kb = 0; kb < kbs; ++kb, ++block) {
-                const float s = block ? s_next : s_x[0][row_lane] * s_w[0][half];
-                s_next = s_x[(block + 1) % kSlots][row_lane] * s_w[(block + 1) % kSlots][half];
+                float s[kFactors];
+#pragma unroll
+                for (int f = 0; f < kFactors; ++f) s[f] = next[f];
+                ask((block + 1) % kSlots);
                 const uint32_t next_done = smem_u32(&s_done[(block + 1) & 1]), next_parity = (block + 1) >> 1 & 1;
-                ok = sums.block(from + (block & 1) * 256, s, kb + 1 < kbs, from + ((block + 1) & 1) * 256,
+                ok = sums.block(from + (block & 1) * 256, [&](int g) { return g < second ? s[0] : s[kFactors - 1]; }, kb + 1 < kbs, from + ((block + 1) & 1) * 256,
                                 [&]() { if (lane == 0) mbar_arrive_remote_relaxed(smem_u32(&s_free[block & 1]), first); },
                                 [&]() { return mbar_try_wait(next_done, next_parity); },
                                 [&](bool answer) { return mbar_wait_warp_polled(answer, next_done, next_parity, a.wait_budget, true); });
@@ -718,14 +770,14 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
             }
             if (!ok) break;
             const PairTile at(a, tile);
-            if (a.split > 1) {
-                keep_sums(sums.acc, base, row_lane, half);     // the ring is free: the cluster's only tile is done
+            if (kCols == 256 && a.split > 1) {
+                if constexpr (kCols == 256) keep_sums(sums.acc, base, row_lane, half);   // the ring is free: the cluster's only tile is done
             } else {
                 const int64_t row = (2 * static_cast<int64_t>(at.row) + side) * kF8Block + row_lane - lane;
-                const int o = (2 * at.col + half) * kF8Block;
+                const int o = at.col * kCols + half * kHalf;
                 if (row >= a.rows || o >= a.n) continue;
                 add_bias(a, o, sums.acc);
-                if (!a.vector || o + kF8Block > a.n) {
+                if (!a.vector || o + kHalf > a.n) {
                     if (lane == 0) tma_store_wait_read();
                     put_y(a, row, o, out, sums.acc);
                 } else if (a.ftype == QTZ_BF16) {
@@ -739,7 +791,7 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
         }
         if (lane == 0) tma_store_wait_all();
         __syncwarp();
-        if (a.split > 1) {
+        if (kCols == 256 && a.split > 1) {
             const PairTile at(a, tile0);
             cluster_sync();                            // the cluster's sums are there
             join_cluster(a, (2 * static_cast<int64_t>(at.row) + side) * kF8Block, at.col, base, part, side, 2);
@@ -762,7 +814,7 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
 qtz_status learn_clusters(qtz_ctx* h)
 {
     if (h->f8_clusters[1]) return QTZ_OK;
-    for (const void* kernel : {reinterpret_cast<const void*>(pair_kernel), reinterpret_cast<const void*>(stream_kernel<16>), reinterpret_cast<const void*>(stream_kernel<32>),
+    for (const void* kernel : {reinterpret_cast<const void*>(pair_kernel<256>), reinterpret_cast<const void*>(pair_kernel<192>), reinterpret_cast<const void*>(stream_kernel<16>), reinterpret_cast<const void*>(stream_kernel<32>),
                                reinterpret_cast<const void*>(stream_kernel<64>), reinterpret_cast<const void*>(stream_kernel<128>)}) {
         cudaFuncAttributes at;
         QTZ_CUDA(h, cudaFuncGetAttributes(&at, kernel));
@@ -827,6 +879,7 @@ int most_split(const qtz_ctx* h, int64_t tiles, int each, int k_blocks)
     return split;
 }
 
+template <int kCols>
 qtz_status launch_pair(qtz_f8_layer* p, LinearArgs& a, const CUtensorMap& x_map, cudaStream_t st)
 {
     const int size = a.ftype == QTZ_F32 ? 4 : 2;
@@ -836,9 +889,10 @@ qtz_status launch_pair(qtz_f8_layer* p, LinearArgs& a, const CUtensorMap& x_map,
     if (a.vector && !qtz_encode_u8_map(&y_map, a.y, 2, dims, strides, box, 64)) a.vector = 0;   // rows too far apart for one
     qtz_ctx* h = p->h;
     a.row_tiles = static_cast<int32_t>((a.rows + 255) / 256);
-    a.tiles = a.row_tiles * ((a.n_tiles + 1) / 2);
+    a.tiles = a.row_tiles * ((a.n + kCols - 1) / kCols);
     const int pairs = h->num_sms / 2;
-    return launch(h, pair_kernel, a, 2 * a.split, 2 * a.split * (a.split > 1 || a.tiles < pairs ? a.tiles : pairs), 1024 + kPairStages * kPairStage + 8 * 2 * kOutBytes, st, p->w_map, x_map, y_map);
+    return launch(h, pair_kernel<kCols>, a, 2 * a.split, 2 * a.split * (a.split > 1 || a.tiles < pairs ? a.tiles : pairs), Pair<kCols>::kSmem, st,
+                  kCols == 256 ? p->w_map : p->w_map_32, x_map, y_map);
 }
 
 }  // namespace
@@ -891,8 +945,9 @@ extern "C" qtz_status qtz_f8_linear_create(qtz_handle h, int32_t n, int32_t k, c
     }
     if (e == cudaSuccess) e = cudaStreamSynchronize(st);   // later calls may fetch the tiles before they wait for the stream
     const uint64_t dims[2] = {kF8Block, places * kF8Block}, strides[1] = {kF8Block};
-    const uint32_t box[2] = {kF8Block, kF8Block};
-    if (e == cudaSuccess && !qtz_encode_u8_map(&p->w_map, p->tiles, 2, dims, strides, box, 128)) e = cudaErrorInvalidValue;
+    const uint32_t box[2] = {kF8Block, kF8Block}, box_32[2] = {kF8Block, 32};
+    if (e == cudaSuccess && !(qtz_encode_u8_map(&p->w_map, p->tiles, 2, dims, strides, box, 128) && qtz_encode_u8_map(&p->w_map_32, p->tiles, 2, dims, strides, box_32, 128)))
+        e = cudaErrorInvalidValue;
     if (e != cudaSuccess) {
         qtz_cuda_fail(h, e, "qtz_f8_linear_create");
         qtz_f8_linear_destroy(p);
@@ -919,10 +974,15 @@ extern "C" qtz_status qtz_f8_linear(qtz_f8_linear_plan p, const uint8_t* codes_d
     // Up to 128 rows single CTAs, whose tiles those are.  More: a tile's block of 128 columns takes a pair 10 and a CTA about 13 units of time,
     // and the longest of either has so many of them (us, CTAs | pairs: 160 x 4096 -> 4096 13.8 | 14.8, 160 x 8192 -> 10240 42 | 33,
     // 800 x 10001 -> 5003 51 | 82, 512 x 4096 -> 6144 23 | 20); CTAs that take several tiles are slower than that (1777 x 4096 -> 4096 63 | 35).
+    // A pair's block of 192 weights takes 9 units, so that such tiles are taken where the pairs are through with them in no more rounds
+    // (us, 256 | 192: 256 x 8192 -> 10240, one round of either, 32.2 | 28.2; 777 x 4096 -> 11008, three rounds or four, 45.5 | 53) and
+    // there are blocks enough to make up for a later start (256 x 4096 -> 11008 18.7 | 17.2, 200 x 1000 -> 12000 8.6 | 9.0).
     const int64_t cols = (p->n_tiles + 1) / 2, pair_tiles = (rows + 255) / 256 * cols, tiles = (rows + 127) / 128 * cols, pairs = h->num_sms / 2;
     const int pair_split = most_split(h, pair_tiles, 2, p->k_blocks), split = most_split(h, tiles, 1, p->k_blocks);
-    const int64_t pair_blocks = (pair_tiles + pairs - 1) / pairs * ((p->k_blocks + pair_split - 1) / pair_split), blocks = (p->k_blocks + split - 1) / split;
-    const bool pair = rows > 128 && (tiles > h->num_sms || 10 * pair_blocks < 13 * blocks);
+    const int64_t rounds = (pair_tiles + pairs - 1) / pairs, narrow_tiles = (rows + 255) / 256 * ((p->n + 191) / 192);
+    const bool narrow = pair_split == 1 && p->k_blocks >= 16 && (narrow_tiles + pairs - 1) / pairs == rounds;
+    const int64_t pair_blocks = rounds * ((p->k_blocks + pair_split - 1) / pair_split), blocks = (p->k_blocks + split - 1) / split;
+    const bool pair = rows > 128 && (tiles > h->num_sms || (narrow ? 9 : 10) * pair_blocks < 13 * blocks);
     a.split = pair ? pair_split : split;
     const int box_rows = pair ? 128 : rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
     CUtensorMap x_map;                                 // columns beyond k and rows beyond the last read as zero
@@ -930,7 +990,7 @@ extern "C" qtz_status qtz_f8_linear(qtz_f8_linear_plan p, const uint8_t* codes_d
     const uint64_t dims[2] = {static_cast<uint64_t>(p->k), static_cast<uint64_t>(rows)}, strides[1] = {static_cast<uint64_t>(pitch)};
     const uint32_t box[2] = {kF8Block, static_cast<uint32_t>(box_rows)};
     if (!qtz_encode_u8_map(&x_map, codes_dev, 2, dims, strides, box, 128)) return qtz_cuda_fail(h, cudaErrorInvalidValue, "tensor map of the activations");
-    if (pair) return launch_pair(p, a, x_map, st);
+    if (pair) return narrow ? launch_pair<192>(p, a, x_map, st) : launch_pair<256>(p, a, x_map, st);
     switch (box_rows) {
     case 16: return launch_stream<16>(p, a, x_map, st);
     case 32: return launch_stream<32>(p, a, x_map, st);
