@@ -185,18 +185,36 @@ __device__ __forceinline__ void put_y(const LinearArgs& a, int64_t row, int o, u
     else put_rows(static_cast<float*>(a.y) + at, a.y_stride, rows, cols, a.vector, out, acc);
 }
 
+// Rows leave by copies in `steps` steps each time, which fill two places in turn, the first one at the start.  How many of the last copies
+// may still be reading when a step fills its place: the last but one had it before, or, at the start behind an odd number of steps,
+// the last one.
+__host__ __device__ constexpr int still_reading(int steps, int step) { return step == 0 && steps % 2 == 1 ? 0 : 1; }
+
+// Whether no step, of two times in a row, fills a place that a copy may be reading.
+__host__ __device__ constexpr bool places_are_free(int steps)
+{
+    for (int i = 0; i < 2 * steps; ++i)
+        for (int j = i - 1; j >= 0 && j >= i - still_reading(steps, i % steps); --j)
+            if (j % steps % 2 == i % steps % 2) return false;
+    return true;
+}
+
 // 32 rows of kCols columns where rows of y start on 16 bytes, by copies that run on behind the caller: 64 bytes of each row at a time in the
 // order of a 64-byte swizzle, in two places of `out` in turn.  Rows beyond the last the tensor map leaves out; of columns it would write whole
 // pieces of 16 bytes.
 template <typename T, int kCols>
 __device__ __forceinline__ void send_rows(const CUtensorMap& y_map, int64_t row, int o, uint32_t out, const float (&acc)[kCols])
 {
-    constexpr int kPer = 16 / sizeof(T), kStep = 64 / sizeof(T);
+    constexpr int kPer = 16 / sizeof(T), kStep = 64 / sizeof(T), kSteps = kCols / kStep;
+    static_assert(places_are_free(kSteps), "");
     const int lane = threadIdx.x & 31;
 #pragma unroll
     for (int c0 = 0; c0 < kCols; c0 += kStep) {
         const uint32_t to = out + c0 / kStep % 2 * kOutBytes;
-        if (lane == 0) tma_store_wait_read_n<1>();
+        if (lane == 0) {
+            if (still_reading(kSteps, c0 / kStep) == 0) tma_store_wait_read();
+            else tma_store_wait_read_n<1>();
+        }
         __syncwarp();
 #pragma unroll
         for (int q = 0; q < 4; ++q) sts128(to + lane * 64 + (q ^ (lane >> 1 & 3)) * 16, pack16<T>(acc + c0 + q * kPer));

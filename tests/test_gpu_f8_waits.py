@@ -11,8 +11,9 @@ from paper_1806_08342_b200 import qtz
 pytestmark = pytest.mark.gpu
 
 LEAST, USUAL = 1000, 2_000_000_000
-CASES = [  # rows, n, k: single CTAs whose columns are shared (three) or not, pairs that share columns, pairs with a tile or several
-    (1, 4096, 8192), (30, 5000, 2048), (200, 2000, 8192), (128, 40000, 2048), (1000, 1000, 8192), (1000, 4096, 4096), (2500, 9000, 4000)]
+CASES = [  # rows, n, k: single CTAs whose columns are shared (three) or not, pairs that share columns, pairs with a tile or several, of either width
+    (1, 4096, 8192), (30, 5000, 2048), (200, 2000, 8192), (128, 40000, 2048), (1000, 1000, 8192), (1000, 4096, 4096), (2500, 9000, 4000),
+    (777, 6144, 4096)]
 
 
 def layer(h, rows, n, k, seed):
@@ -60,3 +61,20 @@ def test_calls_straight_behind_one_whose_waits_run_out(case):
     assert ran_out > 0 or rows < 100                                     # few rows' scales may arrive within the polls that a wait always makes
     h.close()
     other.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows,n,k", [(777, 6144, 4096), (777, 6144, 2048), (1500, 4608, 2100)])
+def test_rows_on_their_way_are_not_overtaken_by_the_next_tile(rows, n, k, dtype):
+    """Pairs with several tiles of 192 columns: 96 columns of 16 bits leave in three steps through two places.  The sums are those of the
+    call in 32 bits, while the memory is busy with copies."""
+    h = qtz.Handle(0)
+    plan, codes, scales = layer(h, rows, n, k, 3)
+    want = plan(codes, scales, dtype=torch.float32).to(dtype)
+    busy, side = torch.empty(2, 128 << 20, device="cuda"), torch.cuda.Stream()
+    for _ in range(10):
+        with torch.cuda.stream(side):
+            busy[0].copy_(busy[1])
+        assert torch.equal(plan(codes, scales, dtype=dtype), want)
+    assert h.device_status() == (0, 0)
+    h.close()
