@@ -112,6 +112,14 @@ class Block:
         return ff(self.attention(values, starts, lens, slots, table), x if residual is None else total)
 
 
+def run_blocks(blocks, x, starts, lens, slots, table):
+    """Hidden states behind `blocks` of x [tokens][hidden]: the residual stream with what the last block adds to it."""
+    residual = None
+    for block in blocks:
+        x, residual = block(x, residual, starts, lens, slots, table)
+    return x if residual is None else x + residual
+
+
 def main(argv=None) -> dict:
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     for name, value in (("requests", 16), ("prompt", 500), ("steps", 64), ("layers", 4), ("hidden", 2048), ("q-heads", 16),
@@ -138,12 +146,10 @@ def main(argv=None) -> dict:
 
     def step(x, added):
         plan = requests.admit(added, x.shape[0])
-        residual = None
+        if o.ffn:
+            return run_blocks(layers, x, *plan, requests.table)
         for layer in layers:
-            if o.ffn:
-                x, residual = layer(x, residual, *plan, requests.table)
-            else:
-                x = layer(x, *plan, requests.table)
+            x = layer(x, *plan, requests.table)
         return x
 
     lengths = [max(1, o.prompt * (r + 1) // o.requests) for r in range(o.requests)]      # ragged prompts
