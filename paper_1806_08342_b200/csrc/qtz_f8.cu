@@ -206,19 +206,21 @@ __global__ void __launch_bounds__(kChunks == 1 ? kNormThreads : kWideThreads) no
                 sum.store(static_cast<T*>(a.sum) + row * a.sum_stride + col, a.k - col);
             }
         }
-        float squares, eps = a.eps;
+        float mean, eps = a.eps;                       // of the squares, with eps
 #pragma unroll 1
-        for (;;) {
-            squares = sum_of_squares(h, s_part[turn]);
+        for (int again = 3;; --again) {
+            mean = sum_of_squares(h, s_part[turn]) / static_cast<float>(a.k) + eps;
             turn ^= 1;
-            if (squares != INFINITY || eps == 0.f) break;
-            eps = 0.f;                                 // too large to be squared in fp32 (eps is nothing beside it), or infinite
+            if (mean != INFINITY || again == 0) break;
+            // Too large to be squared in fp32, or infinite: 2^-24 of it, three times at most, since 32768 squares of less than 2^56 are finite.
+            // The largest, or the root of eps, is above 2^32 then, so that what falls below fp32 here would do so in v as well.
+            eps *= 3.5527136788005009e-15f;            // 2^-48
 #pragma unroll
             for (int j = 0; j < kChunks; ++j)
 #pragma unroll
-                for (int i = 0; i < kCols; ++i) h[j][i] *= kF8MinScale;
+                for (int i = 0; i < kCols; ++i) h[j][i] *= 5.9604644775390625e-8f;
         }
-        const float factor = 1.f / sqrtf(squares / static_cast<float>(a.k) + eps);
+        const float factor = 1.f / sqrtf(mean);
 #pragma unroll
         for (int j = 0; j < kChunks; ++j) {
             const int col = (j * blockDim.x + threadIdx.x) * kCols, valid = a.k - col;
