@@ -576,6 +576,12 @@ struct Pair {
     static constexpr int kHalf = kCols / 2, kStage = kTileBytes + kHalf * kF8Block;
     static constexpr int kStages = kCols == 256 ? 5 : 6;              // what the rows on their way to y leave room for
     static constexpr int kSmem = 1024 + kStages * kStage + 8 * 2 * kOutBytes;
+    // Blocks that scales are asked for ahead, in a place whose factors have been used when the arrivals were made that the wait before rests
+    // on: those arrivals say that tensor memory has been read, and are no order for reads of shared memory.  128 columns use a block's factors
+    // before they give its buffer back, 96 behind that.
+    static constexpr int kScalesAhead = kCols == 256 ? kAhead : kAhead - 1;
+    // The wait is for the product two blocks before the one whose scales have landed, and that began when the block two before it was read.
+    static_assert(kScalesAhead + 4 + (kCols == 256 ? 0 : 1) <= kSlots, "");
     // registers of a thread; those of 96 columns are all read at once
     static constexpr int kFewRegs = kCols == 256 ? kFew : 56, kManyRegs = kCols == 256 ? kMany : 224;
     static_assert(4 * 32 * kFewRegs + 8 * 32 * kManyRegs <= kThreads * kLaunchRegs, "more registers than the CTA was launched with");
@@ -729,15 +735,15 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
             if (side == 0 && elect_one()) mma_commit_pair(smem_u32(&s_drain), first);
             __syncwarp();
         } else if (warp == 2) {
-            // ======== scales: on their way four blocks ahead, counted with the products of the block ========
+            // ======== scales: on their way three or four blocks ahead, counted with the products of the block ========
             grid_dependency_wait();
             const int blocks = (a.tiles - 1 - tile0) / step * kbs + kbs;
             int tile = tile0, kb = 0;
             const float* from[5];                      // four rows of x; lanes 0 and 1: a tile of weights
-            for (int block = 0; block < blocks + kAhead; ++block) {
-                const int now = block - kAhead;
+            for (int block = 0; block < blocks + P::kScalesAhead; ++block) {
+                const int now = block - P::kScalesAhead;
                 if (now >= 0) {
-                    cp_async_wait<kAhead - 2>();
+                    cp_async_wait<P::kScalesAhead - 2>();
                     __syncwarp();
                     if (now >= 2) ok = mbar_wait_warp(smem_u32(&s_done[now & 1]), (now >> 1 & 1) ^ 1, a.wait_budget, ok);
                     if (!ok) break;
@@ -751,7 +757,7 @@ pair_kernel(const __grid_constant__ LinearArgs a, const __grid_constant__ CUtens
                         for (int j = 0; j < 4; ++j) from[j] = a.x_scales + min(row0 + 32 * j, a.rows - 1) * a.row_stride + kb0 * a.block_stride;
                         from[4] = a.w_scales + static_cast<int64_t>(min(at.col * kCols / kF8Block + (lane & 1), a.n_tiles - 1)) * a.k_blocks + kb0;
                     }
-                    const int slot = block % kSlots;   // of the block eight before, which the sums are through with: the product four before is done
+                    const int slot = block % kSlots;   // of the block eight before, whose factors have been used
 #pragma unroll
                     for (int j = 0; j < 4; ++j) cp_async_4(smem_u32(&s_x[slot][32 * j + lane]), from[j] + kb * a.block_stride);
                     if (lane < 2) cp_async_4(smem_u32(&s_w[slot][lane]), from[4] + kb);

@@ -241,7 +241,8 @@ __device__ __forceinline__ void mbar_arrive_remote(uint32_t bar, uint32_t rank)
 }
 
 // The same without ordering what this thread wrote before: for arrivals that only say that tensor memory has been read (the loads are
-// complete by then).  The release form waits for the thread's memory operations, about 1000 cycles a time.
+// complete by then), or that a value read of shared memory has been used.  The release form waits for the thread's memory operations,
+// about 1000 cycles a time.
 __device__ __forceinline__ void mbar_arrive_remote_relaxed(uint32_t bar, uint32_t rank)
 {
     asm volatile(
