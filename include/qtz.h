@@ -508,6 +508,7 @@ QTZ_API qtz_status qtz_linear_w4(qtz_linear_plan p, const void* x_dev, int64_t x
  * 2.2's symmetric quantizer with a floating-point code in the integer's place, at a finer granularity than Section 2.6's channels.  The
  * last blocks of a row or a column may be short.  For a block whose largest finite magnitude is m:
  *   s = max(m / 448, 2^-100),  code = e4m3(v * (1 / s)) with fp32 steps, rounded to nearest even.
+ * It is the product that is rounded: where v / s lies half way between two codes, or next to that, the code may be either neighbour.
  * Infinities saturate and do not count in m; NaN becomes the code NaN.
  *
  * qtz_f8_rmsnorm: root-mean-square norm of rows of k values with the residual's addition before it,
@@ -516,7 +517,7 @@ QTZ_API qtz_status qtz_linear_w4(qtz_linear_plan p, const void* x_dev, int64_t x
  * infinity gives NaN there and zeros elsewhere, as the formula does; one that holds NaN gives NaN.
  *   x, residual, gain, sum, values   of type `ftype` (QTZ_F32, QTZ_F16, QTZ_BF16); residual, sum and values may be NULL
  *   codes, scales                    NULL (then values is not), or [rows][k] and [rows][ceil(k / 128)]
- *   eps                              at least 1e-30
+ *   eps                              finite, at least 1e-30
  * Strides are in elements; bases and rows start on 16 bytes (the stride of a single row does not matter; scales have no alignment
  * rule), and a row's values lie next to each other.  sum and values may be x or residual themselves; otherwise nothing overlaps.
  * Bytes past k in a row are neither read nor written.  At most 32768 columns (QTZ_ERR_TOO_LARGE).  Asynchronous on `stream`; rows == 0
@@ -531,7 +532,7 @@ QTZ_API qtz_status qtz_f8_quantize(qtz_handle h, const void* x_dev, int64_t x_st
                                    int32_t k, int32_t ftype, uint8_t* codes_dev, int64_t codes_stride, float* scales_dev, int64_t scales_stride,
                                    void* stream);
 /* Weights w [n][k] (any `ftype`, rows w_stride elements apart, no alignment rule): codes [n][k] dense, scales
- * [ceil(n / 128)][ceil(k / 128)].  Asynchronous on `stream`.                                                         */
+ * [ceil(n / 128)][ceil(k / 128)].  QTZ_ERR_TOO_LARGE beyond 65535 blocks either way.  Asynchronous on `stream`.       */
 QTZ_API qtz_status qtz_f8_quantize_weights(qtz_handle h, const void* w_dev, int64_t w_stride, int32_t n, int32_t k, int32_t ftype,
                                            uint8_t* codes_dev, float* scales_dev, void* stream);
 
@@ -539,11 +540,13 @@ QTZ_API qtz_status qtz_f8_quantize_weights(qtz_handle h, const void* w_dev, int6
  * Products of codes are exact, their sum over a block of 128 columns and the sum over blocks are held in fp32 (of 32 columns that are
  * summed together, what lies 2^-25 below the largest product is cut off), and y is rounded once.  Results are the same whenever
  * repeated; a row's do not depend on the other rows, but may differ in the last places with the number of rows in the call.
- * A NaN code gives NaN in its row (of x) or column (of w).  Scales are finite, and so are the products of two that meet.
+ * A NaN code gives NaN in its row (of x) or column (of w).  Scales are finite, and so are the products of two that meet; a product
+ * below 2^-126 has the bits that fp32 leaves it, none below 2^-150.
  *
  * One-time preparation: copies codes (rows codes_stride bytes apart, no alignment rule), scales and bias (n values of type
  * bias_ftype, or NULL) into the order the kernels read.  BLOCKS until `stream` has finished; the caller may then free or overwrite
- * all inputs.                                                                                                     */
+ * all inputs (until then the device holds the weights twice).  QTZ_ERR_TOO_LARGE beyond 65535 blocks of rows or 2^23 blocks of
+ * 128 x 128 in all.                                                                                               */
 QTZ_API qtz_status qtz_f8_linear_create(qtz_handle h, int32_t n, int32_t k, const uint8_t* codes_dev, int64_t codes_stride, const float* scales_dev,
                                         const void* bias_dev, int32_t bias_ftype, qtz_f8_linear_plan* out, void* stream);
 QTZ_API qtz_status qtz_f8_linear_destroy(qtz_f8_linear_plan p);
