@@ -8,9 +8,11 @@
 // What bounds them: bytes.  Every value is read once, kept in registers between the row's sum of squares, the block's maximum and the
 // code, and written once.  A thread holds 32 bytes of neighbouring columns, so that 8 or 16 lanes hold a block and its maximum takes three or
 // four shuffles; warps and CTAs go over several rows and have the next row's values on their way while they work on one.
-// Measured: norm of 16384 rows of 8192 with residual, bf16, 144 us, 6.5 TB/s, the copy rate (with nothing on its way behind the row at work
-// 248); gated quantizer 8192 x 28672 180 us, 6.5 TB/s (with 32 instructions a value instead of about 16 409), plain 111; 8192 x 10001
-// gated 72 us, 5.7 TB/s; one row of 2048 1.9 us.
+// Measured, device time of ten calls in a CUDA graph, inputs in turn: norm of 16384 rows of 8192 with residual, bf16, 148 us, 6.4 TB/s, the
+// copy rate (with nothing on its way behind the row at work 248); gated quantizer 8192 x 28672 180 us, 6.6 TB/s (with 32 instructions a
+// value instead of about 16 409), plain 111; 8192 x 10001 gated 71 us, 5.8 TB/s; one row of 2048 2.2 us.  Rows that take a thread more than
+// 32 bytes (above 16384 columns of 16 bits, 8192 of fp32) have nothing on its way: 4096 x 32768 bf16 217 to 290 us where its bytes take
+// 146, 4096 x 12288 fp32 142 to 149 where they take 102, both with residual.
 #include "qtz_f8.cuh"
 #include "qtz_ptx.cuh"
 

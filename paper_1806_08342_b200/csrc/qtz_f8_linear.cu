@@ -18,9 +18,12 @@
 // left: halves of 128 columns with four buffers (the same), single CTAs of 128 x 256 (1090 cycles: shared memory brings and reads 192
 // bytes a clock), tiles dealt out block by block with parts in global memory (128 KB a part: 33 -> 55 us for 256 x 8192 -> 10240),
 // a launch of clusters for the tiles beyond whole rounds (a launch and a join cost 10 us: 777 rows through 11008 x 4096 49.8 -> 53.0).
-// Measured, device time: 8192 rows through 28672 x 8192 1.53 ms, 2.5 PFLOP/s, under the power cap (1.8 ms in a long run); 1777 rows
-// through 6144 x 4096 46.6 us (three rounds of 74 pairs for 2.3 of tiles); 256 rows through 10240 x 8192 28 us (54 tiles of 192
-// weights for 74 pairs); 45 rows through 5003 x 10001 12.1 us; one row through 28672 x 8192 36.8 us, 6.4 TB/s; one row through 1000 x 1024 4.1 us.
+// Measured (the figures above: when the step they name was taken), device time of ten calls in a CUDA graph, layers in turn that
+// do not fit the L2 together, bf16 y but as said: 8192 rows through 28672 x 8192 1.6 ms, 2.4 PFLOP/s,
+// in the first calls and 1.8 ms under the power cap; 1777 rows through 6144 x 4096 47 us (three rounds of 74 pairs for 2.3 of tiles); 256
+// rows through 10240 x 8192 28.6 us (54 tiles of 192 weights for 74 pairs); 45 rows through 5003 x 10001, fp16 with bias, 14.6 us (12.4
+// with the weights in the L2); one row through 28672 x 8192 38 us, 6.2 TB/s; one row through 1000 x 1024, fp16 with bias, 4.4 us.  Rows of y
+// that do not start on 16 bytes leave value by value: 2048 rows through 5003 x 4096 65 us, through 5008 x 4096 43.
 #include <new>
 
 #include "qtz_f8.cuh"
